@@ -339,7 +339,7 @@ int abs_profile_timeline(abs_ctx *ctx, abs_span *out, size_t capacity, size_t *n
 uint64_t abs_launch_count(abs_ctx *ctx);
 
 /* Text of the last error on this context (never NULL; "" if none).  ctx may be NULL: then
- * the text of the last failed abs_init on this thread. */
+ * the text of the last failed abs_init, or refused call of abs_llm.h, on this thread. */
 const char *abs_last_error(abs_ctx *ctx);
 
 /* Waits for the context's enqueued work, releases events and host state.  The workspace

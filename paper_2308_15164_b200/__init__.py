@@ -1,17 +1,19 @@
 """Delayed synchronous step of ABS-SGD (arXiv 2308.15164, Algorithm 1) on one B200.
 
-The package holds three things:
+The package holds:
 
 * ``csrc/``      -- the sm_100a CUDA kernels and the C-ABI library built from them
-                   (entry points declared in ``include/abs_sgd.h``),
+                   (entry points declared in ``include/abs_sgd.h`` and ``include/abs_llm.h``),
 * ``binding``    -- a ctypes binding with the same names (argument marshalling only),
+* ``llm``        -- the operators of ``abs_llm.h`` on tensors (losses on logits, the residual join of a
+                   transformer block, 8-bit activation checkpoints),
 * ``workloads``  -- seeded synthetic input generators (no optimiser arithmetic).
 
 Nothing here falls back to a CPU implementation: importing ``binding`` raises if the
 shared library has not been built.
 """
 
-__all__ = ["binding", "workloads", "build", "dist"]
+__all__ = ["binding", "llm", "workloads", "build", "dist"]
 
 
 def __getattr__(name):

@@ -1,4 +1,4 @@
-"""ctypes binding of the C ABI declared in include/abs_sgd.h.
+"""ctypes binding of the C ABI declared in include/abs_sgd.h (and the signatures of include/abs_llm.h; see llm.py).
 
 Argument marshalling only: every step of the delayed synchronous step runs in the CUDA
 kernels of libabs_sgd.so.  PyTorch is used for device memory and stream handles.  There is
@@ -53,7 +53,7 @@ class AbsPeerTable(ctypes.Structure):
     _fields_ = [("n_ranks", ctypes.c_uint32), ("rank", ctypes.c_uint32), ("workspace_dev", ctypes.c_void_p * MAX_RANKS)]
 
 
-_vp, _u32, _u64 = ctypes.c_void_p, ctypes.c_uint32, ctypes.c_uint64
+_vp, _u32, _u64, _f32 = ctypes.c_void_p, ctypes.c_uint32, ctypes.c_uint64, ctypes.c_float
 _sig = {
     "abs_workspace_bytes": (ctypes.c_size_t, [ctypes.POINTER(AbsConfig)]),
     "abs_init": (ctypes.c_int, [ctypes.POINTER(_vp), ctypes.POINTER(AbsConfig), _vp, ctypes.c_size_t, _vp]),
@@ -98,6 +98,20 @@ _sig = {
     "abs_state_import": (ctypes.c_int, [_vp, _vp, ctypes.c_size_t]),
     "abs_sync_step_noalloc": (ctypes.c_int, [_vp, _vp, _vp, _u64, _u64, _u32, _vp, ctypes.c_float, ctypes.c_float,
                                              ctypes.c_float, _vp]),
+    # abs_llm.h
+    "abs_policy_loss_workspace": (ctypes.c_size_t, []),
+    "abs_policy_loss": (ctypes.c_int, [_vp, _u32, _u64, _u64, _u64] + [_vp] * 5 + [_f32] * 3 + [_vp, _vp, _vp, _u64, _vp, ctypes.c_size_t, _vp]),
+    "abs_preference_loss_workspace": (ctypes.c_size_t, [_u64]),
+    "abs_preference_loss": (ctypes.c_int, [_vp, _u32, _u64, _u64, _u64, _vp, _vp, _u64, _vp] + [_f32] * 3 + [_vp] * 4 + [_u64, _vp, ctypes.c_size_t, _vp]),
+    "abs_residual_norm": (ctypes.c_int, [_vp, _u64] * 3 + [_u32, _vp, _vp, _f32, _f32, _u32, _u64, _u64, _vp, _u64, _vp, _u64, _vp]),
+    "abs_residual_norm_workspace": (ctypes.c_size_t, [_u64, _u64]),
+    "abs_residual_norm_backward": (ctypes.c_int, [_vp, _u64] * 5 + [_u32, _vp, _vp, _f32, _f32, _u32, _u64, _u64] + [_vp, _u64] * 3
+                                   + [_vp, _vp, ctypes.c_int, _vp, ctypes.c_size_t, _vp]),
+    "abs_ckpt8_quantize": (ctypes.c_int, [_vp, _u64, _u32, _u64, _u64, _vp, _vp, _vp]),
+    "abs_ckpt8_dequantize": (ctypes.c_int, [_vp, _vp, _u64, _u64, _vp, _u64, _u32, _vp]),
+    "abs_ckpt8_wgrad_workspace": (ctypes.c_size_t, [_u64, _u64, _u64, _vp, _u64]),
+    "abs_ckpt8_wgrad": (ctypes.c_int, [_vp, _vp, _vp, _u64, _u64, _u64, _u64, _vp, _u64, ctypes.c_int, _vp, ctypes.c_size_t, _vp]),
+    "abs_llm_check": (ctypes.c_int, [_vp]),
 }
 for _name, (_res, _args) in _sig.items():
     _fn = getattr(lib, _name)

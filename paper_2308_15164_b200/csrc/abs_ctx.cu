@@ -690,6 +690,16 @@ int coalesce_one(abs_ctx* c, uint32_t worker, const void* x_dev, const int32_t* 
 
 }  // namespace
 
+namespace abs_sgd {
+int thread_error(int code, const char* text) {
+    try {
+        g_init_error = text;
+    } catch (...) {      // out of host memory: the code alone has to do
+    }
+    return code;
+}
+}  // namespace abs_sgd
+
 extern "C" {
 
 size_t abs_workspace_bytes(const abs_config* cfg) {

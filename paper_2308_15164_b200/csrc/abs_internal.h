@@ -43,6 +43,9 @@ inline cudaError_t launch_kernel(void (*kernel)(KArgs...), dim3 grid, dim3 block
     return cudaLaunchKernelEx(&cfg, kernel, static_cast<Args&&>(args)...);
 }
 
+// Sets the text that abs_last_error(NULL) returns on this thread (calls without a context) and returns `code`.
+int thread_error(int code, const char* text);
+
 // ---- Step 2: acc_row[j] += g[j], cnt[0] += 1 (Algorithm 1, Step 2) ------------------------
 // grad_dtype: ABS_GRAD_F32 / ABS_GRAD_BF16.  P = number of valid elements in g.
 // overwrite: acc_row[j] = g[j] instead (first micro-batch of a worker when the row is not kept zeroed).

@@ -1,0 +1,503 @@
+// Activations held in 8 bits between the forward and the backward pass (abs_ckpt8_*).
+//
+// A block of 32 consecutive values of a row: int8 q and one power of two, value = q 2^(e - 127), the smallest e with
+// amax <= 127 2^(e - 127).  int8 and not an 8-bit float: inside a block of 32 an activation's values are within a few
+// octaves of its largest, where 7 bits of magnitude below the block's maximum are 3 to 4 times as fine (rms) as a
+// 3-bit mantissa.  A power of two and not amax / 127: q 2^k is exactly a bf16 number (7 significant bits), so that the
+// weight gradient feeds it to the bf16 tensor cores without a rounding of its own.
+#include <algorithm>
+
+#include "abs_internal.h"
+#include "abs_llm.h"
+#include "row_ops.cuh"
+#include "tcgen05.cuh"
+
+namespace abs_sgd {
+namespace {
+
+__device__ int g_status;     // ABS_ETIMEOUT once a bounded wait of k_wgrad has run out; read and cleared by abs_llm_check
+
+// Exponent byte of a block from the bits of its largest magnitude (a NaN's bits are above infinity's).
+__device__ __forceinline__ uint32_t block_exponent(uint32_t amax_bits) {
+    const uint32_t field = amax_bits >> 23;
+    if (field == 255u) return 255u;
+    // amax = 1.f 2^(field - 127) <= 127 2^k = 1.984375 2^(6 + k)
+    const int e = (int)field - 6 + ((amax_bits & 0x7FFFFFu) > 0x7E0000u ? 1 : 0);
+    return e < 0 ? 0u : (uint32_t)e;
+}
+// 2^(e - 127) and its reciprocal; e = 255: NaN.
+__device__ __forceinline__ float pow2_of(uint32_t e) {
+    return __uint_as_float(e == 0u ? 0x00400000u : e == 255u ? 0x7FC00000u : e << 23);
+}
+__device__ __forceinline__ float inv_pow2_of(uint32_t e) { return __uint_as_float((254u - e) << 23); }   // e <= 249
+
+// Eight consecutive values per thread, so that four neighbouring lanes hold a block.  kWide: the row allows 16-byte loads.
+template <typename T, bool kWide>
+__global__ void __launch_bounds__(256) k_ckpt8_quantize(const T* x, size_t ld, size_t n8, uint32_t per_row, int D, uint2* q, uint8_t* e) {
+    pdl_wait();
+    pdl_trigger();
+    for (size_t i0 = (size_t)blockIdx.x * 256; i0 < n8; i0 += (size_t)gridDim.x * 256) {
+        const size_t i = i0 + threadIdx.x;           // n8 is a multiple of 4: a block's lanes are all in or all out
+        const size_t t = i / per_row;
+        const int c = (int)(i - t * per_row) * 8;
+        float v[8];
+        if (i < n8) {
+            const T* p = x + t * ld + c;
+            if (kWide && c + 8 <= D) {
+                constexpr int kN = kVec<T>;
+#pragma unroll
+                for (int k = 0; k < 8 / kN; ++k) Pack<T, kN>::load(p + k * kN, *reinterpret_cast<float(*)[kN]>(v + k * kN));
+            } else {
+#pragma unroll
+                for (int k = 0; k < 8; ++k) v[k] = c + k < D ? to_f(p[k]) : 0.f;
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] = 0.f;
+        }
+        uint32_t m = 0;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) m = max(m, __float_as_uint(v[k]) & 0x7FFFFFFFu);
+        m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
+        m = max(m, __shfl_xor_sync(0xffffffffu, m, 2));
+        const uint32_t code = block_exponent(m);
+        const float inv = code == 255u ? 0.f : inv_pow2_of(code);
+        uint32_t w[2] = {0u, 0u};
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const int b = code == 255u ? 0 : __float2int_rn(v[k] * inv);
+            w[k / 4] |= ((uint32_t)b & 0xFFu) << (8 * (k % 4));
+        }
+        if (i < n8) {
+            q[i] = make_uint2(w[0], w[1]);
+            if (i % 4 == 0) e[i / 4] = (uint8_t)code;
+        }
+    }
+}
+
+template <typename T, bool kWide>
+__global__ void __launch_bounds__(256) k_ckpt8_dequantize(const uint2* q, const uint8_t* e, T* x, size_t ld, size_t n8, uint32_t per_row, int D) {
+    pdl_wait();
+    pdl_trigger();
+    for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < n8; i += (size_t)gridDim.x * 256) {
+        const size_t t = i / per_row;
+        const int c = (int)(i - t * per_row) * 8;
+        if (c >= D) continue;
+        const uint2 w = q[i];
+        const float s = pow2_of(e[i / 4]);
+        float v[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = (float)(int)(int8_t)((k < 4 ? w.x : w.y) >> (8 * (k % 4))) * s;
+        T* p = x + t * ld + c;
+        if (kWide && c + 8 <= D) {
+            constexpr int kN = kVec<T>;
+#pragma unroll
+            for (int k = 0; k < 8 / kN; ++k) Pack<T, kN>::store(p + k * kN, *reinterpret_cast<const float(*)[kN]>(v + k * kN));
+        } else {
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                if (c + k < D) p[k] = from_f<T>(v[k]);
+        }
+    }
+}
+
+// ------------------------------------------------------------------------------------------------
+// dw[i, o] = sum_t x^[t, i] dy[t, o].  Both operands lie with the contraction index t along the rows, i.e. "MN-major": a
+// TMA box of 64 columns x 64 tokens is 64 swizzled 128-byte rows, one per token.
+//   warp 0      TMA producer: per 64 tokens the 128 columns of q (8 KB) and the 256 columns of dy (four boxes, 32 KB)
+//   warp 1      MMA issuer: four tcgen05.mma (M 128, N 256, K 16) per 64 tokens into one of two TMEM accumulators
+//   warps 2-5   epilogue: TMEM -> registers -> dw (or a partial sum), coalesced through a padded staging tile
+//   warps 6-13  q -> bf16 operand tile: thread = (token, block of 32), the two 16-byte pieces of q become four of bf16
+// A work item is an output tile and a run of tokens; items are dealt out round-robin.
+// ------------------------------------------------------------------------------------------------
+constexpr int kTM = 128, kTN = 256, kTK = 64;
+constexpr int kStages = 3;
+constexpr int kRawBytes = kTK * kTM, kABytes = kTK * kTM * 2, kBBytes = kTK * kTN * 2;
+constexpr int kWgThreads = 448;
+constexpr int kPitch = 33;
+
+struct WgSmem {
+    alignas(1024) uint8_t raw[kStages][kRawBytes];
+    alignas(1024) uint8_t a[kStages][kABytes];
+    alignas(1024) uint8_t b[kStages][kBBytes];
+    float out[4][32 * kPitch];
+    alignas(8) uint64_t full[kStages];
+    uint64_t ready[kStages];
+    uint64_t empty[kStages];
+    uint64_t acc_full[2];
+    uint64_t acc_empty[2];
+    uint32_t tmem_base;
+    uint32_t failed;
+};
+
+struct WgArgs {
+    const uint8_t* e;
+    size_t e_ld;             // W / 32
+    int T, D, N;
+    int tiles_n, tiles, splits, kb_per_split;   // kb: runs of 64 tokens
+    float* out;              // dw, or the partial sums [splits][D][ld] when splits > 1
+    size_t ld, split_stride;
+    int accumulate;
+};
+
+__global__ void __launch_bounds__(kWgThreads, 1) k_wgrad(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_dy,
+                                                         const __grid_constant__ WgArgs a) {
+    extern __shared__ uint8_t smem_raw[];
+    WgSmem& s = *reinterpret_cast<WgSmem*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const int items = a.tiles * a.splits;
+    const int kb_total = (a.T + kTK - 1) / kTK;
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&s.tmem_base)), "r"(512) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < kStages; ++i) {
+            mbar_init(&s.full[i], 1);
+            mbar_init(&s.ready[i], 256);
+            mbar_init(&s.empty[i], 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&s.acc_full[i], 1);
+            mbar_init(&s.acc_empty[i], 128);
+        }
+        s.failed = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    const uint32_t tmem = s.tmem_base;
+    volatile uint32_t* failed = &s.failed;
+    pdl_wait();
+    pdl_trigger();
+
+    // item -> its first output row and column, and its runs of tokens [kb0, kb1)
+    auto item_of = [&](int it, int* m0, int* n0, int* kb0, int* kb1) {
+        const int tile = it % a.tiles, sp = it / a.tiles;
+        *m0 = (tile / a.tiles_n) * kTM;
+        *n0 = (tile % a.tiles_n) * kTN;
+        *kb0 = min(kb_total, sp * a.kb_per_split);
+        *kb1 = min(kb_total, *kb0 + a.kb_per_split);
+    };
+
+    if (warp == 0) {
+        if (lane == 0) {                             // ---- TMA producer
+            uint32_t st = 0, round = 0;
+            for (int it = blockIdx.x; it < items && !*failed; it += gridDim.x) {
+                int m0, n0, kb0, kb1;
+                item_of(it, &m0, &n0, &kb0, &kb1);
+                for (int kb = kb0; kb < kb1; ++kb) {
+                    if (round > 0 && !mbar_wait(&s.empty[st], (round - 1) & 1)) { *failed = 1; break; }
+                    mbar_expect_tx(&s.full[st], kRawBytes + kBBytes);
+                    tma_load_2d(s.raw[st], &tm_q, m0, kb * kTK, &s.full[st]);
+#pragma unroll
+                    for (int j = 0; j < kTN / 64; ++j)
+                        tma_load_2d(s.b[st] + j * 8192, &tm_dy, n0 + 64 * j, kb * kTK, &s.full[st]);
+                    if (++st == kStages) { st = 0; ++round; }
+                }
+            }
+            // copies in flight must have landed before the CTA's shared memory is released
+            for (int i = 0; i < kStages && *failed; ++i) mbar_wait(&s.full[i], round & 1, 4096u);
+        }
+    } else if (warp == 1) {
+        if (lane == 0) {                             // ---- MMA issuer
+            constexpr uint32_t idesc = umma_idesc_bf16(kTM, kTN) | (1u << 15) | (1u << 16);   // both operands MN-major
+            uint32_t st = 0, round = 0;
+            int i = 0;
+            bool ok = true;
+            for (int it = blockIdx.x; it < items && ok; it += gridDim.x, ++i) {
+                int m0, n0, kb0, kb1;
+                item_of(it, &m0, &n0, &kb0, &kb1);
+                const int ab = i & 1;
+                if (i >= 2 && !mbar_wait(&s.acc_empty[ab], ((i / 2) - 1) & 1)) { ok = false; break; }
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                for (int kb = kb0; kb < kb1; ++kb) {
+                    if (!mbar_wait(&s.full[st], round & 1) || !mbar_wait(&s.ready[st], round & 1)) { ok = false; break; }
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                    const uint32_t a0 = smem_u32(s.a[st]), b0 = smem_u32(s.b[st]);
+#pragma unroll
+                    for (int k = 0; k < kTK / 16; ++k)
+                        umma_bf16(tmem + ab * kTN, umma_desc_mn_sw128(a0 + k * 2048, 8192), umma_desc_mn_sw128(b0 + k * 2048, 8192), idesc,
+                                  kb > kb0 || k > 0);
+                    umma_commit(&s.empty[st]);
+                    if (++st == kStages) { st = 0; ++round; }
+                }
+                if (ok) umma_commit(&s.acc_full[ab]);
+            }
+            if (!ok) *failed = 1;
+        }
+    } else if (warp < 6) {                           // ---- epilogue
+        const int qd = warp % 4;
+        float* stage = s.out[warp - 2];
+        int i = 0;
+        for (int it = blockIdx.x; it < items; it += gridDim.x, ++i) {
+            int m0, n0, kb0, kb1;
+            item_of(it, &m0, &n0, &kb0, &kb1);
+            const int ab = i & 1;
+            bool ok = mbar_wait(&s.acc_full[ab], (i / 2) & 1);
+            ok = __all_sync(0xffffffffu, ok) && !*failed;
+            if (!__all_sync(0xffffffffu, ok)) {
+                *failed = 1;
+                break;
+            }
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            float* base = a.out + (size_t)(it / a.tiles) * a.split_stride + (size_t)(m0 + qd * 32) * a.ld + n0;
+            const int rows = min(32, a.D - (m0 + qd * 32)), cols = a.N - n0;
+            for (int c = 0; c < kTN / 32; ++c) {
+                uint32_t v[32];
+                tmem_ld_32(tmem + ((uint32_t)(qd * 32) << 16) + (uint32_t)(ab * kTN + c * 32), v);
+                if (c == kTN / 32 - 1) {
+                    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                    mbar_arrive(&s.acc_empty[ab]);
+                }
+                if (c * 32 >= cols) continue;
+#pragma unroll
+                for (int j = 0; j < 32; ++j) stage[lane * kPitch + j] = __uint_as_float(v[j]);
+                __syncwarp();
+                float* p = base + c * 32 + lane;
+                if (c * 32 + lane < cols) {
+                    if (a.accumulate) {
+#pragma unroll 8
+                        for (int r = 0; r < rows; ++r) p[(size_t)r * a.ld] += stage[r * kPitch + lane];
+                    } else {
+#pragma unroll 8
+                        for (int r = 0; r < rows; ++r) p[(size_t)r * a.ld] = stage[r * kPitch + lane];
+                    }
+                }
+                __syncwarp();
+            }
+        }
+    } else {                                         // ---- q -> bf16 operand tile
+        const int tid = threadIdx.x - 192;
+        const int r = tid % kTK, blk = tid / kTK;    // token of the run, block of 32 columns
+        const uint32_t sw = (uint32_t)(r & 7);
+        uint32_t st = 0, round = 0;
+        bool ok = true;
+        for (int it = blockIdx.x; it < items && ok; it += gridDim.x) {
+            int m0, n0, kb0, kb1;
+            item_of(it, &m0, &n0, &kb0, &kb1);
+            const size_t ecol = (size_t)(m0 / 32 + blk);
+            const bool have = ecol < a.e_ld;
+            auto exponent = [&](int kb) -> uint32_t {   // of this thread's block; beyond the matrix q is filled with zeros
+                const int t = kb * kTK + r;
+                return have && kb < kb1 && t < a.T ? a.e[(size_t)t * a.e_ld + ecol] : 0u;
+            };
+            uint32_t e0 = exponent(kb0), e1 = exponent(kb0 + 1);
+            for (int kb = kb0; kb < kb1; ++kb) {
+                const uint32_t e2 = exponent(kb + 2);
+                const float scale = pow2_of(e0);
+                if (!mbar_wait(&s.full[st], round & 1)) { ok = false; break; }
+                const uint8_t* src = s.raw[st] + r * 128;
+                uint8_t* dst = s.a[st] + (blk / 2) * 8192 + r * 128;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const uint4 q = *reinterpret_cast<const uint4*>(src + ((uint32_t)(blk * 2 + h) ^ sw) * 16);
+                    const uint32_t w[4] = {q.x ^ 0x80808080u, q.y ^ 0x80808080u, q.z ^ 0x80808080u, q.w ^ 0x80808080u};
+#pragma unroll
+                    for (int p = 0; p < 2; ++p) {
+                        uint32_t o[4];
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const uint32_t word = w[2 * p + j / 2];
+                            // the byte q + 128 as the low mantissa byte of 2^23: subtracting 2^23 + 128 leaves q exactly
+                            const float f0 = __uint_as_float(__byte_perm(word, 0x4B000000u, 0x7540 + 2 * (j % 2))) - 8388736.f;
+                            const float f1 = __uint_as_float(__byte_perm(word, 0x4B000000u, 0x7541 + 2 * (j % 2))) - 8388736.f;
+                            const __nv_bfloat162 b2 = __floats2bfloat162_rn(f0 * scale, f1 * scale);
+                            o[j] = *reinterpret_cast<const uint32_t*>(&b2);
+                        }
+                        const uint32_t chunk = (uint32_t)((blk % 2) * 4 + h * 2 + p);
+                        *reinterpret_cast<uint4*>(dst + (chunk ^ sw) * 16) = make_uint4(o[0], o[1], o[2], o[3]);
+                    }
+                }
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                mbar_arrive(&s.ready[st]);
+                if (++st == kStages) { st = 0; ++round; }
+                e0 = e1;
+                e1 = e2;
+            }
+        }
+        if (!ok) *failed = 1;
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    if (threadIdx.x == 0 && *failed) atomicExch(&g_status, ABS_ETIMEOUT);
+    if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+}
+
+// dw (+)= the partial sums, in split order.
+__global__ void __launch_bounds__(256) k_wgrad_join(const float* part, int splits, size_t split_stride, int N, size_t n, float* dw, size_t ld,
+                                                    int accumulate) {
+    pdl_wait();
+    pdl_trigger();
+    for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (size_t)gridDim.x * 256) {
+        float s = part[i];
+        for (int k = 1; k < splits; ++k) s += part[(size_t)k * split_stride + i];
+        float* p = dw + (i / N) * ld + i % N;
+        *p = accumulate ? *p + s : s;
+    }
+}
+
+// dy with rows that TMA cannot start at, copied to rows of `ld8` elements (16-byte aligned).
+__global__ void __launch_bounds__(256) k_pack_rows(const bf16* x, size_t ld, int N, int ld8, size_t n, bf16* out) {
+    pdl_wait();
+    pdl_trigger();
+    for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (size_t)gridDim.x * 256) {
+        const size_t t = i / ld8;
+        const int c = (int)(i - t * ld8);
+        out[i] = c < N ? x[t * ld + c] : __float2bfloat16_rn(0.f);
+    }
+}
+
+bool misaligned(const void* p, size_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) != 0; }
+size_t up256(size_t n) { return (n + 255) / 256 * 256; }
+
+int grid_for(size_t n, int per_cta) {
+    const size_t want = (n + per_cta - 1) / per_cta;
+    return (int)std::min<size_t>(want, 148 * 16);
+}
+
+constexpr int kSms = 148;
+
+// How the work is cut: output tiles, and runs of tokens where there are fewer tiles than SMs.
+struct WgPlan {
+    int tiles_m, tiles_n, splits, kb_per_split;
+    bool repack;
+    size_t ld8, part_bytes, pack_bytes;
+};
+WgPlan plan_of(uint64_t T, uint64_t D, uint64_t N, const void* dy, uint64_t ld_dy) {
+    WgPlan p{};
+    p.tiles_m = (int)((D + kTM - 1) / kTM);
+    p.tiles_n = (int)((N + kTN - 1) / kTN);
+    const int kb = (int)((T + kTK - 1) / kTK);
+    const int64_t tiles = (int64_t)p.tiles_m * p.tiles_n;
+    int splits = (int)std::max<int64_t>(1, std::min<int64_t>(tiles ? kSms / tiles : 1, kb / 4));
+    p.kb_per_split = std::max(1, (kb + splits - 1) / splits);
+    p.splits = std::max(1, (kb + p.kb_per_split - 1) / p.kb_per_split);
+    p.repack = misaligned(dy, 16) || ld_dy % 8 != 0;
+    p.ld8 = (N + 7) / 8 * 8;
+    p.part_bytes = p.splits > 1 ? up256((size_t)p.splits * D * N * 4) : 0;
+    p.pack_bytes = p.repack ? up256((size_t)T * p.ld8 * 2) : 0;
+    return p;
+}
+
+}  // namespace
+}  // namespace abs_sgd
+
+using namespace abs_sgd;
+
+extern "C" int abs_ckpt8_quantize(const void* x, uint64_t ld_x, uint32_t dtype, uint64_t tokens, uint64_t width, int8_t* q, uint8_t* e,
+                                  void* stream) {
+    if (dtype != ABS_F32 && dtype != ABS_BF16) return thread_error(ABS_EINVAL, "dtype must be ABS_F32 or ABS_BF16");
+    const size_t es = dtype == ABS_F32 ? 4 : 2;
+    if (width == 0 || ld_x < width) return thread_error(ABS_EINVAL, "width must be at least 1 and ld_x at least width");
+    if (width > 0x7fffffe0ull) return thread_error(ABS_ELIMIT, "width exceeds 2^31 - 32");
+    if (tokens == 0) return ABS_OK;
+    if (!x || !q || !e) return thread_error(ABS_EINVAL, "x, q and e must not be NULL");
+    if (misaligned(x, es) || misaligned(q, 16) || misaligned(e, 4)) return thread_error(ABS_EINVAL, "x must be aligned to its elements, q to 16 and e to 4 bytes");
+    const uint32_t per_row = (uint32_t)((width + 31) / 32 * 4);
+    const size_t n8 = (size_t)tokens * per_row;
+    const bool wide = !misaligned(x, 16) && ld_x * es % 16 == 0;
+    const int grid = grid_for(n8, 256);
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    auto go = [&](auto* p) {
+        using T = std::remove_cv_t<std::remove_pointer_t<decltype(p)>>;
+        return launch_kernel(wide ? k_ckpt8_quantize<T, true> : k_ckpt8_quantize<T, false>, grid, 256, 0, s, true, (const T*)x, (size_t)ld_x, n8,
+                             per_row, (int)width, reinterpret_cast<uint2*>(q), e);
+    };
+    const cudaError_t r = dtype == ABS_F32 ? go((float*)nullptr) : go((bf16*)nullptr);
+    return r == cudaSuccess ? ABS_OK : thread_error(ABS_ECUDA, cudaGetErrorString(r));
+}
+
+extern "C" int abs_ckpt8_dequantize(const int8_t* q, const uint8_t* e, uint64_t tokens, uint64_t width, void* x, uint64_t ld_x, uint32_t dtype,
+                                    void* stream) {
+    if (dtype != ABS_F32 && dtype != ABS_BF16) return thread_error(ABS_EINVAL, "dtype must be ABS_F32 or ABS_BF16");
+    const size_t es = dtype == ABS_F32 ? 4 : 2;
+    if (width == 0 || ld_x < width) return thread_error(ABS_EINVAL, "width must be at least 1 and ld_x at least width");
+    if (width > 0x7fffffe0ull) return thread_error(ABS_ELIMIT, "width exceeds 2^31 - 32");
+    if (tokens == 0) return ABS_OK;
+    if (!x || !q || !e) return thread_error(ABS_EINVAL, "x, q and e must not be NULL");
+    if (misaligned(x, es) || misaligned(q, 16) || misaligned(e, 4)) return thread_error(ABS_EINVAL, "x must be aligned to its elements, q to 16 and e to 4 bytes");
+    const uint32_t per_row = (uint32_t)((width + 31) / 32 * 4);
+    const size_t n8 = (size_t)tokens * per_row;
+    const bool wide = !misaligned(x, 16) && ld_x * es % 16 == 0;
+    const int grid = grid_for(n8, 256);
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    auto go = [&](auto* p) {
+        using T = std::remove_cv_t<std::remove_pointer_t<decltype(p)>>;
+        return launch_kernel(wide ? k_ckpt8_dequantize<T, true> : k_ckpt8_dequantize<T, false>, grid, 256, 0, s, true,
+                             reinterpret_cast<const uint2*>(q), e, static_cast<T*>(x), (size_t)ld_x, n8, per_row, (int)width);
+    };
+    const cudaError_t r = dtype == ABS_F32 ? go((float*)nullptr) : go((bf16*)nullptr);
+    return r == cudaSuccess ? ABS_OK : thread_error(ABS_ECUDA, cudaGetErrorString(r));
+}
+
+extern "C" size_t abs_ckpt8_wgrad_workspace(uint64_t tokens, uint64_t width, uint64_t out, const void* dy, uint64_t ld_dy) {
+    if (tokens > 0x7fffffffull || width > 0x7fffffffull || out > 0x7fffffffull) return 0;
+    const WgPlan p = plan_of(tokens, width, out, dy, ld_dy);
+    return p.part_bytes + p.pack_bytes;
+}
+
+extern "C" int abs_ckpt8_wgrad(const int8_t* q, const uint8_t* e, const void* dy, uint64_t ld_dy, uint64_t tokens, uint64_t width,
+                               uint64_t out, float* dw, uint64_t ld_dw, int accumulate, void* workspace, size_t workspace_bytes, void* stream) {
+    if (width == 0 || out == 0 || ld_dy < out || ld_dw < out) return thread_error(ABS_EINVAL, "width and out must be at least 1, ld_dy and ld_dw at least out");
+    if (tokens > 0x7fffffffull || width > 0x7fffffffull || out > 0x7fffffffull) return thread_error(ABS_ELIMIT, "a size exceeds 2^31 - 1");
+    if (!dw || misaligned(dw, 4)) return thread_error(ABS_EINVAL, "dw must be non-NULL and 4-byte aligned");
+    if (tokens && (!q || !e || !dy)) return thread_error(ABS_EINVAL, "q, e and dy must not be NULL");
+    if (misaligned(q, 16) || misaligned(e, 4) || misaligned(dy, 2)) return thread_error(ABS_EINVAL, "q must be aligned to 16 bytes, e to 4, dy to its elements");
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    cudaError_t r = cudaSuccess;
+    if (tokens == 0) {
+        if (!accumulate) r = cudaMemset2DAsync(dw, ld_dw * 4, 0, out * 4, width, s);
+        return r == cudaSuccess ? ABS_OK : thread_error(ABS_ECUDA, cudaGetErrorString(r));
+    }
+    const WgPlan p = plan_of(tokens, width, out, dy, ld_dy);
+    if ((int64_t)p.tiles_m * p.tiles_n * p.splits > 0x7fffffff / 2) return thread_error(ABS_ELIMIT, "too many output tiles");
+    if (p.part_bytes + p.pack_bytes) {
+        if (!workspace || misaligned(workspace, 256)) return thread_error(ABS_EINVAL, "workspace must be non-NULL and 256-byte aligned");
+        if (workspace_bytes < p.part_bytes + p.pack_bytes) return thread_error(ABS_ENOMEM, "workspace too small");
+    }
+    float* part = static_cast<float*>(workspace);
+    if (p.repack) {
+        bf16* packed = reinterpret_cast<bf16*>(static_cast<char*>(workspace) + p.part_bytes);
+        const size_t n = (size_t)tokens * p.ld8;
+        r = launch_kernel(k_pack_rows, grid_for(n, 1024), 256, 0, s, true, static_cast<const bf16*>(dy), (size_t)ld_dy, (int)out, (int)p.ld8, n, packed);
+        if (r != cudaSuccess) return thread_error(ABS_ECUDA, cudaGetErrorString(r));
+        dy = packed;
+        ld_dy = p.ld8;
+    }
+    const uint64_t W = (width + 31) / 32 * 32;
+    CUtensorMap tq, td;
+    if (!encode_2d(&tq, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, const_cast<int8_t*>(q), tokens, W, kTK, kTM) ||
+        !encode_2d(&td, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(dy), tokens, out, kTK, 64, ld_dy))
+        return thread_error(ABS_ECUDA, "cuTensorMapEncodeTiled failed");
+    WgArgs a{};
+    a.e = e; a.e_ld = W / 32; a.T = (int)tokens; a.D = (int)width; a.N = (int)out;
+    a.tiles_n = p.tiles_n; a.tiles = p.tiles_m * p.tiles_n; a.splits = p.splits; a.kb_per_split = p.kb_per_split;
+    a.out = p.splits > 1 ? part : dw;
+    a.ld = p.splits > 1 ? out : ld_dw;
+    a.split_stride = p.splits > 1 ? (size_t)width * out : 0;
+    a.accumulate = p.splits > 1 ? 0 : accumulate;
+    const size_t smem = sizeof(WgSmem) + 1024;
+    r = cudaFuncSetAttribute(k_wgrad, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (r == cudaSuccess) r = launch_kernel(k_wgrad, std::min(a.tiles * a.splits, kSms), kWgThreads, smem, s, true, tq, td, a);
+    if (r == cudaSuccess && p.splits > 1) {
+        const size_t n = (size_t)width * out;
+        r = launch_kernel(k_wgrad_join, grid_for(n, 256), 256, 0, s, true, (const float*)part, p.splits, a.split_stride, (int)out, n, dw, (size_t)ld_dw, accumulate);
+    }
+    return r == cudaSuccess ? ABS_OK : thread_error(ABS_ECUDA, cudaGetErrorString(r));
+}
+
+extern "C" int abs_llm_check(void* stream) {
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    int st = 0;
+    const int zero = 0;
+    cudaError_t r = cudaMemcpyFromSymbolAsync(&st, g_status, sizeof(int), 0, cudaMemcpyDeviceToHost, s);
+    if (r == cudaSuccess) r = cudaStreamSynchronize(s);
+    if (r == cudaSuccess && st != 0) {
+        r = cudaMemcpyToSymbolAsync(g_status, &zero, sizeof(int), 0, cudaMemcpyHostToDevice, s);
+        if (r == cudaSuccess) r = cudaStreamSynchronize(s);
+    }
+    if (r != cudaSuccess) return thread_error(ABS_ECUDA, cudaGetErrorString(r));
+    return st == 0 ? ABS_OK : thread_error(st, "a bounded wait inside a kernel ran out");
+}
