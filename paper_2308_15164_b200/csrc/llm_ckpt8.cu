@@ -9,13 +9,12 @@
 
 #include "abs_internal.h"
 #include "abs_llm.h"
+#include "llm_status.cuh"
 #include "row_ops.cuh"
 #include "tcgen05.cuh"
 
 namespace abs_sgd {
 namespace {
-
-__device__ int g_status;     // ABS_ETIMEOUT once a bounded wait of k_wgrad has run out; read and cleared by abs_llm_check
 
 // Exponent byte of a block from the bits of its largest magnitude (a NaN's bits are above infinity's).
 __device__ __forceinline__ uint32_t block_exponent(uint32_t amax_bits) {
@@ -321,7 +320,7 @@ __global__ void __launch_bounds__(kWgThreads, 1) k_wgrad(const __grid_constant__
     }
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
-    if (threadIdx.x == 0 && *failed) atomicExch(&g_status, ABS_ETIMEOUT);
+    if (threadIdx.x == 0 && *failed) report_timeout();
     if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
 }
 
@@ -490,14 +489,9 @@ extern "C" int abs_ckpt8_wgrad(const int8_t* q, const uint8_t* e, const void* dy
 
 extern "C" int abs_llm_check(void* stream) {
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    int st = 0;
-    const int zero = 0;
-    cudaError_t r = cudaMemcpyFromSymbolAsync(&st, g_status, sizeof(int), 0, cudaMemcpyDeviceToHost, s);
-    if (r == cudaSuccess) r = cudaStreamSynchronize(s);
-    if (r == cudaSuccess && st != 0) {
-        r = cudaMemcpyToSymbolAsync(g_status, &zero, sizeof(int), 0, cudaMemcpyHostToDevice, s);
-        if (r == cudaSuccess) r = cudaStreamSynchronize(s);
-    }
+    int st[2] = {0, 0};
+    cudaError_t r = take_status(&st[0], s);
+    if (r == cudaSuccess) r = take_status_norm(&st[1], s);
     if (r != cudaSuccess) return thread_error(ABS_ECUDA, cudaGetErrorString(r));
-    return st == 0 ? ABS_OK : thread_error(st, "a bounded wait inside a kernel ran out");
+    return st[0] == 0 && st[1] == 0 ? ABS_OK : thread_error(ABS_ETIMEOUT, "a bounded wait inside a kernel ran out");
 }

@@ -57,66 +57,74 @@ def _refuse(rc):
     raise _b.AbsError(rc, _lib.abs_last_error(None).decode())
 
 
-def _matrix(t, name, dtype=None, shape=None):
-    if not isinstance(t, torch.Tensor) or t.dim() != 2 or not t.is_cuda:
+_empty, _Tensor = torch.empty, torch.Tensor
+_stream_of = torch._C._cuda_getCurrentRawStream      # what torch.cuda.current_stream(d).cuda_stream returns, 2 us sooner
+
+
+def _first(t, name):
+    """(dtype code, rows, columns, device index) of the matrix that the others have to agree with."""
+    if not isinstance(t, _Tensor) or not t.is_cuda or t.dim() != 2:
         raise TypeError(f"{name} must be a CUDA tensor of two dimensions")
-    if t.dtype not in _DTYPE if dtype is None else t.dtype != dtype:
-        raise TypeError(f"{name} has dtype {t.dtype}" + (f", {dtype} is wanted" if dtype else ", float32 or bfloat16 is wanted"))
-    if shape is not None and t.shape != shape:
-        raise ValueError(f"{name} has shape {tuple(t.shape)}, {tuple(shape)} is wanted")
-    if t.stride(1) != 1 and t.shape[1] > 1 or t.stride(0) < t.shape[1] and t.shape[0] > 1:
+    code = _DTYPE.get(t.dtype)
+    if code is None:
+        raise TypeError(f"{name} has dtype {t.dtype}, float32 or bfloat16 is wanted")
+    rows, cols = t.shape
+    return code, rows, cols, t.get_device()
+
+
+def _matrix(t, name, dtype, rows, cols, index):
+    """(address, leading dimension) of a [rows, cols] matrix on CUDA device `index`."""
+    if not isinstance(t, _Tensor) or t.dtype is not dtype or t.get_device() != index:
+        raise TypeError(f"{name} must be a {dtype} tensor on cuda:{index}")
+    if t.shape != (rows, cols):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, {(rows, cols)} is wanted")
+    if t.is_contiguous():
+        return t.data_ptr(), cols
+    down, along = t.stride()
+    if along != 1 and cols > 1 or down < cols and rows > 1:
         raise ValueError(f"{name}: rows must be contiguous and must not overlap")
-    return t
+    return t.data_ptr(), max(down, cols)
 
 
-def _vector(t, name, n, dtype, device):
-    if not isinstance(t, torch.Tensor) or t.dtype != dtype or t.device != device:
-        raise TypeError(f"{name} must be a {dtype} tensor on {device}")
-    if t.dim() != 1 or t.shape[0] != n or n > 1 and t.stride(0) != 1:
+def _vector(t, name, n, dtype, index):
+    """Address of a contiguous vector of n elements on CUDA device `index`."""
+    if not isinstance(t, _Tensor) or t.dtype is not dtype or t.get_device() != index:
+        raise TypeError(f"{name} must be a {dtype} tensor on cuda:{index}")
+    if t.shape != (n,) or not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous with {n} elements")
-    return t
+    return t.data_ptr()
 
 
-def _same_device(device, *ts):
-    for t in ts:
-        if t is not None and t.device != device:
-            raise ValueError("the tensors are on different devices")
-
-
-def _ld(t):
-    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
-
-
-def _addr(t):
-    return None if t is None else t.data_ptr()
-
-
-def _call(device, fn, *args):
-    """fn(*args, stream) with `device` current, on its current stream."""
-    stream = torch.cuda.current_stream(device).cuda_stream
-    if device.index == torch.cuda.current_device():
-        rc = fn(*args, stream)
+def _call(index, fn, *args):
+    """fn(*args, stream) with device `index` current, on its current stream."""
+    if index == torch._C._cuda_getDevice():
+        rc = fn(*args, _stream_of(index))
     else:
-        with torch.cuda.device(device):
-            rc = fn(*args, stream)
-    if rc != _b.OK:
+        with torch.cuda.device(index):
+            rc = fn(*args, _stream_of(index))
+    if rc:
         _refuse(rc)
 
 
-def _workspace(n, device):
-    return torch.empty(n, dtype=torch.uint8, device=device)
+def _workspace(n, like):
+    return _empty(n, dtype=torch.uint8, device=like.device)
 
 
-def _dlogits(logits, dlogits, need_grad):
-    if not need_grad:
-        if dlogits is not None:
-            raise ValueError("dlogits is given but need_grad is False")
-        return None
-    if dlogits is None:
-        return torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
-    _matrix(dlogits, "dlogits", logits.dtype, logits.shape)
-    _same_device(logits.device, dlogits)
-    return dlogits
+def _out(t, name, like, index):
+    """(tensor, address, leading dimension) of an output of `like`'s type and shape; made if not given."""
+    rows, cols = like.shape
+    if t is None:
+        t = torch.empty_like(like, memory_format=torch.contiguous_format)
+        return t, t.data_ptr(), cols
+    return (t, *_matrix(t, name, like.dtype, rows, cols, index))
+
+
+def _dlogits(logits, dlogits, need_grad, index):
+    if need_grad:
+        return _out(dlogits, "dlogits", logits, index)
+    if dlogits is not None:
+        raise ValueError("dlogits is given but need_grad is False")
+    return None, None, 0
 
 
 def policy_loss(logits, labels, logp_old, advantage, weight, logp_ref=None, clip_low: float = 0.2, clip_high: float = 0.2,
@@ -126,22 +134,21 @@ def policy_loss(logits, labels, logp_old, advantage, weight, logp_ref=None, clip
     logits [tokens, vocab] float32 / bfloat16; labels int32; logp_old, advantage, weight, logp_ref float32 [tokens].
     weight is a token's share of the loss (1 / n for the mean over n tokens); tokens of weight 0 or with a label outside
     [0, vocab) are left out.  dlogits may be the logits themselves."""
-    T, V = _matrix(logits, "logits").shape
-    dev = logits.device
-    _vector(labels, "labels", T, _I32, dev)
-    for t, name in ((logp_old, "logp_old"), (advantage, "advantage"), (weight, "weight")):
-        _vector(t, name, T, _F32, dev)
-    if logp_ref is not None:
-        _vector(logp_ref, "logp_ref", T, _F32, dev)
-    d = _dlogits(logits, dlogits, need_grad)
-    out = torch.empty(T + 3, dtype=_F32, device=dev)
-    n = _POLICY_WORKSPACE
-    ws = _workspace(n, dev)
+    code, T, V, dev = _first(logits, "logits")
+    z, ld = _matrix(logits, "logits", logits.dtype, T, V, dev)
+    y = _vector(labels, "labels", T, _I32, dev)
+    old = _vector(logp_old, "logp_old", T, _F32, dev)
+    adv = _vector(advantage, "advantage", T, _F32, dev)
+    w = _vector(weight, "weight", T, _F32, dev)
+    ref = None if logp_ref is None else _vector(logp_ref, "logp_ref", T, _F32, dev)
+    d, da, ld_d = _dlogits(logits, dlogits, need_grad, dev)
+    out = _empty(T + 3, dtype=_F32, device=logits.device)
+    ws = _workspace(_POLICY_WORKSPACE, logits)
     at = out.data_ptr()
-    _call(dev, _lib.abs_policy_loss, logits.data_ptr(), _DTYPE[logits.dtype], T, V, _ld(logits), labels.data_ptr(), logp_old.data_ptr(),
-          _addr(logp_ref), advantage.data_ptr(), weight.data_ptr(), clip_low, clip_high, kl_coef, at, at + 12, _addr(d),
-          _ld(d) if d is not None else 0, ws.data_ptr(), n)
-    return PolicyLoss(out[0], out[1], out[2], out[3:], d)
+    _call(dev, _lib.abs_policy_loss, z, code, T, V, ld, y, old, ref, adv, w, clip_low, clip_high, kl_coef, at, at + 12, da, ld_d, ws.data_ptr(),
+          _POLICY_WORKSPACE)
+    loss, kl, clipped, logp = out.split_with_sizes((1, 1, 1, T))
+    return PolicyLoss(loss.view(()), kl.view(()), clipped.view(()), logp, d)
 
 
 _POLICY_WORKSPACE = int(_lib.abs_policy_loss_workspace())
@@ -154,42 +161,34 @@ def preference_loss(logits, labels, offsets, logp_ref, beta: float = 0.1, smooth
     logits [tokens, vocab]: the rows of the answers one after the other, answers 2 p and 2 p + 1 the preferred and the
     other one of pair p; offsets int32 [2 pairs + 1]: their first rows; labels int32 [tokens], outside [0, vocab) for rows
     that do not count; logp_ref float32 [2 pairs]: the reference model's log-probabilities.  scale: 1 / pairs if not given."""
-    T, V = _matrix(logits, "logits").shape
-    dev = logits.device
-    _vector(labels, "labels", T, _I32, dev)
-    if not isinstance(offsets, torch.Tensor) or offsets.dim() != 1 or offsets.shape[0] % 2 != 1:
+    code, T, V, dev = _first(logits, "logits")
+    z, ld = _matrix(logits, "logits", logits.dtype, T, V, dev)
+    y = _vector(labels, "labels", T, _I32, dev)
+    if not isinstance(offsets, _Tensor) or offsets.dim() != 1 or offsets.shape[0] % 2 != 1:
         raise ValueError("offsets must have 2 pairs + 1 elements")
     pairs = offsets.shape[0] // 2
-    _vector(offsets, "offsets", 2 * pairs + 1, _I32, dev)
-    _vector(logp_ref, "logp_ref", 2 * pairs, _F32, dev)
-    d = _dlogits(logits, dlogits, need_grad)
-    out = torch.empty(3 * pairs + 1, dtype=_F32, device=dev)
-    n = int(_lib.abs_preference_loss_workspace(T))
-    ws = _workspace(n, dev)
+    off = _vector(offsets, "offsets", 2 * pairs + 1, _I32, dev)
+    ref = _vector(logp_ref, "logp_ref", 2 * pairs, _F32, dev)
+    d, da, ld_d = _dlogits(logits, dlogits, need_grad, dev)
+    out = _empty(3 * pairs + 1, dtype=_F32, device=logits.device)
+    n = _lib.abs_preference_loss_workspace(T)
+    ws = _workspace(n, logits)
     at = out.data_ptr()
-    _call(dev, _lib.abs_preference_loss, logits.data_ptr(), _DTYPE[logits.dtype], T, V, _ld(logits), labels.data_ptr(), offsets.data_ptr(),
-          pairs, logp_ref.data_ptr(), beta, smoothing, (1.0 / pairs if pairs else 0.0) if scale is None else scale, at, at + 4,
-          at + 4 + 4 * pairs, _addr(d), _ld(d) if d is not None else 0, ws.data_ptr(), n)
-    return PreferenceLoss(out[0], out[1:1 + pairs], out[1 + pairs:], d)
+    if scale is None:
+        scale = 1.0 / pairs if pairs else 0.0
+    _call(dev, _lib.abs_preference_loss, z, code, T, V, ld, y, off, pairs, ref, beta, smoothing, scale, at, at + 4, at + 4 + 4 * pairs, da, ld_d,
+          ws.data_ptr(), n)
+    loss, pair_loss, seq_logp = out.split_with_sizes((1, pairs, 2 * pairs))
+    return PreferenceLoss(loss.view(()), pair_loss, seq_logp, d)
 
 
-def _gate_kind(gate, like, width):
+def _gate(gate, like, rows, cols, index):
+    """(kind, address, leading dimension)"""
     if gate is None:
-        return _GATE_NONE
-    if isinstance(gate, torch.Tensor) and gate.dim() == 1:
-        _vector(gate, "gate", width, _F32, like.device)
-        return _GATE_CHANNEL
-    _matrix(gate, "gate", like.dtype, like.shape)
-    _same_device(like.device, gate)
-    return _GATE_ELEMENT
-
-
-def _out_matrix(t, name, like):
-    if t is None:
-        return torch.empty(like.shape, dtype=like.dtype, device=like.device)
-    _matrix(t, name, like.dtype, like.shape)
-    _same_device(like.device, t)
-    return t
+        return _GATE_NONE, None, 0
+    if isinstance(gate, _Tensor) and gate.dim() == 1:
+        return _GATE_CHANNEL, _vector(gate, "gate", cols, _F32, index), 0
+    return (_GATE_ELEMENT, *_matrix(gate, "gate", like.dtype, rows, cols, index))
 
 
 def residual_norm(x, h, w_pre, w_post=None, gate=None, scale: float = 1.0, eps: float = 1e-6, y=None, n=None):
@@ -197,17 +196,16 @@ def residual_norm(x, h, w_pre, w_post=None, gate=None, scale: float = 1.0, eps: 
 
     x, h [tokens, width] float32 / bfloat16; w_pre, w_post float32 [width].  gate: None (G = 1), float32 [width] (G = gate)
     or [tokens, width] of x's dtype (G = sigmoid(gate)).  y may be x, n may be h."""
-    T, D = _matrix(x, "x").shape
-    dev = x.device
-    _matrix(h, "h", x.dtype, x.shape)
-    _same_device(dev, h)
-    _vector(w_pre, "w_pre", D, _F32, dev)
-    if w_post is not None:
-        _vector(w_post, "w_post", D, _F32, dev)
-    kind = _gate_kind(gate, x, D)
-    y, n = _out_matrix(y, "y", x), _out_matrix(n, "n", x)
-    _call(dev, _lib.abs_residual_norm, x.data_ptr(), _ld(x), h.data_ptr(), _ld(h), _addr(gate), _ld(gate) if kind == _GATE_ELEMENT else 0, kind,
-          _addr(w_post), w_pre.data_ptr(), scale, eps, _DTYPE[x.dtype], T, D, y.data_ptr(), _ld(y), n.data_ptr(), _ld(n))
+    code, T, D, dev = _first(x, "x")
+    dt = x.dtype
+    xa, ld_x = _matrix(x, "x", dt, T, D, dev)
+    ha, ld_h = _matrix(h, "h", dt, T, D, dev)
+    pre = _vector(w_pre, "w_pre", D, _F32, dev)
+    post = None if w_post is None else _vector(w_post, "w_post", D, _F32, dev)
+    kind, ga, ld_g = _gate(gate, x, T, D, dev)
+    y, ya, ld_y = _out(y, "y", x, dev)
+    n, na, ld_n = _out(n, "n", x, dev)
+    _call(dev, _lib.abs_residual_norm, xa, ld_x, ha, ld_h, ga, ld_g, kind, post, pre, scale, eps, code, T, D, ya, ld_y, na, ld_n)
     return y, n
 
 
@@ -217,74 +215,76 @@ def residual_norm_backward(dn, dy, y, h, w_pre, w_post=None, gate=None, scale: f
 
     dw_pre, dw_post and a channel gate's dgate (float32 [width]) may be slices of a flat gradient; with accumulate the
     sums are added to what the given ones hold (those that are not given start at zero)."""
-    T, D = _matrix(y, "y").shape
-    dev, dt, shape = y.device, y.dtype, y.shape
-    _matrix(dn, "dn", dt, shape)
-    _matrix(h, "h", dt, shape)
-    if dy is not None:
-        _matrix(dy, "dy", dt, shape)
-    _same_device(dev, dn, h, dy)
-    _vector(w_pre, "w_pre", D, _F32, dev)
-    if w_post is not None:
-        _vector(w_post, "w_post", D, _F32, dev)
-    kind = _gate_kind(gate, y, D)
-    dx, dh = _out_matrix(dx, "dx", y), _out_matrix(dh, "dh", y)
-    fresh = torch.zeros if accumulate else torch.empty
+    code, T, D, dev = _first(y, "y")
+    dt = y.dtype
+    ya, ld_y = _matrix(y, "y", dt, T, D, dev)
+    dna, ld_dn = _matrix(dn, "dn", dt, T, D, dev)
+    ha, ld_h = _matrix(h, "h", dt, T, D, dev)
+    dya, ld_dy = (None, 0) if dy is None else _matrix(dy, "dy", dt, T, D, dev)
+    pre = _vector(w_pre, "w_pre", D, _F32, dev)
+    post = None if w_post is None else _vector(w_post, "w_post", D, _F32, dev)
+    kind, ga, ld_g = _gate(gate, y, T, D, dev)
+    dx, dxa, ld_dx = _out(dx, "dx", y, dev)
+    dh, dha, ld_dh = _out(dh, "dh", y, dev)
 
     def column(t, name):
-        return fresh(D, dtype=_F32, device=dev) if t is None else _vector(t, name, D, _F32, dev)
+        if t is None:
+            t = (torch.zeros if accumulate else _empty)(D, dtype=_F32, device=y.device)
+            return t, t.data_ptr()
+        return t, _vector(t, name, D, _F32, dev)
 
-    dw_pre = column(dw_pre, "dw_pre")
-    if w_post is not None:
-        dw_post = column(dw_post, "dw_post")
+    dw_pre, dpre = column(dw_pre, "dw_pre")
+    dpost, dga, ld_dg = None, None, 0
+    if post is not None:
+        dw_post, dpost = column(dw_post, "dw_post")
     elif dw_post is not None:
         raise ValueError("dw_post without w_post")
     if kind == _GATE_CHANNEL:
-        dgate = column(dgate, "dgate")
+        dgate, dga = column(dgate, "dgate")
     elif kind == _GATE_ELEMENT:
-        dgate = _out_matrix(dgate, "dgate", y)
+        dgate, dga, ld_dg = _out(dgate, "dgate", y, dev)
     elif dgate is not None:
         raise ValueError("dgate without a gate")
-    n = int(_lib.abs_residual_norm_workspace(T, D))
-    ws = _workspace(n, dev)
-    element = kind == _GATE_ELEMENT
-    _call(dev, _lib.abs_residual_norm_backward, dn.data_ptr(), _ld(dn), _addr(dy), _ld(dy) if dy is not None else 0, y.data_ptr(), _ld(y),
-          h.data_ptr(), _ld(h), _addr(gate), _ld(gate) if element else 0, kind, _addr(w_post), w_pre.data_ptr(), scale, eps, _DTYPE[dt], T, D,
-          dx.data_ptr(), _ld(dx), dh.data_ptr(), _ld(dh), _addr(dgate), _ld(dgate) if element else 0, dw_pre.data_ptr(), _addr(dw_post),
-          int(accumulate), ws.data_ptr(), n)
+    n = _lib.abs_residual_norm_workspace(T, D)
+    ws = _workspace(n, y)
+    _call(dev, _lib.abs_residual_norm_backward, dna, ld_dn, dya, ld_dy, ya, ld_y, ha, ld_h, ga, ld_g, kind, post, pre, scale, eps, code, T, D,
+          dxa, ld_dx, dha, ld_dh, dga, ld_dg, dpre, dpost, bool(accumulate), ws.data_ptr(), n)
     return ResidualGrads(dx, dh, dgate, dw_pre, dw_post)
 
 
 def ckpt8_quantize(x) -> Ckpt8:
     """An activation [tokens, width] (float32 / bfloat16) in 8 bits (``abs_ckpt8_quantize``)."""
-    T, D = _matrix(x, "x").shape
+    code, T, D, dev = _first(x, "x")
+    xa, ld = _matrix(x, "x", x.dtype, T, D, dev)
     W = (D + 31) // 32 * 32
-    q = torch.empty((T, W), dtype=torch.int8, device=x.device)
-    e = torch.empty((T, W // 32), dtype=torch.uint8, device=x.device)
-    _call(x.device, _lib.abs_ckpt8_quantize, x.data_ptr(), _ld(x), _DTYPE[x.dtype], T, D, q.data_ptr(), e.data_ptr())
+    q = _empty((T, W), dtype=torch.int8, device=x.device)
+    e = _empty((T, W // 32), dtype=torch.uint8, device=x.device)
+    _call(dev, _lib.abs_ckpt8_quantize, xa, ld, code, T, D, q.data_ptr(), e.data_ptr())
     return Ckpt8(q, e, D)
 
 
 def _ckpt(c):
-    W = (c.width + 31) // 32 * 32
+    """(address of q, address of e, tokens, device index)"""
     q, e = c.q, c.e
-    if q.dtype != torch.int8 or e.dtype != torch.uint8 or not q.is_cuda or q.device != e.device:
+    W = (c.width + 31) // 32 * 32
+    dev = q.get_device()
+    if q.dtype is not torch.int8 or e.dtype is not torch.uint8 or dev < 0 or e.get_device() != dev:
         raise TypeError("a Ckpt8 holds an int8 and a uint8 tensor on one CUDA device")
     if q.dim() != 2 or q.shape[1] != W or e.shape != (q.shape[0], W // 32) or not q.is_contiguous() or not e.is_contiguous():
         raise ValueError("a Ckpt8 holds q [tokens, width rounded up to 32] and e [tokens, same / 32], contiguous")
-    return q, e
+    return q.data_ptr(), e.data_ptr(), q.shape[0], dev
 
 
 def ckpt8_dequantize(c: Ckpt8, dtype=torch.bfloat16, out=None):
     """The values that a Ckpt8 stands for, [tokens, width]."""
-    q, e = _ckpt(c)
-    if out is None:
-        out = torch.empty((q.shape[0], c.width), dtype=dtype, device=q.device)
-    _matrix(out, "out", dtype, (q.shape[0], c.width))
-    _same_device(q.device, out)
-    if dtype not in _DTYPE:
+    qa, ea, T, dev = _ckpt(c)
+    code = _DTYPE.get(dtype)
+    if code is None:
         raise TypeError("dtype must be float32 or bfloat16")
-    _call(q.device, _lib.abs_ckpt8_dequantize, q.data_ptr(), e.data_ptr(), q.shape[0], c.width, out.data_ptr(), _ld(out), _DTYPE[dtype])
+    if out is None:
+        out = _empty((T, c.width), dtype=dtype, device=c.q.device)
+    oa, ld = _matrix(out, "out", dtype, T, c.width, dev)
+    _call(dev, _lib.abs_ckpt8_dequantize, qa, ea, T, c.width, oa, ld, code)
     return out
 
 
@@ -292,28 +292,23 @@ def ckpt8_wgrad(c: Ckpt8, dy, out=None, accumulate: bool = False):
     """x^T dy of the activation x that `c` stands for: the gradient of a weight stored [in, out] (``abs_ckpt8_wgrad``).
 
     dy bfloat16 [tokens, out].  out float32 [width, out], for instance a view of a flat gradient; accumulate adds to it."""
-    q, e = _ckpt(c)
-    T, N = _matrix(dy, "dy", _BF16).shape
-    if T != q.shape[0]:
-        raise ValueError(f"dy has {T} rows, the checkpoint {q.shape[0]}")
-    dev = q.device
-    _same_device(dev, dy)
+    qa, ea, T, dev = _ckpt(c)
+    if not isinstance(dy, _Tensor) or dy.dim() != 2:
+        raise TypeError("dy must be a CUDA tensor of two dimensions")
+    N = dy.shape[1]
+    ya, ld = _matrix(dy, "dy", _BF16, T, N, dev)
     if out is None:
         if accumulate:
             raise ValueError("accumulate needs an out to add to")
-        out = torch.empty((c.width, N), dtype=_F32, device=dev)
-    else:
-        _matrix(out, "out", _F32, (c.width, N))
-        _same_device(dev, out)
-    ld = _ld(dy)
-    n = int(_lib.abs_ckpt8_wgrad_workspace(T, c.width, N, dy.data_ptr(), ld))
-    ws = _workspace(n, dev) if n else None
-    _call(dev, _lib.abs_ckpt8_wgrad, q.data_ptr(), e.data_ptr(), dy.data_ptr(), ld, T, c.width, N, out.data_ptr(), _ld(out), int(accumulate),
-          _addr(ws), n)
+        out = _empty((c.width, N), dtype=_F32, device=dy.device)
+    oa, ld_o = _matrix(out, "out", _F32, c.width, N, dev)
+    n = _lib.abs_ckpt8_wgrad_workspace(T, c.width, N, ya, ld)
+    ws = _workspace(n, dy) if n else None
+    _call(dev, _lib.abs_ckpt8_wgrad, qa, ea, ya, ld, T, c.width, N, oa, ld_o, bool(accumulate), ws.data_ptr() if n else None, n)
     return out
 
 
 def check(device=None):
     """Blocks until the current stream has finished; raises if a kernel of this module gave up a bounded wait."""
-    device = torch.device("cuda", torch.cuda.current_device()) if device is None else torch.device(device)
-    _call(device, _lib.abs_llm_check)
+    index = torch.cuda.current_device() if device is None else torch.device(device).index
+    _call(torch.cuda.current_device() if index is None else index, _lib.abs_llm_check)
