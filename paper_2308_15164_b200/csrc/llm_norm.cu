@@ -1,6 +1,8 @@
 // Residual join of a transformer block with its two norms and its gate, forward and backward (abs_residual_norm*).
 //
 //     u = h / rms(h) * w_post      y = scale x + G u      n = y / rms(y) * w_pre
+// Backward with hn = h / rms(h), yn = y / rms(y): a channel gate g and w_post share one column sum, since
+// dgate = w_post sum_t dY hn and dw_post = g sum_t dY hn.
 // One row of the activations at a time: the two means make a row's work a chain of two reductions, and everything between
 // them is elementwise.  Bound by memory: forward 4 (5 with an element gate) and backward 6 (8) elements per position.
 #include <math.h>
@@ -17,13 +19,14 @@ namespace {
 constexpr int kWidthMax = 32768;
 constexpr int kSms = 148;
 constexpr int kBackCtas = 296;       // CTAs of the plain backward kernel
-constexpr int kRingThreads = 512;    // most threads of a CTA of the ring kernels
-constexpr int kRingSmem = 216 * 1024;   // shared memory of an SM that their CTAs share (1 KB per CTA is the system's)
+constexpr int kRingSmem = 216 * 1024;   // shared memory of an SM that the ring kernels' CTAs share (1 KB per CTA is the system's)
 constexpr size_t kSmemMax = 227 * 1024; // of one CTA
-constexpr int kRingCtasMax = 8;
-// CTAs of an SM: 1024 threads forward (64 registers), 512 backward (the column sums take up to 128).
-constexpr int ctas_per_sm(bool back, int threads) {
-    const int n = (back ? 512 : 1024) / threads;
+constexpr int kRingCtasMax = 16;
+// Threads of an SM for the ring kernels, by the elements that a thread owns: what their registers (weights, column sums,
+// the row's values) leave room for.
+constexpr int ring_threads(bool back, int elems) { return back ? (elems == 32 ? 256 : elems == 16 ? 384 : 640) : (elems == 32 ? 384 : elems == 16 ? 640 : 1024); }
+constexpr int ctas_per_sm(bool back, int threads, int elems) {
+    const int n = ring_threads(back, elems) / threads;
     return n < kRingCtasMax ? n : kRingCtasMax;
 }
 
@@ -40,10 +43,11 @@ struct NormArgs {
     size_t ld_dn, ld_dy;
     void *dx, *dh, *dgate;           // dgate: element gate only
     size_t ld_dx, ld_dh, ld_dgate;
-    float* part;                     // [CTA][3][D]: dw_pre, dw_post, channel dgate
+    float* part;                     // [CTA][2][D]: sum dn yn; sum dY hn (channel gate) or dU hn
 };
 
-__device__ __forceinline__ float sigmoid(float v) { return 1.f / (1.f + expf(-v)); }
+// Relative error below 4e-7 for |v| < 8 (the base-2 exponential's argument is rounded once), 0 and 1 in the limits.
+__device__ __forceinline__ float sigmoid(float v) { return __fdividef(1.f, 1.f + __expf(-v)); }
 
 // kV consecutive elements at a time, kV = 1 for rows that are not 16-byte aligned; a thread keeps its columns throughout.
 template <typename T, int kV, bool kPost, int kGate>
@@ -104,10 +108,10 @@ __global__ void __launch_bounds__(256) k_residual_norm_back(NormArgs a) {
     __shared__ float sh[24];
     pdl_wait();
     pdl_trigger();
-    float* col = a.part + (size_t)blockIdx.x * 3 * a.D;
+    float* col = a.part + (size_t)blockIdx.x * 2 * a.D;
     for (int c = threadIdx.x * kV; c < a.D; c += 256 * kV)
 #pragma unroll
-        for (int k = 0; k < kV; ++k) col[c + k] = col[a.D + c + k] = col[2 * (size_t)a.D + c + k] = 0.f;
+        for (int k = 0; k < kV; ++k) col[c + k] = col[a.D + c + k] = 0.f;
     for (size_t t = blockIdx.x; t < a.T; t += gridDim.x) {
         const T* dn = static_cast<const T*>(a.dn) + t * a.ld_dn;
         const T* dy = a.dy ? static_cast<const T*>(a.dy) + t * a.ld_dy : nullptr;
@@ -152,16 +156,16 @@ __global__ void __launch_bounds__(256) k_residual_norm_back(NormArgs a) {
                 const float w = kPost ? a.w_post[c + k] : 1.f;
                 float du = d;
                 if (kGate == 1) {
-                    col[2 * (size_t)a.D + c + k] += d * (hn * w);
+                    col[a.D + c + k] += d * hn;
                     du *= static_cast<const float*>(a.gate)[c + k];
                 }
                 if (kGate == 2) {
                     const float g = sigmoid(vg[k]);
                     du *= g;
-                    vg[k] = d * (hn * w) * g * (1.f - g);
+                    vg[k] = du * (hn * w) * (1.f - g);
                 }
                 if (kPost) {
-                    col[a.D + c + k] += du * hn;
+                    if (kGate != 1) col[a.D + c + k] += du * hn;
                     q[0] += du * w * hn;
                 }
                 vh[k] = du * w;
@@ -186,14 +190,16 @@ __global__ void __launch_bounds__(256) k_residual_norm_back(NormArgs a) {
 }
 
 // ------------------------------------------------------------------------------------------------
-// The same rows through a ring of row images in shared memory.  A CTA takes rows b, b + G, ...; one thread keeps kS
-// rows of copies in flight (cp.async.bulk, one per input matrix), so that the chain of reductions of a row hides
-// behind the copies of the next ones.  A thread owns kP pieces of 16 bytes and at most one single element.
+// The same rows through a ring of row images in shared memory.  A CTA takes rows b, b + G, ...; one thread keeps the
+// ring's rows of copies in flight (cp.async.bulk, one per input matrix), so that the chain of reductions of a row hides
+// behind the copies of the next ones.  A thread owns kP pieces of 16 bytes, up to 32 elements (what a row costs a thread
+// beside its elements -- reductions, waits, addresses, some 150 instructions -- is spread over them: with 8 elements the
+// kernels were bound by instruction issue at half the memory's rate), and at most one single element.
 // Rows of odd width start at every alignment.  G is a multiple of the period with which the alignment repeats, so that
 // all rows of one CTA are cut alike: single elements up to the first 16-byte boundary, pieces, single elements.  The
 // copies move the pieces (nothing outside the row is read), the single elements are plain loads.  All matrices of the
 // call have to be aligned alike.
-// The weights are kept in shared memory, cut like the rows; the column sums in registers.
+// Weights and column sums stay in registers; two fp32 operations per instruction where the order of a sum allows it.
 // ------------------------------------------------------------------------------------------------
 constexpr int kRingMax = 8;
 
@@ -204,33 +210,82 @@ struct RingArgs {
 };
 
 struct RingCtl {
+    alignas(16) float red[3][3][16]; // [reduction][number][warp]
     alignas(8) uint64_t full[kRingMax];
-    float red[2][3 * 32];
-    float red2[32];
 };
+constexpr size_t kRingCtl = (sizeof(RingCtl) + 15) / 16 * 16;
 
-// Sums over the CTA's threads, one synchronisation: `sh` must not be the buffer of the reduction just before.
+// Pairs of fp32 in one 64-bit register (fma.rn.f32x2 and its kin round like the scalar instructions).
+__device__ __forceinline__ uint64_t as_u64(float2 v) { return *reinterpret_cast<uint64_t*>(&v); }
+__device__ __forceinline__ float2 as_f2(uint64_t v) { return *reinterpret_cast<float2*>(&v); }
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(as_u64(a)), "l"(as_u64(b)), "l"(as_u64(c)));
+    return as_f2(r);
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(as_u64(a)), "l"(as_u64(b)));
+    return as_f2(r);
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(as_u64(a)), "l"(as_u64(b)));
+    return as_f2(r);
+}
+__device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
+__device__ __forceinline__ float sum2(float2 v) { return v.x + v.y; }
+
+// A 16-byte piece as kVec / 2 pairs.
+template <typename T>
+constexpr int kPairs = kVec<T> / 2;
+__device__ __forceinline__ void unpack(uint4 a, float2 (&v)[2], float) {
+    v[0] = make_float2(__uint_as_float(a.x), __uint_as_float(a.y));
+    v[1] = make_float2(__uint_as_float(a.z), __uint_as_float(a.w));
+}
+__device__ __forceinline__ void unpack(uint4 a, float2 (&v)[4], bf16) {
+    const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = make_float2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xFFFF0000u));
+}
+__device__ __forceinline__ uint4 pack(const float2 (&v)[2], float) {
+    return make_uint4(__float_as_uint(v[0].x), __float_as_uint(v[0].y), __float_as_uint(v[1].x), __float_as_uint(v[1].y));
+}
+__device__ __forceinline__ uint4 pack(const float2 (&v)[4], bf16) {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const __nv_bfloat162 b = __float22bfloat162_rn(v[i]);
+        w[i] = *reinterpret_cast<const uint32_t*>(&b);
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// Sums over the CTA's threads, one synchronisation: `sh` (zero beyond the CTA's warps) must not be the buffer of the
+// reduction just before.
 template <int kN>
-__device__ __forceinline__ void cta_sum(float (&v)[kN], float* sh) {
-    const int warps = blockDim.x / 32, warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+__device__ __forceinline__ void cta_sum(float (&v)[kN], float (*sh)[16], int warps) {
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
 #pragma unroll
     for (int k = 0; k < kN; ++k) {
 #pragma unroll
         for (int o = 16; o; o >>= 1) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
-        if (lane == 0) sh[k * 32 + warp] = v[k];
+        if (lane == 0) sh[k][warp] = v[k];
     }
     __syncthreads();
+    if (warps == 1) return;
 #pragma unroll
-    for (int k = 0; k < kN; ++k) {
-        float s = lane < warps ? sh[k * 32 + lane] : 0.f;
+    for (int k = 0; k < kN; ++k) v[k] = 0.f;
+    for (int w = 0; w < warps; w += 4)
 #pragma unroll
-        for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-        v[k] = s;
-    }
+        for (int k = 0; k < kN; ++k) {
+            const float4 f = *reinterpret_cast<const float4*>(&sh[k][w]);
+            v[k] += (f.x + f.y) + (f.z + f.w);
+        }
 }
 
-// What a thread needs to know of its rows' cut, and the ring's copies.
-template <typename T, int kP, int kIn>
+// A CTA's rows: how they are cut, which of them are in flight, which is the current one.
+template <typename T, int kIn>
 struct Ring {
     RowCut cut;
     int extra;                       // column of this thread's single element, or -1
@@ -245,11 +300,22 @@ struct Ring {
     uint32_t phase = 0;
     bool ok = true;
 
-    __device__ __forceinline__ void cut_rows(const T* row0, int D) {
-        cut = cut_row(row0, D);
+    __device__ __forceinline__ void begin(uint8_t* smem, const RingArgs& a, const T* row0) {
+        ctl = reinterpret_cast<RingCtl*>(smem);
+        base = smem + kRingCtl;
+        row_bytes = a.row_bytes;
+        stages = a.stages;
+        rows = a.n.T;
+        cut = cut_row(row0, a.n.D);
         bytes = (uint32_t)cut.pieces * 16u;
         const int tid = threadIdx.x;
-        extra = tid < cut.head ? tid : tid < cut.head + cut.tail ? D - cut.tail + tid - cut.head : -1;
+        extra = tid < cut.head ? tid : tid < cut.head + cut.tail ? a.n.D - cut.tail + tid - cut.head : -1;
+        for (int i = tid; i < 9 * 16; i += blockDim.x) (&ctl->red[0][0][0])[i] = 0.f;
+        if (tid == 0) {
+            for (int i = 0; i < stages; ++i) mbar_init(&ctl->full[i], 1);
+            asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        }
+        __syncthreads();
     }
     __device__ __forceinline__ void load(int stage, size_t t) {       // one thread
         if (t >= rows || bytes == 0) return;
@@ -259,11 +325,16 @@ struct Ring {
         mbar_expect_tx(&ctl->full[stage], total);
 #pragma unroll
         for (int i = 0; i < kIn; ++i)
-            if (in[i]) bulk_load(base + ((size_t)stage * kIn + i) * row_bytes, in[i] + t * ld[i] + cut.head, bytes, &ctl->full[stage]);
+            if (in[i]) bulk_load(base + (size_t)(stage * kIn + i) * row_bytes, in[i] + t * ld[i] + cut.head, bytes, &ctl->full[stage]);
+    }
+    // Everybody has passed the first synchronisation of the current row, t, the k-th: the image of the row before it is free.
+    __device__ __forceinline__ void refill(size_t t, size_t G, int k) {
+        if (threadIdx.x == 0 && k > 0) load((st == 0 ? stages : st) - 1, t + (size_t)(stages - 1) * G);
     }
     __device__ __forceinline__ void load_extra(size_t t, float (&v)[kIn]) const {
+        if (extra < 0 || t >= rows) return;
 #pragma unroll
-        for (int i = 0; i < kIn; ++i) v[i] = extra >= 0 && t < rows && in[i] ? to_f(in[i][t * ld[i] + extra]) : 0.f;
+        for (int i = 0; i < kIn; ++i) v[i] = in[i] ? to_f(in[i][t * ld[i] + extra]) : 0.f;
     }
     __device__ __forceinline__ void wait() {
         if (bytes != 0 && !mbar_wait(&ctl->full[st], phase, ok ? kSpinLimit : 1u)) ok = false;
@@ -272,306 +343,252 @@ struct Ring {
         if (++st == stages) { st = 0; phase ^= 1u; }
     }
     // Piece j of this thread of input i, in the current row's image.
-    __device__ __forceinline__ void piece(int i, int j, float (&v)[kVec<T>]) const {
-        Pack<T, kVec<T>>::load(reinterpret_cast<const T*>(base + ((size_t)st * kIn + i) * row_bytes) + (threadIdx.x + j * blockDim.x) * kVec<T>, v);
+    __device__ __forceinline__ void piece(int i, int j, float2 (&v)[kPairs<T>]) const {
+        unpack(*reinterpret_cast<const uint4*>(base + (size_t)(st * kIn + i) * row_bytes + (threadIdx.x + j * blockDim.x) * 16), v, T());
     }
     __device__ __forceinline__ bool has(int j) const { return (int)(threadIdx.x + j * blockDim.x) < cut.pieces; }
     __device__ __forceinline__ int column(int j) const { return cut.head + (int)(threadIdx.x + j * blockDim.x) * kVec<T>; }
+    __device__ __forceinline__ void store(T* row, int j, const float2 (&v)[kPairs<T>]) const {
+        if (ok) *reinterpret_cast<uint4*>(row + column(j)) = pack(v, T());
+    }
+    // This thread's columns of a weight vector, times those of a second one if there is one; its single element is returned.
+    template <int kP>
+    __device__ __forceinline__ float weights(const float* p, const float* q, float2 (&w)[kP][kPairs<T>]) const {
+        auto at = [&](int c) { return q ? p[c] * q[c] : p[c]; };
+#pragma unroll
+        for (int j = 0; j < kP; ++j)
+#pragma unroll
+            for (int i = 0; i < kPairs<T>; ++i) w[j][i] = has(j) ? make_float2(at(column(j) + 2 * i), at(column(j) + 2 * i + 1)) : both(0.f);
+        return extra >= 0 ? at(extra) : 0.f;
+    }
 };
 
-// A weight vector in shared memory, four floats of a piece side by side: [kP][kVec / 4][threads].
-template <typename T, int kP>
-__device__ __forceinline__ float4* weight_slot(float4* w, int j, int q) { return w + ((size_t)j * (kVec<T> / 4) + q) * blockDim.x + threadIdx.x; }
-template <typename T, int kP>
-constexpr int kWeightVecs = kP * (kVec<T> / 4);      // float4 per thread
-template <typename T, int kP, typename R>
-__device__ __forceinline__ float stage_weight(float4* w, const float* src, const R& r) {
-#pragma unroll
-    for (int j = 0; j < kP; ++j)
-        if (r.has(j))
-#pragma unroll
-            for (int q = 0; q < kVec<T> / 4; ++q) {
-                const float* p = src + r.column(j) + 4 * q;
-                *weight_slot<T, kP>(w, j, q) = make_float4(p[0], p[1], p[2], p[3]);
-            }
-    return r.extra >= 0 ? src[r.extra] : 0.f;
-}
-template <typename T, int kP>
-__device__ __forceinline__ void weight(float4* w, int j, float (&v)[kVec<T>]) {
-#pragma unroll
-    for (int q = 0; q < kVec<T> / 4; ++q) {
-        const float4 f = *weight_slot<T, kP>(w, j, q);
-        v[4 * q] = f.x; v[4 * q + 1] = f.y; v[4 * q + 2] = f.z; v[4 * q + 3] = f.w;
-    }
-}
-
 template <typename T, int kP, bool kPost, int kGate>
-__global__ void __launch_bounds__(512, kP == 4 ? 1 : 2) k_join(const __grid_constant__ RingArgs ra) {
-    constexpr int kV = kVec<T>, kIn = kGate == 2 ? 3 : 2;
+__global__ void __launch_bounds__(ring_threads(false, kP * kVec<T>), 1) k_join(const __grid_constant__ RingArgs ra) {
+    constexpr int kN = kPairs<T>, kIn = kGate == 2 ? 3 : 2;
+    constexpr bool kScaled = kPost || kGate == 1;    // u carries a weight: w_post, the channel gate, or their product
     const NormArgs& a = ra.n;
     extern __shared__ __align__(16) uint8_t smem[];
-    Ring<T, kP, kIn> r;
-    r.ctl = reinterpret_cast<RingCtl*>(smem);
-    float4* w_pre = reinterpret_cast<float4*>(smem + (sizeof(RingCtl) + 15) / 16 * 16);
-    float4* w_post = w_pre + kWeightVecs<T, kP> * blockDim.x;
-    float4* w_gate = w_post + (kPost ? kWeightVecs<T, kP> * blockDim.x : 0);
-    r.base = reinterpret_cast<uint8_t*>(w_gate + (kGate == 1 ? kWeightVecs<T, kP> * blockDim.x : 0));
-    r.row_bytes = ra.row_bytes; r.stages = ra.stages; r.rows = a.T;
+    const int warps = blockDim.x / 32;
+    const size_t t0 = blockIdx.x, G = gridDim.x;
+    Ring<T, kIn> r;
     r.in[0] = static_cast<const T*>(a.x); r.ld[0] = a.ld_x;
     r.in[1] = static_cast<const T*>(a.h); r.ld[1] = a.ld_h;
     if (kGate == 2) { r.in[kIn - 1] = static_cast<const T*>(a.gate); r.ld[kIn - 1] = a.ld_gate; }
-    const size_t t0 = blockIdx.x, G = gridDim.x;
-    r.cut_rows(r.in[0] + t0 * a.ld_x, a.D);
-    if (threadIdx.x == 0) {
-        for (int i = 0; i < r.stages; ++i) mbar_init(&r.ctl->full[i], 1);
-        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    }
-    __syncthreads();
+    r.begin(smem, ra, r.in[0] + t0 * a.ld_x);
     pdl_wait();
     pdl_trigger();
     if (threadIdx.x == 0)
         for (int i = 0; i < r.stages; ++i) r.load(i, t0 + i * G);
-    float ex[kIn], nx[kIn];
+    float nx[kIn] = {};
     r.load_extra(t0, nx);
-    const float xw_pre = stage_weight<T, kP>(w_pre, a.w_pre, r);
-    const float xw_post = kPost ? stage_weight<T, kP>(w_post, a.w_post, r) : 1.f;
-    const float xw_gate = kGate == 1 ? stage_weight<T, kP>(w_gate, static_cast<const float*>(a.gate), r) : 1.f;
+    float2 w_u[kP][kN], w_pre[kP][kN];
+    const float* gate = kGate == 1 ? static_cast<const float*>(a.gate) : nullptr;
+    const float xw_u = kScaled ? r.template weights<kP>(kPost ? a.w_post : gate, kPost ? gate : nullptr, w_u) : 1.f;
+    const float xw_pre = r.template weights<kP>(a.w_pre, nullptr, w_pre);
 
     int k = 0;
     for (size_t t = t0; t < a.T; t += G, ++k, r.next()) {
-        float* red = r.ctl->red[k & 1];
+        float (*red)[16] = r.ctl->red[k & 1];
+        float ex[kIn];
 #pragma unroll
         for (int i = 0; i < kIn; ++i) ex[i] = nx[i];
         r.load_extra(t + G, nx);
         r.wait();
-        const auto refill = [&] {              // everybody has passed the first synchronisation: the previous row's image is free
-            if (threadIdx.x == 0 && k > 0) r.load((r.st == 0 ? r.stages : r.st) - 1, t + (size_t)(r.stages - 1) * G);
-        };
         float rh = 1.f;
         if (kPost) {
-            float s[1] = {r.extra >= 0 ? ex[1] * ex[1] : 0.f};
+            float2 s2 = both(0.f);
 #pragma unroll
             for (int j = 0; j < kP; ++j)
                 if (r.has(j)) {
-                    float v[kV];
+                    float2 v[kN];
                     r.piece(1, j, v);
 #pragma unroll
-                    for (int i = 0; i < kV; ++i) s[0] += v[i] * v[i];
+                    for (int i = 0; i < kN; ++i) s2 = fma2(v[i], v[i], s2);
                 }
-            cta_sum<1>(s, red);
-            refill();
-            rh = 1.f / sqrtf(s[0] * a.inv_d + a.eps);
+            float s[1] = {sum2(s2) + (r.extra >= 0 ? ex[1] * ex[1] : 0.f)};
+            cta_sum<1>(s, red, warps);
+            r.refill(t, G, k);
+            rh = rsqrtf(s[0] * a.inv_d + a.eps);
         }
-        float y[kP][kV], s[1] = {0.f}, xy = 0.f;
+        float2 y[kP][kN], s2 = both(0.f);
         T* yrow = static_cast<T*>(a.y) + t * a.ld_y;
 #pragma unroll
         for (int j = 0; j < kP; ++j)
             if (r.has(j)) {
-                float u[kV], g[kV];
+                float2 u[kN], g[kN];
                 r.piece(0, j, y[j]);
                 r.piece(1, j, u);
-                if (kPost) {
-                    weight<T, kP>(w_post, j, g);
+                if (kGate == 2) r.piece(kIn - 1, j, g);
 #pragma unroll
-                    for (int i = 0; i < kV; ++i) u[i] *= rh * g[i];
+                for (int i = 0; i < kN; ++i) {
+                    if (kPost) u[i] = mul2(u[i], both(rh));
+                    if (kScaled) u[i] = mul2(u[i], w_u[j][i]);
+                    if (kGate == 2) u[i] = mul2(u[i], make_float2(sigmoid(g[i].x), sigmoid(g[i].y)));
+                    y[j][i] = fma2(y[j][i], both(a.scale), u[i]);
+                    s2 = fma2(y[j][i], y[j][i], s2);
                 }
-                if (kGate == 1) {
-                    weight<T, kP>(w_gate, j, g);
-#pragma unroll
-                    for (int i = 0; i < kV; ++i) u[i] *= g[i];
-                }
-                if (kGate == 2) {
-                    r.piece(kIn - 1, j, g);
-#pragma unroll
-                    for (int i = 0; i < kV; ++i) u[i] *= sigmoid(g[i]);
-                }
-#pragma unroll
-                for (int i = 0; i < kV; ++i) {
-                    y[j][i] = a.scale * y[j][i] + u[i];
-                    s[0] += y[j][i] * y[j][i];
-                }
-                if (r.ok) Pack<T, kV>::store(yrow + r.column(j), y[j]);
+                r.store(yrow, j, y[j]);
             }
+        float s[1] = {sum2(s2)}, xy = 0.f;
         if (r.extra >= 0) {
-            float u = ex[1] * rh * xw_post * xw_gate;
+            float u = ex[1] * rh * xw_u;
             if (kGate == 2) u *= sigmoid(ex[kIn - 1]);
             xy = a.scale * ex[0] + u;
             s[0] += xy * xy;
             if (r.ok) yrow[r.extra] = from_f<T>(xy);
         }
-        cta_sum<1>(s, kPost ? r.ctl->red2 : red);
-        if (!kPost) refill();
-        const float ry = 1.f / sqrtf(s[0] * a.inv_d + a.eps);
+        cta_sum<1>(s, kPost ? r.ctl->red[2] : red, warps);
+        if (!kPost) r.refill(t, G, k);
+        const float ry = rsqrtf(s[0] * a.inv_d + a.eps);
         T* nrow = static_cast<T*>(a.n) + t * a.ld_n;
 #pragma unroll
         for (int j = 0; j < kP; ++j)
-            if (r.has(j) && r.ok) {
-                float g[kV];
-                weight<T, kP>(w_pre, j, g);
+            if (r.has(j)) {
 #pragma unroll
-                for (int i = 0; i < kV; ++i) y[j][i] *= ry * g[i];
-                Pack<T, kV>::store(nrow + r.column(j), y[j]);
+                for (int i = 0; i < kN; ++i) y[j][i] = mul2(mul2(y[j][i], both(ry)), w_pre[j][i]);
+                r.store(nrow, j, y[j]);
             }
-        if (r.extra >= 0 && r.ok) nrow[r.extra] = from_f<T>(xy * (ry * xw_pre));
+        if (r.extra >= 0 && r.ok) nrow[r.extra] = from_f<T>(xy * ry * xw_pre);
     }
     if (!r.ok) report_timeout();
 }
 
 template <typename T, int kP, bool kPost, int kGate>
-__global__ void __launch_bounds__(512, 1) k_join_back(const __grid_constant__ RingArgs ra) {
-    constexpr int kV = kVec<T>, kIn = kGate == 2 ? 5 : 4;
+__global__ void __launch_bounds__(ring_threads(true, kP * kVec<T>), 1) k_join_back(const __grid_constant__ RingArgs ra) {
+    constexpr int kN = kPairs<T>, kIn = kGate == 2 ? 5 : 4;
+    constexpr bool kScaled = kPost || kGate == 1;    // dh carries a weight: w_post, the channel gate, or their product
+    constexpr bool kSum = kPost || kGate == 1;       // the second column sum
     const NormArgs& a = ra.n;
     extern __shared__ __align__(16) uint8_t smem[];
-    Ring<T, kP, kIn> r;
-    r.ctl = reinterpret_cast<RingCtl*>(smem);
-    float4* w_pre = reinterpret_cast<float4*>(smem + (sizeof(RingCtl) + 15) / 16 * 16);
-    float4* w_post = w_pre + kWeightVecs<T, kP> * blockDim.x;
-    float4* w_gate = w_post + (kPost ? kWeightVecs<T, kP> * blockDim.x : 0);
-    r.base = reinterpret_cast<uint8_t*>(w_gate + (kGate == 1 ? kWeightVecs<T, kP> * blockDim.x : 0));
-    r.row_bytes = ra.row_bytes; r.stages = ra.stages; r.rows = a.T;
+    const int warps = blockDim.x / 32;
+    const size_t t0 = blockIdx.x, G = gridDim.x;
+    Ring<T, kIn> r;
     r.in[0] = static_cast<const T*>(a.y); r.ld[0] = a.ld_y;
     r.in[1] = static_cast<const T*>(a.dn); r.ld[1] = a.ld_dn;
     r.in[2] = static_cast<const T*>(a.h); r.ld[2] = a.ld_h;
     r.in[3] = static_cast<const T*>(a.dy); r.ld[3] = a.ld_dy;
     if (kGate == 2) { r.in[kIn - 1] = static_cast<const T*>(a.gate); r.ld[kIn - 1] = a.ld_gate; }
     const bool has_dy = a.dy != nullptr;
-    const size_t t0 = blockIdx.x, G = gridDim.x;
-    r.cut_rows(r.in[0] + t0 * a.ld_y, a.D);
-    if (threadIdx.x == 0) {
-        for (int i = 0; i < r.stages; ++i) mbar_init(&r.ctl->full[i], 1);
-        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    }
-    __syncthreads();
+    r.begin(smem, ra, r.in[0] + t0 * a.ld_y);
     pdl_wait();
     pdl_trigger();
     if (threadIdx.x == 0)
         for (int i = 0; i < r.stages; ++i) r.load(i, t0 + i * G);
-    float ex[kIn], nx[kIn];
+    float nx[kIn] = {};
     r.load_extra(t0, nx);
-    const float xw_pre = stage_weight<T, kP>(w_pre, a.w_pre, r);
-    const float xw_post = kPost ? stage_weight<T, kP>(w_post, a.w_post, r) : 1.f;
-    const float xw_gate = kGate == 1 ? stage_weight<T, kP>(w_gate, static_cast<const float*>(a.gate), r) : 1.f;
-    float c_pre[kP][kV], c_post[kP][kV], c_gate[kP][kV], x_pre = 0.f, x_post = 0.f, x_gate = 0.f;
+    float2 w_u[kP][kN], w_pre[kP][kN], c_pre[kP][kN], c_h[kP][kN];
+    const float* gate = kGate == 1 ? static_cast<const float*>(a.gate) : nullptr;
+    const float xw_u = kScaled ? r.template weights<kP>(kPost ? a.w_post : gate, kPost ? gate : nullptr, w_u) : 1.f;
+    const float xw_pre = r.template weights<kP>(a.w_pre, nullptr, w_pre);
+    float x_pre = 0.f, x_h = 0.f;
 #pragma unroll
     for (int j = 0; j < kP; ++j)
 #pragma unroll
-        for (int i = 0; i < kV; ++i) c_pre[j][i] = c_post[j][i] = c_gate[j][i] = 0.f;
+        for (int i = 0; i < kN; ++i) c_pre[j][i] = c_h[j][i] = both(0.f);
 
     int k = 0;
     for (size_t t = t0; t < a.T; t += G, ++k, r.next()) {
+        float ex[kIn];
 #pragma unroll
         for (int i = 0; i < kIn; ++i) ex[i] = nx[i];
         r.load_extra(t + G, nx);
         r.wait();
-        float s[3] = {0.f, 0.f, 0.f};            // sum y^2, sum dn w_pre y, sum h^2
+        float2 s2[3] = {both(0.f), both(0.f), both(0.f)};       // sum y^2, sum dn w_pre y, sum h^2
 #pragma unroll
         for (int j = 0; j < kP; ++j)
             if (r.has(j)) {
-                float y[kV], n[kV], w[kV];
+                float2 y[kN], n[kN];
                 r.piece(0, j, y);
                 r.piece(1, j, n);
-                weight<T, kP>(w_pre, j, w);
 #pragma unroll
-                for (int i = 0; i < kV; ++i) {
-                    s[0] += y[i] * y[i];
-                    s[1] += n[i] * w[i] * y[i];
+                for (int i = 0; i < kN; ++i) {
+                    s2[0] = fma2(y[i], y[i], s2[0]);
+                    s2[1] = fma2(mul2(n[i], w_pre[j][i]), y[i], s2[1]);
                 }
                 if (kPost) {
                     r.piece(2, j, y);
 #pragma unroll
-                    for (int i = 0; i < kV; ++i) s[2] += y[i] * y[i];
+                    for (int i = 0; i < kN; ++i) s2[2] = fma2(y[i], y[i], s2[2]);
                 }
             }
+        float s[kPost ? 3 : 2] = {sum2(s2[0]), sum2(s2[1])};
+        if (kPost) s[kPost ? 2 : 0] = sum2(s2[2]);
         if (r.extra >= 0) {
             s[0] += ex[0] * ex[0];
             s[1] += ex[1] * xw_pre * ex[0];
-            if (kPost) s[2] += ex[2] * ex[2];
+            if (kPost) s[kPost ? 2 : 0] += ex[2] * ex[2];
         }
-        cta_sum<3>(s, r.ctl->red[k & 1]);
-        if (threadIdx.x == 0 && k > 0) r.load((r.st == 0 ? r.stages : r.st) - 1, t + (size_t)(r.stages - 1) * G);   // the previous row's image is free
-        const float ry = 1.f / sqrtf(s[0] * a.inv_d + a.eps);
-        const float along = s[1] * a.inv_d * ry;
-        const float rh = kPost ? 1.f / sqrtf(s[2] * a.inv_d + a.eps) : 1.f;
-        float q[1] = {0.f}, du[kP][kV], xdu = 0.f;
+        cta_sum<kPost ? 3 : 2>(s, r.ctl->red[k & 1], warps);
+        r.refill(t, G, k);
+        const float ry = rsqrtf(s[0] * a.inv_d + a.eps);
+        const float along = -s[1] * a.inv_d * ry * ry;          // d = ry (dn w_pre) + yn along
+        const float rh = kPost ? rsqrtf(s[kPost ? 2 : 0] * a.inv_d + a.eps) : 1.f;
+        float2 q2 = both(0.f), du[kP][kN];
+        float xdu = 0.f;
         T* dx = static_cast<T*>(a.dx) + t * a.ld_dx;
         T* dh = static_cast<T*>(a.dh) + t * a.ld_dh;
         T* dz = static_cast<T*>(a.dgate) + t * a.ld_dgate;
 #pragma unroll
         for (int j = 0; j < kP; ++j)
             if (r.has(j)) {
-                float d[kV], v[kV], w[kV];
-                r.piece(0, j, v);                // yn
-                r.piece(1, j, d);                // dn
-                weight<T, kP>(w_pre, j, w);
+                float2 d[kN], v[kN];
+                r.piece(0, j, v);
+                r.piece(1, j, d);
 #pragma unroll
-                for (int i = 0; i < kV; ++i) {
-                    v[i] *= ry;
-                    c_pre[j][i] += d[i] * v[i];
-                    d[i] = ry * (d[i] * w[i] - v[i] * along);
+                for (int i = 0; i < kN; ++i) {
+                    v[i] = mul2(v[i], both(ry));                 // yn
+                    c_pre[j][i] = fma2(d[i], v[i], c_pre[j][i]);
+                    d[i] = fma2(v[i], both(along), mul2(mul2(d[i], w_pre[j][i]), both(ry)));
                 }
                 if (has_dy) {
                     r.piece(3, j, v);
 #pragma unroll
-                    for (int i = 0; i < kV; ++i) d[i] += v[i];
+                    for (int i = 0; i < kN; ++i) d[i] = add2(d[i], v[i]);
                 }
 #pragma unroll
-                for (int i = 0; i < kV; ++i) v[i] = a.scale * d[i];
-                if (r.ok) Pack<T, kV>::store(dx + r.column(j), v);
-                r.piece(2, j, v);                // hn, or h without w_post
-                if (kPost) {
-                    weight<T, kP>(w_post, j, w);
+                for (int i = 0; i < kN; ++i) v[i] = mul2(d[i], both(a.scale));
+                r.store(dx, j, v);
+                r.piece(2, j, v);                                // hn, or h without w_post
+                if (kPost)
 #pragma unroll
-                    for (int i = 0; i < kV; ++i) v[i] *= rh;
-                }
-                if (kGate == 1) {
-                    float g[kV];
-                    weight<T, kP>(w_gate, j, g);
-#pragma unroll
-                    for (int i = 0; i < kV; ++i) {
-                        c_gate[j][i] += d[i] * (kPost ? v[i] * w[i] : v[i]);
-                        d[i] *= g[i];
-                    }
-                }
+                    for (int i = 0; i < kN; ++i) v[i] = mul2(v[i], both(rh));
                 if (kGate == 2) {
-                    float g[kV];
+                    float2 g[kN];
                     r.piece(kIn - 1, j, g);
 #pragma unroll
-                    for (int i = 0; i < kV; ++i) {
-                        g[i] = sigmoid(g[i]);
-                        const float dg = d[i] * g[i];
-                        g[i] = dg * (1.f - g[i]) * (kPost ? v[i] * w[i] : v[i]);
-                        d[i] = dg;
+                    for (int i = 0; i < kN; ++i) {
+                        g[i] = make_float2(sigmoid(g[i].x), sigmoid(g[i].y));
+                        d[i] = mul2(d[i], g[i]);
+                        float2 u = mul2(d[i], kPost ? mul2(v[i], w_u[j][i]) : v[i]);
+                        g[i] = fma2(make_float2(-g[i].x, -g[i].y), u, u);       // dU u (1 - g)
                     }
-                    if (r.ok) Pack<T, kV>::store(dz + r.column(j), g);
+                    r.store(dz, j, g);
                 }
-                if (kPost) {
 #pragma unroll
-                    for (int i = 0; i < kV; ++i) {
-                        c_post[j][i] += d[i] * v[i];
-                        du[j][i] = d[i] * w[i];
-                        q[0] += du[j][i] * v[i];
-                    }
-                } else if (r.ok) {
-                    Pack<T, kV>::store(dh + r.column(j), d);
+                for (int i = 0; i < kN; ++i) {
+                    if (kSum) c_h[j][i] = fma2(d[i], v[i], c_h[j][i]);
+                    du[j][i] = kScaled ? mul2(d[i], w_u[j][i]) : d[i];
+                    if (kPost) q2 = fma2(du[j][i], v[i], q2);
                 }
+                if (!kPost) r.store(dh, j, du[j]);
             }
+        float q[1] = {sum2(q2)};
         if (r.extra >= 0) {
             const float yn = ex[0] * ry, hn = ex[2] * rh;
             x_pre += ex[1] * yn;
-            float d = ry * (ex[1] * xw_pre - yn * along) + ex[3];
+            float d = yn * along + ex[1] * xw_pre * ry;
+            d += ex[3];
             const float xdx = a.scale * d;
-            if (kGate == 1) {
-                x_gate += d * (hn * xw_post);
-                d *= xw_gate;
-            }
             float xdz = 0.f;
             if (kGate == 2) {
                 const float g = sigmoid(ex[kIn - 1]);
                 d *= g;
-                xdz = d * (1.f - g) * (hn * xw_post);
+                xdz = d * (hn * xw_u);
+                xdz = xdz - g * xdz;
             }
-            x_post += d * hn;
-            xdu = d * xw_post;
+            x_h += d * hn;
+            xdu = d * xw_u;
             q[0] += xdu * hn;
             if (r.ok) {
                 dx[r.extra] = from_f<T>(xdx);
@@ -580,53 +597,55 @@ __global__ void __launch_bounds__(512, 1) k_join_back(const __grid_constant__ Ri
             }
         }
         if (kPost) {
-            cta_sum<1>(q, r.ctl->red2);
-            const float m = q[0] * a.inv_d * rh;
+            cta_sum<1>(q, r.ctl->red[2], warps);
+            const float m = -q[0] * a.inv_d * rh * rh;           // dh = rh du + h m
 #pragma unroll
             for (int j = 0; j < kP; ++j)
                 if (r.has(j)) {
-                    float h[kV];
+                    float2 h[kN];
                     r.piece(2, j, h);
 #pragma unroll
-                    for (int i = 0; i < kV; ++i) h[i] = rh * (du[j][i] - h[i] * m);
-                    if (r.ok) Pack<T, kV>::store(dh + r.column(j), h);
+                    for (int i = 0; i < kN; ++i) h[i] = fma2(h[i], both(m), mul2(du[j][i], both(rh)));
+                    r.store(dh, j, h);
                 }
-            if (r.extra >= 0 && r.ok) dh[r.extra] = from_f<T>(rh * (xdu - ex[2] * m));
+            if (r.extra >= 0 && r.ok) dh[r.extra] = from_f<T>(ex[2] * m + rh * xdu);
         }
     }
-    float* col = a.part + (size_t)blockIdx.x * 3 * a.D;
+    float* col = a.part + (size_t)blockIdx.x * 2 * a.D;
 #pragma unroll
     for (int j = 0; j < kP; ++j)
         if (r.has(j))
 #pragma unroll
-            for (int i = 0; i < kV; ++i) {
-                const int c = r.column(j) + i;
-                col[c] = c_pre[j][i];
-                if (kPost) col[a.D + c] = c_post[j][i];
-                if (kGate == 1) col[2 * (size_t)a.D + c] = c_gate[j][i];
+            for (int i = 0; i < kN; ++i) {
+                float* c = col + r.column(j) + 2 * i;
+                c[0] = c_pre[j][i].x;
+                c[1] = c_pre[j][i].y;
+                if (kSum) {
+                    c[a.D] = c_h[j][i].x;
+                    c[a.D + 1] = c_h[j][i].y;
+                }
             }
     if (r.extra >= 0) {
         col[r.extra] = x_pre;
-        if (kPost) col[a.D + r.extra] = x_post;
-        if (kGate == 1) col[2 * (size_t)a.D + r.extra] = x_gate;
+        if (kSum) col[a.D + r.extra] = x_h;
     }
     if (!r.ok) report_timeout();
 }
 
-// out[c] (+)= sum over the CTAs of part[cta][which][c]: 32 columns per CTA, 32 threads a column, joined in a fixed order.
-__global__ void __launch_bounds__(1024) k_column_sums(const float* part, int n, int D, float* o0, float* o1, float* o2, int accumulate) {
+// Column sums over the CTAs of part[cta][which][c], 32 columns per CTA, 32 threads a column, joined in a fixed order.
+// which 0: dw_pre; which 1, with S the sum: dw_post = S (times the channel gate), channel dgate = S (times w_post).
+__global__ void __launch_bounds__(1024) k_column_sums(const float* part, int n, int D, float* dw_pre, float* dw_post, float* dgate, const float* w_post,
+                                                      const float* gate, int accumulate) {
     __shared__ float sh[32][33];
     pdl_wait();
     pdl_trigger();
-    float* out = blockIdx.y == 0 ? o0 : blockIdx.y == 1 ? o1 : o2;
-    if (!out) return;
     const int lane = threadIdx.x % 32, r = threadIdx.x / 32;
     const int c = blockIdx.x * 32 + lane;
     float s = 0.f;
     if (c < D) {
         const float* p = part + (size_t)blockIdx.y * D + c;
 #pragma unroll 4
-        for (int i = r; i < n; i += 32) s += p[(size_t)i * 3 * D];
+        for (int i = r; i < n; i += 32) s += p[(size_t)i * 2 * D];
     }
     sh[r][lane] = s;
     __syncthreads();
@@ -634,7 +653,13 @@ __global__ void __launch_bounds__(1024) k_column_sums(const float* part, int n, 
 #pragma unroll
     for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
     const int cc = blockIdx.x * 32 + r;
-    if (lane == 0 && cc < D) out[cc] = accumulate ? out[cc] + s : s;
+    if (lane != 0 || cc >= D) return;
+    auto put = [&](float* out, float v) { out[cc] = accumulate ? out[cc] + v : v; };
+    if (blockIdx.y == 0) put(dw_pre, s);
+    else {
+        if (dw_post) put(dw_post, gate ? gate[cc] * s : s);
+        if (dgate) put(dgate, w_post ? w_post[cc] * s : s);
+    }
 }
 
 template <typename K>
@@ -645,7 +670,7 @@ cudaError_t allow_smem(K kernel, size_t bytes) {
 // How a call is launched.  ring: all matrices aligned alike and the row within the pieces that a CTA's threads own.
 struct Plan {
     bool ring;
-    int threads, pieces;             // of a CTA; of a thread
+    int threads, elems;              // of a CTA; elements that a thread owns
     int grid, stages;
     uint32_t row_bytes;
     size_t smem;
@@ -659,24 +684,18 @@ cudaError_t run_plain(const NormArgs& a, bool back, int grid, cudaStream_t s) {
     if (e != cudaSuccess) return e;
     return launch_kernel(k, grid, 256, smem, s, true, a);
 }
-template <typename T, int kP, bool kPost, int kGate>
+template <typename T, int kE, bool kPost, int kGate>
 cudaError_t run_ring(const NormArgs& a, bool back, const Plan& p, cudaStream_t s) {
     const RingArgs r{a, p.stages, p.row_bytes};
-    if (back) {
-        if constexpr (kP <= 2) {
-            const cudaError_t e = allow_smem(k_join_back<T, kP, kPost, kGate>, p.smem);
-            return e != cudaSuccess ? e : launch_kernel(k_join_back<T, kP, kPost, kGate>, p.grid, p.threads, p.smem, s, true, r);
-        }
-        return cudaErrorInvalidValue;
-    }
-    const cudaError_t e = allow_smem(k_join<T, kP, kPost, kGate>, p.smem);
-    return e != cudaSuccess ? e : launch_kernel(k_join<T, kP, kPost, kGate>, p.grid, p.threads, p.smem, s, true, r);
+    auto k = back ? k_join_back<T, kE / kVec<T>, kPost, kGate> : k_join<T, kE / kVec<T>, kPost, kGate>;
+    const cudaError_t e = allow_smem(k, p.smem);
+    return e != cudaSuccess ? e : launch_kernel(k, p.grid, p.threads, p.smem, s, true, r);
 }
 template <typename T, bool kPost, int kGate>
 cudaError_t run(const NormArgs& a, bool back, bool wide, const Plan& p, cudaStream_t s) {
     if (!p.ring) return wide ? run_plain<T, kVec<T>, kPost, kGate>(a, back, p.grid, s) : run_plain<T, 1, kPost, kGate>(a, back, p.grid, s);
-    return p.pieces == 1 ? run_ring<T, 1, kPost, kGate>(a, back, p, s)
-         : p.pieces == 2 ? run_ring<T, 2, kPost, kGate>(a, back, p, s) : run_ring<T, 4, kPost, kGate>(a, back, p, s);
+    return p.elems == 8 ? run_ring<T, 8, kPost, kGate>(a, back, p, s) : p.elems == 16 ? run_ring<T, 16, kPost, kGate>(a, back, p, s)
+                                                                                    : run_ring<T, 32, kPost, kGate>(a, back, p, s);
 }
 template <typename T>
 cudaError_t run_kind(const NormArgs& a, bool back, uint32_t gate, bool wide, const Plan& p, cudaStream_t s) {
@@ -714,34 +733,29 @@ bool rows_aligned(const Mat (&m)[N], size_t es, size_t D) {
         if (q.p) return (reinterpret_cast<uintptr_t>(q.p) & 15) == 0;
     return true;
 }
-// Threads of a CTA for rows of this many pieces, and pieces per thread (at most `most`; 0: more than they can own).
-void ring_shape(size_t pieces, int most, int* threads, int* per_thread) {
-    *per_thread = pieces <= kRingThreads ? 1 : pieces <= 2 * kRingThreads ? 2 : pieces <= 4 * kRingThreads ? 4 : 8;
-    if (*per_thread > most) *per_thread = 0;
-    const size_t per = *per_thread ? (pieces + *per_thread - 1) / *per_thread : kRingThreads;
-    *threads = (int)(per <= 32 ? 32 : (per + 31) / 32 * 32);
+// Elements that a thread owns and threads of a CTA for rows of `D` elements; false: more than a CTA can own.
+bool ring_shape(size_t D, bool back, int* threads, int* elems) {
+    *elems = D <= 8 * 32 ? 8 : D <= 16 * 32 ? 16 : 32;
+    const size_t need = (D + *elems - 1) / *elems;
+    *threads = (int)(need <= 32 ? 32 : (need + 31) / 32 * 32);
+    return *threads <= ring_threads(back, *elems);
 }
 template <int N>
-Plan plan_of(const Mat (&m)[N], size_t es, uint64_t T, uint64_t D, bool back, uint32_t gate_kind, bool post) {
+Plan plan_of(const Mat (&m)[N], size_t es, uint64_t T, uint64_t D, bool back, uint32_t gate_kind) {
     Plan p{};
     size_t period = 1;
-    ring_shape(D * es / 16, back ? 2 : 4, &p.threads, &p.pieces);
-    p.ring = p.pieces > 0 && aligned_alike(m, es, &period);
+    p.ring = ring_shape(D, back, &p.threads, &p.elems) && aligned_alike(m, es, &period);
     p.row_bytes = (uint32_t)((D * es + 15) / 16 * 16);
-    const size_t in = back ? (gate_kind == ABS_GATE_ELEMENT ? 5 : 4) : (gate_kind == ABS_GATE_ELEMENT ? 3 : 2);
-    const size_t weights = 1 + (post ? 1 : 0) + (gate_kind == ABS_GATE_CHANNEL ? 1 : 0);
-    const size_t fixed = (sizeof(RingCtl) + 15) / 16 * 16 + weights * p.pieces * (4 / es) * p.threads * 16;
-    size_t ctas = 0;
+    const size_t images = (back ? 4 : 2) + (gate_kind == ABS_GATE_ELEMENT ? 1 : 0), row = images * p.row_bytes;
+    size_t ctas = 1;
     if (p.ring) {      // as many CTAs as the registers allow, fewer where two rows would not fit; then as many rows as fit
-        ctas = (size_t)ctas_per_sm(back, p.threads);
-        while (ctas > 1 && fixed + 2 * in * p.row_bytes > kRingSmem / ctas) --ctas;
+        ctas = (size_t)ctas_per_sm(back, p.threads, p.elems);
+        while (ctas > 1 && kRingCtl + 2 * row > kRingSmem / ctas) --ctas;
         const size_t room = ctas > 1 ? kRingSmem / ctas : kSmemMax;
-        if (fixed + 2 * in * p.row_bytes > room) p.ring = false;
-        else {
-            const size_t fit = (room - fixed) / (in * p.row_bytes);
-            p.stages = (int)(fit < (size_t)kRingMax ? fit : (size_t)kRingMax);
-            p.smem = fixed + p.stages * in * p.row_bytes;
-        }
+        const size_t fit = (room - kRingCtl) / row;
+        p.ring = fit >= 2;
+        p.stages = (int)(fit < (size_t)kRingMax ? fit : (size_t)kRingMax);
+        p.smem = kRingCtl + p.stages * row;
     }
     if (!p.ring) {
         const uint64_t cap = back ? kBackCtas : kSms * 8;
@@ -799,17 +813,16 @@ extern "C" int abs_residual_norm(const void* x, uint64_t ld_x, const void* h, ui
     a.y = y; a.ld_y = ld_y; a.n = n; a.ld_n = ld_n;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     const bool wide = rows_aligned(m, es, width);
-    const Plan p = plan_of(m, es, tokens, width, false, gate_kind, w_post != nullptr);
+    const Plan p = plan_of(m, es, tokens, width, false, gate_kind);
     const cudaError_t e = dtype == ABS_F32 ? run_kind<float>(a, false, gate_kind, wide, p, s) : run_kind<bf16>(a, false, gate_kind, wide, p, s);
     return e == cudaSuccess ? ABS_OK : thread_error(ABS_ECUDA, cudaGetErrorString(e));
 }
 
 extern "C" size_t abs_residual_norm_workspace(uint64_t tokens, uint64_t width) {
-    int threads = 0, per_thread = 0;
-    ring_shape(width / 8, 2, &threads, &per_thread);      // bf16: the smaller CTAs, so more of them
-    const uint64_t ring = (uint64_t)kSms * ctas_per_sm(true, threads);
+    int threads = 0, elems = 0;
+    const uint64_t ring = ring_shape(width, true, &threads, &elems) ? (uint64_t)kSms * ctas_per_sm(true, threads, elems) : 0;
     const uint64_t most = ring > kBackCtas ? ring : kBackCtas, rows = (tokens + 7) / 8 * 8;
-    return ((size_t)(rows < most ? rows : most) * 3 * width * 4 + 255) / 256 * 256 + 256;
+    return ((size_t)(rows < most ? rows : most) * 2 * width * 4 + 255) / 256 * 256 + 256;
 }
 
 extern "C" int abs_residual_norm_backward(const void* dn, uint64_t ld_dn, const void* dy, uint64_t ld_dy, const void* y, uint64_t ld_y,
@@ -844,11 +857,12 @@ extern "C" int abs_residual_norm_backward(const void* dn, uint64_t ld_dn, const 
     Plan p{};
     if (tokens > 0) {
         const bool wide = rows_aligned(m, es, width);
-        p = plan_of(m, es, tokens, width, true, gate_kind, w_post != nullptr);
+        p = plan_of(m, es, tokens, width, true, gate_kind);
         e = dtype == ABS_F32 ? run_kind<float>(a, true, gate_kind, wide, p, s) : run_kind<bf16>(a, true, gate_kind, wide, p, s);
     }
     if (e == cudaSuccess)
-        e = launch_kernel(k_column_sums, dim3((unsigned)((width + 31) / 32), 3), 1024, 0, s, true, (const float*)a.part, p.grid, (int)width, dw_pre,
-                          dw_post, gate_kind == ABS_GATE_CHANNEL ? static_cast<float*>(dgate) : nullptr, accumulate);
+        e = launch_kernel(k_column_sums, dim3((unsigned)((width + 31) / 32), w_post || gate_kind == ABS_GATE_CHANNEL ? 2 : 1), 1024, 0, s, true,
+                          (const float*)a.part, p.grid, (int)width, dw_pre, dw_post, gate_kind == ABS_GATE_CHANNEL ? static_cast<float*>(dgate) : nullptr,
+                          w_post, gate_kind == ABS_GATE_CHANNEL ? static_cast<const float*>(gate) : nullptr, accumulate);
     return e == cudaSuccess ? ABS_OK : thread_error(ABS_ECUDA, cudaGetErrorString(e));
 }
