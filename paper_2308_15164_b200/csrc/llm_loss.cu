@@ -8,12 +8,14 @@
 
 #include "abs_internal.h"
 #include "abs_llm.h"
+#include "bulk_copy.cuh"
+#include "llm_status.cuh"
 #include "row_ops.cuh"
 
 namespace abs_sgd {
 namespace {
 
-constexpr int kStatCtasMax = 1024;   // CTAs that leave partial sums of the policy loss
+constexpr int kStatCtasMax = 2048;   // CTAs that leave partial sums of the policy loss
 constexpr float kLog2e = 1.4426950408889634f;
 
 // exp(z - m): the difference is rounded once, the base-2 exponential takes the rest (relative error about 2e-7 where
@@ -122,18 +124,24 @@ struct PolicyArgs {
 struct TokenLoss {
     float loss, kl, clipped, slope;   // slope: d loss / d logp; all without the token's weight
 };
-__device__ __forceinline__ TokenLoss token_loss(const PolicyArgs& a, size_t t, float logp) {
+struct TokenIn {
+    float adv, old, ref;
+};
+__device__ __forceinline__ TokenIn token_in(const PolicyArgs& a, size_t t) {
+    return TokenIn{a.adv[t], a.logp_old[t], a.logp_ref ? a.logp_ref[t] : 0.f};
+}
+__device__ __forceinline__ TokenLoss token_loss(const PolicyArgs& a, TokenIn in, float logp) {
     TokenLoss r{0.f, 0.f, 0.f, 0.f};
-    const float A = a.adv[t];
+    const float A = in.adv;
     if (A != 0.f) {      // the term is 0 there whatever the ratio is (exp may overflow for a token that counts for nothing)
-        const float ratio = expf(logp - a.logp_old[t]);
+        const float ratio = expf(logp - in.old);
         const bool up = A > 0.f && ratio > 1.f + a.clip_high, down = A < 0.f && ratio < 1.f - a.clip_low;
         r.loss = -(up ? 1.f + a.clip_high : down ? 1.f - a.clip_low : ratio) * A;
         r.slope = up || down ? 0.f : -ratio * A;
         r.clipped = up || down ? 1.f : 0.f;
     }
     if (a.logp_ref) {
-        const float d = a.logp_ref[t] - logp, e = expm1f(d);
+        const float d = in.ref - logp, e = expm1f(d);
         r.kl = e - d;
         r.loss += a.kl_coef * r.kl;
         r.slope -= a.kl_coef * e;
@@ -163,7 +171,7 @@ __global__ void __launch_bounds__(G * kGroups) k_policy_rows(PolicyArgs a) {
             st = row_stat<T, G>(row, a.V, tid, sh);
             if (st.m != -INFINITY || st.s != 0.f) {
                 logp = zy - st.m - logf(st.s);
-                const TokenLoss l = token_loss(a, t, logp);
+                const TokenLoss l = token_loss(a, token_in(a, t), logp);
                 g = w * l.slope;
                 if (tid == 0) {
                     acc[group][0] += (double)w * l.loss;
@@ -274,6 +282,15 @@ __global__ void __launch_bounds__(256) k_pref_pairs(PrefArgs a) {
     }
 }
 
+// The loss over all pairs; one warp.
+__device__ __forceinline__ void pref_total(const PrefArgs& a) {
+    double s = 0.0;
+    for (size_t p = threadIdx.x % 32; p < a.pairs; p += 32) s += (double)a.pair_loss[p];
+#pragma unroll
+    for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+    if (threadIdx.x % 32 == 0) a.stats[0] = (float)(s * (double)a.scale);
+}
+
 // The gradient of the rows; CTA 0 also adds up the loss.
 template <typename T, int G, int kGroups>
 __global__ void __launch_bounds__(G * kGroups) k_pref_grad(PrefArgs a) {
@@ -286,13 +303,307 @@ __global__ void __launch_bounds__(G * kGroups) k_pref_grad(PrefArgs a) {
             row_grad<T, G>(static_cast<const T*>(a.logits) + t * a.ld, static_cast<T*>(a.dlogits) + t * a.ld_d, a.V,
                            g == 0.f ? -1 : a.labels[t], g, RowStat{a.m[t], a.s[t]}, tid);
         }
-    if (blockIdx.x == 0 && threadIdx.x < 32) {
-        double s = 0.0;
-        for (size_t p = threadIdx.x; p < a.pairs; p += 32) s += (double)a.pair_loss[p];
+    if (blockIdx.x == 0 && threadIdx.x < 32) pref_total(a);
+}
+
+// ------------------------------------------------------------------------------------------------
+// Rows through a ring of chunks in shared memory.  A CTA takes rows b, b + G, ...; a producer warp keeps the ring full
+// (cp.async.bulk), kT consumer threads take a chunk as four 16-byte pieces each.  The gradient needs every number of a row
+// a second time, after its maximum and sum are known: the last kRing chunks of the row are then still in the ring, only what
+// came before them is loaded again (it is in L2).  Rows up to the ring's size are read once.
+// Rows of odd length start at every alignment: the chunks start at the row's first 16-byte boundary, the few elements in
+// front of it and behind the last whole piece are taken by one thread each with plain accesses; nothing outside a row is
+// touched.  logits and dlogits have to be aligned alike.
+// The chain from a row's last number to its first gradient (reductions, logarithm, the token's loss) leaves the memory idle,
+// so an SM holds 512 / kT CTAs whose rows are at different points.
+// Load number i of a row is chunk i, or chunk i - n beyond the first pass; slots are filled and freed in load order:
+//   first pass    loads 0 .. n - 1, of which those before n - kRing are freed at once
+//   second pass   loads n - kRing .. n - 1 from the ring, then loads n ..
+// ------------------------------------------------------------------------------------------------
+constexpr int kRing = 6;
+enum { kPolicy, kStats, kGrad };     // both passes with the policy loss between them; the first; the second
+
+template <int kT>
+struct RowsSmem {
+    alignas(128) uint8_t chunk[kRing][kT * 64];
+    float2 part[2][kT / 32];         // per warp: maximum, sum
+    float4 next[2];                  // m, -g / s, g, z_y of the row
+    alignas(8) uint64_t full[kRing];
+    uint64_t empty[kRing];
+};
+
+template <int kT>
+__device__ __forceinline__ void consumers_sync() { asm volatile("bar.sync 1, %0;" ::"n"(kT) : "memory"); }
+
+template <typename T>
+__device__ __forceinline__ float piece_max(const uint4 (&raw)[4], int n) {
+    float m = -INFINITY;
 #pragma unroll
-        for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-        if (threadIdx.x == 0) a.stats[0] = (float)(s * (double)a.scale);
+    for (int j = 0; j < 4; ++j)
+        if (j < n) {
+            const uint32_t w[4] = {raw[j].x, raw[j].y, raw[j].z, raw[j].w};
+            if (sizeof(T) == 4) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) m = fmaxf(m, __uint_as_float(w[i]));
+            } else {
+                __nv_bfloat162 b = *reinterpret_cast<const __nv_bfloat162*>(&w[0]);
+#pragma unroll
+                for (int i = 1; i < 4; ++i) b = __hmax2(b, *reinterpret_cast<const __nv_bfloat162*>(&w[i]));
+                m = fmaxf(m, fmaxf(__low2float(b), __high2float(b)));
+            }
+        }
+    return m;
+}
+
+struct RowArgs {
+    PolicyArgs p;
+    PrefArgs q;
+};
+
+template <typename T, int kT, int kMode>
+__global__ void __launch_bounds__(kT + 32, 512 / kT) k_rows(const __grid_constant__ RowArgs a) {
+    constexpr int kWarps = kT / 32, kChunk = kT * 64, kN = kPairs<T>;
+    extern __shared__ __align__(128) uint8_t smem_raw[];
+    RowsSmem<kT>& s = *reinterpret_cast<RowsSmem<kT>*>(smem_raw);
+    const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
+    const T* logits = static_cast<const T*>(kMode == kPolicy ? a.p.logits : a.q.logits);
+    T* dlogits = static_cast<T*>(kMode == kPolicy ? a.p.dlogits : kMode == kGrad ? a.q.dlogits : nullptr);
+    const size_t ld = kMode == kPolicy ? a.p.ld : a.q.ld, ld_d = kMode == kPolicy ? a.p.ld_d : a.q.ld_d;
+    const size_t rows = kMode == kPolicy ? a.p.T : a.q.T, G = gridDim.x;
+    const int V = kMode == kPolicy ? a.p.V : a.q.V;
+    const int32_t* labels = kMode == kPolicy ? a.p.labels : a.q.labels;
+    const bool second = kMode == kGrad || (kMode == kPolicy && dlogits != nullptr);
+    if (tid == 0) {
+        for (int i = 0; i < kRing; ++i) {
+            mbar_init(&s.full[i], 1);
+            mbar_init(&s.empty[i], kWarps);
+        }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
+    __syncthreads();
+    pdl_wait();
+    pdl_trigger();
+
+    // the gradient pass goes through the rows from the last to the first: the last ones read are the ones still in L2
+    auto row_of = [&](size_t k) { return kMode == kGrad ? rows - 1 - k : k; };
+    auto live_row = [&](size_t t) {                  // rows that are not are neither read nor waited for
+        if (kMode == kGrad) return a.q.g[t] != 0.f;
+        const int y = labels[t];
+        return y >= 0 && y < V && (kMode != kPolicy || a.p.weight[t] != 0.f);
+    };
+
+    if (warp == kWarps) {
+        if (lane == 0) {                             // ---- producer
+            int slot = 0;
+            uint32_t round = 0;
+            bool ok = true;
+            bool live = blockIdx.x < rows && live_row(row_of(blockIdx.x));
+            for (size_t k = blockIdx.x; k < rows && ok; k += G) {
+                const bool now = live;
+                live = k + G < rows && live_row(row_of(k + G));
+                if (!now) continue;
+                const T* row = logits + row_of(k) * ld;
+                const RowCut c = cut_row(row, V);
+                const uint32_t bytes = (uint32_t)c.pieces * 16u;
+                const int n = (int)((bytes + kChunk - 1) / kChunk);
+                const int loads = kMode == kPolicy && second && n > kRing ? 2 * n - kRing : n;
+                for (int i = 0; i < loads && ok; ++i) {
+                    const uint32_t at = (uint32_t)(i < n ? i : i - n) * kChunk, len = min((uint32_t)kChunk, bytes - at);
+                    if (round > 0 && !mbar_wait(&s.empty[slot], (round - 1) & 1)) { ok = false; break; }
+                    mbar_expect_tx(&s.full[slot], len);
+                    bulk_load(s.chunk[slot], reinterpret_cast<const uint8_t*>(row + c.head) + at, len, &s.full[slot]);
+                    if (++slot == kRing) { slot = 0; ++round; }
+                }
+            }
+            if (!ok) {
+                report_timeout();
+                for (int i = 0; i < kRing; ++i) mbar_wait(&s.full[i], (round + (i < slot ? 0 : 1)) & 1, 4096u);   // copies in flight
+            }
+        }
+        return;
+    }
+
+    // ---- consumers
+    int slot = 0;
+    uint32_t phase = 0;
+    bool ok = true;
+    double sums[3] = {0.0, 0.0, 0.0};                // thread 0: the policy loss's sums
+    int parity = 0;
+    // the next row's numbers are fetched while the current row is worked on
+    struct {
+        int y;
+        float w, g, m, s;            // policy: w; gradient pass: g, m, s
+        TokenIn in;                  // policy, thread 0
+    } now{}, next{};
+    auto fetch = [&](size_t k) {
+        if (k >= rows) return;
+        const size_t t = row_of(k);
+        next.y = labels[t];
+        if (kMode == kPolicy) {
+            next.w = a.p.weight[t];
+            if (tid == 0) next.in = token_in(a.p, t);
+        }
+        if (kMode == kGrad) {
+            next.g = a.q.g[t];
+            next.m = a.q.m[t];
+            next.s = a.q.s[t];
+        }
+    };
+    fetch(blockIdx.x);
+    for (size_t k = blockIdx.x; k < rows; k += G) {
+        now = next;
+        fetch(k + G);
+        const size_t t = row_of(k);
+        const T* row = logits + t * ld;
+        const int y = now.y;
+        const RowCut c = cut_row(row, V);
+        const int extra = tid < c.head ? tid : tid < c.head + c.tail ? V - c.tail + tid - c.head : -1;
+        float m = -INFINITY, mul = 0.f, g = 0.f, zy = 0.f;
+        const bool live = kMode == kGrad ? now.g != 0.f : y >= 0 && y < V && (kMode != kPolicy || now.w != 0.f);
+        float ex = 0.f;
+        if (live && extra >= 0) ex = to_f(row[extra]);
+        const int n = (int)(((uint32_t)c.pieces * 16u + kChunk - 1) / kChunk);
+        const int slot0 = slot;
+        if (kMode == kGrad) {
+            g = now.g;
+            m = now.m;
+            mul = -g / now.s;
+            if (live) zy = to_f(row[y]);
+        }
+        if (kMode != kGrad && live) {
+            if (tid == 0) zy = to_f(row[y]);
+            const int keep_from = second ? n - kRing : n;
+            float2 s2 = both(0.f);
+            for (int i = 0; i < n; ++i) {
+                if (!mbar_wait(&s.full[slot], phase, ok ? kSpinLimit : 1u)) ok = false;
+                uint4 raw[4];
+                const int first = i * (kT * 4) + tid, have = min(4, (c.pieces - first + kT - 1) / kT);
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (j < have) raw[j] = *reinterpret_cast<const uint4*>(s.chunk[slot] + (tid + j * kT) * 16);
+                const float cm = piece_max<T>(raw, have);
+                if (cm > m) {
+                    if (m != -INFINITY) {
+                        const float f = exp_diff(m, cm);
+                        s2 = mul2(s2, both(f));
+                    }
+                    m = cm;
+                }
+                const float ref = m == -INFINITY ? 0.f : -m;
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (j < have) {
+                        float2 z[kN];
+                        unpack(raw[j], z, T());
+#pragma unroll
+                        for (int e = 0; e < kN; ++e) s2 = add2(s2, exp2_of(mul2(add2(z[e], both(ref)), both(kLog2e))));
+                    }
+                if (i < keep_from) {
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&s.empty[slot]);
+                }
+                if (++slot == kRing) { slot = 0; phase ^= 1u; }
+            }
+            RowStat st{m, sum2(s2)};
+            if (extra >= 0) {
+                float z[1] = {ex};
+                stat_add(st, z);
+            }
+            // one pair per warp, joined by every warp that needs it
+            float wm = st.m;
+#pragma unroll
+            for (int o = 16; o; o >>= 1) wm = fmaxf(wm, __shfl_xor_sync(0xffffffffu, wm, o));
+            float ws = st.m == -INFINITY ? st.s : st.s * exp_diff(st.m, wm);
+#pragma unroll
+            for (int o = 16; o; o >>= 1) ws += __shfl_xor_sync(0xffffffffu, ws, o);
+            if (lane == 0) s.part[parity][warp] = make_float2(wm, ws);
+            consumers_sync<kT>();
+            if (tid == 0) {
+                RowStat all{-INFINITY, 0.f};
+                for (int w = 0; w < kWarps; ++w) all.m = fmaxf(all.m, s.part[parity][w].x);
+                for (int w = 0; w < kWarps; ++w) {
+                    const float2 p = s.part[parity][w];
+                    all.s += p.x == -INFINITY ? p.y : p.y * exp_diff(p.x, all.m);
+                }
+                const bool some = all.m != -INFINITY || all.s != 0.f;
+                const float logp = some ? zy - all.m - logf(all.s) : 0.f;
+                if (kMode == kPolicy) {
+                    if (some) {
+                        const float w = now.w;
+                        const TokenLoss l = token_loss(a.p, now.in, logp);
+                        g = w * l.slope;
+                        sums[0] += (double)w * l.loss;
+                        sums[1] += (double)w * l.kl;
+                        sums[2] += (double)w * l.clipped;
+                    }
+                    if (ok) a.p.logp[t] = logp;
+                    s.next[parity] = make_float4(all.m, some ? -g / all.s : 0.f, g, zy);
+                } else if (ok) {
+                    a.q.m[t] = all.m;
+                    a.q.s[t] = all.s;
+                    a.q.logp[t] = logp;
+                    a.q.g[t] = 0.f;
+                }
+            }
+            if (kMode == kPolicy && second) {
+                consumers_sync<kT>();
+                const float4 x = s.next[parity];
+                m = x.x; mul = x.y; g = x.z; zy = x.w;
+            }
+            parity ^= 1;
+        } else if (kMode != kGrad && tid == 0 && ok) {
+            if (kMode == kPolicy) a.p.logp[t] = 0.f;
+            else {
+                a.q.m[t] = -INFINITY;
+                a.q.s[t] = 0.f;
+                a.q.logp[t] = 0.f;
+                a.q.g[t] = 0.f;
+            }
+        }
+        if (!second) continue;
+        T* out = dlogits + t * ld_d;
+        if (!live) {
+            const RowCut o = cut_row(out, V);
+            for (int i = tid; i < o.pieces; i += kT) *reinterpret_cast<uint4*>(out + o.head + i * kVec<T>) = make_uint4(0u, 0u, 0u, 0u);
+            if (tid < o.head + o.tail) out[tid < o.head ? tid : V - o.tail + tid - o.head] = from_f<T>(0.f);
+            continue;
+        }
+        // g ([v = y] - exp(z_v - m) / s): the label's element is written once more by the thread that wrote its piece
+        const bool zero = g == 0.f;
+        const int resident = kMode == kGrad ? 0 : min(n, kRing);
+        int at = kMode == kGrad || n >= kRing ? slot : slot0;
+        for (int i = 0; i < n; ++i) {
+            const int chunk = kMode == kGrad ? i : i < resident ? n - resident + i : i - resident;
+            if (i >= resident) {
+                if (!mbar_wait(&s.full[slot], phase, ok ? kSpinLimit : 1u)) ok = false;
+                at = slot;
+                if (++slot == kRing) { slot = 0; phase ^= 1u; }
+            }
+            const int first = chunk * (kT * 4) + tid, have = min(4, (c.pieces - first + kT - 1) / kT);
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (j < have) {
+                    uint4 raw = *reinterpret_cast<const uint4*>(s.chunk[at] + (tid + j * kT) * 16);
+                    float2 z[kN];
+                    unpack(raw, z, T());
+#pragma unroll
+                    for (int e = 0; e < kN; ++e) z[e] = mul2(exp2_of(mul2(add2(z[e], both(-m)), both(kLog2e))), both(mul));
+                    raw = zero ? make_uint4(0u, 0u, 0u, 0u) : pack(z, T());
+                    if (ok) *reinterpret_cast<uint4*>(out + c.head + (first + j * kT) * kVec<T>) = raw;
+                }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&s.empty[at]);
+            if (++at == kRing) at = 0;
+        }
+        if (extra >= 0 && ok) out[extra] = from_f<T>(zero ? 0.f : exp_diff(ex, m) * mul);
+        const int in_body = y - c.head;
+        const int owner = in_body >= 0 && in_body < c.pieces * kVec<T> ? (in_body / kVec<T>) % kT : y < c.head ? y : y - (V - c.tail) + c.head;
+        if (tid == owner && !zero && ok) out[y] = from_f<T>(exp_diff(zy, m) * mul + g);
+    }
+    if (kMode == kGrad && blockIdx.x == 0 && warp == 0) pref_total(a.q);
+    if (kMode == kPolicy && tid == 0)
+        for (int i = 0; i < 3; ++i) a.p.part[(size_t)blockIdx.x * 3 + i] = sums[i];
+    if (!ok) report_timeout();
 }
 
 constexpr int kWarpRowMax = 1024;    // rows up to this length are taken by one warp each
@@ -303,14 +614,38 @@ int current_sms() {
     return sms;
 }
 
+// Consumer threads of a CTA of k_rows for rows of this many bytes: the smallest whose ring holds the row.
+int rows_threads(size_t bytes) { return bytes <= (size_t)kRing * 64 * 64 ? 64 : bytes <= (size_t)kRing * 128 * 64 ? 128 : 256; }
+// Rows t of both matrices start at the same offset from a 16-byte boundary, for every t.
+bool aligned_alike(const void* a, size_t ld_a, const void* b, size_t ld_b, size_t es) {
+    return (((uintptr_t)a - (uintptr_t)b) & 15) == 0 && ((ld_a - ld_b) * es & 15) == 0;
+}
+
+template <typename T, int kT, int kMode>
+cudaError_t launch_rows_of(const RowArgs& a, size_t rows, int sms, int* grid, cudaStream_t s) {
+    const size_t smem = sizeof(RowsSmem<kT>), most = (size_t)sms * (512 / kT);
+    *grid = (int)(rows < most ? rows : most);
+    const cudaError_t e = cudaFuncSetAttribute(k_rows<T, kT, kMode>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    return e != cudaSuccess ? e : launch_kernel(k_rows<T, kT, kMode>, *grid, kT + 32, smem, s, true, a);
+}
+template <typename T, int kMode>
+cudaError_t launch_rows(const RowArgs& a, size_t rows, int V, int sms, int* grid, cudaStream_t s) {
+    switch (rows_threads((size_t)V * sizeof(T))) {
+        case 64: return launch_rows_of<T, 64, kMode>(a, rows, sms, grid, s);
+        case 128: return launch_rows_of<T, 128, kMode>(a, rows, sms, grid, s);
+        default: return launch_rows_of<T, 256, kMode>(a, rows, sms, grid, s);
+    }
+}
+
 template <typename T>
 cudaError_t launch_policy(const PolicyArgs& a, float* stats, int sms, cudaStream_t s) {
-    const bool warp_rows = a.V <= kWarpRowMax;
+    const bool warp_rows = a.V <= kWarpRowMax, ring = !warp_rows && (!a.dlogits || aligned_alike(a.logits, a.ld, a.dlogits, a.ld_d, sizeof(T)));
     const size_t want = warp_rows ? (a.T + 7) / 8 : a.T;
-    const int grid = (int)(want < (size_t)(4 * sms) ? want : (size_t)(4 * sms));
+    int grid = (int)(want < (size_t)(4 * sms) ? want : (size_t)(4 * sms));
     cudaError_t e = cudaSuccess;
-    if (grid > 0)
-        e = warp_rows ? launch_kernel(k_policy_rows<T, 32, 8>, grid, 256, 0, s, true, a)
+    if (a.T > 0)
+        e = ring ? launch_rows<T, kPolicy>(RowArgs{a, PrefArgs{}}, a.T, a.V, sms, &grid, s)
+          : warp_rows ? launch_kernel(k_policy_rows<T, 32, 8>, grid, 256, 0, s, true, a)
                       : launch_kernel(k_policy_rows<T, 512, 1>, grid, 512, 0, s, true, a);
     if (e != cudaSuccess) return e;
     return launch_kernel(k_policy_stats, 1, 96, 0, s, true, (const double*)a.part, grid, stats);
@@ -318,18 +653,19 @@ cudaError_t launch_policy(const PolicyArgs& a, float* stats, int sms, cudaStream
 
 template <typename T>
 cudaError_t launch_pref(const PrefArgs& a, int sms, cudaStream_t s) {
-    const bool warp_rows = a.V <= kWarpRowMax;
+    const bool warp_rows = a.V <= kWarpRowMax, ring = !warp_rows && a.dlogits && aligned_alike(a.logits, a.ld, a.dlogits, a.ld_d, sizeof(T));
     const size_t want = warp_rows ? (a.T + 7) / 8 : a.T;
     const int grid = (int)(want < (size_t)(4 * sms) ? want : (size_t)(4 * sms));
+    int unused = 0;
     cudaError_t e = cudaSuccess;
-    if (grid > 0)
-        e = warp_rows ? launch_kernel(k_pref_stats<T, 32, 8>, grid, 256, 0, s, true, a)
-                      : launch_kernel(k_pref_stats<T, 512, 1>, grid, 512, 0, s, true, a);
+    if (a.T > 0)
+        e = warp_rows ? launch_kernel(k_pref_stats<T, 32, 8>, grid, 256, 0, s, true, a) : launch_rows<T, kStats>(RowArgs{PolicyArgs{}, a}, a.T, a.V, sms, &unused, s);
     if (e != cudaSuccess) return e;
     if (a.pairs > 0) {
         e = launch_kernel(k_pref_pairs, (int)(a.pairs < (size_t)sms ? a.pairs : (size_t)sms), 256, 0, s, true, a);
         if (e != cudaSuccess) return e;
     }
+    if (ring && a.T > 0) return launch_rows<T, kGrad>(RowArgs{PolicyArgs{}, a}, a.T, a.V, sms, &unused, s);
     const int g2 = a.dlogits && grid > 0 ? grid : 1;
     return warp_rows ? launch_kernel(k_pref_grad<T, 32, 8>, g2, 256, 0, s, true, a)
                      : launch_kernel(k_pref_grad<T, 512, 1>, g2, 512, 0, s, true, a);
@@ -353,6 +689,10 @@ const char* check_logits(const void* logits, uint32_t dtype, uint64_t T, uint64_
 size_t up256(size_t n) { return (n + 255) / 256 * 256; }
 
 }  // namespace
+}  // namespace abs_sgd
+
+namespace abs_sgd {
+cudaError_t take_status_loss(int* status, cudaStream_t s) { return take_status(status, s); }
 }  // namespace abs_sgd
 
 using namespace abs_sgd;

@@ -25,5 +25,6 @@ static inline cudaError_t take_status(int* status, cudaStream_t s) {
 }
 
 cudaError_t take_status_norm(int* status, cudaStream_t s);    // llm_norm.cu
+cudaError_t take_status_loss(int* status, cudaStream_t s);    // llm_loss.cu
 
 }  // namespace abs_sgd

@@ -61,6 +61,59 @@ struct Pack<bf16, 8> {
 template <typename T>
 constexpr int kVec = 16 / (int)sizeof(T);   // elements of a 16-byte piece
 
+// Pairs of fp32 in one 64-bit register (fma.rn.f32x2 and its kin round like the scalar instructions).
+__device__ __forceinline__ uint64_t as_u64(float2 v) { return *reinterpret_cast<uint64_t*>(&v); }
+__device__ __forceinline__ float2 as_f2(uint64_t v) { return *reinterpret_cast<float2*>(&v); }
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(as_u64(a)), "l"(as_u64(b)), "l"(as_u64(c)));
+    return as_f2(r);
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(as_u64(a)), "l"(as_u64(b)));
+    return as_f2(r);
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(as_u64(a)), "l"(as_u64(b)));
+    return as_f2(r);
+}
+__device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
+__device__ __forceinline__ float sum2(float2 v) { return v.x + v.y; }
+
+// A 16-byte piece as kVec / 2 pairs.
+template <typename T>
+constexpr int kPairs = kVec<T> / 2;
+__device__ __forceinline__ void unpack(uint4 a, float2 (&v)[2], float) {
+    v[0] = make_float2(__uint_as_float(a.x), __uint_as_float(a.y));
+    v[1] = make_float2(__uint_as_float(a.z), __uint_as_float(a.w));
+}
+__device__ __forceinline__ void unpack(uint4 a, float2 (&v)[4], bf16) {
+    const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = make_float2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xFFFF0000u));
+}
+__device__ __forceinline__ uint4 pack(const float2 (&v)[2], float) {
+    return make_uint4(__float_as_uint(v[0].x), __float_as_uint(v[0].y), __float_as_uint(v[1].x), __float_as_uint(v[1].y));
+}
+__device__ __forceinline__ uint4 pack(const float2 (&v)[4], bf16) {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const __nv_bfloat162 b = __float22bfloat162_rn(v[i]);
+        w[i] = *reinterpret_cast<const uint32_t*>(&b);
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+// 2^v of both numbers by the approximate unit (relative error 2^-22; results below the normal range become 0).
+__device__ __forceinline__ float2 exp2_of(float2 v) {
+    float2 r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r.x) : "f"(v.x));
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r.y) : "f"(v.y));
+    return r;
+}
+
 // A row cut into single elements up to the first 16-byte boundary, 16-byte pieces, and single elements behind the last.
 struct RowCut {
     int head, pieces, tail;
