@@ -18,13 +18,26 @@ namespace {
 constexpr int kStatCtasMax = 2048;   // CTAs that leave partial sums of the policy loss
 constexpr float kLog2e = 1.4426950408889634f;
 
-// exp(z - m): the difference is rounded once, the base-2 exponential takes the rest (relative error about 2e-7 where
-// the result is not negligible beside exp(0)).  m is finite.
-__device__ __forceinline__ float exp_diff(float z, float m) { return exp2f((z - m) * kLog2e); }
+// exp(z - m) as 2^(a z - m2) with m2 = a m rounded, one fused multiply-add and the approximate base-2 unit (relative error
+// about 2e-7 where the result is not negligible beside 1).  The rounding of m2 is common to all that is computed with one
+// m, and a change of m is a factor 2^(m2 - m2'), so that it cancels in every quotient.  a = log2 e; for |m| > 1e30, where a m
+// may overflow, z - m is 0 or beyond any exponent, and a = 1 does.  m = -inf (nothing above -inf yet): a = 1, m2 = 0.
+struct Base {
+    float a, m2;
+};
+__device__ __forceinline__ Base base_of(float m) {
+    const float a = fabsf(m) > 1e30f ? 1.f : kLog2e;
+    return Base{a, m == -INFINITY ? 0.f : a * m};
+}
+__device__ __forceinline__ float exp_at(float z, Base b) { return exp2_of(fmaf(z, b.a, -b.m2)); }
+__device__ __forceinline__ float2 exp_at(float2 z, Base b) { return exp2_of(fma2(z, both(b.a), both(-b.m2))); }
 
 struct RowStat {
     float m, s;      // largest element; sum of exp(z - m).  m = -inf: no element is above -inf
 };
+
+// The sum of `a`, relative to a maximum m >= a.m (where a.m = -inf it is 0, or NaN from NaN elements).
+__device__ __forceinline__ float at_max(RowStat a, float m) { return a.m == -INFINITY ? a.s : a.s * exp2_of(base_of(a.m).m2 - base_of(m).m2); }
 
 template <int G>
 __device__ __forceinline__ RowStat group_stat(RowStat a, float* sh) {
@@ -41,7 +54,7 @@ __device__ __forceinline__ RowStat group_stat(RowStat a, float* sh) {
 #pragma unroll
         for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
     }
-    float v[1] = {a.m == -INFINITY ? a.s : a.s * exp_diff(a.m, m)};   // a.s is 0 there, or NaN from NaN elements
+    float v[1] = {at_max(a, m)};
     group_sum<G, 1>(v, sh);
     return RowStat{m, v[0]};
 }
@@ -53,12 +66,12 @@ __device__ __forceinline__ void stat_add(RowStat& a, const float (&z)[N]) {
 #pragma unroll
     for (int i = 1; i < N; ++i) m = fmaxf(m, z[i]);
     if (m > a.m) {
-        a.s = a.m == -INFINITY ? a.s : a.s * exp_diff(a.m, m);
+        a.s = at_max(a, m);
         a.m = m;
     }
-    const float ref = a.m == -INFINITY ? 0.f : a.m;
+    const Base b = base_of(a.m);
 #pragma unroll
-    for (int i = 0; i < N; ++i) a.s += exp_diff(z[i], ref);
+    for (int i = 0; i < N; ++i) a.s += exp_at(z[i], b);
 }
 
 template <typename T, int G>
@@ -81,11 +94,12 @@ __device__ __forceinline__ RowStat row_stat(const T* row, int V, int tid, float*
 template <typename T, int G>
 __device__ __forceinline__ void row_grad(const T* row, T* out, int V, int y, float g, RowStat st, int tid) {
     const float c = -g / st.s;
+    const Base b = base_of(st.m);
     const bool zero = g == 0.f;
     const RowCut o = cut_row(out, V);
     const bool same = cut_row(row, V).head == o.head;    // the pieces of row and out are aligned alike
     auto one = [&](int v) {
-        float d = zero ? 0.f : exp_diff(to_f(row[v]), st.m) * c;
+        float d = zero ? 0.f : exp_at(to_f(row[v]), b) * c;
         if (v == y) d += g;
         out[v] = from_f<T>(d);
     };
@@ -99,7 +113,7 @@ __device__ __forceinline__ void row_grad(const T* row, T* out, int V, int y, flo
             } else {
                 Pack<T, kVec<T>>::load(row + v0, z);
 #pragma unroll
-                for (int k = 0; k < kVec<T>; ++k) z[k] = exp_diff(z[k], st.m) * c + (v0 + k == y ? g : 0.f);
+                for (int k = 0; k < kVec<T>; ++k) z[k] = exp_at(z[k], b) * c + (v0 + k == y ? g : 0.f);
             }
             Pack<T, kVec<T>>::store(out + v0, z);
         }
@@ -335,24 +349,54 @@ struct RowsSmem {
 template <int kT>
 __device__ __forceinline__ void consumers_sync() { asm volatile("bar.sync 1, %0;" ::"n"(kT) : "memory"); }
 
-template <typename T>
-__device__ __forceinline__ float piece_max(const uint4 (&raw)[4], int n) {
-    float m = -INFINITY;
+__device__ __forceinline__ float piece_max(uint4 r, float m, float) {
+    return fmaxf(fmaxf(fmaxf(m, __uint_as_float(r.x)), fmaxf(__uint_as_float(r.y), __uint_as_float(r.z))), __uint_as_float(r.w));
+}
+__device__ __forceinline__ float piece_max(uint4 r, float m, bf16) {
+    const auto as2 = [](uint32_t v) { return *reinterpret_cast<const __nv_bfloat162*>(&v); };
+    const __nv_bfloat162 b = __hmax2(__hmax2(as2(r.x), as2(r.y)), __hmax2(as2(r.z), as2(r.w)));
+    return fmaxf(fmaxf(m, __low2float(b)), __high2float(b));
+}
+
+// A thread's pieces of one chunk into its running maximum and sum (two halves); kFull: all four are there.
+template <typename T, int kT, bool kFull>
+__device__ __forceinline__ void chunk_stat(const uint8_t* chunk, int tid, int have, float& m, float2& s2) {
+    uint4 raw[4];
+    float cm = m;
 #pragma unroll
     for (int j = 0; j < 4; ++j)
-        if (j < n) {
-            const uint32_t w[4] = {raw[j].x, raw[j].y, raw[j].z, raw[j].w};
-            if (sizeof(T) == 4) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) m = fmaxf(m, __uint_as_float(w[i]));
-            } else {
-                __nv_bfloat162 b = *reinterpret_cast<const __nv_bfloat162*>(&w[0]);
-#pragma unroll
-                for (int i = 1; i < 4; ++i) b = __hmax2(b, *reinterpret_cast<const __nv_bfloat162*>(&w[i]));
-                m = fmaxf(m, fmaxf(__low2float(b), __high2float(b)));
-            }
+        if (kFull || j < have) {
+            raw[j] = *reinterpret_cast<const uint4*>(chunk + (tid + j * kT) * 16);
+            cm = piece_max(raw[j], cm, T());
         }
-    return m;
+    if (cm > m) {
+        if (m != -INFINITY) s2 = mul2(s2, both(exp2_of(base_of(m).m2 - base_of(cm).m2)));
+        m = cm;
+    }
+    const Base b = base_of(m);
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        if (kFull || j < have) {
+            float2 z[kPairs<T>];
+            unpack(raw[j], z, T());
+#pragma unroll
+            for (int e = 0; e < kPairs<T>; ++e) s2 = add2(s2, exp_at(z[e], b));
+        }
+}
+// Its pieces of the gradient, to `out` (the chunk's first element in memory).
+template <typename T, int kT, bool kFull>
+__device__ __forceinline__ void chunk_grad(const uint8_t* chunk, T* out, int tid, int have, Base b, float mul, bool zero, bool ok) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        if (kFull || j < have) {
+            uint4 raw = *reinterpret_cast<const uint4*>(chunk + (tid + j * kT) * 16);
+            float2 z[kPairs<T>];
+            unpack(raw, z, T());
+#pragma unroll
+            for (int e = 0; e < kPairs<T>; ++e) z[e] = mul2(exp_at(z[e], b), both(mul));
+            raw = zero ? make_uint4(0u, 0u, 0u, 0u) : pack(z, T());
+            if (ok) reinterpret_cast<uint4*>(out)[tid + j * kT] = raw;
+        }
 }
 
 struct RowArgs {
@@ -476,28 +520,9 @@ __global__ void __launch_bounds__(kT + 32, 512 / kT) k_rows(const __grid_constan
             float2 s2 = both(0.f);
             for (int i = 0; i < n; ++i) {
                 if (!mbar_wait(&s.full[slot], phase, ok ? kSpinLimit : 1u)) ok = false;
-                uint4 raw[4];
-                const int first = i * (kT * 4) + tid, have = min(4, (c.pieces - first + kT - 1) / kT);
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    if (j < have) raw[j] = *reinterpret_cast<const uint4*>(s.chunk[slot] + (tid + j * kT) * 16);
-                const float cm = piece_max<T>(raw, have);
-                if (cm > m) {
-                    if (m != -INFINITY) {
-                        const float f = exp_diff(m, cm);
-                        s2 = mul2(s2, both(f));
-                    }
-                    m = cm;
-                }
-                const float ref = m == -INFINITY ? 0.f : -m;
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    if (j < have) {
-                        float2 z[kN];
-                        unpack(raw[j], z, T());
-#pragma unroll
-                        for (int e = 0; e < kN; ++e) s2 = add2(s2, exp2_of(mul2(add2(z[e], both(ref)), both(kLog2e))));
-                    }
+                const int left = c.pieces - i * (kT * 4);
+                if (left >= kT * 4) chunk_stat<T, kT, true>(s.chunk[slot], tid, 4, m, s2);
+                else chunk_stat<T, kT, false>(s.chunk[slot], tid, (left - tid + kT - 1) / kT, m, s2);
                 if (i < keep_from) {
                     __syncwarp();
                     if (lane == 0) mbar_arrive(&s.empty[slot]);
@@ -513,7 +538,7 @@ __global__ void __launch_bounds__(kT + 32, 512 / kT) k_rows(const __grid_constan
             float wm = st.m;
 #pragma unroll
             for (int o = 16; o; o >>= 1) wm = fmaxf(wm, __shfl_xor_sync(0xffffffffu, wm, o));
-            float ws = st.m == -INFINITY ? st.s : st.s * exp_diff(st.m, wm);
+            float ws = at_max(st, wm);
 #pragma unroll
             for (int o = 16; o; o >>= 1) ws += __shfl_xor_sync(0xffffffffu, ws, o);
             if (lane == 0) s.part[parity][warp] = make_float2(wm, ws);
@@ -523,7 +548,7 @@ __global__ void __launch_bounds__(kT + 32, 512 / kT) k_rows(const __grid_constan
                 for (int w = 0; w < kWarps; ++w) all.m = fmaxf(all.m, s.part[parity][w].x);
                 for (int w = 0; w < kWarps; ++w) {
                     const float2 p = s.part[parity][w];
-                    all.s += p.x == -INFINITY ? p.y : p.y * exp_diff(p.x, all.m);
+                    all.s += at_max(RowStat{p.x, p.y}, all.m);
                 }
                 const bool some = all.m != -INFINITY || all.s != 0.f;
                 const float logp = some ? zy - all.m - logf(all.s) : 0.f;
@@ -570,6 +595,7 @@ __global__ void __launch_bounds__(kT + 32, 512 / kT) k_rows(const __grid_constan
         }
         // g ([v = y] - exp(z_v - m) / s): the label's element is written once more by the thread that wrote its piece
         const bool zero = g == 0.f;
+        const Base base = base_of(m);
         const int resident = kMode == kGrad ? 0 : min(n, kRing);
         int at = kMode == kGrad || n >= kRing ? slot : slot0;
         for (int i = 0; i < n; ++i) {
@@ -579,26 +605,18 @@ __global__ void __launch_bounds__(kT + 32, 512 / kT) k_rows(const __grid_constan
                 at = slot;
                 if (++slot == kRing) { slot = 0; phase ^= 1u; }
             }
-            const int first = chunk * (kT * 4) + tid, have = min(4, (c.pieces - first + kT - 1) / kT);
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                if (j < have) {
-                    uint4 raw = *reinterpret_cast<const uint4*>(s.chunk[at] + (tid + j * kT) * 16);
-                    float2 z[kN];
-                    unpack(raw, z, T());
-#pragma unroll
-                    for (int e = 0; e < kN; ++e) z[e] = mul2(exp2_of(mul2(add2(z[e], both(-m)), both(kLog2e))), both(mul));
-                    raw = zero ? make_uint4(0u, 0u, 0u, 0u) : pack(z, T());
-                    if (ok) *reinterpret_cast<uint4*>(out + c.head + (first + j * kT) * kVec<T>) = raw;
-                }
+            const int left = c.pieces - chunk * (kT * 4);
+            T* to = out + c.head + (size_t)chunk * (kT * 4 * kVec<T>);
+            if (left >= kT * 4) chunk_grad<T, kT, true>(s.chunk[at], to, tid, 4, base, mul, zero, ok);
+            else chunk_grad<T, kT, false>(s.chunk[at], to, tid, (left - tid + kT - 1) / kT, base, mul, zero, ok);
             __syncwarp();
             if (lane == 0) mbar_arrive(&s.empty[at]);
             if (++at == kRing) at = 0;
         }
-        if (extra >= 0 && ok) out[extra] = from_f<T>(zero ? 0.f : exp_diff(ex, m) * mul);
+        if (extra >= 0 && ok) out[extra] = from_f<T>(zero ? 0.f : exp_at(ex, base) * mul);
         const int in_body = y - c.head;
         const int owner = in_body >= 0 && in_body < c.pieces * kVec<T> ? (in_body / kVec<T>) % kT : y < c.head ? y : y - (V - c.tail) + c.head;
-        if (tid == owner && !zero && ok) out[y] = from_f<T>(exp_diff(zy, m) * mul + g);
+        if (tid == owner && !zero && ok) out[y] = from_f<T>(exp_at(zy, base) * mul + g);
     }
     if (kMode == kGrad && blockIdx.x == 0 && warp == 0) pref_total(a.q);
     if (kMode == kPolicy && tid == 0)

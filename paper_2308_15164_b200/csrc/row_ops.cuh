@@ -106,13 +106,13 @@ __device__ __forceinline__ uint4 pack(const float2 (&v)[4], bf16) {
     }
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
-// 2^v of both numbers by the approximate unit (relative error 2^-22; results below the normal range become 0).
-__device__ __forceinline__ float2 exp2_of(float2 v) {
-    float2 r;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r.x) : "f"(v.x));
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r.y) : "f"(v.y));
+// 2^v by the approximate unit (relative error 2^-22; results below the normal range become 0).
+__device__ __forceinline__ float exp2_of(float v) {
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
     return r;
 }
+__device__ __forceinline__ float2 exp2_of(float2 v) { return make_float2(exp2_of(v.x), exp2_of(v.y)); }
 
 // A row cut into single elements up to the first 16-byte boundary, 16-byte pieces, and single elements behind the last.
 struct RowCut {
