@@ -36,23 +36,25 @@ struct RowStat {
     float m, s;      // largest element; sum of exp(z - m).  m = -inf: no element is above -inf
 };
 
+// Maximum over a warp (NaN is left out).
+__device__ __forceinline__ float warp_max(float v) {
+    float r;
+    asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
+    return r;
+}
 // The sum of `a`, relative to a maximum m >= a.m (where a.m = -inf it is 0, or NaN from NaN elements).
 __device__ __forceinline__ float at_max(RowStat a, float m) { return a.m == -INFINITY ? a.s : a.s * exp2_of(base_of(a.m).m2 - base_of(m).m2); }
 
 template <int G>
 __device__ __forceinline__ RowStat group_stat(RowStat a, float* sh) {
-    float m = a.m;
-#pragma unroll
-    for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    float m = warp_max(a.m);
     if (G > 32) {
         constexpr int kWarps = G / 32;
         const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
         __syncthreads();
         if (lane == 0) sh[warp] = m;
         __syncthreads();
-        m = lane < kWarps ? sh[lane] : -INFINITY;
-#pragma unroll
-        for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+        m = warp_max(lane < kWarps ? sh[lane] : -INFINITY);
     }
     float v[1] = {at_max(a, m)};
     group_sum<G, 1>(v, sh);
@@ -322,24 +324,26 @@ __global__ void __launch_bounds__(G * kGroups) k_pref_grad(PrefArgs a) {
 
 // ------------------------------------------------------------------------------------------------
 // Rows through a ring of chunks in shared memory.  A CTA takes rows b, b + G, ...; a producer warp keeps the ring full
-// (cp.async.bulk), kT consumer threads take a chunk as four 16-byte pieces each.  The gradient needs every number of a row
+// (cp.async.bulk), kT consumer threads take a chunk as kU 16-byte pieces each.  The gradient needs every number of a row
 // a second time, after its maximum and sum are known: the last kRing chunks of the row are then still in the ring, only what
 // came before them is loaded again (it is in L2).  Rows up to the ring's size are read once.
 // Rows of odd length start at every alignment: the chunks start at the row's first 16-byte boundary, the few elements in
 // front of it and behind the last whole piece are taken by one thread each with plain accesses; nothing outside a row is
 // touched.  logits and dlogits have to be aligned alike.
 // The chain from a row's last number to its first gradient (reductions, logarithm, the token's loss) leaves the memory idle,
-// so an SM holds 512 / kT CTAs whose rows are at different points.
+// so an SM holds kRowThreads / kT CTAs whose rows are at different points.
 // Load number i of a row is chunk i, or chunk i - n beyond the first pass; slots are filled and freed in load order:
 //   first pass    loads 0 .. n - 1, of which those before n - kRing are freed at once
 //   second pass   loads n - kRing .. n - 1 from the ring, then loads n ..
 // ------------------------------------------------------------------------------------------------
 constexpr int kRing = 6;
+constexpr int kRowThreads = 512;     // consumer threads of an SM
 enum { kPolicy, kStats, kGrad };     // both passes with the policy loss between them; the first; the second
 
+constexpr int kU = 4;
 template <int kT>
 struct RowsSmem {
-    alignas(128) uint8_t chunk[kRing][kT * 64];
+    alignas(128) uint8_t chunk[kRing][kT * kU * 16];
     float2 part[2][kT / 32];         // per warp: maximum, sum
     float4 next[2];                  // m, -g / s, g, z_y of the row
     alignas(8) uint64_t full[kRing];
@@ -358,13 +362,13 @@ __device__ __forceinline__ float piece_max(uint4 r, float m, bf16) {
     return fmaxf(fmaxf(m, __low2float(b)), __high2float(b));
 }
 
-// A thread's pieces of one chunk into its running maximum and sum (two halves); kFull: all four are there.
+// A thread's pieces of one chunk into its running maximum and sum (two halves); kFull: all of them are there.
 template <typename T, int kT, bool kFull>
 __device__ __forceinline__ void chunk_stat(const uint8_t* chunk, int tid, int have, float& m, float2& s2) {
-    uint4 raw[4];
+    uint4 raw[kU];
     float cm = m;
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
+    for (int j = 0; j < kU; ++j)
         if (kFull || j < have) {
             raw[j] = *reinterpret_cast<const uint4*>(chunk + (tid + j * kT) * 16);
             cm = piece_max(raw[j], cm, T());
@@ -375,7 +379,7 @@ __device__ __forceinline__ void chunk_stat(const uint8_t* chunk, int tid, int ha
     }
     const Base b = base_of(m);
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
+    for (int j = 0; j < kU; ++j)
         if (kFull || j < have) {
             float2 z[kPairs<T>];
             unpack(raw[j], z, T());
@@ -387,7 +391,7 @@ __device__ __forceinline__ void chunk_stat(const uint8_t* chunk, int tid, int ha
 template <typename T, int kT, bool kFull>
 __device__ __forceinline__ void chunk_grad(const uint8_t* chunk, T* out, int tid, int have, Base b, float mul, bool zero, bool ok) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
+    for (int j = 0; j < kU; ++j)
         if (kFull || j < have) {
             uint4 raw = *reinterpret_cast<const uint4*>(chunk + (tid + j * kT) * 16);
             float2 z[kPairs<T>];
@@ -405,8 +409,8 @@ struct RowArgs {
 };
 
 template <typename T, int kT, int kMode>
-__global__ void __launch_bounds__(kT + 32, 512 / kT) k_rows(const __grid_constant__ RowArgs a) {
-    constexpr int kWarps = kT / 32, kChunk = kT * 64, kN = kPairs<T>;
+__global__ void __launch_bounds__(kT + 32, kRowThreads / kT) k_rows(const __grid_constant__ RowArgs a) {
+    constexpr int kWarps = kT / 32, kChunk = kT * kU * 16;
     extern __shared__ __align__(128) uint8_t smem_raw[];
     RowsSmem<kT>& s = *reinterpret_cast<RowsSmem<kT>*>(smem_raw);
     const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
@@ -520,8 +524,8 @@ __global__ void __launch_bounds__(kT + 32, 512 / kT) k_rows(const __grid_constan
             float2 s2 = both(0.f);
             for (int i = 0; i < n; ++i) {
                 if (!mbar_wait(&s.full[slot], phase, ok ? kSpinLimit : 1u)) ok = false;
-                const int left = c.pieces - i * (kT * 4);
-                if (left >= kT * 4) chunk_stat<T, kT, true>(s.chunk[slot], tid, 4, m, s2);
+                const int left = c.pieces - i * (kT * kU);
+                if (left >= kT * kU) chunk_stat<T, kT, true>(s.chunk[slot], tid, kU, m, s2);
                 else chunk_stat<T, kT, false>(s.chunk[slot], tid, (left - tid + kT - 1) / kT, m, s2);
                 if (i < keep_from) {
                     __syncwarp();
@@ -535,39 +539,39 @@ __global__ void __launch_bounds__(kT + 32, 512 / kT) k_rows(const __grid_constan
                 stat_add(st, z);
             }
             // one pair per warp, joined by every warp that needs it
-            float wm = st.m;
-#pragma unroll
-            for (int o = 16; o; o >>= 1) wm = fmaxf(wm, __shfl_xor_sync(0xffffffffu, wm, o));
+            const float wm = warp_max(st.m);
             float ws = at_max(st, wm);
 #pragma unroll
             for (int o = 16; o; o >>= 1) ws += __shfl_xor_sync(0xffffffffu, ws, o);
             if (lane == 0) s.part[parity][warp] = make_float2(wm, ws);
             consumers_sync<kT>();
-            if (tid == 0) {
-                RowStat all{-INFINITY, 0.f};
-                for (int w = 0; w < kWarps; ++w) all.m = fmaxf(all.m, s.part[parity][w].x);
-                for (int w = 0; w < kWarps; ++w) {
-                    const float2 p = s.part[parity][w];
-                    all.s += at_max(RowStat{p.x, p.y}, all.m);
-                }
-                const bool some = all.m != -INFINITY || all.s != 0.f;
-                const float logp = some ? zy - all.m - logf(all.s) : 0.f;
-                if (kMode == kPolicy) {
-                    if (some) {
-                        const float w = now.w;
-                        const TokenLoss l = token_loss(a.p, now.in, logp);
-                        g = w * l.slope;
-                        sums[0] += (double)w * l.loss;
-                        sums[1] += (double)w * l.kl;
-                        sums[2] += (double)w * l.clipped;
+            if (warp == 0) {
+                const float2 p = lane < kWarps ? s.part[parity][lane] : make_float2(-INFINITY, 0.f);
+                RowStat all{p.x, 0.f};
+                all.m = warp_max(all.m);
+                all.s = at_max(RowStat{p.x, p.y}, all.m);
+#pragma unroll
+                for (int o = kWarps / 2; o; o >>= 1) all.s += __shfl_xor_sync(0xffffffffu, all.s, o);
+                if (lane == 0) {
+                    const bool some = all.m != -INFINITY || all.s != 0.f;
+                    const float logp = some ? zy - all.m - logf(all.s) : 0.f;
+                    if (kMode == kPolicy) {
+                        if (some) {
+                            const float w = now.w;
+                            const TokenLoss l = token_loss(a.p, now.in, logp);
+                            g = w * l.slope;
+                            sums[0] += (double)w * l.loss;
+                            sums[1] += (double)w * l.kl;
+                            sums[2] += (double)w * l.clipped;
+                        }
+                        if (ok) a.p.logp[t] = logp;
+                        s.next[parity] = make_float4(all.m, some ? -g / all.s : 0.f, g, zy);
+                    } else if (ok) {
+                        a.q.m[t] = all.m;
+                        a.q.s[t] = all.s;
+                        a.q.logp[t] = logp;
+                        a.q.g[t] = 0.f;
                     }
-                    if (ok) a.p.logp[t] = logp;
-                    s.next[parity] = make_float4(all.m, some ? -g / all.s : 0.f, g, zy);
-                } else if (ok) {
-                    a.q.m[t] = all.m;
-                    a.q.s[t] = all.s;
-                    a.q.logp[t] = logp;
-                    a.q.g[t] = 0.f;
                 }
             }
             if (kMode == kPolicy && second) {
@@ -605,9 +609,9 @@ __global__ void __launch_bounds__(kT + 32, 512 / kT) k_rows(const __grid_constan
                 at = slot;
                 if (++slot == kRing) { slot = 0; phase ^= 1u; }
             }
-            const int left = c.pieces - chunk * (kT * 4);
-            T* to = out + c.head + (size_t)chunk * (kT * 4 * kVec<T>);
-            if (left >= kT * 4) chunk_grad<T, kT, true>(s.chunk[at], to, tid, 4, base, mul, zero, ok);
+            const int left = c.pieces - chunk * (kT * kU);
+            T* to = out + c.head + (size_t)chunk * (kT * kU * kVec<T>);
+            if (left >= kT * kU) chunk_grad<T, kT, true>(s.chunk[at], to, tid, kU, base, mul, zero, ok);
             else chunk_grad<T, kT, false>(s.chunk[at], to, tid, (left - tid + kT - 1) / kT, base, mul, zero, ok);
             __syncwarp();
             if (lane == 0) mbar_arrive(&s.empty[at]);
@@ -624,6 +628,275 @@ __global__ void __launch_bounds__(kT + 32, 512 / kT) k_rows(const __grid_constan
     if (!ok) report_timeout();
 }
 
+// ------------------------------------------------------------------------------------------------
+// The policy loss with a row's exponentials kept in registers.  A row is taken by a cluster of C CTAs (C = 1 where one CTA
+// can own it), kT threads each, a thread owning up to eight 16-byte pieces: exp(z - m) is formed once, when the element
+// arrives, and scaled when the row's sum is known.  (Forming it twice makes the exponential unit as busy as the memory:
+// 103 us for 4096 rows of 32768 bf16.)  A CTA's slices of the next rows are copied into shared memory meanwhile, so that the
+// memory stays busy through the row's chain -- reductions, the exchange of the cluster's partial sums, the token's loss.
+// No warp of its own issues the copies: registers are given to whole groups of four warps, and the exponentials need them.
+// The CTAs of a cluster exchange (maximum, sum) by st.async into each other's shared memory.
+// Few rows: larger clusters, so that all SMs have a part.
+// ------------------------------------------------------------------------------------------------
+constexpr int kOwnPieces = 8;
+constexpr int kClusterMax = 8;
+constexpr int kStagesMax = 8;
+constexpr int kSliceThreads = 512;           // threads of an SM
+
+struct SliceCtl {
+    float2 part[2][16];              // per warp: maximum, sum
+    float2 peer[2][kClusterMax];     // per CTA of the cluster
+    float4 next[2];                  // m, -g / s, g, z_y of the row
+    float zy[2];
+    alignas(8) uint64_t full[kStagesMax];
+    uint64_t peers[2];
+};
+constexpr size_t kSliceCtl = (sizeof(SliceCtl) + 127) / 128 * 128;
+
+__device__ __forceinline__ uint32_t cluster_rank() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// 8 bytes to the same variable of CTA `rank`, counted on the same barrier there.
+__device__ __forceinline__ void send(float2* var, uint64_t* bar, uint32_t rank, float2 v) {
+    uint32_t a, b;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_u32(var)), "r"(rank));
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(b) : "r"(smem_u32(bar)), "r"(rank));
+    asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.b64 [%0], %1, [%2];" ::"r"(a), "l"(as_u64(v)), "r"(b) : "memory");
+}
+__device__ __forceinline__ bool mbar_wait_cluster(uint64_t* bar, uint32_t parity, uint32_t limit) {
+    for (uint32_t it = 0; it < limit; ++it) {
+        uint32_t ok;
+        asm volatile(
+            "{\n .reg .pred p;\n mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}\n"
+            : "=r"(ok) : "r"(smem_u32(bar)), "r"(parity) : "memory");
+        if (ok) return true;
+    }
+    return false;
+}
+
+template <typename T, int kT>
+__global__ void __launch_bounds__(kT, kSliceThreads / kT) k_policy_slices(const __grid_constant__ PolicyArgs a, int C, int stages, uint32_t stage_bytes) {
+    constexpr int kWarps = kT / 32, kN = kPairs<T>;
+    extern __shared__ __align__(128) uint8_t smem[];
+    SliceCtl& s = *reinterpret_cast<SliceCtl*>(smem);
+    const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
+    const int rank = C > 1 ? (int)cluster_rank() : 0;
+    const size_t row0 = blockIdx.x / C, G = gridDim.x / C;
+    if (tid == 0) {
+        for (int i = 0; i < stages; ++i) mbar_init(&s.full[i], 1);
+        mbar_init(&s.peers[0], 1);
+        mbar_init(&s.peers[1], 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (C > 1) cluster_sync(); else __syncthreads();
+    pdl_wait();
+    pdl_trigger();
+
+    // this CTA's pieces of a row
+    struct Slice {
+        RowCut cut;
+        int first, pieces;
+    };
+    auto slice_of = [&](const T* row) {
+        Slice q;
+        q.cut = cut_row(row, a.V);
+        const int per = (q.cut.pieces + C - 1) / C;
+        q.first = min(rank * per, q.cut.pieces);
+        q.pieces = min(per, q.cut.pieces - q.first);
+        return q;
+    };
+    auto counted = [&](int y, float w) { return y >= 0 && y < a.V && w != 0.f; };   // other rows are neither read nor waited for
+    auto load = [&](int stage, size_t t) {           // thread 0; the row is counted
+        const T* row = static_cast<const T*>(a.logits) + t * a.ld;
+        const Slice q = slice_of(row);
+        if (q.pieces <= 0) return;
+        mbar_expect_tx(&s.full[stage], (uint32_t)q.pieces * 16u);
+        bulk_load(smem + kSliceCtl + (size_t)stage * stage_bytes, reinterpret_cast<const uint8_t*>(row + q.cut.head) + (size_t)q.first * 16,
+                  (uint32_t)q.pieces * 16u, &s.full[stage]);
+    };
+    bool ok = true;
+    int stage = 0, parity = 0;
+    uint32_t phases = 0, peer_phase = 0;             // a bit per barrier
+    double sums[3] = {0.0, 0.0, 0.0};                // thread 0
+    // the numbers of the next row, and (thread 0) of the row whose copy is issued next, are fetched ahead
+    int y_next = 0, y_load = 0;
+    float w_next = 0.f, w_load = 0.f;
+    TokenIn in_next{};                               // thread 0
+    auto fetch = [&](size_t t) {
+        if (t >= a.T) return;
+        y_next = a.labels[t];
+        w_next = a.weight[t];
+        if (tid == 0) in_next = token_in(a, t);
+    };
+    auto fetch_load = [&](size_t t) {
+        if (tid != 0) return;
+        w_load = 0.f;
+        if (t < a.T) {
+            y_load = a.labels[t];
+            w_load = a.weight[t];
+        }
+    };
+    fetch(row0);
+    if (tid == 0)
+        for (int i = 0; i < stages; ++i) {
+            const size_t t = row0 + i * G;
+            if (t < a.T && counted(a.labels[t], a.weight[t])) load(i, t);
+        }
+    fetch_load(row0 + (size_t)stages * G);
+
+    for (size_t t = row0; t < a.T; t += G) {
+        const int y = y_next;
+        const float w = w_next;
+        const TokenIn in = in_next;
+        fetch(t + G);
+        const T* row = static_cast<const T*>(a.logits) + t * a.ld;
+        T* out = static_cast<T*>(a.dlogits) + t * a.ld_d;
+        const Slice q = slice_of(row);
+        const int ends = rank == 0 ? q.cut.head + q.cut.tail : 0;
+        const int extra = tid >= ends ? -1 : tid < q.cut.head ? tid : a.V - q.cut.tail + tid - q.cut.head;
+        const int have = (q.pieces - tid + kT - 1) / kT;             // pieces of this thread: tid, tid + kT, ..
+        auto refill = [&] {                          // the stage has been read by everybody
+            if (tid == 0 && counted(y_load, w_load)) load(stage, t + (size_t)stages * G);
+            fetch_load(t + (size_t)(stages + 1) * G);
+            if (++stage == stages) stage = 0;
+        };
+        if (!counted(y, w)) {
+            if (tid == 0 && rank == 0) a.logp[t] = 0.f;
+            if (a.dlogits) {
+                uint4* o = reinterpret_cast<uint4*>(out + q.cut.head) + q.first + tid;
+                for (int i = 0; i < have; ++i) o[i * kT] = make_uint4(0u, 0u, 0u, 0u);
+                if (extra >= 0) out[extra] = from_f<T>(0.f);
+            }
+            refill();
+            continue;
+        }
+        const float ex = extra >= 0 ? to_f(row[extra]) : -INFINITY;
+        float zy = 0.f;
+        if (tid == 0) zy = to_f(row[y]);
+        if (q.pieces > 0) {
+            if (!mbar_wait(&s.full[stage], (phases >> stage) & 1u, ok ? kSpinLimit : 1u)) ok = false;
+            phases ^= 1u << stage;
+        }
+        float2 e[kOwnPieces][kN], s2 = both(0.f);
+        float m = -INFINITY, ms[kOwnPieces / 2];     // running maximum, and what it was for each two pieces
+        const uint4* src = reinterpret_cast<const uint4*>(smem + kSliceCtl + (size_t)stage * stage_bytes) + tid;
+#pragma unroll
+        for (int j = 0; j < kOwnPieces; j += 2) {
+            if (j < have) {
+                uint4 raw[2];
+                raw[0] = src[j * kT];
+                float cm = piece_max(raw[0], m, T());
+                if (j + 1 < have) {
+                    raw[1] = src[(j + 1) * kT];
+                    cm = piece_max(raw[1], cm, T());
+                }
+                if (cm > m) {
+                    if (m != -INFINITY) s2 = mul2(s2, both(exp2_of(base_of(m).m2 - base_of(cm).m2)));
+                    m = cm;
+                }
+                const Base b = base_of(m);
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+                    if (j + i < have) {
+                        float2 z[kN];
+                        unpack(raw[i], z, T());
+#pragma unroll
+                        for (int k = 0; k < kN; ++k) {
+                            e[j + i][k] = exp_at(z[k], b);
+                            s2 = add2(s2, e[j + i][k]);
+                        }
+                    }
+            }
+            ms[j / 2] = m;
+        }
+        RowStat st{m, sum2(s2)};
+        if (extra >= 0) {
+            const float z[1] = {ex};
+            stat_add(st, z);
+        }
+        const float wm = warp_max(st.m);
+        float ws = at_max(st, wm);
+#pragma unroll
+        for (int o = 16; o; o >>= 1) ws += __shfl_xor_sync(0xffffffffu, ws, o);
+        if (lane == 0) s.part[parity][warp] = make_float2(wm, ws);
+        __syncthreads();
+        refill();
+        if (warp == 0) {
+            // the warps' pairs, then the CTAs': one lane each, joined by shuffles
+            auto join = [&](float2 p) {
+                RowStat all{p.x, 0.f};
+                all.m = warp_max(all.m);
+                all.s = at_max(RowStat{p.x, p.y}, all.m);
+#pragma unroll
+                for (int o = 8; o; o >>= 1) all.s += __shfl_xor_sync(0xffffffffu, all.s, o);
+                return all;
+            };
+            const float2 none = make_float2(-INFINITY, 0.f);
+            RowStat all = join(lane < kWarps ? s.part[parity][lane] : none);
+            if (C > 1) {
+                if (lane == 0) {
+                    s.zy[parity] = zy;               // the logit is read before a peer can overwrite it (dlogits in place of logits)
+                    mbar_expect_tx(&s.peers[parity], (uint32_t)C * 8u);
+                }
+                __syncwarp();
+                if (lane < C) send(&s.peer[parity][rank], &s.peers[parity], (uint32_t)lane, make_float2(all.m, all.s));
+                if (!mbar_wait_cluster(&s.peers[parity], (peer_phase >> parity) & 1u, ok ? kSpinLimit : 1u)) ok = false;
+                peer_phase ^= 1u << parity;
+                all = join(lane < C ? s.peer[parity][lane] : none);
+            }
+            if (lane == 0) {
+                const bool some = all.m != -INFINITY || all.s != 0.f;
+                const float logp = some ? zy - all.m - logf(all.s) : 0.f;
+                float g = 0.f;
+                TokenLoss l{};
+                if (some) {
+                    l = token_loss(a, in, logp);
+                    g = w * l.slope;
+                }
+                s.next[parity] = make_float4(all.m, some ? -g / all.s : 0.f, g, zy);
+                if (ok && rank == 0) a.logp[t] = logp;
+                sums[0] += (double)w * l.loss;
+                sums[1] += (double)w * l.kl;
+                sums[2] += (double)w * l.clipped;
+            }
+        }
+        if (a.dlogits) {
+            __syncthreads();
+            const float4 x = s.next[parity];
+            const float mul = x.y, g = x.z;
+            const Base b = base_of(x.x);
+            const bool zero = g == 0.f;
+            if (ok) {
+                uint4* o = reinterpret_cast<uint4*>(out + q.cut.head) + q.first + tid;
+#pragma unroll
+                for (int j = 0; j < kOwnPieces; ++j)
+                    if (j < have) {
+                        const float at = ms[j / 2], f = at == -INFINITY ? mul : mul * exp2_of(base_of(at).m2 - b.m2);
+                        float2 v[kN];
+#pragma unroll
+                        for (int k = 0; k < kN; ++k) v[k] = mul2(e[j][k], both(f));
+                        o[j * kT] = zero ? make_uint4(0u, 0u, 0u, 0u) : pack(v, T());
+                    }
+                if (extra >= 0) out[extra] = from_f<T>(zero ? 0.f : exp_at(ex, b) * mul);
+                // the label's element, once more, by the thread that wrote its piece
+                const int in_body = y - q.cut.head, piece = in_body / kVec<T> - q.first;
+                const bool inside = in_body >= 0 && y < a.V - q.cut.tail;
+                if (!zero && (inside ? piece >= 0 && piece < q.pieces && tid == piece % kT : extra == y)) out[y] = from_f<T>(exp_at(x.w, b) * mul + g);
+            }
+        }
+        parity ^= 1;
+    }
+    if (tid == 0 && rank == 0)
+        for (int i = 0; i < 3; ++i) a.part[row0 * 3 + i] = sums[i];
+    if (!ok) report_timeout();
+    if (C > 1) cluster_sync();       // no CTA leaves while another may still write to its shared memory
+}
+
 constexpr int kWarpRowMax = 1024;    // rows up to this length are taken by one warp each
 
 int current_sms() {
@@ -633,7 +906,7 @@ int current_sms() {
 }
 
 // Consumer threads of a CTA of k_rows for rows of this many bytes: the smallest whose ring holds the row.
-int rows_threads(size_t bytes) { return bytes <= (size_t)kRing * 64 * 64 ? 64 : bytes <= (size_t)kRing * 128 * 64 ? 128 : 256; }
+int rows_threads(size_t bytes) { return bytes <= (size_t)kRing * 64 * kU * 16 ? 64 : bytes <= (size_t)kRing * 128 * kU * 16 ? 128 : 256; }
 // Rows t of both matrices start at the same offset from a 16-byte boundary, for every t.
 bool aligned_alike(const void* a, size_t ld_a, const void* b, size_t ld_b, size_t es) {
     return (((uintptr_t)a - (uintptr_t)b) & 15) == 0 && ((ld_a - ld_b) * es & 15) == 0;
@@ -641,7 +914,7 @@ bool aligned_alike(const void* a, size_t ld_a, const void* b, size_t ld_b, size_
 
 template <typename T, int kT, int kMode>
 cudaError_t launch_rows_of(const RowArgs& a, size_t rows, int sms, int* grid, cudaStream_t s) {
-    const size_t smem = sizeof(RowsSmem<kT>), most = (size_t)sms * (512 / kT);
+    const size_t smem = sizeof(RowsSmem<kT>), most = (size_t)sms * (kRowThreads / kT);
     *grid = (int)(rows < most ? rows : most);
     const cudaError_t e = cudaFuncSetAttribute(k_rows<T, kT, kMode>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     return e != cudaSuccess ? e : launch_kernel(k_rows<T, kT, kMode>, *grid, kT + 32, smem, s, true, a);
@@ -655,18 +928,56 @@ cudaError_t launch_rows(const RowArgs& a, size_t rows, int V, int sms, int* grid
     }
 }
 
+// k_policy_slices: CTAs of a cluster, threads of a CTA, slices in flight.  As few CTAs as can own the row; more where rows
+// are few, down to slices of 8 KB.
+struct SlicePlan {
+    int cluster, threads, stages;    // cluster 0: more than a cluster can own
+    uint32_t stage_bytes;
+};
+SlicePlan slice_plan(size_t T, size_t pieces, int sms) {
+    SlicePlan p{1, 0, 0, 0};
+    while (p.cluster < kClusterMax && (size_t)p.cluster * kSliceThreads * kOwnPieces < pieces) p.cluster *= 2;
+    if ((size_t)p.cluster * kSliceThreads * kOwnPieces < pieces) return SlicePlan{};
+    while (p.cluster < kClusterMax && T * p.cluster * 2 <= (size_t)sms && pieces / (2 * p.cluster) >= 512) p.cluster *= 2;
+    const size_t own = (pieces + p.cluster - 1) / p.cluster;
+    p.threads = own <= 64 * kOwnPieces ? 64 : own <= 128 * kOwnPieces ? 128 : own <= 256 * kOwnPieces ? 256 : 512;
+    p.stage_bytes = (uint32_t)((own * 16 + 127) / 128 * 128);
+    const size_t room = 216 * 1024 / (kSliceThreads / p.threads) - kSliceCtl;     // three slices of the largest that the threads own
+    const size_t fit = room / p.stage_bytes;
+    p.stages = (int)(fit < (size_t)kStagesMax ? fit : (size_t)kStagesMax);
+    return p;
+}
+template <typename T, int kT>
+cudaError_t launch_slices_of(const PolicyArgs& a, SlicePlan p, int sms, int* parts, cudaStream_t s) {
+    const size_t smem = kSliceCtl + (size_t)p.stages * p.stage_bytes, most = (size_t)sms * (kSliceThreads / kT) / p.cluster;
+    *parts = (int)(a.T < most ? a.T : most);
+    const cudaError_t e = cudaFuncSetAttribute(k_policy_slices<T, kT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    return e != cudaSuccess ? e : launch_cluster(k_policy_slices<T, kT>, *parts * p.cluster, p.cluster, kT, smem, s, a, p.cluster, p.stages, p.stage_bytes);
+}
+template <typename T>
+cudaError_t launch_slices(const PolicyArgs& a, SlicePlan p, int sms, int* parts, cudaStream_t s) {
+    switch (p.threads) {
+        case 64: return launch_slices_of<T, 64>(a, p, sms, parts, s);
+        case 128: return launch_slices_of<T, 128>(a, p, sms, parts, s);
+        case 256: return launch_slices_of<T, 256>(a, p, sms, parts, s);
+        default: return launch_slices_of<T, 512>(a, p, sms, parts, s);
+    }
+}
+
 template <typename T>
 cudaError_t launch_policy(const PolicyArgs& a, float* stats, int sms, cudaStream_t s) {
-    const bool warp_rows = a.V <= kWarpRowMax, ring = !warp_rows && (!a.dlogits || aligned_alike(a.logits, a.ld, a.dlogits, a.ld_d, sizeof(T)));
+    const bool warp_rows = a.V <= kWarpRowMax, alike = !a.dlogits || aligned_alike(a.logits, a.ld, a.dlogits, a.ld_d, sizeof(T));
+    const SlicePlan p = !warp_rows && a.T * 2 <= (size_t)sms ? slice_plan(a.T, (size_t)a.V / kVec<T>, sms) : SlicePlan{};
     const size_t want = warp_rows ? (a.T + 7) / 8 : a.T;
-    int grid = (int)(want < (size_t)(4 * sms) ? want : (size_t)(4 * sms));
+    int parts = (int)(want < (size_t)(4 * sms) ? want : (size_t)(4 * sms));      // CTAs or clusters that leave partial sums
     cudaError_t e = cudaSuccess;
     if (a.T > 0)
-        e = ring ? launch_rows<T, kPolicy>(RowArgs{a, PrefArgs{}}, a.T, a.V, sms, &grid, s)
-          : warp_rows ? launch_kernel(k_policy_rows<T, 32, 8>, grid, 256, 0, s, true, a)
-                      : launch_kernel(k_policy_rows<T, 512, 1>, grid, 512, 0, s, true, a);
+        e = warp_rows          ? launch_kernel(k_policy_rows<T, 32, 8>, parts, 256, 0, s, true, a)
+          : alike && p.cluster ? launch_slices<T>(a, p, sms, &parts, s)
+          : alike              ? launch_rows<T, kPolicy>(RowArgs{a, PrefArgs{}}, a.T, a.V, sms, &parts, s)
+                               : launch_kernel(k_policy_rows<T, 512, 1>, parts, 512, 0, s, true, a);
     if (e != cudaSuccess) return e;
-    return launch_kernel(k_policy_stats, 1, 96, 0, s, true, (const double*)a.part, grid, stats);
+    return launch_kernel(k_policy_stats, 1, 96, 0, s, true, (const double*)a.part, parts, stats);
 }
 
 template <typename T>
