@@ -5,6 +5,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "abs_sgd.h"
 
 namespace abs_sgd {
@@ -61,6 +63,31 @@ inline cudaError_t launch_cluster(void (*kernel)(KArgs...), dim3 grid, int clust
     cfg.attrs = attr;
     cfg.numAttrs = cluster > 1 ? 2 : 1;
     return cudaLaunchKernelEx(&cfg, kernel, static_cast<Args&&>(args)...);
+}
+
+// Lets `kernel` use up to kSmemMax bytes of dynamic shared memory on the current device; asked for once per device.
+constexpr size_t kSmemMax = 224 * 1024;      // leaves a kernel some static shared memory
+template <auto kernel>
+inline cudaError_t allow_smem() {
+    static std::atomic<uint64_t> granted{0};     // a bit per device
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    const uint64_t bit = dev < 64 ? 1ull << dev : 0;
+    if (granted.load(std::memory_order_acquire) & bit) return cudaSuccess;
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemMax);
+    if (e == cudaSuccess) granted.fetch_or(bit, std::memory_order_release);
+    return e;
+}
+// SMs of the current device; 0 if there is none.
+inline int current_sms() {
+    static std::atomic<int> known[64];
+    int dev = 0, n = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return 0;
+    if (dev < 64 && (n = known[dev].load(std::memory_order_relaxed)) > 0) return n;
+    if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 0;
+    if (dev < 64) known[dev].store(n, std::memory_order_relaxed);
+    return n;
 }
 
 // Sets the text that abs_last_error(NULL) returns on this thread (calls without a context) and returns `code`.

@@ -478,7 +478,7 @@ extern "C" int abs_ckpt8_wgrad(const int8_t* q, const uint8_t* e, const void* dy
     a.split_stride = p.splits > 1 ? (size_t)width * out : 0;
     a.accumulate = p.splits > 1 ? 0 : accumulate;
     const size_t smem = sizeof(WgSmem) + 1024;
-    r = cudaFuncSetAttribute(k_wgrad, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    r = allow_smem<k_wgrad>();
     if (r == cudaSuccess) r = launch_kernel(k_wgrad, std::min(a.tiles * a.splits, kSms), kWgThreads, smem, s, true, tq, td, a);
     if (r == cudaSuccess && p.splits > 1) {
         const size_t n = (size_t)width * out;

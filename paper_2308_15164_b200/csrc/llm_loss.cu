@@ -899,12 +899,6 @@ __global__ void __launch_bounds__(kT, kSliceThreads / kT) k_policy_slices(const 
 
 constexpr int kWarpRowMax = 1024;    // rows up to this length are taken by one warp each
 
-int current_sms() {
-    int dev = 0, sms = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 0;
-    return sms;
-}
-
 // Consumer threads of a CTA of k_rows for rows of this many bytes: the smallest whose ring holds the row.
 int rows_threads(size_t bytes) { return bytes <= (size_t)kRing * 64 * kU * 16 ? 64 : bytes <= (size_t)kRing * 128 * kU * 16 ? 128 : 256; }
 // Rows t of both matrices start at the same offset from a 16-byte boundary, for every t.
@@ -916,7 +910,7 @@ template <typename T, int kT, int kMode>
 cudaError_t launch_rows_of(const RowArgs& a, size_t rows, int sms, int* grid, cudaStream_t s) {
     const size_t smem = sizeof(RowsSmem<kT>), most = (size_t)sms * (kRowThreads / kT);
     *grid = (int)(rows < most ? rows : most);
-    const cudaError_t e = cudaFuncSetAttribute(k_rows<T, kT, kMode>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    const cudaError_t e = allow_smem<k_rows<T, kT, kMode>>();
     return e != cudaSuccess ? e : launch_kernel(k_rows<T, kT, kMode>, *grid, kT + 32, smem, s, true, a);
 }
 template <typename T, int kMode>
@@ -951,7 +945,7 @@ template <typename T, int kT>
 cudaError_t launch_slices_of(const PolicyArgs& a, SlicePlan p, int sms, int* parts, cudaStream_t s) {
     const size_t smem = kSliceCtl + (size_t)p.stages * p.stage_bytes, most = (size_t)sms * (kSliceThreads / kT) / p.cluster;
     *parts = (int)(a.T < most ? a.T : most);
-    const cudaError_t e = cudaFuncSetAttribute(k_policy_slices<T, kT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    const cudaError_t e = allow_smem<k_policy_slices<T, kT>>();
     return e != cudaSuccess ? e : launch_cluster(k_policy_slices<T, kT>, *parts * p.cluster, p.cluster, kT, smem, s, a, p.cluster, p.stages, p.stage_bytes);
 }
 template <typename T>

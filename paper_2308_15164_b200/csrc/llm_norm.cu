@@ -20,7 +20,6 @@ constexpr int kWidthMax = 32768;
 constexpr int kSms = 148;
 constexpr int kBackCtas = 296;       // CTAs of the plain backward kernel
 constexpr int kRingSmem = 216 * 1024;   // shared memory of an SM that the ring kernels' CTAs share (1 KB per CTA is the system's)
-constexpr size_t kSmemMax = 227 * 1024; // of one CTA
 constexpr int kRingCtasMax = 16;
 // Threads of an SM for the ring kernels, by the elements that a thread owns: what their registers (weights, column sums,
 // the row's values) leave room for.
@@ -625,11 +624,6 @@ __global__ void __launch_bounds__(1024) k_column_sums(const float* part, int n, 
     }
 }
 
-template <typename K>
-cudaError_t allow_smem(K kernel, size_t bytes) {
-    return bytes > 48 * 1024 ? cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) : cudaSuccess;
-}
-
 // How a call is launched.  ring: all matrices aligned alike and the row within the pieces that a CTA's threads own.
 struct Plan {
     bool ring;
@@ -642,17 +636,16 @@ struct Plan {
 template <typename T, int kV, bool kPost, int kGate>
 cudaError_t run_plain(const NormArgs& a, bool back, int grid, cudaStream_t s) {
     const size_t smem = (size_t)a.D * 4;
-    auto k = back ? k_residual_norm_back<T, kV, kPost, kGate> : k_residual_norm<T, kV, kPost, kGate>;
-    const cudaError_t e = allow_smem(k, smem);
+    const cudaError_t e = back ? allow_smem<k_residual_norm_back<T, kV, kPost, kGate>>() : allow_smem<k_residual_norm<T, kV, kPost, kGate>>();
     if (e != cudaSuccess) return e;
-    return launch_kernel(k, grid, 256, smem, s, true, a);
+    return launch_kernel(back ? k_residual_norm_back<T, kV, kPost, kGate> : k_residual_norm<T, kV, kPost, kGate>, grid, 256, smem, s, true, a);
 }
 template <typename T, int kE, bool kPost, int kGate>
 cudaError_t run_ring(const NormArgs& a, bool back, const Plan& p, cudaStream_t s) {
     const RingArgs r{a, p.stages, p.row_bytes};
-    auto k = back ? k_join_back<T, kE / kVec<T>, kPost, kGate> : k_join<T, kE / kVec<T>, kPost, kGate>;
-    const cudaError_t e = allow_smem(k, p.smem);
-    return e != cudaSuccess ? e : launch_kernel(k, p.grid, p.threads, p.smem, s, true, r);
+    const cudaError_t e = back ? allow_smem<k_join_back<T, kE / kVec<T>, kPost, kGate>>() : allow_smem<k_join<T, kE / kVec<T>, kPost, kGate>>();
+    if (e != cudaSuccess) return e;
+    return launch_kernel(back ? k_join_back<T, kE / kVec<T>, kPost, kGate> : k_join<T, kE / kVec<T>, kPost, kGate>, p.grid, p.threads, p.smem, s, true, r);
 }
 template <typename T, bool kPost, int kGate>
 cudaError_t run(const NormArgs& a, bool back, bool wide, const Plan& p, cudaStream_t s) {

@@ -57,7 +57,7 @@ def _refuse(rc):
     raise _b.AbsError(rc, _lib.abs_last_error(None).decode())
 
 
-_empty, _Tensor = torch.empty, torch.Tensor
+_empty, _empty_like, _Tensor = torch.empty, torch.empty_like, torch.Tensor
 _stream_of = torch._C._cuda_getCurrentRawStream      # what torch.cuda.current_stream(d).cuda_stream returns, 2 us sooner
 
 
@@ -112,10 +112,10 @@ def _workspace(n, like):
 
 def _out(t, name, like, index):
     """(tensor, address, leading dimension) of an output of `like`'s type and shape; made if not given."""
-    rows, cols = like.shape
     if t is None:
-        t = torch.empty_like(like, memory_format=torch.contiguous_format)
-        return t, t.data_ptr(), cols
+        t = _empty_like(like) if like.is_contiguous() else like.new_empty(like.shape)
+        return t, t.data_ptr(), like.shape[1]
+    rows, cols = like.shape
     return (t, *_matrix(t, name, like.dtype, rows, cols, index))
 
 
@@ -142,13 +142,12 @@ def policy_loss(logits, labels, logp_old, advantage, weight, logp_ref=None, clip
     w = _vector(weight, "weight", T, _F32, dev)
     ref = None if logp_ref is None else _vector(logp_ref, "logp_ref", T, _F32, dev)
     d, da, ld_d = _dlogits(logits, dlogits, need_grad, dev)
-    out = _empty(T + 3, dtype=_F32, device=logits.device)
+    logp = _empty_like(weight)
+    stats = weight.new_empty(3)
     ws = _workspace(_POLICY_WORKSPACE, logits)
-    at = out.data_ptr()
-    _call(dev, _lib.abs_policy_loss, z, code, T, V, ld, y, old, ref, adv, w, clip_low, clip_high, kl_coef, at, at + 12, da, ld_d, ws.data_ptr(),
-          _POLICY_WORKSPACE)
-    loss, kl, clipped, logp = out.split_with_sizes((1, 1, 1, T))
-    return PolicyLoss(loss.view(()), kl.view(()), clipped.view(()), logp, d)
+    _call(dev, _lib.abs_policy_loss, z, code, T, V, ld, y, old, ref, adv, w, clip_low, clip_high, kl_coef, stats.data_ptr(), logp.data_ptr(), da,
+          ld_d, ws.data_ptr(), _POLICY_WORKSPACE)
+    return PolicyLoss(*stats.unbind(), logp, d)
 
 
 _POLICY_WORKSPACE = int(_lib.abs_policy_loss_workspace())
@@ -170,16 +169,15 @@ def preference_loss(logits, labels, offsets, logp_ref, beta: float = 0.1, smooth
     off = _vector(offsets, "offsets", 2 * pairs + 1, _I32, dev)
     ref = _vector(logp_ref, "logp_ref", 2 * pairs, _F32, dev)
     d, da, ld_d = _dlogits(logits, dlogits, need_grad, dev)
-    out = _empty(3 * pairs + 1, dtype=_F32, device=logits.device)
+    seq_logp = _empty_like(logp_ref)
+    pair_loss, loss = logp_ref.new_empty(pairs), logp_ref.new_empty(())
     n = _lib.abs_preference_loss_workspace(T)
     ws = _workspace(n, logits)
-    at = out.data_ptr()
     if scale is None:
         scale = 1.0 / pairs if pairs else 0.0
-    _call(dev, _lib.abs_preference_loss, z, code, T, V, ld, y, off, pairs, ref, beta, smoothing, scale, at, at + 4, at + 4 + 4 * pairs, da, ld_d,
-          ws.data_ptr(), n)
-    loss, pair_loss, seq_logp = out.split_with_sizes((1, pairs, 2 * pairs))
-    return PreferenceLoss(loss.view(()), pair_loss, seq_logp, d)
+    _call(dev, _lib.abs_preference_loss, z, code, T, V, ld, y, off, pairs, ref, beta, smoothing, scale, loss.data_ptr(), pair_loss.data_ptr(),
+          seq_logp.data_ptr(), da, ld_d, ws.data_ptr(), n)
+    return PreferenceLoss(loss, pair_loss, seq_logp, d)
 
 
 def _gate(gate, like, rows, cols, index):
@@ -229,7 +227,7 @@ def residual_norm_backward(dn, dy, y, h, w_pre, w_post=None, gate=None, scale: f
 
     def column(t, name):
         if t is None:
-            t = (torch.zeros if accumulate else _empty)(D, dtype=_F32, device=y.device)
+            t = torch.zeros_like(w_pre) if accumulate else _empty_like(w_pre)
             return t, t.data_ptr()
         return t, _vector(t, name, D, _F32, dev)
 
