@@ -103,28 +103,34 @@ __global__ void __launch_bounds__(256) k_ckpt8_dequantize(const uint2* q, const 
 // ------------------------------------------------------------------------------------------------
 // dw[i, o] = sum_t x^[t, i] dy[t, o].  Both operands lie with the contraction index t along the rows, i.e. "MN-major": a
 // TMA box of 64 columns x 64 tokens is 64 swizzled 128-byte rows, one per token.
-//   warp 0      TMA producer: per 64 tokens the 128 columns of q (8 KB) and the 256 columns of dy (four boxes, 32 KB)
-//   warp 1      MMA issuer: four tcgen05.mma (M 128, N 256, K 16) per 64 tokens into one of two TMEM accumulators
+// Two CTAs (two SMs) share an output tile of 256 x 256: each holds the operand columns of its 128 rows and of half of
+// the tile's columns, so that a run of 64 tokens costs an SM 24 KB of copies for 512 cycles of the tensor core (one CTA with
+// a 128 x 256 tile would need 40 KB, more than the L2 gives it).  Roles in each CTA:
+//   warp 0      TMA producer, up to kStages runs ahead: 128 columns of q (8 KB), 128 columns of dy (two boxes, 16 KB)
+//   warp 1      (first CTA only) MMA issuer: four tcgen05.mma.cta_group::2 (M 256, N 256, K 16) per run into one of two TMEM
+//               accumulators
 //   warps 2-5   epilogue: TMEM -> registers -> dw (or a partial sum), coalesced through a padded staging tile
-//   warps 6-13  q -> bf16 operand tile: thread = (token, block of 32), the two 16-byte pieces of q become four of bf16
-// A work item is an output tile and a run of tokens; items are dealt out round-robin.
+//   warps 6-13  q -> bf16 operand tile: thread = (token, block of 32), the two 16-byte pieces of q become four of bf16.  The
+//               exponents come by plain loads four runs ahead.
+// Items are dealt out round-robin to the pairs: the whole tiles, as many as fill all pairs equally often, then the rest, each
+// cut along the tokens into `splits` runs so that they too keep all pairs busy; k_wgrad_join adds those up in order.
 // ------------------------------------------------------------------------------------------------
-constexpr int kTM = 128, kTN = 256, kTK = 64;
-constexpr int kStages = 3;
-constexpr int kRawBytes = kTK * kTM, kABytes = kTK * kTM * 2, kBBytes = kTK * kTN * 2;
+constexpr int kTM = 256, kTN = 256, kTK = 64;    // of a pair
+constexpr int kStages = 6, kASlots = 3;
+constexpr int kRawBytes = kTK * 128, kABytes = kTK * 128 * 2, kBBytes = kTK * 128 * 2;
 constexpr int kWgThreads = 448;
 constexpr int kPitch = 33;
 
 struct WgSmem {
     alignas(1024) uint8_t raw[kStages][kRawBytes];
-    alignas(1024) uint8_t a[kStages][kABytes];
     alignas(1024) uint8_t b[kStages][kBBytes];
+    alignas(1024) uint8_t a[kASlots][kABytes];
     float out[4][32 * kPitch];
-    alignas(8) uint64_t full[kStages];
-    uint64_t ready[kStages];
-    uint64_t empty[kStages];
+    alignas(8) uint64_t full[kStages];       // copies of a run have landed (this CTA's)
+    uint64_t empty[kStages];                 // the run's MMAs have read both CTAs' operands
+    uint64_t ready[kASlots];                 // first CTA: both CTAs' operands of a run are there
     uint64_t acc_full[2];
-    uint64_t acc_empty[2];
+    uint64_t acc_empty[2];                   // first CTA: both CTAs have read the accumulator
     uint32_t tmem_base;
     uint32_t failed;
 };
@@ -133,122 +139,170 @@ struct WgArgs {
     const uint8_t* e;
     size_t e_ld;             // W / 32
     int T, D, N;
-    int tiles_n, tiles, splits, kb_per_split;   // kb: runs of 64 tokens
-    float* out;              // dw, or the partial sums [splits][D][ld] when splits > 1
-    size_t ld, split_stride;
+    int tiles_n, whole, rest, splits, kb_per_split;   // tiles: whole ones, then `rest` cut into `splits` runs; kb: 64 tokens
+    float* dw;
+    size_t ld;
+    float* part;             // [splits][rest][kTM][kTN]
     int accumulate;
 };
+
+__device__ __forceinline__ uint32_t cluster_rank() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// One arrival on the same barrier of the cluster's first CTA.  What it announces -- operand tiles written and fenced for the
+// async proxy, accumulators read and fenced by tcgen05.fence -- is ordered by those fences; a release at cluster scope would
+// make the warp wait for the exponents that it has in flight (617 instead of 350 us).
+__device__ __forceinline__ void arrive_first(uint64_t* bar) {
+    uint32_t a;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(a) : "r"(smem_u32(bar)));
+    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(a) : "memory");
+}
+__device__ __forceinline__ void umma2_bf16(uint32_t tmem_d, uint64_t da, uint64_t db, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
+        " tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}\n"
+        ::"r"(tmem_d), "l"(da), "l"(db), "r"(idesc), "r"(accumulate) : "memory");
+}
+// Arrives on this barrier of both CTAs when the MMAs issued so far are done.
+__device__ __forceinline__ void umma2_commit(uint64_t* bar) {
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
+                 ::"r"(smem_u32(bar)), "h"((uint16_t)3) : "memory");
+}
 
 __global__ void __launch_bounds__(kWgThreads, 1) k_wgrad(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_dy,
                                                          const __grid_constant__ WgArgs a) {
     extern __shared__ uint8_t smem_raw[];
     WgSmem& s = *reinterpret_cast<WgSmem*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-    const int items = a.tiles * a.splits;
+    const int rank = (int)cluster_rank();
+    const int pair = blockIdx.x / 2, pairs = gridDim.x / 2;
+    const int items = a.whole + a.rest * a.splits;
     const int kb_total = (a.T + kTK - 1) / kTK;
     if (warp == 1) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&s.tmem_base)), "r"(512) : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&s.tmem_base)), "r"(512) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
     }
     if (threadIdx.x == 0) {
         for (int i = 0; i < kStages; ++i) {
             mbar_init(&s.full[i], 1);
-            mbar_init(&s.ready[i], 256);
             mbar_init(&s.empty[i], 1);
         }
+        for (int i = 0; i < kASlots; ++i) mbar_init(&s.ready[i], 16);    // eight warps of each CTA
         for (int i = 0; i < 2; ++i) {
             mbar_init(&s.acc_full[i], 1);
-            mbar_init(&s.acc_empty[i], 128);
+            mbar_init(&s.acc_empty[i], 8);                               // four warps of each CTA
         }
         s.failed = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-    __syncthreads();
+    cluster_sync();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem = s.tmem_base;
     volatile uint32_t* failed = &s.failed;
     pdl_wait();
     pdl_trigger();
 
-    // item -> its first output row and column, and its runs of tokens [kb0, kb1)
-    auto item_of = [&](int it, int* m0, int* n0, int* kb0, int* kb1) {
-        const int tile = it % a.tiles, sp = it / a.tiles;
-        *m0 = (tile / a.tiles_n) * kTM;
-        *n0 = (tile % a.tiles_n) * kTN;
-        *kb0 = min(kb_total, sp * a.kb_per_split);
-        *kb1 = min(kb_total, *kb0 + a.kb_per_split);
+    struct Item {
+        int m0, n0, kb0, kb1;        // first row and column of the pair's tile, runs of 64 tokens
+        int part;                    // index of the partial sum, -1: straight to dw
+    };
+    auto item_of = [&](int it) {
+        Item q;
+        int tile = it;
+        q.part = -1;
+        q.kb0 = 0;
+        q.kb1 = kb_total;
+        if (it >= a.whole) {
+            const int r = it - a.whole;
+            tile = a.whole + r % a.rest;
+            if (a.splits > 1) {
+                q.part = r;
+                q.kb0 = min(kb_total, r / a.rest * a.kb_per_split);
+                q.kb1 = min(kb_total, q.kb0 + a.kb_per_split);
+            }
+        }
+        q.m0 = tile / a.tiles_n * kTM;
+        q.n0 = tile % a.tiles_n * kTN;
+        return q;
     };
 
     if (warp == 0) {
         if (lane == 0) {                             // ---- TMA producer
             uint32_t st = 0, round = 0;
-            for (int it = blockIdx.x; it < items && !*failed; it += gridDim.x) {
-                int m0, n0, kb0, kb1;
-                item_of(it, &m0, &n0, &kb0, &kb1);
-                for (int kb = kb0; kb < kb1; ++kb) {
+            for (int it = pair; it < items && !*failed; it += pairs) {
+                const Item q = item_of(it);
+                for (int kb = q.kb0; kb < q.kb1; ++kb) {
                     if (round > 0 && !mbar_wait(&s.empty[st], (round - 1) & 1)) { *failed = 1; break; }
                     mbar_expect_tx(&s.full[st], kRawBytes + kBBytes);
-                    tma_load_2d(s.raw[st], &tm_q, m0, kb * kTK, &s.full[st]);
-#pragma unroll
-                    for (int j = 0; j < kTN / 64; ++j)
-                        tma_load_2d(s.b[st] + j * 8192, &tm_dy, n0 + 64 * j, kb * kTK, &s.full[st]);
+                    tma_load_2d(s.raw[st], &tm_q, q.m0 + rank * 128, kb * kTK, &s.full[st]);
+                    tma_load_2d(s.b[st], &tm_dy, q.n0 + rank * 128, kb * kTK, &s.full[st]);
+                    tma_load_2d(s.b[st] + 8192, &tm_dy, q.n0 + rank * 128 + 64, kb * kTK, &s.full[st]);
                     if (++st == kStages) { st = 0; ++round; }
                 }
             }
-            // copies in flight must have landed before the CTA's shared memory is released
-            for (int i = 0; i < kStages && *failed; ++i) mbar_wait(&s.full[i], round & 1, 4096u);
+            if (*failed)                             // copies in flight land before the CTA's shared memory is released
+                for (uint32_t i = 0; i < kStages; ++i) mbar_wait(&s.full[i], (round + (i < st ? 0u : 1u)) & 1u, 4096u);
         }
     } else if (warp == 1) {
-        if (lane == 0) {                             // ---- MMA issuer
+        if (lane == 0 && rank == 0) {                // ---- MMA issuer
             constexpr uint32_t idesc = umma_idesc_bf16(kTM, kTN) | (1u << 15) | (1u << 16);   // both operands MN-major
-            uint32_t st = 0, round = 0;
+            uint32_t st = 0, sl = 0, sl_phase = 0;
             int i = 0;
             bool ok = true;
-            for (int it = blockIdx.x; it < items && ok; it += gridDim.x, ++i) {
-                int m0, n0, kb0, kb1;
-                item_of(it, &m0, &n0, &kb0, &kb1);
+            for (int it = pair; it < items && ok; it += pairs, ++i) {
+                const Item q = item_of(it);
                 const int ab = i & 1;
                 if (i >= 2 && !mbar_wait(&s.acc_empty[ab], ((i / 2) - 1) & 1)) { ok = false; break; }
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                for (int kb = kb0; kb < kb1; ++kb) {
-                    if (!mbar_wait(&s.full[st], round & 1) || !mbar_wait(&s.ready[st], round & 1)) { ok = false; break; }
+                for (int kb = q.kb0; kb < q.kb1; ++kb) {
+                    if (!mbar_wait(&s.ready[sl], sl_phase)) { ok = false; break; }
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                    const uint32_t a0 = smem_u32(s.a[st]), b0 = smem_u32(s.b[st]);
+                    const uint32_t a0 = smem_u32(s.a[sl]), b0 = smem_u32(s.b[st]);
 #pragma unroll
                     for (int k = 0; k < kTK / 16; ++k)
-                        umma_bf16(tmem + ab * kTN, umma_desc_mn_sw128(a0 + k * 2048, 8192), umma_desc_mn_sw128(b0 + k * 2048, 8192), idesc,
-                                  kb > kb0 || k > 0);
-                    umma_commit(&s.empty[st]);
-                    if (++st == kStages) { st = 0; ++round; }
+                        umma2_bf16(tmem + ab * kTN, umma_desc_mn_sw128(a0 + k * 2048, 8192), umma_desc_mn_sw128(b0 + k * 2048, 8192), idesc,
+                                   kb > q.kb0 || k > 0);
+                    umma2_commit(&s.empty[st]);
+                    if (++st == kStages) st = 0;
+                    if (++sl == kASlots) { sl = 0; sl_phase ^= 1u; }
                 }
-                if (ok) umma_commit(&s.acc_full[ab]);
+                if (ok) umma2_commit(&s.acc_full[ab]);
             }
             if (!ok) *failed = 1;
         }
+        __syncwarp();
     } else if (warp < 6) {                           // ---- epilogue
         const int qd = warp % 4;
         float* stage = s.out[warp - 2];
         int i = 0;
-        for (int it = blockIdx.x; it < items; it += gridDim.x, ++i) {
-            int m0, n0, kb0, kb1;
-            item_of(it, &m0, &n0, &kb0, &kb1);
+        for (int it = pair; it < items; it += pairs, ++i) {
+            const Item q = item_of(it);
             const int ab = i & 1;
-            bool ok = mbar_wait(&s.acc_full[ab], (i / 2) & 1);
-            ok = __all_sync(0xffffffffu, ok) && !*failed;
+            const bool ok = mbar_wait(&s.acc_full[ab], (i / 2) & 1) && !*failed;
             if (!__all_sync(0xffffffffu, ok)) {
                 *failed = 1;
                 break;
             }
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            float* base = a.out + (size_t)(it / a.tiles) * a.split_stride + (size_t)(m0 + qd * 32) * a.ld + n0;
-            const int rows = min(32, a.D - (m0 + qd * 32)), cols = a.N - n0;
+            const int row = rank * 128 + qd * 32;    // of the tile
+            const bool part = q.part >= 0;
+            float* base = part ? a.part + ((size_t)q.part * kTM + row) * kTN : a.dw + (size_t)(q.m0 + row) * a.ld + q.n0;
+            const size_t ld = part ? (size_t)kTN : a.ld;
+            const int rows = min(32, a.D - (q.m0 + row)), cols = a.N - q.n0;
+            const bool add = a.accumulate && !part;
             for (int c = 0; c < kTN / 32; ++c) {
                 uint32_t v[32];
                 tmem_ld_32(tmem + ((uint32_t)(qd * 32) << 16) + (uint32_t)(ab * kTN + c * 32), v);
                 if (c == kTN / 32 - 1) {
                     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-                    mbar_arrive(&s.acc_empty[ab]);
+                    __syncwarp();
+                    if (lane == 0) arrive_first(&s.acc_empty[ab]);
                 }
                 if (c * 32 >= cols) continue;
 #pragma unroll
@@ -256,12 +310,12 @@ __global__ void __launch_bounds__(kWgThreads, 1) k_wgrad(const __grid_constant__
                 __syncwarp();
                 float* p = base + c * 32 + lane;
                 if (c * 32 + lane < cols) {
-                    if (a.accumulate) {
+                    if (add) {
 #pragma unroll 8
-                        for (int r = 0; r < rows; ++r) p[(size_t)r * a.ld] += stage[r * kPitch + lane];
+                        for (int r = 0; r < rows; ++r) p[(size_t)r * ld] += stage[r * kPitch + lane];
                     } else {
 #pragma unroll 8
-                        for (int r = 0; r < rows; ++r) p[(size_t)r * a.ld] = stage[r * kPitch + lane];
+                        for (int r = 0; r < rows; ++r) p[(size_t)r * ld] = stage[r * kPitch + lane];
                     }
                 }
                 __syncwarp();
@@ -271,28 +325,31 @@ __global__ void __launch_bounds__(kWgThreads, 1) k_wgrad(const __grid_constant__
         const int tid = threadIdx.x - 192;
         const int r = tid % kTK, blk = tid / kTK;    // token of the run, block of 32 columns
         const uint32_t sw = (uint32_t)(r & 7);
-        uint32_t st = 0, round = 0;
+        uint32_t st = 0, phase = 0, sl = 0;
+        int n = 0;                                   // runs so far
         bool ok = true;
-        for (int it = blockIdx.x; it < items && ok; it += gridDim.x) {
-            int m0, n0, kb0, kb1;
-            item_of(it, &m0, &n0, &kb0, &kb1);
-            const size_t ecol = (size_t)(m0 / 32 + blk);
+        for (int it = pair; it < items && ok; it += pairs) {
+            const Item q = item_of(it);
+            const size_t ecol = (size_t)((q.m0 + rank * 128) / 32 + blk);
             const bool have = ecol < a.e_ld;
             auto exponent = [&](int kb) -> uint32_t {   // of this thread's block; beyond the matrix q is filled with zeros
                 const int t = kb * kTK + r;
-                return have && kb < kb1 && t < a.T ? a.e[(size_t)t * a.e_ld + ecol] : 0u;
+                return have && kb < q.kb1 && t < a.T ? a.e[(size_t)t * a.e_ld + ecol] : 0u;
             };
-            uint32_t e0 = exponent(kb0), e1 = exponent(kb0 + 1);
-            for (int kb = kb0; kb < kb1; ++kb) {
-                const uint32_t e2 = exponent(kb + 2);
-                const float scale = pow2_of(e0);
-                if (!mbar_wait(&s.full[st], round & 1)) { ok = false; break; }
+            uint32_t e[4] = {exponent(q.kb0), exponent(q.kb0 + 1), exponent(q.kb0 + 2), exponent(q.kb0 + 3)};
+            for (int kb = q.kb0; kb < q.kb1; ++kb, ++n) {
+                const uint32_t e4 = exponent(kb + 4);
+                const float scale = pow2_of(e[0]);
+                e[0] = e[1]; e[1] = e[2]; e[2] = e[3]; e[3] = e4;
+                // the MMAs of the run kASlots back have read this slot of the operand tile
+                if (n >= kASlots && !mbar_wait(&s.empty[(n - kASlots) % kStages], ((n - kASlots) / kStages) & 1)) { ok = false; break; }
+                if (!mbar_wait(&s.full[st], phase)) { ok = false; break; }
                 const uint8_t* src = s.raw[st] + r * 128;
-                uint8_t* dst = s.a[st] + (blk / 2) * 8192 + r * 128;
+                uint8_t* dst = s.a[sl] + (blk / 2) * 8192 + r * 128;
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    const uint4 q = *reinterpret_cast<const uint4*>(src + ((uint32_t)(blk * 2 + h) ^ sw) * 16);
-                    const uint32_t w[4] = {q.x ^ 0x80808080u, q.y ^ 0x80808080u, q.z ^ 0x80808080u, q.w ^ 0x80808080u};
+                    const uint4 v = *reinterpret_cast<const uint4*>(src + ((uint32_t)(blk * 2 + h) ^ sw) * 16);
+                    const uint32_t w[4] = {v.x ^ 0x80808080u, v.y ^ 0x80808080u, v.z ^ 0x80808080u, v.w ^ 0x80808080u};
 #pragma unroll
                     for (int p = 0; p < 2; ++p) {
                         uint32_t o[4];
@@ -300,9 +357,10 @@ __global__ void __launch_bounds__(kWgThreads, 1) k_wgrad(const __grid_constant__
                         for (int j = 0; j < 4; ++j) {
                             const uint32_t word = w[2 * p + j / 2];
                             // the byte q + 128 as the low mantissa byte of 2^23: subtracting 2^23 + 128 leaves q exactly
-                            const float f0 = __uint_as_float(__byte_perm(word, 0x4B000000u, 0x7540 + 2 * (j % 2))) - 8388736.f;
-                            const float f1 = __uint_as_float(__byte_perm(word, 0x4B000000u, 0x7541 + 2 * (j % 2))) - 8388736.f;
-                            const __nv_bfloat162 b2 = __floats2bfloat162_rn(f0 * scale, f1 * scale);
+                            float2 f = make_float2(__uint_as_float(__byte_perm(word, 0x4B000000u, 0x7540 + 2 * (j % 2))),
+                                                   __uint_as_float(__byte_perm(word, 0x4B000000u, 0x7541 + 2 * (j % 2))));
+                            f = mul2(add2(f, both(-8388736.f)), both(scale));
+                            const __nv_bfloat162 b2 = __float22bfloat162_rn(f);
                             o[j] = *reinterpret_cast<const uint32_t*>(&b2);
                         }
                         const uint32_t chunk = (uint32_t)((blk % 2) * 4 + h * 2 + p);
@@ -310,30 +368,35 @@ __global__ void __launch_bounds__(kWgThreads, 1) k_wgrad(const __grid_constant__
                     }
                 }
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                mbar_arrive(&s.ready[st]);
-                if (++st == kStages) { st = 0; ++round; }
-                e0 = e1;
-                e1 = e2;
+                __syncwarp();
+                if (lane == 0) arrive_first(&s.ready[sl]);
+                if (++st == kStages) { st = 0; phase ^= 1u; }
+                if (++sl == kASlots) sl = 0;
             }
         }
         if (!ok) *failed = 1;
     }
+    __syncwarp();
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-    __syncthreads();
+    cluster_sync();                                  // no CTA leaves while the other's arrivals or MMAs may still reach it
     if (threadIdx.x == 0 && *failed) report_timeout();
-    if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+    if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
 }
 
-// dw (+)= the partial sums, in split order.
-__global__ void __launch_bounds__(256) k_wgrad_join(const float* part, int splits, size_t split_stride, int N, size_t n, float* dw, size_t ld,
-                                                    int accumulate) {
+// dw (+)= the partial sums of the tiles that were cut, in order.
+__global__ void __launch_bounds__(256) k_wgrad_join(const __grid_constant__ WgArgs a) {
     pdl_wait();
     pdl_trigger();
-    for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (size_t)gridDim.x * 256) {
-        float s = part[i];
-        for (int k = 1; k < splits; ++k) s += part[(size_t)k * split_stride + i];
-        float* p = dw + (i / N) * ld + i % N;
-        *p = accumulate ? *p + s : s;
+    const size_t step = (size_t)a.rest * kTM * kTN;
+    // one row of a tile at a time
+    for (int i = blockIdx.x; i < a.rest * kTM; i += gridDim.x) {
+        const int tile = a.whole + i / kTM, m = tile / a.tiles_n * kTM + i % kTM, n = tile % a.tiles_n * kTN + threadIdx.x;
+        if (m >= a.D || n >= a.N) continue;
+        const float* p = a.part + (size_t)i * kTN + threadIdx.x;
+        float s = p[0];
+        for (int k = 1; k < a.splits; ++k) s += p[k * step];
+        float* o = a.dw + (size_t)m * a.ld + n;
+        *o = a.accumulate ? *o + s : s;
     }
 }
 
@@ -357,27 +420,33 @@ int grid_for(size_t n, int per_cta) {
 }
 
 constexpr int kSms = 148;
+constexpr int kMinRuns = 4;      // runs of 64 tokens that a part of a cut tile has at least
 
-// How the work is cut: output tiles, and runs of tokens where there are fewer tiles than SMs.
+// How the work is cut: whole output tiles for all pairs of SMs equally often, the rest in runs of tokens.
 struct WgPlan {
-    int tiles_m, tiles_n, splits, kb_per_split;
+    int tiles_m, tiles_n, whole, rest, splits, kb_per_split;
     bool repack;
     size_t ld8, part_bytes, pack_bytes;
 };
-WgPlan plan_of(uint64_t T, uint64_t D, uint64_t N, const void* dy, uint64_t ld_dy) {
+bool plan_of(uint64_t T, uint64_t D, uint64_t N, const void* dy, uint64_t ld_dy, WgPlan* out) {
     WgPlan p{};
     p.tiles_m = (int)((D + kTM - 1) / kTM);
     p.tiles_n = (int)((N + kTN - 1) / kTN);
-    const int kb = (int)((T + kTK - 1) / kTK);
+    const int kb = (int)((T + kTK - 1) / kTK), pairs = kSms / 2;
     const int64_t tiles = (int64_t)p.tiles_m * p.tiles_n;
-    int splits = (int)std::max<int64_t>(1, std::min<int64_t>(tiles ? kSms / tiles : 1, kb / 4));
+    if (tiles > 0x3fffffff) return false;
+    p.whole = (int)(tiles / pairs * pairs);
+    p.rest = (int)(tiles - p.whole);
+    int splits = p.rest ? std::min(pairs / p.rest, kb / kMinRuns) : 1;
+    if (splits < 1) splits = 1;
     p.kb_per_split = std::max(1, (kb + splits - 1) / splits);
     p.splits = std::max(1, (kb + p.kb_per_split - 1) / p.kb_per_split);
     p.repack = misaligned(dy, 16) || ld_dy % 8 != 0;
     p.ld8 = (N + 7) / 8 * 8;
-    p.part_bytes = p.splits > 1 ? up256((size_t)p.splits * D * N * 4) : 0;
+    p.part_bytes = p.splits > 1 ? (size_t)p.splits * p.rest * kTM * kTN * 4 : 0;
     p.pack_bytes = p.repack ? up256((size_t)T * p.ld8 * 2) : 0;
-    return p;
+    *out = p;
+    return true;
 }
 
 }  // namespace
@@ -433,8 +502,8 @@ extern "C" int abs_ckpt8_dequantize(const int8_t* q, const uint8_t* e, uint64_t 
 
 extern "C" size_t abs_ckpt8_wgrad_workspace(uint64_t tokens, uint64_t width, uint64_t out, const void* dy, uint64_t ld_dy) {
     if (tokens > 0x7fffffffull || width > 0x7fffffffull || out > 0x7fffffffull) return 0;
-    const WgPlan p = plan_of(tokens, width, out, dy, ld_dy);
-    return p.part_bytes + p.pack_bytes;
+    WgPlan p;
+    return plan_of(tokens, width, out, dy, ld_dy, &p) ? p.part_bytes + p.pack_bytes : 0;
 }
 
 extern "C" int abs_ckpt8_wgrad(const int8_t* q, const uint8_t* e, const void* dy, uint64_t ld_dy, uint64_t tokens, uint64_t width,
@@ -450,8 +519,8 @@ extern "C" int abs_ckpt8_wgrad(const int8_t* q, const uint8_t* e, const void* dy
         if (!accumulate) r = cudaMemset2DAsync(dw, ld_dw * 4, 0, out * 4, width, s);
         return r == cudaSuccess ? ABS_OK : thread_error(ABS_ECUDA, cudaGetErrorString(r));
     }
-    const WgPlan p = plan_of(tokens, width, out, dy, ld_dy);
-    if ((int64_t)p.tiles_m * p.tiles_n * p.splits > 0x7fffffff / 2) return thread_error(ABS_ELIMIT, "too many output tiles");
+    WgPlan p;
+    if (!plan_of(tokens, width, out, dy, ld_dy, &p)) return thread_error(ABS_ELIMIT, "too many output tiles");
     if (p.part_bytes + p.pack_bytes) {
         if (!workspace || misaligned(workspace, 256)) return thread_error(ABS_EINVAL, "workspace must be non-NULL and 256-byte aligned");
         if (workspace_bytes < p.part_bytes + p.pack_bytes) return thread_error(ABS_ENOMEM, "workspace too small");
@@ -467,23 +536,17 @@ extern "C" int abs_ckpt8_wgrad(const int8_t* q, const uint8_t* e, const void* dy
     }
     const uint64_t W = (width + 31) / 32 * 32;
     CUtensorMap tq, td;
-    if (!encode_2d(&tq, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, const_cast<int8_t*>(q), tokens, W, kTK, kTM) ||
+    if (!encode_2d(&tq, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, const_cast<int8_t*>(q), tokens, W, kTK, 128) ||
         !encode_2d(&td, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(dy), tokens, out, kTK, 64, ld_dy))
         return thread_error(ABS_ECUDA, "cuTensorMapEncodeTiled failed");
     WgArgs a{};
     a.e = e; a.e_ld = W / 32; a.T = (int)tokens; a.D = (int)width; a.N = (int)out;
-    a.tiles_n = p.tiles_n; a.tiles = p.tiles_m * p.tiles_n; a.splits = p.splits; a.kb_per_split = p.kb_per_split;
-    a.out = p.splits > 1 ? part : dw;
-    a.ld = p.splits > 1 ? out : ld_dw;
-    a.split_stride = p.splits > 1 ? (size_t)width * out : 0;
-    a.accumulate = p.splits > 1 ? 0 : accumulate;
-    const size_t smem = sizeof(WgSmem) + 1024;
+    a.tiles_n = p.tiles_n; a.whole = p.whole; a.rest = p.rest; a.splits = p.splits; a.kb_per_split = p.kb_per_split;
+    a.dw = dw; a.ld = ld_dw; a.part = part; a.accumulate = accumulate != 0;
     r = allow_smem<k_wgrad>();
-    if (r == cudaSuccess) r = launch_kernel(k_wgrad, std::min(a.tiles * a.splits, kSms), kWgThreads, smem, s, true, tq, td, a);
-    if (r == cudaSuccess && p.splits > 1) {
-        const size_t n = (size_t)width * out;
-        r = launch_kernel(k_wgrad_join, grid_for(n, 256), 256, 0, s, true, (const float*)part, p.splits, a.split_stride, (int)out, n, dw, (size_t)ld_dw, accumulate);
-    }
+    const int items = p.whole + p.rest * p.splits;
+    if (r == cudaSuccess) r = launch_cluster(k_wgrad, 2 * std::min(items, kSms / 2), 2, kWgThreads, sizeof(WgSmem) + 1024, s, tq, td, a);
+    if (r == cudaSuccess && p.splits > 1) r = launch_kernel(k_wgrad_join, std::min(p.rest * kTM, kSms * 8), 256, 0, s, true, a);
     return r == cudaSuccess ? ABS_OK : thread_error(ABS_ECUDA, cudaGetErrorString(r));
 }
 
