@@ -110,15 +110,16 @@ __global__ void __launch_bounds__(256) k_ckpt8_dequantize(const uint2* q, const 
 //   warp 1      (first CTA only) MMA issuer: four tcgen05.mma.cta_group::2 (M 256, N 256, K 16) per run into one of two TMEM
 //               accumulators
 //   warps 2-5   epilogue: TMEM -> registers -> dw (or a partial sum), coalesced through a padded staging tile
-//   warps 6-13  q -> bf16 operand tile: thread = (token, block of 32), the two 16-byte pieces of q become four of bf16.  The
-//               exponents come by plain loads four runs ahead.
+//   warps 6-21  q -> bf16 operand tile, two groups of eight warps on alternate runs: thread = (token, block of 32), the two
+//               16-byte pieces of q become four of bf16.  The exponents come by plain loads, kAhead of a group's runs ahead.
 // Items are dealt out round-robin to the pairs: the whole tiles, as many as fill all pairs equally often, then the rest, each
 // cut along the tokens into `splits` runs so that they too keep all pairs busy; k_wgrad_join adds those up in order.
 // ------------------------------------------------------------------------------------------------
 constexpr int kTM = 256, kTN = 256, kTK = 64;    // of a pair
-constexpr int kStages = 6, kASlots = 3;
+constexpr int kStages = 5, kASlots = 4;
 constexpr int kRawBytes = kTK * 128, kABytes = kTK * 128 * 2, kBBytes = kTK * 128 * 2;
-constexpr int kWgThreads = 448;
+constexpr int kWgThreads = 704;
+constexpr int kAhead = 4;
 constexpr int kPitch = 33;
 
 struct WgSmem {
@@ -322,57 +323,64 @@ __global__ void __launch_bounds__(kWgThreads, 1) k_wgrad(const __grid_constant__
             }
         }
     } else {                                         // ---- q -> bf16 operand tile
-        const int tid = threadIdx.x - 192;
+        const int tid = (threadIdx.x - 192) % 256, group = (threadIdx.x - 192) / 256;
         const int r = tid % kTK, blk = tid / kTK;    // token of the run, block of 32 columns
         const uint32_t sw = (uint32_t)(r & 7);
-        uint32_t st = 0, phase = 0, sl = 0;
-        int n = 0;                                   // runs so far
+        int n = 0;                                   // runs so far, of both groups
         bool ok = true;
         for (int it = pair; it < items && ok; it += pairs) {
             const Item q = item_of(it);
             const size_t ecol = (size_t)((q.m0 + rank * 128) / 32 + blk);
+            const uint8_t* ep = a.e + (size_t)r * a.e_ld + ecol;
             const bool have = ecol < a.e_ld;
             auto exponent = [&](int kb) -> uint32_t {   // of this thread's block; beyond the matrix q is filled with zeros
-                const int t = kb * kTK + r;
-                return have && kb < q.kb1 && t < a.T ? a.e[(size_t)t * a.e_ld + ecol] : 0u;
+                return have && kb < q.kb1 && kb * kTK + r < a.T ? ep[(size_t)kb * kTK * a.e_ld] : 0u;
             };
-            uint32_t e[4] = {exponent(q.kb0), exponent(q.kb0 + 1), exponent(q.kb0 + 2), exponent(q.kb0 + 3)};
-            for (int kb = q.kb0; kb < q.kb1; ++kb, ++n) {
-                const uint32_t e4 = exponent(kb + 4);
-                const float scale = pow2_of(e[0]);
-                e[0] = e[1]; e[1] = e[2]; e[2] = e[3]; e[3] = e4;
-                // the MMAs of the run kASlots back have read this slot of the operand tile
-                if (n >= kASlots && !mbar_wait(&s.empty[(n - kASlots) % kStages], ((n - kASlots) / kStages) & 1)) { ok = false; break; }
-                if (!mbar_wait(&s.full[st], phase)) { ok = false; break; }
-                const uint8_t* src = s.raw[st] + r * 128;
-                uint8_t* dst = s.a[sl] + (blk / 2) * 8192 + r * 128;
+            const int first = q.kb0 + ((group - n) & 1);     // this group's runs: every other one
+            uint32_t e[kAhead];
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const uint4 v = *reinterpret_cast<const uint4*>(src + ((uint32_t)(blk * 2 + h) ^ sw) * 16);
-                    const uint32_t w[4] = {v.x ^ 0x80808080u, v.y ^ 0x80808080u, v.z ^ 0x80808080u, v.w ^ 0x80808080u};
+            for (int u = 0; u < kAhead; ++u) e[u] = exponent(first + 2 * u);
+            for (int kb0 = first; kb0 < q.kb1 && ok; kb0 += 2 * kAhead) {
 #pragma unroll
-                    for (int p = 0; p < 2; ++p) {
-                        uint32_t o[4];
+                for (int u = 0; u < kAhead; ++u) {
+                    const int kb = kb0 + 2 * u;
+                    if (kb >= q.kb1 || !ok) continue;
+                    const int run = n + (kb - q.kb0);
+                    const int st = run % kStages, sl = run % kASlots;
+                    const float scale = pow2_of(e[u]);
+                    e[u] = exponent(kb + 2 * kAhead);
+                    // the MMAs of the run kASlots back have read this slot of the operand tile
+                    if (run >= kASlots && !mbar_wait(&s.empty[(run - kASlots) % kStages], ((run - kASlots) / kStages) & 1)) { ok = false; continue; }
+                    if (!mbar_wait(&s.full[st], (run / kStages) & 1)) { ok = false; continue; }
+                    const uint8_t* src = s.raw[st] + r * 128;
+                    uint8_t* dst = s.a[sl] + (blk / 2) * 8192 + r * 128;
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            const uint32_t word = w[2 * p + j / 2];
-                            // the byte q + 128 as the low mantissa byte of 2^23: subtracting 2^23 + 128 leaves q exactly
-                            float2 f = make_float2(__uint_as_float(__byte_perm(word, 0x4B000000u, 0x7540 + 2 * (j % 2))),
-                                                   __uint_as_float(__byte_perm(word, 0x4B000000u, 0x7541 + 2 * (j % 2))));
-                            f = mul2(add2(f, both(-8388736.f)), both(scale));
-                            const __nv_bfloat162 b2 = __float22bfloat162_rn(f);
-                            o[j] = *reinterpret_cast<const uint32_t*>(&b2);
+                    for (int h = 0; h < 2; ++h) {
+                        const uint4 v = *reinterpret_cast<const uint4*>(src + ((uint32_t)(blk * 2 + h) ^ sw) * 16);
+                        const uint32_t w[4] = {v.x ^ 0x80808080u, v.y ^ 0x80808080u, v.z ^ 0x80808080u, v.w ^ 0x80808080u};
+#pragma unroll
+                        for (int p = 0; p < 2; ++p) {
+                            uint32_t o[4];
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                const uint32_t word = w[2 * p + j / 2];
+                                // the byte q + 128 as the low mantissa byte of 2^23: subtracting 2^23 + 128 leaves q exactly
+                                float2 f = make_float2(__uint_as_float(__byte_perm(word, 0x4B000000u, 0x7540 + 2 * (j % 2))),
+                                                       __uint_as_float(__byte_perm(word, 0x4B000000u, 0x7541 + 2 * (j % 2))));
+                                f = mul2(add2(f, both(-8388736.f)), both(scale));
+                                const __nv_bfloat162 b2 = __float22bfloat162_rn(f);
+                                o[j] = *reinterpret_cast<const uint32_t*>(&b2);
+                            }
+                            const uint32_t chunk = (uint32_t)((blk % 2) * 4 + h * 2 + p);
+                            *reinterpret_cast<uint4*>(dst + (chunk ^ sw) * 16) = make_uint4(o[0], o[1], o[2], o[3]);
                         }
-                        const uint32_t chunk = (uint32_t)((blk % 2) * 4 + h * 2 + p);
-                        *reinterpret_cast<uint4*>(dst + (chunk ^ sw) * 16) = make_uint4(o[0], o[1], o[2], o[3]);
                     }
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0) arrive_first(&s.ready[sl]);
                 }
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                __syncwarp();
-                if (lane == 0) arrive_first(&s.ready[sl]);
-                if (++st == kStages) { st = 0; phase ^= 1u; }
-                if (++sl == kASlots) sl = 0;
             }
+            n += q.kb1 - q.kb0;
         }
         if (!ok) *failed = 1;
     }
