@@ -112,24 +112,28 @@ __global__ void __launch_bounds__(256) k_ckpt8_dequantize(const uint2* q, const 
 //   warps 2-5   epilogue: TMEM -> registers -> dw (or a partial sum), coalesced through a padded staging tile
 //   warps 6-21  q -> bf16 operand tile, two groups of eight warps on alternate runs: thread = (token, block of 32), the two
 //               16-byte pieces of q become four of bf16.  The exponents come by plain loads, kAhead of a group's runs ahead.
+// Every tile of a row of tiles converts the same operand again.  Beyond kFusedOut output columns the operand is therefore
+// converted once, to bf16 in the workspace (three more bytes of memory traffic per value), and k_wgrad<false> takes both
+// operands by TMA, without converter warps.  Measured, 8192 tokens x 4096, converted in the kernel / before it: 512 output
+// columns 54 / 61 us, 768 77 / 69, 2048 140 / 117, 4096 265 / 216 (a library bf16 product of operands already in bf16: 182).
 // Items are dealt out round-robin to the pairs: the whole tiles, as many as fill all pairs equally often, then the rest, each
 // cut along the tokens into `splits` runs so that they too keep all pairs busy; k_wgrad_join adds those up in order.
 // ------------------------------------------------------------------------------------------------
 constexpr int kTM = 256, kTN = 256, kTK = 64;    // of a pair
-constexpr int kStages = 5, kASlots = 4;
 constexpr int kRawBytes = kTK * 128, kABytes = kTK * 128 * 2, kBBytes = kTK * 128 * 2;
-constexpr int kWgThreads = 704;
 constexpr int kAhead = 4;
 constexpr int kPitch = 33;
 
+template <bool kFused>
 struct WgSmem {
-    alignas(1024) uint8_t raw[kStages][kRawBytes];
+    static constexpr int kStages = kFused ? 5 : 6, kASlots = kFused ? 4 : 6;
+    alignas(1024) uint8_t raw[kFused ? kStages : 1][kFused ? kRawBytes : 1024];
     alignas(1024) uint8_t b[kStages][kBBytes];
     alignas(1024) uint8_t a[kASlots][kABytes];
     float out[4][32 * kPitch];
-    alignas(8) uint64_t full[kStages];       // copies of a run have landed (this CTA's)
+    alignas(8) uint64_t full[kStages];       // fused: this CTA's copies of a run have landed; else, first CTA: both CTAs' have
     uint64_t empty[kStages];                 // the run's MMAs have read both CTAs' operands
-    uint64_t ready[kASlots];                 // first CTA: both CTAs' operands of a run are there
+    uint64_t ready[kASlots];                 // fused, first CTA: both CTAs' operands of a run are there
     uint64_t acc_full[2];
     uint64_t acc_empty[2];                   // first CTA: both CTAs have read the accumulator
     uint32_t tmem_base;
@@ -155,6 +159,14 @@ __device__ __forceinline__ uint32_t cluster_rank() {
 __device__ __forceinline__ void cluster_sync() {
     asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
+// tma_load_2d whose bytes are counted on the same barrier of the cluster's first CTA.
+__device__ __forceinline__ void tma_load_2d_first(void* dst, const CUtensorMap* tm, int x, int y, uint64_t* bar) {
+    uint32_t b;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(b) : "r"(smem_u32(bar)));
+    asm volatile(
+        "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, %3}], [%4];"
+        ::"r"(smem_u32(dst)), "l"(reinterpret_cast<uint64_t>(tm)), "r"(x), "r"(y), "r"(b) : "memory");
+}
 // One arrival on the same barrier of the cluster's first CTA.  What it announces -- operand tiles written and fenced for the
 // async proxy, accumulators read and fenced by tcgen05.fence -- is ordered by those fences; a release at cluster scope would
 // make the warp wait for the exponents that it has in flight (617 instead of 350 us).
@@ -175,10 +187,16 @@ __device__ __forceinline__ void umma2_commit(uint64_t* bar) {
                  ::"r"(smem_u32(bar)), "h"((uint16_t)3) : "memory");
 }
 
-__global__ void __launch_bounds__(kWgThreads, 1) k_wgrad(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_dy,
-                                                         const __grid_constant__ WgArgs a) {
+template <bool kFused>
+constexpr int kWgThreads = kFused ? 704 : 192;
+
+// tm_x: q, or the operand in bf16.
+template <bool kFused>
+__global__ void __launch_bounds__(kWgThreads<kFused>, 1) k_wgrad(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_dy,
+                                                                 const __grid_constant__ WgArgs a) {
+    constexpr int kStages = WgSmem<kFused>::kStages, kASlots = WgSmem<kFused>::kASlots;
     extern __shared__ uint8_t smem_raw[];
-    WgSmem& s = *reinterpret_cast<WgSmem*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+    WgSmem<kFused>& s = *reinterpret_cast<WgSmem<kFused>*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const int rank = (int)cluster_rank();
     const int pair = blockIdx.x / 2, pairs = gridDim.x / 2;
@@ -240,14 +258,23 @@ __global__ void __launch_bounds__(kWgThreads, 1) k_wgrad(const __grid_constant__
                 const Item q = item_of(it);
                 for (int kb = q.kb0; kb < q.kb1; ++kb) {
                     if (round > 0 && !mbar_wait(&s.empty[st], (round - 1) & 1)) { *failed = 1; break; }
-                    mbar_expect_tx(&s.full[st], kRawBytes + kBBytes);
-                    tma_load_2d(s.raw[st], &tm_q, q.m0 + rank * 128, kb * kTK, &s.full[st]);
-                    tma_load_2d(s.b[st], &tm_dy, q.n0 + rank * 128, kb * kTK, &s.full[st]);
-                    tma_load_2d(s.b[st] + 8192, &tm_dy, q.n0 + rank * 128 + 64, kb * kTK, &s.full[st]);
+                    const int m = q.m0 + rank * 128, n = q.n0 + rank * 128, t = kb * kTK;
+                    if constexpr (kFused) {
+                        mbar_expect_tx(&s.full[st], kRawBytes + kBBytes);
+                        tma_load_2d(s.raw[st], &tm_x, m, t, &s.full[st]);
+                        tma_load_2d(s.b[st], &tm_dy, n, t, &s.full[st]);
+                        tma_load_2d(s.b[st] + 8192, &tm_dy, n + 64, t, &s.full[st]);
+                    } else {
+                        if (rank == 0) mbar_expect_tx(&s.full[st], 2 * (kABytes + kBBytes));
+                        tma_load_2d_first(s.a[st], &tm_x, m, t, &s.full[st]);
+                        tma_load_2d_first(s.a[st] + 8192, &tm_x, m + 64, t, &s.full[st]);
+                        tma_load_2d_first(s.b[st], &tm_dy, n, t, &s.full[st]);
+                        tma_load_2d_first(s.b[st] + 8192, &tm_dy, n + 64, t, &s.full[st]);
+                    }
                     if (++st == kStages) { st = 0; ++round; }
                 }
             }
-            if (*failed)                             // copies in flight land before the CTA's shared memory is released
+            if (*failed && (kFused || rank == 0))    // copies in flight land before the CTAs' shared memory is released
                 for (uint32_t i = 0; i < kStages; ++i) mbar_wait(&s.full[i], (round + (i < st ? 0u : 1u)) & 1u, 4096u);
         }
     } else if (warp == 1) {
@@ -262,7 +289,7 @@ __global__ void __launch_bounds__(kWgThreads, 1) k_wgrad(const __grid_constant__
                 if (i >= 2 && !mbar_wait(&s.acc_empty[ab], ((i / 2) - 1) & 1)) { ok = false; break; }
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 for (int kb = q.kb0; kb < q.kb1; ++kb) {
-                    if (!mbar_wait(&s.ready[sl], sl_phase)) { ok = false; break; }
+                    if (!mbar_wait(kFused ? &s.ready[sl] : &s.full[sl], sl_phase)) { ok = false; break; }
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                     const uint32_t a0 = smem_u32(s.a[sl]), b0 = smem_u32(s.b[st]);
 #pragma unroll
@@ -322,7 +349,7 @@ __global__ void __launch_bounds__(kWgThreads, 1) k_wgrad(const __grid_constant__
                 __syncwarp();
             }
         }
-    } else {                                         // ---- q -> bf16 operand tile
+    } else if constexpr (kFused) {                   // ---- q -> bf16 operand tile
         const int tid = (threadIdx.x - 192) % 256, group = (threadIdx.x - 192) / 256;
         const int r = tid % kTK, blk = tid / kTK;    // token of the run, block of 32 columns
         const uint32_t sw = (uint32_t)(r & 7);
@@ -428,13 +455,15 @@ int grid_for(size_t n, int per_cta) {
 }
 
 constexpr int kSms = 148;
+constexpr int kFusedOut = 512;   // output columns up to which the operand is converted in the kernel
 constexpr int kMinRuns = 4;      // runs of 64 tokens that a part of a cut tile has at least
 
 // How the work is cut: whole output tiles for all pairs of SMs equally often, the rest in runs of tokens.
 struct WgPlan {
     int tiles_m, tiles_n, whole, rest, splits, kb_per_split;
-    bool repack;
-    size_t ld8, part_bytes, pack_bytes;
+    bool repack, fused;
+    size_t ld8, part_bytes, pack_bytes, x_bytes;
+    size_t bytes() const { return part_bytes + pack_bytes + x_bytes; }
 };
 bool plan_of(uint64_t T, uint64_t D, uint64_t N, const void* dy, uint64_t ld_dy, WgPlan* out) {
     WgPlan p{};
@@ -453,6 +482,8 @@ bool plan_of(uint64_t T, uint64_t D, uint64_t N, const void* dy, uint64_t ld_dy,
     p.ld8 = (N + 7) / 8 * 8;
     p.part_bytes = p.splits > 1 ? (size_t)p.splits * p.rest * kTM * kTN * 4 : 0;
     p.pack_bytes = p.repack ? up256((size_t)T * p.ld8 * 2) : 0;
+    p.fused = N <= (uint64_t)kFusedOut;
+    p.x_bytes = p.fused ? 0 : up256((size_t)T * ((D + 31) / 32 * 32) * 2);
     *out = p;
     return true;
 }
@@ -511,7 +542,7 @@ extern "C" int abs_ckpt8_dequantize(const int8_t* q, const uint8_t* e, uint64_t 
 extern "C" size_t abs_ckpt8_wgrad_workspace(uint64_t tokens, uint64_t width, uint64_t out, const void* dy, uint64_t ld_dy) {
     if (tokens > 0x7fffffffull || width > 0x7fffffffull || out > 0x7fffffffull) return 0;
     WgPlan p;
-    return plan_of(tokens, width, out, dy, ld_dy, &p) ? p.part_bytes + p.pack_bytes : 0;
+    return plan_of(tokens, width, out, dy, ld_dy, &p) ? p.bytes() : 0;
 }
 
 extern "C" int abs_ckpt8_wgrad(const int8_t* q, const uint8_t* e, const void* dy, uint64_t ld_dy, uint64_t tokens, uint64_t width,
@@ -529,9 +560,9 @@ extern "C" int abs_ckpt8_wgrad(const int8_t* q, const uint8_t* e, const void* dy
     }
     WgPlan p;
     if (!plan_of(tokens, width, out, dy, ld_dy, &p)) return thread_error(ABS_ELIMIT, "too many output tiles");
-    if (p.part_bytes + p.pack_bytes) {
+    if (p.bytes()) {
         if (!workspace || misaligned(workspace, 256)) return thread_error(ABS_EINVAL, "workspace must be non-NULL and 256-byte aligned");
-        if (workspace_bytes < p.part_bytes + p.pack_bytes) return thread_error(ABS_ENOMEM, "workspace too small");
+        if (workspace_bytes < p.bytes()) return thread_error(ABS_ENOMEM, "workspace too small");
     }
     float* part = static_cast<float*>(workspace);
     if (p.repack) {
@@ -543,17 +574,30 @@ extern "C" int abs_ckpt8_wgrad(const int8_t* q, const uint8_t* e, const void* dy
         ld_dy = p.ld8;
     }
     const uint64_t W = (width + 31) / 32 * 32;
-    CUtensorMap tq, td;
-    if (!encode_2d(&tq, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, const_cast<int8_t*>(q), tokens, W, kTK, 128) ||
+    CUtensorMap tx, td;
+    bf16* x = reinterpret_cast<bf16*>(static_cast<char*>(workspace) + p.part_bytes + p.pack_bytes);
+    if (!p.fused) {
+        const size_t n8 = (size_t)tokens * (W / 8);
+        r = launch_kernel(k_ckpt8_dequantize<bf16, true>, grid_for(n8, 256), 256, 0, s, true, reinterpret_cast<const uint2*>(q), e, x, (size_t)W, n8,
+                          (uint32_t)(W / 8), (int)W);
+        if (r != cudaSuccess) return thread_error(ABS_ECUDA, cudaGetErrorString(r));
+    }
+    if (!(p.fused ? encode_2d(&tx, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, const_cast<int8_t*>(q), tokens, W, kTK, 128)
+                  : encode_2d(&tx, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, x, tokens, W, kTK, 64)) ||
         !encode_2d(&td, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(dy), tokens, out, kTK, 64, ld_dy))
         return thread_error(ABS_ECUDA, "cuTensorMapEncodeTiled failed");
     WgArgs a{};
     a.e = e; a.e_ld = W / 32; a.T = (int)tokens; a.D = (int)width; a.N = (int)out;
     a.tiles_n = p.tiles_n; a.whole = p.whole; a.rest = p.rest; a.splits = p.splits; a.kb_per_split = p.kb_per_split;
     a.dw = dw; a.ld = ld_dw; a.part = part; a.accumulate = accumulate != 0;
-    r = allow_smem<k_wgrad>();
-    const int items = p.whole + p.rest * p.splits;
-    if (r == cudaSuccess) r = launch_cluster(k_wgrad, 2 * std::min(items, kSms / 2), 2, kWgThreads, sizeof(WgSmem) + 1024, s, tq, td, a);
+    const int grid = 2 * std::min(p.whole + p.rest * p.splits, kSms / 2);
+    if (p.fused) {
+        r = allow_smem<k_wgrad<true>>();
+        if (r == cudaSuccess) r = launch_cluster(k_wgrad<true>, grid, 2, kWgThreads<true>, sizeof(WgSmem<true>) + 1024, s, tx, td, a);
+    } else {
+        r = allow_smem<k_wgrad<false>>();
+        if (r == cudaSuccess) r = launch_cluster(k_wgrad<false>, grid, 2, kWgThreads<false>, sizeof(WgSmem<false>) + 1024, s, tx, td, a);
+    }
     if (r == cudaSuccess && p.splits > 1) r = launch_kernel(k_wgrad_join, std::min(p.rest * kTM, kSms * 8), 256, 0, s, true, a);
     return r == cudaSuccess ? ABS_OK : thread_error(ABS_ECUDA, cudaGetErrorString(r));
 }
