@@ -30,72 +30,198 @@ __device__ __forceinline__ float pow2_of(uint32_t e) {
 }
 __device__ __forceinline__ float inv_pow2_of(uint32_t e) { return __uint_as_float((254u - e) << 23); }   // e <= 249
 
-// Eight consecutive values per thread, so that four neighbouring lanes hold a block.  kWide: the row allows 16-byte loads.
+// n / d and n % d by a multiplication, for n < 2^31 (d >= 1); larger ranges take the division.
+struct Divide {
+    uint32_t d, mul, shift;
+    int small;               // all n that are asked for are below 2^31
+};
+__device__ __forceinline__ size_t divide(size_t n, const Divide& v, uint32_t* rest) {
+    if (v.small) {
+        const uint32_t m = (uint32_t)n, q = v.d == 1u ? m : __umulhi(m, v.mul) >> v.shift;
+        *rest = m - q * v.d;
+        return q;
+    }
+    const size_t q = n / v.d;
+    *rest = (uint32_t)(n - q * v.d);
+    return q;
+}
+
+struct PackArgs {
+    size_t ld, T;
+    int D;
+    int pieces;              // of eight values in a stored row: W / 8
+    Divide per_row;          // by the units of a row
+    size_t units;
+};
+constexpr int kUnroll = 4;   // units whose loads are issued together
+
+// A unit is eight values; the four lanes of a block are neighbours.  kWide: the rows allow 16-byte loads.
 template <typename T, bool kWide>
-__global__ void __launch_bounds__(256) k_ckpt8_quantize(const T* x, size_t ld, size_t n8, uint32_t per_row, int D, uint2* q, uint8_t* e) {
+__global__ void __launch_bounds__(256) k_ckpt8_quantize(const T* x, const __grid_constant__ PackArgs a, uint2* q, uint8_t* e) {
     pdl_wait();
     pdl_trigger();
-    for (size_t i0 = (size_t)blockIdx.x * 256; i0 < n8; i0 += (size_t)gridDim.x * 256) {
-        const size_t i = i0 + threadIdx.x;           // n8 is a multiple of 4: a block's lanes are all in or all out
-        const size_t t = i / per_row;
-        const int c = (int)(i - t * per_row) * 8;
-        float v[8];
-        if (i < n8) {
-            const T* p = x + t * ld + c;
-            if (kWide && c + 8 <= D) {
+    // units is a multiple of 4: a block's lanes are all in or all out; all lanes of a warp stay in the loop for the exchange
+    for (size_t i0 = (size_t)blockIdx.x * 256 * kUnroll; i0 < a.units; i0 += (size_t)gridDim.x * 256 * kUnroll) {
+        float v[kUnroll][8];
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+            const size_t i = i0 + u * 256 + threadIdx.x;
+            uint32_t piece;
+            const size_t t = divide(i < a.units ? i : 0, a.per_row, &piece);
+            const int c = i < a.units ? (int)piece * 8 : a.D;
+            const T* p = x + t * a.ld + c;
+            if (kWide && c + 8 <= a.D) {
                 constexpr int kN = kVec<T>;
 #pragma unroll
-                for (int k = 0; k < 8 / kN; ++k) Pack<T, kN>::load(p + k * kN, *reinterpret_cast<float(*)[kN]>(v + k * kN));
+                for (int k = 0; k < 8 / kN; ++k) Pack<T, kN>::load(p + k * kN, *reinterpret_cast<float(*)[kN]>(v[u] + k * kN));
             } else {
 #pragma unroll
-                for (int k = 0; k < 8; ++k) v[k] = c + k < D ? to_f(p[k]) : 0.f;
+                for (int k = 0; k < 8; ++k) v[u][k] = c + k < a.D ? to_f(p[k]) : 0.f;
             }
-        } else {
-#pragma unroll
-            for (int k = 0; k < 8; ++k) v[k] = 0.f;
         }
-        uint32_t m = 0;
 #pragma unroll
-        for (int k = 0; k < 8; ++k) m = max(m, __float_as_uint(v[k]) & 0x7FFFFFFFu);
-        m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
-        m = max(m, __shfl_xor_sync(0xffffffffu, m, 2));
-        const uint32_t code = block_exponent(m);
-        const float inv = code == 255u ? 0.f : inv_pow2_of(code);
-        uint32_t w[2] = {0u, 0u};
+        for (int u = 0; u < kUnroll; ++u) {
+            const size_t i = i0 + u * 256 + threadIdx.x;
+            uint32_t m = 0;
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            const int b = code == 255u ? 0 : __float2int_rn(v[k] * inv);
-            w[k / 4] |= ((uint32_t)b & 0xFFu) << (8 * (k % 4));
-        }
-        if (i < n8) {
-            q[i] = make_uint2(w[0], w[1]);
-            if (i % 4 == 0) e[i / 4] = (uint8_t)code;
+            for (int k = 0; k < 8; ++k) m = max(m, __float_as_uint(v[u][k]) & 0x7FFFFFFFu);
+            m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
+            m = max(m, __shfl_xor_sync(0xffffffffu, m, 2));
+            const uint32_t code = block_exponent(m);
+            const float inv = code == 255u ? 0.f : inv_pow2_of(code);
+            // the sum with 1.5 2^23 is rounded to an integer (to nearest even), whose low byte is q
+            uint32_t w[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                uint32_t b[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) b[k] = __float_as_uint(__fadd_rn(v[u][4 * h + k] * inv, 12582912.f));
+                w[h] = code == 255u ? 0u : __byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410);
+            }
+            if (i < a.units) {
+                q[i] = make_uint2(w[0], w[1]);
+                if (i % 4 == 0) e[i / 4] = (uint8_t)code;
+            }
         }
     }
 }
 
-template <typename T, bool kWide>
-__global__ void __launch_bounds__(256) k_ckpt8_dequantize(const uint2* q, const uint8_t* e, T* x, size_t ld, size_t n8, uint32_t per_row, int D) {
+// The values of kV stored bytes (raw) with exponent byte `code`, as a 16-byte piece.
+template <typename T>
+__device__ __forceinline__ void unpack8(const uint32_t (&raw)[kVec<T> / 4], uint32_t code, float2 (&v)[kPairs<T>]) {
+    const float s = pow2_of(code);
+#pragma unroll
+    for (int k = 0; k < kPairs<T>; ++k) {
+        const uint32_t w = raw[k / 2] ^ 0x80808080u;     // the byte q + 128 as the low mantissa byte of 2^23
+        const float2 f = make_float2(__uint_as_float(__byte_perm(w, 0x4B000000u, 0x7540 + 2 * (k % 2))),
+                                     __uint_as_float(__byte_perm(w, 0x4B000000u, 0x7541 + 2 * (k % 2))));
+        v[k] = mul2(add2(f, both(-8388736.f)), both(s));
+    }
+}
+
+// Rows on 16-byte boundaries: a unit is one 16-byte piece of a row.
+template <typename T>
+__global__ void __launch_bounds__(256) k_ckpt8_dequantize(const uint8_t* q, const uint8_t* e, T* x, const __grid_constant__ PackArgs a) {
+    constexpr int kV = kVec<T>;
+    const size_t width = (size_t)a.pieces * 8;           // of a stored row
     pdl_wait();
     pdl_trigger();
-    for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < n8; i += (size_t)gridDim.x * 256) {
-        const size_t t = i / per_row;
-        const int c = (int)(i - t * per_row) * 8;
-        if (c >= D) continue;
-        const uint2 w = q[i];
-        const float s = pow2_of(e[i / 4]);
-        float v[8];
+    for (size_t i0 = (size_t)blockIdx.x * 256 * kUnroll + threadIdx.x; i0 < a.units; i0 += (size_t)gridDim.x * 256 * kUnroll) {
+        uint32_t raw[kUnroll][kV / 4], code[kUnroll], piece[kUnroll];
+        size_t t[kUnroll];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] = (float)(int)(int8_t)((k < 4 ? w.x : w.y) >> (8 * (k % 4))) * s;
-        T* p = x + t * ld + c;
-        if (kWide && c + 8 <= D) {
-            constexpr int kN = kVec<T>;
+        for (int u = 0; u < kUnroll; ++u) {
+            const size_t i = i0 + u * 256;
+            t[u] = divide(i < a.units ? i : 0, a.per_row, &piece[u]);
+            const size_t at = t[u] * width + (size_t)piece[u] * kV;
+            code[u] = e[at / 32];
+            if (kV == 8) {
+                const uint2 r = *reinterpret_cast<const uint2*>(q + at);
+                raw[u][0] = r.x;
+                raw[u][kV / 4 - 1] = r.y;
+            } else raw[u][0] = *reinterpret_cast<const uint32_t*>(q + at);
+        }
 #pragma unroll
-            for (int k = 0; k < 8 / kN; ++k) Pack<T, kN>::store(p + k * kN, *reinterpret_cast<const float(*)[kN]>(v + k * kN));
-        } else {
+        for (int u = 0; u < kUnroll; ++u) {
+            if (i0 + u * 256 >= a.units) break;
+            float2 v[kPairs<T>];
+            unpack8<T>(raw[u], code[u], v);
+            const int c = (int)piece[u] * kV;
+            T* p = x + t[u] * a.ld + c;
+            if (c + kV <= a.D) *reinterpret_cast<uint4*>(p) = pack(v, T());
+            else {
 #pragma unroll
-            for (int k = 0; k < 8; ++k)
-                if (c + k < D) p[k] = from_f<T>(v[k]);
+                for (int k = 0; k < kV; ++k)
+                    if (c + k < a.D) p[k] = from_f<T>(k % 2 ? v[k / 2].y : v[k / 2].x);
+            }
+        }
+    }
+}
+
+// Rows that start anywhere: a unit is the part of a row that kLanes lanes make together, a piece each.  The pieces are put
+// down in shared memory at the offset that the part has from a 16-byte boundary in memory, and leave from there in whole
+// 16-byte pieces, the ends as single elements (element stores straight from the registers took four times as long).
+template <typename T, int kLanes>
+__global__ void __launch_bounds__(256) k_ckpt8_dequantize_any(const uint8_t* q, const uint8_t* e, T* x, const __grid_constant__ PackArgs a) {
+    constexpr int kV = kVec<T>, kGroups = 256 / kLanes, kBuf = kLanes * 16 + 16;
+    __shared__ __align__(16) uint8_t buf[kGroups * kBuf];
+    const int lane = threadIdx.x % kLanes;
+    uint8_t* mine = buf + (threadIdx.x / kLanes) * kBuf;
+    const size_t width = (size_t)a.pieces * 8;
+    pdl_wait();
+    pdl_trigger();
+    // all lanes of a warp stay in the loop
+    for (size_t g0 = (size_t)blockIdx.x * kGroups * kUnroll; g0 < a.units; g0 += (size_t)gridDim.x * kGroups * kUnroll) {
+        uint32_t raw[kUnroll][kV / 4], code[kUnroll], step[kUnroll];
+        size_t t[kUnroll];
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+            const size_t i = g0 + u * kGroups + threadIdx.x / kLanes;
+            t[u] = divide(i < a.units ? i : 0, a.per_row, &step[u]);
+            const int c = ((int)step[u] * kLanes + lane) * kV;
+            const size_t at = t[u] * width + (size_t)c;
+#pragma unroll
+            for (int k = 0; k < kV / 4; ++k) raw[u][k] = 0u;
+            code[u] = 0u;
+            if (c < a.D) {
+                code[u] = e[at / 32];
+                if (kV == 8) {
+                    const uint2 r = *reinterpret_cast<const uint2*>(q + at);
+                    raw[u][0] = r.x;
+                    raw[u][kV / 4 - 1] = r.y;
+                } else raw[u][0] = *reinterpret_cast<const uint32_t*>(q + at);
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+            float2 v[kPairs<T>];
+            unpack8<T>(raw[u], code[u], v);
+            const uint4 out = pack(v, T());
+            const uint32_t w[4] = {out.x, out.y, out.z, out.w};
+            const int c0 = (int)step[u] * kLanes * kV, c1 = min(a.D, c0 + kLanes * kV);      // the part of the row
+            const uintptr_t to = reinterpret_cast<uintptr_t>(x + t[u] * a.ld + c0);
+            const uint32_t off = (uint32_t)(to & 15);
+            uint8_t* put = mine + off + lane * 16;
+            if (sizeof(T) == 4 || off % 4 == 0) {
+#pragma unroll
+                for (int k = 0; k < 4; ++k) reinterpret_cast<uint32_t*>(put)[k] = w[k];
+            } else {
+#pragma unroll
+                for (int k = 0; k < 8; ++k) reinterpret_cast<uint16_t*>(put)[k] = (uint16_t)(w[k / 2] >> (16 * (k % 2)));
+            }
+            __syncwarp();
+            if (g0 + u * kGroups + threadIdx.x / kLanes < a.units) {
+                const uint32_t end = off + (uint32_t)(c1 - c0) * sizeof(T);              // in the buffer
+                T* base = reinterpret_cast<T*>(to - off);
+                const T* have = reinterpret_cast<const T*>(mine);
+                for (uint32_t g = (uint32_t)lane * 16; g < end; g += kLanes * 16)        // at most two
+                    if (g >= off && g + 16 <= end) reinterpret_cast<uint4*>(base)[g / 16] = reinterpret_cast<const uint4*>(mine)[g / 16];
+                const uint32_t head = min(off ? 16u : 0u, end) / (uint32_t)sizeof(T);
+                for (uint32_t k = off / sizeof(T) + lane; k < head; k += kLanes) base[k] = have[k];
+                const uint32_t tail = max(end & ~15u, off ? 16u : 0u) / (uint32_t)sizeof(T);
+                for (uint32_t k = tail + lane; k < end / sizeof(T); k += kLanes) base[k] = have[k];
+            }
+            __syncwarp();
         }
     }
 }
@@ -114,8 +240,10 @@ __global__ void __launch_bounds__(256) k_ckpt8_dequantize(const uint2* q, const 
 //               16-byte pieces of q become four of bf16.  The exponents come by plain loads, kAhead of a group's runs ahead.
 // Every tile of a row of tiles converts the same operand again.  Beyond kFusedOut output columns the operand is therefore
 // converted once, to bf16 in the workspace (three more bytes of memory traffic per value), and k_wgrad<false> takes both
-// operands by TMA, without converter warps.  Measured, 8192 tokens x 4096, converted in the kernel / before it: 512 output
+// operands by TMA, without converter warps (from kFusedTokens tokens on).  Measured, 8192 tokens x 4096, converted in the kernel / before it: 512 output
 // columns 54 / 61 us, 768 77 / 69, 2048 140 / 117, 4096 265 / 216 (a library bf16 product of operands already in bf16: 182).
+// The kernel is launched in plain stream order and starts no successor early: chained by programmatic dependent launch, calls
+// in a row hung (each of its waits on a barrier is bounded; the allocation of TMEM and the cluster's barrier are not).
 // Items are dealt out round-robin to the pairs: the whole tiles, as many as fill all pairs equally often, then the rest, each
 // cut along the tokens into `splits` runs so that they too keep all pairs busy; k_wgrad_join adds those up in order.
 // ------------------------------------------------------------------------------------------------
@@ -224,8 +352,6 @@ __global__ void __launch_bounds__(kWgThreads<kFused>, 1) k_wgrad(const __grid_co
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem = s.tmem_base;
     volatile uint32_t* failed = &s.failed;
-    pdl_wait();
-    pdl_trigger();
 
     struct Item {
         int m0, n0, kb0, kb1;        // first row and column of the pair's tile, runs of 64 tokens
@@ -455,8 +581,9 @@ int grid_for(size_t n, int per_cta) {
 }
 
 constexpr int kSms = 148;
-constexpr int kFusedOut = 512;   // output columns up to which the operand is converted in the kernel
-constexpr int kMinRuns = 4;      // runs of 64 tokens that a part of a cut tile has at least
+constexpr int kFusedOut = 512;   // output columns up to which the operand is converted in the kernel ..
+constexpr int kFusedTokens = 1024;   // .. or tokens, where the extra launch costs more than the repeated conversion
+constexpr int kMinRuns = 12;     // runs of 64 tokens that a part of a cut tile has at least: shorter ones do not pay for the join
 
 // How the work is cut: whole output tiles for all pairs of SMs equally often, the rest in runs of tokens.
 struct WgPlan {
@@ -482,7 +609,7 @@ bool plan_of(uint64_t T, uint64_t D, uint64_t N, const void* dy, uint64_t ld_dy,
     p.ld8 = (N + 7) / 8 * 8;
     p.part_bytes = p.splits > 1 ? (size_t)p.splits * p.rest * kTM * kTN * 4 : 0;
     p.pack_bytes = p.repack ? up256((size_t)T * p.ld8 * 2) : 0;
-    p.fused = N <= (uint64_t)kFusedOut;
+    p.fused = N <= (uint64_t)kFusedOut || T <= (uint64_t)kFusedTokens;
     p.x_bytes = p.fused ? 0 : up256((size_t)T * ((D + 31) / 32 * 32) * 2);
     *out = p;
     return true;
@@ -493,49 +620,87 @@ bool plan_of(uint64_t T, uint64_t D, uint64_t N, const void* dy, uint64_t ld_dy,
 
 using namespace abs_sgd;
 
+namespace abs_sgd {
+namespace {
+// The arguments for rows of `per_row` units.
+PackArgs pack_args(uint64_t tokens, uint64_t width, uint64_t ld, uint32_t per_row) {
+    PackArgs a{};
+    a.ld = (size_t)ld;
+    a.T = (size_t)tokens;
+    a.D = (int)width;
+    a.pieces = (int)((width + 31) / 32 * 4);
+    a.units = a.T * per_row;
+    Divide& v = a.per_row;
+    v.d = per_row;
+    v.small = a.units < 0x7fffffffull;
+    uint32_t log = 0;
+    while ((1ull << log) < per_row) ++log;
+    if (log) {               // mul = ceil(2^(31 + log) / d) < 2^32; exact for n < 2^31
+        v.mul = (uint32_t)(((1ull << (31 + log)) + per_row - 1) / per_row);
+        v.shift = log - 1;
+    }
+    return a;
+}
+int pack_grid(size_t units, int per_cta) {
+    const size_t want = (units + (size_t)per_cta * kUnroll - 1) / ((size_t)per_cta * kUnroll);
+    return (int)std::min<size_t>(want, kSms * 8);
+}
+const char* check_ckpt(const void* x, uint64_t ld, uint32_t dtype, uint64_t tokens, uint64_t width, const void* q, const void* e, int* code) {
+    *code = ABS_EINVAL;
+    if (dtype != ABS_F32 && dtype != ABS_BF16) return "dtype must be ABS_F32 or ABS_BF16";
+    if (width == 0 || ld < width) return "width must be at least 1 and ld_x at least width";
+    if (width > 0x7fffff00ull) {
+        *code = ABS_ELIMIT;
+        return "width exceeds 2^31 - 256";
+    }
+    if (tokens && (!x || !q || !e)) return "x, q and e must not be NULL";
+    if (misaligned(x, dtype == ABS_F32 ? 4 : 2) || misaligned(q, 16) || misaligned(e, 4)) return "x must be aligned to its elements, q to 16 and e to 4 bytes";
+    return nullptr;
+}
+template <typename T>
+cudaError_t quantize(const void* x, uint64_t ld, uint64_t tokens, uint64_t width, int8_t* q, uint8_t* e, cudaStream_t s) {
+    const bool wide = !misaligned(x, 16) && ld * sizeof(T) % 16 == 0;
+    const PackArgs a = pack_args(tokens, width, ld, (uint32_t)((width + 31) / 32 * 4));
+    return launch_kernel(wide ? k_ckpt8_quantize<T, true> : k_ckpt8_quantize<T, false>, pack_grid(a.units, 256), 256, 0, s, true, static_cast<const T*>(x), a,
+                         reinterpret_cast<uint2*>(q), e);
+}
+template <typename T, int kLanes>
+cudaError_t dequantize_any(const int8_t* q, const uint8_t* e, void* x, uint64_t ld, uint64_t tokens, uint64_t width, uint32_t pieces, cudaStream_t s) {
+    const PackArgs a = pack_args(tokens, width, ld, (pieces + kLanes - 1) / kLanes);
+    return launch_kernel(k_ckpt8_dequantize_any<T, kLanes>, pack_grid(a.units, 256 / kLanes), 256, 0, s, true, reinterpret_cast<const uint8_t*>(q), e,
+                         static_cast<T*>(x), a);
+}
+template <typename T>
+cudaError_t dequantize(const int8_t* q, const uint8_t* e, void* x, uint64_t ld, uint64_t tokens, uint64_t width, cudaStream_t s) {
+    const uint32_t pieces = (uint32_t)((width + kVec<T> - 1) / kVec<T>);
+    if (!misaligned(x, 16) && ld * sizeof(T) % 16 == 0) {
+        const PackArgs a = pack_args(tokens, width, ld, pieces);
+        return launch_kernel(k_ckpt8_dequantize<T>, pack_grid(a.units, 256), 256, 0, s, true, reinterpret_cast<const uint8_t*>(q), e, static_cast<T*>(x), a);
+    }
+    // lanes of a row's part: as many as the row has pieces, within a warp
+    return pieces <= 4 ? dequantize_any<T, 4>(q, e, x, ld, tokens, width, pieces, s) : pieces <= 8 ? dequantize_any<T, 8>(q, e, x, ld, tokens, width, pieces, s)
+         : pieces <= 16 ? dequantize_any<T, 16>(q, e, x, ld, tokens, width, pieces, s) : dequantize_any<T, 32>(q, e, x, ld, tokens, width, pieces, s);
+}
+}  // namespace
+}  // namespace abs_sgd
+
 extern "C" int abs_ckpt8_quantize(const void* x, uint64_t ld_x, uint32_t dtype, uint64_t tokens, uint64_t width, int8_t* q, uint8_t* e,
                                   void* stream) {
-    if (dtype != ABS_F32 && dtype != ABS_BF16) return thread_error(ABS_EINVAL, "dtype must be ABS_F32 or ABS_BF16");
-    const size_t es = dtype == ABS_F32 ? 4 : 2;
-    if (width == 0 || ld_x < width) return thread_error(ABS_EINVAL, "width must be at least 1 and ld_x at least width");
-    if (width > 0x7fffffe0ull) return thread_error(ABS_ELIMIT, "width exceeds 2^31 - 32");
+    int code = 0;
+    if (const char* why = check_ckpt(x, ld_x, dtype, tokens, width, q, e, &code)) return thread_error(code, why);
     if (tokens == 0) return ABS_OK;
-    if (!x || !q || !e) return thread_error(ABS_EINVAL, "x, q and e must not be NULL");
-    if (misaligned(x, es) || misaligned(q, 16) || misaligned(e, 4)) return thread_error(ABS_EINVAL, "x must be aligned to its elements, q to 16 and e to 4 bytes");
-    const uint32_t per_row = (uint32_t)((width + 31) / 32 * 4);
-    const size_t n8 = (size_t)tokens * per_row;
-    const bool wide = !misaligned(x, 16) && ld_x * es % 16 == 0;
-    const int grid = grid_for(n8, 256);
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    auto go = [&](auto* p) {
-        using T = std::remove_cv_t<std::remove_pointer_t<decltype(p)>>;
-        return launch_kernel(wide ? k_ckpt8_quantize<T, true> : k_ckpt8_quantize<T, false>, grid, 256, 0, s, true, (const T*)x, (size_t)ld_x, n8,
-                             per_row, (int)width, reinterpret_cast<uint2*>(q), e);
-    };
-    const cudaError_t r = dtype == ABS_F32 ? go((float*)nullptr) : go((bf16*)nullptr);
+    const cudaError_t r = dtype == ABS_F32 ? quantize<float>(x, ld_x, tokens, width, q, e, s) : quantize<bf16>(x, ld_x, tokens, width, q, e, s);
     return r == cudaSuccess ? ABS_OK : thread_error(ABS_ECUDA, cudaGetErrorString(r));
 }
 
 extern "C" int abs_ckpt8_dequantize(const int8_t* q, const uint8_t* e, uint64_t tokens, uint64_t width, void* x, uint64_t ld_x, uint32_t dtype,
                                     void* stream) {
-    if (dtype != ABS_F32 && dtype != ABS_BF16) return thread_error(ABS_EINVAL, "dtype must be ABS_F32 or ABS_BF16");
-    const size_t es = dtype == ABS_F32 ? 4 : 2;
-    if (width == 0 || ld_x < width) return thread_error(ABS_EINVAL, "width must be at least 1 and ld_x at least width");
-    if (width > 0x7fffffe0ull) return thread_error(ABS_ELIMIT, "width exceeds 2^31 - 32");
+    int code = 0;
+    if (const char* why = check_ckpt(x, ld_x, dtype, tokens, width, q, e, &code)) return thread_error(code, why);
     if (tokens == 0) return ABS_OK;
-    if (!x || !q || !e) return thread_error(ABS_EINVAL, "x, q and e must not be NULL");
-    if (misaligned(x, es) || misaligned(q, 16) || misaligned(e, 4)) return thread_error(ABS_EINVAL, "x must be aligned to its elements, q to 16 and e to 4 bytes");
-    const uint32_t per_row = (uint32_t)((width + 31) / 32 * 4);
-    const size_t n8 = (size_t)tokens * per_row;
-    const bool wide = !misaligned(x, 16) && ld_x * es % 16 == 0;
-    const int grid = grid_for(n8, 256);
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    auto go = [&](auto* p) {
-        using T = std::remove_cv_t<std::remove_pointer_t<decltype(p)>>;
-        return launch_kernel(wide ? k_ckpt8_dequantize<T, true> : k_ckpt8_dequantize<T, false>, grid, 256, 0, s, true,
-                             reinterpret_cast<const uint2*>(q), e, static_cast<T*>(x), (size_t)ld_x, n8, per_row, (int)width);
-    };
-    const cudaError_t r = dtype == ABS_F32 ? go((float*)nullptr) : go((bf16*)nullptr);
+    const cudaError_t r = dtype == ABS_F32 ? dequantize<float>(q, e, x, ld_x, tokens, width, s) : dequantize<bf16>(q, e, x, ld_x, tokens, width, s);
     return r == cudaSuccess ? ABS_OK : thread_error(ABS_ECUDA, cudaGetErrorString(r));
 }
 
@@ -577,9 +742,7 @@ extern "C" int abs_ckpt8_wgrad(const int8_t* q, const uint8_t* e, const void* dy
     CUtensorMap tx, td;
     bf16* x = reinterpret_cast<bf16*>(static_cast<char*>(workspace) + p.part_bytes + p.pack_bytes);
     if (!p.fused) {
-        const size_t n8 = (size_t)tokens * (W / 8);
-        r = launch_kernel(k_ckpt8_dequantize<bf16, true>, grid_for(n8, 256), 256, 0, s, true, reinterpret_cast<const uint2*>(q), e, x, (size_t)W, n8,
-                          (uint32_t)(W / 8), (int)W);
+        r = dequantize<bf16>(q, e, x, W, tokens, W, s);
         if (r != cudaSuccess) return thread_error(ABS_ECUDA, cudaGetErrorString(r));
     }
     if (!(p.fused ? encode_2d(&tx, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, const_cast<int8_t*>(q), tokens, W, kTK, 128)
@@ -593,12 +756,12 @@ extern "C" int abs_ckpt8_wgrad(const int8_t* q, const uint8_t* e, const void* dy
     const int grid = 2 * std::min(p.whole + p.rest * p.splits, kSms / 2);
     if (p.fused) {
         r = allow_smem<k_wgrad<true>>();
-        if (r == cudaSuccess) r = launch_cluster(k_wgrad<true>, grid, 2, kWgThreads<true>, sizeof(WgSmem<true>) + 1024, s, tx, td, a);
+        if (r == cudaSuccess) r = launch_cluster(k_wgrad<true>, grid, 2, false, kWgThreads<true>, sizeof(WgSmem<true>) + 1024, s, tx, td, a);
     } else {
         r = allow_smem<k_wgrad<false>>();
-        if (r == cudaSuccess) r = launch_cluster(k_wgrad<false>, grid, 2, kWgThreads<false>, sizeof(WgSmem<false>) + 1024, s, tx, td, a);
+        if (r == cudaSuccess) r = launch_cluster(k_wgrad<false>, grid, 2, false, kWgThreads<false>, sizeof(WgSmem<false>) + 1024, s, tx, td, a);
     }
-    if (r == cudaSuccess && p.splits > 1) r = launch_kernel(k_wgrad_join, std::min(p.rest * kTM, kSms * 8), 256, 0, s, true, a);
+    if (r == cudaSuccess && p.splits > 1) r = launch_kernel(k_wgrad_join, std::min(p.rest * kTM, kSms * 8), 256, 0, s, false, a);
     return r == cudaSuccess ? ABS_OK : thread_error(ABS_ECUDA, cudaGetErrorString(r));
 }
 
