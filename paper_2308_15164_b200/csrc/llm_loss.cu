@@ -234,35 +234,11 @@ struct PrefArgs {
     float *m, *s, *logp, *g;     // workspace, [T] each
 };
 
-template <typename T, int G, int kGroups>
-__global__ void __launch_bounds__(G * kGroups) k_pref_stats(PrefArgs a) {
-    __shared__ float sh[32];
-    const int group = threadIdx.x / G, tid = threadIdx.x % G;
-    pdl_wait();
-    pdl_trigger();
-    for (size_t t = (size_t)blockIdx.x * kGroups + group; t < a.T; t += (size_t)gridDim.x * kGroups) {
-        const T* row = static_cast<const T*>(a.logits) + t * a.ld;
-        const int y = a.labels[t];
-        RowStat st{-INFINITY, 0.f};
-        float logp = 0.f;
-        if (y >= 0 && y < a.V) {
-            const float zy = to_f(row[y]);
-            st = row_stat<T, G>(row, a.V, tid, sh);
-            if (st.m != -INFINITY || st.s != 0.f) logp = zy - st.m - logf(st.s);
-        }
-        if (tid == 0) {
-            a.m[t] = st.m;
-            a.s[t] = st.s;
-            a.logp[t] = logp;
-            a.g[t] = 0.f;
-        }
-    }
-}
-
 // One CTA per pair at a time: the two sums, the loss, and g of every counted row.
-__global__ void __launch_bounds__(256) k_pref_pairs(PrefArgs a) {
-    __shared__ double sh[8];
+__global__ void __launch_bounds__(1024) k_pref_pairs(PrefArgs a) {
+    __shared__ double sh[32];
     __shared__ double total[2];
+    __shared__ float slope;
     pdl_wait();
     pdl_trigger();
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
@@ -272,27 +248,31 @@ __global__ void __launch_bounds__(256) k_pref_pairs(PrefArgs a) {
         for (int k = 0; k < 3; ++k) at[k] = min(max((long long)a.offsets[2 * p + k], 0ll), T);
         for (int k = 0; k < 2; ++k) {
             double s = 0.0;
-            for (long long t = at[k] + threadIdx.x; t < at[k + 1]; t += 256) s += (double)a.logp[t];
+            for (long long t = at[k] + threadIdx.x; t < at[k + 1]; t += 1024) s += (double)a.logp[t];
 #pragma unroll
             for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
             __syncthreads();
             if (lane == 0) sh[warp] = s;
             __syncthreads();
             if (threadIdx.x == 0) {
-                for (int i = 1; i < 8; ++i) s += sh[i];
+                for (int i = 1; i < 32; ++i) s += sh[i];
                 total[k] = s;
                 a.seq_logp[2 * p + k] = (float)s;
             }
         }
         __syncthreads();
-        const double h = (double)a.beta * ((total[0] - (double)a.logp_ref[2 * p]) - (total[1] - (double)a.logp_ref[2 * p + 1]));
-        const double e = exp(-fabs(h)), soft = log1p(e);                     // -log sigmoid(+-h) = soft + max(-+h, 0)
-        const double sig = h >= 0.0 ? 1.0 / (1.0 + e) : e / (1.0 + e);
-        if (threadIdx.x == 0)
+        if (threadIdx.x == 0) {
+            const double h = (double)a.beta * ((total[0] - (double)a.logp_ref[2 * p]) - (total[1] - (double)a.logp_ref[2 * p + 1]));
+            const double e = exp(-fabs(h)), soft = log1p(e);                 // -log sigmoid(+-h) = soft + max(-+h, 0)
+            const double sig = h >= 0.0 ? 1.0 / (1.0 + e) : e / (1.0 + e);
+            // 0 h: NaN where h is one (fmax leaves it out)
             a.pair_loss[p] = (float)((1.0 - (double)a.smoothing) * (soft + fmax(-h, 0.0)) + (double)a.smoothing * (soft + fmax(h, 0.0)) + 0.0 * h);
-        const float g = (float)((double)a.scale * (double)a.beta * (sig - (1.0 - (double)a.smoothing)));
+            slope = (float)((double)a.scale * (double)a.beta * (sig - (1.0 - (double)a.smoothing)));
+        }
+        __syncthreads();
+        const float g = slope;
         for (int k = 0; k < 2; ++k)
-            for (long long t = at[k] + threadIdx.x; t < at[k + 1]; t += 256)
+            for (long long t = at[k] + threadIdx.x; t < at[k + 1]; t += 1024)
                 a.g[t] = a.m[t] == -INFINITY && a.s[t] == 0.f ? 0.f : k ? -g : g;
         __syncthreads();
     }
@@ -331,15 +311,14 @@ __global__ void __launch_bounds__(G * kGroups) k_pref_grad(PrefArgs a) {
 // front of it and behind the last whole piece are taken by one thread each with plain accesses; nothing outside a row is
 // touched.  logits and dlogits have to be aligned alike.
 // The chain from a row's last number to its first gradient (reductions, logarithm, the token's loss) leaves the memory idle,
-// so an SM holds kRowThreads / kT CTAs whose rows are at different points.
+// so an SM holds several CTAs whose rows are at different points.
 // Load number i of a row is chunk i, or chunk i - n beyond the first pass; slots are filled and freed in load order:
 //   first pass    loads 0 .. n - 1, of which those before n - kRing are freed at once
 //   second pass   loads n - kRing .. n - 1 from the ring, then loads n ..
 // ------------------------------------------------------------------------------------------------
-constexpr int kRing = 6;
-constexpr int kRowThreads = 512;     // consumer threads of an SM
 enum { kPolicy, kStats, kGrad };     // both passes with the policy loss between them; the first; the second
-
+constexpr int kRing = 6;             // chunks of a ring
+constexpr int kRowThreads = 512;     // consumer threads of an SM (768 with rings of four: the same)
 constexpr int kU = 4;
 template <int kT>
 struct RowsSmem {
@@ -629,6 +608,203 @@ __global__ void __launch_bounds__(kT + 32, kRowThreads / kT) k_rows(const __grid
 }
 
 // ------------------------------------------------------------------------------------------------
+// Short rows: one warp each, its exponentials (kP 16-byte pieces a lane) in registers, so that each is formed once.  A warp keeps the next rows' pieces in flight in a ring of its own (bulk copies that lane 0 issues); nothing
+// synchronises warps.  With a CTA per row (k_rows) the chain of a row's reductions bounded the rate: 32768 rows of 2000 bf16
+// took 95 us.
+// ------------------------------------------------------------------------------------------------
+constexpr int kWarpRow = 4096;               // bytes of the longest row that a warp takes: eight pieces a lane
+constexpr int kWarpCta = 4;                  // warps of a CTA
+constexpr int kWarpStages = 4;
+constexpr int warp_rows_ctas(int pieces) { return pieces == 1 ? 8 : pieces == 4 ? 5 : 4; }     // CTAs of an SM, by the registers
+
+template <typename T, int kP, int kMode>
+__global__ void __launch_bounds__(kWarpCta * 32, warp_rows_ctas(kP)) k_warp_rows(const __grid_constant__ RowArgs a, int stages, uint32_t stage_bytes) {
+    constexpr int kN = kPairs<T>;
+    extern __shared__ __align__(128) uint8_t smem[];
+    __shared__ uint64_t bars[kWarpCta][kWarpStages];
+    __shared__ double acc[kWarpCta][3];
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    uint64_t* full = bars[warp];
+    uint8_t* ring = smem + (size_t)warp * stages * stage_bytes;
+    const T* logits = static_cast<const T*>(kMode == kPolicy ? a.p.logits : a.q.logits);
+    T* dlogits = static_cast<T*>(kMode == kPolicy ? a.p.dlogits : kMode == kGrad ? a.q.dlogits : nullptr);
+    const size_t ld = kMode == kPolicy ? a.p.ld : a.q.ld, ld_d = kMode == kPolicy ? a.p.ld_d : a.q.ld_d;
+    const size_t rows = kMode == kPolicy ? a.p.T : a.q.T, G = (size_t)gridDim.x * kWarpCta;
+    const int V = kMode == kPolicy ? a.p.V : a.q.V;
+    const int32_t* labels = kMode == kPolicy ? a.p.labels : a.q.labels;
+    if (lane == 0) {
+        for (int i = 0; i < stages; ++i) mbar_init(&full[i], 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    __syncwarp();
+    pdl_wait();
+    pdl_trigger();
+
+    // a row's numbers, fetched ahead
+    struct Row {
+        int y;
+        float w, g, m, s;            // policy: w; gradient pass: g, m, s
+        TokenIn in;                  // policy
+        bool live;                   // others are neither read nor waited for
+    };
+    auto fetch = [&](size_t t) {
+        Row r{};
+        if (t >= rows) return r;
+        r.y = labels[t];
+        r.live = r.y >= 0 && r.y < V;
+        if (kMode == kPolicy) {
+            r.w = a.p.weight[t];
+            r.in = token_in(a.p, t);
+            r.live = r.live && r.w != 0.f;
+        }
+        if (kMode == kGrad) {
+            r.g = a.q.g[t];
+            r.m = a.q.m[t];
+            r.s = a.q.s[t];
+            r.live = r.g != 0.f;
+        }
+        return r;
+    };
+    auto load = [&](int stage, size_t t) {           // lane 0; the row is live
+        const T* row = logits + t * ld;
+        const RowCut c = cut_row(row, V);
+        if (c.pieces == 0) return;
+        mbar_expect_tx(&full[stage], (uint32_t)c.pieces * 16u);
+        bulk_load(ring + (size_t)stage * stage_bytes, row + c.head, (uint32_t)c.pieces * 16u, &full[stage]);
+    };
+    const size_t t0 = (size_t)blockIdx.x * kWarpCta + warp;
+    bool ok = true;
+    int stage = 0;
+    uint32_t phases = 0;
+    double sums[3] = {0.0, 0.0, 0.0};
+    Row next = fetch(t0);
+    // the row whose copy is issued next: its numbers are fetched a row ahead and looked at when it is its turn
+    int y_later = -1;
+    float w_later = 0.f;
+    auto fetch_later = [&](size_t t) {
+        const bool in = t < rows;
+        y_later = in ? labels[t] : -1;
+        if (kMode == kPolicy) w_later = in ? a.p.weight[t] : 0.f;
+        if (kMode == kGrad) w_later = in ? a.q.g[t] : 0.f;
+    };
+    auto later_live = [&] { return (kMode == kGrad || (y_later >= 0 && y_later < V)) && (kMode == kStats || w_later != 0.f); };
+    for (int i = 0; i < stages; ++i) {
+        fetch_later(t0 + i * G);
+        if (lane == 0 && later_live()) load(i, t0 + i * G);
+    }
+    fetch_later(t0 + stages * G);
+    float zy_next = next.live ? to_f(logits[t0 * ld + next.y]) : 0.f;
+    for (size_t t = t0; t < rows; t += G) {
+        const Row now = next;
+        const float zy = zy_next;
+        const T* row = logits + t * ld;
+        T* out = dlogits + t * ld_d;
+        const RowCut c = cut_row(row, V);
+        const int extra = lane < c.head ? lane : lane < c.head + c.tail ? V - c.tail + lane - c.head : -1;
+        const float ex = now.live && extra >= 0 ? to_f(row[extra]) : -INFINITY;
+        next = fetch(t + G);
+        const bool write = kMode == kGrad || (kMode == kPolicy && dlogits != nullptr);
+        float2 e[kP][kN];
+        float m = now.m, mul = 0.f, g = now.g;
+        Base b{};
+        if (now.live) {
+            if (c.pieces > 0) {
+                if (!mbar_wait(&full[stage], (phases >> stage) & 1u, ok ? kSpinLimit : 1u)) ok = false;
+                phases ^= 1u << stage;
+            }
+            const uint4* src = reinterpret_cast<const uint4*>(ring + (size_t)stage * stage_bytes) + lane;
+            if (kMode != kGrad) {
+                m = ex;              // -inf where there is none
+#pragma unroll
+                for (int j = 0; j < kP; ++j)
+                    if (lane + 32 * j < c.pieces) m = piece_max(src[32 * j], m, T());
+                m = warp_max(m);
+            } else mul = -g / now.s;
+            b = base_of(m);
+            float2 s2 = both(0.f);
+            uint4* o = reinterpret_cast<uint4*>(out + c.head) + lane;
+#pragma unroll
+            for (int j = 0; j < kP; ++j)
+                if (lane + 32 * j < c.pieces) {
+                    unpack(src[32 * j], e[j], T());
+#pragma unroll
+                    for (int k = 0; k < kN; ++k) {
+                        e[j][k] = exp_at(e[j][k], b);
+                        if (kMode != kGrad) s2 = add2(s2, e[j][k]);
+                        else e[j][k] = mul2(e[j][k], both(mul));
+                    }
+                    if (kMode == kGrad && ok) o[32 * j] = pack(e[j], T());
+                }
+            if (kMode != kGrad) {
+                float s = sum2(s2) + (extra >= 0 ? exp_at(ex, b) : 0.f);
+#pragma unroll
+                for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+                const bool some = m != -INFINITY || s != 0.f;
+                const float logp = some ? zy - m - logf(s) : 0.f;
+                if (kMode == kPolicy) {
+                    TokenLoss l{};
+                    if (some) l = token_loss(a.p, now.in, logp);
+                    g = now.w * l.slope;
+                    mul = some ? -g / s : 0.f;
+                    if (lane == 0) {
+                        if (ok) a.p.logp[t] = logp;
+                        sums[0] += (double)now.w * l.loss;
+                        sums[1] += (double)now.w * l.kl;
+                        sums[2] += (double)now.w * l.clipped;
+                    }
+                } else if (lane == 0 && ok) {
+                    a.q.m[t] = m;
+                    a.q.s[t] = s;
+                    a.q.logp[t] = logp;
+                    a.q.g[t] = 0.f;
+                }
+            }
+        } else if (kMode != kGrad && lane == 0) {
+            if (kMode == kPolicy) a.p.logp[t] = 0.f;
+            else {
+                a.q.m[t] = -INFINITY;
+                a.q.s[t] = 0.f;
+                a.q.logp[t] = 0.f;
+                a.q.g[t] = 0.f;
+            }
+        }
+        __syncwarp();                                // everybody has read the stage
+        if (lane == 0 && later_live()) load(stage, t + (size_t)stages * G);
+        fetch_later(t + (size_t)(stages + 1) * G);
+        if (++stage == stages) stage = 0;
+        zy_next = next.live ? to_f(logits[(t + G) * ld + next.y]) : 0.f;
+        if (!write || !ok) continue;
+        const bool zero = !now.live || g == 0.f;
+        uint4* o = reinterpret_cast<uint4*>(out + c.head) + lane;
+        if (kMode != kGrad || zero)
+#pragma unroll
+            for (int j = 0; j < kP; ++j)
+                if (lane + 32 * j < c.pieces) {
+#pragma unroll
+                    for (int k = 0; k < kN; ++k) e[j][k] = mul2(e[j][k], both(mul));
+                    o[32 * j] = zero ? make_uint4(0u, 0u, 0u, 0u) : pack(e[j], T());
+                }
+        if (extra >= 0) out[extra] = from_f<T>(zero ? 0.f : exp_at(ex, b) * mul);
+        // the label's element, once more, by the lane that wrote its piece
+        const int in_body = now.y - c.head;
+        const bool inside = in_body >= 0 && now.y < V - c.tail;
+        if (!zero && (inside ? lane == in_body / kVec<T> % 32 : extra == now.y)) out[now.y] = from_f<T>(exp_at(zy, b) * mul + g);
+    }
+    if (kMode == kGrad && blockIdx.x == 0 && warp == 0) pref_total(a.q);
+    if (kMode == kPolicy) {
+        if (lane == 0)
+            for (int i = 0; i < 3; ++i) acc[warp][i] = sums[i];
+        __syncthreads();
+        if (threadIdx.x < 3) {
+            double s = 0.0;
+            for (int w = 0; w < kWarpCta; ++w) s += acc[w][threadIdx.x];
+            a.p.part[(size_t)blockIdx.x * 3 + threadIdx.x] = s;
+        }
+    }
+    if (!ok) report_timeout();
+}
+
+// ------------------------------------------------------------------------------------------------
 // The policy loss with a row's exponentials kept in registers.  A row is taken by a cluster of C CTAs (C = 1 where one CTA
 // can own it), kT threads each, a thread owning up to eight 16-byte pieces: exp(z - m) is formed once, when the element
 // arrives, and scaled when the row's sum is known.  (Forming it twice makes the exponential unit as busy as the memory:
@@ -895,7 +1071,7 @@ __global__ void __launch_bounds__(kT, kSliceThreads / kT) k_policy_slices(const 
     if (C > 1) cluster_sync();       // no CTA leaves while another may still write to its shared memory
 }
 
-constexpr int kWarpRowMax = 1024;    // rows up to this length are taken by one warp each
+constexpr int kPlainWarpRow = 1024;  // the plain kernels take rows up to this length by one warp each
 
 // Consumer threads of a CTA of k_rows for rows of this many bytes: the smallest whose ring holds the row.
 int rows_threads(size_t bytes) { return bytes <= (size_t)kRing * 64 * kU * 16 ? 64 : bytes <= (size_t)kRing * 128 * kU * 16 ? 128 : 256; }
@@ -956,40 +1132,65 @@ cudaError_t launch_slices(const PolicyArgs& a, SlicePlan p, int sms, int* parts,
     }
 }
 
+template <typename T, int kP, int kMode>
+cudaError_t launch_warps_of(const RowArgs& a, size_t rows, int V, int sms, int* grid, cudaStream_t s) {
+    const uint32_t stage_bytes = (uint32_t)((V * sizeof(T) + 15) / 16 * 16);
+    const size_t most = (size_t)sms * warp_rows_ctas(kP), want = (rows + kWarpCta - 1) / kWarpCta;
+    const size_t fit = (size_t)200 * 1024 / (warp_rows_ctas(kP) * kWarpCta) / stage_bytes;      // at least three rows of 4 KB
+    const int stages = (int)(fit < (size_t)kWarpStages ? fit : (size_t)kWarpStages);
+    *grid = (int)(want < most ? want : most);
+    const cudaError_t e = allow_smem<k_warp_rows<T, kP, kMode>>();
+    return e != cudaSuccess ? e : launch_kernel(k_warp_rows<T, kP, kMode>, *grid, kWarpCta * 32, (size_t)kWarpCta * stages * stage_bytes, s, true, a, stages, stage_bytes);
+}
+template <typename T, int kMode>
+cudaError_t launch_warps(const RowArgs& a, size_t rows, int V, int sms, int* grid, cudaStream_t s) {
+    const size_t bytes = V * sizeof(T);
+    return bytes <= 512 ? launch_warps_of<T, 1, kMode>(a, rows, V, sms, grid, s) : bytes <= 2048 ? launch_warps_of<T, 4, kMode>(a, rows, V, sms, grid, s)
+                                                                                              : launch_warps_of<T, 8, kMode>(a, rows, V, sms, grid, s);
+}
+
+// Which kernel takes the rows: logits and dlogits that are not aligned alike go to the plain ones, which read the row twice
+// from memory; short rows to a warp each; few long rows of the policy loss to a cluster each; the rest to k_rows.
 template <typename T>
 cudaError_t launch_policy(const PolicyArgs& a, float* stats, int sms, cudaStream_t s) {
-    const bool warp_rows = a.V <= kWarpRowMax, alike = !a.dlogits || aligned_alike(a.logits, a.ld, a.dlogits, a.ld_d, sizeof(T));
-    const SlicePlan p = !warp_rows && a.T * 2 <= (size_t)sms ? slice_plan(a.T, (size_t)a.V / kVec<T>, sms) : SlicePlan{};
-    const size_t want = warp_rows ? (a.T + 7) / 8 : a.T;
-    int parts = (int)(want < (size_t)(4 * sms) ? want : (size_t)(4 * sms));      // CTAs or clusters that leave partial sums
+    const bool alike = !a.dlogits || aligned_alike(a.logits, a.ld, a.dlogits, a.ld_d, sizeof(T));
+    int parts = 0;           // CTAs or clusters that leave partial sums
     cudaError_t e = cudaSuccess;
-    if (a.T > 0)
-        e = warp_rows          ? launch_kernel(k_policy_rows<T, 32, 8>, parts, 256, 0, s, true, a)
-          : alike && p.cluster ? launch_slices<T>(a, p, sms, &parts, s)
-          : alike              ? launch_rows<T, kPolicy>(RowArgs{a, PrefArgs{}}, a.T, a.V, sms, &parts, s)
-                               : launch_kernel(k_policy_rows<T, 512, 1>, parts, 512, 0, s, true, a);
+    if (a.T > 0) {
+        const RowArgs r{a, PrefArgs{}};
+        const SlicePlan p = alike && a.V * sizeof(T) > kWarpRow && a.T * 2 <= (size_t)sms ? slice_plan(a.T, (size_t)a.V / kVec<T>, sms) : SlicePlan{};
+        if (!alike) {
+            const bool warp_rows = a.V <= kPlainWarpRow;
+            const size_t want = warp_rows ? (a.T + 7) / 8 : a.T;
+            parts = (int)(want < (size_t)(4 * sms) ? want : (size_t)(4 * sms));
+            e = warp_rows ? launch_kernel(k_policy_rows<T, 32, 8>, parts, 256, 0, s, true, a) : launch_kernel(k_policy_rows<T, 512, 1>, parts, 512, 0, s, true, a);
+        } else if (a.V * sizeof(T) <= kWarpRow) e = launch_warps<T, kPolicy>(r, a.T, a.V, sms, &parts, s);
+        else if (p.cluster) e = launch_slices<T>(a, p, sms, &parts, s);
+        else e = launch_rows<T, kPolicy>(r, a.T, a.V, sms, &parts, s);
+    }
     if (e != cudaSuccess) return e;
     return launch_kernel(k_policy_stats, 1, 96, 0, s, true, (const double*)a.part, parts, stats);
 }
 
 template <typename T>
 cudaError_t launch_pref(const PrefArgs& a, int sms, cudaStream_t s) {
-    const bool warp_rows = a.V <= kWarpRowMax, ring = !warp_rows && a.dlogits && aligned_alike(a.logits, a.ld, a.dlogits, a.ld_d, sizeof(T));
-    const size_t want = warp_rows ? (a.T + 7) / 8 : a.T;
-    const int grid = (int)(want < (size_t)(4 * sms) ? want : (size_t)(4 * sms));
-    int unused = 0;
+    const bool alike = a.dlogits && aligned_alike(a.logits, a.ld, a.dlogits, a.ld_d, sizeof(T));
+    const RowArgs r{PolicyArgs{}, a};
+    int grid = 0;
     cudaError_t e = cudaSuccess;
     if (a.T > 0)
-        e = warp_rows ? launch_kernel(k_pref_stats<T, 32, 8>, grid, 256, 0, s, true, a) : launch_rows<T, kStats>(RowArgs{PolicyArgs{}, a}, a.T, a.V, sms, &unused, s);
+        e = a.V * sizeof(T) <= kWarpRow ? launch_warps<T, kStats>(r, a.T, a.V, sms, &grid, s) : launch_rows<T, kStats>(r, a.T, a.V, sms, &grid, s);
     if (e != cudaSuccess) return e;
     if (a.pairs > 0) {
-        e = launch_kernel(k_pref_pairs, (int)(a.pairs < (size_t)sms ? a.pairs : (size_t)sms), 256, 0, s, true, a);
+        e = launch_kernel(k_pref_pairs, (int)(a.pairs < (size_t)sms ? a.pairs : (size_t)sms), 1024, 0, s, true, a);
         if (e != cudaSuccess) return e;
     }
-    if (ring && a.T > 0) return launch_rows<T, kGrad>(RowArgs{PolicyArgs{}, a}, a.T, a.V, sms, &unused, s);
-    const int g2 = a.dlogits && grid > 0 ? grid : 1;
-    return warp_rows ? launch_kernel(k_pref_grad<T, 32, 8>, g2, 256, 0, s, true, a)
-                     : launch_kernel(k_pref_grad<T, 512, 1>, g2, 512, 0, s, true, a);
+    if (alike && a.T > 0)
+        return a.V * sizeof(T) <= kWarpRow ? launch_warps<T, kGrad>(r, a.T, a.V, sms, &grid, s) : launch_rows<T, kGrad>(r, a.T, a.V, sms, &grid, s);
+    const bool warp_rows = a.V <= kPlainWarpRow;
+    const size_t want = !a.dlogits ? 1 : warp_rows ? (a.T + 7) / 8 : a.T;
+    grid = (int)(want < 1 ? 1 : want < (size_t)(4 * sms) ? want : (size_t)(4 * sms));
+    return warp_rows ? launch_kernel(k_pref_grad<T, 32, 8>, grid, 256, 0, s, true, a) : launch_kernel(k_pref_grad<T, 512, 1>, grid, 512, 0, s, true, a);
 }
 
 bool misaligned(const void* p, size_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) != 0; }
