@@ -7,13 +7,14 @@ The package holds:
 * ``binding``    -- a ctypes binding with the same names (argument marshalling only),
 * ``llm``        -- the operators of ``abs_llm.h`` on tensors (losses on logits, the residual join of a
                    transformer block, 8-bit activation checkpoints),
+* ``llm_example`` -- a small model trained with them through the delayed synchronous step,
 * ``workloads``  -- seeded synthetic input generators (no optimiser arithmetic).
 
 Nothing here falls back to a CPU implementation: importing ``binding`` raises if the
 shared library has not been built.
 """
 
-__all__ = ["binding", "llm", "workloads", "build", "dist"]
+__all__ = ["binding", "llm", "llm_example", "workloads", "build", "dist"]
 
 
 def __getattr__(name):

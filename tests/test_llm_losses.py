@@ -131,6 +131,38 @@ def test_policy_masks(llm, V, dtype):
     assert zero.loss == 0 and zero.kl == 0 and (zero.dlogits == 0).all() and (zero.logp == 0).all()
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T,V", [(200, 1500), (160, 5001), (90, 40000), (80, 70001)])
+def test_many_rows(llm, T, V, dtype):
+    """More rows than half the SMs: rows that one warp takes, rows within and beyond what stays in shared memory; some are left
+    out; in place and beside."""
+    z, y, old, adv, w, ref = policy_case(T, V, dtype, T + V)
+    w[::5] = 0.0
+    y[3::11] = -1
+    z[::5] = float("nan")
+    clean = torch.nan_to_num(z)
+    want = R.policy(clean, y, old, adv, w, ref, kl_coef=0.1)
+    a = llm.policy_loss(z, y, old, adv, w, logp_ref=ref, kl_coef=0.1)
+    check_policy(a, want, clean, 0.1)
+    only = llm.policy_loss(z, y, old, adv, w, logp_ref=ref, kl_coef=0.1, need_grad=False)
+    assert torch.equal(only.loss, a.loss) and torch.equal(only.logp, a.logp)
+    lens = (T // 4, T // 3, 0, T - T // 4 - T // 3)
+    off = torch.tensor([0, lens[0], lens[0] + lens[1], lens[0] + lens[1], T], dtype=torch.int32, device=DEV)
+    yy = torch.where(w == 0, torch.full_like(y, -100), y)
+    sums = R.preference(clean, yy, off, torch.zeros(4))["seq_logp"].float().to(DEV)
+    sref = sums + torch.tensor([3.0, -2.0, 0.0, 1.0], device=DEV)
+    p = llm.preference_loss(z, yy, off, sref, beta=0.2)
+    check_pref(p, R.preference(clean, yy, off, sref, 0.2), clean, 0.2, 0.5)
+    q = llm.preference_loss(z.clone(), yy, off, sref, beta=0.2, need_grad=False)
+    assert torch.equal(q.loss, p.loss) and torch.equal(q.pair_loss, p.pair_loss)
+    spare = z.clone()
+    p2 = llm.preference_loss(spare, yy, off, sref, beta=0.2, dlogits=spare)
+    assert torch.equal(p2.dlogits, p.dlogits)
+    b = llm.policy_loss(z, y, old, adv, w, logp_ref=ref, kl_coef=0.1, dlogits=z)
+    for u, v in zip(a, b):
+        assert torch.equal(u, v)
+
+
 def test_policy_nan_in_a_kept_row_is_not_hidden(llm):
     for V in (50, 5000, 40000):
         z, y, old, adv, w, ref = policy_case(4, V, "f32", 5)
