@@ -235,7 +235,10 @@ __global__ void __launch_bounds__(256) k_ckpt8_dequantize_any(const uint8_t* q, 
 //   warp 0      TMA producer, up to kStages runs ahead: 128 columns of q (8 KB), 128 columns of dy (two boxes, 16 KB)
 //   warp 1      (first CTA only) MMA issuer: four tcgen05.mma.cta_group::2 (M 256, N 256, K 16) per run into one of two TMEM
 //               accumulators
-//   warps 2-5   epilogue: TMEM -> registers -> dw (or a partial sum), coalesced through a padded staging tile
+//   warps 2-5   epilogue: TMEM -> registers -> dw (or a partial sum), coalesced through a padded staging tile.  In
+//               k_wgrad<false> eight warps (2-9), which keep the tile's sums in registers and add a finished accumulator to
+//               them every kSegmentRuns runs: the tensor core drops low bits at each of its additions, so that its error grows
+//               with their number (2.8e-6 of the result at 8192 tokens without, 2.2e-7 with, for 4 % of the time)
 //   warps 6-21  q -> bf16 operand tile, two groups of eight warps on alternate runs: thread = (token, block of 32), the two
 //               16-byte pieces of q become four of bf16.  The exponents come by plain loads, kAhead of a group's runs ahead.
 // Every tile of a row of tiles converts the same operand again.  Beyond kFusedOut output columns the operand is therefore
@@ -251,14 +254,16 @@ constexpr int kTM = 256, kTN = 256, kTK = 64;    // of a pair
 constexpr int kRawBytes = kTK * 128, kABytes = kTK * 128 * 2, kBBytes = kTK * 128 * 2;
 constexpr int kAhead = 4;
 constexpr int kPitch = 33;
+constexpr int kSegmentRuns = 16;
 
 template <bool kFused>
 struct WgSmem {
-    static constexpr int kStages = kFused ? 5 : 6, kASlots = kFused ? 4 : 6;
+    static constexpr int kStages = 5, kASlots = kFused ? 4 : kStages;
+    static constexpr int kEpiWarps = kFused ? 4 : 8;
     alignas(1024) uint8_t raw[kFused ? kStages : 1][kFused ? kRawBytes : 1024];
     alignas(1024) uint8_t b[kStages][kBBytes];
     alignas(1024) uint8_t a[kASlots][kABytes];
-    float out[4][32 * kPitch];
+    float out[kEpiWarps][32 * kPitch];
     alignas(8) uint64_t full[kStages];       // fused: this CTA's copies of a run have landed; else, first CTA: both CTAs' have
     uint64_t empty[kStages];                 // the run's MMAs have read both CTAs' operands
     uint64_t ready[kASlots];                 // fused, first CTA: both CTAs' operands of a run are there
@@ -316,7 +321,7 @@ __device__ __forceinline__ void umma2_commit(uint64_t* bar) {
 }
 
 template <bool kFused>
-constexpr int kWgThreads = kFused ? 704 : 192;
+constexpr int kWgThreads = kFused ? 704 : 320;
 
 // tm_x: q, or the operand in bf16.
 template <bool kFused>
@@ -342,7 +347,7 @@ __global__ void __launch_bounds__(kWgThreads<kFused>, 1) k_wgrad(const __grid_co
         for (int i = 0; i < kASlots; ++i) mbar_init(&s.ready[i], 16);    // eight warps of each CTA
         for (int i = 0; i < 2; ++i) {
             mbar_init(&s.acc_full[i], 1);
-            mbar_init(&s.acc_empty[i], 8);                               // four warps of each CTA
+            mbar_init(&s.acc_empty[i], 2 * WgSmem<kFused>::kEpiWarps);   // the epilogue warps of each CTA
         }
         s.failed = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -357,6 +362,7 @@ __global__ void __launch_bounds__(kWgThreads<kFused>, 1) k_wgrad(const __grid_co
         int m0, n0, kb0, kb1;        // first row and column of the pair's tile, runs of 64 tokens
         int part;                    // index of the partial sum, -1: straight to dw
     };
+    constexpr int kSegment = kFused ? 1 << 30 : kSegmentRuns;    // runs that the tensor core adds up on its own
     auto item_of = [&](int it) {
         Item q;
         int tile = it;
@@ -407,30 +413,92 @@ __global__ void __launch_bounds__(kWgThreads<kFused>, 1) k_wgrad(const __grid_co
         if (lane == 0 && rank == 0) {                // ---- MMA issuer
             constexpr uint32_t idesc = umma_idesc_bf16(kTM, kTN) | (1u << 15) | (1u << 16);   // both operands MN-major
             uint32_t st = 0, sl = 0, sl_phase = 0;
-            int i = 0;
+            int i = 0;                               // segments so far: every other one in the same accumulator
             bool ok = true;
-            for (int it = pair; it < items && ok; it += pairs, ++i) {
+            for (int it = pair; it < items && ok; it += pairs) {
                 const Item q = item_of(it);
-                const int ab = i & 1;
-                if (i >= 2 && !mbar_wait(&s.acc_empty[ab], ((i / 2) - 1) & 1)) { ok = false; break; }
-                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                for (int kb = q.kb0; kb < q.kb1; ++kb) {
-                    if (!mbar_wait(kFused ? &s.ready[sl] : &s.full[sl], sl_phase)) { ok = false; break; }
+                for (int kb0 = q.kb0; kb0 < q.kb1 && ok; kb0 += min(kSegment, q.kb1 - kb0), ++i) {
+                    const int ab = i & 1, kb1 = min(q.kb1 - kb0, kSegment) + kb0;
+                    if (i >= 2 && !mbar_wait(&s.acc_empty[ab], ((i / 2) - 1) & 1)) { ok = false; break; }
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                    const uint32_t a0 = smem_u32(s.a[sl]), b0 = smem_u32(s.b[st]);
+                    for (int kb = kb0; kb < kb1; ++kb) {
+                        if (!mbar_wait(kFused ? &s.ready[sl] : &s.full[sl], sl_phase)) { ok = false; break; }
+                        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                        const uint32_t a0 = smem_u32(s.a[sl]), b0 = smem_u32(s.b[st]);
 #pragma unroll
-                    for (int k = 0; k < kTK / 16; ++k)
-                        umma2_bf16(tmem + ab * kTN, umma_desc_mn_sw128(a0 + k * 2048, 8192), umma_desc_mn_sw128(b0 + k * 2048, 8192), idesc,
-                                   kb > q.kb0 || k > 0);
-                    umma2_commit(&s.empty[st]);
-                    if (++st == kStages) st = 0;
-                    if (++sl == kASlots) { sl = 0; sl_phase ^= 1u; }
+                        for (int k = 0; k < kTK / 16; ++k)
+                            umma2_bf16(tmem + ab * kTN, umma_desc_mn_sw128(a0 + k * 2048, 8192), umma_desc_mn_sw128(b0 + k * 2048, 8192), idesc,
+                                       kb > kb0 || k > 0);
+                        umma2_commit(&s.empty[st]);
+                        if (++st == kStages) st = 0;
+                        if (++sl == kASlots) { sl = 0; sl_phase ^= 1u; }
+                    }
+                    if (ok) umma2_commit(&s.acc_full[ab]);
                 }
-                if (ok) umma2_commit(&s.acc_full[ab]);
             }
             if (!ok) *failed = 1;
         }
         __syncwarp();
+    } else if constexpr (!kFused) {                  // ---- epilogue: warps 2-5 the first 128 columns, 6-9 the others
+        const int qd = warp % 4, half = (warp - 2) / 4;
+        float* stage = s.out[warp - 2];
+        const int row = rank * 128 + qd * 32;        // of the tile
+        int i = 0;
+        bool ok = true;
+        for (int it = pair; it < items && ok; it += pairs) {
+            const Item q = item_of(it);
+            float2 sum[4][16];
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) sum[c][j] = both(0.f);
+            for (int kb0 = q.kb0; kb0 < q.kb1; kb0 += kSegment, ++i) {
+                const int ab = i & 1;
+                ok = __all_sync(0xffffffffu, mbar_wait(&s.acc_full[ab], (i / 2) & 1) && !*failed);
+                if (!ok) break;
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    uint32_t v[32];
+                    tmem_ld_32(tmem + ((uint32_t)(qd * 32) << 16) + (uint32_t)(ab * kTN + half * 128 + c * 32), v);
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) sum[c][j] = add2(sum[c][j], make_float2(__uint_as_float(v[2 * j]), __uint_as_float(v[2 * j + 1])));
+                }
+                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) arrive_first(&s.acc_empty[ab]);
+            }
+            if (!ok) {
+                *failed = 1;
+                break;
+            }
+            const bool part = q.part >= 0;
+            float* base = part ? a.part + ((size_t)q.part * kTM + row) * kTN : a.dw + (size_t)(q.m0 + row) * a.ld + q.n0;
+            const size_t ld = part ? (size_t)kTN : a.ld;
+            const int rows = min(32, a.D - (q.m0 + row)), cols = a.N - q.n0 - half * 128;
+            const bool add = a.accumulate && !part;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                if (c * 32 >= cols) continue;
+#pragma unroll
+                for (int j = 0; j < 16; ++j) {
+                    stage[lane * kPitch + 2 * j] = sum[c][j].x;
+                    stage[lane * kPitch + 2 * j + 1] = sum[c][j].y;
+                }
+                __syncwarp();
+                float* p = base + half * 128 + c * 32 + lane;
+                if (c * 32 + lane < cols) {
+                    if (add) {
+#pragma unroll 8
+                        for (int r = 0; r < rows; ++r) p[(size_t)r * ld] += stage[r * kPitch + lane];
+                    } else {
+#pragma unroll 8
+                        for (int r = 0; r < rows; ++r) p[(size_t)r * ld] = stage[r * kPitch + lane];
+                    }
+                }
+                __syncwarp();
+            }
+        }
     } else if (warp < 6) {                           // ---- epilogue
         const int qd = warp % 4;
         float* stage = s.out[warp - 2];
@@ -475,7 +543,7 @@ __global__ void __launch_bounds__(kWgThreads<kFused>, 1) k_wgrad(const __grid_co
                 __syncwarp();
             }
         }
-    } else if constexpr (kFused) {                   // ---- q -> bf16 operand tile
+    } else {                                         // ---- q -> bf16 operand tile
         const int tid = (threadIdx.x - 192) % 256, group = (threadIdx.x - 192) / 256;
         const int r = tid % kTK, blk = tid / kTK;    // token of the run, block of 32 columns
         const uint32_t sw = (uint32_t)(r & 7);
@@ -583,6 +651,7 @@ int grid_for(size_t n, int per_cta) {
 constexpr int kSms = 148;
 constexpr int kFusedOut = 512;   // output columns up to which the operand is converted in the kernel ..
 constexpr int kFusedTokens = 1024;   // .. or tokens, where the extra launch costs more than the repeated conversion
+constexpr int kMaxRuns = 32;     // runs that k_wgrad<true> adds up in one accumulator, where the tiles are cut at all
 constexpr int kMinRuns = 12;     // runs of 64 tokens that a part of a cut tile has at least: shorter ones do not pay for the join
 
 // How the work is cut: whole output tiles for all pairs of SMs equally often, the rest in runs of tokens.
@@ -601,7 +670,9 @@ bool plan_of(uint64_t T, uint64_t D, uint64_t N, const void* dy, uint64_t ld_dy,
     if (tiles > 0x3fffffff) return false;
     p.whole = (int)(tiles / pairs * pairs);
     p.rest = (int)(tiles - p.whole);
+    p.fused = N <= (uint64_t)kFusedOut || T <= (uint64_t)kFusedTokens;
     int splits = p.rest ? std::min(pairs / p.rest, kb / kMinRuns) : 1;
+    if (p.fused && p.whole == 0) splits = std::max(splits, (kb + kMaxRuns - 1) / kMaxRuns);
     if (splits < 1) splits = 1;
     p.kb_per_split = std::max(1, (kb + splits - 1) / splits);
     p.splits = std::max(1, (kb + p.kb_per_split - 1) / p.kb_per_split);
@@ -609,7 +680,6 @@ bool plan_of(uint64_t T, uint64_t D, uint64_t N, const void* dy, uint64_t ld_dy,
     p.ld8 = (N + 7) / 8 * 8;
     p.part_bytes = p.splits > 1 ? (size_t)p.splits * p.rest * kTM * kTN * 4 : 0;
     p.pack_bytes = p.repack ? up256((size_t)T * p.ld8 * 2) : 0;
-    p.fused = N <= (uint64_t)kFusedOut || T <= (uint64_t)kFusedTokens;
     p.x_bytes = p.fused ? 0 : up256((size_t)T * ((D + 31) / 32 * 32) * 2);
     *out = p;
     return true;
