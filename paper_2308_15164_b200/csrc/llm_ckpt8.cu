@@ -55,14 +55,29 @@ struct PackArgs {
 };
 constexpr int kUnroll = 4;   // units whose loads are issued together
 
+__device__ __forceinline__ uint4 bits_of(const float* v) { return make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])); }
+__device__ __forceinline__ uint4 bits_of(const bf16* v) {
+    auto two = [&](int k) { return (uint32_t)__bfloat16_as_ushort(v[k]) | (uint32_t)__bfloat16_as_ushort(v[k + 1]) << 16; };
+    return make_uint4(two(0), two(2), two(4), two(6));
+}
+// Bits of the largest magnitude of a piece, as those of an fp32 (integers order magnitudes; NaN comes out on top).
+__device__ __forceinline__ uint32_t magnitude(uint4 r, float) {
+    return max(max(r.x & 0x7FFFFFFFu, r.y & 0x7FFFFFFFu), max(r.z & 0x7FFFFFFFu, r.w & 0x7FFFFFFFu));
+}
+__device__ __forceinline__ uint32_t magnitude(uint4 r, bf16) {
+    const uint32_t m = __vmaxu2(__vmaxu2(r.x & 0x7FFF7FFFu, r.y & 0x7FFF7FFFu), __vmaxu2(r.z & 0x7FFF7FFFu, r.w & 0x7FFF7FFFu));
+    return max(m << 16, m & 0xFFFF0000u);
+}
+
 // A unit is eight values; the four lanes of a block are neighbours.  kWide: the rows allow 16-byte loads.
 template <typename T, bool kWide>
 __global__ void __launch_bounds__(256) k_ckpt8_quantize(const T* x, const __grid_constant__ PackArgs a, uint2* q, uint8_t* e) {
     pdl_wait();
     pdl_trigger();
     // units is a multiple of 4: a block's lanes are all in or all out; all lanes of a warp stay in the loop for the exchange
+    constexpr int kPacks = 8 / kVec<T>;              // 16-byte pieces of a unit
     for (size_t i0 = (size_t)blockIdx.x * 256 * kUnroll; i0 < a.units; i0 += (size_t)gridDim.x * 256 * kUnroll) {
-        float v[kUnroll][8];
+        uint4 raw[kUnroll][kPacks];
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u) {
             const size_t i = i0 + u * 256 + threadIdx.x;
@@ -71,12 +86,14 @@ __global__ void __launch_bounds__(256) k_ckpt8_quantize(const T* x, const __grid
             const int c = i < a.units ? (int)piece * 8 : a.D;
             const T* p = x + t * a.ld + c;
             if (kWide && c + 8 <= a.D) {
-                constexpr int kN = kVec<T>;
 #pragma unroll
-                for (int k = 0; k < 8 / kN; ++k) Pack<T, kN>::load(p + k * kN, *reinterpret_cast<float(*)[kN]>(v[u] + k * kN));
+                for (int k = 0; k < kPacks; ++k) raw[u][k] = reinterpret_cast<const uint4*>(p)[k];
             } else {
+                T v[8];
 #pragma unroll
-                for (int k = 0; k < 8; ++k) v[u][k] = c + k < a.D ? to_f(p[k]) : 0.f;
+                for (int k = 0; k < 8; ++k) v[k] = c + k < a.D ? p[k] : from_f<T>(0.f);
+#pragma unroll
+                for (int k = 0; k < kPacks; ++k) raw[u][k] = bits_of(v + k * kVec<T>);
             }
         }
 #pragma unroll
@@ -84,20 +101,27 @@ __global__ void __launch_bounds__(256) k_ckpt8_quantize(const T* x, const __grid
             const size_t i = i0 + u * 256 + threadIdx.x;
             uint32_t m = 0;
 #pragma unroll
-            for (int k = 0; k < 8; ++k) m = max(m, __float_as_uint(v[u][k]) & 0x7FFFFFFFu);
+            for (int k = 0; k < kPacks; ++k) m = max(m, magnitude(raw[u][k], T()));
             m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
             m = max(m, __shfl_xor_sync(0xffffffffu, m, 2));
             const uint32_t code = block_exponent(m);
-            const float inv = code == 255u ? 0.f : inv_pow2_of(code);
+            const float2 inv = both(code == 255u ? 0.f : inv_pow2_of(code));
             // the sum with 1.5 2^23 is rounded to an integer (to nearest even), whose low byte is q
-            uint32_t w[2];
+            uint32_t w[2], b[8];
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                uint32_t b[4];
+            for (int k = 0; k < kPacks; ++k) {
+                float2 v[kPairs<T>];
+                unpack(raw[u][k], v, T());
 #pragma unroll
-                for (int k = 0; k < 4; ++k) b[k] = __float_as_uint(__fadd_rn(v[u][4 * h + k] * inv, 12582912.f));
-                w[h] = code == 255u ? 0u : __byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410);
+                for (int j = 0; j < kPairs<T>; ++j) {
+                    const float2 r = add2(mul2(v[j], inv), both(12582912.f));
+                    b[k * kVec<T> + 2 * j] = __float_as_uint(r.x);
+                    b[k * kVec<T> + 2 * j + 1] = __float_as_uint(r.y);
+                }
             }
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                w[h] = code == 255u ? 0u : __byte_perm(__byte_perm(b[4 * h], b[4 * h + 1], 0x0040), __byte_perm(b[4 * h + 2], b[4 * h + 3], 0x0040), 0x5410);
             if (i < a.units) {
                 q[i] = make_uint2(w[0], w[1]);
                 if (i % 4 == 0) e[i / 4] = (uint8_t)code;
@@ -617,15 +641,22 @@ __global__ void __launch_bounds__(256) k_wgrad_join(const __grid_constant__ WgAr
     pdl_wait();
     pdl_trigger();
     const size_t step = (size_t)a.rest * kTM * kTN;
-    // one row of a tile at a time
-    for (int i = blockIdx.x; i < a.rest * kTM; i += gridDim.x) {
-        const int tile = a.whole + i / kTM, m = tile / a.tiles_n * kTM + i % kTM, n = tile % a.tiles_n * kTN + threadIdx.x;
-        if (m >= a.D || n >= a.N) continue;
-        const float* p = a.part + (size_t)i * kTN + threadIdx.x;
-        float s = p[0];
-        for (int k = 1; k < a.splits; ++k) s += p[k * step];
+    constexpr int kRows = 4;                         // rows of tiles at a time
+    for (int i0 = blockIdx.x * kRows; i0 < a.rest * kTM; i0 += gridDim.x * kRows) {
+        float s[kRows];
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) s[r] = 0.f;
+        const float* p = a.part + (size_t)i0 * kTN + threadIdx.x;    // kTM is a multiple of kRows
+#pragma unroll 2
+        for (int k = 0; k < a.splits; ++k)
+#pragma unroll
+            for (int r = 0; r < kRows; ++r) s[r] += p[k * step + (size_t)r * kTN];
+        const int tile = a.whole + i0 / kTM, m = tile / a.tiles_n * kTM + i0 % kTM, n = tile % a.tiles_n * kTN + threadIdx.x;
+        if (n >= a.N) continue;
         float* o = a.dw + (size_t)m * a.ld + n;
-        *o = a.accumulate ? *o + s : s;
+#pragma unroll
+        for (int r = 0; r < kRows; ++r)
+            if (m + r < a.D) o[(size_t)r * a.ld] = a.accumulate ? o[(size_t)r * a.ld] + s[r] : s[r];
     }
 }
 
@@ -831,7 +862,7 @@ extern "C" int abs_ckpt8_wgrad(const int8_t* q, const uint8_t* e, const void* dy
         r = allow_smem<k_wgrad<false>>();
         if (r == cudaSuccess) r = launch_cluster(k_wgrad<false>, grid, 2, false, kWgThreads<false>, sizeof(WgSmem<false>) + 1024, s, tx, td, a);
     }
-    if (r == cudaSuccess && p.splits > 1) r = launch_kernel(k_wgrad_join, std::min(p.rest * kTM, kSms * 8), 256, 0, s, false, a);
+    if (r == cudaSuccess && p.splits > 1) r = launch_kernel(k_wgrad_join, std::min(p.rest * kTM / 4, kSms * 8), 256, 0, s, false, a);
     return r == cudaSuccess ? ABS_OK : thread_error(ABS_ECUDA, cudaGetErrorString(r));
 }
 

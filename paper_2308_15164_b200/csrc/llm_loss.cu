@@ -234,46 +234,43 @@ struct PrefArgs {
     float *m, *s, *logp, *g;     // workspace, [T] each
 };
 
-// One CTA per pair at a time: the two sums, the loss, and g of every counted row.
+// One CTA per pair at a time: the two sums (half of the CTA each, in 64 bits), the loss, and g of every counted row.
 __global__ void __launch_bounds__(1024) k_pref_pairs(PrefArgs a) {
     __shared__ double sh[32];
-    __shared__ double total[2];
     __shared__ float slope;
     pdl_wait();
     pdl_trigger();
-    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-    const long long T = (long long)a.T;
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, half = threadIdx.x / 512, tid = threadIdx.x % 512;
+    const int T = (int)a.T;
     for (size_t p = blockIdx.x; p < a.pairs; p += gridDim.x) {
-        long long at[3];
-        for (int k = 0; k < 3; ++k) at[k] = min(max((long long)a.offsets[2 * p + k], 0ll), T);
-        for (int k = 0; k < 2; ++k) {
-            double s = 0.0;
-            for (long long t = at[k] + threadIdx.x; t < at[k + 1]; t += 1024) s += (double)a.logp[t];
+        const int begin = min(max(a.offsets[2 * p + half], 0), T), end = min(max(a.offsets[2 * p + half + 1], 0), T);
+        double s = 0.0;
+        for (int t = begin + tid; t < end; t += 512) s += (double)a.logp[t];
 #pragma unroll
-            for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-            __syncthreads();
-            if (lane == 0) sh[warp] = s;
-            __syncthreads();
-            if (threadIdx.x == 0) {
-                for (int i = 1; i < 32; ++i) s += sh[i];
-                total[k] = s;
-                a.seq_logp[2 * p + k] = (float)s;
+        for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+        if (lane == 0) sh[warp] = s;
+        __syncthreads();
+        if (warp == 0) {
+            // lanes 0 - 15: the preferred answer's warps, 16 - 31 the other's
+            s = sh[lane];
+#pragma unroll
+            for (int o = 8; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+            const double other = __shfl_sync(0xffffffffu, s, 16);
+            if (lane == 0) {
+                a.seq_logp[2 * p] = (float)s;
+                a.seq_logp[2 * p + 1] = (float)other;
+                // the difference in 64 bits, what comes after it in 32
+                const float h = (float)((double)a.beta * ((s - (double)a.logp_ref[2 * p]) - (other - (double)a.logp_ref[2 * p + 1])));
+                const float e = expf(-fabsf(h)), soft = log1pf(e);               // -log sigmoid(+-h) = soft + max(-+h, 0)
+                const float sig = h >= 0.f ? 1.f / (1.f + e) : e / (1.f + e);
+                const float worse = h < 0.f ? -h : 0.f, better = h > 0.f ? h : 0.f;
+                a.pair_loss[p] = h == h ? (1.f - a.smoothing) * (soft + worse) + a.smoothing * (soft + better) : h;
+                slope = a.scale * a.beta * (sig - (1.f - a.smoothing));
             }
         }
         __syncthreads();
-        if (threadIdx.x == 0) {
-            const double h = (double)a.beta * ((total[0] - (double)a.logp_ref[2 * p]) - (total[1] - (double)a.logp_ref[2 * p + 1]));
-            const double e = exp(-fabs(h)), soft = log1p(e);                 // -log sigmoid(+-h) = soft + max(-+h, 0)
-            const double sig = h >= 0.0 ? 1.0 / (1.0 + e) : e / (1.0 + e);
-            // 0 h: NaN where h is one (fmax leaves it out)
-            a.pair_loss[p] = (float)((1.0 - (double)a.smoothing) * (soft + fmax(-h, 0.0)) + (double)a.smoothing * (soft + fmax(h, 0.0)) + 0.0 * h);
-            slope = (float)((double)a.scale * (double)a.beta * (sig - (1.0 - (double)a.smoothing)));
-        }
-        __syncthreads();
-        const float g = slope;
-        for (int k = 0; k < 2; ++k)
-            for (long long t = at[k] + threadIdx.x; t < at[k + 1]; t += 1024)
-                a.g[t] = a.m[t] == -INFINITY && a.s[t] == 0.f ? 0.f : k ? -g : g;
+        const float g = half ? -slope : slope;
+        for (int t = begin + tid; t < end; t += 512) a.g[t] = a.m[t] == -INFINITY && a.s[t] == 0.f ? 0.f : g;
         __syncthreads();
     }
 }

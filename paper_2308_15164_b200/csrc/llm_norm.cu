@@ -718,6 +718,9 @@ Plan plan_of(const Mat (&m)[N], size_t es, uint64_t T, uint64_t D, bool back, ui
         p.grid = (int)(T < cap ? T : cap);
         return p;
     }
+    // backward: at least four rows per CTA, whose column sums cost as much as a row
+    if (back)
+        while (ctas > 1 && kSms * ctas * 4 > T) --ctas;
     const size_t all = (size_t)kSms * ctas / period * period;       // a multiple of the period: rows of a CTA are cut alike
     const size_t want = (T + period - 1) / period * period;
     p.grid = (int)(want < all ? want : all);
