@@ -85,7 +85,7 @@ int abs_preference_loss(const void *logits, uint32_t dtype, uint64_t tokens, uin
 /* Norm behind a block, gate and scaled residual, norm in front of the next block, in one pass:
  *     u = h / rms(h) * w_post  (w_post NULL: u = h)     y = scale x + G u     n = y / rms(y) * w_pre
  *     rms(v) = sqrt(mean_d v_d^2 + eps)
- * x, h, y, n [tokens, width] of `dtype` (y may be x, n may be h); w_post, w_pre [width] fp32.  n is formed from y before
+ * x, h, y, n [tokens, width] of `dtype` (y may be x, n may be h, with the same leading dimension); w_post, w_pre [width] fp32.  n is formed from y before
  * its rounding.  gate: see ABS_GATE_*; ld_gate is used with ABS_GATE_ELEMENT.  width <= 32768 (ABS_ELIMIT). */
 int abs_residual_norm(const void *x, uint64_t ld_x, const void *h, uint64_t ld_h, const void *gate, uint64_t ld_gate,
                       uint32_t gate_kind, const float *w_post, const float *w_pre, float scale, float eps, uint32_t dtype,
@@ -97,7 +97,7 @@ int abs_residual_norm(const void *x, uint64_t ld_x, const void *h, uint64_t ld_h
  *     dgate = dY u, summed over the tokens (channel) or times sigmoid' (element)
  *     dw_pre = sum_t dn yn      dw_post = sum_t dU hn
  * dx, dh and (element) dgate are of `dtype`, all with leading dimension width or more; dx may be dy or dn, dh may be h,
- * an element dgate may be the gate.  dw_pre, dw_post, (channel) dgate: fp32 [width], 4-byte aligned (slices of a flat
+ * an element dgate may be the gate (each with the same leading dimension).  dw_pre, dw_post, (channel) dgate: fp32 [width], 4-byte aligned (slices of a flat
  * gradient); accumulate != 0 adds to what they hold.  dw_post must be given exactly when w_post is, dgate exactly when
  * there is a gate.  workspace: abs_residual_norm_workspace(tokens, width) bytes. */
 size_t abs_residual_norm_workspace(uint64_t tokens, uint64_t width);
@@ -114,7 +114,7 @@ int abs_residual_norm_backward(const void *dn, uint64_t ld_dn, const void *dy, u
  * 127 2^(e - 127), q rounded to nearest even.  Every such value is a bf16 number, so that a bf16 tensor-core product
  * takes it without a rounding.  A block that holds an infinity or NaN gets e = 255 and stands for NaNs.
  *   x [tokens, width] of `dtype`;  q [tokens, W] int8, e [tokens, W / 32] uint8, W = width rounded up to 32, both packed
- *   (no gaps between rows), q 16-byte aligned, e 4-byte aligned. */
+ *   (no gaps between rows), q 16-byte aligned. */
 int abs_ckpt8_quantize(const void *x, uint64_t ld_x, uint32_t dtype, uint64_t tokens, uint64_t width, int8_t *q, uint8_t *e,
                        void *stream);
 int abs_ckpt8_dequantize(const int8_t *q, const uint8_t *e, uint64_t tokens, uint64_t width, void *x, uint64_t ld_x,
@@ -125,7 +125,7 @@ int abs_ckpt8_dequantize(const int8_t *q, const uint8_t *e, uint64_t tokens, uin
  *   dw [width, out] fp32, ld_dw >= out, 4-byte aligned (a slice of a flat gradient); accumulate != 0 adds to what it holds.
  *   workspace: abs_ckpt8_wgrad_workspace(tokens, width, out, dy, ld_dy) bytes: partial sums where the tokens are split
  *             over the GPU, and a packed copy of a dy whose rows are not 16-byte aligned.  May be 0 (NULL is taken then).
- * tokens, width and out up to 2^31 - 1 (ABS_ELIMIT).  The kernel's waits are bounded; see abs_llm_check. */
+ * tokens, width and out up to 2^31 - 64 (ABS_ELIMIT).  The kernel's waits are bounded; see abs_llm_check. */
 size_t abs_ckpt8_wgrad_workspace(uint64_t tokens, uint64_t width, uint64_t out, const void *dy, uint64_t ld_dy);
 int abs_ckpt8_wgrad(const int8_t *q, const uint8_t *e, const void *dy, uint64_t ld_dy, uint64_t tokens, uint64_t width,
                     uint64_t out, float *dw, uint64_t ld_dw, int accumulate, void *workspace, size_t workspace_bytes,

@@ -692,6 +692,7 @@ int coalesce_one(abs_ctx* c, uint32_t worker, const void* x_dev, const int32_t* 
 
 namespace abs_sgd {
 int thread_error(int code, const char* text) {
+    if (code == ABS_ECUDA) cudaGetLastError();       // the status says it; nobody else should find it again
     try {
         g_init_error = text;
     } catch (...) {      // out of host memory: the code alone has to do

@@ -680,6 +680,7 @@ int grid_for(size_t n, int per_cta) {
 }
 
 constexpr int kSms = 148;
+constexpr uint64_t kSizeMax = 0x7fffffc0ull;     // tokens, width, out: what is rounded up to a tile stays an int
 constexpr int kFusedOut = 512;   // output columns up to which the operand is converted in the kernel ..
 constexpr int kFusedTokens = 1024;   // .. or tokens, where the extra launch costs more than the repeated conversion
 constexpr int kMaxRuns = 32;     // runs that k_wgrad<true> adds up in one accumulator, where the tiles are cut at all
@@ -755,7 +756,7 @@ const char* check_ckpt(const void* x, uint64_t ld, uint32_t dtype, uint64_t toke
         return "width exceeds 2^31 - 256";
     }
     if (tokens && (!x || !q || !e)) return "x, q and e must not be NULL";
-    if (misaligned(x, dtype == ABS_F32 ? 4 : 2) || misaligned(q, 16) || misaligned(e, 4)) return "x must be aligned to its elements, q to 16 and e to 4 bytes";
+    if (misaligned(x, dtype == ABS_F32 ? 4 : 2) || misaligned(q, 16)) return "x must be aligned to its elements, q to 16 bytes";
     return nullptr;
 }
 template <typename T>
@@ -806,7 +807,7 @@ extern "C" int abs_ckpt8_dequantize(const int8_t* q, const uint8_t* e, uint64_t 
 }
 
 extern "C" size_t abs_ckpt8_wgrad_workspace(uint64_t tokens, uint64_t width, uint64_t out, const void* dy, uint64_t ld_dy) {
-    if (tokens > 0x7fffffffull || width > 0x7fffffffull || out > 0x7fffffffull) return 0;
+    if (tokens > kSizeMax || width > kSizeMax || out > kSizeMax) return 0;
     WgPlan p;
     return plan_of(tokens, width, out, dy, ld_dy, &p) ? p.bytes() : 0;
 }
@@ -814,10 +815,10 @@ extern "C" size_t abs_ckpt8_wgrad_workspace(uint64_t tokens, uint64_t width, uin
 extern "C" int abs_ckpt8_wgrad(const int8_t* q, const uint8_t* e, const void* dy, uint64_t ld_dy, uint64_t tokens, uint64_t width,
                                uint64_t out, float* dw, uint64_t ld_dw, int accumulate, void* workspace, size_t workspace_bytes, void* stream) {
     if (width == 0 || out == 0 || ld_dy < out || ld_dw < out) return thread_error(ABS_EINVAL, "width and out must be at least 1, ld_dy and ld_dw at least out");
-    if (tokens > 0x7fffffffull || width > 0x7fffffffull || out > 0x7fffffffull) return thread_error(ABS_ELIMIT, "a size exceeds 2^31 - 1");
+    if (tokens > kSizeMax || width > kSizeMax || out > kSizeMax) return thread_error(ABS_ELIMIT, "a size exceeds 2^31 - 64");
     if (!dw || misaligned(dw, 4)) return thread_error(ABS_EINVAL, "dw must be non-NULL and 4-byte aligned");
     if (tokens && (!q || !e || !dy)) return thread_error(ABS_EINVAL, "q, e and dy must not be NULL");
-    if (misaligned(q, 16) || misaligned(e, 4) || misaligned(dy, 2)) return thread_error(ABS_EINVAL, "q must be aligned to 16 bytes, e to 4, dy to its elements");
+    if (misaligned(q, 16) || misaligned(dy, 2)) return thread_error(ABS_EINVAL, "q must be aligned to 16 bytes, dy to its elements");
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     cudaError_t r = cudaSuccess;
     if (tokens == 0) {

@@ -734,6 +734,8 @@ const char* check_mats(const Mat (&m)[N], size_t es, size_t D) {
     }
     return nullptr;
 }
+// An output in place of an input has to have its leading dimension.
+const char* check_in_place(Mat out, Mat in) { return out.p && out.p == in.p && out.ld != in.ld ? "an output in place of an input needs the same leading dimension" : nullptr; }
 const char* check_common(uint32_t dtype, uint64_t width, uint32_t gate_kind, const void* gate, const float* w_post, const float* w_pre,
                          float scale, float eps) {
     if (dtype != ABS_F32 && dtype != ABS_BF16) return "dtype must be ABS_F32 or ABS_BF16";
@@ -764,6 +766,9 @@ extern "C" int abs_residual_norm(const void* x, uint64_t ld_x, const void* h, ui
     const size_t es = dtype == ABS_F32 ? 4 : 2;
     const Mat m[5] = {{x, ld_x}, {h, ld_h}, {gate_kind == ABS_GATE_ELEMENT ? gate : nullptr, ld_gate}, {y, ld_y}, {n, ld_n}};
     if (const char* why = check_mats(m, es, width)) return thread_error(ABS_EINVAL, why);
+    for (const Mat& out : {m[3], m[4]})
+        for (const Mat& in : {m[0], m[1], m[2]})
+            if (const char* why = check_in_place(out, in)) return thread_error(ABS_EINVAL, why);
     if (tokens == 0) return ABS_OK;
     if (!x || !h || !y || !n) return thread_error(ABS_EINVAL, "x, h, y and n must not be NULL");
     NormArgs a{};
@@ -797,6 +802,9 @@ extern "C" int abs_residual_norm_backward(const void* dn, uint64_t ld_dn, const 
     const Mat m[8] = {{dn, ld_dn}, {dy, ld_dy}, {y, ld_y}, {h, ld_h}, {element ? gate : nullptr, ld_gate},
                       {dx, ld_dx}, {dh, ld_dh}, {element ? dgate : nullptr, ld_dgate}};
     if (const char* why = check_mats(m, es, width)) return thread_error(ABS_EINVAL, why);
+    for (const Mat& out : {m[5], m[6], m[7]})
+        for (const Mat& in : {m[0], m[1], m[2], m[3], m[4]})
+            if (const char* why = check_in_place(out, in)) return thread_error(ABS_EINVAL, why);
     if ((gate != nullptr) != (dgate != nullptr)) return thread_error(ABS_EINVAL, "dgate must be given exactly when there is a gate");
     if ((w_post != nullptr) != (dw_post != nullptr)) return thread_error(ABS_EINVAL, "dw_post must be given exactly when w_post is");
     if (!dw_pre) return thread_error(ABS_EINVAL, "dw_pre must not be NULL");

@@ -171,3 +171,25 @@ def test_streams(llm):
             outs.append(llm.ckpt8_wgrad(llm.ckpt8_quantize(x), dy))
     torch.cuda.synchronize()
     assert all(torch.equal(o, a) for o in outs)
+
+
+def test_rows_beyond_two_gigaelements_and_slices_of_a_checkpoint(llm):
+    T, D, ld = 3, 1030, 1_200_000_000
+    if torch.cuda.mem_get_info()[0] < 12 << 30:
+        pytest.skip("needs 12 GB")
+    store = torch.empty((T - 1) * ld + D, dtype=torch.bfloat16, device=DEV)
+    far = store.as_strided((T, D), (ld, 1))
+    x = randn(4, T, D).bfloat16()
+    far.copy_(x)
+    c = check_pack(llm, far)
+    want = llm.ckpt8_dequantize(c, torch.bfloat16)
+    llm.ckpt8_dequantize(c, torch.bfloat16, out=far)
+    assert torch.equal(far, want)
+    del store, far
+    torch.cuda.empty_cache()
+    part = llm.Ckpt8(c.q[1:], c.e[1:], D)                # the exponents of a slice start at any byte
+    assert torch.equal(llm.ckpt8_dequantize(part, torch.bfloat16), want[1:])
+    dy = randn(5, T, 40).bfloat16()
+    got = llm.ckpt8_wgrad(part, dy[1:])
+    w, tol = wgrad_want(c.q[1:], c.e[1:], D, dy[1:])
+    R.close(got, w, tol, "dw")

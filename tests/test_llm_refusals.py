@@ -62,11 +62,12 @@ CASES = [
     (forward, dict(dtype=3)), (forward, dict(D=0)), (forward, dict(kind=3)), (forward, dict(gate=None)), (forward, dict(kind=0)), (forward, dict(w_pre=None)),
     (forward, dict(eps=0.0)), (forward, dict(eps=NAN)), (forward, dict(scale=INF)), (forward, dict(ld_x=15)), (forward, dict(ld_gate=15)), (forward, dict(ld_n=1)),
     (forward, dict(x=None)), (forward, dict(y=None)), (forward, dict(h=P + 1)), (forward, dict(w_post=P + 2)), (forward, dict(kind=1, gate=P + 2)),
+    (forward, dict(y=P, ld_y=24)), (forward, dict(n=P, ld_n=32)), (backward, dict(dx=P, ld_dx=24)), (backward, dict(dgate=P, ld_dgate=24)),
     (backward, dict(dn=None)), (backward, dict(dw_post=None)), (backward, dict(w_post=None)), (backward, dict(dgate=None)), (backward, dict(gate=None)),
     (backward, dict(dw_pre=None)), (backward, dict(dw_pre=P + 2)), (backward, dict(ws=None)), (backward, dict(ws=P + 16)), (backward, dict(ld_dh=8)),
     (backward, dict(kind=1, dgate=P + 2)), (backward, dict(dx=P + 1)),
     (wgrad, dict(D=0)), (wgrad, dict(N=0)), (wgrad, dict(ld=63)), (wgrad, dict(ld_dw=63)), (wgrad, dict(dw=None)), (wgrad, dict(dw=P + 2)), (wgrad, dict(q=None)),
-    (wgrad, dict(q=P + 8)), (wgrad, dict(e=P + 1)), (wgrad, dict(dy=P + 1)), (wgrad, dict(T=1 << 14, ws=None)), (wgrad, dict(T=1 << 14, ws=P + 8)),
+    (wgrad, dict(q=P + 8)), (wgrad, dict(e=None)), (wgrad, dict(dy=P + 1)), (wgrad, dict(T=1 << 14, ws=None)), (wgrad, dict(T=1 << 14, ws=P + 8)),
 ]
 
 

@@ -186,3 +186,57 @@ def test_many_rows_and_streams_give_equal_bits(llm):
     s.synchronize()
     for u, v in zip(one, two):
         assert torch.equal(u, v)
+
+
+def test_rows_beyond_two_gigaelements(llm):
+    """The last row starts more than 2^31 elements behind the first."""
+    T, D, ld = 3, 1030, 1_200_000_000
+    if torch.cuda.mem_get_info()[0] < 12 << 30:
+        pytest.skip("needs 12 GB")
+    a, p = make(T, D, "bf16", "channel", True, 6)
+    store = torch.empty((T - 1) * ld + D, dtype=torch.bfloat16, device=DEV)
+    far = store.as_strided((T, D), (ld, 1))
+    far.copy_(a["x"])
+    y, n = llm.residual_norm(far, a["h"], **p, scale=0.7, y=far)
+    wy, wn, ty, tn = R.residual(a["x"], a["h"], **p, scale=0.7)
+    R.close(y, wy, ty, "y")
+    R.close(n, wn, tn, "n")
+    far.copy_(a["y"])
+    check_backward(llm, a | {"y": far}, p, 0.7)
+    del store, far, y
+    torch.cuda.empty_cache()
+
+
+def test_in_a_captured_graph(llm):
+    """All operators of a step captured once and replayed on new values."""
+    from paper_2308_15164_b200 import llm as L
+
+    T, D, V = 130, 256, 1000
+    a, p = make(T, D, "bf16", "channel", True, 9)
+    w = (torch.randn(D, V, device=DEV) * D ** -0.5).bfloat16()
+    lab = torch.randint(0, V, (T,), device=DEV, dtype=torch.int32)
+    adv, wt, old = torch.randn(T, device=DEV), torch.full((T,), 1.0 / T, device=DEV), torch.full((T,), -7.0, device=DEV)
+    x, h = a["x"].clone(), a["h"].clone()
+
+    def step():
+        y, n = L.residual_norm(x, h, **p, scale=0.7)
+        c = L.ckpt8_quantize(n)
+        r = L.policy_loss(n @ w, lab, old, adv, wt)
+        g = L.residual_norm_backward(r.dlogits @ w.t(), None, y, h, **p, scale=0.7)
+        return [r.loss, r.logp, L.ckpt8_wgrad(c, r.dlogits), *g]
+
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = step()
+    for seed in (1, 2):
+        b, _ = make(T, D, "bf16", "channel", True, 20 + seed)
+        x.copy_(b["x"])
+        h.copy_(b["h"])
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in out]
+        for u, v in zip(got, step()):
+            assert torch.equal(u, v)
+    L.check()
