@@ -240,3 +240,22 @@ def test_in_a_captured_graph(llm):
         for u, v in zip(got, step()):
             assert torch.equal(u, v)
     L.check()
+
+
+@pytest.mark.parametrize("dtype,T,D", [("f32", 310, 8192), ("f32", 301, 7001), ("bf16", 700, 5000), ("bf16", 610, 3500), ("f32", 1203, 1537), ("bf16", 305, 8192)])
+@pytest.mark.parametrize("gate", ["channel", "element"])
+def test_several_rows_per_cta_at_every_split_of_a_row(llm, dtype, T, D, gate):
+    a, p = make(T, D, dtype, gate, True, 29)
+    check_forward(llm, a, p, 0.7)
+    check_backward(llm, a, p, 0.7, dy=True)
+    check_backward(llm, a, p, 0.7, dy=False)
+
+
+@pytest.mark.parametrize("gate", ["none", "channel", "element"])
+def test_inner_products_that_cancel(llm, gate):
+    """dn w_pre nearly along y: dY is a small difference of large terms, and so is its product with h."""
+    a, p = make(40, 1024, "f32", gate, True, 31)
+    p["w_pre"] = p["w_pre"].abs() + 0.1
+    a["dn"] = a["y"] / p["w_pre"] * (1 + 0.01 * a["dn"])
+    check_backward(llm, a, p, 0.7, dy=False)
+    check_backward(llm, a, p, 0.7, dy=True)
