@@ -23,12 +23,19 @@ constexpr int kRingSmem = 216 * 1024;   // shared memory of an SM that the ring 
 constexpr int kRingCtasMax = 16;
 // Threads of an SM for the ring kernels, by the elements that a thread owns: what their registers (weights, column sums,
 // the row's values) leave room for.
-constexpr int ring_threads(bool back, int elems) { return back ? (elems == 32 ? 256 : elems == 16 ? 512 : 640) : (elems == 8 ? 1024 : 512); }
+constexpr int ring_threads(bool back, int elems) { return back && elems == 32 ? 256 : 512; }
+// Rows that one warp owns: CTAs of eight warps, each with rows of its own, copied by the lanes.  Bulk copies of short rows are bound by
+// their number (some 35 ns each on an SM).  us with a warp per row / a CTA of one warp per row, forward and backward, bf16: 60000 x 100 with an
+// element gate 33 / 44, 55 / 86; 32768 x 256 18 / 21, 34 / 47; 30000 x 300 22 / 29, 42 / 53; 20000 x 384 17 / 16, 30 / 36; 30000 x 512 34 / 29,
+// 68 / 56.  fp32, 20000 x 320: 20 / 18, 36 / 33.  warp_ctas: how many CTAs an SM has registers for.
+constexpr int kRowWarps = 8;
+constexpr size_t warp_row(size_t es) { return es == 2 ? 384 : 256; }
+constexpr int warp_ctas(bool back, int elems) { return back ? 2 : elems == 8 ? 4 : 3; }
 // Elements of a thread.  Forward, 4096 columns, bf16, 16384 rows: 92 us with 16 (two CTAs of 256 threads an SM), 101 with 32
 // (three of 128), 109 with 8 (two of 512).  Backward: 16 leave four warps a scheduler, 32 spread a row's fixed work further and pay
 // where they fill two CTAs of 128 threads, or rows that are wide enough.  8192 rows of bf16, us with 16 / 32: 2560 columns 74 / 97, 3584 66 / 70,
 // 4096 109 / 108 (without gate and w_post 76 / 70), 5120 178 / 200, 6144 147 / 157; 4096 rows: 7168 121 / 112.  fp32: 4096 columns 132 / 157,
-// 5120 215 / 241.  Narrow rows: what one warp can own.
+// 5120 215 / 241.  Up to 256 columns: what a warp has to own.
 constexpr int ring_elems(bool back, size_t es, size_t D) {
     if (D <= 8 * 32) return 8;
     if (!back || es == 4) return D <= 16 * 512 ? 16 : 32;
@@ -38,6 +45,9 @@ constexpr int ctas_per_sm(bool back, int threads, int elems) {
     const int n = ring_threads(back, elems) / threads;
     return n < kRingCtasMax ? n : kRingCtasMax;
 }
+
+// Columns of a row of partial sums: 16-byte pieces.
+constexpr __host__ __device__ size_t part_width(size_t D) { return (D + 3) / 4 * 4; }
 
 struct NormArgs {
     const void *x, *h, *gate;        // backward: x is unused
@@ -52,7 +62,7 @@ struct NormArgs {
     size_t ld_dn, ld_dy;
     void *dx, *dh, *dgate;           // dgate: element gate only
     size_t ld_dx, ld_dh, ld_dgate;
-    float* part;                     // [CTA][2][D]: sum dn yn; sum dY hn (channel gate) or dU hn
+    float* part;                     // [CTA][2][part_width(D)]: sum dn yn; sum dY hn (channel gate) or dU hn
 };
 
 // 1 / (1 + 2^(-v log2 e)).  Relative error below 4e-7 for |v| < 8 (the exponent is rounded once), 0 and 1 in the limits.
@@ -122,10 +132,10 @@ __global__ void __launch_bounds__(256) k_residual_norm_back(NormArgs a) {
     __shared__ float sh[24];
     pdl_wait();
     pdl_trigger();
-    float* col = a.part + (size_t)blockIdx.x * 2 * a.D;
+    float *col = a.part + blockIdx.x * 2 * part_width(a.D), *col_h = col + part_width(a.D);
     for (int c = threadIdx.x * kV; c < a.D; c += 256 * kV)
 #pragma unroll
-        for (int k = 0; k < kV; ++k) col[c + k] = col[a.D + c + k] = 0.f;
+        for (int k = 0; k < kV; ++k) col[c + k] = col_h[c + k] = 0.f;
     for (size_t t = blockIdx.x; t < a.T; t += gridDim.x) {
         const T* dn = static_cast<const T*>(a.dn) + t * a.ld_dn;
         const T* dy = a.dy ? static_cast<const T*>(a.dy) + t * a.ld_dy : nullptr;
@@ -170,7 +180,7 @@ __global__ void __launch_bounds__(256) k_residual_norm_back(NormArgs a) {
                 const float w = kPost ? a.w_post[c + k] : 1.f;
                 float du = d;
                 if (kGate == 1) {
-                    col[a.D + c + k] += d * hn;
+                    col_h[c + k] += d * hn;
                     du *= static_cast<const float*>(a.gate)[c + k];
                 }
                 if (kGate == 2) {
@@ -179,7 +189,7 @@ __global__ void __launch_bounds__(256) k_residual_norm_back(NormArgs a) {
                     vg[k] = du * (hn * w) * (1.f - g);
                 }
                 if (kPost) {
-                    if (kGate != 1) col[a.D + c + k] += du * hn;
+                    if (kGate != 1) col_h[c + k] += du * hn;
                     q[0] += du * w * hn;
                 }
                 vh[k] = du * w;
@@ -212,7 +222,7 @@ __global__ void __launch_bounds__(256) k_residual_norm_back(NormArgs a) {
 // Rows of odd width start at every alignment.  G is a multiple of the period with which the alignment repeats, so that
 // all rows of one CTA are cut alike: single elements up to the first 16-byte boundary, pieces, single elements.  The
 // copies move the pieces (nothing outside the row is read), the single elements are plain loads.  All matrices of the
-// call have to be aligned alike.
+// call have to be aligned alike.  Short rows: a warp per row, each lane copies the pieces that it reads (kWarp).
 // Weights and column sums stay in registers; two fp32 operations per instruction where the order of a sum allows it.
 // ------------------------------------------------------------------------------------------------
 constexpr int kRingMax = 8;
@@ -230,18 +240,19 @@ struct RingCtl {
 };
 constexpr size_t kRingCtl = (sizeof(RingCtl) + 15) / 16 * 16;
 
-// Sums over the CTA's threads, one synchronisation: `sh` (zero beyond the CTA's warps) must not be the buffer of the
-// reduction just before.
-template <int kN>
-__device__ __forceinline__ void cta_sum(float (&v)[kN], float (*sh)[16], int warps) {
+// Sums over a row's threads: the warp (kWarp), or the CTA with one synchronisation, where `sh` (zero beyond the CTA's warps) must
+// not be the buffer of the reduction just before.
+template <bool kWarp, int kN>
+__device__ __forceinline__ void row_sum(float (&v)[kN], float (*sh)[16], int warps) {
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     if (kN <= 2) {
 #pragma unroll
         for (int k = 0; k < kN; ++k) {
 #pragma unroll
             for (int o = 16; o; o >>= 1) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
-            if (lane == 0) sh[k][warp] = v[k];
+            if (!kWarp && lane == 0) sh[k][warp] = v[k];
         }
+        if (kWarp) return;
     } else {                         // up to eight: a step halves the numbers of a lane, number k ends in lanes 16 k0 + 8 k1 + 4 k2
         float w[8];
 #pragma unroll
@@ -256,6 +267,11 @@ __device__ __forceinline__ void cta_sum(float (&v)[kN], float (*sh)[16], int war
             }
         w[0] += __shfl_xor_sync(0xffffffffu, w[0], 2);
         w[0] += __shfl_xor_sync(0xffffffffu, w[0], 1);
+        if (kWarp) {
+#pragma unroll
+            for (int k = 0; k < kN; ++k) v[k] = __shfl_sync(0xffffffffu, w[0], (k & 1) << 4 | (k & 2) << 2 | (k & 4));
+            return;
+        }
         const int k = (lane >> 4 & 1) | (lane >> 2 & 2) | (lane & 4);
         if (k < kN && (lane & 3) == 0) sh[k][warp] = w[0];
     }
@@ -271,8 +287,12 @@ __device__ __forceinline__ void cta_sum(float (&v)[kN], float (*sh)[16], int war
         }
 }
 
-// A CTA's rows: how they are cut, which of them are in flight, which is the current one.
-template <typename T, int kIn>
+__device__ __forceinline__ void copy_piece(void* to, const void* from) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from) : "memory");
+}
+
+// A CTA's rows (kWarp: a warp's): how they are cut, which of them are in flight, which is the current one.
+template <typename T, int kIn, int kP, bool kWarp>
 struct Ring {
     RowCut cut;
     int extra;                       // column of this thread's single element, or -1
@@ -287,25 +307,41 @@ struct Ring {
     uint32_t phase = 0;
     bool ok = true;
 
+    static __device__ __forceinline__ int tid() { return kWarp ? threadIdx.x % 32 : threadIdx.x; }
+    static __device__ __forceinline__ int step() { return kWarp ? 32 : blockDim.x; }
     __device__ __forceinline__ void begin(uint8_t* smem, const RingArgs& a, const T* row0) {
         ctl = reinterpret_cast<RingCtl*>(smem);
-        base = smem + kRingCtl;
         row_bytes = a.row_bytes;
         stages = a.stages;
+        base = smem + kRingCtl + (kWarp ? (size_t)(threadIdx.x / 32) * stages * kIn * row_bytes : 0);
         rows = a.n.T;
         cut = cut_row(row0, a.n.D);
         bytes = (uint32_t)cut.pieces * 16u;
-        const int tid = threadIdx.x;
+        const int tid = Ring::tid();
         extra = tid < cut.head ? tid : tid < cut.head + cut.tail ? a.n.D - cut.tail + tid - cut.head : -1;
-        for (int i = tid; i < 18 * 16; i += blockDim.x) (&ctl->red[0][0][0])[i] = 0.f;
-        if (tid == 0) {
-            ctl->done = 0;
-            for (int i = 0; i < stages; ++i) mbar_init(&ctl->full[i], 1);
-            asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        if (!kWarp) {
+            for (int i = tid; i < 18 * 16; i += blockDim.x) (&ctl->red[0][0][0])[i] = 0.f;
+            if (tid == 0) {
+                ctl->done = 0;
+                for (int i = 0; i < stages; ++i) mbar_init(&ctl->full[i], 1);
+                asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+            }
+            __syncthreads();
         }
-        __syncthreads();
     }
-    __device__ __forceinline__ void load(int stage, size_t t) {       // one thread
+    // One thread; kWarp: every lane its own pieces, one group of copies for each row.
+    __device__ __forceinline__ void load(int stage, size_t t) {
+        if (kWarp) {
+            if (t < rows)
+#pragma unroll
+                for (int i = 0; i < kIn; ++i)
+                    if (in[i])
+#pragma unroll
+                        for (int j = 0; j < kP; ++j)
+                            if (has(j)) copy_piece(base + (size_t)(stage * kIn + i) * row_bytes + (tid() + j * 32) * 16, in[i] + t * ld[i] + column(j));
+            asm volatile("cp.async.commit_group;" ::: "memory");
+            return;
+        }
         if (t >= rows || bytes == 0) return;
         uint32_t total = 0;
 #pragma unroll
@@ -322,6 +358,7 @@ struct Ring {
     // This warp has read the image of the current row, t, for the last time; the last of the CTA's warps fills it again.  (No warp
     // is a row ahead: there is a synchronisation of the CTA in every row.)
     __device__ __forceinline__ void release(size_t t, size_t G, int warps) {
+        if (kWarp) return load(st, t + (size_t)stages * G);          // a lane reads its own copies only
         __syncwarp();
         if (threadIdx.x % 32 != 0) return;
         __threadfence_block();
@@ -335,6 +372,12 @@ struct Ring {
         for (int i = 0; i < kIn; ++i) v[i] = in[i] ? to_f(in[i][t * ld[i] + extra]) : 0.f;
     }
     __device__ __forceinline__ void wait() {
+        if (kWarp) {                 // a group per row: all but the last stages - 1 have arrived
+            if (stages == 2) asm volatile("cp.async.wait_group 1;" ::: "memory");
+            else if (stages == 3) asm volatile("cp.async.wait_group 2;" ::: "memory");
+            else asm volatile("cp.async.wait_group 3;" ::: "memory");
+            return;
+        }
         if (bytes != 0 && !mbar_wait(&ctl->full[st], phase, ok ? kSpinLimit : 1u)) ok = false;
     }
     __device__ __forceinline__ void next() {
@@ -342,15 +385,14 @@ struct Ring {
     }
     // Piece j of this thread of input i, in the current row's image.
     __device__ __forceinline__ void piece(int i, int j, float2 (&v)[kPairs<T>]) const {
-        unpack(*reinterpret_cast<const uint4*>(base + (size_t)(st * kIn + i) * row_bytes + (threadIdx.x + j * blockDim.x) * 16), v, T());
+        unpack(*reinterpret_cast<const uint4*>(base + (size_t)(st * kIn + i) * row_bytes + (tid() + j * step()) * 16), v, T());
     }
-    __device__ __forceinline__ bool has(int j) const { return (int)(threadIdx.x + j * blockDim.x) < cut.pieces; }
-    __device__ __forceinline__ int column(int j) const { return cut.head + (int)(threadIdx.x + j * blockDim.x) * kVec<T>; }
+    __device__ __forceinline__ bool has(int j) const { return tid() + j * step() < cut.pieces; }
+    __device__ __forceinline__ int column(int j) const { return cut.head + (tid() + j * step()) * kVec<T>; }
     __device__ __forceinline__ void store(T* row, int j, const float2 (&v)[kPairs<T>]) const {
         if (ok) *reinterpret_cast<uint4*>(row + column(j)) = pack(v, T());
     }
     // This thread's columns of a weight vector, times those of a second one if there is one; its single element is returned.
-    template <int kP>
     __device__ __forceinline__ float weights(const float* p, const float* q, float2 (&w)[kP][kPairs<T>]) const {
         auto at = [&](int c) { return q ? p[c] * q[c] : p[c]; };
 #pragma unroll
@@ -361,29 +403,29 @@ struct Ring {
     }
 };
 
-template <typename T, int kP, bool kPost, int kGate>
-__global__ void __launch_bounds__(ring_threads(false, kP * kVec<T>), 1) k_join(const __grid_constant__ RingArgs ra) {
+template <typename T, int kP, bool kPost, int kGate, bool kWarp>
+__global__ void __launch_bounds__(kWarp ? kRowWarps * 32 : ring_threads(false, kP * kVec<T>), kWarp ? warp_ctas(false, kP * kVec<T>) : 1) k_join(const __grid_constant__ RingArgs ra) {
     constexpr int kN = kPairs<T>, kIn = kGate == 2 ? 3 : 2;
     constexpr bool kScaled = kPost || kGate == 1;    // u carries a weight: w_post, the channel gate, or their product
     const NormArgs& a = ra.n;
     extern __shared__ __align__(16) uint8_t smem[];
     const int warps = blockDim.x / 32;
-    const size_t t0 = blockIdx.x, G = gridDim.x;
-    Ring<T, kIn> r;
+    const size_t t0 = kWarp ? (size_t)blockIdx.x * kRowWarps + threadIdx.x / 32 : blockIdx.x, G = kWarp ? (size_t)gridDim.x * kRowWarps : gridDim.x;
+    Ring<T, kIn, kP, kWarp> r;
     r.in[0] = static_cast<const T*>(a.x); r.ld[0] = a.ld_x;
     r.in[1] = static_cast<const T*>(a.h); r.ld[1] = a.ld_h;
     if (kGate == 2) { r.in[kIn - 1] = static_cast<const T*>(a.gate); r.ld[kIn - 1] = a.ld_gate; }
     r.begin(smem, ra, r.in[0] + t0 * a.ld_x);
     pdl_wait();
     pdl_trigger();
-    if (threadIdx.x == 0)
+    if (kWarp || threadIdx.x == 0)
         for (int i = 0; i < r.stages; ++i) r.load(i, t0 + i * G);
     float nx[kIn] = {};
     r.load_extra(t0, nx);
     float2 w_u[kP][kN], w_pre[kP][kN];
     const float* gate = kGate == 1 ? static_cast<const float*>(a.gate) : nullptr;
-    const float xw_u = kScaled ? r.template weights<kP>(kPost ? a.w_post : gate, kPost ? gate : nullptr, w_u) : 1.f;
-    const float xw_pre = r.template weights<kP>(a.w_pre, nullptr, w_pre);
+    const float xw_u = kScaled ? r.weights(kPost ? a.w_post : gate, kPost ? gate : nullptr, w_u) : 1.f;
+    const float xw_pre = r.weights(a.w_pre, nullptr, w_pre);
 
     int k = 0;
     for (size_t t = t0; t < a.T; t += G, ++k, r.next()) {
@@ -405,8 +447,8 @@ __global__ void __launch_bounds__(ring_threads(false, kP * kVec<T>), 1) k_join(c
                     for (int i = 0; i < kN; ++i) s2 = fma2(v[i], v[i], s2);
                 }
             float s[1] = {sum2(s2) + (r.extra >= 0 ? ex[1] * ex[1] : 0.f)};
-            cta_sum<1>(s, red, warps);
-            r.refill(t, G, k);
+            row_sum<kWarp>(s, red, warps);
+            if (!kWarp) r.refill(t, G, k);
             rh = rsqrtf(s[0] * a.inv_d + a.eps);
         }
         float2 y[kP][kN], s2 = both(0.f);
@@ -428,6 +470,7 @@ __global__ void __launch_bounds__(ring_threads(false, kP * kVec<T>), 1) k_join(c
                 }
                 r.store(yrow, j, y[j]);
             }
+        if (kWarp) r.release(t, G, warps);
         float s[1] = {sum2(s2)}, xy = 0.f;
         if (r.extra >= 0) {
             float u = ex[1] * rh * xw_u;
@@ -436,8 +479,8 @@ __global__ void __launch_bounds__(ring_threads(false, kP * kVec<T>), 1) k_join(c
             s[0] += xy * xy;
             if (r.ok) yrow[r.extra] = from_f<T>(xy);
         }
-        cta_sum<1>(s, kPost ? r.ctl->red[2] : red, warps);
-        if (!kPost) r.refill(t, G, k);
+        row_sum<kWarp>(s, kPost ? r.ctl->red[2] : red, warps);
+        if (!kPost && !kWarp) r.refill(t, G, k);
         const float ry = rsqrtf(s[0] * a.inv_d + a.eps);
         T* nrow = static_cast<T*>(a.n) + t * a.ld_n;
 #pragma unroll
@@ -452,8 +495,8 @@ __global__ void __launch_bounds__(ring_threads(false, kP * kVec<T>), 1) k_join(c
     if (!r.ok) report_timeout();
 }
 
-template <typename T, int kP, bool kPost, int kGate>
-__global__ void __launch_bounds__(ring_threads(true, kP * kVec<T>), 1) k_join_back(const __grid_constant__ RingArgs ra) {
+template <typename T, int kP, bool kPost, int kGate, bool kWarp>
+__global__ void __launch_bounds__(kWarp ? kRowWarps * 32 : ring_threads(true, kP * kVec<T>), kWarp ? warp_ctas(true, kP * kVec<T>) : 1) k_join_back(const __grid_constant__ RingArgs ra) {
     constexpr int kN = kPairs<T>, kIn = kGate == 2 ? 5 : 4;
     constexpr bool kScaled = kPost || kGate == 1;    // dh carries a weight: w_post, the channel gate, or their product
     constexpr bool kSum = kPost || kGate == 1;       // the second column sum
@@ -461,8 +504,8 @@ __global__ void __launch_bounds__(ring_threads(true, kP * kVec<T>), 1) k_join_ba
     const NormArgs& a = ra.n;
     extern __shared__ __align__(16) uint8_t smem[];
     const int warps = blockDim.x / 32;
-    const size_t t0 = blockIdx.x, G = gridDim.x;
-    Ring<T, kIn> r;
+    const size_t t0 = kWarp ? (size_t)blockIdx.x * kRowWarps + threadIdx.x / 32 : blockIdx.x, G = kWarp ? (size_t)gridDim.x * kRowWarps : gridDim.x;
+    Ring<T, kIn, kP, kWarp> r;
     r.in[0] = static_cast<const T*>(a.y); r.ld[0] = a.ld_y;
     r.in[1] = static_cast<const T*>(a.dn); r.ld[1] = a.ld_dn;
     r.in[2] = static_cast<const T*>(a.h); r.ld[2] = a.ld_h;
@@ -472,14 +515,14 @@ __global__ void __launch_bounds__(ring_threads(true, kP * kVec<T>), 1) k_join_ba
     r.begin(smem, ra, r.in[0] + t0 * a.ld_y);
     pdl_wait();
     pdl_trigger();
-    if (threadIdx.x == 0)
+    if (kWarp || threadIdx.x == 0)
         for (int i = 0; i < r.stages; ++i) r.load(i, t0 + i * G);
     float nx[kIn] = {};
     r.load_extra(t0, nx);
     float2 w_u[kP][kN], w_pre[kP][kN], c_pre[kP][kN], c_h[kP][kN];
     const float* gate = kGate == 1 ? static_cast<const float*>(a.gate) : nullptr;
-    const float xw_u = kScaled ? r.template weights<kP>(kPost ? a.w_post : gate, kPost ? gate : nullptr, w_u) : 1.f;
-    const float xw_pre = r.template weights<kP>(a.w_pre, nullptr, w_pre);
+    const float xw_u = kScaled ? r.weights(kPost ? a.w_post : gate, kPost ? gate : nullptr, w_u) : 1.f;
+    const float xw_pre = r.weights(a.w_pre, nullptr, w_pre);
     float x_pre = 0.f, x_h = 0.f;
 #pragma unroll
     for (int j = 0; j < kP; ++j)
@@ -549,7 +592,7 @@ __global__ void __launch_bounds__(ring_threads(true, kP * kVec<T>), 1) k_join_ba
                 s[kDy] += f * ex[3];
             }
         }
-        cta_sum<kSums>(s, r.ctl->red[k & 1], warps);
+        row_sum<kWarp>(s, r.ctl->red[k & 1], warps);
         const float ry = rsqrtf(s[0] * a.inv_d + a.eps);
         const float along = -s[1] * a.inv_d * ry * ry;          // d = ry (dn w_pre) + yn along
         const float rh = kPost ? rsqrtf(s[kH] * a.inv_d + a.eps) : 1.f;
@@ -620,7 +663,12 @@ __global__ void __launch_bounds__(ring_threads(true, kP * kVec<T>), 1) k_join_ba
             }
         }
     }
-    float* col = a.part + (size_t)blockIdx.x * 2 * a.D;
+    float* const part = a.part + blockIdx.x * 2 * part_width(a.D);
+    float* const col = kWarp ? reinterpret_cast<float*>(r.base) : part;      // a warp's sums go over its row images, 8 bytes a column
+    if (kWarp) {
+        asm volatile("cp.async.wait_all;" ::: "memory");
+        __syncwarp();
+    }
 #pragma unroll
     for (int j = 0; j < kP; ++j)
         if (r.has(j))
@@ -630,35 +678,57 @@ __global__ void __launch_bounds__(ring_threads(true, kP * kVec<T>), 1) k_join_ba
                 c[0] = c_pre[j][i].x;
                 c[1] = c_pre[j][i].y;
                 if (kSum) {
-                    c[a.D] = c_h[j][i].x;
-                    c[a.D + 1] = c_h[j][i].y;
+                    c[part_width(a.D)] = c_h[j][i].x;
+                    c[part_width(a.D) + 1] = c_h[j][i].y;
                 }
             }
     if (r.extra >= 0) {
         col[r.extra] = x_pre;
-        if (kSum) col[a.D + r.extra] = x_h;
+        if (kSum) col[part_width(a.D) + r.extra] = x_h;
+    }
+    if (kWarp) {
+        __syncthreads();
+        const size_t next = (size_t)r.stages * kIn * r.row_bytes / 4;
+        const float* first = reinterpret_cast<const float*>(smem + kRingCtl);
+        for (int c = threadIdx.x; c < (kSum ? 2 : 1) * (int)part_width(a.D); c += kRowWarps * 32) {
+            float v = 0.f;
+#pragma unroll
+            for (int w = 0; w < kRowWarps; ++w) v += first[w * next + c];
+            part[c] = v;
+        }
     }
     if (!r.ok) report_timeout();
 }
 
-// Column sums over the CTAs of part[cta][which][c], 32 columns per CTA, 32 threads a column, joined in a fixed order.
+// Column sums over the CTAs of part[cta][which][c], 32 columns per CTA, joined in a fixed order: eight threads with a piece of 16 bytes
+// each make a line, 128 lines and four loads of each thread are in flight (few CTAs, latency: 16384 x 1024 bf16, 1184 partial sums, 8.1 us
+// with a cold cache, 14.6 with a thread per column).
 // which 0: dw_pre; which 1, with S the sum: dw_post = S (times the channel gate), channel dgate = S (times w_post).
 __global__ void __launch_bounds__(1024) k_column_sums(const float* part, int n, int D, float* dw_pre, float* dw_post, float* dgate, const float* w_post,
                                                       const float* gate, int accumulate) {
-    __shared__ float sh[32][33];
+    __shared__ __align__(16) float sh[128][36];
     pdl_wait();
     pdl_trigger();
-    const int lane = threadIdx.x % 32, r = threadIdx.x / 32;
-    const int c = blockIdx.x * 32 + lane;
-    float s = 0.f;
-    if (c < D) {
-        const float* p = part + (size_t)blockIdx.y * D + c;
-#pragma unroll 4
-        for (int i = r; i < n; i += 32) s += p[(size_t)i * 2 * D];
+    const int piece = threadIdx.x % 8, line = threadIdx.x / 8;
+    const size_t width = part_width(D), c = (size_t)blockIdx.x * 32 + piece * 4;
+    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (c < width) {
+        const float* p = part + blockIdx.y * width + c;
+        for (int i = line; i < n; i += 4 * 128) {
+            float4 v[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                v[k] = i + 128 * k < n ? *reinterpret_cast<const float4*>(p + (size_t)(i + 128 * k) * 2 * width) : make_float4(0.f, 0.f, 0.f, 0.f);
+            sum.x += (v[0].x + v[1].x) + (v[2].x + v[3].x);
+            sum.y += (v[0].y + v[1].y) + (v[2].y + v[3].y);
+            sum.z += (v[0].z + v[1].z) + (v[2].z + v[3].z);
+            sum.w += (v[0].w + v[1].w) + (v[2].w + v[3].w);
+        }
     }
-    sh[r][lane] = s;
+    *reinterpret_cast<float4*>(&sh[line][piece * 4]) = sum;
     __syncthreads();
-    s = sh[lane][r];                               // column r of this CTA's 32, partial sum `lane`
+    const int lane = threadIdx.x % 32, r = threadIdx.x / 32;       // a warp per column
+    float s = (sh[lane][r] + sh[lane + 32][r]) + (sh[lane + 64][r] + sh[lane + 96][r]);
 #pragma unroll
     for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
     const int cc = blockIdx.x * 32 + r;
@@ -673,7 +743,7 @@ __global__ void __launch_bounds__(1024) k_column_sums(const float* part, int n, 
 
 // How a call is launched.  ring: all matrices aligned alike and the row within the pieces that a CTA's threads own.
 struct Plan {
-    bool ring;
+    bool ring, warp;                 // warp: a warp per row
     int threads, elems;              // of a CTA; elements that a thread owns
     int grid, stages;
     uint32_t row_bytes;
@@ -687,18 +757,21 @@ cudaError_t run_plain(const NormArgs& a, bool back, int grid, cudaStream_t s) {
     if (e != cudaSuccess) return e;
     return launch_kernel(back ? k_residual_norm_back<T, kV, kPost, kGate> : k_residual_norm<T, kV, kPost, kGate>, grid, 256, smem, s, true, a);
 }
-template <typename T, int kE, bool kPost, int kGate>
+template <typename T, int kE, bool kPost, int kGate, bool kWarp>
 cudaError_t run_ring(const NormArgs& a, bool back, const Plan& p, cudaStream_t s) {
+    constexpr int kP = kE / kVec<T>;
     const RingArgs r{a, p.stages, p.row_bytes};
-    const cudaError_t e = back ? allow_smem<k_join_back<T, kE / kVec<T>, kPost, kGate>>() : allow_smem<k_join<T, kE / kVec<T>, kPost, kGate>>();
+    const cudaError_t e = back ? allow_smem<k_join_back<T, kP, kPost, kGate, kWarp>>() : allow_smem<k_join<T, kP, kPost, kGate, kWarp>>();
     if (e != cudaSuccess) return e;
-    return launch_kernel(back ? k_join_back<T, kE / kVec<T>, kPost, kGate> : k_join<T, kE / kVec<T>, kPost, kGate>, p.grid, p.threads, p.smem, s, true, r);
+    return launch_kernel(back ? k_join_back<T, kP, kPost, kGate, kWarp> : k_join<T, kP, kPost, kGate, kWarp>, p.grid, p.threads, p.smem, s, true, r);
 }
 template <typename T, bool kPost, int kGate>
 cudaError_t run(const NormArgs& a, bool back, bool wide, const Plan& p, cudaStream_t s) {
     if (!p.ring) return wide ? run_plain<T, kVec<T>, kPost, kGate>(a, back, p.grid, s) : run_plain<T, 1, kPost, kGate>(a, back, p.grid, s);
-    return p.elems == 8 ? run_ring<T, 8, kPost, kGate>(a, back, p, s) : p.elems == 16 ? run_ring<T, 16, kPost, kGate>(a, back, p, s)
-                                                                                    : run_ring<T, 32, kPost, kGate>(a, back, p, s);
+    if (p.warp && p.elems == 8) return run_ring<T, 8, kPost, kGate, true>(a, back, p, s);
+    if constexpr (warp_row(sizeof(T)) > 256)
+        if (p.warp) return run_ring<T, 16, kPost, kGate, true>(a, back, p, s);
+    return p.elems == 16 ? run_ring<T, 16, kPost, kGate, false>(a, back, p, s) : run_ring<T, 32, kPost, kGate, false>(a, back, p, s);
 }
 template <typename T>
 cudaError_t run_kind(const NormArgs& a, bool back, uint32_t gate, bool wide, const Plan& p, cudaStream_t s) {
@@ -749,20 +822,27 @@ Plan plan_of(const Mat (&m)[N], size_t es, uint64_t T, uint64_t D, bool back, ui
     size_t period = 1;
     p.ring = ring_shape(es, D, back, &p.threads, &p.elems) && aligned_alike(m, es, &period);
     p.row_bytes = (uint32_t)((D * es + 15) / 16 * 16);
-    const size_t images = (back ? 4 : 2) + (gate_kind == ABS_GATE_ELEMENT ? 1 : 0), row = images * p.row_bytes;
+    p.warp = D <= warp_row(es);
+    if (p.warp) p.threads = kRowWarps * 32;
+    const size_t images = (back ? 4 : 2) + (gate_kind == ABS_GATE_ELEMENT ? 1 : 0), row = images * p.row_bytes * (p.warp ? kRowWarps : 1);
     size_t ctas = 1;
     if (p.ring) {      // as many CTAs as the registers allow, fewer where two rows would not fit; then as many rows as fit
-        ctas = (size_t)ctas_per_sm(back, p.threads, p.elems);
+        ctas = (size_t)(p.warp ? warp_ctas(back, p.elems) : ctas_per_sm(back, p.threads, p.elems));
         while (ctas > 1 && kRingCtl + 2 * row > kRingSmem / ctas) --ctas;
-        const size_t room = ctas > 1 ? kRingSmem / ctas : kSmemMax;
+        const size_t room = ctas > 1 ? kRingSmem / ctas : kSmemMax, most = p.warp ? 4 : kRingMax;
         const size_t fit = (room - kRingCtl) / row;
         p.ring = fit >= (back ? 1 : 2);
-        p.stages = (int)(fit < (size_t)kRingMax ? fit : (size_t)kRingMax);
+        p.stages = (int)(fit < most ? fit : most);
         p.smem = kRingCtl + p.stages * row;
     }
     if (!p.ring) {
         const uint64_t cap = back ? kBackCtas : kSms * 8;
         p.grid = (int)(T < cap ? T : cap);
+        return p;
+    }
+    if (p.warp) {
+        const uint64_t want = (T + kRowWarps - 1) / kRowWarps, all = (uint64_t)kSms * ctas;
+        p.grid = (int)(want < all ? want : all);
         return p;
     }
     // backward: at least two rows per CTA, whose column sums cost as much as a row (1003 x 1537 fp32: 16.4 us, with four 19.4)
@@ -833,11 +913,11 @@ extern "C" size_t abs_residual_norm_workspace(uint64_t tokens, uint64_t width) {
     uint64_t most = kBackCtas;       // of either type
     for (size_t es : {2, 4}) {
         int threads = 0, elems = 0;
-        const uint64_t ring = ring_shape(es, width, true, &threads, &elems) ? (uint64_t)kSms * ctas_per_sm(true, threads, elems) : 0;
+        const uint64_t ring = width > warp_row(es) && ring_shape(es, width, true, &threads, &elems) ? (uint64_t)kSms * ctas_per_sm(true, threads, elems) : 0;
         if (ring > most) most = ring;
     }
     const uint64_t rows = (tokens + 7) / 8 * 8;
-    return ((size_t)(rows < most ? rows : most) * 2 * width * 4 + 255) / 256 * 256 + 256;
+    return ((size_t)(rows < most ? rows : most) * 2 * part_width(width) * 4 + 255) / 256 * 256 + 256;
 }
 
 extern "C" int abs_residual_norm_backward(const void* dn, uint64_t ld_dn, const void* dy, uint64_t ld_dy, const void* y, uint64_t ld_y,

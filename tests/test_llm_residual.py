@@ -259,3 +259,23 @@ def test_inner_products_that_cancel(llm, gate):
     a["dn"] = a["y"] / p["w_pre"] * (1 + 0.01 * a["dn"])
     check_backward(llm, a, p, 0.7, dy=False)
     check_backward(llm, a, p, 0.7, dy=True)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T,D", [(9003, 100), (9600, 257), (7301, 512), (12000, 8), (20001, 33)])
+@pytest.mark.parametrize("gate,post", [("none", False), ("channel", True), ("element", True)])
+def test_many_narrow_rows(llm, dtype, T, D, gate, post):
+    a, p = make(T, D, dtype, gate, post, 37)
+    check_forward(llm, a, p, 0.7)
+    check_backward(llm, a, p, 0.7, dy=True)
+    for k in ("x", "h", "y", "dn", "dy"):             # rows at a distance of D + 3
+        wide = torch.full((T, D + 3), float("nan"), dtype=a[k].dtype, device=DEV)
+        wide[:, :D] = a[k]
+        a[k] = wide[:, :D]
+    if gate == "element":
+        wide = torch.full((T, D + 3), float("nan"), dtype=p["gate"].dtype, device=DEV)
+        wide[:, :D] = p["gate"]
+        p["gate"] = wide[:, :D]
+    out = [torch.empty(T, D + 3, dtype=a["x"].dtype, device=DEV)[:, :D] for _ in range(3)]
+    check_forward(llm, a, p, 0.7, y=out[0], n=out[1])
+    check_backward(llm, a, p, 0.7, dy=False, dx=out[0], dh=out[1], dgate=out[2] if gate == "element" else None)
