@@ -69,7 +69,9 @@ __device__ __forceinline__ uint32_t magnitude(uint4 r, bf16) {
     return max(m << 16, m & 0xFFFF0000u);
 }
 
-// A unit is eight values; the four lanes of a block are neighbours.  kWide: the rows allow 16-byte loads.
+// A unit is eight values; the four lanes of a block are neighbours.  kWide: the rows allow 16-byte loads.  A block's maximum by
+// two exchanges, its exponent from the maximum's bits; kUnroll units of a thread are loaded before the first is used.  Bound by
+// memory: 16384 x 4096 bf16 41 to 44 us (203 MB).
 template <typename T, bool kWide>
 __global__ void __launch_bounds__(256) k_ckpt8_quantize(const T* x, const __grid_constant__ PackArgs a, uint2* q, uint8_t* e) {
     pdl_wait();
@@ -143,7 +145,7 @@ __device__ __forceinline__ void unpack8(const uint32_t (&raw)[kVec<T> / 4], uint
     }
 }
 
-// Rows on 16-byte boundaries: a unit is one 16-byte piece of a row.
+// Rows on 16-byte boundaries: a unit is one 16-byte piece of a row.  16384 x 4096 bf16: 37 us (203 MB).
 template <typename T>
 __global__ void __launch_bounds__(256) k_ckpt8_dequantize(const uint8_t* q, const uint8_t* e, T* x, const __grid_constant__ PackArgs a) {
     constexpr int kV = kVec<T>;
@@ -267,8 +269,10 @@ __global__ void __launch_bounds__(256) k_ckpt8_dequantize_any(const uint8_t* q, 
 //               16-byte pieces of q become four of bf16.  The exponents come by plain loads, kAhead of a group's runs ahead.
 // Every tile of a row of tiles converts the same operand again.  Beyond kFusedOut output columns the operand is therefore
 // converted once, to bf16 in the workspace (three more bytes of memory traffic per value), and k_wgrad<false> takes both
-// operands by TMA, without converter warps (from kFusedTokens tokens on).  Measured, 8192 tokens x 4096, converted in the kernel / before it: 512 output
-// columns 54 / 61 us, 768 77 / 69, 2048 140 / 117, 4096 265 / 216 (a library bf16 product of operands already in bf16: 182).
+// operands by TMA, without converter warps (from kFusedTokens tokens on).  Measured, 8192 tokens x 4096, converted in the kernel /
+// before it: 512 output columns 57 / 58 us, 768 77 / 71, 2048 141 / 115, 4096 253 / 209 (in a loop that the power limit slows 246; a
+// library bf16 product of operands already in bf16: 182).  Bound by the tensor core there (pipe 74 % busy); on few tokens by the
+// launch, the first copies and the epilogue: 40 x 128 x 128 9.8 us, 515 x 1000 x 1111 17 + 5 for dy's odd rows.
 // The kernel is launched in plain stream order and starts no successor early: chained by programmatic dependent launch, calls
 // in a row hung (each of its waits on a barrier is bounded; the allocation of TMEM and the cluster's barrier are not).
 // Items are dealt out round-robin to the pairs: the whole tiles, as many as fill all pairs equally often, then the rest, each
@@ -326,7 +330,7 @@ __device__ __forceinline__ void tma_load_2d_first(void* dst, const CUtensorMap* 
 }
 // One arrival on the same barrier of the cluster's first CTA.  What it announces -- operand tiles written and fenced for the
 // async proxy, accumulators read and fenced by tcgen05.fence -- is ordered by those fences; a release at cluster scope would
-// make the warp wait for the exponents that it has in flight (617 instead of 350 us).
+// make the warp wait for the exponents that it has in flight (617 instead of 350 us when this form was chosen).
 __device__ __forceinline__ void arrive_first(uint64_t* bar) {
     uint32_t a;
     asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(a) : "r"(smem_u32(bar)));
