@@ -43,7 +43,7 @@ extern "C" {
  *     L = sum_t weight_t loss_t
  *     dL/dz_v = g_t ([v = y] - softmax(z)_v),  g_t = weight_t (-(r A, 0 where clipped) + kl_coef (1 - exp(logp_ref - logp)))
  * (clipped: A > 0 and r > 1 + clip_high, or A < 0 and r < 1 - clip_low).
- *   logits    [tokens, vocab], ld >= vocab.  -inf entries have probability zero.
+ *   logits    [tokens, vocab], ld >= vocab.  -inf entries have probability zero.  A row may have 2^32 - 2^16 bytes (ABS_ELIMIT).
  *   labels    [tokens] int32; weight [tokens]: the token's share of L (for the mean over n tokens 1/n).  A token whose
  *             weight is 0, whose label lies outside [0, vocab), or whose logits are all -inf is left out: its logp is 0, it
  *             adds nothing, its row of dlogits is zero.  (Logits of the first two kinds are not read.)
@@ -64,6 +64,7 @@ int abs_policy_loss(const void *logits, uint32_t dtype, uint64_t tokens, uint64_
  *     s_q = sum of logp over the answer's counted rows      h_p = beta ((s_2p - ref_2p) - (s_2p+1 - ref_2p+1))
  *     pair_loss_p = -(1 - smoothing) log sigmoid(h_p) - smoothing log sigmoid(-h_p)        L = scale sum_p pair_loss_p
  *     dL/dz_v = +-scale beta (sigmoid(h_p) - (1 - smoothing)) ([v = y] - softmax(z)_v)     (+ for the preferred answer)
+ *   logits    as for abs_policy_loss; tokens up to 2^31 - 513 (ABS_ELIMIT)
  *   labels    [tokens] int32; a row whose label lies outside [0, vocab) (a prompt's token), whose logits are all -inf, or
  *             that belongs to no answer is not counted: its row of dlogits is zero.  (Logits of the first kind are not read.)
  *   offsets   [2 pairs + 1] int32 on the device, ascending; values outside [0, tokens] are clamped.  Empty answers are

@@ -1195,6 +1195,11 @@ cudaError_t launch_pref(const PrefArgs& a, int sms, cudaStream_t s) {
 
 bool misaligned(const void* p, size_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) != 0; }
 
+// A row's bytes and its chunks of up to 16 KB are counted in 32 bits; a row's columns, and the rows of an answer in steps of 512, in 31.
+constexpr uint64_t kRowBytesMax = (1ull << 32) - (1ull << 16);
+constexpr uint64_t kTokensMax = (1ull << 31) - 513;
+bool too_wide(uint64_t V, uint32_t dtype) { return V > kRowBytesMax / (dtype == ABS_F32 ? 4 : 2); }
+
 // What the two losses ask of logits, labels and dlogits; nullptr if all is well.
 const char* check_logits(const void* logits, uint32_t dtype, uint64_t T, uint64_t V, uint64_t ld, const int32_t* labels,
                          const void* dlogits, uint64_t ld_d) {
@@ -1226,7 +1231,7 @@ extern "C" int abs_policy_loss(const void* logits, uint32_t dtype, uint64_t toke
                                float clip_low, float clip_high, float kl_coef, float* stats, float* logp, void* dlogits,
                                uint64_t ld_d, void* workspace, size_t workspace_bytes, void* stream) {
     if (const char* why = check_logits(logits, dtype, tokens, vocab, ld, labels, dlogits, ld_d)) return thread_error(ABS_EINVAL, why);
-    if (vocab > 0x7fffffffull) return thread_error(ABS_ELIMIT, "vocab exceeds 2^31 - 1");
+    if (too_wide(vocab, dtype)) return thread_error(ABS_ELIMIT, "vocab: a row of logits exceeds 2^32 - 2^16 bytes");
     if (tokens && (!logp_old || !advantage || !weight || !logp)) return thread_error(ABS_EINVAL, "a per-token array is NULL");
     if (!stats) return thread_error(ABS_EINVAL, "stats must not be NULL");
     if (misaligned(logp_old, 4) || misaligned(logp_ref, 4) || misaligned(advantage, 4) || misaligned(weight, 4) || misaligned(stats, 4) || misaligned(logp, 4))
@@ -1254,7 +1259,8 @@ extern "C" int abs_preference_loss(const void* logits, uint32_t dtype, uint64_t 
                                    float scale, float* stats, float* pair_loss, float* seq_logp, void* dlogits, uint64_t ld_d,
                                    void* workspace, size_t workspace_bytes, void* stream) {
     if (const char* why = check_logits(logits, dtype, tokens, vocab, ld, labels, dlogits, ld_d)) return thread_error(ABS_EINVAL, why);
-    if (vocab > 0x7fffffffull || tokens > 0x7fffffffull) return thread_error(ABS_ELIMIT, "vocab or tokens exceeds 2^31 - 1");
+    if (too_wide(vocab, dtype)) return thread_error(ABS_ELIMIT, "vocab: a row of logits exceeds 2^32 - 2^16 bytes");
+    if (tokens > kTokensMax) return thread_error(ABS_ELIMIT, "tokens exceeds 2^31 - 513");
     if (pairs && (!offsets || !logp_ref || !pair_loss || !seq_logp)) return thread_error(ABS_EINVAL, "a per-pair array is NULL");
     if (!stats) return thread_error(ABS_EINVAL, "stats must not be NULL");
     if (misaligned(offsets, 4) || misaligned(logp_ref, 4) || misaligned(stats, 4) || misaligned(pair_loss, 4) || misaligned(seq_logp, 4))

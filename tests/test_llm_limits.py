@@ -1,0 +1,24 @@
+"""What the language-model operators refuse because they could not do it right, and workspaces that stay within bounds.  Nothing
+here needs a GPU: every call returns from its checks."""
+
+import pytest
+
+from tests.test_llm_refusals import B, P, policy, preference  # noqa: F401  (B: the fixture)
+
+
+@pytest.mark.parametrize("call", [policy, preference])
+@pytest.mark.parametrize("dtype,size", [(0, 4), (1, 2)])
+def test_rows_whose_bytes_pass_32_bits(B, call, dtype, size):  # noqa: F811
+    """A row's bytes are counted in 32 bits, in chunks of up to 16 KB."""
+    for V in ((1 << 32) // size, (1 << 32) // size - 1, ((1 << 32) - (1 << 14)) // size + 1, (1 << 31) - 1 if size == 2 else 1 << 30):
+        assert call(B, V=V, ld=V, ld_d=V, dtype=dtype) == B.ELIMIT
+        assert b"vocab" in B.lib.abs_last_error(None)
+    for V in (((1 << 32) - (1 << 16)) // size, 1 << 20):                  # refused for something that is looked at later
+        assert call(B, V=V, ld=V, ld_d=V, dtype=dtype, n=0) == B.ENOMEM
+
+
+def test_tokens_whose_steps_pass_31_bits(B):  # noqa: F811
+    """An answer's rows are counted in 32 bits, in steps of 512."""
+    for T in ((1 << 31) - 1, (1 << 31) - 512):
+        assert preference(B, T=T) == B.ELIMIT
+    assert preference(B, T=(1 << 31) - 513, n=0) == B.ENOMEM
