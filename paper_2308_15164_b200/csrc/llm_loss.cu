@@ -20,14 +20,15 @@ constexpr float kLog2e = 1.4426950408889634f;
 
 // exp(z - m) as 2^(a z - m2) with m2 = a m rounded, one fused multiply-add and the approximate base-2 unit (relative error
 // about 2e-7 where the result is not negligible beside 1).  The rounding of m2 is common to all that is computed with one
-// m, and a change of m is a factor 2^(m2 - m2'), so that it cancels in every quotient.  a = log2 e; for |m| > 1e30, where a m
-// may overflow, z - m is 0 or beyond any exponent, and a = 1 does.  m = -inf (nothing above -inf yet): a = 1, m2 = 0.
+// m, and a change of m is a factor 2^(m2 - m2'), so that it cancels in every quotient; a logarithm of such a sum is corrected
+// for it (log_sum).  a = log2 e; for |m| > 1e30, where a m may overflow, z - m is 0 or beyond any exponent, and a = 1 does.
+// m = -inf (nothing above -inf yet): a = 1, m2 = 0.
 struct Base {
     float a, m2;
 };
 __device__ __forceinline__ Base base_of(float m) {
     const float a = fabsf(m) > 1e30f ? 1.f : kLog2e;
-    return Base{a, m == -INFINITY ? 0.f : a * m};
+    return Base{a, m == -INFINITY ? 0.f : __fmul_rn(a, m)};      // rounded: not to be drawn into a fused multiply-add
 }
 __device__ __forceinline__ float exp_at(float z, Base b) { return exp2_of(fmaf(z, b.a, -b.m2)); }
 __device__ __forceinline__ float2 exp_at(float2 z, Base b) { return exp2_of(fma2(z, both(b.a), both(-b.m2))); }
@@ -35,6 +36,12 @@ __device__ __forceinline__ float2 exp_at(float2 z, Base b) { return exp2_of(fma2
 struct RowStat {
     float m, s;      // largest element; sum of exp(z - m).  m = -inf: no element is above -inf
 };
+// log sum exp(z - m).  s carries the factor 2^(a m - m2), up to half a unit in the last place of m2 (4e-4 in the logarithm at m = 5000);
+// the product's rounding is exact by one fused multiply-add.
+__device__ __forceinline__ float log_sum(RowStat a) {
+    const Base b = base_of(a.m);
+    return logf(a.s) - 0.693147180559945309f * fmaf(a.m, b.a, -b.m2);
+}
 
 // Maximum over a warp (NaN is left out).
 __device__ __forceinline__ float warp_max(float v) {
@@ -186,7 +193,7 @@ __global__ void __launch_bounds__(G * kGroups) k_policy_rows(PolicyArgs a) {
             const float zy = to_f(row[y]);
             st = row_stat<T, G>(row, a.V, tid, sh);
             if (st.m != -INFINITY || st.s != 0.f) {
-                logp = zy - st.m - logf(st.s);
+                logp = zy - st.m - log_sum(st);
                 const TokenLoss l = token_loss(a, token_in(a, t), logp);
                 g = w * l.slope;
                 if (tid == 0) {
@@ -533,7 +540,7 @@ __global__ void __launch_bounds__(kT + 32, kRowThreads / kT) k_rows(const __grid
                 for (int o = kWarps / 2; o; o >>= 1) all.s += __shfl_xor_sync(0xffffffffu, all.s, o);
                 if (lane == 0) {
                     const bool some = all.m != -INFINITY || all.s != 0.f;
-                    const float logp = some ? zy - all.m - logf(all.s) : 0.f;
+                    const float logp = some ? zy - all.m - log_sum(all) : 0.f;
                     if (kMode == kPolicy) {
                         if (some) {
                             const float w = now.w;
@@ -740,7 +747,7 @@ __global__ void __launch_bounds__(kWarpCta * 32, warp_rows_ctas(kP)) k_warp_rows
 #pragma unroll
                 for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
                 const bool some = m != -INFINITY || s != 0.f;
-                const float logp = some ? zy - m - logf(s) : 0.f;
+                const float logp = some ? zy - m - log_sum(RowStat{m, s}) : 0.f;
                 if (kMode == kPolicy) {
                     TokenLoss l{};
                     if (some) l = token_loss(a.p, now.in, logp);
@@ -1025,7 +1032,7 @@ __global__ void __launch_bounds__(kT, kSliceThreads / kT) k_policy_slices(const 
             }
             if (lane == 0) {
                 const bool some = all.m != -INFINITY || all.s != 0.f;
-                const float logp = some ? zy - all.m - logf(all.s) : 0.f;
+                const float logp = some ? zy - all.m - log_sum(all) : 0.f;
                 float g = 0.f;
                 TokenLoss l{};
                 if (some) {
