@@ -17,17 +17,19 @@ namespace {
 
 constexpr int kStatCtasMax = 2048;   // CTAs that leave partial sums of the policy loss
 constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kHuge = 1073741824.f;      // 2^30
 
 // exp(z - m) as 2^(a z - m2) with m2 = a m rounded, one fused multiply-add and the approximate base-2 unit (relative error
 // about 2e-7 where the result is not negligible beside 1).  The rounding of m2 is common to all that is computed with one
 // m, and a change of m is a factor 2^(m2 - m2'), so that it cancels in every quotient; a logarithm of such a sum is corrected
-// for it (log_sum).  a = log2 e; for |m| > 1e30, where a m may overflow, z - m is 0 or beyond any exponent, and a = 1 does.
-// m = -inf (nothing above -inf yet): a = 1, m2 = 0.
+// for it (log_sum).  a = log2 e below 2^30, where half a unit in the last place of m2, the exponent of that common factor, is at
+// most 64; from there on different z are 64 or more apart (128 in general), exp(z - m) is 1 or nothing beside it, and a = 1 gives that
+// exactly where z = m.  m = -inf (nothing above -inf yet): a = 1, m2 = 0.
 struct Base {
     float a, m2;
 };
 __device__ __forceinline__ Base base_of(float m) {
-    const float a = fabsf(m) > 1e30f ? 1.f : kLog2e;
+    const float a = fabsf(m) >= kHuge ? 1.f : kLog2e;
     return Base{a, m == -INFINITY ? 0.f : __fmul_rn(a, m)};      // rounded: not to be drawn into a fused multiply-add
 }
 __device__ __forceinline__ float exp_at(float z, Base b) { return exp2_of(fmaf(z, b.a, -b.m2)); }
@@ -49,8 +51,14 @@ __device__ __forceinline__ float warp_max(float v) {
     asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
     return r;
 }
+// The factor that takes sums relative to the maximum `from` (above -inf) to those relative to `to` >= from.  Maxima on
+// either side of kHuge are 64 or more apart: nothing is left.
+__device__ __forceinline__ float rescale(float from, float to) {
+    const Base f = base_of(from), t = base_of(to);
+    return f.a == t.a ? exp2_of(f.m2 - t.m2) : 0.f;
+}
 // The sum of `a`, relative to a maximum m >= a.m (where a.m = -inf it is 0, or NaN from NaN elements).
-__device__ __forceinline__ float at_max(RowStat a, float m) { return a.m == -INFINITY ? a.s : a.s * exp2_of(base_of(a.m).m2 - base_of(m).m2); }
+__device__ __forceinline__ float at_max(RowStat a, float m) { return a.m == -INFINITY ? a.s : a.s * rescale(a.m, m); }
 
 template <int G>
 __device__ __forceinline__ RowStat group_stat(RowStat a, float* sh) {
@@ -360,7 +368,7 @@ __device__ __forceinline__ void chunk_stat(const uint8_t* chunk, int tid, int ha
             cm = piece_max(raw[j], cm, T());
         }
     if (cm > m) {
-        if (m != -INFINITY) s2 = mul2(s2, both(exp2_of(base_of(m).m2 - base_of(cm).m2)));
+        if (m != -INFINITY) s2 = mul2(s2, both(rescale(m, cm)));
         m = cm;
     }
     const Base b = base_of(m);
@@ -977,7 +985,7 @@ __global__ void __launch_bounds__(kT, kSliceThreads / kT) k_policy_slices(const 
                     cm = piece_max(raw[1], cm, T());
                 }
                 if (cm > m) {
-                    if (m != -INFINITY) s2 = mul2(s2, both(exp2_of(base_of(m).m2 - base_of(cm).m2)));
+                    if (m != -INFINITY) s2 = mul2(s2, both(rescale(m, cm)));
                     m = cm;
                 }
                 const Base b = base_of(m);
@@ -1057,7 +1065,7 @@ __global__ void __launch_bounds__(kT, kSliceThreads / kT) k_policy_slices(const 
 #pragma unroll
                 for (int j = 0; j < kOwnPieces; ++j)
                     if (j < have) {
-                        const float at = ms[j / 2], f = at == -INFINITY ? mul : mul * exp2_of(base_of(at).m2 - b.m2);
+                        const float at = ms[j / 2], f = at == -INFINITY ? mul : mul * rescale(at, x.x);
                         float2 v[kN];
 #pragma unroll
                         for (int k = 0; k < kN; ++k) v[k] = mul2(e[j][k], both(f));

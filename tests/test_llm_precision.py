@@ -65,3 +65,67 @@ def test_log_probabilities_do_not_depend_on_a_common_offset(llm, T, V, shift, dt
     s = torch.stack([want[: T // 2].sum(), want[T // 2:].sum()])
     # a sum in 64 bits of T / 2 such numbers, rounded once
     assert ((R.d(r.seq_logp) - s).abs() <= T * (1e-6 + R.U32 * float(want.abs().max())) + R.U32 * s.abs()).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T,V", ROWS)
+def test_maxima_on_either_side_of_1e30(llm, T, V, dtype):
+    """Logits of 1e30 and more: of two different ones the smaller has probability 0, wherever in the row they stand."""
+    z, y = logits(T, V, dtype, V), labels(T, V, 3)
+    at, c = torch.arange(T, device=DEV), torch.tensor
+    small, large = (c(v).to(DT[dtype]).to(DEV) for v in (0.99e30, 1.1e30))
+    first = torch.randint(0, V - 1, (T,), generator=gen(5), device=DEV)
+    second = first + 1 + (torch.rand(T, generator=gen(6), device=DEV) * (V - 1 - first)).long()
+    z[at, first], z[at, second] = small, large                    # the larger one comes later
+    half = T // 2
+    z[half:] = small                                              # all of one value but one that is below it
+    z[half:] *= -1
+    z[at[half:], first[half:]] = -large
+    y[:half] = second[:half].int()
+    want = torch.zeros(T, dtype=R.D)                              # logp of the only largest one
+    y[half:] = second[half:].int()
+    want[half:] = -torch.log(torch.tensor(float(V - 1), dtype=R.D))
+    one = torch.ones(T, device=DEV)
+    for kw in (dict(), dict(dlogits=at_another_alignment(z))):
+        r = llm.policy_loss(z, y, want.float().to(DEV), one, one, **kw)
+        R.close(r.logp, want, 1e-5, "logp")
+        R.close(r.loss[None], torch.tensor([-float(T)], dtype=R.D), T * 1e-5, "loss")
+        p = torch.zeros(T, V, dtype=R.D)
+        p[half:] = 1.0 / (V - 1)
+        p[torch.arange(T)[half:], first[half:].cpu()] = 0
+        p[torch.arange(half), second[:half].cpu()] = 1
+        grad = p.clone()
+        grad[torch.arange(T), y.cpu().long()] -= 1
+        R.close(r.dlogits, grad, 1e-5 * torch.ones(T, V, dtype=R.D) * p + 1e-5 * (grad != 0), "dlogits")
+    r = llm.preference_loss(z, y, torch.tensor([0, half, T], dtype=torch.int32, device=DEV), torch.zeros(2, device=DEV))
+    R.close(r.seq_logp, torch.stack([want[:half].sum(), want[half:].sum()]), 1e-5 * T, "seq_logp")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("size", [2.0 ** 24, 1e8, 2.0 ** 30, 1e9, 1.5e9, 1e10, 1e15, 1e25])
+@pytest.mark.parametrize("T,V", ROWS)
+def test_rows_of_large_numbers(llm, T, V, size, dtype):
+    """All logits around +-size, a few units in the last place apart (masks of -1e9 or -1e10 over a whole row, for one)."""
+    unit = float(torch.finfo(DT[dtype]).eps) / 2 * 2.0 ** torch.tensor(size).log2().ceil().item()
+    z = size + unit * torch.randint(-2, 3, (T, V), generator=gen(3), device=DEV).double()
+    z[::2] *= -1
+    z[1::4, : V // 2] /= 4
+    z = z.to(DT[dtype])
+    y = labels(T, V, 3)
+    want, p, _ = R.rows_logp(z, y)
+    w = torch.where(want > -60, 1.0 / T, 0.0).float().to(DEV)      # beyond that a ratio or a probability is nothing
+    live = (w != 0).cpu()
+    want = torch.where(live, want, torch.zeros((), dtype=R.D))
+    one = torch.ones(T, device=DEV)
+    grad = p * live[:, None]
+    grad[torch.arange(T), y.cpu().long()] -= live.to(R.D)
+    # an exponential's exponent has up to 64 units of the common factor in it: off by 2^-18, 2.7e-6 of it; the sum's logarithm likewise
+    tol = 2e-5
+    for kw in (dict(), dict(dlogits=at_another_alignment(z))):
+        r = llm.policy_loss(z, y, want.float().to(DEV), one, w, **kw)
+        R.close(r.logp, want, tol + 4 * R.U32 * want.abs(), "logp")
+        R.close(r.loss[None], -live.to(R.D).mean()[None], 3 * tol, "loss")
+        R.close(r.dlogits, grad / T, (3 * tol * (p + (grad < 0)) + 1e-18) / T, "dlogits")
+    yy = torch.where(w != 0, y, torch.full_like(y, -1))
+    r = llm.preference_loss(z, yy, torch.tensor([0, T // 2, T], dtype=torch.int32, device=DEV), torch.zeros(2, device=DEV))
+    R.close(r.seq_logp, torch.stack([want[: T // 2].sum(), want[T // 2:].sum()]), T * tol + 4 * R.U32 * want.abs().sum(), "seq_logp")
