@@ -277,10 +277,11 @@ __global__ void __launch_bounds__(1024) k_pref_pairs(PrefArgs a) {
                 // the difference in 64 bits, what comes after it in 32
                 const float h = (float)((double)a.beta * ((s - (double)a.logp_ref[2 * p]) - (other - (double)a.logp_ref[2 * p + 1])));
                 const float e = expf(-fabsf(h)), soft = log1pf(e);               // -log sigmoid(+-h) = soft + max(-+h, 0)
-                const float sig = h >= 0.f ? 1.f / (1.f + e) : e / (1.f + e);
+                const float tail = e / (1.f + e), head = 1.f / (1.f + e);         // sigmoid(-|h|), sigmoid(|h|)
                 const float worse = h < 0.f ? -h : 0.f, better = h > 0.f ? h : 0.f;
                 a.pair_loss[p] = h == h ? (1.f - a.smoothing) * (soft + worse) + a.smoothing * (soft + better) : h;
-                slope = a.scale * a.beta * (sig - (1.f - a.smoothing));
+                // sigmoid(h) - (1 - smoothing) without the difference of nearly equal numbers that it is for a well separated pair
+                slope = a.scale * a.beta * (a.smoothing * (h >= 0.f ? head : tail) - (1.f - a.smoothing) * (h >= 0.f ? tail : head));
             }
         }
         __syncthreads();

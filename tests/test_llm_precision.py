@@ -129,3 +129,30 @@ def test_rows_of_large_numbers(llm, T, V, size, dtype):
     yy = torch.where(w != 0, y, torch.full_like(y, -1))
     r = llm.preference_loss(z, yy, torch.tensor([0, T // 2, T], dtype=torch.int32, device=DEV), torch.zeros(2, device=DEV))
     R.close(r.seq_logp, torch.stack([want[: T // 2].sum(), want[T // 2:].sum()]), T * tol + 4 * R.U32 * want.abs().sum(), "seq_logp")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("smoothing", [0.0, 0.1, 1.0])
+def test_preference_gradient_at_large_margins(llm, smoothing, dtype):
+    """A well separated pair's gradient is small, not lost: relative to itself it is as exact as any other."""
+    V, margins = 500, [0.0, 1.0, -1.0, 4.0, 8.0, -8.0, 12.0, -12.0, 16.0, -16.0, 17.0, 20.0, -20.0, 40.0, -40.0, 80.0, -80.0]
+    n = len(margins)
+    z, y = logits(4 * n, V, dtype, 1), labels(4 * n, V, 2)
+    off = torch.arange(0, 4 * n + 1, 2, dtype=torch.int32, device=DEV)
+    s = R.preference(z, y, off, torch.zeros(2 * n))["seq_logp"]
+    ref = s.float()
+    ref[0::2] -= torch.tensor(margins)
+    r = llm.preference_loss(z, y, off, ref.to(DEV), beta=1.0, smoothing=smoothing, scale=1.0)
+    want = R.preference(z, y, off, ref, 1.0, smoothing, 1.0)
+    sm = float(torch.tensor(smoothing))
+    h = want["h"]
+    # without a difference of nearly equal numbers; h is off by the four rows' logp, 1.5e-5 together
+    g = sm * torch.sigmoid(h) - (1 - sm) * torch.sigmoid(-h)
+    assert torch.allclose(g, want["g"][::4], rtol=1e-6, atol=1e-15)
+    eh = 1.5e-5
+    eg = eh * (sm * torch.sigmoid(h) * torch.sigmoid(-h) + (1 - sm) * torch.sigmoid(-h) * torch.sigmoid(h)) + 4e-7 * (sm * torch.sigmoid(h) + (1 - sm) * torch.sigmoid(-h))
+    row = g.repeat_interleave(4) * torch.tensor([1.0, 1.0, -1.0, -1.0], dtype=R.D).repeat(n)
+    _, p, _ = R.rows_logp(z, y)
+    grad = -row[:, None] * p
+    grad[torch.arange(4 * n), y.cpu().long()] += row
+    R.close(r.dlogits, grad, (eg.repeat_interleave(4) + 1e-5 * row.abs())[:, None], "dlogits")
