@@ -47,7 +47,8 @@ extern "C" {
  *   labels    [tokens] int32; weight [tokens]: the token's share of L (for the mean over n tokens 1/n).  A token whose
  *             weight is 0, whose label lies outside [0, vocab), or whose logits are all -inf is left out: its logp is 0, it
  *             adds nothing, its row of dlogits is zero.  (Logits of the first two kinds are not read.)
- *   logp_old, advantage [tokens]; logp_ref [tokens] or NULL (then no KL term, kl_coef must be 0)
+ *   logp_old, advantage [tokens]; logp_ref [tokens] or NULL (then no KL term, kl_coef must be 0);
+ *             with kl_coef 0 it gives the statistic and nothing else
  *   stats     [3] out: L, sum weight_t kl_t (without kl_coef), sum weight_t [t clipped]
  *   logp      [tokens] out
  *   dlogits   [tokens, vocab] out, ld_d >= vocab, or NULL (loss only).  May be the logits themselves (then ld_d = ld);

@@ -174,8 +174,10 @@ __device__ __forceinline__ TokenLoss token_loss(const PolicyArgs& a, TokenIn in,
     if (a.logp_ref) {
         const float d = in.ref - logp, e = expm1f(d);
         r.kl = e - d;
-        r.loss += a.kl_coef * r.kl;
-        r.slope -= a.kl_coef * e;
+        if (a.kl_coef != 0.f) {      // as above: e may be infinite where the term counts for nothing
+            r.loss += a.kl_coef * r.kl;
+            r.slope -= a.kl_coef * e;
+        }
     }
     return r;
 }

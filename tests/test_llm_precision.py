@@ -156,3 +156,21 @@ def test_preference_gradient_at_large_margins(llm, smoothing, dtype):
     grad = -row[:, None] * p
     grad[torch.arange(4 * n), y.cpu().long()] += row
     R.close(r.dlogits, grad, (eg.repeat_interleave(4) + 1e-5 * row.abs())[:, None], "dlogits")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T,V", ROWS)
+def test_a_reference_without_a_coefficient_changes_nothing(llm, T, V, dtype):
+    """logp_ref given for its statistic alone: however far it is, a term with coefficient 0 adds nothing to loss and gradient."""
+    z, y = logits(T, V, dtype, 9), labels(T, V, 10)
+    old = R.rows_logp(z, y)[0].float().to(DEV)
+    z[1, y[1].long()] = float("-inf")                             # the label has probability 0: its kl_t has no bound
+    adv, w = torch.randn(T, generator=gen(4), device=DEV), torch.full((T,), 1.0 / T, device=DEV)
+    ref = old.clone()
+    ref[2], ref[3] = 200.0, float("inf")
+    for place in (lambda: None, lambda: at_another_alignment(z)):
+        a = llm.policy_loss(z, y, old, adv, w, dlogits=place())
+        b = llm.policy_loss(z, y, old, adv, w, logp_ref=ref, kl_coef=0.0, dlogits=place())
+        assert torch.isfinite(a.loss) and torch.isfinite(a.dlogits).all()
+        assert torch.equal(a.loss, b.loss) and torch.equal(a.logp, b.logp) and torch.equal(a.clipped, b.clipped)
+        assert torch.equal(a.dlogits, b.dlogits)
