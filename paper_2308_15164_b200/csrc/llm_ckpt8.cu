@@ -264,7 +264,10 @@ __global__ void __launch_bounds__(256) k_ckpt8_dequantize_any(const uint8_t* q, 
 //   warps 2-5   epilogue: TMEM -> registers -> dw (or a partial sum), coalesced through a padded staging tile.  In
 //               k_wgrad<false> eight warps (2-9), which keep the tile's sums in registers and add a finished accumulator to
 //               them every kSegmentRuns runs: the tensor core drops low bits at each of its additions, so that its error grows
-//               with their number (2.8e-6 of the result at 8192 tokens without, 2.2e-7 with, for 4 % of the time)
+//               with their number (2.8e-6 of the result at 8192 tokens without, 2.2e-7 with, for 4 % of the time).  k_wgrad<true>
+//               has no registers for that; where an item has more than kFusedRuns runs it adds a finished accumulator to what the
+//               same threads wrote before (16384 tokens, 18944 x 256: error 7.0e-6 -> 4.5e-7 for 147 -> 161 us; 8192 tokens, 9728 x 512:
+//               2.7e-6 -> 4.4e-7, 93 -> 100).  The code for it is an instantiation of its own: in the others' epilogue it cost 1 to 2 us
 //   warps 6-21  q -> bf16 operand tile, two groups of eight warps on alternate runs: thread = (token, block of 32), the two
 //               16-byte pieces of q become four of bf16.  The exponents come by plain loads, kAhead of a group's runs ahead.
 // Every tile of a row of tiles converts the same operand again.  Beyond kFusedOut output columns the operand is therefore
@@ -283,6 +286,7 @@ constexpr int kRawBytes = kTK * 128, kABytes = kTK * 128 * 2, kBBytes = kTK * 12
 constexpr int kAhead = 4;
 constexpr int kPitch = 33;
 constexpr int kSegmentRuns = 16;
+constexpr int kFusedRuns = 32;
 
 template <bool kFused>
 struct WgSmem {
@@ -351,8 +355,8 @@ __device__ __forceinline__ void umma2_commit(uint64_t* bar) {
 template <bool kFused>
 constexpr int kWgThreads = kFused ? 704 : 320;
 
-// tm_x: q, or the operand in bf16.
-template <bool kFused>
+// tm_x: q, or the operand in bf16.  kLong (with kFused): items may have more than kFusedRuns runs.
+template <bool kFused, bool kLong>
 __global__ void __launch_bounds__(kWgThreads<kFused>, 1) k_wgrad(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_dy,
                                                                  const __grid_constant__ WgArgs a) {
     constexpr int kStages = WgSmem<kFused>::kStages, kASlots = WgSmem<kFused>::kASlots;
@@ -390,7 +394,7 @@ __global__ void __launch_bounds__(kWgThreads<kFused>, 1) k_wgrad(const __grid_co
         int m0, n0, kb0, kb1;        // first row and column of the pair's tile, runs of 64 tokens
         int part;                    // index of the partial sum, -1: straight to dw
     };
-    constexpr int kSegment = kFused ? 1 << 30 : kSegmentRuns;    // runs that the tensor core adds up on its own
+    constexpr int kSegment = !kFused ? kSegmentRuns : kLong ? kFusedRuns : 1 << 30;    // runs that the tensor core adds up on its own
     auto item_of = [&](int it) {
         Item q;
         int tile = it;
@@ -531,7 +535,7 @@ __global__ void __launch_bounds__(kWgThreads<kFused>, 1) k_wgrad(const __grid_co
         const int qd = warp % 4;
         float* stage = s.out[warp - 2];
         int i = 0;
-        for (int it = pair; it < items; it += pairs, ++i) {
+        for (int it = pair, done = 0; it < items; ++i) {     // done: runs of the item in the segments before
             const Item q = item_of(it);
             const int ab = i & 1;
             const bool ok = mbar_wait(&s.acc_full[ab], (i / 2) & 1) && !*failed;
@@ -545,7 +549,7 @@ __global__ void __launch_bounds__(kWgThreads<kFused>, 1) k_wgrad(const __grid_co
             float* base = part ? a.part + ((size_t)q.part * kTM + row) * kTN : a.dw + (size_t)(q.m0 + row) * a.ld + q.n0;
             const size_t ld = part ? (size_t)kTN : a.ld;
             const int rows = min(32, a.D - (q.m0 + row)), cols = a.N - q.n0;
-            const bool add = a.accumulate && !part;
+            const bool add = a.accumulate && !part, more = kLong && done > 0;
             for (int c = 0; c < kTN / 32; ++c) {
                 uint32_t v[32];
                 tmem_ld_32(tmem + ((uint32_t)(qd * 32) << 16) + (uint32_t)(ab * kTN + c * 32), v);
@@ -560,7 +564,11 @@ __global__ void __launch_bounds__(kWgThreads<kFused>, 1) k_wgrad(const __grid_co
                 __syncwarp();
                 float* p = base + c * 32 + lane;
                 if (c * 32 + lane < cols) {
-                    if (add) {
+                    if (more) {                      // to this thread's own sums of the segments before, in order and with no load to wait for
+#pragma unroll 8
+                        for (int r = 0; r < rows; ++r)
+                            asm volatile("red.global.add.f32 [%0], %1;" ::"l"(p + (size_t)r * ld), "f"(stage[r * kPitch + lane]) : "memory");
+                    } else if (add) {
 #pragma unroll 8
                         for (int r = 0; r < rows; ++r) p[(size_t)r * ld] += stage[r * kPitch + lane];
                     } else {
@@ -569,6 +577,11 @@ __global__ void __launch_bounds__(kWgThreads<kFused>, 1) k_wgrad(const __grid_co
                     }
                 }
                 __syncwarp();
+            }
+            done += kSegment;
+            if (!kLong || done >= q.kb1 - q.kb0) {
+                done = 0;
+                it += pairs;
             }
         }
     } else {                                         // ---- q -> bf16 operand tile
@@ -687,7 +700,6 @@ constexpr int kSms = 148;
 constexpr uint64_t kSizeMax = 0x7fffffc0ull;     // tokens, width, out: what is rounded up to a tile stays an int
 constexpr int kFusedOut = 512;   // output columns up to which the operand is converted in the kernel ..
 constexpr int kFusedTokens = 1024;   // .. or tokens, where the extra launch costs more than the repeated conversion
-constexpr int kMaxRuns = 32;     // runs that k_wgrad<true> adds up in one accumulator, where the tiles are cut at all
 constexpr int kMinRuns = 12;     // runs of 64 tokens that a part of a cut tile has at least: shorter ones do not pay for the join
 
 // How the work is cut: whole output tiles for all pairs of SMs equally often, the rest in runs of tokens.
@@ -708,7 +720,6 @@ bool plan_of(uint64_t T, uint64_t D, uint64_t N, const void* dy, uint64_t ld_dy,
     p.rest = (int)(tiles - p.whole);
     p.fused = N <= (uint64_t)kFusedOut || T <= (uint64_t)kFusedTokens;
     int splits = p.rest ? std::min(pairs / p.rest, kb / kMinRuns) : 1;
-    if (p.fused && p.whole == 0) splits = std::max(splits, (kb + kMaxRuns - 1) / kMaxRuns);
     if (splits < 1) splits = 1;
     p.kb_per_split = std::max(1, (kb + splits - 1) / splits);
     p.splits = std::max(1, (kb + p.kb_per_split - 1) / p.kb_per_split);
@@ -787,6 +798,11 @@ cudaError_t dequantize(const int8_t* q, const uint8_t* e, void* x, uint64_t ld, 
     return pieces <= 4 ? dequantize_any<T, 4>(q, e, x, ld, tokens, width, pieces, s) : pieces <= 8 ? dequantize_any<T, 8>(q, e, x, ld, tokens, width, pieces, s)
          : pieces <= 16 ? dequantize_any<T, 16>(q, e, x, ld, tokens, width, pieces, s) : dequantize_any<T, 32>(q, e, x, ld, tokens, width, pieces, s);
 }
+template <bool kFused, bool kLong>
+cudaError_t launch_wgrad(const CUtensorMap& tx, const CUtensorMap& td, const WgArgs& a, int grid, cudaStream_t s) {
+    const cudaError_t e = allow_smem<k_wgrad<kFused, kLong>>();
+    return e != cudaSuccess ? e : launch_cluster(k_wgrad<kFused, kLong>, grid, 2, false, kWgThreads<kFused>, sizeof(WgSmem<kFused>) + 1024, s, tx, td, a);
+}
 }  // namespace
 }  // namespace abs_sgd
 
@@ -860,13 +876,10 @@ extern "C" int abs_ckpt8_wgrad(const int8_t* q, const uint8_t* e, const void* dy
     a.tiles_n = p.tiles_n; a.whole = p.whole; a.rest = p.rest; a.splits = p.splits; a.kb_per_split = p.kb_per_split;
     a.dw = dw; a.ld = ld_dw; a.part = part; a.accumulate = accumulate != 0;
     const int grid = 2 * std::min(p.whole + p.rest * p.splits, kSms / 2);
-    if (p.fused) {
-        r = allow_smem<k_wgrad<true>>();
-        if (r == cudaSuccess) r = launch_cluster(k_wgrad<true>, grid, 2, false, kWgThreads<true>, sizeof(WgSmem<true>) + 1024, s, tx, td, a);
-    } else {
-        r = allow_smem<k_wgrad<false>>();
-        if (r == cudaSuccess) r = launch_cluster(k_wgrad<false>, grid, 2, false, kWgThreads<false>, sizeof(WgSmem<false>) + 1024, s, tx, td, a);
-    }
+    const int most = p.whole > 0 || p.splits == 1 ? (a.T + kTK - 1) / kTK : a.kb_per_split;      // runs of the longest item
+    r = !p.fused          ? launch_wgrad<false, false>(tx, td, a, grid, s)
+        : most > kFusedRuns ? launch_wgrad<true, true>(tx, td, a, grid, s)
+                            : launch_wgrad<true, false>(tx, td, a, grid, s);
     if (r == cudaSuccess && p.splits > 1) r = launch_kernel(k_wgrad_join, std::min(p.rest * kTM / 4, kSms * 8), 256, 0, s, false, a);
     return r == cudaSuccess ? ABS_OK : thread_error(ABS_ECUDA, cudaGetErrorString(r));
 }

@@ -22,3 +22,10 @@ def test_tokens_whose_steps_pass_31_bits(B):  # noqa: F811
     for T in ((1 << 31) - 1, (1 << 31) - 512):
         assert preference(B, T=T) == B.ELIMIT
     assert preference(B, T=(1 << 31) - 513, n=0) == B.ENOMEM
+
+
+@pytest.mark.parametrize("D,N", [(4096, 512), (128, 256), (100, 64), (18944, 256)])
+def test_partial_sums_do_not_grow_with_the_tokens(B, D, N):  # noqa: F811
+    """The weight gradient's workspace for few output columns: partial sums of at most one tile for each pair of SMs."""
+    for T in (4096, 1 << 17, 1 << 20, 1 << 24):
+        assert B.lib.abs_ckpt8_wgrad_workspace(T, D, N, P, N) <= 74 * 256 * 256 * 4
