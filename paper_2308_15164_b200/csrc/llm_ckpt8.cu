@@ -264,7 +264,8 @@ __global__ void __launch_bounds__(256) k_ckpt8_dequantize_any(const uint8_t* q, 
 //   warps 2-5   epilogue: TMEM -> registers -> dw (or a partial sum), coalesced through a padded staging tile.  In
 //               k_wgrad<false> eight warps (2-9), which keep the tile's sums in registers and add a finished accumulator to
 //               them every kSegmentRuns runs: the tensor core drops low bits at each of its additions, so that its error grows
-//               with their number (2.8e-6 of the result at 8192 tokens without, 2.2e-7 with, for 4 % of the time).  k_wgrad<true>
+//               with their number (of the result's norm at 8192 tokens 2.8e-6 without, 2.0e-7 every 16 runs, 1.6e-7 every 12; half
+//               as much again where a few tokens are much larger than the others; every 8: 1.2e-7, 2 to 7 % slower).  k_wgrad<true>
 //               has no registers for that; where an item has more than kFusedRuns runs it adds a finished accumulator to what the
 //               same threads wrote before (16384 tokens, 18944 x 256: error 7.0e-6 -> 4.5e-7 for 147 -> 161 us; 8192 tokens, 9728 x 512:
 //               2.7e-6 -> 4.4e-7, 93 -> 100).  The code for it is an instantiation of its own: in the others' epilogue it cost 1 to 2 us
@@ -285,7 +286,7 @@ constexpr int kTM = 256, kTN = 256, kTK = 64;    // of a pair
 constexpr int kRawBytes = kTK * 128, kABytes = kTK * 128 * 2, kBBytes = kTK * 128 * 2;
 constexpr int kAhead = 4;
 constexpr int kPitch = 33;
-constexpr int kSegmentRuns = 16;
+constexpr int kSegmentRuns = 12;
 constexpr int kFusedRuns = 32;
 
 template <bool kFused>
@@ -490,11 +491,12 @@ __global__ void __launch_bounds__(kWgThreads<kFused>, 1) k_wgrad(const __grid_co
                 if (!ok) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    uint32_t v[32];
-                    tmem_ld_32(tmem + ((uint32_t)(qd * 32) << 16) + (uint32_t)(ab * kTN + half * 128 + c * 32), v);
+                for (int c = 0; c < 8; ++c) {            // 16 columns: the sums and 32 loaded ones do not fit the registers
+                    uint32_t v[16];
+                    tmem_ld_16(tmem + ((uint32_t)(qd * 32) << 16) + (uint32_t)(ab * kTN + half * 128 + c * 16), v);
 #pragma unroll
-                    for (int j = 0; j < 16; ++j) sum[c][j] = add2(sum[c][j], make_float2(__uint_as_float(v[2 * j]), __uint_as_float(v[2 * j + 1])));
+                    for (int j = 0; j < 8; ++j)
+                        sum[c / 2][c % 2 * 8 + j] = add2(sum[c / 2][c % 2 * 8 + j], make_float2(__uint_as_float(v[2 * j]), __uint_as_float(v[2 * j + 1])));
                 }
                 asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                 __syncwarp();
