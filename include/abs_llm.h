@@ -87,7 +87,7 @@ int abs_preference_loss(const void *logits, uint32_t dtype, uint64_t tokens, uin
 /* Norm behind a block, gate and scaled residual, norm in front of the next block, in one pass:
  *     u = h / rms(h) * w_post  (w_post NULL: u = h)     y = scale x + G u     n = y / rms(y) * w_pre
  *     rms(v) = sqrt(mean_d v_d^2 + eps)
- * x, h, y, n [tokens, width] of `dtype` (y may be x, n may be h, with the same leading dimension); w_post, w_pre [width] fp32.  n is formed from y before
+ * x, h, y, n [tokens, width] of `dtype` (y may be x, n may be h, with the same leading dimension; y and n are different); w_post, w_pre [width] fp32.  n is formed from y before
  * its rounding.  gate: see ABS_GATE_*; ld_gate is used with ABS_GATE_ELEMENT.  width <= 32768 (ABS_ELIMIT). */
 int abs_residual_norm(const void *x, uint64_t ld_x, const void *h, uint64_t ld_h, const void *gate, uint64_t ld_gate,
                       uint32_t gate_kind, const float *w_post, const float *w_pre, float scale, float eps, uint32_t dtype,
@@ -99,7 +99,8 @@ int abs_residual_norm(const void *x, uint64_t ld_x, const void *h, uint64_t ld_h
  *     dgate = dY u, summed over the tokens (channel) or times sigmoid' (element)
  *     dw_pre = sum_t dn yn      dw_post = sum_t dU hn
  * dx, dh and (element) dgate are of `dtype`, all with leading dimension width or more; dx may be dy or dn, dh may be h,
- * an element dgate may be the gate (each with the same leading dimension).  dw_pre, dw_post, (channel) dgate: fp32 [width], 4-byte aligned (slices of a flat
+ * an element dgate may be the gate (each with the same leading dimension); with w_post dx and dgate may not be h, and no two
+ * outputs may be the same (ABS_EINVAL).  dw_pre, dw_post, (channel) dgate: fp32 [width], 4-byte aligned (slices of a flat
  * gradient); accumulate != 0 adds to what they hold.  dw_post must be given exactly when w_post is, dgate exactly when
  * there is a gate.  workspace: abs_residual_norm_workspace(tokens, width) bytes. */
 size_t abs_residual_norm_workspace(uint64_t tokens, uint64_t width);

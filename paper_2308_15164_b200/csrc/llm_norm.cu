@@ -863,6 +863,14 @@ const char* check_mats(const Mat (&m)[N], size_t es, size_t D) {
 }
 // An output in place of an input has to have its leading dimension.
 const char* check_in_place(Mat out, Mat in) { return out.p && out.p == in.p && out.ld != in.ld ? "an output in place of an input needs the same leading dimension" : nullptr; }
+// Outputs have to be different ones.
+template <int N>
+const char* check_apart(const void* const (&out)[N]) {
+    for (int i = 0; i < N; ++i)
+        for (int j = 0; j < i; ++j)
+            if (out[i] && out[i] == out[j]) return "two outputs are the same";
+    return nullptr;
+}
 const char* check_common(uint32_t dtype, uint64_t width, uint32_t gate_kind, const void* gate, const float* w_post, const float* w_pre,
                          float scale, float eps) {
     if (dtype != ABS_F32 && dtype != ABS_BF16) return "dtype must be ABS_F32 or ABS_BF16";
@@ -898,6 +906,7 @@ extern "C" int abs_residual_norm(const void* x, uint64_t ld_x, const void* h, ui
             if (const char* why = check_in_place(out, in)) return thread_error(ABS_EINVAL, why);
     if (tokens == 0) return ABS_OK;
     if (!x || !h || !y || !n) return thread_error(ABS_EINVAL, "x, h, y and n must not be NULL");
+    if (const char* why = check_apart({y, n})) return thread_error(ABS_EINVAL, why);
     NormArgs a{};
     a.x = x; a.ld_x = ld_x; a.h = h; a.ld_h = ld_h; a.gate = gate; a.ld_gate = ld_gate;
     a.w_post = w_post; a.w_pre = w_pre; a.scale = scale; a.eps = eps; a.inv_d = 1.f / (float)width; a.T = tokens; a.D = (int)width;
@@ -944,6 +953,11 @@ extern "C" int abs_residual_norm_backward(const void* dn, uint64_t ld_dn, const 
     if (tokens && (!dn || !y || !h || !dx || !dh)) return thread_error(ABS_EINVAL, "dn, y, h, dx and dh must not be NULL");
     if (!workspace || misaligned(workspace, 256)) return thread_error(ABS_EINVAL, "workspace must be non-NULL and 256-byte aligned");
     if (workspace_bytes < abs_residual_norm_workspace(tokens, width)) return thread_error(ABS_ENOMEM, "workspace too small");
+    if (tokens) {
+        if (const char* why = check_apart({dx, dh, dgate, static_cast<void*>(dw_pre), static_cast<void*>(dw_post)})) return thread_error(ABS_EINVAL, why);
+        // dh is formed from h after dx and dgate of the row are written (k_residual_norm_back)
+        if (w_post && (dx == h || (element && dgate == h))) return thread_error(ABS_EINVAL, "with w_post dx and dgate must not be h");
+    }
     NormArgs a{};
     a.h = h; a.ld_h = ld_h; a.gate = gate; a.ld_gate = ld_gate;
     a.w_post = w_post; a.w_pre = w_pre; a.scale = scale; a.eps = eps; a.inv_d = 1.f / (float)width; a.T = tokens; a.D = (int)width;

@@ -3,7 +3,7 @@ here needs a GPU: every call returns from its checks."""
 
 import pytest
 
-from tests.test_llm_refusals import B, P, policy, preference  # noqa: F401  (B: the fixture)
+from tests.test_llm_refusals import B, P, backward, forward, policy, preference  # noqa: F401  (B: the fixture)
 
 
 @pytest.mark.parametrize("call", [policy, preference])
@@ -29,3 +29,18 @@ def test_partial_sums_do_not_grow_with_the_tokens(B, D, N):  # noqa: F811
     """The weight gradient's workspace for few output columns: partial sums of at most one tile for each pair of SMs."""
     for T in (4096, 1 << 17, 1 << 20, 1 << 24):
         assert B.lib.abs_ckpt8_wgrad_workspace(T, D, N, P, N) <= 74 * 256 * 256 * 4
+
+
+@pytest.mark.parametrize("kw,text", [
+    (dict(dx=2 * P, dh=3 * P, dgate=2 * P), b"two outputs"), (dict(dx=2 * P, dh=2 * P, dgate=4 * P), b"two outputs"), (dict(dx=2 * P, dh=3 * P, dgate=3 * P), b"two outputs"),
+    (dict(dx=2 * P, dh=3 * P, dgate=4 * P, dw_pre=5 * P, dw_post=5 * P), b"two outputs"),
+    # dh is formed from h when dx and dgate of the row are written already
+    (dict(h=2 * P, dx=2 * P, dh=3 * P, dgate=4 * P), b"must not be h"), (dict(h=4 * P, dx=2 * P, dh=3 * P, dgate=4 * P), b"must not be h"),
+    (dict(h=2 * P, kind=1, dx=2 * P, dh=3 * P, dgate=4 * P), b"must not be h")])
+def test_outputs_that_would_spoil_each_other(B, kw, text):  # noqa: F811
+    assert backward(B, **(dict(dw_pre=6 * P, dw_post=7 * P) | kw)) == B.EINVAL
+    assert text in B.lib.abs_last_error(None)
+
+
+def test_two_outputs_of_the_join_at_one_place(B):  # noqa: F811
+    assert forward(B, y=2 * P, n=2 * P) == B.EINVAL and b"two outputs" in B.lib.abs_last_error(None)
