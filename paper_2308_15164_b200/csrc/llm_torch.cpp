@@ -175,6 +175,15 @@ void launch(int index, F fn) {
     throw Refused{nullptr, {}};
 }
 
+// Given outputs (None: not given) that have been written: autograd notices when it has saved one of them.
+template <typename... O>
+void written(O... objects) {
+    auto bump = [](PyObject* o) {
+        if (o != Py_None && !THPVariable_Unpack(o).is_inference()) THPVariable_Unpack(o).unsafeGetTensorImpl()->bump_version();
+    };
+    (bump(objects), ...);
+}
+
 // A tuple of what is given: tensors, None for one that is not defined.
 template <typename... T>
 PyObject* tuple(T&&... tensors) {
@@ -215,6 +224,7 @@ PyObject* policy_loss(PyObject* const* a) {
     launch(l.index, [&](void* s) {
         return abs_policy_loss(l.m.p, l.code, T, l.cols, l.m.ld, y, old, ref, adv, w, lo, hi, kl, stats_p, logp_p, d.m.p, d.m.ld, ws_p, n, s);
     });
+    written(a[9]);
     return tuple(element(stats, 0), element(stats, 1), element(stats, 2), std::move(logp), std::move(d.t));
 }
 
@@ -239,6 +249,7 @@ PyObject* preference_loss(PyObject* const* a) {
         return abs_preference_loss(l.m.p, l.code, l.rows, l.cols, l.m.ld, y, off, pairs, ref, beta, smoothing, scale, loss_p, each_p, seq_p, d.m.p, d.m.ld, ws_p,
                                    n, s);
     });
+    written(a[7]);
     return tuple(std::move(loss), std::move(each), std::move(seq), std::move(d.t));
 }
 
@@ -272,6 +283,7 @@ PyObject* residual_norm(PyObject* const* a) {
     launch(l.index, [&](void* s) {
         return abs_residual_norm(l.m.p, l.m.ld, h.p, h.ld, g.m.p, g.m.ld, g.kind, post, pre, scale, eps, l.code, l.rows, l.cols, y.m.p, y.m.ld, n.m.p, n.m.ld, s);
     });
+    written(a[7], a[8]);
     return tuple(std::move(y.t), std::move(n.t));
 }
 
@@ -302,6 +314,7 @@ PyObject* residual_norm_backward(PyObject* const* a) {
         return abs_residual_norm_backward(dn.p, dn.ld, dy.p, dy.ld, l.m.p, l.m.ld, h.p, h.ld, g.m.p, g.m.ld, g.kind, post, pre, scale, eps, l.code, l.rows, l.cols,
                                           dx.m.p, dx.m.ld, dh.m.p, dh.m.ld, dg.m.p, dg.m.ld, dpre.p, dpost.p, accumulate, ws_p, n, s);
     });
+    written(a[9], a[10], a[11], a[12], a[13]);
     return tuple(std::move(dx.t), std::move(dh.t), std::move(dg.t), std::move(dpre.t), std::move(dpost.t));
 }
 
@@ -341,6 +354,7 @@ PyObject* ckpt8_dequantize(PyObject* const* a) {
     const Like l{nullptr, half ? at::kBFloat16 : at::kFloat, half ? ABS_BF16 : ABS_F32, c.rows, c.width, c.index, {}};
     Out x = out(a[4], "out", l);
     launch(l.index, [&](void* s) { return abs_ckpt8_dequantize(c.q, c.e, c.rows, c.width, x.m.p, x.m.ld, l.code, s); });
+    written(a[4]);
     return THPVariable_Wrap(std::move(x.t));
 }
 
@@ -362,6 +376,7 @@ PyObject* ckpt8_wgrad(PyObject* const* a) {
     launch(c.index, [&](void* s) {
         return abs_ckpt8_wgrad(c.q, c.e, dy.p, dy.ld, c.rows, c.width, N, (float*)dw.m.p, dw.m.ld, accumulate, ws_p, n, s);
     });
+    written(a[4]);
     return THPVariable_Wrap(std::move(dw.t));
 }
 

@@ -3,7 +3,7 @@
 They are the parts of a forward and backward pass that lie around its matrix products; the flat gradient that comes out
 goes to ``AbsSgd.accumulate``.  Every function checks its arguments, allocates its outputs and workspace from PyTorch's
 allocator and enqueues on the current stream of the tensors' device; nothing synchronises.  Outputs that are given are
-used as they are.  Refused arguments raise ``ValueError`` / ``TypeError`` here or ``binding.AbsError`` from the library.
+used as they are, and count as modified in place where autograd has saved them.  Refused arguments raise ``ValueError`` / ``TypeError`` here or ``binding.AbsError`` from the library.
 Matrices may have any row stride; a row is contiguous.  Shapes are [tokens, width]: flatten leading dimensions with
 ``view``.
 """
