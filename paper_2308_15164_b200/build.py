@@ -1,10 +1,12 @@
 """Builds the C-ABI library (sm_100a only) from csrc/*.cu into paper_2308_15164_b200/libabs_sgd.so, and the extension
 module of llm.py (host code: its functions on PyTorch tensors) from csrc/llm_torch.cpp into paper_2308_15164_b200/_llm.so.
+Without PyTorch the library alone is built: its C interface does not need it.
 """
 
 from __future__ import annotations
 
 import glob
+import importlib.util
 import os
 import subprocess
 import sys
@@ -63,6 +65,8 @@ def _module_command(target):
 def build(force: bool = False, verbose: bool = False, extra=()) -> str:
     if force or needs_build():
         _run([os.environ.get("NVCC", "nvcc")] + NVCC_FLAGS + list(extra) + (["-Xptxas", "-v"] if verbose else []) + ["-o", LIB] + sources(), verbose)
+    if importlib.util.find_spec("torch") is None:
+        return LIB
     if force or _older(MODULE, [MODULE_SOURCE, os.path.join(ROOT, "include", "abs_llm.h"), os.path.join(ROOT, "include", "abs_sgd.h"),
                                 os.path.abspath(__file__)]):
         _run(_module_command(MODULE), verbose)
