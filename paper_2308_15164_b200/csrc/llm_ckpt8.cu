@@ -277,8 +277,9 @@ __global__ void __launch_bounds__(256) k_ckpt8_dequantize_any(const uint8_t* q, 
 // before it: 512 output columns 57 / 58 us, 768 77 / 71, 2048 141 / 115, 4096 253 / 209 (in a loop that the power limit slows 246; a
 // library bf16 product of operands already in bf16: 182).  Bound by the tensor core there (pipe 74 % busy); on few tokens by the
 // launch, the first copies and the epilogue: 40 x 128 x 128 9.8 us, 515 x 1000 x 1111 17 + 5 for dy's odd rows.
-// The kernel is launched in plain stream order and starts no successor early: chained by programmatic dependent launch, calls
-// in a row hung (each of its waits on a barrier is bounded; the allocation of TMEM and the cluster's barrier are not).
+// The kernel is launched in plain stream order and starts no successor early: chained by programmatic dependent launch, calls in a
+// row hung, for a reason that is not known.  Every wait on a barrier is bounded, so it was not one of those; nor can a call's TMEM
+// allocation have waited for the call ahead on the same SM, where the shared memory of two such CTAs has no room.
 // Items are dealt out round-robin to the pairs: the whole tiles, as many as fill all pairs equally often, then the rest, each
 // cut along the tokens into `splits` runs so that they too keep all pairs busy; k_wgrad_join adds those up in order.
 // ------------------------------------------------------------------------------------------------
@@ -803,7 +804,7 @@ cudaError_t dequantize(const int8_t* q, const uint8_t* e, void* x, uint64_t ld, 
 template <bool kFused, bool kLong>
 cudaError_t launch_wgrad(const CUtensorMap& tx, const CUtensorMap& td, const WgArgs& a, int grid, cudaStream_t s) {
     const cudaError_t e = allow_smem<k_wgrad<kFused, kLong>>();
-    return e != cudaSuccess ? e : launch_cluster(k_wgrad<kFused, kLong>, grid, 2, false, kWgThreads<kFused>, sizeof(WgSmem<kFused>) + 1024, s, tx, td, a);
+    return e != cudaSuccess ? e : launch_cluster(k_wgrad<kFused, kLong>, grid, 2, kWgThreads<kFused>, sizeof(WgSmem<kFused>) + 1024, s, tx, td, a);
 }
 }  // namespace
 }  // namespace abs_sgd

@@ -1138,7 +1138,7 @@ cudaError_t launch_slices_of(const PolicyArgs& a, SlicePlan p, int sms, int* par
     const size_t smem = kSliceCtl + (size_t)p.stages * p.stage_bytes, most = (size_t)sms * (kSliceThreads / kT) / p.cluster;
     *parts = (int)(a.T < most ? a.T : most);
     const cudaError_t e = allow_smem<k_policy_slices<T, kT>>();
-    return e != cudaSuccess ? e : launch_cluster(k_policy_slices<T, kT>, *parts * p.cluster, p.cluster, false, kT, smem, s, a, p.cluster, p.stages, p.stage_bytes);
+    return e != cudaSuccess ? e : launch_cluster(k_policy_slices<T, kT>, *parts * p.cluster, p.cluster, kT, smem, s, a, p.cluster, p.stages, p.stage_bytes);
 }
 template <typename T>
 cudaError_t launch_slices(const PolicyArgs& a, SlicePlan p, int sms, int* parts, cudaStream_t s) {
