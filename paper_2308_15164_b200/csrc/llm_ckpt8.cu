@@ -273,10 +273,13 @@ __global__ void __launch_bounds__(256) k_ckpt8_dequantize_any(const uint8_t* q, 
 //               16-byte pieces of q become four of bf16.  The exponents come by plain loads, kAhead of a group's runs ahead.
 // Every tile of a row of tiles converts the same operand again.  Beyond kFusedOut output columns the operand is therefore
 // converted once, to bf16 in the workspace (three more bytes of memory traffic per value), and k_wgrad<false> takes both
-// operands by TMA, without converter warps (from kFusedTokens tokens on).  Measured, 8192 tokens x 4096, converted in the kernel /
-// before it: 512 output columns 57 / 58 us, 768 77 / 71, 2048 141 / 115, 4096 253 / 209 (in a loop that the power limit slows 246; a
-// library bf16 product of operands already in bf16: 182).  Bound by the tensor core there (pipe 74 % busy); on few tokens by the
-// launch, the first copies and the epilogue: 40 x 128 x 128 9.8 us, 515 x 1000 x 1111 17 + 5 for dy's odd rows.
+// operands by TMA, without converter warps.  Measured, converted in the kernel / before it, us: 512 output columns 8192 x 1000 27.0 / 27.5,
+// 8192 x 4096 57 / 60, 3000 x 512 24.8 / 24.0; 300 columns 32768 x 512 58 / 70; 256 columns 4096 x 4096 28 / 33, 16384 x 128 24.9 / 23.5; 640 columns
+// 8192 x 4096 82 / 68, 2048 x 4096 30.7 / 24.9, 515 x 4096 18.7 / 15.7, 16 x 4096 14.5 / 12.6; 1111 columns 515 x 600 19.9 / 18.2; 4096 columns
+// 3000 x 4096 125 / 92, 1024 x 4096 57.7 / 41.3, 128 x 4096 36.6 / 28.9.
+// 8192 x 4096 x 4096 210 (in a loop that the power limit slows 255; a library bf16 product of operands already in bf16: 182): bound by the
+// tensor core (pipe 74 % busy); on few tokens by the launch, the first copies and the epilogue: 40 x 128 x 128 10.4 us, 515 x 1000 x 1111 18.4, of which
+// 5 for dy's odd rows.
 // The kernel is launched in plain stream order and starts no successor early: chained by programmatic dependent launch, calls in a
 // row hung, for a reason that is not known.  Every wait on a barrier is bounded, so it was not one of those; nor can a call's TMEM
 // allocation have waited for the call ahead on the same SM, where the shared memory of two such CTAs has no room.
@@ -701,8 +704,7 @@ int grid_for(size_t n, int per_cta) {
 
 constexpr int kSms = 148;
 constexpr uint64_t kSizeMax = 0x7fffffc0ull;     // tokens, width, out: what is rounded up to a tile stays an int
-constexpr int kFusedOut = 512;   // output columns up to which the operand is converted in the kernel ..
-constexpr int kFusedTokens = 1024;   // .. or tokens, where the extra launch costs more than the repeated conversion
+constexpr int kFusedOut = 512;   // output columns up to which the operand is converted in the kernel
 constexpr int kMinRuns = 12;     // runs of 64 tokens that a part of a cut tile has at least: shorter ones do not pay for the join
 
 // How the work is cut: whole output tiles for all pairs of SMs equally often, the rest in runs of tokens.
@@ -721,7 +723,7 @@ bool plan_of(uint64_t T, uint64_t D, uint64_t N, const void* dy, uint64_t ld_dy,
     if (tiles > 0x3fffffff) return false;
     p.whole = (int)(tiles / pairs * pairs);
     p.rest = (int)(tiles - p.whole);
-    p.fused = N <= (uint64_t)kFusedOut || T <= (uint64_t)kFusedTokens;
+    p.fused = N <= (uint64_t)kFusedOut;
     int splits = p.rest ? std::min(pairs / p.rest, kb / kMinRuns) : 1;
     if (splits < 1) splits = 1;
     p.kb_per_split = std::max(1, (kb + splits - 1) / splits);
