@@ -327,9 +327,10 @@ __global__ void __launch_bounds__(G * kGroups) k_pref_grad(PrefArgs a) {
 // touched.  logits and dlogits have to be aligned alike.
 // The chain from a row's last number to its first gradient (reductions, logarithm, the token's loss) leaves the memory idle,
 // so an SM holds several CTAs whose rows are at different points.
-// Bound by the exponential unit and instruction issue, both near half busy: policy loss of 4096 x 32768 bf16 104 us (4.9 TB/s; 87
-// without the exponentials, 98 to 101 without the memory), 1531 x 50257 fp32 124 us; preference, 6.2 thousand rows of 32000 bf16,
-// statistics 72 us, gradient 112.
+// Bound by latency: policy loss of 4096 x 32768 bf16 105 us (4.8 TB/s) with a quarter of the warps there, the exponential unit 54 % busy, issue
+// slots 44 %, DRAM three quarters; 87 us without the exponentials, 98 to 101 without the memory, so that neither alone is what it waits for.
+// 1531 x 50257 fp32 128 us; preference, 6.2 thousand rows of 32000 bf16 (three quarters counted), 185 us, of which the statistics 72; losses
+// without gradient 62 us at 4096 x 32768 bf16 and 55 at 1531 x 50257 fp32 (41 and 47 us of memory).
 // Load number i of a row is chunk i, or chunk i - n beyond the first pass; slots are filled and freed in load order:
 //   first pass    loads 0 .. n - 1, of which those before n - kRing are freed at once
 //   second pass   loads n - kRing .. n - 1 from the ring, then loads n ..

@@ -33,9 +33,14 @@ constexpr size_t warp_row(size_t es) { return es == 2 ? 384 : 256; }
 constexpr int warp_ctas(bool back, int elems) { return back ? 2 : elems == 8 ? 4 : 3; }
 // Elements of a thread.  Forward, 4096 columns, bf16, 16384 rows: 92 us with 16 (two CTAs of 256 threads an SM), 101 with 32
 // (three of 128), 109 with 8 (two of 512).  Backward: 16 leave four warps a scheduler, 32 spread a row's fixed work further and pay
-// where they fill two CTAs of 128 threads, or rows that are wide enough.  8192 rows of bf16, us with 16 / 32: 2560 columns 74 / 97, 3584 66 / 70,
-// 4096 109 / 108 (without gate and w_post 76 / 70), 5120 178 / 200, 6144 147 / 157; 4096 rows: 7168 121 / 112.  fp32: 4096 columns 132 / 157,
-// 5120 215 / 241.  Up to 256 columns: what a warp has to own.
+// where they fill two CTAs of 128 threads, or rows that are wide enough.  8192 rows of bf16, us with 16 / 32 by the gate (none without w_post,
+// the others with it):
+//     columns      2560       3584       3840       4096       4608       5120       6144       7168       8192
+//     none       47 / 60    62 / 64    68 / 65    75 / 69    90 / 114   92 / 118   97 / 118  111 / 118  144 / 130
+//     channel    65 / 79    88 / 84    89 / 86    94 / 91   142 / 151  145 / 157  150 / 160  175 / 162  180 / 170
+//     element    72 / 97   105 / 105  104 / 104  109 / 109  170 / 192  179 / 202  183 / 202  218 / 207  217 / 211
+// (beyond 4096 columns one CTA fills an SM).  4096 rows of fp32, channel / element gate, 16 / 32: 4096 columns 73 / 86, 93 / 111; 5120 columns
+// 86 / 97, 110 / 124; 8192 columns 155 / 157, 192 / 192.  Up to 256 columns: what a warp has to own.
 constexpr int ring_elems(bool back, size_t es, size_t D) {
     if (D <= 8 * 32) return 8;
     if (!back || es == 4) return D <= 16 * 512 ? 16 : 32;
@@ -65,7 +70,9 @@ struct NormArgs {
     float* part;                     // [CTA][2][part_width(D)]: sum dn yn; sum dY hn (channel gate) or dU hn
 };
 
-// 1 / (1 + 2^(-v log2 e)).  Relative error below 4e-7 for |v| < 8 (the exponent is rounded once), 0 and 1 in the limits.
+// 1 / (1 + 2^(-v log2 e)).  Relative error below 4e-7 for |v| < 8 (the exponent is rounded once), 0 and 1 in the limits.  The
+// gradient's factor 1 - sigmoid is a difference and has an error of that size beside 1, as in any form that keeps the sigmoid alone:
+// 1e-3 of itself at v = 8, zero from v = 17 on.  Formed to its own size, 2^(-v log2 e) sigmoid, it costs 3 to 7 % of the backward pass.
 __device__ __forceinline__ float sigmoid(float v) {
     float e, r;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(v * -1.4426950408889634f));

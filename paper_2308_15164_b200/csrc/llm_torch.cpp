@@ -2,9 +2,10 @@
 //
 // A call on a few tokens is bound by the host: through ctypes a policy loss of 7 x 8192 took 21.7 us a call, of which the
 // library's own function was 6.7 us and the rest the interpreter's (arguments checked, outputs made, addresses converted);
-// compiled, 9.7 us (preference of one pair 22.5 -> 11.4, residual forward of 5 x 1024 11.7 -> 4.6).  Arguments are checked, outputs and workspace come from PyTorch's allocator on the current stream, the library's
-// function is called without the interpreter's lock, and nothing synchronises.  What is refused raises TypeError / ValueError,
-// a status of the library binding.AbsError; no C++ exception leaves a function.
+// compiled, 9.2 us (preference of one pair 22.5 -> 12.2, residual forward of 5 x 1024 11.7 -> 4.2).  Arguments are checked,
+// outputs and workspace come from PyTorch's allocator on the current stream, the library's function is called without the
+// interpreter's lock, and nothing synchronises.  What is refused raises TypeError / ValueError, a status of the library
+// binding.AbsError; no C++ exception leaves a function.
 
 #include <ATen/cuda/EmptyTensor.h>
 #include <c10/cuda/CUDAGuard.h>
