@@ -50,3 +50,19 @@ def test_many_tokens_and_few_output_columns(llm, T, D, N):
     assert off_by(out, want + keep.double()) <= MANY
     assert torch.equal(llm.ckpt8_wgrad(c, dy), got)
     llm.check()
+
+
+@pytest.mark.parametrize("T,D,N", [(1, 19000, 200), (1000, 10000, 300), (2048, 18944, 256), (700, 9728, 512), (130, 40000, 40)])
+def test_more_tiles_than_pairs_of_multiprocessors(llm, T, D, N):
+    """Few tokens and output columns, many input columns: several tiles for each pair, whole ones and what is left of them."""
+    c = llm.ckpt8_quantize(randn(4, T, D))
+    dy = randn(5, T, N).bfloat16()
+    got = llm.ckpt8_wgrad(c, dy)
+    assert off_by(got, want_of(c, dy)) <= MANY
+    flat = torch.full((D * N + 5,), 3.0, device=DEV)
+    view = flat[3:3 + D * N].view(D, N)
+    llm.ckpt8_wgrad(c, dy, out=view)
+    assert torch.equal(view, got)
+    llm.ckpt8_wgrad(c, dy, out=view, accumulate=True)
+    assert torch.equal(view, got + got) and (flat[:3] == 3).all() and (flat[3 + D * N:] == 3).all()
+    llm.check()
