@@ -10,6 +10,12 @@
  *     abs_residual_norm_backward  its gradients
  *     abs_ckpt8_quantize / _dequantize   an activation kept for the backward pass in 8 bits
  *     abs_ckpt8_wgrad             gradient of a linear layer's weight from such an activation
+ *     abs_embed, _backward        scaled embedding lookup and its gradient
+ *     abs_layer_norm, _backward   layer norm and its gradients
+ *     abs_linear, _dgrad, _wgrad  linear layer with bias, activation and residual, and its gradients
+ *     abs_activation_backward     through an activation that no abs_linear_dgrad follows
+ *     abs_recurrence, _backward   gated linear recurrence over packed sequences and its gradients
+ *     abs_recurrence_step         one token of each sequence
  *
  * Conventions
  *   - No context: a call works on the CURRENT device, enqueues on `stream` (a cudaStream_t, NULL = default stream) and
@@ -133,6 +139,111 @@ size_t abs_ckpt8_wgrad_workspace(uint64_t tokens, uint64_t width, uint64_t out, 
 int abs_ckpt8_wgrad(const int8_t *q, const uint8_t *e, const void *dy, uint64_t ld_dy, uint64_t tokens, uint64_t width,
                     uint64_t out, float *dw, uint64_t ld_dw, int accumulate, void *workspace, size_t workspace_bytes,
                     void *stream);
+
+/* y[t, :] = scale table[ids[t], :]; a row whose id lies outside [0, vocab) (padding) is zero.
+ *   ids [tokens] int32;  table [vocab, width] fp32, ld_table >= width;  y [tokens, width] of `dtype`.
+ * tokens and vocab up to 2^31 - 64, width up to 2^23 (ABS_ELIMIT). */
+int abs_embed(const int32_t *ids, uint64_t tokens, const float *table, uint64_t ld_table, uint64_t vocab, uint64_t width, float scale,
+              uint32_t dtype, void *y, uint64_t ld_y, void *stream);
+
+/* dtable[v, :] = scale sum over the tokens with id v of dy[t, :], in the tokens' order; every row is written, those of no token
+ * with zeros.  accumulate != 0: added to what the table holds, rows of no token are not touched.
+ *   dy [tokens, width] of `dtype`; dtable [vocab, width] fp32, ld_dtable >= width, 4-byte aligned (a slice of a flat gradient).
+ * Limits as for abs_embed.  workspace: abs_embed_backward_workspace() bytes. */
+size_t abs_embed_backward_workspace(uint64_t tokens, uint64_t vocab, uint64_t width);
+int abs_embed_backward(const void *dy, uint64_t ld_dy, uint32_t dtype, const int32_t *ids, uint64_t tokens, uint64_t vocab, uint64_t width,
+                       float scale, float *dtable, uint64_t ld_dtable, int accumulate, void *workspace, size_t workspace_bytes,
+                       void *stream);
+
+/* n = (x - mean) r w + b,  r = 1 / sqrt(mean_d (x - mean)^2 + eps).
+ *   x, n [tokens, width] of `dtype` (n may be x, with the same leading dimension); w, b [width] fp32, b NULL: no shift.
+ *   width <= 32768 (ABS_ELIMIT). */
+int abs_layer_norm(const void *x, uint64_t ld_x, const float *w, const float *b, float eps, uint32_t dtype, uint64_t tokens,
+                   uint64_t width, void *n, uint64_t ld_n, void *stream);
+
+/* Gradients of abs_layer_norm from dn at the stored x, with xh = (x - mean) r and a = dn w:
+ *     dx = dskip + r (a - mean(a) - xh mean(a xh))      dw = sum_t dn xh      db = sum_t dn
+ * dskip: what reaches x around the norm (a residual stream's gradient), NULL: nothing.  dx may be dn, x or dskip (same leading
+ * dimension).  dw, db: fp32 [width], 4-byte aligned; db NULL: not wanted; accumulate != 0 adds to what they hold.
+ * workspace: abs_layer_norm_workspace(tokens, width) bytes. */
+size_t abs_layer_norm_workspace(uint64_t tokens, uint64_t width);
+int abs_layer_norm_backward(const void *dn, uint64_t ld_dn, const void *x, uint64_t ld_x, const void *dskip, uint64_t ld_dskip,
+                            const float *w, float eps, uint32_t dtype, uint64_t tokens, uint64_t width, void *dx, uint64_t ld_dx,
+                            float *dw, float *db, int accumulate, void *workspace, size_t workspace_bytes, void *stream);
+
+#define ABS_ACT_NONE 0u  /* z                                                */
+#define ABS_ACT_RELU 1u  /* max(z, 0); slope 0 at 0                          */
+#define ABS_ACT_GELU 2u  /* z Phi(z), Phi the normal distribution function   */
+#define ABS_ACT_SILU 3u  /* z / (1 + exp(-z))                                */
+
+/* A linear layer on the tcgen05 tensor cores, operands bf16, sums fp32:
+ *     z = x w + bias      y = act(z) + residual
+ *   x [tokens, in], w [in, out] bf16;  bias [out] fp32 or NULL;  residual [tokens, out] of `dtype` or NULL
+ *   y [tokens, out] of `dtype` (may be the residual, with the same leading dimension), formed from z before any rounding
+ *   z [tokens, out] bf16 out, NULL: not kept (abs_linear_dgrad and abs_activation_backward take it)
+ * No output may be an operand of the product, or another output.  tokens, in and out up to 2^31 - 64 (ABS_ELIMIT).
+ * workspace: abs_linear_workspace(...) bytes for the same sizes and operands: partial sums where `in` is split over the GPU, copies of
+ * operands whose rows are not 16-byte aligned.  May be 0 (NULL is taken then).  The kernel's waits are bounded; see abs_llm_check. */
+size_t abs_linear_workspace(uint64_t tokens, uint64_t in, uint64_t out, const void *x, uint64_t ld_x, const void *w, uint64_t ld_w);
+int abs_linear(const void *x, uint64_t ld_x, const void *w, uint64_t ld_w, const float *bias, uint32_t act, const void *residual,
+               uint64_t ld_residual, uint32_t dtype, uint64_t tokens, uint64_t in, uint64_t out, void *y, uint64_t ld_y, void *z,
+               uint64_t ld_z, void *workspace, size_t workspace_bytes, void *stream);
+
+/* The gradient of a linear layer's input, through the activation that made this input:
+ *     dx = (dy w^T) act'(z) + residual
+ *   dy [tokens, out], w [in, out] bf16;  z [tokens, in] bf16: the pre-activation whose activation was x (NULL exactly with
+ *   ABS_ACT_NONE);  residual [tokens, in] of `dtype` or NULL: what else reaches x's origin;  dx [tokens, in] of `dtype`; it may be the
+ *   residual, or, as bf16, z (same leading dimension).
+ * workspace: abs_linear_dgrad_workspace(...), as above. */
+size_t abs_linear_dgrad_workspace(uint64_t tokens, uint64_t in, uint64_t out, const void *dy, uint64_t ld_dy, const void *w, uint64_t ld_w);
+int abs_linear_dgrad(const void *dy, uint64_t ld_dy, const void *w, uint64_t ld_w, uint32_t act, const void *z, uint64_t ld_z,
+                     const void *residual, uint64_t ld_residual, uint32_t dtype, uint64_t tokens, uint64_t in, uint64_t out, void *dx,
+                     uint64_t ld_dx, void *workspace, size_t workspace_bytes, void *stream);
+
+/* The gradients of a linear layer's weight and bias:  dw (+)= x^T dy,  db (+)= sum_t dy[t, :].
+ *   x [tokens, in], dy [tokens, out] bf16;  dw [in, out] fp32, ld_dw >= out, 4-byte aligned;  db [out] fp32 or NULL
+ *   accumulate != 0 adds to what they hold.  workspace: abs_linear_wgrad_workspace(...) bytes, as above. */
+size_t abs_linear_wgrad_workspace(uint64_t tokens, uint64_t in, uint64_t out, const void *x, uint64_t ld_x, const void *dy, uint64_t ld_dy);
+int abs_linear_wgrad(const void *x, uint64_t ld_x, const void *dy, uint64_t ld_dy, uint64_t tokens, uint64_t in, uint64_t out, float *dw,
+                     uint64_t ld_dw, float *db, int accumulate, void *workspace, size_t workspace_bytes, void *stream);
+
+/* dz = dy act'(z): dy [tokens, width] of `dtype`, z and dz [tokens, width] bf16 (what the products take).  dz may be z or, as bf16, dy
+ * (same leading dimension). */
+int abs_activation_backward(const void *dy, uint64_t ld_dy, uint32_t dtype, const void *z, uint64_t ld_z, uint32_t act, uint64_t tokens,
+                            uint64_t width, void *dz, uint64_t ld_dz, void *stream);
+
+#define ABS_RECURRENCE_BLEND 0u  /* h_t = a_t h_{t-1} + (1 - a_t) x_t   */
+#define ABS_RECURRENCE_ADD   1u  /* h_t = a_t h_{t-1} + x_t             */
+
+/* Gated linear recurrence, every channel on its own, a_t = sigmoid(g_t), over packed sequences:
+ *   sequence q holds the rows offsets[q] .. offsets[q + 1] - 1; before its first row h is h0[q] (h0 NULL: 0)
+ *   x, g [tokens, width] of `dtype`;  y [tokens, width] of `dtype` out: h_t (may be x or g, with the same leading dimension); rows of no
+ *   sequence are zero.  The state itself stays fp32.
+ *   offsets [seqs + 1] int32 on the device, ascending, values outside [0, tokens] are clamped; empty sequences are allowed.
+ *   NULL: one sequence of all rows (seqs = 1).
+ *   h0, last [seqs, width] fp32, packed; last out (NULL: not wanted): h behind the last row (of an empty sequence h0).  last may be h0.
+ * tokens, width and seqs up to 2^31 - 1024 (ABS_ELIMIT).  workspace: abs_recurrence_workspace(tokens, width) bytes, may be 0.  The kernel's waits
+ * are bounded; see abs_llm_check. */
+size_t abs_recurrence_workspace(uint64_t tokens, uint64_t width);
+int abs_recurrence(const void *x, uint64_t ld_x, const void *g, uint64_t ld_g, const int32_t *offsets, uint64_t seqs, const float *h0,
+                   uint32_t kind, uint32_t dtype, uint64_t tokens, uint64_t width, void *y, uint64_t ld_y, float *last, void *workspace,
+                   size_t workspace_bytes, void *stream);
+
+/* Gradients of abs_recurrence at the stored x, g and y, from dy and dlast (NULL: nothing reads last), with h_{t-1} the row of y
+ * before (h0 in front of a sequence's first):
+ *     d_t = dy_t + a_{t+1} d_{t+1}  (a sequence's last row: dy_t + dlast)      dh0 = a d of its first row (of an empty one: dlast)
+ *     dx = (1 - a) d,  dg = d (h_{t-1} - x) a (1 - a)   (BLEND)         dx = d,  dg = d h_{t-1} a (1 - a)   (ADD)
+ *   dx and dg are different ones; each may be dy, x or g, with the same leading dimension, neither may be y.  dh0 [seqs, width] fp32
+ *   out, NULL: not wanted; it may be dlast.  Rows of no sequence get zeros.  workspace as for abs_recurrence. */
+int abs_recurrence_backward(const void *dy, uint64_t ld_dy, const void *x, uint64_t ld_x, const void *g, uint64_t ld_g, const void *y,
+                            uint64_t ld_y, const int32_t *offsets, uint64_t seqs, const float *h0, const float *dlast, uint32_t kind,
+                            uint32_t dtype, uint64_t tokens, uint64_t width, void *dx, uint64_t ld_dx, void *dg, uint64_t ld_dg, float *dh0,
+                            void *workspace, size_t workspace_bytes, void *stream);
+
+/* One row for each of `seqs` sequences: y and out = a h + (1 - a) x (or + x).  x, g, y [seqs, width] of `dtype` (y may be x or g);
+ * h, out [seqs, width] fp32, packed; out may be h. */
+int abs_recurrence_step(const void *x, uint64_t ld_x, const void *g, uint64_t ld_g, const float *h, uint32_t kind, uint32_t dtype,
+                        uint64_t seqs, uint64_t width, void *y, uint64_t ld_y, float *out, void *stream);
 
 /* Blocks until `stream` has finished and reports the device-side status of the calls of this header on the current
  * device: ABS_OK, ABS_ECUDA, or once ABS_ETIMEOUT (a bounded wait inside a kernel ran out; its tile was not written). */

@@ -111,6 +111,24 @@ _sig = {
     "abs_ckpt8_dequantize": (ctypes.c_int, [_vp, _vp, _u64, _u64, _vp, _u64, _u32, _vp]),
     "abs_ckpt8_wgrad_workspace": (ctypes.c_size_t, [_u64, _u64, _u64, _vp, _u64]),
     "abs_ckpt8_wgrad": (ctypes.c_int, [_vp, _vp, _vp, _u64, _u64, _u64, _u64, _vp, _u64, ctypes.c_int, _vp, ctypes.c_size_t, _vp]),
+    "abs_embed": (ctypes.c_int, [_vp, _u64, _vp, _u64, _u64, _u64, _f32, _u32, _vp, _u64, _vp]),
+    "abs_embed_backward_workspace": (ctypes.c_size_t, [_u64] * 3),
+    "abs_embed_backward": (ctypes.c_int, [_vp, _u64, _u32, _vp, _u64, _u64, _u64, _f32, _vp, _u64, ctypes.c_int, _vp, ctypes.c_size_t, _vp]),
+    "abs_layer_norm": (ctypes.c_int, [_vp, _u64, _vp, _vp, _f32, _u32, _u64, _u64, _vp, _u64, _vp]),
+    "abs_layer_norm_workspace": (ctypes.c_size_t, [_u64, _u64]),
+    "abs_layer_norm_backward": (ctypes.c_int, [_vp, _u64] * 3 + [_vp, _f32, _u32, _u64, _u64, _vp, _u64, _vp, _vp, ctypes.c_int, _vp, ctypes.c_size_t, _vp]),
+    "abs_linear_workspace": (ctypes.c_size_t, [_u64] * 3 + [_vp, _u64] * 2),
+    "abs_linear": (ctypes.c_int, [_vp, _u64] * 2 + [_vp, _u32, _vp, _u64, _u32, _u64, _u64, _u64] + [_vp, _u64] * 2 + [_vp, ctypes.c_size_t, _vp]),
+    "abs_linear_dgrad_workspace": (ctypes.c_size_t, [_u64] * 3 + [_vp, _u64] * 2),
+    "abs_linear_dgrad": (ctypes.c_int, [_vp, _u64] * 2 + [_u32] + [_vp, _u64] * 2 + [_u32, _u64, _u64, _u64, _vp, _u64, _vp, ctypes.c_size_t, _vp]),
+    "abs_linear_wgrad_workspace": (ctypes.c_size_t, [_u64] * 3 + [_vp, _u64] * 2),
+    "abs_linear_wgrad": (ctypes.c_int, [_vp, _u64] * 2 + [_u64] * 3 + [_vp, _u64, _vp, ctypes.c_int, _vp, ctypes.c_size_t, _vp]),
+    "abs_activation_backward": (ctypes.c_int, [_vp, _u64, _u32, _vp, _u64, _u32, _u64, _u64, _vp, _u64, _vp]),
+    "abs_recurrence_workspace": (ctypes.c_size_t, [_u64, _u64]),
+    "abs_recurrence": (ctypes.c_int, [_vp, _u64] * 2 + [_vp, _u64, _vp, _u32, _u32, _u64, _u64, _vp, _u64, _vp, _vp, ctypes.c_size_t, _vp]),
+    "abs_recurrence_backward": (ctypes.c_int, [_vp, _u64] * 4 + [_vp, _u64, _vp, _vp, _u32, _u32, _u64, _u64] + [_vp, _u64] * 2 + [_vp, _vp, ctypes.c_size_t,
+                                                                                                                            _vp]),
+    "abs_recurrence_step": (ctypes.c_int, [_vp, _u64] * 2 + [_vp, _u32, _u32, _u64, _u64, _vp, _u64, _vp, _vp]),
     "abs_llm_check": (ctypes.c_int, [_vp]),
 }
 for _name, (_res, _args) in _sig.items():

@@ -891,10 +891,12 @@ extern "C" int abs_ckpt8_wgrad(const int8_t* q, const uint8_t* e, const void* dy
 
 extern "C" int abs_llm_check(void* stream) {
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    int st[3] = {0, 0, 0};
-    cudaError_t r = take_status(&st[0], s);
-    if (r == cudaSuccess) r = take_status_norm(&st[1], s);
-    if (r == cudaSuccess) r = take_status_loss(&st[2], s);
-    if (r != cudaSuccess) return thread_error(ABS_ECUDA, cudaGetErrorString(r));
-    return st[0] == 0 && st[1] == 0 && st[2] == 0 ? ABS_OK : thread_error(ABS_ETIMEOUT, "a bounded wait inside a kernel ran out");
+    int any = 0;
+    for (const auto take : {&take_status, &take_status_norm, &take_status_loss, &take_status_layer_norm, &take_status_linear, &take_status_recurrence}) {
+        int st = 0;
+        const cudaError_t r = take(&st, s);
+        if (r != cudaSuccess) return thread_error(ABS_ECUDA, cudaGetErrorString(r));
+        any |= st;
+    }
+    return any == 0 ? ABS_OK : thread_error(ABS_ETIMEOUT, "a bounded wait inside a kernel ran out");
 }

@@ -1,0 +1,491 @@
+// Layer norm, forward and backward (abs_layer_norm*).
+//
+//     n = (x - mean) r w + b,  r = 1 / sqrt(mean (x - mean)^2 + eps)
+// Backward with c = x - mean, xh = c r, a = dn w:  dx = dskip + r (a - mean(a)) - c r^3 mean(a c),  dw = sum dn xh,  db = sum dn.
+// The variance is taken about the row's own mean, from the values that the thread holds (x^2 - mean^2 would lose what a large
+// common offset leaves), so that a row is a chain of two reductions.  Bound by memory: forward 2, backward 3 (4 with dskip)
+// elements per position.
+#include <math.h>
+
+#include "abs_internal.h"
+#include "abs_llm.h"
+#include "llm_host.h"
+#include "llm_status.cuh"
+#include "row_ring.cuh"
+
+namespace abs_sgd {
+namespace {
+
+constexpr int kWidthMax = 32768;
+constexpr int kSms = 148;
+constexpr int kBackCtas = 296;       // CTAs of the plain backward kernel
+constexpr int kRingCtasMax = 16;
+// Threads of an SM for the ring kernels and CTAs of the form with a warp per row, by the elements that a thread owns: what the
+// registers leave room for.
+constexpr int ring_threads(bool back, int elems) { return back && elems == 32 ? 256 : 512; }
+constexpr int warp_ctas(bool back, int elems) { return back ? 2 : elems == 8 ? 4 : 3; }
+constexpr size_t warp_row(size_t es) { return es == 2 ? 384 : 256; }
+constexpr int ring_elems(size_t D) { return D <= 8 * 32 ? 8 : D <= 16 * 512 ? 16 : 32; }
+
+struct LnArgs {
+    const void *x, *dn, *skip;       // forward: x only
+    size_t ld_x, ld_dn, ld_skip;
+    const float *w, *b;
+    float eps, inv_d;
+    size_t T;
+    int D;
+    void* out;                       // n; backward dx
+    size_t ld_out;
+    float* part;                     // [CTA][2][part_width(D)]: sum dn xh, sum dn
+    int stages;
+    uint32_t row_bytes;
+};
+
+// kV consecutive elements at a time, kV = 1 for rows that are not 16-byte aligned.
+template <typename T, int kV>
+__global__ void __launch_bounds__(256) k_layer_norm_plain(const __grid_constant__ LnArgs a) {
+    __shared__ float sh[8];
+    pdl_wait();
+    pdl_trigger();
+    for (size_t t = blockIdx.x; t < a.T; t += gridDim.x) {
+        const T* x = static_cast<const T*>(a.x) + t * a.ld_x;
+        T* n = static_cast<T*>(a.out) + t * a.ld_out;
+        float s[1] = {0.f};
+        for (int c = threadIdx.x * kV; c < a.D; c += 256 * kV) {
+            float v[kV];
+            Pack<T, kV>::load(x + c, v);
+#pragma unroll
+            for (int k = 0; k < kV; ++k) s[0] += v[k];
+        }
+        group_sum<256, 1>(s, sh);
+        const float mean = s[0] * a.inv_d;
+        s[0] = 0.f;
+        for (int c = threadIdx.x * kV; c < a.D; c += 256 * kV) {
+            float v[kV];
+            Pack<T, kV>::load(x + c, v);
+#pragma unroll
+            for (int k = 0; k < kV; ++k) s[0] += (v[k] - mean) * (v[k] - mean);
+        }
+        group_sum<256, 1>(s, sh);
+        const float r = 1.f / sqrtf(s[0] * a.inv_d + a.eps);
+        for (int c = threadIdx.x * kV; c < a.D; c += 256 * kV) {
+            float v[kV];
+            Pack<T, kV>::load(x + c, v);
+#pragma unroll
+            for (int k = 0; k < kV; ++k) v[k] = (v[k] - mean) * r * a.w[c + k] + (a.b ? a.b[c + k] : 0.f);
+            Pack<T, kV>::store(n + c, v);
+        }
+    }
+}
+
+template <typename T, int kV>
+__global__ void __launch_bounds__(256) k_layer_norm_back_plain(const __grid_constant__ LnArgs a) {
+    __shared__ float sh[24];
+    pdl_wait();
+    pdl_trigger();
+    float *col = a.part + blockIdx.x * 2 * part_width(a.D), *col_b = col + part_width(a.D);
+    for (int c = threadIdx.x * kV; c < a.D; c += 256 * kV)
+#pragma unroll
+        for (int k = 0; k < kV; ++k) col[c + k] = col_b[c + k] = 0.f;
+    for (size_t t = blockIdx.x; t < a.T; t += gridDim.x) {
+        const T* x = static_cast<const T*>(a.x) + t * a.ld_x;
+        const T* dn = static_cast<const T*>(a.dn) + t * a.ld_dn;
+        const T* skip = a.skip ? static_cast<const T*>(a.skip) + t * a.ld_skip : nullptr;
+        T* dx = static_cast<T*>(a.out) + t * a.ld_out;
+        float m[1] = {0.f};
+        for (int c = threadIdx.x * kV; c < a.D; c += 256 * kV) {
+            float v[kV];
+            Pack<T, kV>::load(x + c, v);
+#pragma unroll
+            for (int k = 0; k < kV; ++k) m[0] += v[k];
+        }
+        group_sum<256, 1>(m, sh);
+        const float mean = m[0] * a.inv_d;
+        float s[3] = {0.f, 0.f, 0.f};            // sum c^2, a, a c
+        for (int c = threadIdx.x * kV; c < a.D; c += 256 * kV) {
+            float v[kV], d[kV];
+            Pack<T, kV>::load(x + c, v);
+            Pack<T, kV>::load(dn + c, d);
+#pragma unroll
+            for (int k = 0; k < kV; ++k) {
+                const float e = v[k] - mean, f = d[k] * a.w[c + k];
+                s[0] += e * e;
+                s[1] += f;
+                s[2] += f * e;
+            }
+        }
+        group_sum<256, 3>(s, sh);
+        const float r = 1.f / sqrtf(s[0] * a.inv_d + a.eps), level = s[1] * a.inv_d, along = s[2] * a.inv_d * r;
+        for (int c = threadIdx.x * kV; c < a.D; c += 256 * kV) {
+            float v[kV], d[kV], o[kV];
+            Pack<T, kV>::load(x + c, v);
+            Pack<T, kV>::load(dn + c, d);
+            if (skip) Pack<T, kV>::load(skip + c, o);
+#pragma unroll
+            for (int k = 0; k < kV; ++k) {
+                const float xh = (v[k] - mean) * r;
+                col[c + k] += d[k] * xh;
+                col_b[c + k] += d[k];
+                o[k] = (skip ? o[k] : 0.f) + r * (d[k] * a.w[c + k] - level - xh * along);
+            }
+            Pack<T, kV>::store(dx + c, o);
+        }
+    }
+}
+
+// Rows through a ring of images (row_ring.cuh); a thread owns kP pieces of 16 bytes and at most one single element.
+template <typename T, int kP, bool kWarp>
+__global__ void __launch_bounds__(kWarp ? kRowWarps * 32 : ring_threads(false, kP * kVec<T>), kWarp ? warp_ctas(false, kP * kVec<T>) : 1)
+    k_layer_norm(const __grid_constant__ LnArgs a) {
+    constexpr int kN = kPairs<T>;
+    extern __shared__ __align__(16) uint8_t smem[];
+    const int warps = blockDim.x / 32;
+    const size_t t0 = kWarp ? (size_t)blockIdx.x * kRowWarps + threadIdx.x / 32 : blockIdx.x, G = kWarp ? (size_t)gridDim.x * kRowWarps : gridDim.x;
+    Ring<T, 1, kP, kWarp> r;
+    r.in[0] = static_cast<const T*>(a.x); r.ld[0] = a.ld_x;
+    r.begin(smem, a.T, a.D, a.stages, a.row_bytes, r.in[0] + t0 * a.ld_x);
+    pdl_wait();
+    pdl_trigger();
+    if (kWarp || threadIdx.x == 0)
+        for (int i = 0; i < r.stages; ++i) r.load(i, t0 + i * G);
+    float nx[1] = {};
+    r.load_extra(t0, nx);
+    float2 w[kP][kN], b[kP][kN];
+    const float xw = r.weights(a.w, nullptr, w);
+    float xb = 0.f;
+    if (a.b) xb = r.weights(a.b, nullptr, b);
+    else
+#pragma unroll
+        for (int j = 0; j < kP; ++j)
+#pragma unroll
+            for (int i = 0; i < kN; ++i) b[j][i] = both(0.f);
+
+    int k = 0;
+    for (size_t t = t0; t < a.T; t += G, ++k, r.next()) {
+        const float ex = nx[0];
+        r.load_extra(t + G, nx);
+        r.wait();
+        float2 v[kP][kN], s2 = both(0.f);
+#pragma unroll
+        for (int j = 0; j < kP; ++j)
+            if (r.has(j)) {
+                r.piece(0, j, v[j]);
+#pragma unroll
+                for (int i = 0; i < kN; ++i) s2 = add2(s2, v[j][i]);
+            }
+        if (kWarp) r.release(t, G, warps);
+        float s[1] = {sum2(s2) + (r.extra >= 0 ? ex : 0.f)};
+        row_sum<kWarp>(s, r.ctl->red[k & 1], warps);
+        if (!kWarp) {
+            // every warp has read this row's image: it is filled again at once
+            if (threadIdx.x == 0) r.load(r.st, t + (size_t)r.stages * G);
+        }
+        const float mean = s[0] * a.inv_d;
+        s2 = both(0.f);
+#pragma unroll
+        for (int j = 0; j < kP; ++j)
+            if (r.has(j))
+#pragma unroll
+                for (int i = 0; i < kN; ++i) {
+                    v[j][i] = add2(v[j][i], both(-mean));
+                    s2 = fma2(v[j][i], v[j][i], s2);
+                }
+        s[0] = sum2(s2) + (r.extra >= 0 ? (ex - mean) * (ex - mean) : 0.f);
+        row_sum<kWarp>(s, r.ctl->red[2], warps);
+        const float q = rsqrtf(s[0] * a.inv_d + a.eps);
+        T* n = static_cast<T*>(a.out) + t * a.ld_out;
+#pragma unroll
+        for (int j = 0; j < kP; ++j)
+            if (r.has(j)) {
+#pragma unroll
+                for (int i = 0; i < kN; ++i) v[j][i] = fma2(mul2(v[j][i], both(q)), w[j][i], b[j][i]);
+                r.store(n, j, v[j]);
+            }
+        if (r.extra >= 0 && r.ok) n[r.extra] = from_f<T>((ex - mean) * q * xw + xb);
+    }
+    if (!r.ok) report_timeout();
+}
+
+template <typename T, int kP, bool kWarp>
+__global__ void __launch_bounds__(kWarp ? kRowWarps * 32 : ring_threads(true, kP * kVec<T>), kWarp ? warp_ctas(true, kP * kVec<T>) : 1)
+    k_layer_norm_back(const __grid_constant__ LnArgs a) {
+    constexpr int kN = kPairs<T>, kIn = 3;
+    extern __shared__ __align__(16) uint8_t smem[];
+    const int warps = blockDim.x / 32;
+    const size_t t0 = kWarp ? (size_t)blockIdx.x * kRowWarps + threadIdx.x / 32 : blockIdx.x, G = kWarp ? (size_t)gridDim.x * kRowWarps : gridDim.x;
+    Ring<T, kIn, kP, kWarp> r;
+    r.in[0] = static_cast<const T*>(a.x); r.ld[0] = a.ld_x;
+    r.in[1] = static_cast<const T*>(a.dn); r.ld[1] = a.ld_dn;
+    r.in[2] = static_cast<const T*>(a.skip); r.ld[2] = a.ld_skip;
+    const bool has_skip = a.skip != nullptr;
+    r.begin(smem, a.T, a.D, a.stages, a.row_bytes, r.in[0] + t0 * a.ld_x);
+    pdl_wait();
+    pdl_trigger();
+    if (kWarp || threadIdx.x == 0)
+        for (int i = 0; i < r.stages; ++i) r.load(i, t0 + i * G);
+    float nx[kIn] = {};
+    r.load_extra(t0, nx);
+    float2 w[kP][kN], c_w[kP][kN], c_b[kP][kN];
+    const float xw = r.weights(a.w, nullptr, w);
+    float x_w = 0.f, x_b = 0.f;
+#pragma unroll
+    for (int j = 0; j < kP; ++j)
+#pragma unroll
+        for (int i = 0; i < kN; ++i) c_w[j][i] = c_b[j][i] = both(0.f);
+
+    int k = 0;
+    for (size_t t = t0; t < a.T; t += G, ++k, r.next()) {
+        float ex[kIn];
+#pragma unroll
+        for (int i = 0; i < kIn; ++i) ex[i] = nx[i];
+        r.load_extra(t + G, nx);
+        r.wait();
+        float2 c[kP][kN], s2 = both(0.f);
+#pragma unroll
+        for (int j = 0; j < kP; ++j)
+            if (r.has(j)) {
+                r.piece(0, j, c[j]);
+#pragma unroll
+                for (int i = 0; i < kN; ++i) s2 = add2(s2, c[j][i]);
+            }
+        float m[1] = {sum2(s2) + (r.extra >= 0 ? ex[0] : 0.f)};
+        row_sum<kWarp>(m, r.ctl->red[k & 1], warps);
+        const float mean = m[0] * a.inv_d;
+        float2 q2[3] = {both(0.f), both(0.f), both(0.f)};        // sum c^2, a, a c
+#pragma unroll
+        for (int j = 0; j < kP; ++j)
+            if (r.has(j)) {
+                float2 d[kN];
+                r.piece(1, j, d);
+#pragma unroll
+                for (int i = 0; i < kN; ++i) {
+                    c[j][i] = add2(c[j][i], both(-mean));
+                    c_b[j][i] = add2(c_b[j][i], d[i]);
+                    d[i] = mul2(d[i], w[j][i]);
+                    q2[0] = fma2(c[j][i], c[j][i], q2[0]);
+                    q2[1] = add2(q2[1], d[i]);
+                    q2[2] = fma2(d[i], c[j][i], q2[2]);
+                }
+            }
+        float s[3] = {sum2(q2[0]), sum2(q2[1]), sum2(q2[2])};
+        const float xc = ex[0] - mean, xa = ex[1] * xw;
+        if (r.extra >= 0) {
+            s[0] += xc * xc;
+            s[1] += xa;
+            s[2] += xa * xc;
+        }
+        row_sum<kWarp>(s, r.ctl->red[2], warps);
+        const float q = rsqrtf(s[0] * a.inv_d + a.eps);
+        const float level = -q * s[1] * a.inv_d, along = -q * q * q * s[2] * a.inv_d;     // dx = q a + c along + level
+        T* dx = static_cast<T*>(a.out) + t * a.ld_out;
+#pragma unroll
+        for (int j = 0; j < kP; ++j)
+            if (r.has(j)) {
+                float2 d[kN], o[kN];
+                r.piece(1, j, d);
+                if (has_skip) r.piece(2, j, o);
+#pragma unroll
+                for (int i = 0; i < kN; ++i) {
+                    c_w[j][i] = fma2(mul2(d[i], both(q)), c[j][i], c_w[j][i]);
+                    d[i] = fma2(mul2(d[i], w[j][i]), both(q), fma2(c[j][i], both(along), both(level)));
+                    if (has_skip) d[i] = add2(d[i], o[i]);
+                }
+                r.store(dx, j, d);
+            }
+        r.release(t, G, warps);
+        if (r.extra >= 0) {
+            x_w += ex[1] * q * xc;
+            x_b += ex[1];
+            if (r.ok) dx[r.extra] = from_f<T>(xa * q + (xc * along + level) + ex[2]);
+        }
+    }
+    float* const part = a.part + blockIdx.x * 2 * part_width(a.D);
+    float* const col = kWarp ? reinterpret_cast<float*>(r.base) : part;      // a warp's sums go over its row images, 8 bytes a column
+    if (kWarp) {
+        asm volatile("cp.async.wait_all;" ::: "memory");
+        __syncwarp();
+    }
+#pragma unroll
+    for (int j = 0; j < kP; ++j)
+        if (r.has(j))
+#pragma unroll
+            for (int i = 0; i < kN; ++i) {
+                float* p = col + r.column(j) + 2 * i;
+                p[0] = c_w[j][i].x;
+                p[1] = c_w[j][i].y;
+                p[part_width(a.D)] = c_b[j][i].x;
+                p[part_width(a.D) + 1] = c_b[j][i].y;
+            }
+    if (r.extra >= 0) {
+        col[r.extra] = x_w;
+        col[part_width(a.D) + r.extra] = x_b;
+    }
+    if (kWarp) {
+        __syncthreads();
+        const size_t next = (size_t)r.stages * kIn * r.row_bytes / 4;
+        const float* first = reinterpret_cast<const float*>(smem + kRingCtl);
+        for (int c = threadIdx.x; c < 2 * (int)part_width(a.D); c += kRowWarps * 32) {
+            float v = 0.f;
+#pragma unroll
+            for (int i = 0; i < kRowWarps; ++i) v += first[i * next + c];
+            part[c] = v;
+        }
+    }
+    if (!r.ok) report_timeout();
+}
+
+// How a call is launched.  ring: all matrices aligned alike and the row within the pieces that a CTA's threads own.
+struct Plan {
+    bool ring, warp;                 // warp: a warp per row
+    int threads, elems;              // of a CTA; elements that a thread owns
+    int grid, stages;
+    uint32_t row_bytes;
+    size_t smem;
+};
+bool ring_shape(size_t D, bool back, int* threads, int* elems) {
+    *elems = ring_elems(D);
+    const size_t need = (D + *elems - 1) / *elems;
+    *threads = (int)(need <= 32 ? 32 : (need + 31) / 32 * 32);
+    return *threads <= ring_threads(back, *elems);
+}
+int ring_ctas(bool back, int threads, int elems) {
+    const int n = ring_threads(back, elems) / threads;
+    return n < kRingCtasMax ? n : kRingCtasMax;
+}
+template <int N>
+Plan plan_of(const Mat (&m)[N], size_t es, uint64_t T, uint64_t D, bool back) {
+    Plan p{};
+    size_t period = 1;
+    p.ring = ring_shape(D, back, &p.threads, &p.elems) && aligned_alike(m, es, &period);
+    p.row_bytes = (uint32_t)((D * es + 15) / 16 * 16);
+    p.warp = D <= warp_row(es);
+    if (p.warp) p.threads = kRowWarps * 32;
+    const size_t images = back ? 3 : 1, row = images * p.row_bytes * (p.warp ? kRowWarps : 1);
+    size_t ctas = 1;
+    if (p.ring) {      // as many CTAs as the registers allow, fewer where two rows would not fit; then as many rows as fit
+        ctas = (size_t)(p.warp ? warp_ctas(back, p.elems) : ring_ctas(back, p.threads, p.elems));
+        while (ctas > 1 && kRingCtl + 2 * row > kRingSmem / ctas) --ctas;
+        const size_t room = ctas > 1 ? kRingSmem / ctas : kSmemMax, most = p.warp ? 4 : kRingMax;
+        const size_t fit = (room - kRingCtl) / row;
+        p.ring = fit >= (p.warp ? 2 : 1);
+        p.stages = (int)(fit < most ? fit : most);
+        p.smem = kRingCtl + p.stages * row;
+    }
+    if (!p.ring) {
+        const uint64_t cap = back ? kBackCtas : kSms * 8;
+        p.grid = (int)(T < cap ? T : cap);
+        return p;
+    }
+    if (p.warp) {
+        const uint64_t want = (T + kRowWarps - 1) / kRowWarps, all = (uint64_t)kSms * ctas;
+        p.grid = (int)(want < all ? want : all);
+        return p;
+    }
+    if (back)          // at least two rows per CTA, whose column sums cost as much as a row
+        while (ctas > 1 && kSms * ctas * 2 > T) --ctas;
+    const size_t all = (size_t)kSms * ctas / period * period;       // a multiple of the period: rows of a CTA are cut alike
+    const size_t want = (T + period - 1) / period * period;
+    p.grid = (int)(want < all ? want : all);
+    return p;
+}
+
+template <typename T, int kE, bool kWarp>
+cudaError_t run_ring(LnArgs a, bool back, const Plan& p, cudaStream_t s) {
+    constexpr int kP = kE / kVec<T>;
+    a.stages = p.stages;
+    a.row_bytes = p.row_bytes;
+    const cudaError_t e = back ? allow_smem<k_layer_norm_back<T, kP, kWarp>>() : allow_smem<k_layer_norm<T, kP, kWarp>>();
+    if (e != cudaSuccess) return e;
+    return launch_kernel(back ? k_layer_norm_back<T, kP, kWarp> : k_layer_norm<T, kP, kWarp>, p.grid, p.threads, p.smem, s, true, a);
+}
+template <typename T, int kV>
+cudaError_t run_plain(const LnArgs& a, bool back, int grid, cudaStream_t s) {
+    return launch_kernel(back ? k_layer_norm_back_plain<T, kV> : k_layer_norm_plain<T, kV>, grid, 256, 0, s, true, a);
+}
+template <typename T>
+cudaError_t run(const LnArgs& a, bool back, bool wide, const Plan& p, cudaStream_t s) {
+    if (!p.ring) return wide ? run_plain<T, kVec<T>>(a, back, p.grid, s) : run_plain<T, 1>(a, back, p.grid, s);
+    if (p.warp && p.elems == 8) return run_ring<T, 8, true>(a, back, p, s);
+    if constexpr (warp_row(sizeof(T)) > 256)
+        if (p.warp) return run_ring<T, 16, true>(a, back, p, s);
+    return p.elems == 16 ? run_ring<T, 16, false>(a, back, p, s) : run_ring<T, 32, false>(a, back, p, s);
+}
+
+const char* check_common(uint32_t dtype, uint64_t width, const float* w, const float* b, float eps) {
+    if (!known_dtype(dtype)) return "dtype must be ABS_F32 or ABS_BF16";
+    if (width == 0) return "width must be at least 1";
+    if (!w) return "w must not be NULL";
+    if (misaligned(w, 4) || misaligned(b, 4)) return "a weight is not 4-byte aligned";
+    if (!(eps > 0.f) || !isfinite(eps)) return "eps must be positive";
+    return nullptr;
+}
+
+}  // namespace
+
+cudaError_t take_status_layer_norm(int* status, cudaStream_t s) { return take_status(status, s); }
+
+}  // namespace abs_sgd
+
+using namespace abs_sgd;
+
+extern "C" int abs_layer_norm(const void* x, uint64_t ld_x, const float* w, const float* b, float eps, uint32_t dtype, uint64_t tokens, uint64_t width, void* n,
+                              uint64_t ld_n, void* stream) {
+    if (const char* why = check_common(dtype, width, w, b, eps)) return thread_error(ABS_EINVAL, why);
+    if (width > kWidthMax) return thread_error(ABS_ELIMIT, "width exceeds 32768");
+    const size_t es = size_of(dtype);
+    const MatrixArg q[2] = {{x, ld_x, width, es}, {n, ld_n, width, es}};
+    if (const char* why = check_matrices(q)) return thread_error(ABS_EINVAL, why);
+    if (const char* why = check_in_place(q[1], q[0], true)) return thread_error(ABS_EINVAL, why);
+    if (tokens == 0) return ABS_OK;
+    if (!x || !n) return thread_error(ABS_EINVAL, "x and n must not be NULL");
+    const Mat m[2] = {{x, ld_x}, {n, ld_n}};
+    LnArgs a{};
+    a.x = x; a.ld_x = ld_x; a.w = w; a.b = b; a.eps = eps; a.inv_d = 1.f / (float)width; a.T = tokens; a.D = (int)width; a.out = n; a.ld_out = ld_n;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    const Plan p = plan_of(m, es, tokens, width, false);
+    const bool wide = rows_aligned(m, es, width);
+    const cudaError_t e = dtype == ABS_F32 ? run<float>(a, false, wide, p, s) : run<bf16>(a, false, wide, p, s);
+    return e == cudaSuccess ? ABS_OK : thread_error(ABS_ECUDA, cudaGetErrorString(e));
+}
+
+extern "C" size_t abs_layer_norm_workspace(uint64_t tokens, uint64_t width) {
+    uint64_t most = kBackCtas;
+    int threads = 0, elems = 0;
+    if (ring_shape(width, true, &threads, &elems)) {
+        const uint64_t ring = (uint64_t)kSms * ring_ctas(true, threads, elems);
+        if (ring > most) most = ring;
+    }
+    const uint64_t rows = (tokens + 7) / 8 * 8;
+    return ((size_t)(rows < most ? rows : most) * 2 * part_width(width) * 4 + 255) / 256 * 256 + 256;
+}
+
+extern "C" int abs_layer_norm_backward(const void* dn, uint64_t ld_dn, const void* x, uint64_t ld_x, const void* dskip, uint64_t ld_dskip, const float* w, float eps,
+                                       uint32_t dtype, uint64_t tokens, uint64_t width, void* dx, uint64_t ld_dx, float* dw, float* db, int accumulate,
+                                       void* workspace, size_t workspace_bytes, void* stream) {
+    if (const char* why = check_common(dtype, width, w, nullptr, eps)) return thread_error(ABS_EINVAL, why);
+    if (width > kWidthMax) return thread_error(ABS_ELIMIT, "width exceeds 32768");
+    const size_t es = size_of(dtype);
+    const MatrixArg q[4] = {{dn, ld_dn, width, es}, {x, ld_x, width, es}, {dskip, ld_dskip, width, es}, {dx, ld_dx, width, es}};
+    if (const char* why = check_matrices(q)) return thread_error(ABS_EINVAL, why);
+    for (int i = 0; i < 3; ++i)
+        if (const char* why = check_in_place(q[3], q[i], true)) return thread_error(ABS_EINVAL, why);
+    if (!dw || misaligned(dw, 4) || misaligned(db, 4)) return thread_error(ABS_EINVAL, "dw must not be NULL, dw and db 4-byte aligned");
+    if (dw == db) return thread_error(ABS_EINVAL, "two outputs are the same");
+    if (tokens && (!dn || !x || !dx)) return thread_error(ABS_EINVAL, "dn, x and dx must not be NULL");
+    if (!workspace || misaligned(workspace, 256)) return thread_error(ABS_EINVAL, "workspace must be non-NULL and 256-byte aligned");
+    if (workspace_bytes < abs_layer_norm_workspace(tokens, width)) return thread_error(ABS_ENOMEM, "workspace too small");
+    LnArgs a{};
+    a.x = x; a.ld_x = ld_x; a.dn = dn; a.ld_dn = ld_dn; a.skip = dskip; a.ld_skip = ld_dskip; a.w = w; a.eps = eps; a.inv_d = 1.f / (float)width;
+    a.T = tokens; a.D = (int)width; a.out = dx; a.ld_out = ld_dx; a.part = static_cast<float*>(workspace);
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    cudaError_t e = cudaSuccess;
+    Plan p{};
+    if (tokens > 0) {
+        const Mat m[4] = {{dn, ld_dn}, {x, ld_x}, {dskip, ld_dskip}, {dx, ld_dx}};
+        p = plan_of(m, es, tokens, width, true);
+        const bool wide = rows_aligned(m, es, width);
+        e = dtype == ABS_F32 ? run<float>(a, true, wide, p, s) : run<bf16>(a, true, wide, p, s);
+    }
+    if (e == cudaSuccess) e = launch_column_sums(a.part, p.grid, (int)width, dw, db, accumulate, s);
+    return e == cudaSuccess ? ABS_OK : thread_error(ABS_ECUDA, cudaGetErrorString(e));
+}

@@ -1,0 +1,712 @@
+// Linear layer with bias, activation and residual, and its gradients (abs_linear*).
+//
+//     forward   y = act(x w + bias) + residual          A = x  [T, in]  K-major      B = w  [in, out]  N-major
+//     dgrad     dx = (dy w^T) act'(z) + residual        A = dy [T, out] K-major      B = w^T           K-major
+//     wgrad     dw (+)= x^T dy                          A = x^T         M-major      B = dy [T, out]   N-major
+// One kernel, k_linear, for the three: C[M, N] = A[M, K] B[K, N] with the operands read as they lie (an operand whose contraction
+// index runs along its rows is "K-major", the others "MN-major"; TMA boxes of 64 columns, 128-byte swizzled rows, either way), and
+// the layer's elementwise work on the sums while they are still in registers.
+#include <math.h>
+
+#include <algorithm>
+
+#include "abs_internal.h"
+#include "abs_llm.h"
+#include "llm_host.h"
+#include "llm_status.cuh"
+#include "row_ops.cuh"
+#include "tcgen05.cuh"
+
+namespace abs_sgd {
+namespace {
+
+enum { kForward, kDgrad, kWgrad };
+
+struct LinArgs {
+    int M, N, K;
+    int tiles_n, whole, rest, splits, kb_per_split;   // tiles: whole ones, then `rest` cut into `splits` runs; kb: 64 of K
+    float* part;                     // [splits][rest][kTM][kTN]
+    void* out;
+    size_t ld;
+    const float* bias;
+    const void* res;                 // type of the output
+    size_t ld_res;
+    const bf16* z_in;                // dgrad
+    bf16* z_out;                     // forward
+    size_t ld_z;
+    uint32_t act;
+    int accumulate;
+    int wide;                        // rows of out, res and z are 16-byte aligned
+};
+
+// ---- activations
+__device__ __forceinline__ float activate(uint32_t act, float z) {
+    if (act == ABS_ACT_RELU) return z > 0.f ? z : z == z ? 0.f : z;
+    if (act == ABS_ACT_GELU) return z * normcdff(z);
+    if (act == ABS_ACT_SILU) return z / (1.f + __expf(-z));
+    return z;
+}
+__device__ __forceinline__ float slope(uint32_t act, float z) {
+    if (act == ABS_ACT_RELU) return z > 0.f ? 1.f : z == z ? 0.f : z;
+    if (act == ABS_ACT_GELU) return fmaf(z, 0.3989422804014327f * __expf(-0.5f * z * z), normcdff(z));
+    if (act == ABS_ACT_SILU) {
+        const float s = 1.f / (1.f + __expf(-z));
+        return s * fmaf(z, 1.f / (1.f + __expf(z)), 1.f);
+    }
+    return 1.f;
+}
+
+template <typename T>
+__device__ __forceinline__ void load8(const T* p, int n, bool wide, float (&v)[8]) {
+    if (wide && n == 8) {
+#pragma unroll
+        for (int h = 0; h < 8 / kVec<T>; ++h) {
+            float w[kVec<T>];
+            Pack<T, kVec<T>>::load(p + h * kVec<T>, w);
+#pragma unroll
+            for (int i = 0; i < kVec<T>; ++i) v[h * kVec<T> + i] = w[i];
+        }
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = i < n ? to_f(p[i]) : 0.f;
+}
+template <typename T>
+__device__ __forceinline__ void store8(T* p, int n, bool wide, const float (&v)[8]) {
+    if (wide && n == 8) {
+#pragma unroll
+        for (int h = 0; h < 8 / kVec<T>; ++h) {
+            float w[kVec<T>];
+#pragma unroll
+            for (int i = 0; i < kVec<T>; ++i) w[i] = v[h * kVec<T> + i];
+            Pack<T, kVec<T>>::store(p + h * kVec<T>, w);
+        }
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (i < n) p[i] = from_f<T>(v[i]);
+}
+
+// The layer's work on n (1 .. 8) sums of row `row` from column `col`.
+template <int kEpi, typename T>
+__device__ __forceinline__ void finish(const LinArgs& a, int row, int col, int n, float (&v)[8]) {
+    T* out = static_cast<T*>(a.out) + (size_t)row * a.ld + col;
+    const bool wide = a.wide != 0;
+    float w[8];
+    if constexpr (kEpi == kWgrad) {
+        if (a.accumulate) {
+            load8(out, n, wide, w);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] += w[i];
+        }
+    } else {
+        if constexpr (kEpi == kForward) {
+            if (a.bias)
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (i < n) v[i] += __ldg(a.bias + col + i);
+            if (a.z_out) store8(a.z_out + (size_t)row * a.ld_z + col, n, wide, v);
+            if (a.act != ABS_ACT_NONE)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] = activate(a.act, v[i]);
+        } else if (a.act != ABS_ACT_NONE) {
+            load8(a.z_in + (size_t)row * a.ld_z + col, n, wide, w);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] *= slope(a.act, w[i]);
+        }
+        if (a.res) {
+            load8(static_cast<const T*>(a.res) + (size_t)row * a.ld_res + col, n, wide, w);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] += w[i];
+        }
+    }
+    store8(out, n, wide, v);
+}
+
+// ------------------------------------------------------------------------------------------------
+// Two CTAs (two SMs) share an output tile of 256 x 256: each holds the operand's 128 rows of A and 128 columns of B, 32 KB for a run of
+// 64 along K.  Roles in each CTA:
+//   warp 0      TMA producer, up to kStages runs ahead
+//   warp 1      (first CTA only) MMA issuer: four tcgen05.mma.cta_group::2 (M 256, N 256, K 16) per run into one of two TMEM accumulators
+//   warps 2-9   epilogue: they keep the tile's sums in registers and add a finished accumulator to them every kSegmentRuns runs (the
+//               tensor core drops low bits at each of its additions, so that its error grows with their number); then the layer's
+//               elementwise work, in rows of eight columns a thread, through a staging tile in shared memory.
+// Items are dealt out round-robin to the pairs: the whole tiles, as many as fill all pairs equally often, then the rest, each cut along K
+// into `splits` parts so that they too keep all pairs busy; k_linear_join adds those up in order and does the elementwise work.
+// Launched in plain stream order, and starts no successor early (see llm_ckpt8.cu).  Every wait on a barrier is bounded.
+// ------------------------------------------------------------------------------------------------
+constexpr int kTM = 256, kTN = 256, kTK = 64;    // of a pair
+constexpr int kStages = 5, kEpiWarps = 8, kThreads = 64 + kEpiWarps * 32;
+constexpr int kHalf = kTK * 128 * 2;             // bytes of an operand's share of a CTA and run
+constexpr int kPitch = 36;                       // floats of a staged row: 16-byte pieces, eight rows on different banks
+constexpr int kSegmentRuns = 12;
+constexpr int kSms = 148;
+constexpr uint64_t kSizeMax = 0x7fffffc0ull;
+constexpr int kMinRuns = 12;     // runs of 64 that a part of a cut tile has at least
+
+struct LinSmem {
+    alignas(1024) uint8_t a[kStages][kHalf];
+    alignas(1024) uint8_t b[kStages][kHalf];
+    alignas(16) float out[kEpiWarps][32 * kPitch];
+    alignas(8) uint64_t full[kStages];       // first CTA: both CTAs' copies of a run have landed
+    uint64_t empty[kStages];                 // the run's MMAs have read both CTAs' operands
+    uint64_t acc_full[2];
+    uint64_t acc_empty[2];                   // first CTA: both CTAs have read the accumulator
+    uint32_t tmem_base;
+    uint32_t failed;
+};
+
+__device__ __forceinline__ uint32_t cluster_rank() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// tma_load_2d whose bytes are counted on the same barrier of the cluster's first CTA.
+__device__ __forceinline__ void tma_load_2d_first(void* dst, const CUtensorMap* tm, int x, int y, uint64_t* bar) {
+    uint32_t b;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(b) : "r"(smem_u32(bar)));
+    asm volatile(
+        "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, %3}], [%4];"
+        ::"r"(smem_u32(dst)), "l"(reinterpret_cast<uint64_t>(tm)), "r"(x), "r"(y), "r"(b) : "memory");
+}
+// One arrival on the same barrier of the cluster's first CTA; what it announces is ordered by tcgen05.fence.
+__device__ __forceinline__ void arrive_first(uint64_t* bar) {
+    uint32_t a;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(a) : "r"(smem_u32(bar)));
+    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(a) : "memory");
+}
+__device__ __forceinline__ void umma2_bf16(uint32_t tmem_d, uint64_t da, uint64_t db, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
+        " tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}\n"
+        ::"r"(tmem_d), "l"(da), "l"(db), "r"(idesc), "r"(accumulate) : "memory");
+}
+// Arrives on this barrier of both CTAs when the MMAs issued so far are done.
+__device__ __forceinline__ void umma2_commit(uint64_t* bar) {
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
+                 ::"r"(smem_u32(bar)), "h"((uint16_t)3) : "memory");
+}
+
+// This CTA's share of an operand, 128 rows (or columns) from `mn` and 64 of K from `k`.
+template <bool kMn>
+__device__ __forceinline__ void load_operand(uint8_t* dst, const CUtensorMap* tm, int mn, int k, uint64_t* bar) {
+    if constexpr (kMn) {
+        tma_load_2d_first(dst, tm, mn, k, bar);
+        tma_load_2d_first(dst + kHalf / 2, tm, mn + 64, k, bar);
+    } else {
+        tma_load_2d_first(dst, tm, k, mn, bar);
+    }
+}
+// Its descriptor for the k16-th step of 16.
+template <bool kMn>
+__device__ __forceinline__ uint64_t operand_desc(uint32_t at, int k16) {
+    return kMn ? umma_desc_mn_sw128(at + k16 * 2048, kHalf / 2) : umma_desc_k_sw128(at + k16 * 32);
+}
+
+template <int kEpi, typename T>
+__global__ void __launch_bounds__(kThreads, 1) k_linear(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_b,
+                                                        const __grid_constant__ LinArgs a) {
+    constexpr bool kAMn = kEpi == kWgrad, kBMn = kEpi != kDgrad;
+    extern __shared__ uint8_t smem_raw[];
+    LinSmem& s = *reinterpret_cast<LinSmem*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const int rank = (int)cluster_rank();
+    const int pair = blockIdx.x / 2, pairs = gridDim.x / 2;
+    const int items = a.whole + a.rest * a.splits;
+    const int kb_total = (a.K + kTK - 1) / kTK;
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&s.tmem_base)), "r"(512) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < kStages; ++i) {
+            mbar_init(&s.full[i], 1);
+            mbar_init(&s.empty[i], 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&s.acc_full[i], 1);
+            mbar_init(&s.acc_empty[i], 2 * kEpiWarps);       // the epilogue warps of each CTA
+        }
+        s.failed = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    cluster_sync();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    const uint32_t tmem = s.tmem_base;
+    volatile uint32_t* failed = &s.failed;
+
+    struct Item {
+        int m0, n0, kb0, kb1;        // first row and column of the pair's tile, runs of 64 of K
+        int part;                    // index of the partial sum, -1: straight to the output
+    };
+    auto item_of = [&](int it) {
+        Item q;
+        int tile = it;
+        q.part = -1;
+        q.kb0 = 0;
+        q.kb1 = kb_total;
+        if (it >= a.whole) {
+            const int r = it - a.whole;
+            tile = a.whole + r % a.rest;
+            if (a.splits > 1) {
+                q.part = r;
+                q.kb0 = min(kb_total, r / a.rest * a.kb_per_split);
+                q.kb1 = min(kb_total, q.kb0 + a.kb_per_split);
+            }
+        }
+        q.m0 = tile / a.tiles_n * kTM;
+        q.n0 = tile % a.tiles_n * kTN;
+        return q;
+    };
+
+    if (warp == 0) {
+        if (lane == 0) {                             // ---- TMA producer
+            uint32_t st = 0, round = 0;
+            for (int it = pair; it < items && !*failed; it += pairs) {
+                const Item q = item_of(it);
+                for (int kb = q.kb0; kb < q.kb1; ++kb) {
+                    if (round > 0 && !mbar_wait(&s.empty[st], (round - 1) & 1)) { *failed = 1; break; }
+                    if (rank == 0) mbar_expect_tx(&s.full[st], 4 * kHalf);
+                    load_operand<kAMn>(s.a[st], &tm_a, q.m0 + rank * 128, kb * kTK, &s.full[st]);
+                    load_operand<kBMn>(s.b[st], &tm_b, q.n0 + rank * 128, kb * kTK, &s.full[st]);
+                    if (++st == kStages) { st = 0; ++round; }
+                }
+            }
+            if (*failed && rank == 0)                // copies in flight land before the CTAs' shared memory is released
+                for (uint32_t i = 0; i < kStages; ++i) mbar_wait(&s.full[i], (round + (i < st ? 0u : 1u)) & 1u, 4096u);
+        }
+    } else if (warp == 1) {
+        if (lane == 0 && rank == 0) {                // ---- MMA issuer
+            constexpr uint32_t idesc = umma_idesc_bf16(kTM, kTN) | (kAMn ? 1u << 15 : 0u) | (kBMn ? 1u << 16 : 0u);
+            uint32_t st = 0, phase = 0;
+            int i = 0;                               // segments so far: every other one in the same accumulator
+            bool ok = true;
+            for (int it = pair; it < items && ok; it += pairs) {
+                const Item q = item_of(it);
+                for (int kb0 = q.kb0; kb0 < q.kb1 && ok; kb0 += kSegmentRuns, ++i) {
+                    const int ab = i & 1, kb1 = min(q.kb1, kb0 + kSegmentRuns);
+                    if (i >= 2 && !mbar_wait(&s.acc_empty[ab], ((i / 2) - 1) & 1)) { ok = false; break; }
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                    for (int kb = kb0; kb < kb1; ++kb) {
+                        if (!mbar_wait(&s.full[st], phase)) { ok = false; break; }
+                        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                        const uint32_t a0 = smem_u32(s.a[st]), b0 = smem_u32(s.b[st]);
+#pragma unroll
+                        for (int k = 0; k < kTK / 16; ++k)
+                            umma2_bf16(tmem + ab * kTN, operand_desc<kAMn>(a0, k), operand_desc<kBMn>(b0, k), idesc, kb > kb0 || k > 0);
+                        umma2_commit(&s.empty[st]);
+                        if (++st == kStages) { st = 0; phase ^= 1u; }
+                    }
+                    if (ok) umma2_commit(&s.acc_full[ab]);
+                }
+            }
+            if (!ok) *failed = 1;
+        }
+        __syncwarp();
+    } else {                                         // ---- epilogue: warps 2-5 the first 128 columns, 6-9 the others
+        const int qd = warp % 4, half = (warp - 2) / 4;
+        float* stage = s.out[warp - 2];
+        const int row = rank * 128 + qd * 32;        // of the tile
+        int i = 0;
+        bool ok = true;
+        for (int it = pair; it < items && ok; it += pairs) {
+            const Item q = item_of(it);
+            float2 sum[4][16];
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) sum[c][j] = both(0.f);
+            for (int kb0 = q.kb0; kb0 < q.kb1; kb0 += kSegmentRuns, ++i) {
+                const int ab = i & 1;
+                ok = __all_sync(0xffffffffu, mbar_wait(&s.acc_full[ab], (i / 2) & 1) && !*failed);
+                if (!ok) break;
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+#pragma unroll
+                for (int c = 0; c < 8; ++c) {
+                    uint32_t v[16];
+                    tmem_ld_16(tmem + ((uint32_t)(qd * 32) << 16) + (uint32_t)(ab * kTN + half * 128 + c * 16), v);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        sum[c / 2][c % 2 * 8 + j] = add2(sum[c / 2][c % 2 * 8 + j], make_float2(__uint_as_float(v[2 * j]), __uint_as_float(v[2 * j + 1])));
+                }
+                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) arrive_first(&s.acc_empty[ab]);
+            }
+            if (!ok) {
+                *failed = 1;
+                break;
+            }
+            float* part = q.part >= 0 ? a.part + ((size_t)q.part * kTM + row) * kTN + half * 128 : nullptr;
+            const int rows = min(32, a.M - (q.m0 + row)), col0 = q.n0 + half * 128, cols = min(128, a.N - col0);
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                if (c * 32 >= cols || rows <= 0) continue;
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    *reinterpret_cast<float4*>(stage + lane * kPitch + 4 * j) = make_float4(sum[c][2 * j].x, sum[c][2 * j].y, sum[c][2 * j + 1].x, sum[c][2 * j + 1].y);
+                __syncwarp();
+                const int cc = c * 32 + lane % 4 * 8, n = min(8, cols - cc);
+#pragma unroll
+                for (int p = 0; p < 4; ++p) {
+                    const int r = p * 8 + lane / 4;
+                    if (r >= rows || n <= 0) continue;
+                    const float4 lo = *reinterpret_cast<const float4*>(stage + r * kPitch + lane % 4 * 8);
+                    const float4 hi = *reinterpret_cast<const float4*>(stage + r * kPitch + lane % 4 * 8 + 4);
+                    if (part) {
+                        *reinterpret_cast<float4*>(part + (size_t)r * kTN + cc) = lo;
+                        *reinterpret_cast<float4*>(part + (size_t)r * kTN + cc + 4) = hi;
+                    } else {
+                        float v[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+                        finish<kEpi, T>(a, q.m0 + row + r, col0 + cc, n, v);
+                    }
+                }
+                __syncwarp();
+            }
+        }
+    }
+    __syncwarp();
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    cluster_sync();                                  // no CTA leaves while the other's arrivals or MMAs may still reach it
+    if (threadIdx.x == 0 && *failed) report_timeout();
+    if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+}
+
+// The tiles that were cut: their partial sums added up in order.  A warp per row of a tile, eight columns a thread.
+template <int kEpi, typename T>
+__global__ void __launch_bounds__(256) k_linear_join(const __grid_constant__ LinArgs a) {
+    pdl_wait();
+    pdl_trigger();
+    const size_t step = (size_t)a.rest * kTM * kTN;
+    const int lane = threadIdx.x % 32;
+    for (int i = blockIdx.x * 8 + threadIdx.x / 32; i < a.rest * kTM; i += gridDim.x * 8) {
+        const int tile = a.whole + i / kTM, row = tile / a.tiles_n * kTM + i % kTM, col = tile % a.tiles_n * kTN + lane * 8, n = min(8, a.N - col);
+        if (row >= a.M || n <= 0) continue;
+        float v[8] = {};
+        const float* p = a.part + (size_t)i * kTN + lane * 8;
+#pragma unroll 4
+        for (int k = 0; k < a.splits; ++k) {
+            const float4 lo = *reinterpret_cast<const float4*>(p + k * step), hi = *reinterpret_cast<const float4*>(p + k * step + 4);
+            v[0] += lo.x; v[1] += lo.y; v[2] += lo.z; v[3] += lo.w;
+            v[4] += hi.x; v[5] += hi.y; v[6] += hi.z; v[7] += hi.w;
+        }
+        finish<kEpi, T>(a, row, col, n, v);
+    }
+}
+
+// Rows that TMA cannot start at, copied to rows of `to_ld` elements (16-byte aligned).
+__global__ void __launch_bounds__(256) k_copy_rows(const bf16* x, size_t ld, int width, size_t to_ld, size_t rows, bf16* to) {
+    pdl_wait();
+    pdl_trigger();
+    for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < rows * to_ld; i += (size_t)gridDim.x * 256) {
+        const size_t t = i / to_ld;
+        const int c = (int)(i - t * to_ld);
+        to[i] = c < width ? x[t * ld + c] : __float2bfloat16_rn(0.f);
+    }
+}
+
+// Column sums of dy: 256 columns and every gridDim.y-th group of eight rows for a CTA, then the CTAs' sums in order.
+__global__ void __launch_bounds__(256) k_bias_part(const bf16* dy, size_t ld, int T, int N, int wide, float* part) {
+    __shared__ float sh[8][264];
+    pdl_wait();
+    pdl_trigger();
+    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, col = blockIdx.x * 256 + lane * 8, n = min(8, N - col);
+    float sum[8] = {};
+    if (n > 0)
+#pragma unroll 4
+        for (int64_t t = (int64_t)blockIdx.y * 8 + warp; t < T; t += (int64_t)gridDim.y * 8) {
+            float v[8];
+            load8(dy + (size_t)t * ld + col, n, wide != 0, v);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum[i] += v[i];
+        }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sh[warp][lane * 8 + i] = sum[i];
+    __syncthreads();
+    const int c = blockIdx.x * 256 + threadIdx.x;
+    if (c >= N) return;
+    float v = 0.f;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) v += sh[w][threadIdx.x];
+    part[(size_t)blockIdx.y * N + c] = v;
+}
+__global__ void __launch_bounds__(256) k_bias_join(const float* part, int parts, int N, float* db, int accumulate) {
+    pdl_wait();
+    pdl_trigger();
+    const int c = blockIdx.x * 256 + threadIdx.x;
+    if (c >= N) return;
+    float v = 0.f;
+#pragma unroll 8
+    for (int i = 0; i < parts; ++i) v += part[(size_t)i * N + c];
+    db[c] = accumulate ? db[c] + v : v;
+}
+
+template <typename T>
+__global__ void __launch_bounds__(256) k_activation_backward(const T* dy, size_t ld_dy, const bf16* z, size_t ld_z, uint32_t act, size_t rows, int width, int wide,
+                                                             bf16* dz, size_t ld_dz) {
+    pdl_wait();
+    pdl_trigger();
+    const size_t per_row = ((size_t)width + 7) / 8;
+    for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < rows * per_row; i += (size_t)gridDim.x * 256) {
+        const size_t t = i / per_row;
+        const int c = (int)(i - t * per_row) * 8, n = min(8, width - c);
+        float v[8], w[8];
+        load8(dy + t * ld_dy + c, n, wide != 0, v);
+        load8(z + t * ld_z + c, n, wide != 0, w);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] *= slope(act, w[k]);
+        store8(dz + t * ld_dz + c, n, wide != 0, v);
+    }
+}
+
+// How the work is cut: whole output tiles for all pairs equally often, the rest in runs of K.
+struct LinPlan {
+    int tiles_m, tiles_n, whole, rest, splits, kb_per_split;
+    bool pack_a, pack_b;
+    uint64_t ld_a, ld_b;             // of the packed copies
+    size_t part_bytes, a_bytes, b_bytes, bias_bytes;
+    int bias_parts;
+    size_t bytes() const { return part_bytes + a_bytes + b_bytes + bias_bytes; }
+};
+// An operand as it lies in memory: rows of `cols` elements.
+struct Operand {
+    const void* p;
+    uint64_t ld, rows, cols;
+};
+bool tma_ready(const Operand& o) { return !misaligned(o.p, 16) && o.ld % 8 == 0; }
+bool plan_of(uint64_t M, uint64_t N, uint64_t K, const Operand& a, const Operand& b, LinPlan* out) {
+    LinPlan p{};
+    p.tiles_m = (int)((M + kTM - 1) / kTM);
+    p.tiles_n = (int)((N + kTN - 1) / kTN);
+    const int kb = (int)((K + kTK - 1) / kTK), pairs = kSms / 2;
+    const int64_t tiles = (int64_t)p.tiles_m * p.tiles_n;
+    if (tiles > 0x3fffffff) return false;
+    p.whole = (int)(tiles / pairs * pairs);
+    p.rest = (int)(tiles - p.whole);
+    int splits = p.rest ? std::min(pairs / p.rest, kb / kMinRuns) : 1;
+    if (splits < 1) splits = 1;
+    p.kb_per_split = std::max(1, (kb + splits - 1) / splits);
+    p.splits = std::max(1, (kb + p.kb_per_split - 1) / p.kb_per_split);
+    p.part_bytes = p.splits > 1 ? (size_t)p.splits * p.rest * kTM * kTN * 4 : 0;
+    p.pack_a = !tma_ready(a);
+    p.pack_b = !tma_ready(b);
+    p.ld_a = (a.cols + 7) / 8 * 8;
+    p.ld_b = (b.cols + 7) / 8 * 8;
+    p.a_bytes = p.pack_a ? up256(a.rows * p.ld_a * 2) : 0;
+    p.b_bytes = p.pack_b ? up256(b.rows * p.ld_b * 2) : 0;
+    *out = p;
+    return true;
+}
+int bias_parts(uint64_t T, uint64_t N) {
+    const uint64_t blocks = (N + 255) / 256, want = std::max<uint64_t>(1, 2 * kSms / blocks);
+    return (int)std::max<uint64_t>(1, std::min((T + 63) / 64, want));
+}
+
+cudaError_t copy_rows(const Operand& o, uint64_t to_ld, bf16* to, cudaStream_t s) {
+    const size_t n = (size_t)o.rows * to_ld;
+    return launch_kernel(k_copy_rows, (int)std::min<size_t>((n + 1023) / 1024, kSms * 16), 256, 0, s, true, static_cast<const bf16*>(o.p), (size_t)o.ld, (int)o.cols, (size_t)to_ld,
+                         (size_t)o.rows, to);
+}
+
+template <int kEpi, typename T>
+cudaError_t run(const CUtensorMap& ta, const CUtensorMap& tb, const LinArgs& a, cudaStream_t s) {
+    cudaError_t e = allow_smem<k_linear<kEpi, T>>();
+    if (e != cudaSuccess) return e;
+    const int grid = 2 * std::min(a.whole + a.rest * a.splits, kSms / 2);
+    e = launch_cluster(k_linear<kEpi, T>, grid, 2, kThreads, sizeof(LinSmem) + 1024, s, ta, tb, a);
+    if (e == cudaSuccess && a.splits > 1) e = launch_kernel(k_linear_join<kEpi, T>, std::min(a.rest * kTM / 8, kSms * 8), 256, 0, s, false, a);
+    return e;
+}
+
+// The product and its epilogue; `kind`: kForward, kDgrad, kWgrad; workspace checked against `p`.
+int product(int kind, uint32_t dtype, Operand oa, Operand ob, uint64_t M, uint64_t N, uint64_t K, const LinPlan& p, LinArgs a, char* ws, cudaStream_t s) {
+    cudaError_t e = cudaSuccess;
+    if (p.pack_a) {
+        bf16* to = reinterpret_cast<bf16*>(ws + p.part_bytes);
+        e = copy_rows(oa, p.ld_a, to, s);
+        oa.p = to; oa.ld = p.ld_a;
+    }
+    if (p.pack_b && e == cudaSuccess) {
+        bf16* to = reinterpret_cast<bf16*>(ws + p.part_bytes + p.a_bytes);
+        e = copy_rows(ob, p.ld_b, to, s);
+        ob.p = to; ob.ld = p.ld_b;
+    }
+    if (e != cudaSuccess) return thread_error(ABS_ECUDA, cudaGetErrorString(e));
+    CUtensorMap ta, tb;
+    const uint32_t rows_a = kind == kWgrad ? kTK : 128, rows_b = kind == kDgrad ? 128 : kTK;
+    if (!encode_2d(&ta, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(oa.p), oa.rows, oa.cols, rows_a, 64, oa.ld) ||
+        !encode_2d(&tb, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(ob.p), ob.rows, ob.cols, rows_b, 64, ob.ld))
+        return thread_error(ABS_ECUDA, "cuTensorMapEncodeTiled failed");
+    a.M = (int)M; a.N = (int)N; a.K = (int)K;
+    a.tiles_n = p.tiles_n; a.whole = p.whole; a.rest = p.rest; a.splits = p.splits; a.kb_per_split = p.kb_per_split;
+    a.part = reinterpret_cast<float*>(ws);
+    if (kind == kForward) e = dtype == ABS_F32 ? run<kForward, float>(ta, tb, a, s) : run<kForward, bf16>(ta, tb, a, s);
+    else if (kind == kDgrad) e = dtype == ABS_F32 ? run<kDgrad, float>(ta, tb, a, s) : run<kDgrad, bf16>(ta, tb, a, s);
+    else e = run<kWgrad, float>(ta, tb, a, s);
+    return e == cudaSuccess ? ABS_OK : thread_error(ABS_ECUDA, cudaGetErrorString(e));
+}
+
+const char* check_sizes(uint64_t tokens, uint64_t in, uint64_t out, uint32_t dtype, uint32_t act, int* code) {
+    *code = ABS_EINVAL;
+    if (!known_dtype(dtype)) return "dtype must be ABS_F32 or ABS_BF16";
+    if (act > ABS_ACT_SILU) return "unknown activation";
+    if (in == 0 || out == 0) return "in and out must be at least 1";
+    if (tokens <= kSizeMax && in <= kSizeMax && out <= kSizeMax) return nullptr;
+    *code = ABS_ELIMIT;
+    return "a size exceeds 2^31 - 64";
+}
+// An operand of the product must not be an output.
+const char* check_operands(const void* const (&out)[2], const void* a, const void* b) {
+    for (const void* o : out)
+        if (o && (o == a || o == b)) return "an output must not be an operand of the product";
+    return out[0] && out[0] == out[1] ? "two outputs are the same" : nullptr;
+}
+const char* check_workspace(const LinPlan& p, const void* workspace, size_t bytes, int* code) {
+    *code = ABS_EINVAL;
+    if (p.bytes() == 0) return nullptr;
+    if (!workspace || misaligned(workspace, 256)) return "workspace must be non-NULL and 256-byte aligned";
+    *code = ABS_ENOMEM;
+    return bytes < p.bytes() ? "workspace too small" : nullptr;
+}
+
+}  // namespace
+
+cudaError_t take_status_linear(int* status, cudaStream_t s) { return take_status(status, s); }
+
+}  // namespace abs_sgd
+
+using namespace abs_sgd;
+
+extern "C" size_t abs_linear_workspace(uint64_t tokens, uint64_t in, uint64_t out, const void* x, uint64_t ld_x, const void* w, uint64_t ld_w) {
+    LinPlan p;
+    if (tokens == 0 || tokens > kSizeMax || in > kSizeMax || out > kSizeMax) return 0;
+    return plan_of(tokens, out, in, {x, ld_x, tokens, in}, {w, ld_w, in, out}, &p) ? p.bytes() : 0;
+}
+
+extern "C" int abs_linear(const void* x, uint64_t ld_x, const void* w, uint64_t ld_w, const float* bias, uint32_t act, const void* residual, uint64_t ld_residual,
+                          uint32_t dtype, uint64_t tokens, uint64_t in, uint64_t out, void* y, uint64_t ld_y, void* z, uint64_t ld_z, void* workspace,
+                          size_t workspace_bytes, void* stream) {
+    int code = 0;
+    if (const char* why = check_sizes(tokens, in, out, dtype, act, &code)) return thread_error(code, why);
+    const size_t es = size_of(dtype);
+    const MatrixArg m[5] = {{x, ld_x, in, 2}, {w, ld_w, out, 2}, {residual, ld_residual, out, es}, {y, ld_y, out, es}, {z, ld_z, out, 2}};
+    if (const char* why = check_matrices(m)) return thread_error(ABS_EINVAL, why);
+    if (misaligned(bias, 4)) return thread_error(ABS_EINVAL, "bias must be 4-byte aligned");
+    if (tokens == 0) return ABS_OK;
+    if (!x || !w || !y) return thread_error(ABS_EINVAL, "x, w and y must not be NULL");
+    if (const char* why = check_operands({y, z}, x, w)) return thread_error(ABS_EINVAL, why);
+    if (const char* why = check_in_place(m[3], m[2], true)) return thread_error(ABS_EINVAL, why);
+    if (const char* why = check_in_place(m[4], m[2], false)) return thread_error(ABS_EINVAL, why);
+    LinPlan p;
+    const Operand oa{x, ld_x, tokens, in}, ob{w, ld_w, in, out};
+    if (!plan_of(tokens, out, in, oa, ob, &p)) return thread_error(ABS_ELIMIT, "too many output tiles");
+    if (const char* why = check_workspace(p, workspace, workspace_bytes, &code)) return thread_error(code, why);
+    LinArgs a{};
+    a.out = y; a.ld = ld_y; a.bias = bias; a.res = residual; a.ld_res = ld_residual; a.z_out = static_cast<bf16*>(z); a.ld_z = ld_z; a.act = act;
+    a.wide = rows_at(m[2], 16) && rows_at(m[3], 16) && rows_at(m[4], 16);
+    return product(kForward, dtype, oa, ob, tokens, out, in, p, a, static_cast<char*>(workspace), static_cast<cudaStream_t>(stream));
+}
+
+extern "C" size_t abs_linear_dgrad_workspace(uint64_t tokens, uint64_t in, uint64_t out, const void* dy, uint64_t ld_dy, const void* w, uint64_t ld_w) {
+    LinPlan p;
+    if (tokens == 0 || tokens > kSizeMax || in > kSizeMax || out > kSizeMax) return 0;
+    return plan_of(tokens, in, out, {dy, ld_dy, tokens, out}, {w, ld_w, in, out}, &p) ? p.bytes() : 0;
+}
+
+extern "C" int abs_linear_dgrad(const void* dy, uint64_t ld_dy, const void* w, uint64_t ld_w, uint32_t act, const void* z, uint64_t ld_z, const void* residual,
+                                uint64_t ld_residual, uint32_t dtype, uint64_t tokens, uint64_t in, uint64_t out, void* dx, uint64_t ld_dx, void* workspace,
+                                size_t workspace_bytes, void* stream) {
+    int code = 0;
+    if (const char* why = check_sizes(tokens, in, out, dtype, act, &code)) return thread_error(code, why);
+    const size_t es = size_of(dtype);
+    const MatrixArg m[5] = {{dy, ld_dy, out, 2}, {w, ld_w, out, 2}, {z, ld_z, in, 2}, {residual, ld_residual, in, es}, {dx, ld_dx, in, es}};
+    if (const char* why = check_matrices(m)) return thread_error(ABS_EINVAL, why);
+    if (tokens == 0) return ABS_OK;
+    if ((act != ABS_ACT_NONE) != (z != nullptr)) return thread_error(ABS_EINVAL, "z must be given exactly with an activation");
+    if (!dy || !w || !dx) return thread_error(ABS_EINVAL, "dy, w and dx must not be NULL");
+    if (const char* why = check_operands({dx, nullptr}, dy, w)) return thread_error(ABS_EINVAL, why);
+    for (int i = 2; i < 4; ++i)
+        if (const char* why = check_in_place(m[4], m[i], true)) return thread_error(ABS_EINVAL, why);
+    LinPlan p;
+    const Operand oa{dy, ld_dy, tokens, out}, ob{w, ld_w, in, out};
+    if (!plan_of(tokens, in, out, oa, ob, &p)) return thread_error(ABS_ELIMIT, "too many output tiles");
+    if (const char* why = check_workspace(p, workspace, workspace_bytes, &code)) return thread_error(code, why);
+    LinArgs a{};
+    a.out = dx; a.ld = ld_dx; a.res = residual; a.ld_res = ld_residual; a.z_in = static_cast<const bf16*>(z); a.ld_z = ld_z; a.act = act;
+    a.wide = rows_at(m[2], 16) && rows_at(m[3], 16) && rows_at(m[4], 16);
+    return product(kDgrad, dtype, oa, ob, tokens, in, out, p, a, static_cast<char*>(workspace), static_cast<cudaStream_t>(stream));
+}
+
+static bool wgrad_plan(uint64_t tokens, uint64_t in, uint64_t out, const Operand& x, const Operand& dy, LinPlan* p) {
+    if (!plan_of(in, out, tokens, x, dy, p)) return false;
+    p->bias_parts = bias_parts(tokens, out);
+    p->bias_bytes = up256((size_t)p->bias_parts * out * 4);
+    return true;
+}
+
+extern "C" size_t abs_linear_wgrad_workspace(uint64_t tokens, uint64_t in, uint64_t out, const void* x, uint64_t ld_x, const void* dy, uint64_t ld_dy) {
+    LinPlan p;
+    if (tokens == 0 || out == 0 || tokens > kSizeMax || in > kSizeMax || out > kSizeMax) return 0;
+    return wgrad_plan(tokens, in, out, {x, ld_x, tokens, in}, {dy, ld_dy, tokens, out}, &p) ? p.bytes() : 0;
+}
+
+extern "C" int abs_linear_wgrad(const void* x, uint64_t ld_x, const void* dy, uint64_t ld_dy, uint64_t tokens, uint64_t in, uint64_t out, float* dw, uint64_t ld_dw,
+                                float* db, int accumulate, void* workspace, size_t workspace_bytes, void* stream) {
+    int code = 0;
+    if (const char* why = check_sizes(tokens, in, out, ABS_F32, ABS_ACT_NONE, &code)) return thread_error(code, why);
+    const MatrixArg m[3] = {{x, ld_x, in, 2}, {dy, ld_dy, out, 2}, {dw, ld_dw, out, 4}};
+    if (const char* why = check_matrices(m)) return thread_error(ABS_EINVAL, why);
+    if (!dw || misaligned(db, 4)) return thread_error(ABS_EINVAL, "dw must not be NULL, db 4-byte aligned");
+    if (dw == db) return thread_error(ABS_EINVAL, "two outputs are the same");
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    cudaError_t e = cudaSuccess;
+    if (tokens == 0) {
+        if (!accumulate) {
+            e = cudaMemset2DAsync(dw, ld_dw * 4, 0, out * 4, in, s);
+            if (e == cudaSuccess && db) e = cudaMemsetAsync(db, 0, out * 4, s);
+        }
+        return e == cudaSuccess ? ABS_OK : thread_error(ABS_ECUDA, cudaGetErrorString(e));
+    }
+    if (!x || !dy) return thread_error(ABS_EINVAL, "x and dy must not be NULL");
+    if (const char* why = check_operands({dw, db}, x, dy)) return thread_error(ABS_EINVAL, why);
+    LinPlan p;
+    const Operand oa{x, ld_x, tokens, in}, ob{dy, ld_dy, tokens, out};
+    if (!wgrad_plan(tokens, in, out, oa, ob, &p)) return thread_error(ABS_ELIMIT, "too many output tiles");
+    if (const char* why = check_workspace(p, workspace, workspace_bytes, &code)) return thread_error(code, why);
+    if (db) {
+        float* part = reinterpret_cast<float*>(static_cast<char*>(workspace) + p.part_bytes + p.a_bytes + p.b_bytes);
+        const unsigned blocks = (unsigned)((out + 255) / 256);
+        e = launch_kernel(k_bias_part, dim3(blocks, p.bias_parts), 256, 0, s, true, static_cast<const bf16*>(dy), (size_t)ld_dy, (int)tokens, (int)out, (int)tma_ready(ob), part);
+        if (e == cudaSuccess) e = launch_kernel(k_bias_join, blocks, 256, 0, s, true, (const float*)part, p.bias_parts, (int)out, db, accumulate);
+        if (e != cudaSuccess) return thread_error(ABS_ECUDA, cudaGetErrorString(e));
+    }
+    LinArgs a{};
+    a.out = dw; a.ld = ld_dw; a.accumulate = accumulate != 0; a.wide = rows_at(m[2], 16);
+    return product(kWgrad, ABS_F32, oa, ob, in, out, tokens, p, a, static_cast<char*>(workspace), s);
+}
+
+extern "C" int abs_activation_backward(const void* dy, uint64_t ld_dy, uint32_t dtype, const void* z, uint64_t ld_z, uint32_t act, uint64_t tokens, uint64_t width,
+                                       void* dz, uint64_t ld_dz, void* stream) {
+    int code = 0;
+    if (const char* why = check_sizes(tokens, width, 1, dtype, act, &code)) return thread_error(code, why);
+    const MatrixArg m[3] = {{dy, ld_dy, width, size_of(dtype)}, {z, ld_z, width, 2}, {dz, ld_dz, width, 2}};
+    if (const char* why = check_matrices(m)) return thread_error(ABS_EINVAL, why);
+    for (int i = 0; i < 2; ++i)
+        if (const char* why = check_in_place(m[2], m[i], true)) return thread_error(ABS_EINVAL, why);
+    if (tokens == 0) return ABS_OK;
+    if (!dy || !z || !dz) return thread_error(ABS_EINVAL, "dy, z and dz must not be NULL");
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    const int wide = rows_at(m[0], 16) && rows_at(m[1], 16) && rows_at(m[2], 16);
+    const size_t want = ((size_t)tokens * ((width + 7) / 8) + 511) / 512;
+    const int grid = (int)std::min<size_t>(want, kSms * 8);
+    const cudaError_t e = dtype == ABS_F32 ? launch_kernel(k_activation_backward<float>, grid, 256, 0, s, true, static_cast<const float*>(dy), (size_t)ld_dy, static_cast<const bf16*>(z),
+                                                           (size_t)ld_z, act, (size_t)tokens, (int)width, wide, static_cast<bf16*>(dz), (size_t)ld_dz)
+                                           : launch_kernel(k_activation_backward<bf16>, grid, 256, 0, s, true, static_cast<const bf16*>(dy), (size_t)ld_dy, static_cast<const bf16*>(z),
+                                                           (size_t)ld_z, act, (size_t)tokens, (int)width, wide, static_cast<bf16*>(dz), (size_t)ld_dz);
+    return e == cudaSuccess ? ABS_OK : thread_error(ABS_ECUDA, cudaGetErrorString(e));
+}

@@ -26,5 +26,8 @@ static inline cudaError_t take_status(int* status, cudaStream_t s) {
 
 cudaError_t take_status_norm(int* status, cudaStream_t s);    // llm_norm.cu
 cudaError_t take_status_loss(int* status, cudaStream_t s);    // llm_loss.cu
+cudaError_t take_status_layer_norm(int* status, cudaStream_t s);   // llm_layer_norm.cu
+cudaError_t take_status_linear(int* status, cudaStream_t s);  // llm_linear.cu
+cudaError_t take_status_recurrence(int* status, cudaStream_t s);   // llm_recurrence.cu
 
 }  // namespace abs_sgd

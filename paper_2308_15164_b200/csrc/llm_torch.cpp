@@ -381,6 +381,241 @@ PyObject* ckpt8_wgrad(PyObject* const* a) {
     return THPVariable_Wrap(std::move(dw.t));
 }
 
+// A tensor of other sizes and type on the device of `l`.
+Like sized(const Like& l, ScalarType dtype, int64_t rows, int64_t cols) { return {nullptr, dtype, dtype == at::kFloat ? ABS_F32 : ABS_BF16, rows, cols, l.index, {}}; }
+Matrix given(PyObject* o, const char* name, const Like& l) { return o == Py_None ? Matrix{} : same(o, name, l); }
+const float* maybe_vector(PyObject* o, const char* name, int64_t n, int index) {
+    return o == Py_None ? nullptr : (const float*)vector(o, name, n, at::kFloat, index);
+}
+int64_t whole(PyObject* o) {
+    const int64_t v = PyLong_AsLongLong(o);
+    if (v == -1 && PyErr_Occurred()) throw Refused{nullptr, {}};
+    return v;
+}
+Like bf16_first(PyObject* o, const char* name) {
+    const Like l = first(o, name);
+    if (l.dtype != at::kBFloat16) type_error(std::string(name) + " must be bfloat16");
+    return l;
+}
+// Workspace of n bytes; the tensor keeps it while the call is enqueued.
+struct Workspace {
+    Tensor t;
+    void* p = nullptr;
+    size_t n;
+    Workspace(size_t bytes, int index) : n(bytes) {
+        if (!n) return;
+        t = made({(int64_t)n}, at::kByte, index);
+        p = t.mutable_data_ptr();
+    }
+};
+
+// ids, table, scale, bfloat16 (else float32), y
+PyObject* embed(PyObject* const* a) {
+    const Like table = first(a[1], "table");
+    if (table.dtype != at::kFloat) type_error("table must be float32");
+    const Tensor* t = tensor_of(a[0]);
+    if (!t || t->dim() != 1) type_error("ids must be a CUDA tensor of one dimension");
+    const int64_t T = t->size(0);
+    const auto* ids = (const int32_t*)vector(a[0], "ids", T, at::kInt, table.index);
+    const float scale = number(a[2]);
+    const Like l = sized(table, truth(a[3]) ? at::kBFloat16 : at::kFloat, T, table.cols);
+    Out y = out(a[4], "y", l);
+    launch(l.index, [&](void* s) { return abs_embed(ids, T, (const float*)table.m.p, table.m.ld, table.rows, table.cols, scale, l.code, y.m.p, y.m.ld, s); });
+    written(a[4]);
+    return THPVariable_Wrap(std::move(y.t));
+}
+
+// dy, ids, vocab, scale, out, accumulate
+PyObject* embed_backward(PyObject* const* a) {
+    const Like l = first(a[0], "dy");
+    const auto* ids = (const int32_t*)vector(a[1], "ids", l.rows, at::kInt, l.index);
+    const int64_t V = whole(a[2]);
+    if (V < 1) value_error("vocab must be at least 1");
+    const float scale = number(a[3]);
+    const bool accumulate = truth(a[5]);
+    if (accumulate && a[4] == Py_None) value_error("accumulate needs an out to add to");
+    Out d = out(a[4], "out", sized(l, at::kFloat, V, l.cols));
+    const Workspace ws(abs_embed_backward_workspace(l.rows, V, l.cols), l.index);
+    launch(l.index, [&](void* s) { return abs_embed_backward(l.m.p, l.m.ld, l.code, ids, l.rows, V, l.cols, scale, (float*)d.m.p, d.m.ld, accumulate, ws.p, ws.n, s); });
+    written(a[4]);
+    return THPVariable_Wrap(std::move(d.t));
+}
+
+// x, w, b, eps, n
+PyObject* layer_norm(PyObject* const* a) {
+    const Like l = first(a[0], "x");
+    const auto* w = (const float*)vector(a[1], "w", l.cols, at::kFloat, l.index);
+    const float* b = maybe_vector(a[2], "b", l.cols, l.index);
+    const float eps = number(a[3]);
+    Out n = out(a[4], "n", l);
+    launch(l.index, [&](void* s) { return abs_layer_norm(l.m.p, l.m.ld, w, b, eps, l.code, l.rows, l.cols, n.m.p, n.m.ld, s); });
+    written(a[4]);
+    return THPVariable_Wrap(std::move(n.t));
+}
+
+// dn, x, w, dskip, bias, eps, dx, dw, db, accumulate
+PyObject* layer_norm_backward(PyObject* const* a) {
+    const Like l = first(a[1], "x");
+    const Matrix dn = same(a[0], "dn", l), skip = given(a[3], "dskip", l);
+    const auto* w = (const float*)vector(a[2], "w", l.cols, at::kFloat, l.index);
+    const bool bias = truth(a[4]), accumulate = truth(a[9]);
+    const float eps = number(a[5]);
+    if (!bias && a[8] != Py_None) value_error("db is given but bias is False");
+    c10::cuda::CUDAGuard guard((c10::DeviceIndex)l.index);           // new sums are cleared on the stream of that device
+    Out dx = out(a[6], "dx", l);
+    Column dw = column(a[7], "dw", l, accumulate), db;
+    if (bias) db = column(a[8], "db", l, accumulate);
+    const Workspace ws(abs_layer_norm_workspace(l.rows, l.cols), l.index);
+    launch(l.index, [&](void* s) {
+        return abs_layer_norm_backward(dn.p, dn.ld, l.m.p, l.m.ld, skip.p, skip.ld, w, eps, l.code, l.rows, l.cols, dx.m.p, dx.m.ld, dw.p, db.p, accumulate, ws.p, ws.n, s);
+    });
+    written(a[6], a[7], a[8]);
+    return tuple(std::move(dx.t), std::move(dw.t), std::move(db.t));
+}
+
+// x, w, b, act, residual, keep, bfloat16 (else float32), y, z
+PyObject* linear(PyObject* const* a) {
+    const Like x = bf16_first(a[0], "x"), w = bf16_first(a[1], "w");
+    if (w.index != x.index || w.rows != x.cols) value_error("w must have as many rows as x has columns, on its device");
+    const Like l = sized(x, truth(a[6]) ? at::kBFloat16 : at::kFloat, x.rows, w.cols), lz = sized(x, at::kBFloat16, x.rows, w.cols);
+    const float* b = maybe_vector(a[2], "b", w.cols, x.index);
+    const uint32_t act = (uint32_t)whole(a[3]);
+    const Matrix res = given(a[4], "residual", l);
+    const bool keep = truth(a[5]);
+    if (!keep && a[8] != Py_None) value_error("z is given but keep is False");
+    Out y = out(a[7], "y", l), z;
+    if (keep) z = out(a[8], "z", lz);
+    const Workspace ws(abs_linear_workspace(x.rows, x.cols, w.cols, x.m.p, x.m.ld, w.m.p, w.m.ld), x.index);
+    launch(x.index, [&](void* s) {
+        return abs_linear(x.m.p, x.m.ld, w.m.p, w.m.ld, b, act, res.p, res.ld, l.code, x.rows, x.cols, w.cols, y.m.p, y.m.ld, z.m.p, z.m.ld, ws.p, ws.n, s);
+    });
+    written(a[7], a[8]);
+    return tuple(std::move(y.t), std::move(z.t));
+}
+
+// dy, w, act, z, residual, bfloat16 (else float32), dx
+PyObject* linear_dgrad(PyObject* const* a) {
+    const Like dy = bf16_first(a[0], "dy"), w = bf16_first(a[1], "w");
+    if (w.index != dy.index || w.cols != dy.cols) value_error("w must have as many columns as dy, on its device");
+    const Like l = sized(dy, truth(a[5]) ? at::kBFloat16 : at::kFloat, dy.rows, w.rows), lz = sized(dy, at::kBFloat16, dy.rows, w.rows);
+    const uint32_t act = (uint32_t)whole(a[2]);
+    const Matrix z = given(a[3], "z", lz), res = given(a[4], "residual", l);
+    if ((act != ABS_ACT_NONE) != (a[3] != Py_None)) value_error("z must be given exactly with an activation");
+    Out dx = out(a[6], "dx", l);
+    const Workspace ws(abs_linear_dgrad_workspace(dy.rows, w.rows, dy.cols, dy.m.p, dy.m.ld, w.m.p, w.m.ld), dy.index);
+    launch(dy.index, [&](void* s) {
+        return abs_linear_dgrad(dy.m.p, dy.m.ld, w.m.p, w.m.ld, act, z.p, z.ld, res.p, res.ld, l.code, dy.rows, w.rows, dy.cols, dx.m.p, dx.m.ld, ws.p, ws.n, s);
+    });
+    written(a[6]);
+    return THPVariable_Wrap(std::move(dx.t));
+}
+
+// x, dy, bias, dw, db, accumulate
+PyObject* linear_wgrad(PyObject* const* a) {
+    const Like x = bf16_first(a[0], "x"), dy = bf16_first(a[1], "dy");
+    if (dy.index != x.index || dy.rows != x.rows) value_error("dy must have as many rows as x, on its device");
+    const bool bias = truth(a[2]), accumulate = truth(a[5]);
+    if (!bias && a[4] != Py_None) value_error("db is given but bias is False");
+    if (accumulate && (a[3] == Py_None || (bias && a[4] == Py_None))) value_error("accumulate needs sums to add to");
+    Out dw = out(a[3], "dw", sized(x, at::kFloat, x.cols, dy.cols));
+    Column db;
+    if (bias) db = column(a[4], "db", dy, false);
+    const Workspace ws(abs_linear_wgrad_workspace(x.rows, x.cols, dy.cols, x.m.p, x.m.ld, dy.m.p, dy.m.ld), x.index);
+    launch(x.index, [&](void* s) {
+        return abs_linear_wgrad(x.m.p, x.m.ld, dy.m.p, dy.m.ld, x.rows, x.cols, dy.cols, (float*)dw.m.p, dw.m.ld, db.p, accumulate, ws.p, ws.n, s);
+    });
+    written(a[3], a[4]);
+    return tuple(std::move(dw.t), std::move(db.t));
+}
+
+// dy, z, act, dz
+PyObject* activation_backward(PyObject* const* a) {
+    const Like dy = first(a[0], "dy"), l = sized(dy, at::kBFloat16, dy.rows, dy.cols);
+    const Matrix z = same(a[1], "z", l);
+    const uint32_t act = (uint32_t)whole(a[2]);
+    Out dz = out(a[3], "dz", l);
+    launch(l.index, [&](void* s) { return abs_activation_backward(dy.m.p, dy.m.ld, dy.code, z.p, z.ld, act, l.rows, l.cols, dz.m.p, dz.m.ld, s); });
+    written(a[3]);
+    return THPVariable_Wrap(std::move(dz.t));
+}
+
+// Sequences of a packed matrix: offsets (None: one sequence) and how many there are.
+struct Sequences {
+    const int32_t* offsets = nullptr;
+    int64_t n = 1;
+};
+Sequences sequences(PyObject* o, int index) {
+    if (o == Py_None) return {};
+    const Tensor* t = tensor_of(o);
+    if (!t || t->dim() != 1 || t->size(0) < 1) value_error("offsets must have sequences + 1 elements on the device of x");
+    return {(const int32_t*)vector(o, "offsets", t->size(0), at::kInt, index), t->size(0) - 1};
+}
+// [sequences, width] fp32, packed.
+float* state(PyObject* o, const char* name, int64_t n, int64_t width, int index, bool is_out) {
+    const Tensor& t = typed(o, name, at::kFloat, index);
+    if (t.dim() != 2 || t.size(0) != n || t.size(1) != width || !t.is_contiguous())
+        value_error(std::string(name) + " must be contiguous of shape " + shape_of({n, width}));
+    return is_out ? t.mutable_data_ptr<float>() : const_cast<float*>(t.const_data_ptr<float>());
+}
+Out state_out(PyObject* o, const char* name, int64_t n, int64_t width, int index) {
+    Out r;
+    if (o == Py_None) {
+        r.t = made({n, width}, at::kFloat, index);
+        r.m.p = r.t.mutable_data_ptr();
+    } else {
+        r.m.p = state(o, name, n, width, index, true);
+        r.t = THPVariable_Unpack(o);
+    }
+    return r;
+}
+
+// x, g, offsets, h0, kind, y, last
+PyObject* recurrence(PyObject* const* a) {
+    const Like l = first(a[0], "x");
+    const Matrix g = same(a[1], "g", l);
+    const Sequences q = sequences(a[2], l.index);
+    const float* h0 = a[3] == Py_None ? nullptr : state(a[3], "h0", q.n, l.cols, l.index, false);
+    const uint32_t kind = (uint32_t)whole(a[4]);
+    Out y = out(a[5], "y", l), last = state_out(a[6], "last", q.n, l.cols, l.index);
+    const Workspace ws(abs_recurrence_workspace(l.rows, l.cols), l.index);
+    launch(l.index, [&](void* s) {
+        return abs_recurrence(l.m.p, l.m.ld, g.p, g.ld, q.offsets, q.n, h0, kind, l.code, l.rows, l.cols, y.m.p, y.m.ld, (float*)last.m.p, ws.p, ws.n, s);
+    });
+    written(a[5], a[6]);
+    return tuple(std::move(y.t), std::move(last.t));
+}
+
+// dy, x, g, y, offsets, h0, dlast, kind, dx, dg, dh0
+PyObject* recurrence_backward(PyObject* const* a) {
+    const Like l = first(a[1], "x");
+    const Matrix dy = same(a[0], "dy", l), g = same(a[2], "g", l), y = same(a[3], "y", l);
+    const Sequences q = sequences(a[4], l.index);
+    const float* h0 = a[5] == Py_None ? nullptr : state(a[5], "h0", q.n, l.cols, l.index, false);
+    const float* dlast = a[6] == Py_None ? nullptr : state(a[6], "dlast", q.n, l.cols, l.index, false);
+    const uint32_t kind = (uint32_t)whole(a[7]);
+    Out dx = out(a[8], "dx", l), dg = out(a[9], "dg", l), dh0;
+    if (h0 || a[10] != Py_None) dh0 = state_out(a[10], "dh0", q.n, l.cols, l.index);
+    const Workspace ws(abs_recurrence_workspace(l.rows, l.cols), l.index);
+    launch(l.index, [&](void* s) {
+        return abs_recurrence_backward(dy.p, dy.ld, l.m.p, l.m.ld, g.p, g.ld, y.p, y.ld, q.offsets, q.n, h0, dlast, kind, l.code, l.rows, l.cols, dx.m.p, dx.m.ld, dg.m.p, dg.m.ld,
+                                       (float*)dh0.m.p, ws.p, ws.n, s);
+    });
+    written(a[8], a[9], a[10]);
+    return tuple(std::move(dx.t), std::move(dg.t), std::move(dh0.t));
+}
+
+// x, g, h, kind, y, out
+PyObject* recurrence_step(PyObject* const* a) {
+    const Like l = first(a[0], "x");
+    const Matrix g = same(a[1], "g", l);
+    const float* h = state(a[2], "h", l.rows, l.cols, l.index, false);
+    const uint32_t kind = (uint32_t)whole(a[3]);
+    Out y = out(a[4], "y", l), o = state_out(a[5], "out", l.rows, l.cols, l.index);
+    launch(l.index, [&](void* s) { return abs_recurrence_step(l.m.p, l.m.ld, g.p, g.ld, h, kind, l.code, l.rows, l.cols, y.m.p, y.m.ld, (float*)o.m.p, s); });
+    written(a[4], a[5]);
+    return tuple(std::move(y.t), std::move(o.t));
+}
+
 template <PyObject* (*fn)(PyObject* const*), int kArgs>
 PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) {
     if (n != kArgs) {
@@ -423,6 +658,17 @@ PyMethodDef kMethods[] = {
     method<ckpt8_quantize, 1>("ckpt8_quantize"),
     method<ckpt8_dequantize, 5>("ckpt8_dequantize"),
     method<ckpt8_wgrad, 6>("ckpt8_wgrad"),
+    method<embed, 5>("embed"),
+    method<embed_backward, 6>("embed_backward"),
+    method<layer_norm, 5>("layer_norm"),
+    method<layer_norm_backward, 10>("layer_norm_backward"),
+    method<linear, 9>("linear"),
+    method<linear_dgrad, 7>("linear_dgrad"),
+    method<linear_wgrad, 6>("linear_wgrad"),
+    method<activation_backward, 4>("activation_backward"),
+    method<recurrence, 7>("recurrence"),
+    method<recurrence_backward, 11>("recurrence_backward"),
+    method<recurrence_step, 6>("recurrence_step"),
     {"set_errors", set_errors, METH_VARARGS, "The exceptions of a status, called with (status, text), and of an allocation that failed."},
     {nullptr, nullptr, 0, nullptr},
 };
