@@ -34,94 +34,161 @@ struct LinArgs {
     const bf16* z_in;                // dgrad
     bf16* z_out;                     // forward
     size_t ld_z;
-    uint32_t act;
     int accumulate;
     int wide;                        // rows of out, res and z are 16-byte aligned
 };
 
-// ---- activations
-__device__ __forceinline__ float activate(uint32_t act, float z) {
-    if (act == ABS_ACT_RELU) return z > 0.f ? z : z == z ? 0.f : z;
-    if (act == ABS_ACT_GELU) return z * normcdff(z);
-    if (act == ABS_ACT_SILU) return z / (1.f + __expf(-z));
+// ---- activations, two numbers at a time
+// Phi(-|z|) = exp(-z^2 / 2) P(1 / (1 + 0.35 |z|)) with P of degree 7 fitted to the smallest relative error over 0 <= |z| <= 13.5 (beyond, the
+// exponential underflows): 3e-7, in fp32 6e-7, so that the lower tail keeps its precision.  17 instructions a number less than through
+// the error function.  E: 2^24 times the exponential (which then stays above the unit's flush to zero), q: Phi(-|z|), m: |z| up to 14 (q is next to
+// nothing from there on, also times an infinity).
+__device__ __forceinline__ void normal_tail(float2 z, float2& E, float2& q, float2& m) {
+    const float2 w = make_float2(fabsf(z.x), fabsf(z.y)), d = fma2(w, both(0.35f), both(1.f));
+    float2 t;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(t.x) : "f"(d.x));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(t.y) : "f"(d.y));
+    E = exp2_of(fma2(mul2(z, z), both(-0.72134752044448170f), both(24.f)));
+    constexpr float k = 0x1p-24f;
+    float2 p = fma2(t, both(0.04894255149557414f * k), both(-0.20211968521483073f * k));
+    p = fma2(p, t, both(0.24064142309471856f * k));
+    p = fma2(p, t, both(-0.017023902126677096f * k));
+    p = fma2(p, t, both(0.15596167730976151f * k));
+    p = fma2(p, t, both(0.1333550587912772f * k));
+    p = fma2(p, t, both(0.14027034589594403f * k));
+    p = fma2(p, t, both(-2.731542404448325e-05f * k));
+    q = mul2(p, E);
+    m = make_float2(fminf(w.x, 14.f), fminf(w.y, 14.f));
+}
+// sigmoid(z) and 1 - sigmoid(z), each to its own precision.
+__device__ __forceinline__ void sigmoids(float2 z, float2& s, float2& rest) {
+    float2 v = mul2(z, both(-1.4426950408889634f));
+    v.x = v.x > 126.f ? 126.f : v.x;             // keeps a NaN
+    v.y = v.y > 126.f ? 126.f : v.y;
+    const float2 e = exp2_of(v), d = add2(e, both(1.f));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(s.x) : "f"(d.x));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(s.y) : "f"(d.y));
+    rest = mul2(e, s);
+}
+template <uint32_t kAct>
+__device__ __forceinline__ float2 activate(float2 z) {
+    if (kAct == ABS_ACT_RELU) return make_float2(z.x > 0.f ? z.x : z.x == z.x ? 0.f : z.x, z.y > 0.f ? z.y : z.y == z.y ? 0.f : z.y);
+    if (kAct == ABS_ACT_GELU) {                  // max(z, 0) - |z| Phi(-|z|)
+        float2 E, q, m;
+        normal_tail(z, E, q, m);
+        return fma2(make_float2(-m.x, -m.y), q, make_float2(fmaxf(z.x, 0.f), fmaxf(z.y, 0.f)));
+    }
+    if (kAct == ABS_ACT_SILU) {
+        float2 s, rest;
+        sigmoids(z, s, rest);
+        return mul2(z, s);
+    }
     return z;
 }
-__device__ __forceinline__ float slope(uint32_t act, float z) {
-    if (act == ABS_ACT_RELU) return z > 0.f ? 1.f : z == z ? 0.f : z;
-    if (act == ABS_ACT_GELU) return fmaf(z, 0.3989422804014327f * __expf(-0.5f * z * z), normcdff(z));
-    if (act == ABS_ACT_SILU) {
-        const float s = 1.f / (1.f + __expf(-z));
-        return s * fmaf(z, 1.f / (1.f + __expf(z)), 1.f);
+template <uint32_t kAct>
+__device__ __forceinline__ float2 slope(float2 z) {
+    if (kAct == ABS_ACT_RELU) return make_float2(z.x > 0.f ? 1.f : z.x == z.x ? 0.f : z.x, z.y > 0.f ? 1.f : z.y == z.y ? 0.f : z.y);
+    if (kAct == ABS_ACT_GELU) {                  // Phi(z) + z phi(z)
+        float2 E, q, m;
+        normal_tail(z, E, q, m);
+        const float2 phi = make_float2(z.x > 0.f ? 1.f - q.x : q.x, z.y > 0.f ? 1.f - q.y : q.y);
+        return fma2(make_float2(copysignf(m.x, z.x), copysignf(m.y, z.y)), mul2(E, both(0.3989422804014327f * 0x1p-24f)), phi);
     }
-    return 1.f;
+    if (kAct == ABS_ACT_SILU) {                  // s (1 + z (1 - s)); beyond 126 one of the factors is 0
+        float2 s, rest;
+        sigmoids(z, s, rest);
+        return mul2(s, fma2(make_float2(fminf(fmaxf(z.x, -126.f), 126.f), fminf(fmaxf(z.y, -126.f), 126.f)), rest, both(1.f)));
+    }
+    return both(1.f);
 }
 
+// Eight elements of a row, 16-byte aligned.
 template <typename T>
-__device__ __forceinline__ void load8(const T* p, int n, bool wide, float (&v)[8]) {
-    if (wide && n == 8) {
+struct Row8 {
+    static constexpr int kN = 8 / kVec<T>;
+    uint4 w[kN];
+    __device__ __forceinline__ void load(const T* p) {
 #pragma unroll
-        for (int h = 0; h < 8 / kVec<T>; ++h) {
-            float w[kVec<T>];
-            Pack<T, kVec<T>>::load(p + h * kVec<T>, w);
-#pragma unroll
-            for (int i = 0; i < kVec<T>; ++i) v[h * kVec<T> + i] = w[i];
-        }
-        return;
+        for (int h = 0; h < kN; ++h) w[h] = *reinterpret_cast<const uint4*>(p + h * kVec<T>);
     }
+    __device__ __forceinline__ void get(float2 (&v)[4]) const {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = i < n ? to_f(p[i]) : 0.f;
-}
-template <typename T>
-__device__ __forceinline__ void store8(T* p, int n, bool wide, const float (&v)[8]) {
-    if (wide && n == 8) {
+        for (int h = 0; h < kN; ++h) {
+            float2 u[kPairs<T>];
+            unpack(w[h], u, T());
 #pragma unroll
-        for (int h = 0; h < 8 / kVec<T>; ++h) {
-            float w[kVec<T>];
-#pragma unroll
-            for (int i = 0; i < kVec<T>; ++i) w[i] = v[h * kVec<T> + i];
-            Pack<T, kVec<T>>::store(p + h * kVec<T>, w);
+            for (int i = 0; i < kPairs<T>; ++i) v[h * kPairs<T> + i] = u[i];
         }
-        return;
     }
+    __device__ __forceinline__ void put(const float2 (&v)[4]) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-        if (i < n) p[i] = from_f<T>(v[i]);
-}
+        for (int h = 0; h < kN; ++h) {
+            float2 u[kPairs<T>];
+#pragma unroll
+            for (int i = 0; i < kPairs<T>; ++i) u[i] = v[h * kPairs<T> + i];
+            w[h] = pack(u, T());
+        }
+    }
+    __device__ __forceinline__ void store(T* p) const {
+#pragma unroll
+        for (int h = 0; h < kN; ++h) *reinterpret_cast<uint4*>(p + h * kVec<T>) = w[h];
+    }
+};
 
-// The layer's work on n (1 .. 8) sums of row `row` from column `col`.
-template <int kEpi, typename T>
-__device__ __forceinline__ void finish(const LinArgs& a, int row, int col, int n, float (&v)[8]) {
+// The layer's work on eight sums of a row, all of them inside the matrix: what it reads, then what it makes of the sums.
+template <int kEpi, uint32_t kAct, typename T>
+struct Finish {
+    Row8<T> r;                       // residual, or what dw holds
+    Row8<bf16> z;
+    __device__ __forceinline__ void load(const LinArgs& a, int row, int col) {
+        if (kEpi == kWgrad ? a.accumulate != 0 : a.res != nullptr)
+            r.load(kEpi == kWgrad ? static_cast<const T*>(a.out) + (size_t)row * a.ld + col : static_cast<const T*>(a.res) + (size_t)row * a.ld_res + col);
+        if (kEpi == kDgrad && kAct != ABS_ACT_NONE) z.load(a.z_in + (size_t)row * a.ld_z + col);
+    }
+    __device__ __forceinline__ void operator()(const LinArgs& a, int row, int col, const float2 (&bias)[4], float2 (&v)[4]) {
+        float2 w[4];
+        if (kEpi == kForward) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = add2(v[i], bias[i]);
+            if (a.z_out) {
+                Row8<bf16> o;
+                o.put(v);
+                o.store(a.z_out + (size_t)row * a.ld_z + col);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = activate<kAct>(v[i]);
+        }
+        if (kEpi == kDgrad && kAct != ABS_ACT_NONE) {
+            z.get(w);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = mul2(v[i], slope<kAct>(w[i]));
+        }
+        if (kEpi == kWgrad ? a.accumulate != 0 : a.res != nullptr) {
+            r.get(w);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = add2(v[i], w[i]);
+        }
+        Row8<T> o;
+        o.put(v);
+        o.store(static_cast<T*>(a.out) + (size_t)row * a.ld + col);
+    }
+};
+// The same for a single one.
+template <int kEpi, uint32_t kAct, typename T>
+__device__ __forceinline__ void finish_one(const LinArgs& a, int row, int col, float bias, float v) {
     T* out = static_cast<T*>(a.out) + (size_t)row * a.ld + col;
-    const bool wide = a.wide != 0;
-    float w[8];
-    if constexpr (kEpi == kWgrad) {
-        if (a.accumulate) {
-            load8(out, n, wide, w);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] += w[i];
-        }
-    } else {
-        if constexpr (kEpi == kForward) {
-            if (a.bias)
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    if (i < n) v[i] += __ldg(a.bias + col + i);
-            if (a.z_out) store8(a.z_out + (size_t)row * a.ld_z + col, n, wide, v);
-            if (a.act != ABS_ACT_NONE)
-#pragma unroll
-                for (int i = 0; i < 8; ++i) v[i] = activate(a.act, v[i]);
-        } else if (a.act != ABS_ACT_NONE) {
-            load8(a.z_in + (size_t)row * a.ld_z + col, n, wide, w);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] *= slope(a.act, w[i]);
-        }
-        if (a.res) {
-            load8(static_cast<const T*>(a.res) + (size_t)row * a.ld_res + col, n, wide, w);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] += w[i];
-        }
+    if (kEpi == kForward) {
+        v += bias;
+        if (a.z_out) a.z_out[(size_t)row * a.ld_z + col] = __float2bfloat16_rn(v);
+        v = activate<kAct>(both(v)).x;
     }
-    store8(out, n, wide, v);
+    if (kEpi == kDgrad && kAct != ABS_ACT_NONE) v *= slope<kAct>(both(__bfloat162float(a.z_in[(size_t)row * a.ld_z + col]))).x;
+    if (kEpi == kWgrad) {
+        if (a.accumulate) v += to_f(*out);
+    } else if (a.res) {
+        v += to_f(static_cast<const T*>(a.res)[(size_t)row * a.ld_res + col]);
+    }
+    *out = from_f<T>(v);
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -137,9 +204,10 @@ __device__ __forceinline__ void finish(const LinArgs& a, int row, int col, int n
 // Launched in plain stream order, and starts no successor early (see llm_ckpt8.cu).  Every wait on a barrier is bounded.
 // ------------------------------------------------------------------------------------------------
 constexpr int kTM = 256, kTN = 256, kTK = 64;    // of a pair
-constexpr int kStages = 5, kEpiWarps = 8, kThreads = 64 + kEpiWarps * 32;
+constexpr int kStages = 4, kEpiWarps = 16, kThreads = 64 + kEpiWarps * 32;
 constexpr int kHalf = kTK * 128 * 2;             // bytes of an operand's share of a CTA and run
 constexpr int kPitch = 36;                       // floats of a staged row: 16-byte pieces, eight rows on different banks
+constexpr int kWarpCols = kTN / (kEpiWarps / 4); // columns of an epilogue warp
 constexpr int kSegmentRuns = 12;
 constexpr int kSms = 148;
 constexpr uint64_t kSizeMax = 0x7fffffc0ull;
@@ -207,7 +275,7 @@ __device__ __forceinline__ uint64_t operand_desc(uint32_t at, int k16) {
     return kMn ? umma_desc_mn_sw128(at + k16 * 2048, kHalf / 2) : umma_desc_k_sw128(at + k16 * 32);
 }
 
-template <int kEpi, typename T>
+template <int kEpi, uint32_t kAct, typename T>
 __global__ void __launch_bounds__(kThreads, 1) k_linear(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_b,
                                                         const __grid_constant__ LinArgs a) {
     constexpr bool kAMn = kEpi == kWgrad, kBMn = kEpi != kDgrad;
@@ -308,17 +376,17 @@ __global__ void __launch_bounds__(kThreads, 1) k_linear(const __grid_constant__ 
             if (!ok) *failed = 1;
         }
         __syncwarp();
-    } else {                                         // ---- epilogue: warps 2-5 the first 128 columns, 6-9 the others
-        const int qd = warp % 4, half = (warp - 2) / 4;
+    } else {                                         // ---- epilogue: four warps for the rows, four times 64 columns
+        const int qd = warp % 4, part_col = (warp - 2) / 4 * kWarpCols;
         float* stage = s.out[warp - 2];
         const int row = rank * 128 + qd * 32;        // of the tile
         int i = 0;
         bool ok = true;
         for (int it = pair; it < items && ok; it += pairs) {
             const Item q = item_of(it);
-            float2 sum[4][16];
+            float2 sum[kWarpCols / 32][16];
 #pragma unroll
-            for (int c = 0; c < 4; ++c)
+            for (int c = 0; c < kWarpCols / 32; ++c)
 #pragma unroll
                 for (int j = 0; j < 16; ++j) sum[c][j] = both(0.f);
             for (int kb0 = q.kb0; kb0 < q.kb1; kb0 += kSegmentRuns, ++i) {
@@ -327,9 +395,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_linear(const __grid_constant__ 
                 if (!ok) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll
-                for (int c = 0; c < 8; ++c) {
+                for (int c = 0; c < kWarpCols / 16; ++c) {
                     uint32_t v[16];
-                    tmem_ld_16(tmem + ((uint32_t)(qd * 32) << 16) + (uint32_t)(ab * kTN + half * 128 + c * 16), v);
+                    tmem_ld_16(tmem + ((uint32_t)(qd * 32) << 16) + (uint32_t)(ab * kTN + part_col + c * 16), v);
 #pragma unroll
                     for (int j = 0; j < 8; ++j)
                         sum[c / 2][c % 2 * 8 + j] = add2(sum[c / 2][c % 2 * 8 + j], make_float2(__uint_as_float(v[2 * j]), __uint_as_float(v[2 * j + 1])));
@@ -342,29 +410,51 @@ __global__ void __launch_bounds__(kThreads, 1) k_linear(const __grid_constant__ 
                 *failed = 1;
                 break;
             }
-            float* part = q.part >= 0 ? a.part + ((size_t)q.part * kTM + row) * kTN + half * 128 : nullptr;
-            const int rows = min(32, a.M - (q.m0 + row)), col0 = q.n0 + half * 128, cols = min(128, a.N - col0);
+            float* part = q.part >= 0 ? a.part + ((size_t)q.part * kTM + row) * kTN + part_col : nullptr;
+            const int rows = min(32, a.M - (q.m0 + row)), col0 = q.n0 + part_col, cols = min(kWarpCols, a.N - col0);
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
+            for (int c = 0; c < kWarpCols / 32; ++c) {
                 if (c * 32 >= cols || rows <= 0) continue;
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
                     *reinterpret_cast<float4*>(stage + lane * kPitch + 4 * j) = make_float4(sum[c][2 * j].x, sum[c][2 * j].y, sum[c][2 * j + 1].x, sum[c][2 * j + 1].y);
                 __syncwarp();
-                const int cc = c * 32 + lane % 4 * 8, n = min(8, cols - cc);
+                const int cc = c * 32 + lane % 4 * 8;
+                if (part) {
 #pragma unroll
-                for (int p = 0; p < 4; ++p) {
-                    const int r = p * 8 + lane / 4;
-                    if (r >= rows || n <= 0) continue;
-                    const float4 lo = *reinterpret_cast<const float4*>(stage + r * kPitch + lane % 4 * 8);
-                    const float4 hi = *reinterpret_cast<const float4*>(stage + r * kPitch + lane % 4 * 8 + 4);
-                    if (part) {
-                        *reinterpret_cast<float4*>(part + (size_t)r * kTN + cc) = lo;
-                        *reinterpret_cast<float4*>(part + (size_t)r * kTN + cc + 4) = hi;
-                    } else {
-                        float v[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
-                        finish<kEpi, T>(a, q.m0 + row + r, col0 + cc, n, v);
+                    for (int p = 0; p < 4; ++p) {
+                        const int r = p * 8 + lane / 4;
+                        if (r >= rows || cc >= cols) continue;
+                        float* to = part + (size_t)r * kTN + cc;
+                        *reinterpret_cast<float4*>(to) = *reinterpret_cast<const float4*>(stage + r * kPitch + lane % 4 * 8);
+                        *reinterpret_cast<float4*>(to + 4) = *reinterpret_cast<const float4*>(stage + r * kPitch + lane % 4 * 8 + 4);
                     }
+                } else if (a.wide && c * 32 + 32 <= cols) {
+                    float2 bias[4];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        bias[k] = kEpi == kForward && a.bias ? make_float2(__ldg(a.bias + col0 + cc + 2 * k), __ldg(a.bias + col0 + cc + 2 * k + 1)) : both(0.f);
+#pragma unroll
+                    for (int p = 0; p < 4; p += 2) {
+                        Finish<kEpi, kAct, T> f[2];  // the reads of two rows are in flight together
+#pragma unroll
+                        for (int h = 0; h < 2; ++h)
+                            if ((p + h) * 8 + lane / 4 < rows) f[h].load(a, q.m0 + row + (p + h) * 8 + lane / 4, col0 + cc);
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            const int r = (p + h) * 8 + lane / 4;
+                            if (r >= rows) continue;
+                            const float4 lo = *reinterpret_cast<const float4*>(stage + r * kPitch + lane % 4 * 8);
+                            const float4 hi = *reinterpret_cast<const float4*>(stage + r * kPitch + lane % 4 * 8 + 4);
+                            float2 v[4] = {make_float2(lo.x, lo.y), make_float2(lo.z, lo.w), make_float2(hi.x, hi.y), make_float2(hi.z, hi.w)};
+                            f[h](a, q.m0 + row + r, col0 + cc, bias, v);
+                        }
+                    }
+                } else if (c * 32 + lane < cols) {   // a column a thread
+                    const int col = col0 + c * 32 + lane;
+                    const float bias = kEpi == kForward && a.bias ? __ldg(a.bias + col) : 0.f;
+#pragma unroll 4
+                    for (int r = 0; r < rows; ++r) finish_one<kEpi, kAct, T>(a, q.m0 + row + r, col, bias, stage[r * kPitch + lane]);
                 }
                 __syncwarp();
             }
@@ -378,7 +468,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_linear(const __grid_constant__ 
 }
 
 // The tiles that were cut: their partial sums added up in order.  A warp per row of a tile, eight columns a thread.
-template <int kEpi, typename T>
+template <int kEpi, uint32_t kAct, typename T>
 __global__ void __launch_bounds__(256) k_linear_join(const __grid_constant__ LinArgs a) {
     pdl_wait();
     pdl_trigger();
@@ -387,15 +477,32 @@ __global__ void __launch_bounds__(256) k_linear_join(const __grid_constant__ Lin
     for (int i = blockIdx.x * 8 + threadIdx.x / 32; i < a.rest * kTM; i += gridDim.x * 8) {
         const int tile = a.whole + i / kTM, row = tile / a.tiles_n * kTM + i % kTM, col = tile % a.tiles_n * kTN + lane * 8, n = min(8, a.N - col);
         if (row >= a.M || n <= 0) continue;
-        float v[8] = {};
+        const bool wide = a.wide && n == 8;
+        Finish<kEpi, kAct, T> f;
+        if (wide) f.load(a, row, col);
+        float2 v[4] = {};
         const float* p = a.part + (size_t)i * kTN + lane * 8;
 #pragma unroll 4
         for (int k = 0; k < a.splits; ++k) {
             const float4 lo = *reinterpret_cast<const float4*>(p + k * step), hi = *reinterpret_cast<const float4*>(p + k * step + 4);
-            v[0] += lo.x; v[1] += lo.y; v[2] += lo.z; v[3] += lo.w;
-            v[4] += hi.x; v[5] += hi.y; v[6] += hi.z; v[7] += hi.w;
+            v[0] = add2(v[0], make_float2(lo.x, lo.y));
+            v[1] = add2(v[1], make_float2(lo.z, lo.w));
+            v[2] = add2(v[2], make_float2(hi.x, hi.y));
+            v[3] = add2(v[3], make_float2(hi.z, hi.w));
         }
-        finish<kEpi, T>(a, row, col, n, v);
+        float2 bias[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            bias[k] = kEpi == kForward && a.bias ? make_float2(2 * k < n ? a.bias[col + 2 * k] : 0.f, 2 * k + 1 < n ? a.bias[col + 2 * k + 1] : 0.f) : both(0.f);
+        if (wide) {
+            f(a, row, col, bias, v);
+        } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                if (2 * k < n) finish_one<kEpi, kAct, T>(a, row, col + 2 * k, bias[k].x, v[k].x);
+                if (2 * k + 1 < n) finish_one<kEpi, kAct, T>(a, row, col + 2 * k + 1, bias[k].y, v[k].y);
+            }
+        }
     }
 }
 
@@ -420,10 +527,18 @@ __global__ void __launch_bounds__(256) k_bias_part(const bf16* dy, size_t ld, in
     if (n > 0)
 #pragma unroll 4
         for (int64_t t = (int64_t)blockIdx.y * 8 + warp; t < T; t += (int64_t)gridDim.y * 8) {
-            float v[8];
-            load8(dy + (size_t)t * ld + col, n, wide != 0, v);
+            const bf16* p = dy + (size_t)t * ld + col;
+            if (wide && n == 8) {
+                float2 v[4];
+                Row8<bf16> w;
+                w.load(p);
+                w.get(v);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) sum[i] += v[i];
+                for (int i = 0; i < 8; ++i) sum[i] += i % 2 ? v[i / 2].y : v[i / 2].x;
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) sum[i] += i < n ? to_f(p[i]) : 0.f;
+            }
         }
 #pragma unroll
     for (int i = 0; i < 8; ++i) sh[warp][lane * 8 + i] = sum[i];
@@ -446,21 +561,32 @@ __global__ void __launch_bounds__(256) k_bias_join(const float* part, int parts,
     db[c] = accumulate ? db[c] + v : v;
 }
 
-template <typename T>
-__global__ void __launch_bounds__(256) k_activation_backward(const T* dy, size_t ld_dy, const bf16* z, size_t ld_z, uint32_t act, size_t rows, int width, int wide,
-                                                             bf16* dz, size_t ld_dz) {
+template <uint32_t kAct, typename T>
+__global__ void __launch_bounds__(256) k_activation_backward(const T* dy, size_t ld_dy, const bf16* z, size_t ld_z, size_t rows, int width, int wide, bf16* dz, size_t ld_dz) {
     pdl_wait();
     pdl_trigger();
     const size_t per_row = ((size_t)width + 7) / 8;
     for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < rows * per_row; i += (size_t)gridDim.x * 256) {
         const size_t t = i / per_row;
         const int c = (int)(i - t * per_row) * 8, n = min(8, width - c);
-        float v[8], w[8];
-        load8(dy + t * ld_dy + c, n, wide != 0, v);
-        load8(z + t * ld_z + c, n, wide != 0, w);
+        const T* p = dy + t * ld_dy + c;
+        const bf16* q = z + t * ld_z + c;
+        bf16* o = dz + t * ld_dz + c;
+        if (wide && n == 8) {
+            Row8<T> g;
+            Row8<bf16> w;
+            float2 v[4], u[4];
+            g.load(p);
+            w.load(q);
+            g.get(v);
+            w.get(u);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] *= slope(act, w[k]);
-        store8(dz + t * ld_dz + c, n, wide != 0, v);
+            for (int k = 0; k < 4; ++k) v[k] = mul2(v[k], slope<kAct>(u[k]));
+            w.put(v);
+            w.store(o);
+        } else {
+            for (int k = 0; k < n; ++k) o[k] = __float2bfloat16_rn(to_f(p[k]) * slope<kAct>(both(__bfloat162float(q[k]))).x);
+        }
     }
 }
 
@@ -513,18 +639,27 @@ cudaError_t copy_rows(const Operand& o, uint64_t to_ld, bf16* to, cudaStream_t s
                          (size_t)o.rows, to);
 }
 
-template <int kEpi, typename T>
-cudaError_t run(const CUtensorMap& ta, const CUtensorMap& tb, const LinArgs& a, cudaStream_t s) {
-    cudaError_t e = allow_smem<k_linear<kEpi, T>>();
+template <int kEpi, uint32_t kAct, typename T>
+cudaError_t run_act(const CUtensorMap& ta, const CUtensorMap& tb, const LinArgs& a, cudaStream_t s) {
+    cudaError_t e = allow_smem<k_linear<kEpi, kAct, T>>();
     if (e != cudaSuccess) return e;
     const int grid = 2 * std::min(a.whole + a.rest * a.splits, kSms / 2);
-    e = launch_cluster(k_linear<kEpi, T>, grid, 2, kThreads, sizeof(LinSmem) + 1024, s, ta, tb, a);
-    if (e == cudaSuccess && a.splits > 1) e = launch_kernel(k_linear_join<kEpi, T>, std::min(a.rest * kTM / 8, kSms * 8), 256, 0, s, false, a);
+    e = launch_cluster(k_linear<kEpi, kAct, T>, grid, 2, kThreads, sizeof(LinSmem) + 1024, s, ta, tb, a);
+    if (e == cudaSuccess && a.splits > 1) e = launch_kernel(k_linear_join<kEpi, kAct, T>, std::min(a.rest * kTM / 8, kSms * 8), 256, 0, s, false, a);
     return e;
+}
+template <int kEpi, typename T>
+cudaError_t run(uint32_t act, const CUtensorMap& ta, const CUtensorMap& tb, const LinArgs& a, cudaStream_t s) {
+    switch (act) {
+        case ABS_ACT_RELU: return run_act<kEpi, ABS_ACT_RELU, T>(ta, tb, a, s);
+        case ABS_ACT_GELU: return run_act<kEpi, ABS_ACT_GELU, T>(ta, tb, a, s);
+        case ABS_ACT_SILU: return run_act<kEpi, ABS_ACT_SILU, T>(ta, tb, a, s);
+        default: return run_act<kEpi, ABS_ACT_NONE, T>(ta, tb, a, s);
+    }
 }
 
 // The product and its epilogue; `kind`: kForward, kDgrad, kWgrad; workspace checked against `p`.
-int product(int kind, uint32_t dtype, Operand oa, Operand ob, uint64_t M, uint64_t N, uint64_t K, const LinPlan& p, LinArgs a, char* ws, cudaStream_t s) {
+int product(int kind, uint32_t act, uint32_t dtype, Operand oa, Operand ob, uint64_t M, uint64_t N, uint64_t K, const LinPlan& p, LinArgs a, char* ws, cudaStream_t s) {
     cudaError_t e = cudaSuccess;
     if (p.pack_a) {
         bf16* to = reinterpret_cast<bf16*>(ws + p.part_bytes);
@@ -545,9 +680,9 @@ int product(int kind, uint32_t dtype, Operand oa, Operand ob, uint64_t M, uint64
     a.M = (int)M; a.N = (int)N; a.K = (int)K;
     a.tiles_n = p.tiles_n; a.whole = p.whole; a.rest = p.rest; a.splits = p.splits; a.kb_per_split = p.kb_per_split;
     a.part = reinterpret_cast<float*>(ws);
-    if (kind == kForward) e = dtype == ABS_F32 ? run<kForward, float>(ta, tb, a, s) : run<kForward, bf16>(ta, tb, a, s);
-    else if (kind == kDgrad) e = dtype == ABS_F32 ? run<kDgrad, float>(ta, tb, a, s) : run<kDgrad, bf16>(ta, tb, a, s);
-    else e = run<kWgrad, float>(ta, tb, a, s);
+    if (kind == kForward) e = dtype == ABS_F32 ? run<kForward, float>(act, ta, tb, a, s) : run<kForward, bf16>(act, ta, tb, a, s);
+    else if (kind == kDgrad) e = dtype == ABS_F32 ? run<kDgrad, float>(act, ta, tb, a, s) : run<kDgrad, bf16>(act, ta, tb, a, s);
+    else e = run_act<kWgrad, ABS_ACT_NONE, float>(ta, tb, a, s);
     return e == cudaSuccess ? ABS_OK : thread_error(ABS_ECUDA, cudaGetErrorString(e));
 }
 
@@ -607,9 +742,9 @@ extern "C" int abs_linear(const void* x, uint64_t ld_x, const void* w, uint64_t 
     if (!plan_of(tokens, out, in, oa, ob, &p)) return thread_error(ABS_ELIMIT, "too many output tiles");
     if (const char* why = check_workspace(p, workspace, workspace_bytes, &code)) return thread_error(code, why);
     LinArgs a{};
-    a.out = y; a.ld = ld_y; a.bias = bias; a.res = residual; a.ld_res = ld_residual; a.z_out = static_cast<bf16*>(z); a.ld_z = ld_z; a.act = act;
+    a.out = y; a.ld = ld_y; a.bias = bias; a.res = residual; a.ld_res = ld_residual; a.z_out = static_cast<bf16*>(z); a.ld_z = ld_z;
     a.wide = rows_at(m[2], 16) && rows_at(m[3], 16) && rows_at(m[4], 16);
-    return product(kForward, dtype, oa, ob, tokens, out, in, p, a, static_cast<char*>(workspace), static_cast<cudaStream_t>(stream));
+    return product(kForward, act, dtype, oa, ob, tokens, out, in, p, a, static_cast<char*>(workspace), static_cast<cudaStream_t>(stream));
 }
 
 extern "C" size_t abs_linear_dgrad_workspace(uint64_t tokens, uint64_t in, uint64_t out, const void* dy, uint64_t ld_dy, const void* w, uint64_t ld_w) {
@@ -637,9 +772,9 @@ extern "C" int abs_linear_dgrad(const void* dy, uint64_t ld_dy, const void* w, u
     if (!plan_of(tokens, in, out, oa, ob, &p)) return thread_error(ABS_ELIMIT, "too many output tiles");
     if (const char* why = check_workspace(p, workspace, workspace_bytes, &code)) return thread_error(code, why);
     LinArgs a{};
-    a.out = dx; a.ld = ld_dx; a.res = residual; a.ld_res = ld_residual; a.z_in = static_cast<const bf16*>(z); a.ld_z = ld_z; a.act = act;
+    a.out = dx; a.ld = ld_dx; a.res = residual; a.ld_res = ld_residual; a.z_in = static_cast<const bf16*>(z); a.ld_z = ld_z;
     a.wide = rows_at(m[2], 16) && rows_at(m[3], 16) && rows_at(m[4], 16);
-    return product(kDgrad, dtype, oa, ob, tokens, in, out, p, a, static_cast<char*>(workspace), static_cast<cudaStream_t>(stream));
+    return product(kDgrad, act, dtype, oa, ob, tokens, in, out, p, a, static_cast<char*>(workspace), static_cast<cudaStream_t>(stream));
 }
 
 static bool wgrad_plan(uint64_t tokens, uint64_t in, uint64_t out, const Operand& x, const Operand& dy, LinPlan* p) {
@@ -687,7 +822,7 @@ extern "C" int abs_linear_wgrad(const void* x, uint64_t ld_x, const void* dy, ui
     }
     LinArgs a{};
     a.out = dw; a.ld = ld_dw; a.accumulate = accumulate != 0; a.wide = rows_at(m[2], 16);
-    return product(kWgrad, ABS_F32, oa, ob, in, out, tokens, p, a, static_cast<char*>(workspace), s);
+    return product(kWgrad, ABS_ACT_NONE, ABS_F32, oa, ob, in, out, tokens, p, a, static_cast<char*>(workspace), s);
 }
 
 extern "C" int abs_activation_backward(const void* dy, uint64_t ld_dy, uint32_t dtype, const void* z, uint64_t ld_z, uint32_t act, uint64_t tokens, uint64_t width,
@@ -704,9 +839,15 @@ extern "C" int abs_activation_backward(const void* dy, uint64_t ld_dy, uint32_t 
     const int wide = rows_at(m[0], 16) && rows_at(m[1], 16) && rows_at(m[2], 16);
     const size_t want = ((size_t)tokens * ((width + 7) / 8) + 511) / 512;
     const int grid = (int)std::min<size_t>(want, kSms * 8);
-    const cudaError_t e = dtype == ABS_F32 ? launch_kernel(k_activation_backward<float>, grid, 256, 0, s, true, static_cast<const float*>(dy), (size_t)ld_dy, static_cast<const bf16*>(z),
-                                                           (size_t)ld_z, act, (size_t)tokens, (int)width, wide, static_cast<bf16*>(dz), (size_t)ld_dz)
-                                           : launch_kernel(k_activation_backward<bf16>, grid, 256, 0, s, true, static_cast<const bf16*>(dy), (size_t)ld_dy, static_cast<const bf16*>(z),
-                                                           (size_t)ld_z, act, (size_t)tokens, (int)width, wide, static_cast<bf16*>(dz), (size_t)ld_dz);
+    auto go = [&](auto kernel, auto zero) {
+        return launch_kernel(kernel, grid, 256, 0, s, true, static_cast<const decltype(zero)*>(dy), (size_t)ld_dy, static_cast<const bf16*>(z), (size_t)ld_z, (size_t)tokens,
+                             (int)width, wide, static_cast<bf16*>(dz), (size_t)ld_dz);
+    };
+    auto with = [&](auto zero) {
+        using T = decltype(zero);
+        return act == ABS_ACT_RELU ? go(k_activation_backward<ABS_ACT_RELU, T>, zero) : act == ABS_ACT_GELU ? go(k_activation_backward<ABS_ACT_GELU, T>, zero)
+             : act == ABS_ACT_SILU ? go(k_activation_backward<ABS_ACT_SILU, T>, zero) : go(k_activation_backward<ABS_ACT_NONE, T>, zero);
+    };
+    const cudaError_t e = dtype == ABS_F32 ? with(0.f) : with(bf16());
     return e == cudaSuccess ? ABS_OK : thread_error(ABS_ECUDA, cudaGetErrorString(e));
 }
