@@ -222,7 +222,7 @@ int abs_activation_backward(const void *dy, uint64_t ld_dy, uint32_t dtype, cons
  *   offsets [seqs + 1] int32 on the device, ascending, values outside [0, tokens] are clamped; empty sequences are allowed.
  *   NULL: one sequence of all rows (seqs = 1).
  *   h0, last [seqs, width] fp32, packed; last out (NULL: not wanted): h behind the last row (of an empty sequence h0).  last may be h0.
- * tokens, width and seqs up to 2^31 - 1024 (ABS_ELIMIT).  workspace: abs_recurrence_workspace(tokens, width) bytes, may be 0.  The kernel's waits
+ * tokens, width and seqs up to 2^31 - 1024, tiles of 32 rows and 64 columns likewise (ABS_ELIMIT).  workspace: abs_recurrence_workspace(tokens, width) bytes, may be 0.  The kernel's waits
  * are bounded; see abs_llm_check. */
 size_t abs_recurrence_workspace(uint64_t tokens, uint64_t width);
 int abs_recurrence(const void *x, uint64_t ld_x, const void *g, uint64_t ld_g, const int32_t *offsets, uint64_t seqs, const float *h0,

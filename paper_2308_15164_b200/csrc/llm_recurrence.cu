@@ -12,17 +12,29 @@
 
 #include "abs_internal.h"
 #include "abs_llm.h"
-#include "bulk_copy.cuh"
 #include "llm_host.h"
 #include "llm_status.cuh"
 #include "row_ops.cuh"
+#include "tcgen05.cuh"
 
 namespace abs_sgd {
 namespace {
 
-constexpr int kWarps = 8, kRows = 16, kTile = kWarps * kRows;   // rows of a warp, of a CTA
-constexpr int kGroup = 32;               // tiles between two published states
+constexpr int kWarps = 8, kCols = 64;    // of a tile; a lane owns two columns
+constexpr int kGroupMax = 32;
+constexpr int kSms = 148;
 constexpr uint64_t kSizeMax = 0x7ffffc00ull;
+// Rows of a warp: 32 KB of inputs for a tile (two matrices forward, four backward).
+template <typename T, bool kBack>
+constexpr int kRowsOf = (kBack ? 8 : 16) * 2 / (int)sizeof(T);
+template <typename T, bool kBack>
+constexpr int kTileOf = kWarps * kRowsOf<T, kBack>;
+template <bool kBack>
+constexpr int kStagesOf = kBack ? 2 : 3;
+template <bool kBack>
+constexpr int kCtasOf = kBack ? 3 : 2;   // of an SM
+constexpr int kTileMin = kTileOf<float, true>;
+constexpr int kStageBytes = 32768;
 
 struct RecArgs {
     const void *x, *g, *dy, *y;          // y: of the forward pass (backward only)
@@ -33,24 +45,26 @@ struct RecArgs {
     const float *h0, *before;            // before: h0, backward dlast: the state in front of a sequence in scan order
     float* after;                        // last, backward dh0
     int T, D, seqs;
-    int tiles, strips;
+    int tiles, strips, group;
+    int pairs;                           // a lane's two columns are aligned to two elements in every matrix
     uint32_t* ctl;                       // [0]: tickets; then a flag per (tile, strip)
-    float2* maps;                        // [tile][strip][lanes' columns]: a tile's map (A, B), or (0, state) for the last of a group
+    float4* maps;                        // [tile][strip][lane]: a tile's map (A, B) for two columns, or (-0, state) for the last of a group
 };
 
 // sigmoid(g) and 1 - sigmoid(g), each to its own precision.
-__device__ __forceinline__ void gate_of(float g, float& a, float& rest, bf16) {
-    float v = g * -1.4426950408889634f;
-    v = v > 126.f ? 126.f : v;           // keeps a NaN
-    const float e = exp2_of(v);
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(a) : "f"(1.f + e));
-    rest = e * a;
+__device__ __forceinline__ void gate_of(float2 g, float2& a, float2& rest, bf16) {
+    float2 v = mul2(g, both(-1.4426950408889634f));
+    v.x = v.x > 126.f ? 126.f : v.x;     // keeps a NaN
+    v.y = v.y > 126.f ? 126.f : v.y;
+    const float2 e = exp2_of(v), d = add2(e, both(1.f));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(a.x) : "f"(d.x));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(a.y) : "f"(d.y));
+    rest = mul2(e, a);
 }
-__device__ __forceinline__ void gate_of(float g, float& a, float& rest, float) {
-    const float v = g < -87.f ? 87.f : -g;
-    const float e = expf(v);
-    a = 1.f / (1.f + e);
-    rest = e * a;
+__device__ __forceinline__ void gate_of(float2 g, float2& a, float2& rest, float) {
+    const float2 e = make_float2(expf(g.x < -87.f ? 87.f : -g.x), expf(g.y < -87.f ? 87.f : -g.y));
+    a = make_float2(1.f / (1.f + e.x), 1.f / (1.f + e.y));
+    rest = mul2(e, a);
 }
 __device__ __forceinline__ bool forgets(float A) { return __float_as_uint(A) == 0x80000000u; }
 // (A, B) followed by (A2, B2).
@@ -64,38 +78,30 @@ __device__ __forceinline__ void compose(float& A, float& B, float A2, float B2) 
     }
 }
 __device__ __forceinline__ float apply(float A, float B, float s) { return forgets(A) ? B : fmaf(A, s, B); }
-
-template <typename T, int kV>
-__device__ __forceinline__ void load_v(const T* p, int n, float (&v)[kV]) {
-    if (kV == 2 && n == 2) {
-        if constexpr (sizeof(T) == 2) {
-            const uint32_t w = *reinterpret_cast<const uint32_t*>(p);
-            v[0] = __uint_as_float(w << 16);
-            v[kV - 1] = __uint_as_float(w & 0xFFFF0000u);
-        } else {
-            const float2 f = *reinterpret_cast<const float2*>(p);
-            v[0] = f.x;
-            v[kV - 1] = f.y;
-        }
-        return;
-    }
-#pragma unroll
-    for (int i = 0; i < kV; ++i) v[i] = i < n ? to_f(p[i]) : 0.f;
+__device__ __forceinline__ void compose2(float4& m, float4 then) {
+    compose(m.x, m.y, then.x, then.y);
+    compose(m.z, m.w, then.z, then.w);
 }
-template <typename T, int kV>
-__device__ __forceinline__ void store_v(T* p, int n, const float (&v)[kV]) {
-    if (kV == 2 && n == 2) {
-        if constexpr (sizeof(T) == 2) {
-            const __nv_bfloat162 b = __floats2bfloat162_rn(v[0], v[kV - 1]);
-            *reinterpret_cast<__nv_bfloat162*>(p) = b;
-        } else {
-            *reinterpret_cast<float2*>(p) = make_float2(v[0], v[kV - 1]);
-        }
-        return;
-    }
-#pragma unroll
-    for (int i = 0; i < kV; ++i)
-        if (i < n) p[i] = from_f<T>(v[i]);
+__device__ __forceinline__ float2 apply2(float4 m, float2 s) { return make_float2(apply(m.x, m.y, s.x), apply(m.z, m.w, s.y)); }
+
+// Two elements from shared or aligned global memory; n of two elements at any address.
+__device__ __forceinline__ float2 pair_of(const float* p) { return *reinterpret_cast<const float2*>(p); }
+__device__ __forceinline__ float2 pair_of(const bf16* p) {
+    const uint32_t w = *reinterpret_cast<const uint32_t*>(p);
+    return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u));
+}
+template <typename T>
+__device__ __forceinline__ float2 load2(const T* p, int n, bool aligned) {
+    if (n == 2 && aligned) return pair_of(p);
+    return make_float2(n > 0 ? to_f(p[0]) : 0.f, n > 1 ? to_f(p[1]) : 0.f);
+}
+__device__ __forceinline__ void put_pair(float* p, float2 v) { *reinterpret_cast<float2*>(p) = v; }
+__device__ __forceinline__ void put_pair(bf16* p, float2 v) { *reinterpret_cast<__nv_bfloat162*>(p) = __float22bfloat162_rn(v); }
+template <typename T>
+__device__ __forceinline__ void store2(T* p, int n, bool aligned, float2 v) {
+    if (n == 2 && aligned) return put_pair(p, v);
+    if (n > 0) p[0] = from_f<T>(v.x);
+    if (n > 1) p[1] = from_f<T>(v.y);
 }
 
 // Which sequence row t belongs to: the number of sequences that end at or before it.
@@ -110,234 +116,264 @@ __device__ __forceinline__ int sequence_of(const RecArgs& a, int t) {
     return lo;
 }
 
-// A tile: kTile rows (in scan order: backward from the last one) of 32 kV columns; a lane owns kV columns, a warp kRows rows.
-template <typename T, int kV, uint32_t kKind, bool kBack>
-__global__ void __launch_bounds__(kWarps * 32) k_recurrence(const __grid_constant__ RecArgs a) {
-    __shared__ float2 sh_map[kWarps][32 * kV];
-    __shared__ float sh_state[32 * kV];
-    __shared__ int sh_ticket;
-    __shared__ int sh_ok;
+struct RecSmem {
+    alignas(16) float4 map[2][kWarps][32];       // of a warp's rows, by the tile's parity
+    float4 look[kWarps][32];                     // of the tiles in front, a run of them for each warp
+    alignas(8) uint64_t full[3];
+    int ticket[4];
+    uint32_t copies[4];                          // into each stage so far
+    int load_failed, look_failed;
+};
+
+constexpr size_t kRecSmem = (sizeof(RecSmem) + 127) / 128 * 128;
+
+// A tile: kTileOf rows (in scan order: backward from the last one) of 64 columns.  A CTA takes tiles by ticket, tiles of all strips at the
+// same rows before the next rows, so that whoever waits for a tile in front waits for one that a running CTA has.
+//   1. a lane reads its rows of two columns, forms the gates, and the map of its warp's rows
+//   2. the warps' maps give the tile's map, which is published; the state in front of the tile is that behind the last tile of the group
+//      in front (published as such), followed by the maps of the group's tiles so far: always the same tiles in the same order, so
+//      that equal inputs give equal bits whoever comes first
+//   3. a lane goes over its rows again from their state
+// kTma: the tiles that a CTA takes next are copied to shared memory meanwhile.  Otherwise (rows that are not 16-byte aligned) the lanes read memory.
+template <typename T, uint32_t kKind, bool kBack, bool kTma>
+__global__ void __launch_bounds__(kWarps * 32, kCtasOf<kBack>) k_recurrence(const __grid_constant__ RecArgs a, const __grid_constant__ CUtensorMap tm_g,
+                                                                            const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_dy,
+                                                                            const __grid_constant__ CUtensorMap tm_y) {
+    constexpr int kRows = kRowsOf<T, kBack>, kTile = kTileOf<T, kBack>, kStages = kStagesOf<kBack>, kInputs = kBack ? 4 : 2;
+    constexpr int kInput = kTile * kCols * (int)sizeof(T);       // bytes of an input's tile
+    static_assert(kInput * kInputs == kStageBytes, "");
+    enum { kG, kX, kDy, kY };
+    extern __shared__ uint8_t raw[];
+    RecSmem& s = *reinterpret_cast<RecSmem*>((reinterpret_cast<uintptr_t>(raw) + 127) & ~(uintptr_t)127);
+    uint8_t* const ring = reinterpret_cast<uint8_t*>(&s) + kRecSmem;
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const int total = a.tiles * a.strips;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < kStages; ++i) {
+            mbar_init(&s.full[i], 1);
+            s.copies[i] = 0;
+        }
+        s.load_failed = s.look_failed = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
     pdl_wait();
     pdl_trigger();
+    // thread 0: the next tile, and its copies
+    int coming = 0;                                              // thread 0: a ticket taken, not yet used
+    auto take = [&]() { return a.ctl ? (int)atomicAdd(&a.ctl[0], 1u) : coming + (int)gridDim.x; };
+    auto start = [&](int stage) {
+        s.ticket[stage] = coming;
+        if (coming >= total) return;
+        if constexpr (kTma) {
+            const int u0 = coming / a.strips * kTile, c = coming % a.strips * kCols;
+            const int t = kBack ? a.T - u0 - kTile : u0;         // a first row below 0 reads zeros
+            uint8_t* to = ring + stage * kStageBytes;
+            mbar_expect_tx(&s.full[stage], kStageBytes);
+            ++s.copies[stage];
+            tma_load_2d(to + kG * kInput, &tm_g, c, t, &s.full[stage]);
+            tma_load_2d(to + kX * kInput, &tm_x, c, t, &s.full[stage]);
+            if constexpr (kBack) {
+                tma_load_2d(to + kDy * kInput, &tm_dy, c, t, &s.full[stage]);
+                tma_load_2d(to + kY * kInput, &tm_y, c, t - 1, &s.full[stage]);
+            }
+        }
+        coming = take();
+    };
     if (threadIdx.x == 0) {
-        sh_ticket = a.tiles > 1 ? (int)atomicAdd(&a.ctl[0], 1u) : blockIdx.x;
-        sh_ok = 1;
+        coming = a.ctl ? take() : (int)blockIdx.x;
+        for (int i = 0; i < kStages; ++i) start(i);
     }
     __syncthreads();
-    const int tile = sh_ticket / a.strips, strip = sh_ticket % a.strips;
-    const int c = (strip * 32 + lane) * kV, n = min(max(a.D - c, 0), kV);
-    const int u0 = tile * kTile + warp * kRows;          // first row of the warp, in scan order
-    auto row = [&](int u) { return kBack ? a.T - 1 - u : u; };
 
-    // ---- rows
-    float keep[kRows][kV], feed[kRows][kV];              // a; b, backward dy
-    float rest[kBack ? kRows : 1][kV], other[kBack ? kRows : 1][kV];   // 1 - a; h_{t-1} (- x)
-    int seq = 0;
-    uint32_t member, first, final;                       // of the warp's rows: in a sequence; first and last one in scan order
-    {
-        bool m = false, f = false, l = false;
-        if (lane < kRows && u0 + lane < a.T) {
-            const int t = row(u0 + lane);
-            seq = sequence_of(a, t);
-            m = seq < a.seqs && t >= begin_of(a, seq);
-            if (m) {
-                f = t == begin_of(a, seq);
-                l = t == begin_of(a, seq + 1) - 1;
+    int stage = 0, n_tile = 0;
+    uint32_t phase = 0;
+    for (;;) {
+        const int mine = s.ticket[stage];
+        if (mine >= total) break;
+        const int tile = mine / a.strips, strip = mine % a.strips;
+        const int c = strip * kCols + lane * 2, n = min(max(a.D - c, 0), 2);
+        const int u0 = tile * kTile + warp * kRows;              // first row of the warp, in scan order
+        auto row = [&](int r) { return kBack ? a.T - 1 - (u0 + r) : u0 + r; };
+        // ---- which rows are in a sequence, and are the first and last one in scan order
+        int seq = 0;
+        uint32_t member, first, final;
+        {
+            bool m = false, f = false, l = false;
+            if (lane < kRows && u0 + lane < a.T) {
+                const int t = row(lane);
+                seq = sequence_of(a, t);
+                const int from = seq < a.seqs ? begin_of(a, seq) : a.T;
+                m = t >= from;
+                f = m && t == from;
+                l = m && t == begin_of(a, seq + 1) - 1;
             }
+            member = __ballot_sync(0xffffffffu, m);
+            first = __ballot_sync(0xffffffffu, kBack ? l : f);
+            final = __ballot_sync(0xffffffffu, kBack ? f : l);
         }
-        member = __ballot_sync(0xffffffffu, m);
-        first = __ballot_sync(0xffffffffu, kBack ? l : f);
-        final = __ballot_sync(0xffffffffu, kBack ? f : l);
-    }
-#pragma unroll
-    for (int r = 0; r < kRows; ++r) {
-        float gv[kV], xv[kV], dv[kV], hv[kV];
-#pragma unroll
-        for (int i = 0; i < kV; ++i) gv[i] = xv[i] = dv[i] = hv[i] = 0.f;
-        const bool in = (member >> r & 1) != 0;
-        if (in && n > 0) {
-            const size_t t = (size_t)row(u0 + r);
-            load_v<T, kV>(static_cast<const T*>(a.g) + t * a.ld_g + c, n, gv);
-            load_v<T, kV>(static_cast<const T*>(a.x) + t * a.ld_x + c, n, xv);
-            if (kBack) {
-                load_v<T, kV>(static_cast<const T*>(a.dy) + t * a.ld_dy + c, n, dv);
-                if (!(final >> r & 1)) load_v<T, kV>(static_cast<const T*>(a.y) + (t - 1) * a.ld_y + c, n, hv);
-            }
-        }
-        if (kBack && (final >> r & 1) && a.h0) {
-            const int q = __shfl_sync(0xffffffffu, seq, r);
-#pragma unroll
-            for (int i = 0; i < kV; ++i)
-                if (i < n) hv[i] = a.h0[(size_t)q * a.D + c + i];
-        }
-        // the state in front of a sequence goes into its first row's input: read once, since `after` may be `before`
-        float init[kV];
-#pragma unroll
-        for (int i = 0; i < kV; ++i) init[i] = 0.f;
-        if ((first >> r & 1) && a.before) {
-            const int q = __shfl_sync(0xffffffffu, seq, r);
-#pragma unroll
-            for (int i = 0; i < kV; ++i)
-                if (i < n) init[i] = a.before[(size_t)q * a.D + c + i];
-        }
-#pragma unroll
-        for (int i = 0; i < kV; ++i) {
-            float k, z;
-            gate_of(gv[i], k, z, T());
-            keep[r][i] = in ? k : 1.f;
-            if (kBack) {
-                feed[r][i] = dv[i] + init[i];
-                rest[r % (kBack ? kRows : 1)][i] = z;
-                other[r % (kBack ? kRows : 1)][i] = kKind == ABS_RECURRENCE_BLEND ? hv[i] - xv[i] : hv[i];
+        // two columns of the r-th row of an input; not for rows of no sequence
+        auto fetch = [&](int which, int r) {
+            if constexpr (kTma) {
+                const int at = kBack ? kTile - 1 - (warp * kRows + r) : warp * kRows + r;
+                return pair_of(reinterpret_cast<const T*>(ring + stage * kStageBytes + which * kInput) + at * kCols + lane * 2);
             } else {
-                feed[r][i] = !in ? 0.f : kKind == ABS_RECURRENCE_BLEND ? xv[i] * z : xv[i];
-                if (first >> r & 1) feed[r][i] = fmaf(k, init[i], feed[r][i]);
+                const void* p = which == kG ? a.g : which == kX ? a.x : which == kDy ? a.dy : a.y;
+                const size_t ld = which == kG ? a.ld_g : which == kX ? a.ld_x : which == kDy ? a.ld_dy : a.ld_y;
+                return load2(static_cast<const T*>(p) + (size_t)(row(r) - (which == kY)) * ld + c, n, a.pairs != 0);
             }
-        }
-    }
-    // ---- the warp's map, then what is in front of the warp within the tile
-    float A[kV], B[kV];
+        };
+        auto given = [&](const float* p, int r) {                // two columns of the r-th row's sequence in a state
+            const int q = __shfl_sync(0xffffffffu, seq, r);
+            const float* f = p + (size_t)q * a.D + c;
+            return make_float2(n > 0 ? f[0] : 0.f, n > 1 ? f[1] : 0.f);
+        };
+        if (kTma && !mbar_wait(&s.full[stage], phase)) s.load_failed = 1;
+
+        // ---- 1
+        float2 keep[kRows], feed[kRows];                         // a; forward b, backward 1 - a
+        float4 m = make_float4(1.f, 0.f, 1.f, 0.f);
 #pragma unroll
-    for (int i = 0; i < kV; ++i) {
-        A[i] = 1.f;
-        B[i] = 0.f;
-    }
-#pragma unroll
-    for (int r = 0; r < kRows; ++r) {
-        if (first >> r & 1)
-#pragma unroll
-            for (int i = 0; i < kV; ++i) {
-                A[i] = -0.f;
-                B[i] = 0.f;
+        for (int r = 0; r < kRows; ++r) {
+            const bool in = (member >> r & 1) != 0;
+            float2 gv = both(0.f), v = both(0.f), z;             // v: x, backward dy
+            if (in) {
+                gv = fetch(kG, r);
+                v = fetch(kBack ? kDy : kX, r);
             }
-#pragma unroll
-        for (int i = 0; i < kV; ++i) {
-            B[i] = kBack ? keep[r][i] * (B[i] + feed[r][i]) : fmaf(keep[r][i], B[i], feed[r][i]);
-            A[i] *= keep[r][i];
-        }
-    }
-#pragma unroll
-    for (int i = 0; i < kV; ++i) sh_map[warp][lane * kV + i] = make_float2(A[i], B[i]);
-    __syncthreads();
-    float s[kV];                                         // state in front of the tile
-#pragma unroll
-    for (int i = 0; i < kV; ++i) s[i] = 0.f;
-    if (a.tiles > 1) {
-        constexpr int kCols = 32 * kV;
-        uint32_t* flags = a.ctl + 1;
-        if (warp == 0) {
-            const bool closes = tile % kGroup == kGroup - 1;
-            float P[kV], Q[kV];
-#pragma unroll
-            for (int i = 0; i < kV; ++i) {
-                P[i] = 1.f;
-                Q[i] = 0.f;
-            }
-#pragma unroll
-            for (int w = 0; w < kWarps; ++w)
-#pragma unroll
-                for (int i = 0; i < kV; ++i) {
-                    const float2 m = sh_map[w][lane * kV + i];
-                    compose(P[i], Q[i], m.x, m.y);
+            gate_of(gv, keep[r], z, T());
+            if (!in) keep[r] = both(1.f);
+            if (first >> r & 1) {
+                m = make_float4(-0.f, 0.f, -0.f, 0.f);
+                if (a.before) {                                  // read once and here: `after` may be `before`
+                    const float2 i = given(a.before, r);
+                    m.y = i.x;
+                    m.w = i.y;
                 }
+            }
+            float2 B = make_float2(m.y, m.w);
+            if (kBack) {
+                feed[r] = (first >> r & 1) ? B : z;              // a first row's 1 - a is formed again
+                B = mul2(keep[r], add2(B, v));
+            } else {
+                feed[r] = !in ? both(0.f) : kKind == ABS_RECURRENCE_BLEND ? mul2(v, z) : v;
+                if (first >> r & 1) feed[r] = fma2(keep[r], B, feed[r]);
+                B = (first >> r & 1) ? feed[r] : fma2(keep[r], B, feed[r]);
+            }
+            m = make_float4(m.x * keep[r].x, B.x, m.z * keep[r].y, B.y);
+        }
+        s.map[n_tile & 1][warp][lane] = m;
+        __syncthreads();
+        if (s.load_failed) break;
+        // forward the tile's image has been read, backward that of the tile before
+        if (threadIdx.x == 0) {
+            if (!kBack) start(stage);
+            else if (n_tile > 0) start(stage ^ 1);
+        }
+        // ---- 2
+        float2 state = both(0.f);
+        if (a.tiles > 1) {
+            uint32_t* flags = a.ctl + 1;
+            const bool closes = tile % a.group == a.group - 1;
+            float4 whole = make_float4(1.f, 0.f, 1.f, 0.f);
             auto publish = [&]() {
-                float2* p = a.maps + ((size_t)tile * a.strips + strip) * kCols + lane * kV;
-#pragma unroll
-                for (int i = 0; i < kV; ++i) p[i] = make_float2(P[i], Q[i]);
+                a.maps[((size_t)tile * a.strips + strip) * 32 + lane] = whole;
                 __threadfence();
                 __syncwarp();
                 if (lane == 0) asm volatile("st.release.gpu.global.u32 [%0], %1;" ::"l"(flags + (size_t)tile * a.strips + strip), "r"(1u) : "memory");
             };
-            if (!closes) publish();
-            // the state behind the last group, then the maps of the tiles since, in order
-            const int from = max(tile / kGroup * kGroup - 1, 0), count = tile - from;
+            if (warp == 0) {
+#pragma unroll
+                for (int w = 0; w < kWarps; ++w) compose2(whole, s.map[n_tile & 1][w][lane]);
+                if (!closes) publish();
+            }
+            const int from = max(tile / a.group * a.group - 1, 0), count = tile - from, per = (count + kWarps - 1) / kWarps;
+            constexpr int kPer = (kGroupMax + kWarps - 1) / kWarps;
+            const int k0 = from + warp * per, k1 = min(k0 + per, tile);
             bool ok = true;
-            if (lane < count) {
-                const uint32_t* f = flags + (size_t)(from + lane) * a.strips + strip;
-                uint32_t seen = 0, it = 0;
-                while (it++ < kSpinLimit) {
-                    asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(seen) : "l"(f) : "memory");
-                    if (seen) break;
-                }
+            if (k0 + lane < k1) {
+                const uint32_t* f = flags + (size_t)(k0 + lane) * a.strips + strip;
+                uint32_t seen = 0;
+                for (uint32_t it = 0; it < kSpinLimit && !seen; ++it) asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(seen) : "l"(f) : "memory");
                 ok = seen != 0;
             }
-            ok = __all_sync(0xffffffffu, ok);
-            if (ok) {
-                for (int k = 0; k < count; ++k) {
-                    const float2* p = a.maps + ((size_t)(from + k) * a.strips + strip) * kCols + lane * kV;
+            if (__all_sync(0xffffffffu, ok)) {
+                float4 v[kPer], run = make_float4(1.f, 0.f, 1.f, 0.f);
 #pragma unroll
-                    for (int i = 0; i < kV; ++i) {
-                        const float2 m = __ldcg(p + i);
-                        s[i] = apply(m.x, m.y, s[i]);
-                    }
-                }
-                if (closes) {
+                for (int k = 0; k < kPer; ++k)
+                    if (k0 + k < k1) v[k] = __ldcg(a.maps + ((size_t)(k0 + k) * a.strips + strip) * 32 + lane);
 #pragma unroll
-                    for (int i = 0; i < kV; ++i) {
-                        Q[i] = apply(P[i], Q[i], s[i]);
-                        P[i] = -0.f;
-                    }
-                    publish();
-                }
-            } else if (lane == 0) {
-                report_timeout();
-                sh_ok = 0;
-            }
-#pragma unroll
-            for (int i = 0; i < kV; ++i) sh_state[lane * kV + i] = s[i];
-        }
-        __syncthreads();
-        if (!sh_ok) return;
-#pragma unroll
-        for (int i = 0; i < kV; ++i) s[i] = sh_state[lane * kV + i];
-    }
-    for (int w = 0; w < warp; ++w)
-#pragma unroll
-        for (int i = 0; i < kV; ++i) {
-            const float2 m = sh_map[w][lane * kV + i];
-            s[i] = apply(m.x, m.y, s[i]);
-        }
-    // ---- the rows from their state
-#pragma unroll
-    for (int r = 0; r < kRows; ++r) {
-        if (first >> r & 1)
-#pragma unroll
-            for (int i = 0; i < kV; ++i) s[i] = 0.f;
-        const bool in = (member >> r & 1) != 0;
-        float o[kV], o2[kV];
-#pragma unroll
-        for (int i = 0; i < kV; ++i) {
-            if (kBack) {
-                const float d = s[i] + feed[r][i], z = rest[r % (kBack ? kRows : 1)][i];
-                s[i] = keep[r][i] * d;
-                o[i] = kKind == ABS_RECURRENCE_BLEND ? z * d : d;
-                o2[i] = s[i] * z * other[r % (kBack ? kRows : 1)][i];
+                for (int k = 0; k < kPer; ++k)
+                    if (k0 + k < k1) compose2(run, v[k]);
+                s.look[warp][lane] = run;
             } else {
-                s[i] = fmaf(keep[r][i], s[i], feed[r][i]);
-                o[i] = s[i];
+                s.look_failed = 1;
             }
-            if (!in) o[i] = o2[i] = 0.f;
-        }
-        if (n > 0 && u0 + r < a.T) {
-            const size_t t = (size_t)row(u0 + r);
-            store_v<T, kV>(static_cast<T*>(a.out) + t * a.ld_out + c, n, o);
-            if (kBack) store_v<T, kV>(static_cast<T*>(a.out2) + t * a.ld_out2 + c, n, o2);
-        }
-        if ((final >> r & 1) && a.after) {
-            const int q = __shfl_sync(0xffffffffu, seq, r);
+            __syncthreads();
+            if (s.look_failed) break;
 #pragma unroll
-            for (int i = 0; i < kV; ++i)
-                if (i < n) a.after[(size_t)q * a.D + c + i] = s[i];
+            for (int w = 0; w < kWarps; ++w)
+                if (w * per < count) state = apply2(s.look[w][lane], state);
+            if (closes && warp == 0) {
+                const float2 end = apply2(whole, state);
+                whole = make_float4(-0.f, end.x, -0.f, end.y);
+                publish();
+            }
+        }
+        if (kBack && a.tiles == 1) __syncthreads();              // the next tile's ticket
+        for (int w = 0; w < warp; ++w) state = apply2(s.map[n_tile & 1][w][lane], state);
+        // ---- 3
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) {
+            const bool in = (member >> r & 1) != 0;
+            float2 o = both(0.f), o2 = both(0.f);
+            if (kBack) {
+                if (first >> r & 1) {
+                    float2 k;
+                    state = feed[r];
+                    gate_of(fetch(kG, r), k, feed[r], T());
+                }
+                if (in) {
+                    float2 h = both(0.f);
+                    if (!(final >> r & 1)) h = fetch(kY, r);
+                    if ((final >> r & 1) && a.h0) h = given(a.h0, r);
+                    const float2 d = add2(state, fetch(kDy, r)), z = feed[r];
+                    state = mul2(keep[r], d);
+                    o = kKind == ABS_RECURRENCE_BLEND ? mul2(z, d) : d;
+                    if (kKind == ABS_RECURRENCE_BLEND) h = fma2(fetch(kX, r), both(-1.f), h);
+                    o2 = mul2(mul2(state, z), h);
+                }
+            } else {
+                state = (first >> r & 1) ? feed[r] : fma2(keep[r], state, feed[r]);
+                if (in) o = state;
+            }
+            if (n > 0 && u0 + r < a.T) {
+                const size_t t = (size_t)row(r);
+                store2(static_cast<T*>(a.out) + t * a.ld_out + c, n, a.pairs != 0, o);
+                if (kBack) store2(static_cast<T*>(a.out2) + t * a.ld_out2 + c, n, a.pairs != 0, o2);
+            }
+            if ((final >> r & 1) && a.after) {
+                const int q = __shfl_sync(0xffffffffu, seq, r);
+                float* p = a.after + (size_t)q * a.D + c;
+                if (n > 0) p[0] = state.x;
+                if (n > 1) p[1] = state.y;
+            }
+        }
+        // ---- sequences without rows
+        if (tile == 0 && a.after && (a.T == 0 || a.offsets))
+            for (int q = warp; q < a.seqs; q += kWarps)
+                if (begin_of(a, q + 1) <= begin_of(a, q))
+                    for (int i = 0; i < n; ++i) a.after[(size_t)q * a.D + c + i] = a.before ? a.before[(size_t)q * a.D + c + i] : 0.f;
+        ++n_tile;
+        if (++stage == kStages) {
+            stage = 0;
+            phase ^= 1u;
         }
     }
-    // ---- sequences without rows
-    if (tile == 0 && a.after && (a.T == 0 || a.offsets))
-        for (int q = warp; q < a.seqs; q += kWarps)
-            if (begin_of(a, q + 1) <= begin_of(a, q))
-#pragma unroll
-                for (int i = 0; i < kV; ++i)
-                    if (i < n) a.after[(size_t)q * a.D + c + i] = a.before ? a.before[(size_t)q * a.D + c + i] : 0.f;
+    if (threadIdx.x == 0 && (s.load_failed || s.look_failed)) {
+        report_timeout();
+        for (int i = 0; i < kStages; ++i)                        // copies in flight land before the CTA's shared memory is released
+            if (s.copies[i]) mbar_wait(&s.full[i], (s.copies[i] - 1) & 1u, 4096u);
+    }
 }
 
 template <typename T, uint32_t kKind>
@@ -348,9 +384,9 @@ __global__ void __launch_bounds__(256) k_recurrence_step(const T* x, size_t ld_x
     for (size_t t = blockIdx.y; t < rows; t += gridDim.y) {
         const int c = blockIdx.x * 256 + threadIdx.x;
         if (c >= D) return;
-        float a, z;
-        gate_of(to_f(g[t * ld_g + c]), a, z, T());
-        const float v = to_f(x[t * ld_x + c]), s = fmaf(a, h[t * D + c], kKind == ABS_RECURRENCE_BLEND ? z * v : v);
+        float2 a, z;
+        gate_of(both(to_f(g[t * ld_g + c])), a, z, T());
+        const float v = to_f(x[t * ld_x + c]), s = fmaf(a.x, h[t * D + c], kKind == ABS_RECURRENCE_BLEND ? z.x * v : v);
         out[t * D + c] = s;
         y[t * ld_y + c] = from_f<T>(s);
     }
@@ -358,14 +394,47 @@ __global__ void __launch_bounds__(256) k_recurrence_step(const T* x, size_t ld_x
 
 size_t flags_bytes(uint64_t tiles, uint64_t strips) { return up256((1 + tiles * strips) * 4); }
 
-template <typename T, int kV, uint32_t kKind>
-cudaError_t run_tiles(const RecArgs& a, bool back, cudaStream_t s) {
-    return launch_kernel(back ? k_recurrence<T, kV, kKind, true> : k_recurrence<T, kV, kKind, false>, dim3((unsigned)(a.tiles * a.strips)), kWarps * 32, 0, s, a.tiles == 1, a);
+// An input's tiles: kTile rows of 64 columns, as they lie.
+bool encode_tiles(CUtensorMap* tm, const void* p, size_t ld, size_t es, const RecArgs& a, int rows) {
+    const EncodeTiledFn enc = get_encode();
+    if (!enc) return false;
+    const cuuint64_t dims[2] = {(cuuint64_t)a.D, (cuuint64_t)a.T}, strides[1] = {ld * es};
+    const cuuint32_t box[2] = {kCols, (cuuint32_t)rows}, one[2] = {1, 1};
+    return enc(tm, es == 4 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(p), dims, strides, box, one,
+               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <typename T, uint32_t kKind, bool kBack>
+cudaError_t run_tiles(RecArgs a, bool tma, char* workspace, cudaStream_t s) {
+    constexpr int kTile = kTileOf<T, kBack>;
+    a.tiles = std::max(1, (a.T + kTile - 1) / kTile);
+    a.strips = (a.D + kCols - 1) / kCols;
+    // the chain of published states takes some 2.5 us a link: a group's tiles of all strips have to keep the memory busy for that long
+    a.group = std::min(std::max(331 / a.strips, 1), kGroupMax);
+    if (a.tiles > 1) {
+        const size_t flags = flags_bytes(a.tiles, a.strips);
+        a.ctl = reinterpret_cast<uint32_t*>(workspace);
+        a.maps = reinterpret_cast<float4*>(workspace + flags);
+        const cudaError_t e = cudaMemsetAsync(workspace, 0, flags, s);
+        if (e != cudaSuccess) return e;
+    }
+    const int grid = std::min(a.tiles * a.strips, kSms * kCtasOf<kBack>);
+    CUtensorMap g{}, x{}, dy{}, y{};
+    if (!tma) return launch_kernel(k_recurrence<T, kKind, kBack, false>, grid, kWarps * 32, kRecSmem + 128, s, a.tiles == 1, a, g, x, dy, y);
+    bool ok = encode_tiles(&g, a.g, a.ld_g, sizeof(T), a, kTile) && encode_tiles(&x, a.x, a.ld_x, sizeof(T), a, kTile);
+    if (kBack) ok = ok && encode_tiles(&dy, a.dy, a.ld_dy, sizeof(T), a, kTile) && encode_tiles(&y, a.y, a.ld_y, sizeof(T), a, kTile);
+    if (!ok) return cudaErrorInvalidValue;
+    const cudaError_t e = allow_smem<k_recurrence<T, kKind, kBack, true>>();
+    if (e != cudaSuccess) return e;
+    return launch_kernel(k_recurrence<T, kKind, kBack, true>, grid, kWarps * 32, kRecSmem + kStagesOf<kBack> * kStageBytes + 128, s, a.tiles == 1, a, g, x, dy, y);
+}
+template <typename T, uint32_t kKind>
+cudaError_t run_kind(const RecArgs& a, bool back, bool tma, char* ws, cudaStream_t s) {
+    return back ? run_tiles<T, kKind, true>(a, tma, ws, s) : run_tiles<T, kKind, false>(a, tma, ws, s);
 }
 template <typename T>
-cudaError_t run(const RecArgs& a, uint32_t kind, bool back, bool pairs, cudaStream_t s) {
-    if (kind == ABS_RECURRENCE_BLEND) return pairs ? run_tiles<T, 2, ABS_RECURRENCE_BLEND>(a, back, s) : run_tiles<T, 1, ABS_RECURRENCE_BLEND>(a, back, s);
-    return pairs ? run_tiles<T, 2, ABS_RECURRENCE_ADD>(a, back, s) : run_tiles<T, 1, ABS_RECURRENCE_ADD>(a, back, s);
+cudaError_t run(const RecArgs& a, uint32_t kind, bool back, bool tma, char* ws, cudaStream_t s) {
+    return kind == ABS_RECURRENCE_BLEND ? run_kind<T, ABS_RECURRENCE_BLEND>(a, back, tma, ws, s) : run_kind<T, ABS_RECURRENCE_ADD>(a, back, tma, ws, s);
 }
 
 const char* check_sizes(uint64_t tokens, uint64_t width, uint64_t seqs, uint32_t kind, uint32_t dtype, int* code) {
@@ -373,28 +442,28 @@ const char* check_sizes(uint64_t tokens, uint64_t width, uint64_t seqs, uint32_t
     if (!known_dtype(dtype)) return "dtype must be ABS_F32 or ABS_BF16";
     if (kind > ABS_RECURRENCE_ADD) return "unknown kind of recurrence";
     if (width == 0) return "width must be at least 1";
-    if (tokens <= kSizeMax && width <= kSizeMax && seqs <= kSizeMax && ((tokens + kTile - 1) / kTile) * ((width + 31) / 32) <= kSizeMax) return nullptr;
+    if (tokens <= kSizeMax && width <= kSizeMax && seqs <= kSizeMax && ((tokens + kTileMin - 1) / kTileMin) * ((width + kCols - 1) / kCols) <= kSizeMax)
+        return nullptr;
     *code = ABS_ELIMIT;
-    return "a size exceeds 2^31 - 1024, or there are too many tiles of 128 rows and 32 columns";
+    return "a size exceeds 2^31 - 1024, or there are too many tiles of 32 rows and 64 columns";
 }
 
-// tokens > 0: `mats` are the matrices that the vector form depends on.
+// `mats`: the inputs, then the outputs.
 template <int N>
-int launch_scan(RecArgs& a, const MatrixArg (&mats)[N], uint32_t kind, uint32_t dtype, bool back, void* workspace, size_t workspace_bytes, cudaStream_t s) {
-    bool pairs = true;
-    for (const MatrixArg& m : mats) pairs = pairs && rows_at(m, 2 * m.es);
-    a.tiles = std::max(1, (a.T + kTile - 1) / kTile);
-    a.strips = (a.D + (pairs ? 63 : 31)) / (pairs ? 64 : 32);
-    cudaError_t e = cudaSuccess;
-    if (a.tiles > 1) {
-        if (!workspace || misaligned(workspace, 256)) return thread_error(ABS_EINVAL, "workspace must be non-NULL and 256-byte aligned");
-        if (workspace_bytes < abs_recurrence_workspace((uint64_t)a.T, (uint64_t)a.D)) return thread_error(ABS_ENOMEM, "workspace too small");
-        const size_t flags = flags_bytes(a.tiles, a.strips);
-        a.ctl = static_cast<uint32_t*>(workspace);
-        a.maps = reinterpret_cast<float2*>(static_cast<char*>(workspace) + flags);
-        e = cudaMemsetAsync(workspace, 0, flags, s);
+int launch_scan(RecArgs& a, const MatrixArg (&mats)[N], int inputs, uint32_t kind, uint32_t dtype, bool back, void* workspace, size_t workspace_bytes, cudaStream_t s) {
+    bool pairs = true, tma = a.T > 0;
+    for (int i = 0; i < N; ++i) {
+        pairs = pairs && rows_at(mats[i], 2 * mats[i].es);
+        if (i < inputs) tma = tma && rows_at(mats[i], 16);
     }
-    if (e == cudaSuccess) e = dtype == ABS_F32 ? run<float>(a, kind, back, pairs, s) : run<bf16>(a, kind, back, pairs, s);
+    a.pairs = pairs;
+    const size_t need = abs_recurrence_workspace((uint64_t)a.T, (uint64_t)a.D);
+    if (need) {
+        if (!workspace || misaligned(workspace, 256)) return thread_error(ABS_EINVAL, "workspace must be non-NULL and 256-byte aligned");
+        if (workspace_bytes < need) return thread_error(ABS_ENOMEM, "workspace too small");
+    }
+    char* ws = static_cast<char*>(workspace);
+    const cudaError_t e = dtype == ABS_F32 ? run<float>(a, kind, back, tma, ws, s) : run<bf16>(a, kind, back, tma, ws, s);
     return e == cudaSuccess ? ABS_OK : thread_error(ABS_ECUDA, cudaGetErrorString(e));
 }
 
@@ -408,8 +477,8 @@ using namespace abs_sgd;
 
 extern "C" size_t abs_recurrence_workspace(uint64_t tokens, uint64_t width) {
     if (tokens > kSizeMax || width > kSizeMax) return 0;
-    const uint64_t tiles = (tokens + kTile - 1) / kTile, strips = (width + 31) / 32;
-    return tiles > 1 ? flags_bytes(tiles, strips) + tiles * (strips + 1) * 32 * sizeof(float2) : 0;
+    const uint64_t tiles = (tokens + kTileMin - 1) / kTileMin, strips = (width + kCols - 1) / kCols;
+    return tiles > 1 ? flags_bytes(tiles, strips) + tiles * strips * 32 * sizeof(float4) : 0;
 }
 
 extern "C" int abs_recurrence(const void* x, uint64_t ld_x, const void* g, uint64_t ld_g, const int32_t* offsets, uint64_t seqs, const float* h0, uint32_t kind,
@@ -429,7 +498,7 @@ extern "C" int abs_recurrence(const void* x, uint64_t ld_x, const void* g, uint6
     RecArgs a{};
     a.x = x; a.ld_x = ld_x; a.g = g; a.ld_g = ld_g; a.out = y; a.ld_out = ld_y;
     a.offsets = offsets; a.before = h0; a.after = last; a.T = (int)tokens; a.D = (int)width; a.seqs = (int)seqs;
-    return launch_scan(a, m, kind, dtype, false, workspace, workspace_bytes, static_cast<cudaStream_t>(stream));
+    return launch_scan(a, m, 2, kind, dtype, false, workspace, workspace_bytes, static_cast<cudaStream_t>(stream));
 }
 
 extern "C" int abs_recurrence_backward(const void* dy, uint64_t ld_dy, const void* x, uint64_t ld_x, const void* g, uint64_t ld_g, const void* y, uint64_t ld_y,
@@ -455,7 +524,7 @@ extern "C" int abs_recurrence_backward(const void* dy, uint64_t ld_dy, const voi
     a.x = x; a.ld_x = ld_x; a.g = g; a.ld_g = ld_g; a.dy = dy; a.ld_dy = ld_dy; a.y = y; a.ld_y = ld_y;
     a.out = dx; a.ld_out = ld_dx; a.out2 = dg; a.ld_out2 = ld_dg;
     a.offsets = offsets; a.h0 = h0; a.before = dlast; a.after = dh0; a.T = (int)tokens; a.D = (int)width; a.seqs = (int)seqs;
-    return launch_scan(a, m, kind, dtype, true, workspace, workspace_bytes, static_cast<cudaStream_t>(stream));
+    return launch_scan(a, m, 4, kind, dtype, true, workspace, workspace_bytes, static_cast<cudaStream_t>(stream));
 }
 
 extern "C" int abs_recurrence_step(const void* x, uint64_t ld_x, const void* g, uint64_t ld_g, const float* h, uint32_t kind, uint32_t dtype, uint64_t seqs,
