@@ -221,7 +221,7 @@ int abs_activation_backward(const void *dy, uint64_t ld_dy, uint32_t dtype, cons
  *   sequence are zero.  The state itself stays fp32.
  *   offsets [seqs + 1] int32 on the device, ascending, values outside [0, tokens] are clamped; empty sequences are allowed.
  *   NULL: one sequence of all rows (seqs = 1).
- *   h0, last [seqs, width] fp32, packed; last out (NULL: not wanted): h behind the last row (of an empty sequence h0).  last may be h0.
+ *   h0, last [seqs, width] fp32, packed; last out (NULL: not wanted): h behind the last row (of an empty sequence h0); not h0 itself.
  * tokens, width and seqs up to 2^31 - 1024, tiles of 32 rows and 64 columns likewise (ABS_ELIMIT).  workspace: abs_recurrence_workspace(tokens, width) bytes, may be 0.  The kernel's waits
  * are bounded; see abs_llm_check. */
 size_t abs_recurrence_workspace(uint64_t tokens, uint64_t width);
@@ -234,7 +234,7 @@ int abs_recurrence(const void *x, uint64_t ld_x, const void *g, uint64_t ld_g, c
  *     d_t = dy_t + a_{t+1} d_{t+1}  (a sequence's last row: dy_t + dlast)      dh0 = a d of its first row (of an empty one: dlast)
  *     dx = (1 - a) d,  dg = d (h_{t-1} - x) a (1 - a)   (BLEND)         dx = d,  dg = d h_{t-1} a (1 - a)   (ADD)
  *   dx and dg are different ones; each may be dy, x or g, with the same leading dimension, neither may be y.  dh0 [seqs, width] fp32
- *   out, NULL: not wanted; it may be dlast.  Rows of no sequence get zeros.  workspace as for abs_recurrence. */
+ *   out, NULL: not wanted; neither h0 nor dlast.  Rows of no sequence get zeros.  workspace as for abs_recurrence. */
 int abs_recurrence_backward(const void *dy, uint64_t ld_dy, const void *x, uint64_t ld_x, const void *g, uint64_t ld_g, const void *y,
                             uint64_t ld_y, const int32_t *offsets, uint64_t seqs, const float *h0, const float *dlast, uint32_t kind,
                             uint32_t dtype, uint64_t tokens, uint64_t width, void *dx, uint64_t ld_dx, void *dg, uint64_t ld_dg, float *dh0,

@@ -9,6 +9,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "abs_internal.h"
 #include "abs_llm.h"
@@ -21,7 +22,6 @@ namespace abs_sgd {
 namespace {
 
 constexpr int kWarps = 8, kCols = 64;    // of a tile; a lane owns two columns
-constexpr int kGroupMax = 32;
 constexpr int kSms = 148;
 constexpr uint64_t kSizeMax = 0x7ffffc00ull;
 // Rows of a warp: 32 KB of inputs for a tile (two matrices forward, four backward).
@@ -45,17 +45,17 @@ struct RecArgs {
     const float *h0, *before;            // before: h0, backward dlast: the state in front of a sequence in scan order
     float* after;                        // last, backward dh0
     int T, D, seqs;
-    int tiles, strips, group;
+    int tiles, strips;
+    int segs, per;                       // segments, tiles of one (the last may have fewer)
     int pairs;                           // a lane's two columns are aligned to two elements in every matrix
-    uint32_t* ctl;                       // [0]: tickets; then a flag per (tile, strip)
-    float4* maps;                        // [tile][strip][lane]: a tile's map (A, B) for two columns, or (-0, state) for the last of a group
+    float4* maps;                        // [segment][strip][lane]: a segment's map (A, B) for two columns
 };
 
 // sigmoid(g) and 1 - sigmoid(g), each to its own precision.
 __device__ __forceinline__ void gate_of(float2 g, float2& a, float2& rest, bf16) {
     float2 v = mul2(g, both(-1.4426950408889634f));
-    v.x = v.x > 126.f ? 126.f : v.x;     // keeps a NaN
-    v.y = v.y > 126.f ? 126.f : v.y;
+    asm("min.NaN.f32 %0, %0, 0f42FC0000;" : "+f"(v.x));  // 126
+    asm("min.NaN.f32 %0, %0, 0f42FC0000;" : "+f"(v.y));
     const float2 e = exp2_of(v), d = add2(e, both(1.f));
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(a.x) : "f"(d.x));
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(a.y) : "f"(d.y));
@@ -106,102 +106,129 @@ __device__ __forceinline__ void store2(T* p, int n, bool aligned, float2 v) {
 
 // Which sequence row t belongs to: the number of sequences that end at or before it.
 __device__ __forceinline__ int begin_of(const RecArgs& a, int q) { return a.offsets ? min(max(a.offsets[q], 0), a.T) : q == 0 ? 0 : a.T; }
+// The same row for all lanes of a warp, 32 ends looked at in a step.
 __device__ __forceinline__ int sequence_of(const RecArgs& a, int t) {
     int lo = 0, hi = a.seqs;
     while (lo < hi) {
-        const int mid = (lo + hi) / 2;
-        if (begin_of(a, mid + 1) <= t) lo = mid + 1;
-        else hi = mid;
+        const int step = (hi - lo + 31) / 32;
+        const int64_t at = lo + (int64_t)(threadIdx.x % 32 + 1) * step - 1;
+        const bool over = at < hi && begin_of(a, (int)at + 1) <= t;
+        lo += __popc(__ballot_sync(0xffffffffu, over)) * step;
+        hi = min(hi, lo + step - 1);
     }
     return lo;
+}
+// From a sequence at or before that of row t on.
+__device__ __forceinline__ int sequence_from(const RecArgs& a, int q, int t) {
+    for (int i = 0; i < 4 && q < a.seqs && begin_of(a, q + 1) <= t; ++i) ++q;
+    int hi = a.seqs;
+    while (q < hi && begin_of(a, q + 1) <= t) {
+        const int mid = q + (hi - q) / 2;
+        if (begin_of(a, mid + 1) <= t) q = mid + 1;
+        else hi = mid;
+    }
+    return q;
 }
 
 struct RecSmem {
     alignas(16) float4 map[2][kWarps][32];       // of a warp's rows, by the tile's parity
-    float4 look[kWarps][32];                     // of the tiles in front, a run of them for each warp
+    float4 front[kWarps][32];                    // of the segments in front, a run of them for each warp
     alignas(8) uint64_t full[3];
-    int ticket[4];
-    uint32_t copies[4];                          // into each stage so far
-    int load_failed, look_failed;
+    int begins[2];                               // a sequence begins in the tile
+    int failed[2];
 };
-
 constexpr size_t kRecSmem = (sizeof(RecSmem) + 127) / 128 * 128;
 
-// A tile: kTileOf rows (in scan order: backward from the last one) of 64 columns.  A CTA takes tiles by ticket, tiles of all strips at the
-// same rows before the next rows, so that whoever waits for a tile in front waits for one that a running CTA has.
-//   1. a lane reads its rows of two columns, forms the gates, and the map of its warp's rows
-//   2. the warps' maps give the tile's map, which is published; the state in front of the tile is that behind the last tile of the group
-//      in front (published as such), followed by the maps of the group's tiles so far: always the same tiles in the same order, so
-//      that equal inputs give equal bits whoever comes first
-//   3. a lane goes over its rows again from their state
-// kTma: the tiles that a CTA takes next are copied to shared memory meanwhile.  Otherwise (rows that are not 16-byte aligned) the lanes read memory.
-template <typename T, uint32_t kKind, bool kBack, bool kTma>
+// A CTA takes a segment of a strip of 64 columns, tile by tile (kTileOf rows in scan order: backward from the last one).
+//   kMaps   the segment's map: from its last tile to its first, or to the first in which a sequence begins (nothing in front of that
+//           matters), so that what was read last is what the second pass reads first
+//   else    the state in front of the segment from the maps of those in front, in order; then for each tile
+//             1. a lane reads its rows of two columns, forms the gates, and the map of its warp's rows
+//             2. the maps of the warps in front give the state in front of its rows, those of all warps the state of the next tile
+//             3. it goes over its rows again
+// kTma: the next tiles are copied to shared memory meanwhile.  Otherwise (rows that are not 16-byte aligned) the lanes read memory.
+template <typename T, uint32_t kKind, bool kBack, bool kTma, bool kMaps>
 __global__ void __launch_bounds__(kWarps * 32, kCtasOf<kBack>) k_recurrence(const __grid_constant__ RecArgs a, const __grid_constant__ CUtensorMap tm_g,
                                                                             const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_dy,
                                                                             const __grid_constant__ CUtensorMap tm_y) {
-    constexpr int kRows = kRowsOf<T, kBack>, kTile = kTileOf<T, kBack>, kStages = kStagesOf<kBack>, kInputs = kBack ? 4 : 2;
+    constexpr int kRows = kRowsOf<T, kBack>, kTile = kTileOf<T, kBack>, kStages = kStagesOf<kBack>;
     constexpr int kInput = kTile * kCols * (int)sizeof(T);       // bytes of an input's tile
-    static_assert(kInput * kInputs == kStageBytes, "");
-    enum { kG, kX, kDy, kY };
+    constexpr int kInputs = kBack && !kMaps ? 4 : 2;
+    static_assert(kInput * (kBack ? 4 : 2) == kStageBytes, "");
+    enum { kG, kIn, kX, kY };                                    // kIn: x, backward dy; kX backward only
     extern __shared__ uint8_t raw[];
     RecSmem& s = *reinterpret_cast<RecSmem*>((reinterpret_cast<uintptr_t>(raw) + 127) & ~(uintptr_t)127);
     uint8_t* const ring = reinterpret_cast<uint8_t*>(&s) + kRecSmem;
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-    const int total = a.tiles * a.strips;
+    const int strip = blockIdx.x % a.strips, seg = blockIdx.x / a.strips;
+    const int first_tile = seg * a.per, tiles = min(a.per, a.tiles - first_tile);
+    auto tile_at = [&](int i) { return kMaps ? first_tile + tiles - 1 - i : first_tile + i; };
     if (threadIdx.x == 0) {
-        for (int i = 0; i < kStages; ++i) {
-            mbar_init(&s.full[i], 1);
-            s.copies[i] = 0;
-        }
-        s.load_failed = s.look_failed = 0;
+        for (int i = 0; i < kStages; ++i) mbar_init(&s.full[i], 1);
+        s.failed[0] = s.failed[1] = s.begins[0] = s.begins[1] = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     pdl_wait();
     pdl_trigger();
-    // thread 0: the next tile, and its copies
-    int coming = 0;                                              // thread 0: a ticket taken, not yet used
-    auto take = [&]() { return a.ctl ? (int)atomicAdd(&a.ctl[0], 1u) : coming + (int)gridDim.x; };
-    auto start = [&](int stage) {
-        s.ticket[stage] = coming;
-        if (coming >= total) return;
+    int copied = 0;                                              // thread 0: tiles whose copies are under way or done
+    auto copy_next = [&]() {
         if constexpr (kTma) {
-            const int u0 = coming / a.strips * kTile, c = coming % a.strips * kCols;
+            if (copied >= tiles) return;
+            const int u0 = tile_at(copied) * kTile, c = strip * kCols, st = copied % kStages;
             const int t = kBack ? a.T - u0 - kTile : u0;         // a first row below 0 reads zeros
-            uint8_t* to = ring + stage * kStageBytes;
-            mbar_expect_tx(&s.full[stage], kStageBytes);
-            ++s.copies[stage];
-            tma_load_2d(to + kG * kInput, &tm_g, c, t, &s.full[stage]);
-            tma_load_2d(to + kX * kInput, &tm_x, c, t, &s.full[stage]);
-            if constexpr (kBack) {
-                tma_load_2d(to + kDy * kInput, &tm_dy, c, t, &s.full[stage]);
-                tma_load_2d(to + kY * kInput, &tm_y, c, t - 1, &s.full[stage]);
+            uint8_t* to = ring + st * kStageBytes;
+            mbar_expect_tx(&s.full[st], kInput * kInputs);
+            tma_load_2d(to + kG * kInput, &tm_g, c, t, &s.full[st]);
+            tma_load_2d(to + kIn * kInput, kBack ? &tm_dy : &tm_x, c, t, &s.full[st]);
+            if constexpr (kInputs == 4) {
+                tma_load_2d(to + kX * kInput, &tm_x, c, t, &s.full[st]);
+                tma_load_2d(to + kY * kInput, &tm_y, c, t - 1, &s.full[st]);
             }
+            ++copied;
         }
-        coming = take();
     };
-    if (threadIdx.x == 0) {
-        coming = a.ctl ? take() : (int)blockIdx.x;
-        for (int i = 0; i < kStages; ++i) start(i);
-    }
     __syncthreads();
+    if (threadIdx.x == 0)
+        for (int i = 0; i < kStages; ++i) copy_next();
 
-    int stage = 0, n_tile = 0;
+    const int c = strip * kCols + lane * 2, n = min(max(a.D - c, 0), 2);
+    float4 behind = make_float4(1.f, 0.f, 1.f, 0.f);             // kMaps, warp 0: of the tiles so far
+    float2 start = both(0.f);                                    // else: the state in front of the tile
+    if (!kMaps && seg > 0) {
+        const int per = (seg + kWarps - 1) / kWarps, k0 = warp * per, k1 = min(k0 + per, seg);
+        const float4* p = a.maps + (size_t)strip * 32 + lane;
+        float4 run = make_float4(1.f, 0.f, 1.f, 0.f);
+        for (int k = k0; k < k1; k += 8) {
+            float4 v[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (k + i < k1) v[i] = p[(size_t)(k + i) * a.strips * 32];
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (k + i < k1) compose2(run, v[i]);
+        }
+        s.front[warp][lane] = run;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) start = apply2(s.front[w][lane], start);
+    }
+
+    int stage = 0;
     uint32_t phase = 0;
-    for (;;) {
-        const int mine = s.ticket[stage];
-        if (mine >= total) break;
-        const int tile = mine / a.strips, strip = mine % a.strips;
-        const int c = strip * kCols + lane * 2, n = min(max(a.D - c, 0), 2);
-        const int u0 = tile * kTile + warp * kRows;              // first row of the warp, in scan order
+    bool failed = false;
+    for (int i = 0; i < tiles; ++i) {
+        const int u0 = tile_at(i) * kTile + warp * kRows;        // first row of the warp, in scan order
         auto row = [&](int r) { return kBack ? a.T - 1 - (u0 + r) : u0 + r; };
         // ---- which rows are in a sequence, and are the first and last one in scan order
         int seq = 0;
         uint32_t member, first, final;
         {
             bool m = false, f = false, l = false;
+            const int low = max(kBack ? a.T - u0 - kRows : u0, 0);
+            const int q0 = sequence_of(a, low);
             if (lane < kRows && u0 + lane < a.T) {
                 const int t = row(lane);
-                seq = sequence_of(a, t);
+                seq = sequence_from(a, q0, t);
                 const int from = seq < a.seqs ? begin_of(a, seq) : a.T;
                 m = t >= from;
                 f = m && t == from;
@@ -211,14 +238,16 @@ __global__ void __launch_bounds__(kWarps * 32, kCtasOf<kBack>) k_recurrence(cons
             first = __ballot_sync(0xffffffffu, kBack ? l : f);
             final = __ballot_sync(0xffffffffu, kBack ? f : l);
         }
+        // rows inside one sequence and whole strips, nearly all there are: no row needs a look of its own
+        const bool plain = member == (kRows == 32 ? 0xffffffffu : (1u << kRows) - 1) && (first | final) == 0 && (strip + 1) * kCols <= a.D && a.pairs;
         // two columns of the r-th row of an input; not for rows of no sequence
         auto fetch = [&](int which, int r) {
             if constexpr (kTma) {
                 const int at = kBack ? kTile - 1 - (warp * kRows + r) : warp * kRows + r;
                 return pair_of(reinterpret_cast<const T*>(ring + stage * kStageBytes + which * kInput) + at * kCols + lane * 2);
             } else {
-                const void* p = which == kG ? a.g : which == kX ? a.x : which == kDy ? a.dy : a.y;
-                const size_t ld = which == kG ? a.ld_g : which == kX ? a.ld_x : which == kDy ? a.ld_dy : a.ld_y;
+                const void* p = which == kG ? a.g : which == kIn ? (kBack ? a.dy : a.x) : which == kX ? a.x : a.y;
+                const size_t ld = which == kG ? a.ld_g : which == kIn ? (kBack ? a.ld_dy : a.ld_x) : which == kX ? a.ld_x : a.ld_y;
                 return load2(static_cast<const T*>(p) + (size_t)(row(r) - (which == kY)) * ld + c, n, a.pairs != 0);
             }
         };
@@ -227,152 +256,129 @@ __global__ void __launch_bounds__(kWarps * 32, kCtasOf<kBack>) k_recurrence(cons
             const float* f = p + (size_t)q * a.D + c;
             return make_float2(n > 0 ? f[0] : 0.f, n > 1 ? f[1] : 0.f);
         };
-        if (kTma && !mbar_wait(&s.full[stage], phase)) s.load_failed = 1;
+        if (kTma && !mbar_wait(&s.full[stage], phase)) s.failed[i & 1] = 1;
 
         // ---- 1
         float2 keep[kRows], feed[kRows];                         // a; forward b, backward 1 - a
         float4 m = make_float4(1.f, 0.f, 1.f, 0.f);
+        auto collect = [&](auto all) {
+            constexpr bool kAll = decltype(all)::value;
 #pragma unroll
-        for (int r = 0; r < kRows; ++r) {
-            const bool in = (member >> r & 1) != 0;
-            float2 gv = both(0.f), v = both(0.f), z;             // v: x, backward dy
-            if (in) {
-                gv = fetch(kG, r);
-                v = fetch(kBack ? kDy : kX, r);
-            }
-            gate_of(gv, keep[r], z, T());
-            if (!in) keep[r] = both(1.f);
-            if (first >> r & 1) {
-                m = make_float4(-0.f, 0.f, -0.f, 0.f);
-                if (a.before) {                                  // read once and here: `after` may be `before`
-                    const float2 i = given(a.before, r);
-                    m.y = i.x;
-                    m.w = i.y;
-                }
-            }
-            float2 B = make_float2(m.y, m.w);
-            if (kBack) {
-                feed[r] = (first >> r & 1) ? B : z;              // a first row's 1 - a is formed again
-                B = mul2(keep[r], add2(B, v));
-            } else {
-                feed[r] = !in ? both(0.f) : kKind == ABS_RECURRENCE_BLEND ? mul2(v, z) : v;
-                if (first >> r & 1) feed[r] = fma2(keep[r], B, feed[r]);
-                B = (first >> r & 1) ? feed[r] : fma2(keep[r], B, feed[r]);
-            }
-            m = make_float4(m.x * keep[r].x, B.x, m.z * keep[r].y, B.y);
-        }
-        s.map[n_tile & 1][warp][lane] = m;
-        __syncthreads();
-        if (s.load_failed) break;
-        // forward the tile's image has been read, backward that of the tile before
-        if (threadIdx.x == 0) {
-            if (!kBack) start(stage);
-            else if (n_tile > 0) start(stage ^ 1);
-        }
-        // ---- 2
-        float2 state = both(0.f);
-        if (a.tiles > 1) {
-            uint32_t* flags = a.ctl + 1;
-            const bool closes = tile % a.group == a.group - 1;
-            float4 whole = make_float4(1.f, 0.f, 1.f, 0.f);
-            auto publish = [&]() {
-                a.maps[((size_t)tile * a.strips + strip) * 32 + lane] = whole;
-                __threadfence();
-                __syncwarp();
-                if (lane == 0) asm volatile("st.release.gpu.global.u32 [%0], %1;" ::"l"(flags + (size_t)tile * a.strips + strip), "r"(1u) : "memory");
-            };
-            if (warp == 0) {
-#pragma unroll
-                for (int w = 0; w < kWarps; ++w) compose2(whole, s.map[n_tile & 1][w][lane]);
-                if (!closes) publish();
-            }
-            const int from = max(tile / a.group * a.group - 1, 0), count = tile - from, per = (count + kWarps - 1) / kWarps;
-            constexpr int kPer = (kGroupMax + kWarps - 1) / kWarps;
-            const int k0 = from + warp * per, k1 = min(k0 + per, tile);
-            bool ok = true;
-            if (k0 + lane < k1) {
-                const uint32_t* f = flags + (size_t)(k0 + lane) * a.strips + strip;
-                uint32_t seen = 0;
-                for (uint32_t it = 0; it < kSpinLimit && !seen; ++it) asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(seen) : "l"(f) : "memory");
-                ok = seen != 0;
-            }
-            if (__all_sync(0xffffffffu, ok)) {
-                float4 v[kPer], run = make_float4(1.f, 0.f, 1.f, 0.f);
-#pragma unroll
-                for (int k = 0; k < kPer; ++k)
-                    if (k0 + k < k1) v[k] = __ldcg(a.maps + ((size_t)(k0 + k) * a.strips + strip) * 32 + lane);
-#pragma unroll
-                for (int k = 0; k < kPer; ++k)
-                    if (k0 + k < k1) compose2(run, v[k]);
-                s.look[warp][lane] = run;
-            } else {
-                s.look_failed = 1;
-            }
-            __syncthreads();
-            if (s.look_failed) break;
-#pragma unroll
-            for (int w = 0; w < kWarps; ++w)
-                if (w * per < count) state = apply2(s.look[w][lane], state);
-            if (closes && warp == 0) {
-                const float2 end = apply2(whole, state);
-                whole = make_float4(-0.f, end.x, -0.f, end.y);
-                publish();
-            }
-        }
-        if (kBack && a.tiles == 1) __syncthreads();              // the next tile's ticket
-        for (int w = 0; w < warp; ++w) state = apply2(s.map[n_tile & 1][w][lane], state);
-        // ---- 3
-#pragma unroll
-        for (int r = 0; r < kRows; ++r) {
-            const bool in = (member >> r & 1) != 0;
-            float2 o = both(0.f), o2 = both(0.f);
-            if (kBack) {
-                if (first >> r & 1) {
-                    float2 k;
-                    state = feed[r];
-                    gate_of(fetch(kG, r), k, feed[r], T());
-                }
+            for (int r = 0; r < kRows; ++r) {
+                const bool in = kAll || (member >> r & 1) != 0, begins = !kAll && (first >> r & 1) != 0;
+                float2 gv = both(0.f), v = both(0.f), z;
                 if (in) {
-                    float2 h = both(0.f);
-                    if (!(final >> r & 1)) h = fetch(kY, r);
-                    if ((final >> r & 1) && a.h0) h = given(a.h0, r);
-                    const float2 d = add2(state, fetch(kDy, r)), z = feed[r];
-                    state = mul2(keep[r], d);
-                    o = kKind == ABS_RECURRENCE_BLEND ? mul2(z, d) : d;
-                    if (kKind == ABS_RECURRENCE_BLEND) h = fma2(fetch(kX, r), both(-1.f), h);
-                    o2 = mul2(mul2(state, z), h);
+                    gv = fetch(kG, r);
+                    v = fetch(kIn, r);
                 }
-            } else {
-                state = (first >> r & 1) ? feed[r] : fma2(keep[r], state, feed[r]);
-                if (in) o = state;
+                gate_of(gv, keep[r], z, T());
+                if (!in) keep[r] = both(1.f);
+                if (begins) {
+                    const float2 b = a.before ? given(a.before, r) : both(0.f);
+                    m = make_float4(-0.f, b.x, -0.f, b.y);
+                }
+                float2 B = make_float2(m.y, m.w);
+                if (kBack) {
+                    feed[r] = z;
+                    B = mul2(keep[r], add2(B, v));
+                } else {
+                    feed[r] = !in ? both(0.f) : kKind == ABS_RECURRENCE_BLEND ? mul2(v, z) : v;
+                    B = fma2(keep[r], B, feed[r]);
+                    if (begins) feed[r] = B;                     // the sequence's first state
+                }
+                const float2 A = mul2(make_float2(m.x, m.z), keep[r]);
+                m = make_float4(A.x, B.x, A.y, B.y);
             }
-            if (n > 0 && u0 + r < a.T) {
-                const size_t t = (size_t)row(r);
-                store2(static_cast<T*>(a.out) + t * a.ld_out + c, n, a.pairs != 0, o);
-                if (kBack) store2(static_cast<T*>(a.out2) + t * a.ld_out2 + c, n, a.pairs != 0, o2);
+        };
+        if (plain) collect(std::true_type());
+        else collect(std::false_type());
+        s.map[i & 1][warp][lane] = m;
+        if (kMaps && first != 0 && lane == 0) s.begins[i & 1] = 1;
+        __syncthreads();
+        // by the tile's parity: who is a tile ahead writes the other one, and nobody is two ahead
+        failed = s.failed[i & 1] != 0;
+        if (failed) break;
+        // forward the tile's image has been read, backward that of the tile before
+        if (threadIdx.x == 0 && (!kBack || kMaps || i > 0)) copy_next();
+        // ---- 2
+        if constexpr (kMaps) {
+            if (warp == 0) {
+                float4 whole = make_float4(1.f, 0.f, 1.f, 0.f);
+#pragma unroll
+                for (int w = 0; w < kWarps; ++w) compose2(whole, s.map[i & 1][w][lane]);
+                compose2(whole, behind);
+                behind = whole;
             }
-            if ((final >> r & 1) && a.after) {
-                const int q = __shfl_sync(0xffffffffu, seq, r);
-                float* p = a.after + (size_t)q * a.D + c;
-                if (n > 0) p[0] = state.x;
-                if (n > 1) p[1] = state.y;
+            if (s.begins[i & 1]) break;
+        } else {
+            float2 state = start;
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) {
+                if (w == warp) state = start;
+                start = apply2(s.map[i & 1][w][lane], start);
             }
+            // ---- 3
+            auto finish = [&](auto all) {
+                constexpr bool kAll = decltype(all)::value;
+                T* out = static_cast<T*>(a.out) + (int64_t)row(0) * (int64_t)a.ld_out + c;
+                T* out2 = kBack ? static_cast<T*>(a.out2) + (int64_t)row(0) * (int64_t)a.ld_out2 + c : nullptr;
+                const int64_t step = kBack ? -(int64_t)a.ld_out : (int64_t)a.ld_out, step2 = -(int64_t)a.ld_out2;
+#pragma unroll
+                for (int r = 0; r < kRows; ++r) {
+                    const bool in = kAll || (member >> r & 1) != 0, begins = !kAll && (first >> r & 1) != 0, ends = !kAll && (final >> r & 1) != 0;
+                    float2 o = both(0.f), o2 = both(0.f);
+                    if (kBack) {
+                        if (begins) state = a.before ? given(a.before, r) : both(0.f);
+                        if (in) {
+                            float2 h = both(0.f);
+                            if (!ends) h = fetch(kY, r);
+                            else if (a.h0) h = given(a.h0, r);
+                            const float2 d = add2(state, fetch(kIn, r)), z = feed[r];
+                            state = mul2(keep[r], d);
+                            o = kKind == ABS_RECURRENCE_BLEND ? mul2(z, d) : d;
+                            if (kKind == ABS_RECURRENCE_BLEND) h = fma2(fetch(kX, r), both(-1.f), h);
+                            o2 = mul2(mul2(state, z), h);
+                        }
+                    } else {
+                        state = begins ? feed[r] : fma2(keep[r], state, feed[r]);
+                        if (in) o = state;
+                    }
+                    if (kAll) {
+                        put_pair(out, o);
+                        if (kBack) put_pair(out2, o2);
+                    } else if (n > 0 && u0 + r < a.T) {
+                        store2(out, n, a.pairs != 0, o);
+                        if (kBack) store2(out2, n, a.pairs != 0, o2);
+                    }
+                    out += step;
+                    if (kBack) out2 += step2;
+                    if (ends && a.after) {
+                        const int q = __shfl_sync(0xffffffffu, seq, r);
+                        float* p = a.after + (size_t)q * a.D + c;
+                        if (n > 0) p[0] = state.x;
+                        if (n > 1) p[1] = state.y;
+                    }
+                }
+            };
+            if (plain) finish(std::true_type());
+            else finish(std::false_type());
         }
-        // ---- sequences without rows
-        if (tile == 0 && a.after && (a.T == 0 || a.offsets))
-            for (int q = warp; q < a.seqs; q += kWarps)
-                if (begin_of(a, q + 1) <= begin_of(a, q))
-                    for (int i = 0; i < n; ++i) a.after[(size_t)q * a.D + c + i] = a.before ? a.before[(size_t)q * a.D + c + i] : 0.f;
-        ++n_tile;
         if (++stage == kStages) {
             stage = 0;
             phase ^= 1u;
         }
     }
-    if (threadIdx.x == 0 && (s.load_failed || s.look_failed)) {
-        report_timeout();
-        for (int i = 0; i < kStages; ++i)                        // copies in flight land before the CTA's shared memory is released
-            if (s.copies[i]) mbar_wait(&s.full[i], (s.copies[i] - 1) & 1u, 4096u);
+    if constexpr (kMaps) {
+        if (warp == 0 && !failed) a.maps[((size_t)seg * a.strips + strip) * 32 + lane] = behind;
+    } else if (seg == 0 && a.after && (a.T == 0 || a.offsets)) { // sequences without rows
+        for (int q = warp; q < a.seqs; q += kWarps)
+            if (begin_of(a, q + 1) <= begin_of(a, q))
+                for (int k = 0; k < n; ++k) a.after[(size_t)q * a.D + c + k] = a.before ? a.before[(size_t)q * a.D + c + k] : 0.f;
+    }
+    if (threadIdx.x == 0) {
+        if (failed) report_timeout();
+        for (int i = max(copied - kStages, 0); i < copied; ++i)  // copies in flight land before the CTA's shared memory is released
+            mbar_wait(&s.full[i % kStages], (i / kStages) & 1u, failed ? 4096u : kSpinLimit);
     }
 }
 
@@ -392,8 +398,6 @@ __global__ void __launch_bounds__(256) k_recurrence_step(const T* x, size_t ld_x
     }
 }
 
-size_t flags_bytes(uint64_t tiles, uint64_t strips) { return up256((1 + tiles * strips) * 4); }
-
 // An input's tiles: kTile rows of 64 columns, as they lie.
 bool encode_tiles(CUtensorMap* tm, const void* p, size_t ld, size_t es, const RecArgs& a, int rows) {
     const EncodeTiledFn enc = get_encode();
@@ -404,29 +408,40 @@ bool encode_tiles(CUtensorMap* tm, const void* p, size_t ld, size_t es, const Re
                CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// Segments of a strip: as many as fill the GPU once, or twice where that leaves fewer SMs idle.  One where that fills more than 60 % of
+// it, since two and more are read twice (but for what lies in front of a sequence's begin).
+void cut_segments(RecArgs& a, int resident) {
+    int segs = 1;
+    if (a.strips * 10 <= resident * 6) {
+        const int once = resident / a.strips, twice = 2 * resident / a.strips;
+        segs = twice > 2 * once && once < 8 ? twice : once;
+    }
+    a.per = (a.tiles + segs - 1) / segs;
+    a.segs = (a.tiles + a.per - 1) / a.per;
+}
+
+template <typename T, uint32_t kKind, bool kBack, bool kTma>
+cudaError_t run_passes(const RecArgs& a, const CUtensorMap (&tm)[4], cudaStream_t s) {
+    const size_t smem = kRecSmem + (kTma ? kStagesOf<kBack> * kStageBytes : 0) + 128;
+    cudaError_t e = allow_smem<k_recurrence<T, kKind, kBack, kTma, true>>();
+    if (e == cudaSuccess) e = allow_smem<k_recurrence<T, kKind, kBack, kTma, false>>();
+    if (e == cudaSuccess && a.segs > 1)
+        e = launch_kernel(k_recurrence<T, kKind, kBack, kTma, true>, (a.segs - 1) * a.strips, kWarps * 32, smem, s, true, a, tm[0], tm[1], tm[2], tm[3]);
+    if (e != cudaSuccess) return e;
+    return launch_kernel(k_recurrence<T, kKind, kBack, kTma, false>, a.segs * a.strips, kWarps * 32, smem, s, true, a, tm[0], tm[1], tm[2], tm[3]);
+}
 template <typename T, uint32_t kKind, bool kBack>
 cudaError_t run_tiles(RecArgs a, bool tma, char* workspace, cudaStream_t s) {
     constexpr int kTile = kTileOf<T, kBack>;
     a.tiles = std::max(1, (a.T + kTile - 1) / kTile);
     a.strips = (a.D + kCols - 1) / kCols;
-    // the chain of published states takes some 2.5 us a link: a group's tiles of all strips have to keep the memory busy for that long
-    a.group = std::min(std::max(331 / a.strips, 1), kGroupMax);
-    if (a.tiles > 1) {
-        const size_t flags = flags_bytes(a.tiles, a.strips);
-        a.ctl = reinterpret_cast<uint32_t*>(workspace);
-        a.maps = reinterpret_cast<float4*>(workspace + flags);
-        const cudaError_t e = cudaMemsetAsync(workspace, 0, flags, s);
-        if (e != cudaSuccess) return e;
-    }
-    const int grid = std::min(a.tiles * a.strips, kSms * kCtasOf<kBack>);
-    CUtensorMap g{}, x{}, dy{}, y{};
-    if (!tma) return launch_kernel(k_recurrence<T, kKind, kBack, false>, grid, kWarps * 32, kRecSmem + 128, s, a.tiles == 1, a, g, x, dy, y);
-    bool ok = encode_tiles(&g, a.g, a.ld_g, sizeof(T), a, kTile) && encode_tiles(&x, a.x, a.ld_x, sizeof(T), a, kTile);
-    if (kBack) ok = ok && encode_tiles(&dy, a.dy, a.ld_dy, sizeof(T), a, kTile) && encode_tiles(&y, a.y, a.ld_y, sizeof(T), a, kTile);
-    if (!ok) return cudaErrorInvalidValue;
-    const cudaError_t e = allow_smem<k_recurrence<T, kKind, kBack, true>>();
-    if (e != cudaSuccess) return e;
-    return launch_kernel(k_recurrence<T, kKind, kBack, true>, grid, kWarps * 32, kRecSmem + kStagesOf<kBack> * kStageBytes + 128, s, a.tiles == 1, a, g, x, dy, y);
+    cut_segments(a, kSms * kCtasOf<kBack>);
+    a.maps = reinterpret_cast<float4*>(workspace);
+    CUtensorMap tm[4] = {};
+    if (!tma) return run_passes<T, kKind, kBack, false>(a, tm, s);
+    bool ok = encode_tiles(&tm[0], a.g, a.ld_g, sizeof(T), a, kTile) && encode_tiles(&tm[1], a.x, a.ld_x, sizeof(T), a, kTile);
+    if (kBack) ok = ok && encode_tiles(&tm[2], a.dy, a.ld_dy, sizeof(T), a, kTile) && encode_tiles(&tm[3], a.y, a.ld_y, sizeof(T), a, kTile);
+    return ok ? run_passes<T, kKind, kBack, true>(a, tm, s) : cudaErrorInvalidValue;
 }
 template <typename T, uint32_t kKind>
 cudaError_t run_kind(const RecArgs& a, bool back, bool tma, char* ws, cudaStream_t s) {
@@ -477,8 +492,10 @@ using namespace abs_sgd;
 
 extern "C" size_t abs_recurrence_workspace(uint64_t tokens, uint64_t width) {
     if (tokens > kSizeMax || width > kSizeMax) return 0;
-    const uint64_t tiles = (tokens + kTileMin - 1) / kTileMin, strips = (width + kCols - 1) / kCols;
-    return tiles > 1 ? flags_bytes(tiles, strips) + tiles * strips * 32 * sizeof(float4) : 0;
+    if (tokens <= (uint64_t)kTileMin) return 0;
+    // maps of the segments but the last: at most twice as many as CTAs fill the GPU
+    const uint64_t strips = (width + kCols - 1) / kCols, most = std::min<uint64_t>(2 * 3 * kSms, (tokens + kTileMin - 1) / kTileMin * strips);
+    return up256((size_t)std::max(most, strips) * 32 * sizeof(float4));
 }
 
 extern "C" int abs_recurrence(const void* x, uint64_t ld_x, const void* g, uint64_t ld_g, const int32_t* offsets, uint64_t seqs, const float* h0, uint32_t kind,
@@ -493,6 +510,7 @@ extern "C" int abs_recurrence(const void* x, uint64_t ld_x, const void* g, uint6
         if (const char* why = check_in_place(m[2], m[i], true)) return thread_error(ABS_EINVAL, why);
     if (!offsets && seqs != 1) return thread_error(ABS_EINVAL, "without offsets there is one sequence");
     if (misaligned(offsets, 4) || misaligned(h0, 4) || misaligned(last, 4)) return thread_error(ABS_EINVAL, "offsets, h0 and last must be 4-byte aligned");
+    if (last && last == h0) return thread_error(ABS_EINVAL, "last must not be h0");
     if (tokens && (!x || !g || !y)) return thread_error(ABS_EINVAL, "x, g and y must not be NULL");
     if (tokens == 0 && (!last || seqs == 0)) return ABS_OK;
     RecArgs a{};
@@ -518,7 +536,7 @@ extern "C" int abs_recurrence_backward(const void* dy, uint64_t ld_dy, const voi
         return thread_error(ABS_EINVAL, "offsets, h0, dlast and dh0 must be 4-byte aligned");
     if (tokens && (!dy || !x || !g || !y || !dx || !dg)) return thread_error(ABS_EINVAL, "dy, x, g, y, dx and dg must not be NULL");
     if (tokens && dx == dg) return thread_error(ABS_EINVAL, "two outputs are the same");
-    if (dh0 && dh0 == h0) return thread_error(ABS_EINVAL, "dh0 must not be h0");
+    if (dh0 && (dh0 == h0 || dh0 == dlast)) return thread_error(ABS_EINVAL, "dh0 must be neither h0 nor dlast");
     if (tokens == 0 && (!dh0 || seqs == 0)) return ABS_OK;
     RecArgs a{};
     a.x = x; a.ld_x = ld_x; a.g = g; a.ld_g = ld_g; a.dy = dy; a.ld_dy = ld_dy; a.y = y; a.ld_y = ld_y;

@@ -223,7 +223,7 @@ def gated_recurrence(x, g, offsets=None, h0=None, kind: str = "blend", y=None, l
 
     x, g [tokens, width] float32 / bfloat16: the rows of the sequences one after the other; offsets int32 [sequences + 1]: their first
     rows (None: one sequence); h0 float32 [sequences, width]: the states in front (None: zero).  y: h_t, zeros in rows of no sequence; y may
-    be x or g, last may be h0."""
+    be x or g."""
     return Recurrence(*_t.recurrence(x, g, offsets, h0, _choice(RECURRENCES, kind, "kind"), y, last))
 
 

@@ -54,7 +54,7 @@ def scan(B, **kw):  # noqa: F811
 
 
 def scan_back(B, **kw):  # noqa: F811
-    a = dict(dy=P, ld_dy=16, x=2 * P, ld_x=16, g=3 * P, ld_g=16, y=4 * P, ld_y=16, off=P, seqs=2, h0=P, dlast=P, kind=0, dtype=1, T=400, D=16, dx=5 * P, ld_dx=16,
+    a = dict(dy=P, ld_dy=16, x=2 * P, ld_x=16, g=3 * P, ld_g=16, y=4 * P, ld_y=16, off=P, seqs=2, h0=P, dlast=9 * P, kind=0, dtype=1, T=400, D=16, dx=5 * P, ld_dx=16,
              dg=6 * P, ld_dg=16, dh0=7 * P, ws=P, n=WS) | kw
     return B.lib.abs_recurrence_backward(*a.values(), None)
 
@@ -85,12 +85,12 @@ CASES = [
     (wgrad, dict(dy=None)), (wgrad, dict(dw=P)), (wgrad, dict(db=2 * P)), (wgrad, dict(ld_dw=23)), (wgrad, dict(ws=None)),
     (through, dict(dtype=2)), (through, dict(act=5)), (through, dict(D=0)), (through, dict(dy=None)), (through, dict(z=None)), (through, dict(dz=None)), (through, dict(ld_dz=1)),
     (through, dict(dz=P)), (through, dict(dz=2 * P, ld_dz=20)),
-    (scan, dict(dtype=2)), (scan, dict(kind=2)), (scan, dict(D=0)), (scan, dict(off=None)), (scan, dict(off=P + 2)), (scan, dict(h0=P + 1)), (scan, dict(last=P + 2)),
+    (scan, dict(dtype=2)), (scan, dict(kind=2)), (scan, dict(D=0)), (scan, dict(off=None)), (scan, dict(off=P + 2)), (scan, dict(h0=P + 1)), (scan, dict(last=P + 2)), (scan, dict(last=P)),
     (scan, dict(x=None)), (scan, dict(g=None)), (scan, dict(y=None)), (scan, dict(ld_x=15)), (scan, dict(ld_y=15)), (scan, dict(y=P, ld_y=20)), (scan, dict(ws=None)),
     (scan, dict(ws=P + 8)),
     (scan_back, dict(dtype=2)), (scan_back, dict(kind=5)), (scan_back, dict(off=None)), (scan_back, dict(dy=None)), (scan_back, dict(x=None)), (scan_back, dict(g=None)),
     (scan_back, dict(y=None)), (scan_back, dict(dx=None)), (scan_back, dict(dg=None)), (scan_back, dict(dx=6 * P)), (scan_back, dict(dx=4 * P)), (scan_back, dict(dg=4 * P)),
-    (scan_back, dict(dx=P, ld_dx=24)), (scan_back, dict(dh0=P)), (scan_back, dict(dh0=P + 2)), (scan_back, dict(dlast=P + 2)), (scan_back, dict(ws=None)),
+    (scan_back, dict(dx=P, ld_dx=24)), (scan_back, dict(dh0=P)), (scan_back, dict(dh0=9 * P)), (scan_back, dict(dh0=P + 2)), (scan_back, dict(dlast=P + 2)), (scan_back, dict(ws=None)),
     (step, dict(dtype=2)), (step, dict(kind=2)), (step, dict(D=0)), (step, dict(x=None)), (step, dict(h=None)), (step, dict(out=None)), (step, dict(y=None)), (step, dict(h=P + 2)),
     (step, dict(y=P, ld_y=24)), (step, dict(ld_g=1)),
 ]
