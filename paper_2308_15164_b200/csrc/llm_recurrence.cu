@@ -24,17 +24,18 @@ namespace {
 constexpr int kWarps = 8, kCols = 64;    // of a tile; a lane owns two columns
 constexpr int kSms = 148;
 constexpr uint64_t kSizeMax = 0x7ffffc00ull;
-// Rows of a warp: 32 KB of inputs for a tile (two matrices forward, four backward).
-template <typename T, bool kBack>
-constexpr int kRowsOf = (kBack ? 8 : 16) * 2 / (int)sizeof(T);
-template <typename T, bool kBack>
-constexpr int kTileOf = kWarps * kRowsOf<T, kBack>;
-template <bool kBack>
-constexpr int kStagesOf = kBack ? 2 : 3;
-template <bool kBack>
-constexpr int kCtasOf = kBack ? 3 : 2;   // of an SM
-constexpr int kTileMin = kTileOf<float, true>;
-constexpr int kStageBytes = 32768;
+// Rows of a warp: 32 KB of inputs for a tile (two matrices forward, four backward); of the first pass 16 KB.
+template <typename T, bool kBack, bool kMaps>
+constexpr int kRowsOf = (kBack || kMaps ? 8 : 16) * 2 / (int)sizeof(T);
+template <typename T, bool kBack, bool kMaps>
+constexpr int kTileOf = kWarps * kRowsOf<T, kBack, kMaps>;
+template <bool kBack, bool kMaps>
+constexpr int kStagesOf = kBack && !kMaps ? 2 : 3;
+template <bool kBack, bool kMaps>
+constexpr int kCtasOf = kMaps ? 4 : kBack ? 3 : 2;       // of an SM
+template <bool kMaps>
+constexpr int kStageBytes = kMaps ? 16384 : 32768;
+constexpr int kTileMin = kTileOf<float, true, false>;
 
 struct RecArgs {
     const void *x, *g, *dy, *y;          // y: of the forward pass (backward only)
@@ -45,10 +46,11 @@ struct RecArgs {
     const float *h0, *before;            // before: h0, backward dlast: the state in front of a sequence in scan order
     float* after;                        // last, backward dh0
     int T, D, seqs;
-    int tiles, strips;
-    int segs, per;                       // segments, tiles of one (the last may have fewer)
+    int strips;
+    int segs, rows;                      // segments, rows of one (a multiple of a tile; the last may have fewer)
+    int parts, part_rows;                // of a segment, in the first pass: a map for each
     int pairs;                           // a lane's two columns are aligned to two elements in every matrix
-    float4* maps;                        // [segment][strip][lane]: a segment's map (A, B) for two columns
+    float4* maps;                        // [segment][part][strip][lane]: a map (A, B) for two columns
 };
 
 // sigmoid(g) and 1 - sigmoid(g), each to its own precision.
@@ -148,21 +150,24 @@ constexpr size_t kRecSmem = (sizeof(RecSmem) + 127) / 128 * 128;
 //             3. it goes over its rows again
 // kTma: the next tiles are copied to shared memory meanwhile.  Otherwise (rows that are not 16-byte aligned) the lanes read memory.
 template <typename T, uint32_t kKind, bool kBack, bool kTma, bool kMaps>
-__global__ void __launch_bounds__(kWarps * 32, kCtasOf<kBack>) k_recurrence(const __grid_constant__ RecArgs a, const __grid_constant__ CUtensorMap tm_g,
+__global__ void __launch_bounds__(kWarps * 32, kCtasOf<kBack, kMaps>) k_recurrence(const __grid_constant__ RecArgs a, const __grid_constant__ CUtensorMap tm_g,
                                                                             const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_dy,
                                                                             const __grid_constant__ CUtensorMap tm_y) {
-    constexpr int kRows = kRowsOf<T, kBack>, kTile = kTileOf<T, kBack>, kStages = kStagesOf<kBack>;
+    constexpr int kRows = kRowsOf<T, kBack, kMaps>, kTile = kTileOf<T, kBack, kMaps>, kStages = kStagesOf<kBack, kMaps>;
     constexpr int kInput = kTile * kCols * (int)sizeof(T);       // bytes of an input's tile
     constexpr int kInputs = kBack && !kMaps ? 4 : 2;
-    static_assert(kInput * (kBack ? 4 : 2) == kStageBytes, "");
+    static_assert(kInput * kInputs == kStageBytes<kMaps>, "");
     enum { kG, kIn, kX, kY };                                    // kIn: x, backward dy; kX backward only
     extern __shared__ uint8_t raw[];
     RecSmem& s = *reinterpret_cast<RecSmem*>((reinterpret_cast<uintptr_t>(raw) + 127) & ~(uintptr_t)127);
     uint8_t* const ring = reinterpret_cast<uint8_t*>(&s) + kRecSmem;
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-    const int strip = blockIdx.x % a.strips, seg = blockIdx.x / a.strips;
-    const int first_tile = seg * a.per, tiles = min(a.per, a.tiles - first_tile);
-    auto tile_at = [&](int i) { return kMaps ? first_tile + tiles - 1 - i : first_tile + i; };
+    const int strip = blockIdx.x % a.strips, index = blockIdx.x / a.strips, seg = kMaps ? index / a.parts : index;
+    // its rows in scan order, the first pass's from the segment's last part on
+    const int64_t row0 = (int64_t)seg * a.rows + (kMaps ? (int64_t)(index % a.parts) * a.part_rows : 0);
+    const int rows = (int)(min(kMaps ? min(row0 + a.part_rows, (int64_t)(seg + 1) * a.rows) : row0 + a.rows, (int64_t)a.T) - row0);
+    const int tiles = kMaps ? max((rows + kTile - 1) / kTile, 0) : max((rows + kTile - 1) / kTile, 1);       // one at least, for sequences without rows
+    auto tile_row = [&](int i) { return (int)row0 + (kMaps ? tiles - 1 - i : i) * kTile; };
     if (threadIdx.x == 0) {
         for (int i = 0; i < kStages; ++i) mbar_init(&s.full[i], 1);
         s.failed[0] = s.failed[1] = s.begins[0] = s.begins[1] = 0;
@@ -174,9 +179,9 @@ __global__ void __launch_bounds__(kWarps * 32, kCtasOf<kBack>) k_recurrence(cons
     auto copy_next = [&]() {
         if constexpr (kTma) {
             if (copied >= tiles) return;
-            const int u0 = tile_at(copied) * kTile, c = strip * kCols, st = copied % kStages;
+            const int u0 = tile_row(copied), c = strip * kCols, st = copied % kStages;
             const int t = kBack ? a.T - u0 - kTile : u0;         // a first row below 0 reads zeros
-            uint8_t* to = ring + st * kStageBytes;
+            uint8_t* to = ring + st * kStageBytes<kMaps>;
             mbar_expect_tx(&s.full[st], kInput * kInputs);
             tma_load_2d(to + kG * kInput, &tm_g, c, t, &s.full[st]);
             tma_load_2d(to + kIn * kInput, kBack ? &tm_dy : &tm_x, c, t, &s.full[st]);
@@ -195,7 +200,7 @@ __global__ void __launch_bounds__(kWarps * 32, kCtasOf<kBack>) k_recurrence(cons
     float4 behind = make_float4(1.f, 0.f, 1.f, 0.f);             // kMaps, warp 0: of the tiles so far
     float2 start = both(0.f);                                    // else: the state in front of the tile
     if (!kMaps && seg > 0) {
-        const int per = (seg + kWarps - 1) / kWarps, k0 = warp * per, k1 = min(k0 + per, seg);
+        const int all = seg * a.parts, per = (all + kWarps - 1) / kWarps, k0 = warp * per, k1 = min(k0 + per, all);
         const float4* p = a.maps + (size_t)strip * 32 + lane;
         float4 run = make_float4(1.f, 0.f, 1.f, 0.f);
         for (int k = k0; k < k1; k += 8) {
@@ -213,38 +218,48 @@ __global__ void __launch_bounds__(kWarps * 32, kCtasOf<kBack>) k_recurrence(cons
         for (int w = 0; w < kWarps; ++w) start = apply2(s.front[w][lane], start);
     }
 
+    const bool plain_strip = (strip + 1) * kCols <= a.D && a.pairs;
+    int from = 0, to = 0;                                        // a sequence that the warp has met
     int stage = 0;
     uint32_t phase = 0;
     bool failed = false;
     for (int i = 0; i < tiles; ++i) {
-        const int u0 = tile_at(i) * kTile + warp * kRows;        // first row of the warp, in scan order
+        const int u0 = tile_row(i) + warp * kRows;        // first row of the warp, in scan order
         auto row = [&](int r) { return kBack ? a.T - 1 - (u0 + r) : u0 + r; };
-        // ---- which rows are in a sequence, and are the first and last one in scan order
+        // rows inside one sequence, nearly all there are: none needs a look of its own.  Otherwise: which are in a sequence, and which are the
+        // first and last one in scan order
+        const int low = kBack ? a.T - u0 - kRows : u0;
+        bool plain = low > from && low + kRows < to && plain_strip;
         int seq = 0;
-        uint32_t member, first, final;
-        {
+        uint32_t member = 0, first = 0, final = 0;
+        if (!plain) {
+            int b = a.T, e = a.T;
             bool m = false, f = false, l = false;
-            const int low = max(kBack ? a.T - u0 - kRows : u0, 0);
-            const int q0 = sequence_of(a, low);
+            const int q0 = sequence_of(a, max(low, 0));
             if (lane < kRows && u0 + lane < a.T) {
                 const int t = row(lane);
                 seq = sequence_from(a, q0, t);
-                const int from = seq < a.seqs ? begin_of(a, seq) : a.T;
-                m = t >= from;
-                f = m && t == from;
-                l = m && t == begin_of(a, seq + 1) - 1;
+                if (seq < a.seqs) {
+                    b = begin_of(a, seq);
+                    e = begin_of(a, seq + 1);
+                }
+                m = t >= b && t < e;
+                f = m && t == b;
+                l = m && t == e - 1;
             }
             member = __ballot_sync(0xffffffffu, m);
             first = __ballot_sync(0xffffffffu, kBack ? l : f);
             final = __ballot_sync(0xffffffffu, kBack ? f : l);
+            constexpr int kNext = kMaps ? 0 : kRows - 1;         // towards the next tile
+            from = __shfl_sync(0xffffffffu, b, kNext);
+            to = __shfl_sync(0xffffffffu, e, kNext);
+            plain = low > from && low + kRows < to && plain_strip;
         }
-        // rows inside one sequence and whole strips, nearly all there are: no row needs a look of its own
-        const bool plain = member == (kRows == 32 ? 0xffffffffu : (1u << kRows) - 1) && (first | final) == 0 && (strip + 1) * kCols <= a.D && a.pairs;
         // two columns of the r-th row of an input; not for rows of no sequence
         auto fetch = [&](int which, int r) {
             if constexpr (kTma) {
                 const int at = kBack ? kTile - 1 - (warp * kRows + r) : warp * kRows + r;
-                return pair_of(reinterpret_cast<const T*>(ring + stage * kStageBytes + which * kInput) + at * kCols + lane * 2);
+                return pair_of(reinterpret_cast<const T*>(ring + stage * kStageBytes<kMaps> + which * kInput) + at * kCols + lane * 2);
             } else {
                 const void* p = which == kG ? a.g : which == kIn ? (kBack ? a.dy : a.x) : which == kX ? a.x : a.y;
                 const size_t ld = which == kG ? a.ld_g : which == kIn ? (kBack ? a.ld_dy : a.ld_x) : which == kX ? a.ld_x : a.ld_y;
@@ -369,7 +384,7 @@ __global__ void __launch_bounds__(kWarps * 32, kCtasOf<kBack>) k_recurrence(cons
         }
     }
     if constexpr (kMaps) {
-        if (warp == 0 && !failed) a.maps[((size_t)seg * a.strips + strip) * 32 + lane] = behind;
+        if (warp == 0 && !failed) a.maps[((size_t)index * a.strips + strip) * 32 + lane] = behind;
     } else if (seg == 0 && a.after && (a.T == 0 || a.offsets)) { // sequences without rows
         for (int q = warp; q < a.seqs; q += kWarps)
             if (begin_of(a, q + 1) <= begin_of(a, q))
@@ -409,39 +424,52 @@ bool encode_tiles(CUtensorMap* tm, const void* p, size_t ld, size_t es, const Re
 }
 
 // Segments of a strip: as many as fill the GPU once, or twice where that leaves fewer SMs idle.  One where that fills more than 60 % of
-// it, since two and more are read twice (but for what lies in front of a sequence's begin).
-void cut_segments(RecArgs& a, int resident) {
+// it, since two and more are read twice (but for what lies in front of a sequence's begin).  In the first pass, whose CTAs are smaller,
+// a segment is cut again.
+template <typename T, bool kBack>
+void cut_segments(RecArgs& a) {
+    constexpr int kTile = kTileOf<T, kBack, false>, kMapTile = kTileOf<T, kBack, true>, kResident = kSms * kCtasOf<kBack, false>;
+    const int tiles = std::max(1, (a.T + kTile - 1) / kTile);
     int segs = 1;
-    if (a.strips * 10 <= resident * 6) {
-        const int once = resident / a.strips, twice = 2 * resident / a.strips;
+    if (a.strips * 10 <= kResident * 6) {
+        const int once = kResident / a.strips, twice = 2 * kResident / a.strips;
         segs = twice > 2 * once && once < 8 ? twice : once;
     }
-    a.per = (a.tiles + segs - 1) / segs;
-    a.segs = (a.tiles + a.per - 1) / a.per;
+    const int per = (tiles + segs - 1) / segs;
+    a.segs = (tiles + per - 1) / per;
+    a.rows = per * kTile;
+    const int map_tiles = per * (kTile / kMapTile);
+    a.parts = a.segs > 1 ? std::max(1, std::min(kSms * kCtasOf<kBack, true> / ((a.segs - 1) * a.strips), map_tiles)) : 1;
+    a.part_rows = (map_tiles + a.parts - 1) / a.parts * kMapTile;
 }
 
-template <typename T, uint32_t kKind, bool kBack, bool kTma>
-cudaError_t run_passes(const RecArgs& a, const CUtensorMap (&tm)[4], cudaStream_t s) {
-    const size_t smem = kRecSmem + (kTma ? kStagesOf<kBack> * kStageBytes : 0) + 128;
-    cudaError_t e = allow_smem<k_recurrence<T, kKind, kBack, kTma, true>>();
-    if (e == cudaSuccess) e = allow_smem<k_recurrence<T, kKind, kBack, kTma, false>>();
-    if (e == cudaSuccess && a.segs > 1)
-        e = launch_kernel(k_recurrence<T, kKind, kBack, kTma, true>, (a.segs - 1) * a.strips, kWarps * 32, smem, s, true, a, tm[0], tm[1], tm[2], tm[3]);
+template <typename T, uint32_t kKind, bool kBack, bool kTma, bool kMaps>
+cudaError_t run_pass(const RecArgs& a, cudaStream_t s) {
+    constexpr int kTile = kTileOf<T, kBack, kMaps>;
+    CUtensorMap g{}, x{}, dy{}, y{};
+    if (kTma) {
+        bool ok = encode_tiles(&g, a.g, a.ld_g, sizeof(T), a, kTile);
+        if (!kBack || !kMaps) ok = ok && encode_tiles(&x, a.x, a.ld_x, sizeof(T), a, kTile);
+        if (kBack) ok = ok && encode_tiles(&dy, a.dy, a.ld_dy, sizeof(T), a, kTile);
+        if (kBack && !kMaps) ok = ok && encode_tiles(&y, a.y, a.ld_y, sizeof(T), a, kTile);
+        if (!ok) return cudaErrorInvalidValue;
+    }
+    const cudaError_t e = allow_smem<k_recurrence<T, kKind, kBack, kTma, kMaps>>();
     if (e != cudaSuccess) return e;
-    return launch_kernel(k_recurrence<T, kKind, kBack, kTma, false>, a.segs * a.strips, kWarps * 32, smem, s, true, a, tm[0], tm[1], tm[2], tm[3]);
+    return launch_kernel(k_recurrence<T, kKind, kBack, kTma, kMaps>, (kMaps ? (a.segs - 1) * a.parts : a.segs) * a.strips, kWarps * 32,
+                         kRecSmem + (kTma ? kStagesOf<kBack, kMaps> * kStageBytes<kMaps> : 0) + 128, s, true, a, g, x, dy, y);
+}
+template <typename T, uint32_t kKind, bool kBack, bool kTma>
+cudaError_t run_passes(const RecArgs& a, cudaStream_t s) {
+    const cudaError_t e = a.segs > 1 ? run_pass<T, kKind, kBack, kTma, true>(a, s) : cudaSuccess;
+    return e != cudaSuccess ? e : run_pass<T, kKind, kBack, kTma, false>(a, s);
 }
 template <typename T, uint32_t kKind, bool kBack>
 cudaError_t run_tiles(RecArgs a, bool tma, char* workspace, cudaStream_t s) {
-    constexpr int kTile = kTileOf<T, kBack>;
-    a.tiles = std::max(1, (a.T + kTile - 1) / kTile);
     a.strips = (a.D + kCols - 1) / kCols;
-    cut_segments(a, kSms * kCtasOf<kBack>);
+    cut_segments<T, kBack>(a);
     a.maps = reinterpret_cast<float4*>(workspace);
-    CUtensorMap tm[4] = {};
-    if (!tma) return run_passes<T, kKind, kBack, false>(a, tm, s);
-    bool ok = encode_tiles(&tm[0], a.g, a.ld_g, sizeof(T), a, kTile) && encode_tiles(&tm[1], a.x, a.ld_x, sizeof(T), a, kTile);
-    if (kBack) ok = ok && encode_tiles(&tm[2], a.dy, a.ld_dy, sizeof(T), a, kTile) && encode_tiles(&tm[3], a.y, a.ld_y, sizeof(T), a, kTile);
-    return ok ? run_passes<T, kKind, kBack, true>(a, tm, s) : cudaErrorInvalidValue;
+    return tma ? run_passes<T, kKind, kBack, true>(a, s) : run_passes<T, kKind, kBack, false>(a, s);
 }
 template <typename T, uint32_t kKind>
 cudaError_t run_kind(const RecArgs& a, bool back, bool tma, char* ws, cudaStream_t s) {
@@ -493,8 +521,8 @@ using namespace abs_sgd;
 extern "C" size_t abs_recurrence_workspace(uint64_t tokens, uint64_t width) {
     if (tokens > kSizeMax || width > kSizeMax) return 0;
     if (tokens <= (uint64_t)kTileMin) return 0;
-    // maps of the segments but the last: at most twice as many as CTAs fill the GPU
-    const uint64_t strips = (width + kCols - 1) / kCols, most = std::min<uint64_t>(2 * 3 * kSms, (tokens + kTileMin - 1) / kTileMin * strips);
+    // maps of the segments' parts: at most twice as many as the CTAs that fill the GPU
+    const uint64_t strips = (width + kCols - 1) / kCols, most = std::min<uint64_t>(2 * 4 * kSms, (tokens + kTileMin - 1) / kTileMin * strips);
     return up256((size_t)std::max(most, strips) * 32 * sizeof(float4));
 }
 
