@@ -9,6 +9,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <initializer_list>
 
 #include "abs_internal.h"
 #include "abs_llm.h"
@@ -35,13 +36,12 @@ struct LinArgs {
     bf16* z_out;                     // forward
     size_t ld_z;
     int accumulate;
-    int wide;                        // rows of out, res and z are 16-byte aligned
+    int wide;                        // what the rows of out, res and z are aligned to: 32, 16 bytes, or 0: less
 };
 
 // ---- activations, two numbers at a time
 // Phi(-|z|) = exp(-z^2 / 2) P(1 / (1 + 0.35 |z|)) with P of degree 7 fitted to the smallest relative error over 0 <= |z| <= 13.5 (beyond, the
-// exponential underflows): 3e-7, in fp32 6e-7, so that the lower tail keeps its precision.  17 instructions a number less than through
-// the error function.  E: 2^24 times the exponential (which then stays above the unit's flush to zero), q: Phi(-|z|), m: |z| up to 14 (q is next to
+// exponential underflows), so that the lower tail keeps its precision: 3e-7, in fp32 6e-7.  E: 2^24 times the exponential (which then stays above the unit's flush to zero), q: Phi(-|z|), m: |z| up to 14 (q is next to
 // nothing from there on, also times an infinity).
 __device__ __forceinline__ void normal_tail(float2 z, float2& E, float2& q, float2& m) {
     const float2 w = make_float2(fabsf(z.x), fabsf(z.y)), d = fma2(w, both(0.35f), both(1.f));
@@ -50,7 +50,8 @@ __device__ __forceinline__ void normal_tail(float2 z, float2& E, float2& q, floa
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(t.y) : "f"(d.y));
     E = exp2_of(fma2(mul2(z, z), both(-0.72134752044448170f), both(24.f)));
     constexpr float k = 0x1p-24f;
-    float2 p = fma2(t, both(0.04894255149557414f * k), both(-0.20211968521483073f * k));
+    float2 p;
+    p = fma2(t, both(0.04894255149557414f * k), both(-0.20211968521483073f * k));
     p = fma2(p, t, both(0.24064142309471856f * k));
     p = fma2(p, t, both(-0.017023902126677096f * k));
     p = fma2(p, t, both(0.15596167730976151f * k));
@@ -102,16 +103,35 @@ __device__ __forceinline__ float2 slope(float2 z) {
     return both(1.f);
 }
 
-// Eight elements of a row, 16-byte aligned.
-template <typename T>
-struct Row8 {
-    static constexpr int kN = 8 / kVec<T>;
+// kC consecutive elements of a row; `to32`: 32-byte aligned, otherwise 16-byte.
+template <typename T, int kC>
+struct Piece {
+    static constexpr int kN = kC / kVec<T>;
     uint4 w[kN];
-    __device__ __forceinline__ void load(const T* p) {
+    __device__ __forceinline__ void load(const T* p, bool to32) {
+        if (kN % 2 == 0 && to32) {
 #pragma unroll
-        for (int h = 0; h < kN; ++h) w[h] = *reinterpret_cast<const uint4*>(p + h * kVec<T>);
+            for (int h = 0; h + 1 < kN; h += 2)
+                asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                             : "=r"(w[h].x), "=r"(w[h].y), "=r"(w[h].z), "=r"(w[h].w), "=r"(w[h + 1].x), "=r"(w[h + 1].y), "=r"(w[h + 1].z), "=r"(w[h + 1].w)
+                             : "l"(p + h * kVec<T>) : "memory");
+        } else {
+#pragma unroll
+            for (int h = 0; h < kN; ++h) w[h] = *reinterpret_cast<const uint4*>(p + h * kVec<T>);
+        }
     }
-    __device__ __forceinline__ void get(float2 (&v)[4]) const {
+    __device__ __forceinline__ void store(T* p, bool to32) const {
+        if (kN % 2 == 0 && to32) {
+#pragma unroll
+            for (int h = 0; h + 1 < kN; h += 2)
+                asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p + h * kVec<T>), "r"(w[h].x), "r"(w[h].y), "r"(w[h].z), "r"(w[h].w),
+                             "r"(w[h + 1].x), "r"(w[h + 1].y), "r"(w[h + 1].z), "r"(w[h + 1].w) : "memory");
+        } else {
+#pragma unroll
+            for (int h = 0; h < kN; ++h) *reinterpret_cast<uint4*>(p + h * kVec<T>) = w[h];
+        }
+    }
+    __device__ __forceinline__ void get(float2 (&v)[kC / 2]) const {
 #pragma unroll
         for (int h = 0; h < kN; ++h) {
             float2 u[kPairs<T>];
@@ -120,7 +140,7 @@ struct Row8 {
             for (int i = 0; i < kPairs<T>; ++i) v[h * kPairs<T> + i] = u[i];
         }
     }
-    __device__ __forceinline__ void put(const float2 (&v)[4]) {
+    __device__ __forceinline__ void put(const float2 (&v)[kC / 2]) {
 #pragma unroll
         for (int h = 0; h < kN; ++h) {
             float2 u[kPairs<T>];
@@ -129,48 +149,47 @@ struct Row8 {
             w[h] = pack(u, T());
         }
     }
-    __device__ __forceinline__ void store(T* p) const {
-#pragma unroll
-        for (int h = 0; h < kN; ++h) *reinterpret_cast<uint4*>(p + h * kVec<T>) = w[h];
-    }
 };
 
-// The layer's work on eight sums of a row, all of them inside the matrix: what it reads, then what it makes of the sums.
-template <int kEpi, uint32_t kAct, typename T>
+// The layer's work on kC sums of a row, all of them inside the matrix: what it reads, then what it makes of the sums.
+template <int kEpi, uint32_t kAct, typename T, int kC>
 struct Finish {
-    Row8<T> r;                       // residual, or what dw holds
-    Row8<bf16> z;
+    Piece<T, kC> r;                  // residual, or what dw holds
+    Piece<bf16, kC> z;
     __device__ __forceinline__ void load(const LinArgs& a, int row, int col) {
         if (kEpi == kWgrad ? a.accumulate != 0 : a.res != nullptr)
-            r.load(kEpi == kWgrad ? static_cast<const T*>(a.out) + (size_t)row * a.ld + col : static_cast<const T*>(a.res) + (size_t)row * a.ld_res + col);
-        if (kEpi == kDgrad && kAct != ABS_ACT_NONE) z.load(a.z_in + (size_t)row * a.ld_z + col);
+            r.load(kEpi == kWgrad ? static_cast<const T*>(a.out) + (size_t)row * a.ld + col : static_cast<const T*>(a.res) + (size_t)row * a.ld_res + col, a.wide == 32);
+        if (kEpi == kDgrad && kAct != ABS_ACT_NONE) z.load(a.z_in + (size_t)row * a.ld_z + col, a.wide == 32);
     }
-    __device__ __forceinline__ void operator()(const LinArgs& a, int row, int col, const float2 (&bias)[4], float2 (&v)[4]) {
-        float2 w[4];
+    __device__ __forceinline__ void operator()(const LinArgs& a, int row, int col, float2 (&v)[kC / 2]) {
+        float2 w[kC / 2];
         if (kEpi == kForward) {
+            if (a.bias) {
+                const float* b = a.bias + col;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = add2(v[i], bias[i]);
+                for (int i = 0; i < kC / 2; ++i) v[i] = add2(v[i], make_float2(__ldg(b + 2 * i), __ldg(b + 2 * i + 1)));
+            }
             if (a.z_out) {
-                Row8<bf16> o;
+                Piece<bf16, kC> o;
                 o.put(v);
-                o.store(a.z_out + (size_t)row * a.ld_z + col);
+                o.store(a.z_out + (size_t)row * a.ld_z + col, a.wide == 32);
             }
 #pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = activate<kAct>(v[i]);
+            for (int i = 0; i < kC / 2; ++i) v[i] = activate<kAct>(v[i]);
         }
         if (kEpi == kDgrad && kAct != ABS_ACT_NONE) {
             z.get(w);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = mul2(v[i], slope<kAct>(w[i]));
+            for (int i = 0; i < kC / 2; ++i) v[i] = mul2(v[i], slope<kAct>(w[i]));
         }
         if (kEpi == kWgrad ? a.accumulate != 0 : a.res != nullptr) {
             r.get(w);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = add2(v[i], w[i]);
+            for (int i = 0; i < kC / 2; ++i) v[i] = add2(v[i], w[i]);
         }
-        Row8<T> o;
+        Piece<T, kC> o;
         o.put(v);
-        o.store(static_cast<T*>(a.out) + (size_t)row * a.ld + col);
+        o.store(static_cast<T*>(a.out) + (size_t)row * a.ld + col, a.wide == 32);
     }
 };
 // The same for a single one.
@@ -204,11 +223,20 @@ __device__ __forceinline__ void finish_one(const LinArgs& a, int row, int col, f
 // Launched in plain stream order, and starts no successor early (see llm_ckpt8.cu).  Every wait on a barrier is bounded.
 // ------------------------------------------------------------------------------------------------
 constexpr int kTM = 256, kTN = 256, kTK = 64;    // of a pair
-constexpr int kStages = 4, kEpiWarps = 16, kThreads = 64 + kEpiWarps * 32;
+constexpr int kStages = 5;
 constexpr int kHalf = kTK * 128 * 2;             // bytes of an operand's share of a CTA and run
-constexpr int kPitch = 36;                       // floats of a staged row: 16-byte pieces, eight rows on different banks
-constexpr int kWarpCols = kTN / (kEpiWarps / 4); // columns of an epilogue warp
+constexpr int kPitch = 20;                       // floats of a staged row of 16: 16-byte pieces, eight rows on different banks
 constexpr int kSegmentRuns = 12;
+// fp32 outputs: sums out of TMEM every kSegmentRuns runs.  bf16 ones are rounded to 2^-9 anyway, and go straight from TMEM: without the sums the
+// epilogue's registers do not spill.
+template <typename T>
+constexpr bool kSum = sizeof(T) == 4;
+template <typename T>
+constexpr int kEpiWarps = kSum<T> ? 8 : 16;
+template <typename T>
+constexpr int kWarpCols = kTN / (kEpiWarps<T> / 4);  // columns of an epilogue warp
+template <typename T>
+constexpr int kThreads = 64 + kEpiWarps<T> * 32;
 constexpr int kSms = 148;
 constexpr uint64_t kSizeMax = 0x7fffffc0ull;
 constexpr int kMinRuns = 12;     // runs of 64 that a part of a cut tile has at least
@@ -216,7 +244,7 @@ constexpr int kMinRuns = 12;     // runs of 64 that a part of a cut tile has at 
 struct LinSmem {
     alignas(1024) uint8_t a[kStages][kHalf];
     alignas(1024) uint8_t b[kStages][kHalf];
-    alignas(16) float out[kEpiWarps][32 * kPitch];
+    alignas(16) float out[16][32 * kPitch];
     alignas(8) uint64_t full[kStages];       // first CTA: both CTAs' copies of a run have landed
     uint64_t empty[kStages];                 // the run's MMAs have read both CTAs' operands
     uint64_t acc_full[2];
@@ -276,9 +304,10 @@ __device__ __forceinline__ uint64_t operand_desc(uint32_t at, int k16) {
 }
 
 template <int kEpi, uint32_t kAct, typename T>
-__global__ void __launch_bounds__(kThreads, 1) k_linear(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_b,
+__global__ void __launch_bounds__(kThreads<T>, 1) k_linear(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_b,
                                                         const __grid_constant__ LinArgs a) {
     constexpr bool kAMn = kEpi == kWgrad, kBMn = kEpi != kDgrad;
+    constexpr int kSegment = kSum<T> ? kSegmentRuns : 1 << 30;       // runs that the tensor core adds up on its own
     extern __shared__ uint8_t smem_raw[];
     LinSmem& s = *reinterpret_cast<LinSmem*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
@@ -297,7 +326,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_linear(const __grid_constant__ 
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(&s.acc_full[i], 1);
-            mbar_init(&s.acc_empty[i], 2 * kEpiWarps);       // the epilogue warps of each CTA
+            mbar_init(&s.acc_empty[i], 2 * kEpiWarps<T>);       // the epilogue warps of each CTA
         }
         s.failed = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -356,8 +385,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_linear(const __grid_constant__ 
             bool ok = true;
             for (int it = pair; it < items && ok; it += pairs) {
                 const Item q = item_of(it);
-                for (int kb0 = q.kb0; kb0 < q.kb1 && ok; kb0 += kSegmentRuns, ++i) {
-                    const int ab = i & 1, kb1 = min(q.kb1, kb0 + kSegmentRuns);
+                for (int kb0 = q.kb0; kb0 < q.kb1 && ok; kb0 += min(kSegment, q.kb1 - kb0), ++i) {
+                    const int ab = i & 1, kb1 = kb0 + min(kSegment, q.kb1 - kb0);
                     if (i >= 2 && !mbar_wait(&s.acc_empty[ab], ((i / 2) - 1) & 1)) { ok = false; break; }
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                     for (int kb = kb0; kb < kb1; ++kb) {
@@ -376,89 +405,104 @@ __global__ void __launch_bounds__(kThreads, 1) k_linear(const __grid_constant__ 
             if (!ok) *failed = 1;
         }
         __syncwarp();
-    } else {                                         // ---- epilogue: four warps for the rows, four times 64 columns
-        const int qd = warp % 4, part_col = (warp - 2) / 4 * kWarpCols;
+    } else {                                         // ---- epilogue: four warps for the rows, kWarpCols columns each
+        const int qd = warp % 4, part_col = (warp - 2) / 4 * kWarpCols<T>;
         float* stage = s.out[warp - 2];
         const int row = rank * 128 + qd * 32;        // of the tile
+        const uint32_t lanes = tmem + ((uint32_t)(qd * 32) << 16) + (uint32_t)part_col;
         int i = 0;
         bool ok = true;
         for (int it = pair; it < items && ok; it += pairs) {
             const Item q = item_of(it);
-            float2 sum[kWarpCols / 32][16];
+            float* part = q.part >= 0 ? a.part + ((size_t)q.part * kTM + row) * kTN + part_col : nullptr;
+            const int rows = min(32, a.M - (q.m0 + row)), col0 = q.n0 + part_col, cols = min(kWarpCols<T>, a.N - col0);
+            using Work = Finish<kEpi, kAct, T, 16>;
+            const bool mine = lane < rows;           // a thread has a row of the tile
+            auto whole = [&](int c) { return a.wide && !part && c * 16 + 16 <= cols; };
+            auto load = [&](Work& f, int c) {
+                if (whole(c) && mine) f.load(a, q.m0 + row + lane, col0 + c * 16);
+            };
+            // the 16 columns of chunk c
+            auto emit = [&](Work& f, int c, float2 (&v)[8]) {
+                if (c * 16 >= cols) return;
+                if (part) {
+                    if (mine)
 #pragma unroll
-            for (int c = 0; c < kWarpCols / 32; ++c)
+                        for (int j = 0; j < 4; ++j)
+                            *reinterpret_cast<float4*>(part + (size_t)lane * kTN + c * 16 + 4 * j) = make_float4(v[2 * j].x, v[2 * j].y, v[2 * j + 1].x, v[2 * j + 1].y);
+                } else if (whole(c)) {
+                    if (mine) f(a, q.m0 + row + lane, col0 + c * 16, v);
+                } else {                             // a column a thread, two rows at a time, through the staging tile
 #pragma unroll
-                for (int j = 0; j < 16; ++j) sum[c][j] = both(0.f);
-            for (int kb0 = q.kb0; kb0 < q.kb1; kb0 += kSegmentRuns, ++i) {
+                    for (int j = 0; j < 4; ++j)
+                        *reinterpret_cast<float4*>(stage + lane * kPitch + 4 * j) = make_float4(v[2 * j].x, v[2 * j].y, v[2 * j + 1].x, v[2 * j + 1].y);
+                    __syncwarp();
+                    const int col = col0 + c * 16 + lane % 16;
+                    if (c * 16 + lane % 16 < cols) {
+                        const float bias = kEpi == kForward && a.bias ? __ldg(a.bias + col) : 0.f;
+#pragma unroll 4
+                        for (int k = lane / 16; k < rows; k += 2) finish_one<kEpi, kAct, T>(a, q.m0 + row + k, col, bias, stage[k * kPitch + lane % 16]);
+                    }
+                    __syncwarp();
+                }
+            };
+            if constexpr (kSum<T>) {
+                float2 sum[kWarpCols<T> / 16][8];
+#pragma unroll
+                for (int c = 0; c < kWarpCols<T> / 16; ++c)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) sum[c][j] = both(0.f);
+                for (int kb0 = q.kb0; kb0 < q.kb1; kb0 += kSegmentRuns, ++i) {
+                    const int ab = i & 1;
+                    ok = __all_sync(0xffffffffu, mbar_wait(&s.acc_full[ab], (i / 2) & 1) && !*failed);
+                    if (!ok) break;
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+#pragma unroll
+                    for (int c = 0; c < kWarpCols<T> / 16; ++c) {
+                        uint32_t v[16];
+                        tmem_ld_16(lanes + (uint32_t)(ab * kTN + c * 16), v);
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) sum[c][j] = add2(sum[c][j], make_float2(__uint_as_float(v[2 * j]), __uint_as_float(v[2 * j + 1])));
+                    }
+                    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0) arrive_first(&s.acc_empty[ab]);
+                }
+                if (!ok) break;
+                Work f;
+#pragma unroll
+                for (int c = 0; c < kWarpCols<T> / 16; ++c) {
+                    load(f, c);
+                    emit(f, c, sum[c]);
+                }
+            } else {
                 const int ab = i & 1;
+                Work f, next;
+                load(f, 0);                          // while the product runs
                 ok = __all_sync(0xffffffffu, mbar_wait(&s.acc_full[ab], (i / 2) & 1) && !*failed);
                 if (!ok) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll
-                for (int c = 0; c < kWarpCols / 16; ++c) {
-                    uint32_t v[16];
-                    tmem_ld_16(tmem + ((uint32_t)(qd * 32) << 16) + (uint32_t)(ab * kTN + part_col + c * 16), v);
-#pragma unroll
-                    for (int j = 0; j < 8; ++j)
-                        sum[c / 2][c % 2 * 8 + j] = add2(sum[c / 2][c % 2 * 8 + j], make_float2(__uint_as_float(v[2 * j]), __uint_as_float(v[2 * j + 1])));
-                }
-                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-                __syncwarp();
-                if (lane == 0) arrive_first(&s.acc_empty[ab]);
-            }
-            if (!ok) {
-                *failed = 1;
-                break;
-            }
-            float* part = q.part >= 0 ? a.part + ((size_t)q.part * kTM + row) * kTN + part_col : nullptr;
-            const int rows = min(32, a.M - (q.m0 + row)), col0 = q.n0 + part_col, cols = min(kWarpCols, a.N - col0);
-#pragma unroll
-            for (int c = 0; c < kWarpCols / 32; ++c) {
-                if (c * 32 >= cols || rows <= 0) continue;
-#pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    *reinterpret_cast<float4*>(stage + lane * kPitch + 4 * j) = make_float4(sum[c][2 * j].x, sum[c][2 * j].y, sum[c][2 * j + 1].x, sum[c][2 * j + 1].y);
-                __syncwarp();
-                const int cc = c * 32 + lane % 4 * 8;
-                if (part) {
-#pragma unroll
-                    for (int p = 0; p < 4; ++p) {
-                        const int r = p * 8 + lane / 4;
-                        if (r >= rows || cc >= cols) continue;
-                        float* to = part + (size_t)r * kTN + cc;
-                        *reinterpret_cast<float4*>(to) = *reinterpret_cast<const float4*>(stage + r * kPitch + lane % 4 * 8);
-                        *reinterpret_cast<float4*>(to + 4) = *reinterpret_cast<const float4*>(stage + r * kPitch + lane % 4 * 8 + 4);
+                for (int c = 0; c < kWarpCols<T> / 16; ++c) {
+                    uint32_t u[16];
+                    tmem_ld_16(lanes + (uint32_t)(ab * kTN + c * 16), u);
+                    if (c == kWarpCols<T> / 16 - 1) {
+                        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                        __syncwarp();
+                        if (lane == 0) arrive_first(&s.acc_empty[ab]);
+                    } else {
+                        load(next, c + 1);
                     }
-                } else if (a.wide && c * 32 + 32 <= cols) {
-                    float2 bias[4];
+                    float2 v[8];
 #pragma unroll
-                    for (int k = 0; k < 4; ++k)
-                        bias[k] = kEpi == kForward && a.bias ? make_float2(__ldg(a.bias + col0 + cc + 2 * k), __ldg(a.bias + col0 + cc + 2 * k + 1)) : both(0.f);
-#pragma unroll
-                    for (int p = 0; p < 4; p += 2) {
-                        Finish<kEpi, kAct, T> f[2];  // the reads of two rows are in flight together
-#pragma unroll
-                        for (int h = 0; h < 2; ++h)
-                            if ((p + h) * 8 + lane / 4 < rows) f[h].load(a, q.m0 + row + (p + h) * 8 + lane / 4, col0 + cc);
-#pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-                            const int r = (p + h) * 8 + lane / 4;
-                            if (r >= rows) continue;
-                            const float4 lo = *reinterpret_cast<const float4*>(stage + r * kPitch + lane % 4 * 8);
-                            const float4 hi = *reinterpret_cast<const float4*>(stage + r * kPitch + lane % 4 * 8 + 4);
-                            float2 v[4] = {make_float2(lo.x, lo.y), make_float2(lo.z, lo.w), make_float2(hi.x, hi.y), make_float2(hi.z, hi.w)};
-                            f[h](a, q.m0 + row + r, col0 + cc, bias, v);
-                        }
-                    }
-                } else if (c * 32 + lane < cols) {   // a column a thread
-                    const int col = col0 + c * 32 + lane;
-                    const float bias = kEpi == kForward && a.bias ? __ldg(a.bias + col) : 0.f;
-#pragma unroll 4
-                    for (int r = 0; r < rows; ++r) finish_one<kEpi, kAct, T>(a, q.m0 + row + r, col, bias, stage[r * kPitch + lane]);
+                    for (int j = 0; j < 8; ++j) v[j] = make_float2(__uint_as_float(u[2 * j]), __uint_as_float(u[2 * j + 1]));
+                    emit(f, c, v);
+                    f = next;
                 }
-                __syncwarp();
+                ++i;
             }
         }
+        if (!ok) *failed = 1;
     }
     __syncwarp();
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -478,7 +522,7 @@ __global__ void __launch_bounds__(256) k_linear_join(const __grid_constant__ Lin
         const int tile = a.whole + i / kTM, row = tile / a.tiles_n * kTM + i % kTM, col = tile % a.tiles_n * kTN + lane * 8, n = min(8, a.N - col);
         if (row >= a.M || n <= 0) continue;
         const bool wide = a.wide && n == 8;
-        Finish<kEpi, kAct, T> f;
+        Finish<kEpi, kAct, T, 8> f;
         if (wide) f.load(a, row, col);
         float2 v[4] = {};
         const float* p = a.part + (size_t)i * kTN + lane * 8;
@@ -490,17 +534,14 @@ __global__ void __launch_bounds__(256) k_linear_join(const __grid_constant__ Lin
             v[2] = add2(v[2], make_float2(hi.x, hi.y));
             v[3] = add2(v[3], make_float2(hi.z, hi.w));
         }
-        float2 bias[4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-            bias[k] = kEpi == kForward && a.bias ? make_float2(2 * k < n ? a.bias[col + 2 * k] : 0.f, 2 * k + 1 < n ? a.bias[col + 2 * k + 1] : 0.f) : both(0.f);
         if (wide) {
-            f(a, row, col, bias, v);
+            f(a, row, col, v);
         } else {
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                if (2 * k < n) finish_one<kEpi, kAct, T>(a, row, col + 2 * k, bias[k].x, v[k].x);
-                if (2 * k + 1 < n) finish_one<kEpi, kAct, T>(a, row, col + 2 * k + 1, bias[k].y, v[k].y);
+                auto bias = [&](int c) { return kEpi == kForward && a.bias ? a.bias[c] : 0.f; };
+                if (2 * k < n) finish_one<kEpi, kAct, T>(a, row, col + 2 * k, bias(col + 2 * k), v[k].x);
+                if (2 * k + 1 < n) finish_one<kEpi, kAct, T>(a, row, col + 2 * k + 1, bias(col + 2 * k + 1), v[k].y);
             }
         }
     }
@@ -530,8 +571,8 @@ __global__ void __launch_bounds__(256) k_bias_part(const bf16* dy, size_t ld, in
             const bf16* p = dy + (size_t)t * ld + col;
             if (wide && n == 8) {
                 float2 v[4];
-                Row8<bf16> w;
-                w.load(p);
+                Piece<bf16, 8> w;
+                w.load(p, false);
                 w.get(v);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) sum[i] += i % 2 ? v[i / 2].y : v[i / 2].x;
@@ -573,17 +614,17 @@ __global__ void __launch_bounds__(256) k_activation_backward(const T* dy, size_t
         const bf16* q = z + t * ld_z + c;
         bf16* o = dz + t * ld_dz + c;
         if (wide && n == 8) {
-            Row8<T> g;
-            Row8<bf16> w;
+            Piece<T, 8> g;
+            Piece<bf16, 8> w;
             float2 v[4], u[4];
-            g.load(p);
-            w.load(q);
+            g.load(p, false);
+            w.load(q, false);
             g.get(v);
             w.get(u);
 #pragma unroll
             for (int k = 0; k < 4; ++k) v[k] = mul2(v[k], slope<kAct>(u[k]));
             w.put(v);
-            w.store(o);
+            w.store(o, false);
         } else {
             for (int k = 0; k < n; ++k) o[k] = __float2bfloat16_rn(to_f(p[k]) * slope<kAct>(both(__bfloat162float(q[k]))).x);
         }
@@ -644,7 +685,7 @@ cudaError_t run_act(const CUtensorMap& ta, const CUtensorMap& tb, const LinArgs&
     cudaError_t e = allow_smem<k_linear<kEpi, kAct, T>>();
     if (e != cudaSuccess) return e;
     const int grid = 2 * std::min(a.whole + a.rest * a.splits, kSms / 2);
-    e = launch_cluster(k_linear<kEpi, kAct, T>, grid, 2, kThreads, sizeof(LinSmem) + 1024, s, ta, tb, a);
+    e = launch_cluster(k_linear<kEpi, kAct, T>, grid, 2, kThreads<T>, sizeof(LinSmem) + 1024, s, ta, tb, a);
     if (e == cudaSuccess && a.splits > 1) e = launch_kernel(k_linear_join<kEpi, kAct, T>, std::min(a.rest * kTM / 8, kSms * 8), 256, 0, s, false, a);
     return e;
 }
@@ -695,6 +736,13 @@ const char* check_sizes(uint64_t tokens, uint64_t in, uint64_t out, uint32_t dty
     *code = ABS_ELIMIT;
     return "a size exceeds 2^31 - 64";
 }
+// What the rows of these matrices are aligned to: 32, 16 bytes, or 0.
+int alignment(std::initializer_list<MatrixArg> all) {
+    int to = 32;
+    for (const MatrixArg& m : all)
+        while (to && !rows_at(m, to)) to = to == 32 ? 16 : 0;
+    return to;
+}
 // An operand of the product must not be an output.
 const char* check_operands(const void* const (&out)[2], const void* a, const void* b) {
     for (const void* o : out)
@@ -743,7 +791,7 @@ extern "C" int abs_linear(const void* x, uint64_t ld_x, const void* w, uint64_t 
     if (const char* why = check_workspace(p, workspace, workspace_bytes, &code)) return thread_error(code, why);
     LinArgs a{};
     a.out = y; a.ld = ld_y; a.bias = bias; a.res = residual; a.ld_res = ld_residual; a.z_out = static_cast<bf16*>(z); a.ld_z = ld_z;
-    a.wide = rows_at(m[2], 16) && rows_at(m[3], 16) && rows_at(m[4], 16);
+    a.wide = alignment({m[2], m[3], m[4]});
     return product(kForward, act, dtype, oa, ob, tokens, out, in, p, a, static_cast<char*>(workspace), static_cast<cudaStream_t>(stream));
 }
 
@@ -773,7 +821,7 @@ extern "C" int abs_linear_dgrad(const void* dy, uint64_t ld_dy, const void* w, u
     if (const char* why = check_workspace(p, workspace, workspace_bytes, &code)) return thread_error(code, why);
     LinArgs a{};
     a.out = dx; a.ld = ld_dx; a.res = residual; a.ld_res = ld_residual; a.z_in = static_cast<const bf16*>(z); a.ld_z = ld_z;
-    a.wide = rows_at(m[2], 16) && rows_at(m[3], 16) && rows_at(m[4], 16);
+    a.wide = alignment({m[2], m[3], m[4]});
     return product(kDgrad, act, dtype, oa, ob, tokens, in, out, p, a, static_cast<char*>(workspace), static_cast<cudaStream_t>(stream));
 }
 
@@ -821,7 +869,7 @@ extern "C" int abs_linear_wgrad(const void* x, uint64_t ld_x, const void* dy, ui
         if (e != cudaSuccess) return thread_error(ABS_ECUDA, cudaGetErrorString(e));
     }
     LinArgs a{};
-    a.out = dw; a.ld = ld_dw; a.accumulate = accumulate != 0; a.wide = rows_at(m[2], 16);
+    a.out = dw; a.ld = ld_dw; a.accumulate = accumulate != 0; a.wide = alignment({m[2]});
     return product(kWgrad, ABS_ACT_NONE, ABS_F32, oa, ob, in, out, tokens, p, a, static_cast<char*>(workspace), s);
 }
 
