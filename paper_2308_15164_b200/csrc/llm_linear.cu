@@ -15,7 +15,7 @@
 #include "abs_llm.h"
 #include "llm_host.h"
 #include "llm_status.cuh"
-#include "row_ops.cuh"
+#include "row_ring.cuh"
 #include "tcgen05.cuh"
 
 namespace abs_sgd {
@@ -192,23 +192,25 @@ struct Finish {
         o.store(static_cast<T*>(a.out) + (size_t)row * a.ld + col, a.wide == 32);
     }
 };
-// The same for a single one.
+// The same for single ones.
 template <int kEpi, uint32_t kAct, typename T>
-__device__ __forceinline__ void finish_one(const LinArgs& a, int row, int col, float bias, float v) {
-    T* out = static_cast<T*>(a.out) + (size_t)row * a.ld + col;
-    if (kEpi == kForward) {
-        v += bias;
-        if (a.z_out) a.z_out[(size_t)row * a.ld_z + col] = __float2bfloat16_rn(v);
-        v = activate<kAct>(both(v)).x;
+struct FinishOne {
+    float r, z;
+    __device__ __forceinline__ void load(const LinArgs& a, int row, int col) {
+        if (kEpi == kWgrad) r = a.accumulate ? to_f(static_cast<const T*>(a.out)[(size_t)row * a.ld + col]) : 0.f;
+        else r = a.res ? to_f(static_cast<const T*>(a.res)[(size_t)row * a.ld_res + col]) : 0.f;
+        if (kEpi == kDgrad && kAct != ABS_ACT_NONE) z = __bfloat162float(a.z_in[(size_t)row * a.ld_z + col]);
     }
-    if (kEpi == kDgrad && kAct != ABS_ACT_NONE) v *= slope<kAct>(both(__bfloat162float(a.z_in[(size_t)row * a.ld_z + col]))).x;
-    if (kEpi == kWgrad) {
-        if (a.accumulate) v += to_f(*out);
-    } else if (a.res) {
-        v += to_f(static_cast<const T*>(a.res)[(size_t)row * a.ld_res + col]);
+    __device__ __forceinline__ void operator()(const LinArgs& a, int row, int col, float bias, float v) {
+        if (kEpi == kForward) {
+            v += bias;
+            if (a.z_out) a.z_out[(size_t)row * a.ld_z + col] = __float2bfloat16_rn(v);
+            v = activate<kAct>(both(v)).x;
+        }
+        if (kEpi == kDgrad && kAct != ABS_ACT_NONE) v *= slope<kAct>(both(z)).x;
+        static_cast<T*>(a.out)[(size_t)row * a.ld + col] = from_f<T>(v + r);
     }
-    *out = from_f<T>(v);
-}
+};
 
 // ------------------------------------------------------------------------------------------------
 // Two CTAs (two SMs) share an output tile of 256 x 256: each holds the operand's 128 rows of A and 128 columns of B, 32 KB for a run of
@@ -416,11 +418,12 @@ __global__ void __launch_bounds__(kThreads<T>, 1) k_linear(const __grid_constant
             const Item q = item_of(it);
             float* part = q.part >= 0 ? a.part + ((size_t)q.part * kTM + row) * kTN + part_col : nullptr;
             const int rows = min(32, a.M - (q.m0 + row)), col0 = q.n0 + part_col, cols = min(kWarpCols<T>, a.N - col0);
-            using Work = Finish<kEpi, kAct, T, 16>;
+            constexpr int kC = kSum<T> ? 8 : 16;     // columns at a time, as the registers allow
+            using Work = Finish<kEpi, kAct, T, kC>;
             const bool mine = lane < rows;           // a thread has a row of the tile
             auto whole = [&](int c) { return a.wide && !part && c * 16 + 16 <= cols; };
-            auto load = [&](Work& f, int c) {
-                if (whole(c) && mine) f.load(a, q.m0 + row + lane, col0 + c * 16);
+            auto load = [&](Work& f, int c, int half) {
+                if (whole(c) && mine) f.load(a, q.m0 + row + lane, col0 + c * 16 + half * 8);
             };
             // the 16 columns of chunk c
             auto emit = [&](Work& f, int c, float2 (&v)[8]) {
@@ -431,7 +434,16 @@ __global__ void __launch_bounds__(kThreads<T>, 1) k_linear(const __grid_constant
                         for (int j = 0; j < 4; ++j)
                             *reinterpret_cast<float4*>(part + (size_t)lane * kTN + c * 16 + 4 * j) = make_float4(v[2 * j].x, v[2 * j].y, v[2 * j + 1].x, v[2 * j + 1].y);
                 } else if (whole(c)) {
-                    if (mine) f(a, q.m0 + row + lane, col0 + c * 16, v);
+                    if constexpr (kC == 16) {
+                        if (mine) f(a, q.m0 + row + lane, col0 + c * 16, v);
+                    } else {
+#pragma unroll
+                        for (int half = 0; half < 2; ++half) {
+                            float2 u[4] = {v[half * 4], v[half * 4 + 1], v[half * 4 + 2], v[half * 4 + 3]};
+                            load(f, c, half);
+                            if (mine) f(a, q.m0 + row + lane, col0 + c * 16 + half * 8, u);
+                        }
+                    }
                 } else {                             // a column a thread, two rows at a time, through the staging tile
 #pragma unroll
                     for (int j = 0; j < 4; ++j)
@@ -440,8 +452,16 @@ __global__ void __launch_bounds__(kThreads<T>, 1) k_linear(const __grid_constant
                     const int col = col0 + c * 16 + lane % 16;
                     if (c * 16 + lane % 16 < cols) {
                         const float bias = kEpi == kForward && a.bias ? __ldg(a.bias + col) : 0.f;
-#pragma unroll 4
-                        for (int k = lane / 16; k < rows; k += 2) finish_one<kEpi, kAct, T>(a, q.m0 + row + k, col, bias, stage[k * kPitch + lane % 16]);
+#pragma unroll 1
+                        for (int k0 = lane / 16; k0 < rows; k0 += 16) {
+                            FinishOne<kEpi, kAct, T> one[8];         // the reads of eight rows are in flight together
+#pragma unroll
+                            for (int k = 0; k < 8; ++k)
+                                if (k0 + 2 * k < rows) one[k].load(a, q.m0 + row + k0 + 2 * k, col);
+#pragma unroll
+                            for (int k = 0; k < 8; ++k)
+                                if (k0 + 2 * k < rows) one[k](a, q.m0 + row + k0 + 2 * k, col, bias, stage[(k0 + 2 * k) * kPitch + lane % 16]);
+                        }
                     }
                     __syncwarp();
                 }
@@ -471,14 +491,11 @@ __global__ void __launch_bounds__(kThreads<T>, 1) k_linear(const __grid_constant
                 if (!ok) break;
                 Work f;
 #pragma unroll
-                for (int c = 0; c < kWarpCols<T> / 16; ++c) {
-                    load(f, c);
-                    emit(f, c, sum[c]);
-                }
+                for (int c = 0; c < kWarpCols<T> / 16; ++c) emit(f, c, sum[c]);
             } else {
                 const int ab = i & 1;
                 Work f, next;
-                load(f, 0);                          // while the product runs
+                load(f, 0, 0);                       // while the product runs
                 ok = __all_sync(0xffffffffu, mbar_wait(&s.acc_full[ab], (i / 2) & 1) && !*failed);
                 if (!ok) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
@@ -491,7 +508,7 @@ __global__ void __launch_bounds__(kThreads<T>, 1) k_linear(const __grid_constant
                         __syncwarp();
                         if (lane == 0) arrive_first(&s.acc_empty[ab]);
                     } else {
-                        load(next, c + 1);
+                        load(next, c + 1, 0);
                     }
                     float2 v[8];
 #pragma unroll
@@ -538,68 +555,74 @@ __global__ void __launch_bounds__(256) k_linear_join(const __grid_constant__ Lin
             f(a, row, col, v);
         } else {
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                auto bias = [&](int c) { return kEpi == kForward && a.bias ? a.bias[c] : 0.f; };
-                if (2 * k < n) finish_one<kEpi, kAct, T>(a, row, col + 2 * k, bias(col + 2 * k), v[k].x);
-                if (2 * k + 1 < n) finish_one<kEpi, kAct, T>(a, row, col + 2 * k + 1, bias(col + 2 * k + 1), v[k].y);
-            }
+            for (int k = 0; k < 8; ++k)
+                if (k < n) {
+                    FinishOne<kEpi, kAct, T> one;
+                    one.load(a, row, col + k);
+                    one(a, row, col + k, kEpi == kForward && a.bias ? a.bias[col + k] : 0.f, k % 2 ? v[k / 2].y : v[k / 2].x);
+                }
         }
     }
 }
 
-// Rows that TMA cannot start at, copied to rows of `to_ld` elements (16-byte aligned).
+// Rows that TMA cannot start at, copied to rows of `to_ld` elements (16-byte aligned), a warp per row.
 __global__ void __launch_bounds__(256) k_copy_rows(const bf16* x, size_t ld, int width, size_t to_ld, size_t rows, bf16* to) {
     pdl_wait();
     pdl_trigger();
-    for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < rows * to_ld; i += (size_t)gridDim.x * 256) {
-        const size_t t = i / to_ld;
-        const int c = (int)(i - t * to_ld);
-        to[i] = c < width ? x[t * ld + c] : __float2bfloat16_rn(0.f);
+    const int lane = threadIdx.x % 32;
+    for (size_t t = (size_t)blockIdx.x * 8 + threadIdx.x / 32; t < rows; t += (size_t)gridDim.x * 8) {
+        const uint16_t* from = reinterpret_cast<const uint16_t*>(x + t * ld);
+#pragma unroll 2
+        for (int c = lane * 8; c < width; c += 256) {
+            uint32_t v[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] = c + k < width ? from[c + k] : 0u;
+            *reinterpret_cast<uint4*>(to + t * to_ld + c) = make_uint4(v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16);
+        }
     }
 }
 
-// Column sums of dy: 256 columns and every gridDim.y-th group of eight rows for a CTA, then the CTAs' sums in order.
-__global__ void __launch_bounds__(256) k_bias_part(const bf16* dy, size_t ld, int T, int N, int wide, float* part) {
+// Column sums of dy over the rows of a CTA: 256 columns, every gridDim.y-th group of eight rows.  launch_column_sums adds them up.
+__global__ void __launch_bounds__(256) k_bias_part(const bf16* dy, size_t ld, int T, int N, int wide, float* part, size_t part_ld) {
     __shared__ float sh[8][264];
     pdl_wait();
     pdl_trigger();
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, col = blockIdx.x * 256 + lane * 8, n = min(8, N - col);
-    float sum[8] = {};
-    if (n > 0)
-#pragma unroll 4
-        for (int64_t t = (int64_t)blockIdx.y * 8 + warp; t < T; t += (int64_t)gridDim.y * 8) {
-            const bf16* p = dy + (size_t)t * ld + col;
+    float2 sum[4] = {};
+    const int64_t step = (int64_t)gridDim.y * 8;
+    for (int64_t t = (int64_t)blockIdx.y * 8 + warp; t < T && n > 0; t += 8 * step) {
+        Piece<bf16, 8> w[8];                         // eight rows in flight
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            w[k].w[0] = make_uint4(0, 0, 0, 0);
+            if (t + k * step >= T) continue;
+            const bf16* p = dy + (size_t)(t + k * step) * ld + col;
             if (wide && n == 8) {
-                float2 v[4];
-                Piece<bf16, 8> w;
-                w.load(p, false);
-                w.get(v);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) sum[i] += i % 2 ? v[i / 2].y : v[i / 2].x;
+                w[k].load(p, false);
             } else {
+                uint32_t v[8];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) sum[i] += i < n ? to_f(p[i]) : 0.f;
+                for (int i = 0; i < 8; ++i) v[i] = i < n ? reinterpret_cast<const uint16_t*>(p)[i] : 0u;
+                w[k].w[0] = make_uint4(v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16);
             }
         }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) sh[warp][lane * 8 + i] = sum[i];
+        for (int k = 0; k < 8; ++k) {
+            float2 v[4];
+            w[k].get(v);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sum[i] = add2(sum[i], v[i]);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) *reinterpret_cast<float2*>(&sh[warp][lane * 8 + 2 * i]) = sum[i];
     __syncthreads();
     const int c = blockIdx.x * 256 + threadIdx.x;
     if (c >= N) return;
     float v = 0.f;
 #pragma unroll
     for (int w = 0; w < 8; ++w) v += sh[w][threadIdx.x];
-    part[(size_t)blockIdx.y * N + c] = v;
-}
-__global__ void __launch_bounds__(256) k_bias_join(const float* part, int parts, int N, float* db, int accumulate) {
-    pdl_wait();
-    pdl_trigger();
-    const int c = blockIdx.x * 256 + threadIdx.x;
-    if (c >= N) return;
-    float v = 0.f;
-#pragma unroll 8
-    for (int i = 0; i < parts; ++i) v += part[(size_t)i * N + c];
-    db[c] = accumulate ? db[c] + v : v;
+    part[(size_t)blockIdx.y * 2 * part_ld + c] = v;
 }
 
 template <uint32_t kAct, typename T>
@@ -675,8 +698,7 @@ int bias_parts(uint64_t T, uint64_t N) {
 }
 
 cudaError_t copy_rows(const Operand& o, uint64_t to_ld, bf16* to, cudaStream_t s) {
-    const size_t n = (size_t)o.rows * to_ld;
-    return launch_kernel(k_copy_rows, (int)std::min<size_t>((n + 1023) / 1024, kSms * 16), 256, 0, s, true, static_cast<const bf16*>(o.p), (size_t)o.ld, (int)o.cols, (size_t)to_ld,
+    return launch_kernel(k_copy_rows, (int)std::min<size_t>((o.rows + 7) / 8, kSms * 16), 256, 0, s, true, static_cast<const bf16*>(o.p), (size_t)o.ld, (int)o.cols, (size_t)to_ld,
                          (size_t)o.rows, to);
 }
 
@@ -828,7 +850,7 @@ extern "C" int abs_linear_dgrad(const void* dy, uint64_t ld_dy, const void* w, u
 static bool wgrad_plan(uint64_t tokens, uint64_t in, uint64_t out, const Operand& x, const Operand& dy, LinPlan* p) {
     if (!plan_of(in, out, tokens, x, dy, p)) return false;
     p->bias_parts = bias_parts(tokens, out);
-    p->bias_bytes = up256((size_t)p->bias_parts * out * 4);
+    p->bias_bytes = up256((size_t)p->bias_parts * 2 * part_width(out) * 4);
     return true;
 }
 
@@ -864,8 +886,9 @@ extern "C" int abs_linear_wgrad(const void* x, uint64_t ld_x, const void* dy, ui
     if (db) {
         float* part = reinterpret_cast<float*>(static_cast<char*>(workspace) + p.part_bytes + p.a_bytes + p.b_bytes);
         const unsigned blocks = (unsigned)((out + 255) / 256);
-        e = launch_kernel(k_bias_part, dim3(blocks, p.bias_parts), 256, 0, s, true, static_cast<const bf16*>(dy), (size_t)ld_dy, (int)tokens, (int)out, (int)tma_ready(ob), part);
-        if (e == cudaSuccess) e = launch_kernel(k_bias_join, blocks, 256, 0, s, true, (const float*)part, p.bias_parts, (int)out, db, accumulate);
+        e = launch_kernel(k_bias_part, dim3(blocks, p.bias_parts), 256, 0, s, true, static_cast<const bf16*>(dy), (size_t)ld_dy, (int)tokens, (int)out, (int)tma_ready(ob), part,
+                          part_width(out));
+        if (e == cudaSuccess) e = launch_column_sums(part, p.bias_parts, (int)out, db, nullptr, accumulate, s);
         if (e != cudaSuccess) return thread_error(ABS_ECUDA, cudaGetErrorString(e));
     }
     LinArgs a{};
