@@ -25,7 +25,7 @@ enum { kForward, kDgrad, kWgrad };
 
 struct LinArgs {
     int M, N, K;
-    int tiles_n, whole, rest, splits, kb_per_split;   // tiles: whole ones, then `rest` cut into `splits` runs; kb: 64 of K
+    int tiles_m, tiles_n, whole, rest, splits, kb_per_split;   // tiles: whole ones, then `rest` cut into `splits` runs; kb: 64 of K
     float* part;                     // [splits][rest][kTM][kTN]
     void* out;
     size_t ld;
@@ -289,6 +289,15 @@ __device__ __forceinline__ void umma2_commit(uint64_t* bar) {
                  ::"r"(smem_u32(bar)), "h"((uint16_t)3) : "memory");
 }
 
+// First row and column of a tile.  Eight rows of tiles at a time, column by column: the tiles that run together then share as few parts of
+// the operands as they can (8192 x 8192 x 8192 row by row read one operand 14 times).
+__device__ __forceinline__ void place(const LinArgs& a, int tile, int& m0, int& n0) {
+    constexpr int kBand = 8;
+    const int band = tile / (kBand * a.tiles_n), r = tile - band * kBand * a.tiles_n, high = min(kBand, a.tiles_m - band * kBand);
+    m0 = (band * kBand + r % high) * kTM;
+    n0 = r / high * kTN;
+}
+
 // This CTA's share of an operand, 128 rows (or columns) from `mn` and 64 of K from `k`.
 template <bool kMn>
 __device__ __forceinline__ void load_operand(uint8_t* dst, const CUtensorMap* tm, int mn, int k, uint64_t* bar) {
@@ -358,8 +367,7 @@ __global__ void __launch_bounds__(kThreads<T>, 1) k_linear(const __grid_constant
                 q.kb1 = min(kb_total, q.kb0 + a.kb_per_split);
             }
         }
-        q.m0 = tile / a.tiles_n * kTM;
-        q.n0 = tile % a.tiles_n * kTN;
+        place(a, tile, q.m0, q.n0);
         return q;
     };
 
@@ -536,7 +544,9 @@ __global__ void __launch_bounds__(256) k_linear_join(const __grid_constant__ Lin
     const size_t step = (size_t)a.rest * kTM * kTN;
     const int lane = threadIdx.x % 32;
     for (int i = blockIdx.x * 8 + threadIdx.x / 32; i < a.rest * kTM; i += gridDim.x * 8) {
-        const int tile = a.whole + i / kTM, row = tile / a.tiles_n * kTM + i % kTM, col = tile % a.tiles_n * kTN + lane * 8, n = min(8, a.N - col);
+        int m0, n0;
+        place(a, a.whole + i / kTM, m0, n0);
+        const int row = m0 + i % kTM, col = n0 + lane * 8, n = min(8, a.N - col);
         if (row >= a.M || n <= 0) continue;
         const bool wide = a.wide && n == 8;
         Finish<kEpi, kAct, T, 8> f;
@@ -741,7 +751,7 @@ int product(int kind, uint32_t act, uint32_t dtype, Operand oa, Operand ob, uint
         !encode_2d(&tb, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(ob.p), ob.rows, ob.cols, rows_b, 64, ob.ld))
         return thread_error(ABS_ECUDA, "cuTensorMapEncodeTiled failed");
     a.M = (int)M; a.N = (int)N; a.K = (int)K;
-    a.tiles_n = p.tiles_n; a.whole = p.whole; a.rest = p.rest; a.splits = p.splits; a.kb_per_split = p.kb_per_split;
+    a.tiles_m = p.tiles_m; a.tiles_n = p.tiles_n; a.whole = p.whole; a.rest = p.rest; a.splits = p.splits; a.kb_per_split = p.kb_per_split;
     a.part = reinterpret_cast<float*>(ws);
     if (kind == kForward) e = dtype == ABS_F32 ? run<kForward, float>(act, ta, tb, a, s) : run<kForward, bf16>(act, ta, tb, a, s);
     else if (kind == kDgrad) e = dtype == ABS_F32 ? run<kDgrad, float>(act, ta, tb, a, s) : run<kDgrad, bf16>(act, ta, tb, a, s);
