@@ -80,12 +80,23 @@ __global__ void __launch_bounds__(256) k_embed(const int32_t* ids, size_t tokens
 // Tokens sorted by id: pairs (id, token), ids outside the vocabulary as `vocab`, behind all others.  Digits of kBits bits from the
 // lowest; a pass counts each block's digits, adds the counts up over digits and blocks, and places the pairs.  Within a
 // block a warp owns consecutive pairs and takes 32 at a time, in order: equal digits of the 32 find one another by
-// match.any, so every pair's place is known without a comparison.  Up to kBlock tokens one CTA does all passes.
+// match.any, so every pair's place is known without a comparison.  Up to kBlock tokens one CTA does all passes, up to kClusterMost a
+// cluster of eight, in one launch (8192 tokens: 13 us, one CTA 27); more tokens take two launches a pass (65536: 24 us, one cluster 38).
 // ------------------------------------------------------------------------------------------------
 constexpr int kBits = 8, kDigits = 1 << kBits;
-constexpr int kSortThreads = 512, kSortWarps = kSortThreads / 32, kRounds = 16;
+constexpr int kSortThreads = 512, kSortWarps = kSortThreads / 32, kRounds = 4;
 constexpr int kBlock = kSortThreads * kRounds;           // pairs of a block and step
 constexpr int kBlocksMax = 512;
+constexpr int kCluster = 8, kClusterMost = kCluster * kBlock;
+
+// Rows of the table, first .. last - 1, that are cleared meanwhile by the CTAs that do not sort: all rows are, before the sums go to those
+// that have a token (8192 tokens have some 3000 of 32000).
+struct Clear {
+    float* out;
+    size_t ld;
+    int64_t first, last;
+    int width, wide;                                     // wide: rows of whole 16-byte pieces, aligned
+};
 
 struct SortArgs {
     const int32_t* ids;
@@ -97,7 +108,7 @@ struct SortArgs {
 };
 
 __device__ __forceinline__ uint2 pair_at(const SortArgs& a, int pass, int i) {
-    if (pass > 0) return a.buf[(pass - 1) & 1][i];
+    if (pass > 0) return __ldcg(a.buf[(pass - 1) & 1] + i);
     const int id = a.ids[i];
     return make_uint2(id >= 0 && id < a.vocab ? (uint32_t)id : (uint32_t)a.vocab, (uint32_t)i);
 }
@@ -108,6 +119,31 @@ struct SortSmem {
     uint32_t base[kDigits];                              // first place of the block's pairs of a digit
     uint32_t scan[kSortWarps];
 };
+
+// By the CTAs from `first_cta` on.
+__device__ __forceinline__ void clear_rows(const Clear& c, int first_cta) {
+    const int64_t rows = c.last - c.first, at = (int64_t)(blockIdx.x - first_cta) * kSortThreads + threadIdx.x, all = (int64_t)(gridDim.x - first_cta) * kSortThreads;
+    float* from = c.out + c.first * (int64_t)c.ld;
+    const bool packed = c.ld == (size_t)c.width;         // one piece of memory
+    const int64_t lines = packed ? 1 : rows, length = packed ? rows * c.width : c.width;
+    if (c.wide) {
+        const int64_t pieces = length / 4;
+        if (packed) {
+#pragma unroll 4
+            for (int64_t i = at; i < pieces; i += all) reinterpret_cast<float4*>(from)[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+        } else {
+            for (int64_t i = at; i < lines * pieces; i += all) {
+                const int64_t r = i / pieces;
+                *reinterpret_cast<float4*>(from + r * (int64_t)c.ld + (i - r * pieces) * 4) = make_float4(0.f, 0.f, 0.f, 0.f);
+            }
+        }
+    } else {
+        for (int64_t i = at; i < lines * length; i += all) {
+            const int64_t r = packed ? 0 : i / length;
+            from[r * (int64_t)c.ld + (i - r * length)] = 0.f;
+        }
+    }
+}
 
 // Exclusive sum over kDigits values, one for each of the first kDigits threads; all threads call.
 __device__ __forceinline__ uint32_t digit_scan(uint32_t v, SortSmem& s) {
@@ -175,10 +211,11 @@ __device__ void count_digits(const SortArgs& a, SortSmem& s, int pass, int first
     for (int i = threadIdx.x; i < n; i += kSortThreads) atomicAdd(&s.base[digit_of(pair_at(a, pass, first + i), pass)], 1u);
 }
 
-__global__ void __launch_bounds__(kSortThreads) k_sort_small(const __grid_constant__ SortArgs a) {
+__global__ void __launch_bounds__(kSortThreads) k_sort_small(const __grid_constant__ SortArgs a, const __grid_constant__ Clear c) {
     __shared__ SortSmem s;
     pdl_wait();
     pdl_trigger();
+    if (blockIdx.x > 0) return clear_rows(c, 1);
     for (int pass = 0; pass < a.passes; ++pass) {
         if (threadIdx.x < kDigits) s.base[threadIdx.x] = 0;
         __syncthreads();
@@ -191,10 +228,44 @@ __global__ void __launch_bounds__(kSortThreads) k_sort_small(const __grid_consta
     }
 }
 
-__global__ void __launch_bounds__(kSortThreads) k_sort_count(const __grid_constant__ SortArgs a, int pass) {
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// The first cluster sorts, a run of the tokens for each CTA; the others clear.
+__global__ void __launch_bounds__(kSortThreads) k_sort_cluster(const __grid_constant__ SortArgs a, const __grid_constant__ Clear c) {
+    __shared__ SortSmem s;
+    if (blockIdx.x >= kCluster) return clear_rows(c, kCluster);
+    const int per = (a.tokens + kCluster - 1) / kCluster, first = min((int)blockIdx.x * per, a.tokens), n = min(per, a.tokens - first);
+    for (int pass = 0; pass < a.passes; ++pass) {
+        if (threadIdx.x < kDigits) s.base[threadIdx.x] = 0;
+        __syncthreads();
+        count_digits(a, s, pass, first, n);
+        __syncthreads();
+        if (threadIdx.x < kDigits) a.counts[blockIdx.x * kDigits + threadIdx.x] = s.base[threadIdx.x];
+        __threadfence();
+        cluster_sync();
+        uint32_t before = 0, all = 0;
+        if (threadIdx.x < kDigits)
+#pragma unroll
+            for (int b = 0; b < kCluster; ++b) {
+                const uint32_t v = __ldcg(a.counts + b * kDigits + threadIdx.x);
+                all += v;
+                before += b < (int)blockIdx.x ? v : 0;
+            }
+        const uint32_t at = digit_scan(all, s);
+        if (threadIdx.x < kDigits) s.base[threadIdx.x] = at + before;
+        __syncthreads();
+        for (int k = 0; k < n; k += kBlock) place_block(a, s, pass, first + k, min(kBlock, n - k));
+        __threadfence();
+        cluster_sync();              // all pairs are placed, all counts read
+    }
+}
+
+__global__ void __launch_bounds__(kSortThreads) k_sort_count(const __grid_constant__ SortArgs a, const __grid_constant__ Clear c, int pass) {
     __shared__ SortSmem s;
     pdl_wait();
     pdl_trigger();
+    if ((int)blockIdx.x >= a.blocks) return clear_rows(c, a.blocks);
     if (threadIdx.x < kDigits) s.base[threadIdx.x] = 0;
     __syncthreads();
     const int64_t first = (int64_t)blockIdx.x * a.steps * kBlock;
@@ -204,10 +275,11 @@ __global__ void __launch_bounds__(kSortThreads) k_sort_count(const __grid_consta
     if (threadIdx.x < kDigits) a.counts[blockIdx.x * kDigits + threadIdx.x] = s.base[threadIdx.x];
 }
 
-__global__ void __launch_bounds__(kSortThreads) k_sort_place(const __grid_constant__ SortArgs a, int pass) {
+__global__ void __launch_bounds__(kSortThreads) k_sort_place(const __grid_constant__ SortArgs a, const __grid_constant__ Clear c, int pass) {
     __shared__ SortSmem s;
     pdl_wait();
     pdl_trigger();
+    if ((int)blockIdx.x >= a.blocks) return clear_rows(c, a.blocks);
     uint32_t before = 0, all = 0;
     if (threadIdx.x < kDigits)
 #pragma unroll 8
@@ -229,7 +301,6 @@ __global__ void __launch_bounds__(kSortThreads) k_sort_place(const __grid_consta
 // ------------------------------------------------------------------------------------------------
 // Sums over the sorted list.
 // ------------------------------------------------------------------------------------------------
-constexpr int kChunk = 32;                               // sorted tokens that a group of threads adds up
 
 struct SumArgs {
     const uint2* list;
@@ -241,49 +312,184 @@ struct SumArgs {
     size_t ld_out;
     int accumulate;
     Lanes l;
-    int chunks, zero_ctas;                               // CTAs in front that write the rows of no token
+    int chunk, chunks;                                   // sorted tokens that a group of threads adds up
     float* part;                                         // [chunk][2][width]: of the run that began before, of the one that goes on
     size_t width;
 };
 
-// The first place in the list whose id is at least v.
-__device__ __forceinline__ int lower_bound(const uint2* list, int n, uint32_t v) {
-    int lo = 0, hi = n;
-    while (lo < hi) {
-        const int mid = (lo + hi) / 2;
-        if (list[mid].x < v) lo = mid + 1;
-        else hi = mid;
-    }
-    return lo;
-}
-
+// A row's sum; accumulate: one addition for each element, by the memory (nobody else adds to it, so that the order is no matter; read, added and
+// written by the thread, a chunk's rows wait for one another: 16 us instead of 5 for 8192 x 64).
 template <int kE>
 __device__ __forceinline__ void put_row(const SumArgs& a, uint32_t id, int j, const float (&sum)[kE]) {
     float* p = a.out + (size_t)id * a.ld_out + (size_t)j * kE;
     float v[kE];
-    if (a.accumulate) {
-        load_f<kE>(p, v);
 #pragma unroll
-        for (int i = 0; i < kE; ++i) v[i] = fmaf(a.scale, sum[i], v[i]);
+    for (int i = 0; i < kE; ++i) v[i] = a.scale * sum[i];
+    if (!a.accumulate) return store_f<kE>(p, v);
+    if constexpr (kE == 1) {
+        asm volatile("red.relaxed.gpu.global.add.f32 [%0], %1;" ::"l"(p), "f"(v[0]) : "memory");
     } else {
 #pragma unroll
-        for (int i = 0; i < kE; ++i) v[i] = a.scale * sum[i];
+        for (int i = 0; i < kE; i += 4)
+            asm volatile("red.relaxed.gpu.global.add.v4.f32 [%0], {%1, %2, %3, %4};" ::"l"(p + i), "f"(v[i]), "f"(v[i + 1]), "f"(v[i + 2]), "f"(v[i + 3]) : "memory");
     }
-    store_f<kE>(p, v);
 }
 
+// kE elements as they lie in memory, and their sums (pairs: two fp32 additions an instruction).
 template <typename T, int kE>
-__global__ void __launch_bounds__(256) k_embed_sums(const __grid_constant__ SumArgs a) {
+struct Raw {
+    uint4 w;
+    __device__ __forceinline__ void load(const T* p) { w = *reinterpret_cast<const uint4*>(p); }
+    __device__ __forceinline__ void clear() { w = make_uint4(0, 0, 0, 0); }
+};
+template <typename T>
+struct Raw<T, 1> {
+    T w;
+    __device__ __forceinline__ void load(const T* p) { w = *p; }
+    __device__ __forceinline__ void clear() { w = from_f<T>(0.f); }
+};
+template <typename T, int kE>
+struct Sums {
+    float2 v[kE / 2];
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int i = 0; i < kE / 2; ++i) v[i] = both(0.f);
+    }
+    __device__ __forceinline__ void add(const Raw<T, kE>& r) {
+        float2 u[kE / 2];
+        unpack(r.w, u, T());
+#pragma unroll
+        for (int i = 0; i < kE / 2; ++i) v[i] = add2(v[i], u[i]);
+    }
+    __device__ __forceinline__ void get(float (&f)[kE]) const {
+#pragma unroll
+        for (int i = 0; i < kE; ++i) f[i] = i % 2 ? v[i / 2].y : v[i / 2].x;
+    }
+};
+template <typename T>
+struct Sums<T, 1> {
+    float v;
+    __device__ __forceinline__ void clear() { v = 0.f; }
+    __device__ __forceinline__ void add(const Raw<T, 1>& r) { v += to_f(r.w); }
+    __device__ __forceinline__ void get(float (&f)[1]) const { f[0] = v; }
+};
+
+template <typename T, int kE>
+__global__ void __launch_bounds__(256, 4) k_embed_sums(const __grid_constant__ SumArgs a) {
     pdl_wait();
     pdl_trigger();
-    if ((int)blockIdx.x < a.zero_ctas) {                 // eight rows a warp: who has a token is looked up by a lane each
-        const int lane = threadIdx.x % 32, warps = a.zero_ctas * 8;
-        for (int64_t v0 = ((int64_t)blockIdx.x * 8 + threadIdx.x / 32) * 8; v0 < a.vocab; v0 += (int64_t)warps * 8) {
-            bool absent = false;
-            if (lane < 8 && v0 + lane < a.vocab) {
-                const int at = lower_bound(a.list, a.tokens, (uint32_t)(v0 + lane));
-                absent = at == a.tokens || a.list[at].x != (uint32_t)(v0 + lane);
+    const int lane = threadIdx.x & ((1 << a.l.log) - 1), groups = 256 >> a.l.log;
+    const int64_t chunk = (int64_t)blockIdx.x * groups + (threadIdx.x >> a.l.log);
+    if (chunk >= a.chunks) return;
+    const int first = (int)(chunk * a.chunk), n = min(a.chunk, a.tokens - first);
+    const uint2* list = a.list + first;
+    const uint32_t ahead = first > 0 ? list[-1].x : 0xffffffffu, behind = first + n < a.tokens ? list[n].x : 0xffffffffu;
+    const int j = blockIdx.y * (1 << a.l.log) + lane;
+    if (j >= a.l.pieces) return;
+    const T* dy = static_cast<const T*>(a.dy) + (size_t)j * kE;
+    float* part = a.part + (size_t)chunk * 2 * a.width + (size_t)j * kE;
+    Sums<T, kE> sum;
+    sum.clear();
+    uint32_t id = list[0].x;
+    bool began = id == ahead;                            // the current run began in a chunk before
+    // to: where a run that is not the table's row alone goes
+    auto put = [&](float* to, bool whole) {
+        float v[kE];
+        sum.get(v);
+        if (whole) put_row<kE>(a, id, j, v);
+        else store_f<kE>(to, v);
+    };
+    constexpr int kAhead = 8;                            // rows in flight
+    for (int i0 = 0; i0 < n; i0 += kAhead) {
+        uint2 p[kAhead];
+        Raw<T, kE> v[kAhead];
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) p[k] = i0 + k < n ? list[i0 + k] : make_uint2(0xffffffffu, 0);     // beyond the list: another run
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            v[k].clear();
+            if (p[k].x < (uint32_t)a.vocab) v[k].load(dy + (size_t)p[k].y * a.ld_dy);
+        }
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            if (p[k].x != id) {
+                if (id < (uint32_t)a.vocab) put(part, !began);
+                began = false;
+                id = p[k].x;
+                sum.clear();
             }
+            sum.add(v[k]);
+        }
+    }
+    if (id >= (uint32_t)a.vocab) return;
+    if (began) put(part, false);
+    else put(part + a.width, id != behind);
+}
+
+// The rows whose tokens pass the end of a chunk: that chunk's second partial sum, then the first ones of those behind it, a CTA for each.
+// The CTA's groups of threads take the chunks behind in turn, four loads each in flight; their sums are added up in order.
+template <int kE>
+__global__ void __launch_bounds__(256) k_embed_join(const __grid_constant__ SumArgs a) {
+    __shared__ float sh[256][kE];
+    pdl_wait();
+    pdl_trigger();
+    const int chunk = blockIdx.x, first = chunk * a.chunk, next = first + a.chunk;
+    const uint32_t id = a.list[next - 1].x;
+    if (id != a.list[next].x || id >= (uint32_t)a.vocab || (first > 0 && a.list[first - 1].x == id)) return;
+    int64_t behind = 0;                                  // chunks behind that the run goes into
+    for (bool all = true; all;) {
+        const int64_t k = chunk + 1 + behind + threadIdx.x % 32;
+        const uint32_t on = __ballot_sync(0xffffffffu, k < a.chunks && a.list[k * a.chunk].x == id);
+        all = on == 0xffffffffu;
+        behind += __popc(on);
+    }
+    const size_t step = 2 * a.width;
+    const int lanes = 1 << a.l.log, lane = threadIdx.x & (lanes - 1), line = threadIdx.x >> a.l.log, lines = 256 >> a.l.log;
+    for (int j0 = 0; j0 < a.l.pieces; j0 += lanes) {
+        const int j = j0 + lane;
+        const float* part = a.part + (size_t)chunk * step + (size_t)min(j, a.l.pieces - 1) * kE;
+        float sum[kE] = {};
+        if (line == 0) load_f<kE>(part + a.width, sum);
+        for (int64_t k0 = 1 + line * 4; k0 <= behind; k0 += lines * 4) {
+            float v[4][kE];
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (k0 + k <= behind) load_f<kE>(part + (size_t)(k0 + k) * step, v[k]);
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (k0 + k <= behind)
+#pragma unroll
+                    for (int i = 0; i < kE; ++i) sum[i] += v[k][i];
+        }
+        if (lines > 1) {
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < kE; ++i) sh[threadIdx.x][i] = sum[i];
+            __syncthreads();
+            for (int w = 1; w < lines && line == 0; ++w)
+#pragma unroll
+                for (int i = 0; i < kE; ++i) sum[i] += sh[w * lanes + lane][i];
+        }
+        if (line == 0 && j < a.l.pieces) put_row<kE>(a, id, j, sum);
+    }
+}
+
+// Few tokens: each looks for its own kind among all of them, the first of a kind adds them up; the other rows are cleared by the CTAs
+// behind.  One launch instead of three.
+constexpr int kFew = 128;
+template <typename T, int kE>
+__global__ void __launch_bounds__(256) k_embed_few(const __grid_constant__ SumArgs a, const int32_t* ids, int token_ctas) {
+    __shared__ int32_t sh[kFew];
+    pdl_wait();
+    pdl_trigger();
+    for (int t = threadIdx.x; t < kFew; t += 256) sh[t] = t < a.tokens ? ids[t] : -1;
+    __syncthreads();
+    if ((int)blockIdx.x >= token_ctas) {                 // 32 rows a warp: a lane looks one up
+        const int lane = threadIdx.x % 32;
+        const int64_t step = (int64_t)(gridDim.x - token_ctas) * 8 * 32;
+        for (int64_t v0 = ((int64_t)(blockIdx.x - token_ctas) * 8 + threadIdx.x / 32) * 32; v0 < a.vocab; v0 += step) {
+            bool absent = v0 + lane < a.vocab;
+            for (int t = 0; t < a.tokens; ++t) absent = absent && sh[t] != (int)(v0 + lane);
             uint32_t rows = __ballot_sync(0xffffffffu, absent);
             const float zero[kE] = {};
             while (rows) {
@@ -294,83 +500,50 @@ __global__ void __launch_bounds__(256) k_embed_sums(const __grid_constant__ SumA
         }
         return;
     }
-    const int lane = threadIdx.x & ((1 << a.l.log) - 1), groups = 256 >> a.l.log;
-    const int64_t chunk = (int64_t)(blockIdx.x - a.zero_ctas) * groups + (threadIdx.x >> a.l.log);
-    if (chunk >= a.chunks) return;
-    const int first = (int)(chunk * kChunk), n = min(kChunk, a.tokens - first);
-    const uint32_t ahead = first > 0 ? a.list[first - 1].x : 0xffffffffu, behind = first + n < a.tokens ? a.list[first + n].x : 0xffffffffu;
-    const int j = blockIdx.y * (1 << a.l.log) + lane;
-    if (j >= a.l.pieces) return;
-    const T* dy = static_cast<const T*>(a.dy) + (size_t)j * kE;
-    float* part = a.part + (size_t)chunk * 2 * a.width + (size_t)j * kE;
-    float sum[kE] = {};
-    uint32_t id = a.list[first].x;
-    bool began = id == ahead;                            // the current run began in a chunk before
-    constexpr int kAhead = 8;
-    for (int i0 = 0; i0 < n; i0 += kAhead) {
-        uint2 p[kAhead];
-        float v[kAhead][kE];
+    const int lane = threadIdx.x & ((1 << a.l.log) - 1), t = blockIdx.x * (256 >> a.l.log) + (threadIdx.x >> a.l.log);
+    if (t >= a.tokens || sh[t] < 0 || sh[t] >= a.vocab) return;
+    const int id = sh[t];
+    uint32_t same[kFew / 32];
 #pragma unroll
-        for (int k = 0; k < kAhead; ++k) p[k] = i0 + k < n ? a.list[first + i0 + k] : make_uint2(0xffffffffu, 0);
+    for (int w = 0; w < kFew / 32; ++w) {
+        same[w] = 0;
+#pragma unroll 8
+        for (int i = 0; i < 32; ++i) same[w] |= (sh[w * 32 + i] == id ? 1u : 0u) << i;
+    }
 #pragma unroll
-        for (int k = 0; k < kAhead; ++k) {
-            if (p[k].x < (uint32_t)a.vocab) Pack<T, kE>::load(dy + (size_t)p[k].y * a.ld_dy, v[k]);
-            else
+    for (int w = 0; w < kFew / 32; ++w) {
+        const uint32_t front = t >= w * 32 + 32 ? 0xffffffffu : t > w * 32 ? (1u << (t - w * 32)) - 1 : 0u;
+        if (same[w] & front) return;                     // not the first of its kind
+    }
+    for (int j = lane; j < a.l.pieces; j += 1 << a.l.log) {
+        const T* dy = static_cast<const T*>(a.dy) + (size_t)j * kE;
+        float sum[kE] = {};
 #pragma unroll
-                for (int i = 0; i < kE; ++i) v[k][i] = 0.f;
-        }
+        for (int w = 0; w < kFew / 32; ++w) {
+            uint32_t left = same[w];
+            while (left) {
+                constexpr int kAhead = 4;
+                float v[kAhead][kE];
+                bool have[kAhead];
 #pragma unroll
-        for (int k = 0; k < kAhead; ++k) {
-            if (i0 + k >= n) break;
-            if (p[k].x != id) {
-                if (id < (uint32_t)a.vocab) {
-                    if (began) store_f<kE>(part, sum);
-                    else put_row<kE>(a, id, j, sum);
+                for (int k = 0; k < kAhead; ++k) {
+                    have[k] = left != 0;
+                    if (have[k]) Pack<T, kE>::load(dy + (size_t)(w * 32 + __ffs(left) - 1) * a.ld_dy, v[k]);
+                    left &= left - 1;
                 }
-                began = false;
-                id = p[k].x;
 #pragma unroll
-                for (int i = 0; i < kE; ++i) sum[i] = 0.f;
+                for (int k = 0; k < kAhead; ++k)
+                    if (have[k])
+#pragma unroll
+                        for (int i = 0; i < kE; ++i) sum[i] += v[k][i];
             }
-#pragma unroll
-            for (int i = 0; i < kE; ++i) sum[i] += v[k][i];
         }
+        put_row<kE>(a, (uint32_t)id, j, sum);
     }
-    if (id >= (uint32_t)a.vocab) return;
-    if (began) store_f<kE>(part, sum);
-    else if (id == behind) store_f<kE>(part + a.width, sum);
-    else put_row<kE>(a, id, j, sum);
-}
-
-// The rows whose tokens pass the end of a chunk: that chunk's second partial sum, then the first ones of those behind it.
-template <int kE>
-__global__ void __launch_bounds__(256) k_embed_join(const __grid_constant__ SumArgs a) {
-    pdl_wait();
-    pdl_trigger();
-    const int lane = threadIdx.x & ((1 << a.l.log) - 1), groups = 256 >> a.l.log;
-    const int64_t chunk = (int64_t)blockIdx.x * groups + (threadIdx.x >> a.l.log);
-    if (chunk >= a.chunks - 1) return;
-    const int first = (int)(chunk * kChunk), next = first + kChunk;
-    const uint32_t id = a.list[next - 1].x;
-    if (id != a.list[next].x || id >= (uint32_t)a.vocab || (first > 0 && a.list[first - 1].x == id)) return;
-    const int last = lower_bound(a.list, a.tokens, id + 1) - 1, ends = last / kChunk;      // the chunk with the run's last token
-    const int j = blockIdx.y * (1 << a.l.log) + lane;
-    if (j >= a.l.pieces) return;
-    const float* part = a.part + (size_t)j * kE;
-    float sum[kE];
-    load_f<kE>(part + ((size_t)chunk * 2 + 1) * a.width, sum);
-#pragma unroll 4
-    for (int64_t k = chunk + 1; k <= ends; ++k) {
-        float v[kE];
-        load_f<kE>(part + (size_t)k * 2 * a.width, v);
-#pragma unroll
-        for (int i = 0; i < kE; ++i) sum[i] += v[i];
-    }
-    put_row<kE>(a, id, j, sum);
 }
 
 struct EmbedPlan {
-    int blocks, steps, passes, chunks;
+    int blocks, steps, passes, chunk, chunks;
     size_t width, list_bytes, count_bytes, part_bytes;
     size_t bytes() const { return 2 * list_bytes + count_bytes + part_bytes; }
 };
@@ -381,34 +554,29 @@ EmbedPlan embed_plan(uint64_t tokens, uint64_t vocab, uint64_t width) {
     p.blocks = p.steps ? (int)((steps + p.steps - 1) / p.steps) : 0;
     p.passes = 1;
     while (p.passes * kBits < 32 && vocab >> (p.passes * kBits)) ++p.passes;       // the largest key is `vocab`
-    p.chunks = (int)((tokens + kChunk - 1) / kChunk);
+    // as long as that leaves some 128 thousand threads: a run's partial sums are added up by one CTA
+    const uint64_t most = (tokens << lanes_for(width, 8).log) >> 17;
+    for (p.chunk = 16; p.chunk < 256 && (uint64_t)p.chunk * 2 <= most;) p.chunk *= 2;
+    p.chunks = (int)((tokens + p.chunk - 1) / p.chunk);
     p.width = (width + 7) / 8 * 8;
     p.list_bytes = up256(tokens * sizeof(uint2));
-    p.count_bytes = p.blocks > 1 ? up256((size_t)p.blocks * kDigits * 4) : 0;
+    p.count_bytes = p.blocks > 1 ? up256((size_t)std::max(p.blocks, kCluster) * kDigits * 4) : 0;
     p.part_bytes = p.chunks > 1 ? up256((size_t)p.chunks * 2 * p.width * 4) : 0;
     return p;
 }
 
 template <typename T, int kE>
-cudaError_t sum_rows(SumArgs a, uint64_t width, cudaStream_t s) {
+cudaError_t sum_rows(SumArgs a, uint64_t width, const int32_t* few, cudaStream_t s) {
     a.l = lanes_for(width, kE);
     const int groups = 256 >> a.l.log;
-    const unsigned slabs = (unsigned)((a.l.pieces + (1 << a.l.log) - 1) >> a.l.log);
-    if (a.accumulate == 0) a.zero_ctas = (int)std::min<int64_t>(((int64_t)a.vocab + 63) / 64, kSms * 4);
-    const unsigned ctas = (unsigned)((a.chunks + groups - 1) / groups);
-    // rows of no token: only the first slab's CTAs write them, whole
-    cudaError_t e = cudaSuccess;
-    if (slabs == 1 || a.zero_ctas == 0) {
-        e = launch_kernel(k_embed_sums<T, kE>, dim3(a.zero_ctas + ctas, slabs), 256, 0, s, true, a);
-    } else {
-        SumArgs z = a;
-        z.chunks = 0;
-        e = launch_kernel(k_embed_sums<T, kE>, dim3(a.zero_ctas), 256, 0, s, true, z);
-        a.zero_ctas = 0;
-        if (e == cudaSuccess) e = launch_kernel(k_embed_sums<T, kE>, dim3(ctas, slabs), 256, 0, s, true, a);
+    if (few) {
+        const unsigned tokens = (unsigned)((a.tokens + groups - 1) / groups), rows = a.accumulate ? 0 : (unsigned)std::min<int64_t>(((int64_t)a.vocab + 255) / 256, kSms * 8);
+        return launch_kernel(k_embed_few<T, kE>, tokens + rows, 256, 0, s, true, a, few, (int)tokens);
     }
-    if (e == cudaSuccess && a.chunks > 1) e = launch_kernel(k_embed_join<kE>, dim3(ctas, slabs), 256, 0, s, true, a);
-    return e;
+    const dim3 grid((unsigned)((a.chunks + groups - 1) / groups), (unsigned)((a.l.pieces + (1 << a.l.log) - 1) >> a.l.log));
+    const cudaError_t e = launch_kernel(k_embed_sums<T, kE>, grid, 256, 0, s, true, a);
+    if (e != cudaSuccess || a.chunks == 1) return e;
+    return launch_kernel(k_embed_join<kE>, a.chunks - 1, 256, 0, s, true, a);
 }
 
 }  // namespace
@@ -473,21 +641,28 @@ extern "C" int abs_embed_backward(const void* dy, uint64_t ld_dy, uint32_t dtype
     a.buf[0] = reinterpret_cast<uint2*>(ws);
     a.buf[1] = reinterpret_cast<uint2*>(ws + p.list_bytes);
     a.counts = reinterpret_cast<uint32_t*>(ws + 2 * p.list_bytes);
-    if (p.blocks == 1 && p.steps == 1) {
-        e = launch_kernel(k_sort_small, 1, kSortThreads, 0, s, true, a);
-    } else {
-        for (int pass = 0; pass < p.passes && e == cudaSuccess; ++pass) {
-            e = launch_kernel(k_sort_count, p.blocks, kSortThreads, 0, s, true, a, pass);
-            if (e == cudaSuccess) e = launch_kernel(k_sort_place, p.blocks, kSortThreads, 0, s, true, a, pass);
+    const bool wide = rows_at(m[0], 16) && rows_at(m[1], 16) && width * m[1].es % 16 == 0;
+    const bool few = tokens <= (uint64_t)kFew;
+    if (!few) {
+        const bool one = p.blocks == 1, cluster = !one && tokens <= (uint64_t)kClusterMost;
+        const int launches = one || cluster ? 1 : 2 * p.passes;
+        const int clear = accumulate ? 0 : (int)std::min<uint64_t>((vocab * width / launches + 4 * kSortThreads - 1) / (4 * kSortThreads), 3 * kSms);
+        Clear c{dtable, (size_t)ld_dtable, 0, 0, (int)width, rows_at(m[0], 16) && width % 4 == 0};
+        for (int i = 0; i < launches && e == cudaSuccess; ++i) {
+            c.first = c.last;
+            c.last = (int64_t)(vocab * (i + 1) / launches);
+            if (one) e = launch_kernel(k_sort_small, 1 + clear, kSortThreads, 0, s, true, a, c);
+            else if (cluster) e = launch_cluster(k_sort_cluster, kCluster + (clear + kCluster - 1) / kCluster * kCluster, kCluster, kSortThreads, 0, s, a, c);
+            else e = launch_kernel(i % 2 ? k_sort_place : k_sort_count, p.blocks + clear, kSortThreads, 0, s, true, a, c, i / 2);
         }
+        if (e != cudaSuccess) return thread_error(ABS_ECUDA, cudaGetErrorString(e));
     }
-    if (e != cudaSuccess) return thread_error(ABS_ECUDA, cudaGetErrorString(e));
     SumArgs q{};
     q.list = a.buf[(p.passes - 1) & 1]; q.dy = dy; q.ld_dy = ld_dy; q.tokens = (int)tokens; q.vocab = (int)vocab; q.D = (int)width; q.scale = scale;
-    q.out = dtable; q.ld_out = ld_dtable; q.accumulate = accumulate != 0; q.chunks = p.chunks;
+    q.out = dtable; q.ld_out = ld_dtable; q.accumulate = accumulate != 0; q.chunk = p.chunk; q.chunks = p.chunks;
     q.part = reinterpret_cast<float*>(ws + 2 * p.list_bytes + p.count_bytes); q.width = p.width;
-    const bool wide = rows_at(m[0], 16) && rows_at(m[1], 16) && width * m[1].es % 16 == 0;
-    e = dtype == ABS_F32 ? (wide ? sum_rows<float, 4>(q, width, s) : sum_rows<float, 1>(q, width, s))
-                         : (wide ? sum_rows<bf16, 8>(q, width, s) : sum_rows<bf16, 1>(q, width, s));
+    const int32_t* all = few ? ids : nullptr;
+    e = dtype == ABS_F32 ? (wide ? sum_rows<float, 4>(q, width, all, s) : sum_rows<float, 1>(q, width, all, s))
+                         : (wide ? sum_rows<bf16, 8>(q, width, all, s) : sum_rows<bf16, 1>(q, width, all, s));
     return e == cudaSuccess ? ABS_OK : thread_error(ABS_ECUDA, cudaGetErrorString(e));
 }
