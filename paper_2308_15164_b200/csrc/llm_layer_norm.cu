@@ -2,9 +2,11 @@
 //
 //     n = (x - mean) r w + b,  r = 1 / sqrt(mean (x - mean)^2 + eps)
 // Backward with c = x - mean, xh = c r, a = dn w:  dx = dskip + r (a - mean(a)) - c r^3 mean(a c),  dw = sum dn xh,  db = sum dn.
-// The variance is taken about the row's own mean, from the values that the thread holds (x^2 - mean^2 would lose what a large
-// common offset leaves), so that a row is a chain of two reductions.  Bound by memory: forward 2, backward 3 (4 with dskip)
-// elements per position.
+// Plain sums of x and x^2 would lose what a large common offset leaves of the variance.  A CTA that owns a row takes all sums about
+// a pivot p, the mean of 32 of the row's elements, which every warp finds on its own: one reduction of the CTA instead of two.  The
+// pivot's distance from the mean is at most sqrt(D / 32) standard deviations, whatever the row holds (the 32 are part of the variance),
+// and usually a fifth of one; mean (x - p)^2 - (mean - p)^2 loses that much: D / 32 roundings at worst.  A warp that owns a row takes its
+// mean first.  Bound by memory: forward 2, backward 3 (4 with dskip) elements per position.
 #include <math.h>
 
 #include "abs_internal.h"
@@ -25,7 +27,16 @@ constexpr int kRingCtasMax = 16;
 constexpr int ring_threads(bool back, int elems) { return back && elems == 32 ? 256 : 512; }
 constexpr int warp_ctas(bool back, int elems) { return back ? 2 : elems == 8 ? 4 : 3; }
 constexpr size_t warp_row(size_t es) { return es == 2 ? 384 : 256; }
-constexpr int ring_elems(size_t D) { return D <= 8 * 32 ? 8 : D <= 16 * 512 ? 16 : 32; }
+// Elements of a thread: what a row costs a thread beside its elements (reductions, waits, addresses, some 150 instructions forward and 300
+// backward) is spread over them, but fewer leave more warps.  us with 16 / 32, bf16: forward 16384 x 4096 69 / 51, 8192 x 8192 80 / 54,
+// 16384 x 2048 36 / 31; backward with dskip 16384 x 4096 122 / 119, 8192 x 8192 133 / 126, 16384 x 6144 206 / 218, 16384 x 2048 66 / 68.  fp32 (half
+// the elements a byte) 8192 x 4096 46 / 50, backward 91 / 91, 1003 x 1537 5.1 / 6.4, 11.5 / 12.6.
+constexpr int ring_elems(bool back, size_t es, size_t D) {
+    if (D <= 8 * 32) return 8;
+    if (es == 4) return D <= 16 * 512 ? 16 : 32;
+    if (!back) return D <= 1024 ? 16 : 32;
+    return D <= 3840 || (D > 4096 && D <= 6144) ? 16 : 32;
+}
 
 struct LnArgs {
     const void *x, *dn, *skip;       // forward: x only
@@ -40,6 +51,12 @@ struct LnArgs {
     int stages;
     uint32_t row_bytes;
 };
+
+// The variance from the mean square about a pivot; a NaN stays one.
+__device__ __forceinline__ float var_of(float square, float d) {
+    const float v = square - d * d;
+    return v < 0.f ? 0.f : v;
+}
 
 // kV consecutive elements at a time, kV = 1 for rows that are not 16-byte aligned.
 template <typename T, int kV>
@@ -133,6 +150,17 @@ __global__ void __launch_bounds__(256) k_layer_norm_back_plain(const __grid_cons
     }
 }
 
+// The mean of 32 elements of the current row's image of input 0, the same in every warp.  The image has 32 elements at least.
+template <typename R>
+__device__ __forceinline__ float pivot_of(const R& r) {
+    const uint32_t all = (uint32_t)r.cut.pieces * kVec<typename R::Element>;
+    const auto* image = reinterpret_cast<const typename R::Element*>(r.base + (size_t)r.st * R::kInputs * r.row_bytes);
+    float v = to_f(image[threadIdx.x % 32 * (all / 32)]);
+#pragma unroll
+    for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v * (1.f / 32.f);
+}
+
 // Rows through a ring of images (row_ring.cuh); a thread owns kP pieces of 16 bytes and at most one single element.
 template <typename T, int kP, bool kWarp>
 __global__ void __launch_bounds__(kWarp ? kRowWarps * 32 : ring_threads(false, kP * kVec<T>), kWarp ? warp_ctas(false, kP * kVec<T>) : 1)
@@ -165,43 +193,60 @@ __global__ void __launch_bounds__(kWarp ? kRowWarps * 32 : ring_threads(false, k
         const float ex = nx[0];
         r.load_extra(t + G, nx);
         r.wait();
-        float2 v[kP][kN], s2 = both(0.f);
+        float2 v[kP][kN], s2 = both(0.f), t2 = both(0.f);
+        float pivot = 0.f, d, q;                     // v: x - pivot; d: mean - pivot
+        if (!kWarp) pivot = pivot_of(r);
 #pragma unroll
         for (int j = 0; j < kP; ++j)
             if (r.has(j)) {
                 r.piece(0, j, v[j]);
 #pragma unroll
-                for (int i = 0; i < kN; ++i) s2 = add2(s2, v[j][i]);
+                for (int i = 0; i < kN; ++i) {
+                    if (!kWarp) {
+                        v[j][i] = add2(v[j][i], both(-pivot));
+                        t2 = fma2(v[j][i], v[j][i], t2);
+                    }
+                    s2 = add2(s2, v[j][i]);
+                }
             }
-        if (kWarp) r.release(t, G, warps);
-        float s[1] = {sum2(s2) + (r.extra >= 0 ? ex : 0.f)};
-        row_sum<kWarp>(s, r.ctl->red[k & 1], warps);
-        if (!kWarp) {
+        const float xc = ex - pivot;
+        if (kWarp) {
+            r.release(t, G, warps);
+            float s[1] = {sum2(s2) + (r.extra >= 0 ? xc : 0.f)};
+            row_sum<true>(s, nullptr, 1);
+            d = s[0] * a.inv_d;
+#pragma unroll
+            for (int j = 0; j < kP; ++j)
+                if (r.has(j))
+#pragma unroll
+                    for (int i = 0; i < kN; ++i) {
+                        const float2 c = add2(v[j][i], both(-d));
+                        t2 = fma2(c, c, t2);
+                    }
+            s[0] = sum2(t2) + (r.extra >= 0 ? (xc - d) * (xc - d) : 0.f);
+            row_sum<true>(s, nullptr, 1);
+            q = rsqrtf(s[0] * a.inv_d + a.eps);
+        } else {
+            float s[2] = {sum2(s2), sum2(t2)};
+            if (r.extra >= 0) {
+                s[0] += xc;
+                s[1] += xc * xc;
+            }
+            row_sum<false>(s, r.ctl->red[k & 1], warps);
             // every warp has read this row's image: it is filled again at once
             if (threadIdx.x == 0) r.load(r.st, t + (size_t)r.stages * G);
+            d = s[0] * a.inv_d;
+            q = rsqrtf(var_of(s[1] * a.inv_d, d) + a.eps);
         }
-        const float mean = s[0] * a.inv_d;
-        s2 = both(0.f);
-#pragma unroll
-        for (int j = 0; j < kP; ++j)
-            if (r.has(j))
-#pragma unroll
-                for (int i = 0; i < kN; ++i) {
-                    v[j][i] = add2(v[j][i], both(-mean));
-                    s2 = fma2(v[j][i], v[j][i], s2);
-                }
-        s[0] = sum2(s2) + (r.extra >= 0 ? (ex - mean) * (ex - mean) : 0.f);
-        row_sum<kWarp>(s, r.ctl->red[2], warps);
-        const float q = rsqrtf(s[0] * a.inv_d + a.eps);
         T* n = static_cast<T*>(a.out) + t * a.ld_out;
 #pragma unroll
         for (int j = 0; j < kP; ++j)
             if (r.has(j)) {
 #pragma unroll
-                for (int i = 0; i < kN; ++i) v[j][i] = fma2(mul2(v[j][i], both(q)), w[j][i], b[j][i]);
+                for (int i = 0; i < kN; ++i) v[j][i] = fma2(mul2(add2(v[j][i], both(-d)), both(q)), w[j][i], b[j][i]);
                 r.store(n, j, v[j]);
             }
-        if (r.extra >= 0 && r.ok) n[r.extra] = from_f<T>((ex - mean) * q * xw + xb);
+        if (r.extra >= 0 && r.ok) n[r.extra] = from_f<T>((xc - d) * q * xw + xb);
     }
     if (!r.ok) report_timeout();
 }
@@ -240,43 +285,53 @@ __global__ void __launch_bounds__(kWarp ? kRowWarps * 32 : ring_threads(true, kP
         for (int i = 0; i < kIn; ++i) ex[i] = nx[i];
         r.load_extra(t + G, nx);
         r.wait();
-        float2 c[kP][kN], s2 = both(0.f);
+        float2 c[kP][kN], q2[4] = {both(0.f), both(0.f), both(0.f), both(0.f)};   // x - pivot; sums of c, c^2, a, a c
+        float pivot = 0.f;
+        if (kWarp) {                                             // the mean itself
+            float2 s2 = both(0.f);
 #pragma unroll
-        for (int j = 0; j < kP; ++j)
-            if (r.has(j)) {
-                r.piece(0, j, c[j]);
+            for (int j = 0; j < kP; ++j)
+                if (r.has(j)) {
+                    r.piece(0, j, c[j]);
 #pragma unroll
-                for (int i = 0; i < kN; ++i) s2 = add2(s2, c[j][i]);
-            }
-        float m[1] = {sum2(s2) + (r.extra >= 0 ? ex[0] : 0.f)};
-        row_sum<kWarp>(m, r.ctl->red[k & 1], warps);
-        const float mean = m[0] * a.inv_d;
-        float2 q2[3] = {both(0.f), both(0.f), both(0.f)};        // sum c^2, a, a c
+                    for (int i = 0; i < kN; ++i) s2 = add2(s2, c[j][i]);
+                }
+            float m[1] = {sum2(s2) + (r.extra >= 0 ? ex[0] : 0.f)};
+            row_sum<true>(m, nullptr, 1);
+            pivot = m[0] * a.inv_d;
+        } else {
+            pivot = pivot_of(r);
+        }
 #pragma unroll
         for (int j = 0; j < kP; ++j)
             if (r.has(j)) {
                 float2 d[kN];
+                if (!kWarp) r.piece(0, j, c[j]);
                 r.piece(1, j, d);
 #pragma unroll
                 for (int i = 0; i < kN; ++i) {
-                    c[j][i] = add2(c[j][i], both(-mean));
+                    c[j][i] = add2(c[j][i], both(-pivot));
                     c_b[j][i] = add2(c_b[j][i], d[i]);
                     d[i] = mul2(d[i], w[j][i]);
-                    q2[0] = fma2(c[j][i], c[j][i], q2[0]);
-                    q2[1] = add2(q2[1], d[i]);
-                    q2[2] = fma2(d[i], c[j][i], q2[2]);
+                    if (!kWarp) q2[0] = add2(q2[0], c[j][i]);
+                    q2[1] = fma2(c[j][i], c[j][i], q2[1]);
+                    q2[2] = add2(q2[2], d[i]);
+                    q2[3] = fma2(d[i], c[j][i], q2[3]);
                 }
             }
-        float s[3] = {sum2(q2[0]), sum2(q2[1]), sum2(q2[2])};
-        const float xc = ex[0] - mean, xa = ex[1] * xw;
+        float s[4] = {sum2(q2[0]), sum2(q2[1]), sum2(q2[2]), sum2(q2[3])};
+        const float xc = ex[0] - pivot, xa = ex[1] * xw;
         if (r.extra >= 0) {
-            s[0] += xc * xc;
-            s[1] += xa;
-            s[2] += xa * xc;
+            if (!kWarp) s[0] += xc;
+            s[1] += xc * xc;
+            s[2] += xa;
+            s[3] += xa * xc;
         }
-        row_sum<kWarp>(s, r.ctl->red[2], warps);
-        const float q = rsqrtf(s[0] * a.inv_d + a.eps);
-        const float level = -q * s[1] * a.inv_d, along = -q * q * q * s[2] * a.inv_d;     // dx = q a + c along + level
+        row_sum<kWarp>(s, r.ctl->red[k & 1], warps);
+        const float d0 = kWarp ? 0.f : s[0] * a.inv_d;           // mean - pivot
+        const float q = rsqrtf(var_of(s[1] * a.inv_d, d0) + a.eps);
+        const float along = -q * q * q * (s[3] - d0 * s[2]) * a.inv_d;
+        const float level = -q * s[2] * a.inv_d - d0 * along;    // dx = q a + (x - pivot) along + level
         T* dx = static_cast<T*>(a.out) + t * a.ld_out;
 #pragma unroll
         for (int j = 0; j < kP; ++j)
@@ -286,7 +341,7 @@ __global__ void __launch_bounds__(kWarp ? kRowWarps * 32 : ring_threads(true, kP
                 if (has_skip) r.piece(2, j, o);
 #pragma unroll
                 for (int i = 0; i < kN; ++i) {
-                    c_w[j][i] = fma2(mul2(d[i], both(q)), c[j][i], c_w[j][i]);
+                    c_w[j][i] = fma2(mul2(d[i], both(q)), add2(c[j][i], both(-d0)), c_w[j][i]);
                     d[i] = fma2(mul2(d[i], w[j][i]), both(q), fma2(c[j][i], both(along), both(level)));
                     if (has_skip) d[i] = add2(d[i], o[i]);
                 }
@@ -294,7 +349,7 @@ __global__ void __launch_bounds__(kWarp ? kRowWarps * 32 : ring_threads(true, kP
             }
         r.release(t, G, warps);
         if (r.extra >= 0) {
-            x_w += ex[1] * q * xc;
+            x_w += ex[1] * q * (xc - d0);
             x_b += ex[1];
             if (r.ok) dx[r.extra] = from_f<T>(xa * q + (xc * along + level) + ex[2]);
         }
@@ -342,8 +397,8 @@ struct Plan {
     uint32_t row_bytes;
     size_t smem;
 };
-bool ring_shape(size_t D, bool back, int* threads, int* elems) {
-    *elems = ring_elems(D);
+bool ring_shape(size_t es, size_t D, bool back, int* threads, int* elems) {
+    *elems = ring_elems(back, es, D);
     const size_t need = (D + *elems - 1) / *elems;
     *threads = (int)(need <= 32 ? 32 : (need + 31) / 32 * 32);
     return *threads <= ring_threads(back, *elems);
@@ -356,7 +411,7 @@ template <int N>
 Plan plan_of(const Mat (&m)[N], size_t es, uint64_t T, uint64_t D, bool back) {
     Plan p{};
     size_t period = 1;
-    p.ring = ring_shape(D, back, &p.threads, &p.elems) && aligned_alike(m, es, &period);
+    p.ring = ring_shape(es, D, back, &p.threads, &p.elems) && aligned_alike(m, es, &period);
     p.row_bytes = (uint32_t)((D * es + 15) / 16 * 16);
     p.warp = D <= warp_row(es);
     if (p.warp) p.threads = kRowWarps * 32;
@@ -450,9 +505,9 @@ extern "C" int abs_layer_norm(const void* x, uint64_t ld_x, const float* w, cons
 
 extern "C" size_t abs_layer_norm_workspace(uint64_t tokens, uint64_t width) {
     uint64_t most = kBackCtas;
-    int threads = 0, elems = 0;
-    if (ring_shape(width, true, &threads, &elems)) {
-        const uint64_t ring = (uint64_t)kSms * ring_ctas(true, threads, elems);
+    for (size_t es : {2, 4}) {           // of either type
+        int threads = 0, elems = 0;
+        const uint64_t ring = ring_shape(es, width, true, &threads, &elems) ? (uint64_t)kSms * ring_ctas(true, threads, elems) : 0;
         if (ring > most) most = ring;
     }
     const uint64_t rows = (tokens + 7) / 8 * 8;

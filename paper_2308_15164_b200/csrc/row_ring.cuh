@@ -78,6 +78,8 @@ __device__ __forceinline__ void copy_piece(void* to, const void* from) {
 // A CTA's rows (kWarp: a warp's): how they are cut, which of them are in flight, which is the current one.
 template <typename T, int kIn, int kP, bool kWarp>
 struct Ring {
+    using Element = T;
+    static constexpr int kInputs = kIn;
     RowCut cut;
     int extra;                       // column of this thread's single element, or -1
     const T* in[kIn];
