@@ -1,9 +1,10 @@
-"""A gated residual block with a vocabulary head, trained by W workers with the delayed synchronous step: how the operators
-of ``llm`` are used together, and how their gradients reach the accumulators.
+"""A small model trained by W workers with the delayed synchronous step: how the operators of ``llm`` are used together, and how
+their gradients reach the accumulators.
 
-    python -m paper_2308_15164_b200.llm_example [--objective policy|preference] [--iterations N]
+    python -m paper_2308_15164_b200.llm_example [--block gated|recurrent] [--objective policy|preference] [--iterations N]
 
-One micro-batch of one worker, at the published parameters x_t:
+--block gated: a gated residual block with a vocabulary head, on given hidden states.  --block recurrent: a recurrent language model from its
+tokens on (``llm_recurrent``).  One micro-batch of one worker, at the published parameters x_t, with the gated block:
 
     h = x W_in                                       (a plain product)
     y, n = residual_norm(x, h, w_pre, w_post, gate)  norm behind the block, learned gate, residual, norm in front of the head
@@ -19,6 +20,7 @@ All parameters are slices of the flat vector; every gradient is written straight
 from __future__ import annotations
 
 import argparse
+import sys
 from typing import List, NamedTuple
 
 import torch
@@ -135,24 +137,26 @@ def micro_batch(params, grad, b: Batch, s: Sizes, objective: str) -> torch.Tenso
     return r.loss
 
 
-def train(objective: str = "policy", iterations: int = 8, W: int = 4, micro_batches=(1, 1, 2, 3), lr: float = 0.2, sizes: Sizes = Sizes(),
-          seed: int = 0) -> List[float]:
-    """Mean loss of each iteration.  micro_batches[i]: what worker i manages in an iteration."""
-    from . import binding
+def train(objective: str = "policy", iterations: int = 8, W: int = 4, micro_batches=(1, 1, 2, 3), lr: float = 0.2, sizes=None,
+          seed: int = 0, block: str = "gated") -> List[float]:
+    """Mean loss of each iteration.  micro_batches[i]: what worker i manages in an iteration; sizes: the block's, its own defaults if not given."""
+    from . import binding, llm_recurrent
 
+    model = {"gated": sys.modules[__name__], "recurrent": llm_recurrent}[block]
+    sizes = model.Sizes() if sizes is None else sizes
     device = torch.device("cuda", torch.cuda.current_device())
-    flat = init_params(sizes, seed, device)
+    flat = model.init_params(sizes, seed, device)
     eng = binding.AbsSgd(flat, W, lr, momentum=0.9, pipelined=True)
     losses = []
     with torch.cuda.stream(eng.stream_acc):
-        reference = views(flat.clone(), sizes)
-        batches = [[make_batch(reference, sizes, objective, 1000 * i + k) for k in range(micro_batches[i])] for i in range(W)]
+        reference = model.views(flat.clone(), sizes)
+        batches = [[model.make_batch(reference, sizes, objective, 1000 * i + k) for k in range(micro_batches[i])] for i in range(W)]
         grad = torch.empty_like(flat)
         for _ in range(iterations):
             x_t, step = eng.params(), []
             for i in range(W):
                 for b in batches[i]:
-                    step.append(micro_batch(x_t, grad, b, sizes, objective))
+                    step.append(model.micro_batch(x_t, grad, b, sizes, objective))
                     eng.accumulate(i, grad)
             losses.append(torch.stack(step).mean())
             eng.sync_step()
@@ -164,10 +168,11 @@ def train(objective: str = "policy", iterations: int = 8, W: int = 4, micro_batc
 
 def main() -> None:
     ap = argparse.ArgumentParser(description=__doc__.split("\n\n")[0])
+    ap.add_argument("--block", choices=("gated", "recurrent"), default="gated")
     ap.add_argument("--objective", choices=("policy", "preference"), default="policy")
     ap.add_argument("--iterations", type=int, default=8)
     a = ap.parse_args()
-    for t, v in enumerate(train(a.objective, a.iterations)):
+    for t, v in enumerate(train(a.objective, a.iterations, block=a.block)):
         print(f"iteration {t}: loss {v:.5f}")
 
 
