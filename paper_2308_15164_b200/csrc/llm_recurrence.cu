@@ -50,7 +50,7 @@ struct RecArgs {
     int segs, rows;                      // segments, rows of one (a multiple of a tile; the last may have fewer)
     int parts, part_rows;                // of a segment, in the first pass: a map for each
     int pairs;                           // a lane's two columns are aligned to two elements in every matrix
-    float4* maps;                        // [segment][part][strip][lane]: a map (A, B) for two columns
+    struct Map* maps;                    // [segment][part][strip][lane]
 };
 
 // sigmoid(g) and 1 - sigmoid(g), each to its own precision.
@@ -68,23 +68,33 @@ __device__ __forceinline__ void gate_of(float2 g, float2& a, float2& rest, float
     a = make_float2(1.f / (1.f + e.x), 1.f / (1.f + e.y));
     rest = mul2(e, a);
 }
+// The maps of two columns.
+struct alignas(16) Map {
+    float2 A, B;
+};
+__device__ __forceinline__ Map identity() { return {make_float2(1.f, 1.f), make_float2(0.f, 0.f)}; }
 __device__ __forceinline__ bool forgets(float A) { return __float_as_uint(A) == 0x80000000u; }
-// (A, B) followed by (A2, B2).
-__device__ __forceinline__ void compose(float& A, float& B, float A2, float B2) {
-    if (forgets(A2)) {
-        A = A2;
-        B = B2;
-    } else {
-        B = fmaf(A2, B, B2);
-        A *= A2;
+// m followed by `then`; kForgets: either may forget what is in front of it.
+template <bool kForgets>
+__device__ __forceinline__ Map compose(Map m, Map then) {
+    Map r{mul2(m.A, then.A), fma2(then.A, m.B, then.B)};
+    if (kForgets && forgets(then.A.x)) {
+        r.A.x = then.A.x;
+        r.B.x = then.B.x;
     }
+    if (kForgets && forgets(then.A.y)) {
+        r.A.y = then.A.y;
+        r.B.y = then.B.y;
+    }
+    return r;
 }
-__device__ __forceinline__ float apply(float A, float B, float s) { return forgets(A) ? B : fmaf(A, s, B); }
-__device__ __forceinline__ void compose2(float4& m, float4 then) {
-    compose(m.x, m.y, then.x, then.y);
-    compose(m.z, m.w, then.z, then.w);
+template <bool kForgets>
+__device__ __forceinline__ float2 apply(Map m, float2 s) {
+    float2 r = fma2(m.A, s, m.B);
+    if (kForgets && forgets(m.A.x)) r.x = m.B.x;
+    if (kForgets && forgets(m.A.y)) r.y = m.B.y;
+    return r;
 }
-__device__ __forceinline__ float2 apply2(float4 m, float2 s) { return make_float2(apply(m.x, m.y, s.x), apply(m.z, m.w, s.y)); }
 
 // Two elements from shared or aligned global memory; n of two elements at any address.
 __device__ __forceinline__ float2 pair_of(const float* p) { return *reinterpret_cast<const float2*>(p); }
@@ -133,10 +143,9 @@ __device__ __forceinline__ int sequence_from(const RecArgs& a, int q, int t) {
 }
 
 struct RecSmem {
-    alignas(16) float4 map[2][kWarps][32];       // of a warp's rows, by the tile's parity
-    float4 front[kWarps][32];                    // of the segments in front, a run of them for each warp
+    Map map[2][kWarps][32];                      // of a warp's rows, by the tile's parity
+    Map front[kWarps][32];                       // of the segments in front, a run of them for each warp
     alignas(8) uint64_t full[3];
-    int begins[2];                               // a sequence begins in the tile
     int failed[2];
 };
 constexpr size_t kRecSmem = (sizeof(RecSmem) + 127) / 128 * 128;
@@ -170,7 +179,7 @@ __global__ void __launch_bounds__(kWarps * 32, kCtasOf<kBack, kMaps>) k_recurren
     auto tile_row = [&](int i) { return (int)row0 + (kMaps ? tiles - 1 - i : i) * kTile; };
     if (threadIdx.x == 0) {
         for (int i = 0; i < kStages; ++i) mbar_init(&s.full[i], 1);
-        s.failed[0] = s.failed[1] = s.begins[0] = s.begins[1] = 0;
+        s.failed[0] = s.failed[1] = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     pdl_wait();
@@ -197,25 +206,25 @@ __global__ void __launch_bounds__(kWarps * 32, kCtasOf<kBack, kMaps>) k_recurren
         for (int i = 0; i < kStages; ++i) copy_next();
 
     const int c = strip * kCols + lane * 2, n = min(max(a.D - c, 0), 2);
-    float4 behind = make_float4(1.f, 0.f, 1.f, 0.f);             // kMaps, warp 0: of the tiles so far
+    Map behind = identity();                                     // kMaps, warp 0: of the tiles so far
     float2 start = both(0.f);                                    // else: the state in front of the tile
     if (!kMaps && seg > 0) {
         const int all = seg * a.parts, per = (all + kWarps - 1) / kWarps, k0 = warp * per, k1 = min(k0 + per, all);
-        const float4* p = a.maps + (size_t)strip * 32 + lane;
-        float4 run = make_float4(1.f, 0.f, 1.f, 0.f);
+        const Map* p = a.maps + (size_t)strip * 32 + lane;
+        Map run = identity();
         for (int k = k0; k < k1; k += 8) {
-            float4 v[8];
+            Map v[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i)
                 if (k + i < k1) v[i] = p[(size_t)(k + i) * a.strips * 32];
 #pragma unroll
             for (int i = 0; i < 8; ++i)
-                if (k + i < k1) compose2(run, v[i]);
+                if (k + i < k1) run = compose<true>(run, v[i]);
         }
         s.front[warp][lane] = run;
         __syncthreads();
 #pragma unroll
-        for (int w = 0; w < kWarps; ++w) start = apply2(s.front[w][lane], start);
+        for (int w = 0; w < kWarps; ++w) start = apply<true>(s.front[w][lane], start);
     }
 
     const bool plain_strip = (strip + 1) * kCols <= a.D && a.pairs;
@@ -275,7 +284,7 @@ __global__ void __launch_bounds__(kWarps * 32, kCtasOf<kBack, kMaps>) k_recurren
 
         // ---- 1
         float2 keep[kRows], feed[kRows];                         // a; forward b, backward 1 - a
-        float4 m = make_float4(1.f, 0.f, 1.f, 0.f);
+        Map m = identity();
         auto collect = [&](auto all) {
             constexpr bool kAll = decltype(all)::value;
 #pragma unroll
@@ -289,48 +298,58 @@ __global__ void __launch_bounds__(kWarps * 32, kCtasOf<kBack, kMaps>) k_recurren
                 gate_of(gv, keep[r], z, T());
                 if (!in) keep[r] = both(1.f);
                 if (begins) {
-                    const float2 b = a.before ? given(a.before, r) : both(0.f);
-                    m = make_float4(-0.f, b.x, -0.f, b.y);
+                    m.A = both(-0.f);
+                    m.B = a.before ? given(a.before, r) : both(0.f);
                 }
-                float2 B = make_float2(m.y, m.w);
                 if (kBack) {
                     feed[r] = z;
-                    B = mul2(keep[r], add2(B, v));
+                    m.B = mul2(keep[r], add2(m.B, v));
                 } else {
                     feed[r] = !in ? both(0.f) : kKind == ABS_RECURRENCE_BLEND ? mul2(v, z) : v;
-                    B = fma2(keep[r], B, feed[r]);
-                    if (begins) feed[r] = B;                     // the sequence's first state
+                    m.B = fma2(keep[r], m.B, feed[r]);
+                    if (begins) feed[r] = m.B;                   // the sequence's first state
                 }
-                const float2 A = mul2(make_float2(m.x, m.z), keep[r]);
-                m = make_float4(A.x, B.x, A.y, B.y);
+                m.A = mul2(m.A, keep[r]);
             }
         };
         if (plain) collect(std::true_type());
         else collect(std::false_type());
         s.map[i & 1][warp][lane] = m;
-        if (kMaps && first != 0 && lane == 0) s.begins[i & 1] = 1;
-        __syncthreads();
+        const bool any_begins = __syncthreads_or(first != 0) != 0;     // a sequence begins in the tile
         // by the tile's parity: who is a tile ahead writes the other one, and nobody is two ahead
         failed = s.failed[i & 1] != 0;
         if (failed) break;
         // forward the tile's image has been read, backward that of the tile before
         if (threadIdx.x == 0 && (!kBack || kMaps || i > 0)) copy_next();
         // ---- 2
+        const Map* of = &s.map[i & 1][0][lane];                  // of warp w: of[32 w]
         if constexpr (kMaps) {
             if (warp == 0) {
-                float4 whole = make_float4(1.f, 0.f, 1.f, 0.f);
+                Map whole = of[0];
+                if (any_begins) {
 #pragma unroll
-                for (int w = 0; w < kWarps; ++w) compose2(whole, s.map[i & 1][w][lane]);
-                compose2(whole, behind);
-                behind = whole;
+                    for (int w = 1; w < kWarps; ++w) whole = compose<true>(whole, of[32 * w]);
+                } else {
+#pragma unroll
+                    for (int w = 1; w < kWarps; ++w) whole = compose<false>(whole, of[32 * w]);
+                }
+                behind = compose<false>(whole, behind);          // nothing begins in the tiles behind
             }
-            if (s.begins[i & 1]) break;
+            if (any_begins) break;
         } else {
             float2 state = start;
+            if (any_begins) {
 #pragma unroll
-            for (int w = 0; w < kWarps; ++w) {
-                if (w == warp) state = start;
-                start = apply2(s.map[i & 1][w][lane], start);
+                for (int w = 0; w < kWarps; ++w) {
+                    if (w == warp) state = start;
+                    start = apply<true>(of[32 * w], start);
+                }
+            } else {
+#pragma unroll
+                for (int w = 0; w < kWarps; ++w) {
+                    if (w == warp) state = start;
+                    start = apply<false>(of[32 * w], start);
+                }
             }
             // ---- 3
             auto finish = [&](auto all) {
@@ -468,7 +487,7 @@ template <typename T, uint32_t kKind, bool kBack>
 cudaError_t run_tiles(RecArgs a, bool tma, char* workspace, cudaStream_t s) {
     a.strips = (a.D + kCols - 1) / kCols;
     cut_segments<T, kBack>(a);
-    a.maps = reinterpret_cast<float4*>(workspace);
+    a.maps = reinterpret_cast<Map*>(workspace);
     return tma ? run_passes<T, kKind, kBack, true>(a, s) : run_passes<T, kKind, kBack, false>(a, s);
 }
 template <typename T, uint32_t kKind>
@@ -523,7 +542,7 @@ extern "C" size_t abs_recurrence_workspace(uint64_t tokens, uint64_t width) {
     if (tokens <= (uint64_t)kTileMin) return 0;
     // maps of the segments' parts: at most twice as many as the CTAs that fill the GPU
     const uint64_t strips = (width + kCols - 1) / kCols, most = std::min<uint64_t>(2 * 4 * kSms, (tokens + kTileMin - 1) / kTileMin * strips);
-    return up256((size_t)std::max(most, strips) * 32 * sizeof(float4));
+    return up256((size_t)std::max(most, strips) * 32 * sizeof(Map));
 }
 
 extern "C" int abs_recurrence(const void* x, uint64_t ld_x, const void* g, uint64_t ld_g, const int32_t* offsets, uint64_t seqs, const float* h0, uint32_t kind,
