@@ -24,17 +24,17 @@ namespace {
 constexpr int kWarps = 8, kCols = 64;    // of a tile; a lane owns two columns
 constexpr int kSms = 148;
 constexpr uint64_t kSizeMax = 0x7ffffc00ull;
-// Rows of a warp: 32 KB of inputs for a tile (two matrices forward, four backward); of the first pass 16 KB.
+// Rows of a warp, 16 forward and 8 backward (bf16): 32 KB of inputs for a tile, backward 16 KB in the first pass.
 template <typename T, bool kBack, bool kMaps>
-constexpr int kRowsOf = (kBack || kMaps ? 8 : 16) * 2 / (int)sizeof(T);
+constexpr int kRowsOf = (kBack ? 8 : 16) * 2 / (int)sizeof(T);
 template <typename T, bool kBack, bool kMaps>
 constexpr int kTileOf = kWarps * kRowsOf<T, kBack, kMaps>;
 template <bool kBack, bool kMaps>
-constexpr int kStagesOf = kBack && !kMaps ? 2 : 3;
+constexpr int kStagesOf = kMaps && !kBack ? 2 : 3;
 template <bool kBack, bool kMaps>
-constexpr int kCtasOf = kMaps ? 4 : kBack ? 3 : 2;       // of an SM
-template <bool kMaps>
-constexpr int kStageBytes = kMaps ? 16384 : 32768;
+constexpr int kCtasOf = !kMaps ? 2 : kBack ? 4 : 3;      // of an SM
+template <bool kBack, bool kMaps>
+constexpr int kStageBytes = kBack && kMaps ? 16384 : 32768;
 constexpr int kTileMin = kTileOf<float, true, false>;
 
 struct RecArgs {
@@ -165,7 +165,7 @@ __global__ void __launch_bounds__(kWarps * 32, kCtasOf<kBack, kMaps>) k_recurren
     constexpr int kRows = kRowsOf<T, kBack, kMaps>, kTile = kTileOf<T, kBack, kMaps>, kStages = kStagesOf<kBack, kMaps>;
     constexpr int kInput = kTile * kCols * (int)sizeof(T);       // bytes of an input's tile
     constexpr int kInputs = kBack && !kMaps ? 4 : 2;
-    static_assert(kInput * kInputs == kStageBytes<kMaps>, "");
+    static_assert(kInput * kInputs == kStageBytes<kBack, kMaps>, "");
     enum { kG, kIn, kX, kY };                                    // kIn: x, backward dy; kX backward only
     extern __shared__ uint8_t raw[];
     RecSmem& s = *reinterpret_cast<RecSmem*>((reinterpret_cast<uintptr_t>(raw) + 127) & ~(uintptr_t)127);
@@ -190,7 +190,7 @@ __global__ void __launch_bounds__(kWarps * 32, kCtasOf<kBack, kMaps>) k_recurren
             if (copied >= tiles) return;
             const int u0 = tile_row(copied), c = strip * kCols, st = copied % kStages;
             const int t = kBack ? a.T - u0 - kTile : u0;         // a first row below 0 reads zeros
-            uint8_t* to = ring + st * kStageBytes<kMaps>;
+            uint8_t* to = ring + st * kStageBytes<kBack, kMaps>;
             mbar_expect_tx(&s.full[st], kInput * kInputs);
             tma_load_2d(to + kG * kInput, &tm_g, c, t, &s.full[st]);
             tma_load_2d(to + kIn * kInput, kBack ? &tm_dy : &tm_x, c, t, &s.full[st]);
@@ -268,7 +268,7 @@ __global__ void __launch_bounds__(kWarps * 32, kCtasOf<kBack, kMaps>) k_recurren
         auto fetch = [&](int which, int r) {
             if constexpr (kTma) {
                 const int at = kBack ? kTile - 1 - (warp * kRows + r) : warp * kRows + r;
-                return pair_of(reinterpret_cast<const T*>(ring + stage * kStageBytes<kMaps> + which * kInput) + at * kCols + lane * 2);
+                return pair_of(reinterpret_cast<const T*>(ring + stage * kStageBytes<kBack, kMaps> + which * kInput) + at * kCols + lane * 2);
             } else {
                 const void* p = which == kG ? a.g : which == kIn ? (kBack ? a.dy : a.x) : which == kX ? a.x : a.y;
                 const size_t ld = which == kG ? a.ld_g : which == kIn ? (kBack ? a.ld_dy : a.ld_x) : which == kX ? a.ld_x : a.ld_y;
@@ -476,7 +476,7 @@ cudaError_t run_pass(const RecArgs& a, cudaStream_t s) {
     const cudaError_t e = allow_smem<k_recurrence<T, kKind, kBack, kTma, kMaps>>();
     if (e != cudaSuccess) return e;
     return launch_kernel(k_recurrence<T, kKind, kBack, kTma, kMaps>, (kMaps ? (a.segs - 1) * a.parts : a.segs) * a.strips, kWarps * 32,
-                         kRecSmem + (kTma ? kStagesOf<kBack, kMaps> * kStageBytes<kMaps> : 0) + 128, s, true, a, g, x, dy, y);
+                         kRecSmem + (kTma ? kStagesOf<kBack, kMaps> * kStageBytes<kBack, kMaps> : 0) + 128, s, true, a, g, x, dy, y);
 }
 template <typename T, uint32_t kKind, bool kBack, bool kTma>
 cudaError_t run_passes(const RecArgs& a, cudaStream_t s) {
