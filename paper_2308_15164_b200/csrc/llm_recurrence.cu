@@ -65,7 +65,9 @@ __device__ __forceinline__ void gate_of(float2 g, float2& a, float2& rest, bf16)
 }
 __device__ __forceinline__ void gate_of(float2 g, float2& a, float2& rest, float) {
     const float2 e = make_float2(expf(g.x < -87.f ? 87.f : -g.x), expf(g.y < -87.f ? 87.f : -g.y));
-    a = make_float2(1.f / (1.f + e.x), 1.f / (1.f + e.y));
+    const float2 d = add2(e, both(1.f));         // at most 2^126
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(a.x) : "f"(d.x));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(a.y) : "f"(d.y));
     rest = mul2(e, a);
 }
 // The maps of two columns.
