@@ -484,20 +484,20 @@ __global__ void __launch_bounds__(256) k_embed_few(const __grid_constant__ SumAr
     pdl_trigger();
     for (int t = threadIdx.x; t < kFew; t += 256) sh[t] = t < a.tokens ? ids[t] : -1;
     __syncthreads();
-    if ((int)blockIdx.x >= token_ctas) {                 // 32 rows a warp: a lane looks one up
+    if ((int)blockIdx.x >= token_ctas) {                 // four rows a warp
         const int lane = threadIdx.x % 32;
-        const int64_t step = (int64_t)(gridDim.x - token_ctas) * 8 * 32;
-        for (int64_t v0 = ((int64_t)(blockIdx.x - token_ctas) * 8 + threadIdx.x / 32) * 32; v0 < a.vocab; v0 += step) {
-            bool absent = v0 + lane < a.vocab;
-            for (int t = 0; t < a.tokens; ++t) absent = absent && sh[t] != (int)(v0 + lane);
-            uint32_t rows = __ballot_sync(0xffffffffu, absent);
-            const float zero[kE] = {};
-            while (rows) {
-                const int r = __ffs(rows) - 1;
-                rows &= rows - 1;
+        const int64_t step = (int64_t)(gridDim.x - token_ctas) * 8 * 4;
+        for (int64_t v0 = ((int64_t)(blockIdx.x - token_ctas) * 8 + threadIdx.x / 32) * 4; v0 < a.vocab; v0 += step)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                bool here = false;
+#pragma unroll
+                for (int t = 0; t < kFew; t += 32) here = here || sh[t + lane] == (int)(v0 + r);
+                if (__any_sync(0xffffffffu, here) || v0 + r >= a.vocab) continue;
+                const float zero[kE] = {};
+#pragma unroll 4
                 for (int j = lane; j < a.l.pieces; j += 32) store_f<kE>(a.out + (size_t)(v0 + r) * a.ld_out + (size_t)j * kE, zero);
             }
-        }
         return;
     }
     const int lane = threadIdx.x & ((1 << a.l.log) - 1), t = blockIdx.x * (256 >> a.l.log) + (threadIdx.x >> a.l.log);
@@ -570,7 +570,7 @@ cudaError_t sum_rows(SumArgs a, uint64_t width, const int32_t* few, cudaStream_t
     a.l = lanes_for(width, kE);
     const int groups = 256 >> a.l.log;
     if (few) {
-        const unsigned tokens = (unsigned)((a.tokens + groups - 1) / groups), rows = a.accumulate ? 0 : (unsigned)std::min<int64_t>(((int64_t)a.vocab + 255) / 256, kSms * 8);
+        const unsigned tokens = (unsigned)((a.tokens + groups - 1) / groups), rows = a.accumulate ? 0 : (unsigned)std::min<int64_t>(((int64_t)a.vocab + 31) / 32, kSms * 8);
         return launch_kernel(k_embed_few<T, kE>, tokens + rows, 256, 0, s, true, a, few, (int)tokens);
     }
     const dim3 grid((unsigned)((a.chunks + groups - 1) / groups), (unsigned)((a.l.pieces + (1 << a.l.log) - 1) >> a.l.log));
