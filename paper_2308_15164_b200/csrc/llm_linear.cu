@@ -36,6 +36,7 @@ struct LinArgs {
     bf16* z_out;                     // forward
     size_t ld_z;
     int accumulate;
+    int join;                        // tiles that are cut, or not, go through k_linear_join
     int wide;                        // what the rows of out, res and z are aligned to: 32, 16 bytes, or 0: less
 };
 
@@ -241,7 +242,11 @@ template <typename T>
 constexpr int kThreads = 64 + kEpiWarps<T> * 32;
 constexpr int kSms = 148;
 constexpr uint64_t kSizeMax = 0x7fffffc0ull;
-constexpr int kMinRuns = 12;     // runs of 64 that a part of a cut tile has at least
+constexpr int kMinRuns = 12;     // runs of 64 that a part of a cut tile has at least: shorter ones do not pay for the join (some 7 us)
+// Where rows of the output, residual or z are not 16-byte aligned the epilogue moves single elements; if it has to read some, they are read
+// in many small parts.  Up to kFewTiles tiles, which keep few SMs busy, that is left to k_linear_join, on all of them, and K is cut down to
+// kMinRunsJoin runs: 515 x 1000 x 1111 with residual 25 -> 21 us (without 18.6 / 20.6: stays).
+constexpr int kFewTiles = 37, kMinRunsJoin = 4;
 
 struct LinSmem {
     alignas(1024) uint8_t a[kStages][kHalf];
@@ -361,7 +366,7 @@ __global__ void __launch_bounds__(kThreads<T>, 1) k_linear(const __grid_constant
         if (it >= a.whole) {
             const int r = it - a.whole;
             tile = a.whole + r % a.rest;
-            if (a.splits > 1) {
+            if (a.join) {
                 q.part = r;
                 q.kb0 = min(kb_total, r / a.rest * a.kb_per_split);
                 q.kb1 = min(kb_total, q.kb0 + a.kb_per_split);
@@ -460,14 +465,15 @@ __global__ void __launch_bounds__(kThreads<T>, 1) k_linear(const __grid_constant
                     const int col = col0 + c * 16 + lane % 16;
                     if (c * 16 + lane % 16 < cols) {
                         const float bias = kEpi == kForward && a.bias ? __ldg(a.bias + col) : 0.f;
+                        constexpr int kRows = kSum<T> || (kEpi == kDgrad && kAct != ABS_ACT_NONE) ? 8 : 16;
 #pragma unroll 1
-                        for (int k0 = lane / 16; k0 < rows; k0 += 16) {
-                            FinishOne<kEpi, kAct, T> one[8];         // the reads of eight rows are in flight together
+                        for (int k0 = lane / 16; k0 < rows; k0 += 2 * kRows) {
+                            FinishOne<kEpi, kAct, T> one[kRows];     // the reads of as many rows are in flight together
 #pragma unroll
-                            for (int k = 0; k < 8; ++k)
+                            for (int k = 0; k < kRows; ++k)
                                 if (k0 + 2 * k < rows) one[k].load(a, q.m0 + row + k0 + 2 * k, col);
 #pragma unroll
-                            for (int k = 0; k < 8; ++k)
+                            for (int k = 0; k < kRows; ++k)
                                 if (k0 + 2 * k < rows) one[k](a, q.m0 + row + k0 + 2 * k, col, bias, stage[(k0 + 2 * k) * kPitch + lane % 16]);
                         }
                     }
@@ -536,7 +542,8 @@ __global__ void __launch_bounds__(kThreads<T>, 1) k_linear(const __grid_constant
     if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
 }
 
-// The tiles that were cut: their partial sums added up in order.  A warp per row of a tile, eight columns a thread.
+// The tiles that were cut: their partial sums added up in order.  A warp per row of a tile: eight columns a thread, or, where rows are
+// not aligned, every 32nd one.
 template <int kEpi, uint32_t kAct, typename T>
 __global__ void __launch_bounds__(256) k_linear_join(const __grid_constant__ LinArgs a) {
     pdl_wait();
@@ -546,44 +553,52 @@ __global__ void __launch_bounds__(256) k_linear_join(const __grid_constant__ Lin
     for (int i = blockIdx.x * 8 + threadIdx.x / 32; i < a.rest * kTM; i += gridDim.x * 8) {
         int m0, n0;
         place(a, a.whole + i / kTM, m0, n0);
-        const int row = m0 + i % kTM, col = n0 + lane * 8, n = min(8, a.N - col);
-        if (row >= a.M || n <= 0) continue;
-        const bool wide = a.wide && n == 8;
-        Finish<kEpi, kAct, T, 8> f;
-        if (wide) f.load(a, row, col);
-        float2 v[4] = {};
-        const float* p = a.part + (size_t)i * kTN + lane * 8;
+        const int row = m0 + i % kTM;
+        if (row >= a.M) continue;
+        const float* from = a.part + (size_t)i * kTN;
+        if (a.wide && n0 + kTN <= a.N) {
+            const int col = n0 + lane * 8;
+            const float* p = from + lane * 8;
+            Finish<kEpi, kAct, T, 8> f;
+            f.load(a, row, col);
+            float2 v[4] = {};
 #pragma unroll 4
-        for (int k = 0; k < a.splits; ++k) {
-            const float4 lo = *reinterpret_cast<const float4*>(p + k * step), hi = *reinterpret_cast<const float4*>(p + k * step + 4);
-            v[0] = add2(v[0], make_float2(lo.x, lo.y));
-            v[1] = add2(v[1], make_float2(lo.z, lo.w));
-            v[2] = add2(v[2], make_float2(hi.x, hi.y));
-            v[3] = add2(v[3], make_float2(hi.z, hi.w));
-        }
-        if (wide) {
+            for (int k = 0; k < a.splits; ++k) {
+                const float4 lo = *reinterpret_cast<const float4*>(p + k * step), hi = *reinterpret_cast<const float4*>(p + k * step + 4);
+                v[0] = add2(v[0], make_float2(lo.x, lo.y));
+                v[1] = add2(v[1], make_float2(lo.z, lo.w));
+                v[2] = add2(v[2], make_float2(hi.x, hi.y));
+                v[3] = add2(v[3], make_float2(hi.z, hi.w));
+            }
             f(a, row, col, v);
-        } else {
+            continue;
+        }
+        const int n = min(kTN, a.N - n0);
+        FinishOne<kEpi, kAct, T> one[8];
+        float v[8] = {};
 #pragma unroll
-            for (int k = 0; k < 8; ++k)
-                if (k < n) {
-                    FinishOne<kEpi, kAct, T> one;
-                    one.load(a, row, col + k);
-                    one(a, row, col + k, kEpi == kForward && a.bias ? a.bias[col + k] : 0.f, k % 2 ? v[k / 2].y : v[k / 2].x);
-                }
+        for (int c = 0; c < 8; ++c)
+            if (c * 32 + lane < n) one[c].load(a, row, n0 + c * 32 + lane);
+        for (int k = 0; k < a.splits; ++k)
+#pragma unroll
+            for (int c = 0; c < 8; ++c)
+                if (c * 32 + lane < n) v[c] += from[k * step + c * 32 + lane];
+#pragma unroll
+        for (int c = 0; c < 8; ++c) {
+            const int col = n0 + c * 32 + lane;
+            if (c * 32 + lane < n) one[c](a, row, col, kEpi == kForward && a.bias ? a.bias[col] : 0.f, v[c]);
         }
     }
 }
 
-// Rows that TMA cannot start at, copied to rows of `to_ld` elements (16-byte aligned), a warp per row.
-__global__ void __launch_bounds__(256) k_copy_rows(const bf16* x, size_t ld, int width, size_t to_ld, size_t rows, bf16* to) {
+// Rows that TMA cannot start at, copied to rows of `to_ld` elements (16-byte aligned), a CTA per row.
+__global__ void __launch_bounds__(128) k_copy_rows(const bf16* x, size_t ld, int width, size_t to_ld, size_t rows, bf16* to) {
     pdl_wait();
     pdl_trigger();
-    const int lane = threadIdx.x % 32;
-    for (size_t t = (size_t)blockIdx.x * 8 + threadIdx.x / 32; t < rows; t += (size_t)gridDim.x * 8) {
+    for (size_t t = blockIdx.x; t < rows; t += gridDim.x) {
         const uint16_t* from = reinterpret_cast<const uint16_t*>(x + t * ld);
 #pragma unroll 2
-        for (int c = lane * 8; c < width; c += 256) {
+        for (int c = threadIdx.x * 8; c < width; c += 1024) {
             uint32_t v[8];
 #pragma unroll
             for (int k = 0; k < 8; ++k) v[k] = c + k < width ? from[c + k] : 0u;
@@ -667,6 +682,7 @@ __global__ void __launch_bounds__(256) k_activation_backward(const T* dy, size_t
 // How the work is cut: whole output tiles for all pairs equally often, the rest in runs of K.
 struct LinPlan {
     int tiles_m, tiles_n, whole, rest, splits, kb_per_split;
+    int join_splits, join_kb;        // how K is cut where few tiles have to go through k_linear_join; 0: they have not
     bool pack_a, pack_b;
     uint64_t ld_a, ld_b;             // of the packed copies
     size_t part_bytes, a_bytes, b_bytes, bias_bytes;
@@ -688,11 +704,15 @@ bool plan_of(uint64_t M, uint64_t N, uint64_t K, const Operand& a, const Operand
     if (tiles > 0x3fffffff) return false;
     p.whole = (int)(tiles / pairs * pairs);
     p.rest = (int)(tiles - p.whole);
-    int splits = p.rest ? std::min(pairs / p.rest, kb / kMinRuns) : 1;
-    if (splits < 1) splits = 1;
-    p.kb_per_split = std::max(1, (kb + splits - 1) / splits);
-    p.splits = std::max(1, (kb + p.kb_per_split - 1) / p.kb_per_split);
-    p.part_bytes = p.splits > 1 ? (size_t)p.splits * p.rest * kTM * kTN * 4 : 0;
+    auto cut = [&](int min_runs, int* splits, int* per) {
+        const int want = p.rest ? std::max(1, std::min(pairs / p.rest, kb / min_runs)) : 1;
+        *per = std::max(1, (kb + want - 1) / want);
+        *splits = std::max(1, (kb + *per - 1) / *per);
+    };
+    cut(kMinRuns, &p.splits, &p.kb_per_split);
+    if (tiles <= kFewTiles) cut(kMinRunsJoin, &p.join_splits, &p.join_kb);
+    const int parts = std::max(p.splits > 1 ? p.splits : 0, p.join_splits);
+    p.part_bytes = (size_t)parts * p.rest * kTM * kTN * 4;
     p.pack_a = !tma_ready(a);
     p.pack_b = !tma_ready(b);
     p.ld_a = (a.cols + 7) / 8 * 8;
@@ -708,7 +728,7 @@ int bias_parts(uint64_t T, uint64_t N) {
 }
 
 cudaError_t copy_rows(const Operand& o, uint64_t to_ld, bf16* to, cudaStream_t s) {
-    return launch_kernel(k_copy_rows, (int)std::min<size_t>((o.rows + 7) / 8, kSms * 16), 256, 0, s, true, static_cast<const bf16*>(o.p), (size_t)o.ld, (int)o.cols, (size_t)to_ld,
+    return launch_kernel(k_copy_rows, (int)std::min<size_t>(o.rows, kSms * 16), 128, 0, s, true, static_cast<const bf16*>(o.p), (size_t)o.ld, (int)o.cols, (size_t)to_ld,
                          (size_t)o.rows, to);
 }
 
@@ -718,7 +738,7 @@ cudaError_t run_act(const CUtensorMap& ta, const CUtensorMap& tb, const LinArgs&
     if (e != cudaSuccess) return e;
     const int grid = 2 * std::min(a.whole + a.rest * a.splits, kSms / 2);
     e = launch_cluster(k_linear<kEpi, kAct, T>, grid, 2, kThreads<T>, sizeof(LinSmem) + 1024, s, ta, tb, a);
-    if (e == cudaSuccess && a.splits > 1) e = launch_kernel(k_linear_join<kEpi, kAct, T>, std::min(a.rest * kTM / 8, kSms * 8), 256, 0, s, false, a);
+    if (e == cudaSuccess && a.join) e = launch_kernel(k_linear_join<kEpi, kAct, T>, std::min(a.rest * kTM / 8, kSms * 8), 256, 0, s, false, a);
     return e;
 }
 template <int kEpi, typename T>
@@ -752,6 +772,13 @@ int product(int kind, uint32_t act, uint32_t dtype, Operand oa, Operand ob, uint
         return thread_error(ABS_ECUDA, "cuTensorMapEncodeTiled failed");
     a.M = (int)M; a.N = (int)N; a.K = (int)K;
     a.tiles_m = p.tiles_m; a.tiles_n = p.tiles_n; a.whole = p.whole; a.rest = p.rest; a.splits = p.splits; a.kb_per_split = p.kb_per_split;
+    a.join = p.splits > 1;
+    const bool reads = kind == kWgrad ? a.accumulate != 0 : a.res || a.z_in;
+    if (!a.wide && reads && p.join_splits) {
+        a.splits = p.join_splits;
+        a.kb_per_split = p.join_kb;
+        a.join = 1;
+    }
     a.part = reinterpret_cast<float*>(ws);
     if (kind == kForward) e = dtype == ABS_F32 ? run<kForward, float>(act, ta, tb, a, s) : run<kForward, bf16>(act, ta, tb, a, s);
     else if (kind == kDgrad) e = dtype == ABS_F32 ? run<kDgrad, float>(act, ta, tb, a, s) : run<kDgrad, bf16>(act, ta, tb, a, s);
