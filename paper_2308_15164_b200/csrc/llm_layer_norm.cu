@@ -4,9 +4,8 @@
 // Backward with c = x - mean, xh = c r, a = dn w:  dx = dskip + r (a - mean(a)) - c r^3 mean(a c),  dw = sum dn xh,  db = sum dn.
 // Plain sums of x and x^2 would lose what a large common offset leaves of the variance.  A CTA that owns a row takes all sums about
 // a pivot p, the mean of 32 of the row's elements, which every warp finds on its own: one reduction of the CTA instead of two.  The
-// pivot's distance from the mean is at most sqrt(D / 32) standard deviations, whatever the row holds (the 32 are part of the variance),
-// and usually a fifth of one; mean (x - p)^2 - (mean - p)^2 loses that much: D / 32 roundings at worst.  A warp that owns a row takes its
-// mean first.  Bound by memory: forward 2, backward 3 (4 with dskip) elements per position.
+// pivot is usually within a fifth of a standard deviation of the mean; where it is more than two off (the 32 happen to be far from the rest),
+// mean (x - p)^2 - (mean - p)^2 would lose digits, and the sums are taken again about the mean.  A warp that owns a row takes its mean first.  Bound by memory: forward 2, backward 3 (4 with dskip) elements per position.
 #include <math.h>
 
 #include "abs_internal.h"
@@ -57,6 +56,9 @@ __device__ __forceinline__ float var_of(float square, float d) {
     const float v = square - d * d;
     return v < 0.f ? 0.f : v;
 }
+
+// The pivot is so far from the mean that the sums about it lose digits.
+__device__ __forceinline__ bool far_off(float d, float var) { return d * d > 4.f * var; }
 
 // kV consecutive elements at a time, kV = 1 for rows that are not 16-byte aligned.
 template <typename T, int kV>
@@ -236,7 +238,22 @@ __global__ void __launch_bounds__(kWarp ? kRowWarps * 32 : ring_threads(false, k
             // every warp has read this row's image: it is filled again at once
             if (threadIdx.x == 0) r.load(r.st, t + (size_t)r.stages * G);
             d = s[0] * a.inv_d;
-            q = rsqrtf(var_of(s[1] * a.inv_d, d) + a.eps);
+            float var = var_of(s[1] * a.inv_d, d);
+            if (far_off(d, var)) {                   // the same for all threads
+                t2 = both(0.f);
+#pragma unroll
+                for (int j = 0; j < kP; ++j)
+                    if (r.has(j))
+#pragma unroll
+                        for (int i = 0; i < kN; ++i) {
+                            const float2 c = add2(v[j][i], both(-d));
+                            t2 = fma2(c, c, t2);
+                        }
+                float u[1] = {sum2(t2) + (r.extra >= 0 ? (xc - d) * (xc - d) : 0.f)};
+                row_sum<false>(u, r.ctl->red[2], warps);
+                var = u[0] * a.inv_d;
+            }
+            q = rsqrtf(var + a.eps);
         }
         T* n = static_cast<T*>(a.out) + t * a.ld_out;
 #pragma unroll
@@ -329,8 +346,32 @@ __global__ void __launch_bounds__(kWarp ? kRowWarps * 32 : ring_threads(true, kP
         }
         row_sum<kWarp>(s, r.ctl->red[k & 1], warps);
         const float d0 = kWarp ? 0.f : s[0] * a.inv_d;           // mean - pivot
-        const float q = rsqrtf(var_of(s[1] * a.inv_d, d0) + a.eps);
-        const float along = -q * q * q * (s[3] - d0 * s[2]) * a.inv_d;
+        float var = var_of(s[1] * a.inv_d, d0), inner = s[3] - d0 * s[2];
+        if (!kWarp && far_off(d0, var)) {                        // the same for all threads
+            float2 u2[2] = {both(0.f), both(0.f)};
+#pragma unroll
+            for (int j = 0; j < kP; ++j)
+                if (r.has(j)) {
+                    float2 d[kN];
+                    r.piece(1, j, d);
+#pragma unroll
+                    for (int i = 0; i < kN; ++i) {
+                        const float2 e = add2(c[j][i], both(-d0));
+                        u2[0] = fma2(e, e, u2[0]);
+                        u2[1] = fma2(mul2(d[i], w[j][i]), e, u2[1]);
+                    }
+                }
+            float u[2] = {sum2(u2[0]), sum2(u2[1])};
+            if (r.extra >= 0) {
+                u[0] += (xc - d0) * (xc - d0);
+                u[1] += xa * (xc - d0);
+            }
+            row_sum<kWarp>(u, r.ctl->red[2], warps);
+            var = u[0] * a.inv_d;
+            inner = u[1];
+        }
+        const float q = rsqrtf(var + a.eps);
+        const float along = -q * q * q * inner * a.inv_d;
         const float level = -q * s[2] * a.inv_d - d0 * along;    // dx = q a + (x - pivot) along + level
         T* dx = static_cast<T*>(a.out) + t * a.ld_out;
 #pragma unroll

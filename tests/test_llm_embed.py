@@ -102,6 +102,24 @@ def test_many_tokens(llm):
     R.close(llm.embed_backward(dy, ids, V), *R.embed_backward(dy, ids, V, 1.0))
 
 
+@pytest.mark.parametrize("T,V,W,dtype", [(30000, 40, 2048, "bf16"), (20000, 3, 1500, "f32"), (60000, 500, 520, "bf16"), (3000, 2900, 1030, "bf16"), (16384, 77, 40, "f32"), (16385, 77, 40, "f32")])
+def test_long_runs_of_wide_rows(llm, T, V, W, dtype):
+    """Chunks of more than sixteen tokens, runs over many of them; the sort by one cluster and by launches."""
+    dy = torch.randn(T, W, generator=gen(T), device=DEV).to(DT[dtype])
+    ids = ids_of(T, V, 11)
+    at = torch.where((ids >= 0) & (ids < V), ids, V).long()
+    want = torch.zeros(V + 1, W, dtype=torch.float64, device=DEV).index_add_(0, at, dy.double())[:-1]
+    size = torch.zeros(V + 1, W, dtype=torch.float64, device=DEV).index_add_(0, at, dy.double().abs())[:-1]
+    # a chunk's sum has at most 256 additions, the groups of a join add up the chunks in turn: some thousand at most, as bounded in the reference
+    tol = (torch.bincount(at, minlength=V + 1)[:-1, None] + 2) * R.U32 * size
+    got = llm.embed_backward(dy, ids, V)
+    R.close(got, want.cpu(), tol.cpu())
+    acc = torch.ones_like(got)
+    llm.embed_backward(dy, ids, V, out=acc, accumulate=True)
+    R.close(acc, (1 + want).cpu(), (tol + 2 * R.U32 * (1 + want.abs())).cpu())
+    assert torch.equal(llm.embed_backward(dy, ids, V), got)
+
+
 @pytest.mark.parametrize("shift,pad", [(0, 4), (1, 0), (2, 3)])
 def test_gradient_into_a_slice(llm, shift, pad):
     T, V, W = 200, 50, 40

@@ -121,6 +121,27 @@ def test_a_large_common_offset(llm, W):
     R.close(llm.layer_norm(x, w, b), want, tol)
 
 
+@pytest.mark.parametrize("W", [300, 512, 1000, 4096, 4100, 8192])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_rows_whose_samples_are_far_from_the_rest(llm, W, dtype):
+    """32 elements at equal distances far above the others, every start of the pattern, and rows that are zero but for one element."""
+    T = 2 * (W // 32) if W <= 1000 else 150
+    x = torch.randn(T, W, generator=gen(8), device=DEV)
+    for t in range(T):
+        x[t, t % (W // 32):: W // 32] += 3000.0
+    x[3] = 0.0
+    x[3, W // 2] = 100.0
+    x = x.to(DT[dtype])
+    w, b = weights(W)
+    want, tol, _ = R.layer_norm(x, w, b, EPS)
+    R.close(llm.layer_norm(x, w, b), want, tol)
+    dn = torch.randn(T, W, generator=gen(9), device=DEV).to(DT[dtype])
+    want, tol = R.layer_norm_backward(dn, x, w, None, EPS)
+    got = llm.layer_norm_backward(dn, x, w)
+    for k in want:
+        R.close(getattr(got, k), want[k], tol[k], k)
+
+
 def test_rows_with_what_is_no_number(llm):
     """A NaN or an infinity spoils its own row and the column sums, no other row."""
     T, W = 40, 512
