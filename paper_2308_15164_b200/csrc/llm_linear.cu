@@ -218,20 +218,25 @@ struct FinishOne {
 // 64 along K.  Roles in each CTA:
 //   warp 0      TMA producer, up to kStages runs ahead
 //   warp 1      (first CTA only) MMA issuer: four tcgen05.mma.cta_group::2 (M 256, N 256, K 16) per run into one of two TMEM accumulators
-//   warps 2-9   epilogue: they keep the tile's sums in registers and add a finished accumulator to them every kSegmentRuns runs (the
-//               tensor core drops low bits at each of its additions, so that its error grows with their number); then the layer's
-//               elementwise work, in rows of eight columns a thread, through a staging tile in shared memory.
+//   the others  epilogue, four warps for the rows, 64 or 128 columns each: bf16 results straight from TMEM, a row a thread, 16 columns and
+//               32 bytes at a time, with the reads of the next columns under way (through a staging tile in shared memory the results
+//               took a tenth of its bandwidth from the product: 266 -> 254 us); fp32 results are sums of several accumulators (kSegmentRuns)
 // Items are dealt out round-robin to the pairs: the whole tiles, as many as fill all pairs equally often, then the rest, each cut along K
 // into `splits` parts so that they too keep all pairs busy; k_linear_join adds those up in order and does the elementwise work.
 // Launched in plain stream order, and starts no successor early (see llm_ckpt8.cu).  Every wait on a barrier is bounded.
+// Bound by the tensor core where there is enough to do, and by the power limit in a loop: a library's bf16 product of the same operands alone took
+// (us, this kernel / the library): 8192 x 2048 x 8192 172 / 170, with GELU and z kept 206; 8192 x 8192 x 8192 738 / 674; gradient of the input
+// 8192 x 8192 x 2048 194 / 187; of the weight, with sums of 12 runs, 209 / 187.  Few tokens: 8 us for one tile of one run (launch in plain
+// order, tensor memory, first copies, epilogue), 16 runs of K 4 more.
 // ------------------------------------------------------------------------------------------------
 constexpr int kTM = 256, kTN = 256, kTK = 64;    // of a pair
 constexpr int kStages = 5;
 constexpr int kHalf = kTK * 128 * 2;             // bytes of an operand's share of a CTA and run
 constexpr int kPitch = 20;                       // floats of a staged row of 16: 16-byte pieces, eight rows on different banks
+// fp32 outputs: sums out of TMEM every kSegmentRuns runs, since the tensor core drops low bits at each of its additions.  Weight gradient of 8192
+// tokens, error of the result's norm / us of 8192 x 8192 x 2048: 12 runs 7e-7 / 215, 24 1.5e-6 / 210, 32 2.1e-6 / 208, never 8.6e-6 / 206.  bf16 ones are
+// rounded to 2^-9 anyway, and go straight from TMEM: without the sums the epilogue's registers do not spill.
 constexpr int kSegmentRuns = 12;
-// fp32 outputs: sums out of TMEM every kSegmentRuns runs.  bf16 ones are rounded to 2^-9 anyway, and go straight from TMEM: without the sums the
-// epilogue's registers do not spill.
 template <typename T>
 constexpr bool kSum = sizeof(T) == 4;
 template <typename T>
@@ -607,6 +612,14 @@ __global__ void __launch_bounds__(128) k_copy_rows(const bf16* x, size_t ld, int
     }
 }
 
+// n (1 .. 8) elements of a row, zeros behind them.
+__device__ __forceinline__ void load_row(Piece<bf16, 8>& w, const bf16* p, int n, bool wide) {
+    if (wide && n == 8) return w.load(p, false);
+    uint32_t v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = i < n ? reinterpret_cast<const uint16_t*>(p)[i] : 0u;
+    w.w[0] = make_uint4(v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16);
+}
 // Column sums of dy over the rows of a CTA: 256 columns, every gridDim.y-th group of eight rows.  launch_column_sums adds them up.
 __global__ void __launch_bounds__(256) k_bias_part(const bf16* dy, size_t ld, int T, int N, int wide, float* part, size_t part_ld) {
     __shared__ float sh[8][264];
@@ -621,15 +634,7 @@ __global__ void __launch_bounds__(256) k_bias_part(const bf16* dy, size_t ld, in
         for (int k = 0; k < 8; ++k) {
             w[k].w[0] = make_uint4(0, 0, 0, 0);
             if (t + k * step >= T) continue;
-            const bf16* p = dy + (size_t)(t + k * step) * ld + col;
-            if (wide && n == 8) {
-                w[k].load(p, false);
-            } else {
-                uint32_t v[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) v[i] = i < n ? reinterpret_cast<const uint16_t*>(p)[i] : 0u;
-                w[k].w[0] = make_uint4(v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16);
-            }
+            load_row(w[k], dy + (size_t)(t + k * step) * ld + col, n, wide != 0);
         }
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
@@ -648,6 +653,40 @@ __global__ void __launch_bounds__(256) k_bias_part(const bf16* dy, size_t ld, in
 #pragma unroll
     for (int w = 0; w < 8; ++w) v += sh[w][threadIdx.x];
     part[(size_t)blockIdx.y * 2 * part_ld + c] = v;
+}
+
+// All rows, 64 columns a CTA, in one launch: up to kFewRows rows, where a second launch costs more than the rows that a thread has one after the other.
+constexpr int kFewRows = 1024;
+__global__ void __launch_bounds__(256) k_bias_few(const bf16* dy, size_t ld, int T, int N, int wide, float* db, int accumulate) {
+    __shared__ float sh[32][72];
+    pdl_wait();
+    pdl_trigger();
+    const int piece = threadIdx.x % 8, line = threadIdx.x / 8, col = blockIdx.x * 64 + piece * 8, n = min(8, N - col);
+    float2 sum[4] = {};
+    for (int t = line; t < T && n > 0; t += 8 * 32) {
+        Piece<bf16, 8> w[8];                         // eight rows in flight
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            w[k].w[0] = make_uint4(0, 0, 0, 0);
+            if (t + k * 32 < T) load_row(w[k], dy + (size_t)(t + k * 32) * ld + col, n, wide != 0);
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            float2 v[4];
+            w[k].get(v);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sum[i] = add2(sum[i], v[i]);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) *reinterpret_cast<float2*>(&sh[line][piece * 8 + 2 * i]) = sum[i];
+    __syncthreads();
+    const int c = blockIdx.x * 64 + threadIdx.x;
+    if (threadIdx.x >= 64 || c >= N) return;
+    float v = 0.f;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) v += sh[i][threadIdx.x];
+    db[c] = accumulate ? db[c] + v : v;
 }
 
 template <uint32_t kAct, typename T>
@@ -923,9 +962,13 @@ extern "C" int abs_linear_wgrad(const void* x, uint64_t ld_x, const void* dy, ui
     if (db) {
         float* part = reinterpret_cast<float*>(static_cast<char*>(workspace) + p.part_bytes + p.a_bytes + p.b_bytes);
         const unsigned blocks = (unsigned)((out + 255) / 256);
-        e = launch_kernel(k_bias_part, dim3(blocks, p.bias_parts), 256, 0, s, true, static_cast<const bf16*>(dy), (size_t)ld_dy, (int)tokens, (int)out, (int)tma_ready(ob), part,
+        if (tokens <= (uint64_t)kFewRows)
+            e = launch_kernel(k_bias_few, (unsigned)((out + 63) / 64), 256, 0, s, true, static_cast<const bf16*>(dy), (size_t)ld_dy, (int)tokens, (int)out, (int)tma_ready(ob), db,
+                              accumulate);
+        else
+            e = launch_kernel(k_bias_part, dim3(blocks, p.bias_parts), 256, 0, s, true, static_cast<const bf16*>(dy), (size_t)ld_dy, (int)tokens, (int)out, (int)tma_ready(ob), part,
                           part_width(out));
-        if (e == cudaSuccess) e = launch_column_sums(part, p.bias_parts, (int)out, db, nullptr, accumulate, s);
+        if (e == cudaSuccess && tokens > (uint64_t)kFewRows) e = launch_column_sums(part, p.bias_parts, (int)out, db, nullptr, accumulate, s);
         if (e != cudaSuccess) return thread_error(ABS_ECUDA, cudaGetErrorString(e));
     }
     LinArgs a{};
