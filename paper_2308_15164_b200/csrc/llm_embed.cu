@@ -646,7 +646,7 @@ extern "C" int abs_embed_backward(const void* dy, uint64_t ld_dy, uint32_t dtype
     if (!few) {
         const bool one = p.blocks == 1, cluster = !one && tokens <= (uint64_t)kClusterMost;
         const int launches = one || cluster ? 1 : 2 * p.passes;
-        const int clear = accumulate ? 0 : (int)std::min<uint64_t>((vocab * width / launches + 4 * kSortThreads - 1) / (4 * kSortThreads), 3 * kSms);
+        const int clear = accumulate ? 0 : (int)std::min<uint64_t>(vocab * width / launches / (4 * kSortThreads) + 1, 3 * kSms);
         Clear c{dtable, (size_t)ld_dtable, 0, 0, (int)width, rows_at(m[0], 16) && width % 4 == 0};
         for (int i = 0; i < launches && e == cudaSuccess; ++i) {
             c.first = c.last;

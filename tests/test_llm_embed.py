@@ -94,6 +94,15 @@ def test_gradient_of_crowded_rows(llm, how, T):
     R.close(llm.embed_backward(dy, ids, V), *R.embed_backward(dy, ids, V, 1.0))
 
 
+@pytest.mark.parametrize("T", [1, 200, 5000, 20000])
+@pytest.mark.parametrize("V,W", [(1, 1), (1, 2), (2, 1), (3, 1)])
+def test_tiny_tables_of_padding_alone(llm, T, V, W):
+    """Every row is written, however few there are and however the tokens are sorted."""
+    out = torch.full((V, W), 7.0, device=DEV)
+    llm.embed_backward(torch.ones(T, W, device=DEV), torch.full((T,), -1, dtype=torch.int32, device=DEV), V, out=out)
+    assert (out == 0).all()
+
+
 def test_many_tokens(llm):
     """More blocks of the sort than one, all passes."""
     T, V, W = 300001, 152064, 1
