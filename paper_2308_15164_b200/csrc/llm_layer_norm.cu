@@ -8,6 +8,8 @@
 // mean (x - p)^2 - (mean - p)^2 would lose digits, and the sums are taken again about the mean.  A warp that owns a row takes its mean first.  Bound by memory: forward 2, backward 3 (4 with dskip) elements per position.
 #include <math.h>
 
+#include <algorithm>
+
 #include "abs_internal.h"
 #include "abs_llm.h"
 #include "llm_host.h"
@@ -19,7 +21,7 @@ namespace {
 
 constexpr int kWidthMax = 32768;
 constexpr int kSms = 148;
-constexpr int kBackCtas = 296;       // CTAs of the plain backward kernel
+constexpr int kColumnParts = 296;    // most parts of the rows for the plain column sums
 constexpr int kRingCtasMax = 16;
 // Threads of an SM for the ring kernels and CTAs of the form with a warp per row, by the elements that a thread owns: what the
 // registers leave room for.
@@ -47,6 +49,7 @@ struct LnArgs {
     void* out;                       // n; backward dx
     size_t ld_out;
     float* part;                     // [CTA][2][part_width(D)]: sum dn xh, sum dn
+    float2* stats;                   // [T]: mean, r (plain backward kernels)
     int stages;
     uint32_t row_bytes;
 };
@@ -97,59 +100,102 @@ __global__ void __launch_bounds__(256) k_layer_norm_plain(const __grid_constant_
     }
 }
 
+// The backward pass of matrices that are not aligned alike and of rows too wide for a CTA's registers: every row's mean and r, the column sums (a
+// CTA that kept them for whole rows would add them up in memory: 4096 x 16384 bf16 1660 us), then dx, which may take the place of x or dn.
 template <typename T, int kV>
-__global__ void __launch_bounds__(256) k_layer_norm_back_plain(const __grid_constant__ LnArgs a) {
-    __shared__ float sh[24];
+__global__ void __launch_bounds__(256) k_layer_norm_stats(const __grid_constant__ LnArgs a) {
+    __shared__ float sh[8];
     pdl_wait();
     pdl_trigger();
-    float *col = a.part + blockIdx.x * 2 * part_width(a.D), *col_b = col + part_width(a.D);
-    for (int c = threadIdx.x * kV; c < a.D; c += 256 * kV)
+    for (size_t t = blockIdx.x; t < a.T; t += gridDim.x) {
+        const T* x = static_cast<const T*>(a.x) + t * a.ld_x;
+        float s[1] = {0.f};
+        for (int c = threadIdx.x * kV; c < a.D; c += 256 * kV) {
+            float v[kV];
+            Pack<T, kV>::load(x + c, v);
 #pragma unroll
-        for (int k = 0; k < kV; ++k) col[c + k] = col_b[c + k] = 0.f;
+            for (int k = 0; k < kV; ++k) s[0] += v[k];
+        }
+        group_sum<256, 1>(s, sh);
+        const float mean = s[0] * a.inv_d;
+        s[0] = 0.f;
+        for (int c = threadIdx.x * kV; c < a.D; c += 256 * kV) {
+            float v[kV];
+            Pack<T, kV>::load(x + c, v);
+#pragma unroll
+            for (int k = 0; k < kV; ++k) s[0] += (v[k] - mean) * (v[k] - mean);
+        }
+        group_sum<256, 1>(s, sh);
+        if (threadIdx.x == 0) a.stats[t] = make_float2(mean, 1.f / sqrtf(s[0] * a.inv_d + a.eps));
+    }
+}
+template <typename T, int kV>
+__global__ void __launch_bounds__(256) k_layer_norm_back_plain(const __grid_constant__ LnArgs a) {
+    __shared__ float sh[16];
+    pdl_wait();
+    pdl_trigger();
     for (size_t t = blockIdx.x; t < a.T; t += gridDim.x) {
         const T* x = static_cast<const T*>(a.x) + t * a.ld_x;
         const T* dn = static_cast<const T*>(a.dn) + t * a.ld_dn;
         const T* skip = a.skip ? static_cast<const T*>(a.skip) + t * a.ld_skip : nullptr;
         T* dx = static_cast<T*>(a.out) + t * a.ld_out;
-        float m[1] = {0.f};
-        for (int c = threadIdx.x * kV; c < a.D; c += 256 * kV) {
-            float v[kV];
-            Pack<T, kV>::load(x + c, v);
-#pragma unroll
-            for (int k = 0; k < kV; ++k) m[0] += v[k];
-        }
-        group_sum<256, 1>(m, sh);
-        const float mean = m[0] * a.inv_d;
-        float s[3] = {0.f, 0.f, 0.f};            // sum c^2, a, a c
+        const float mean = a.stats[t].x, r = a.stats[t].y;
+        float s[2] = {0.f, 0.f};                 // sum a, a c
         for (int c = threadIdx.x * kV; c < a.D; c += 256 * kV) {
             float v[kV], d[kV];
             Pack<T, kV>::load(x + c, v);
             Pack<T, kV>::load(dn + c, d);
 #pragma unroll
             for (int k = 0; k < kV; ++k) {
-                const float e = v[k] - mean, f = d[k] * a.w[c + k];
-                s[0] += e * e;
-                s[1] += f;
-                s[2] += f * e;
+                const float f = d[k] * a.w[c + k];
+                s[0] += f;
+                s[1] += f * (v[k] - mean);
             }
         }
-        group_sum<256, 3>(s, sh);
-        const float r = 1.f / sqrtf(s[0] * a.inv_d + a.eps), level = s[1] * a.inv_d, along = s[2] * a.inv_d * r;
+        group_sum<256, 2>(s, sh);
+        const float level = s[0] * a.inv_d, along = s[1] * a.inv_d * r;
         for (int c = threadIdx.x * kV; c < a.D; c += 256 * kV) {
             float v[kV], d[kV], o[kV];
             Pack<T, kV>::load(x + c, v);
             Pack<T, kV>::load(dn + c, d);
             if (skip) Pack<T, kV>::load(skip + c, o);
 #pragma unroll
-            for (int k = 0; k < kV; ++k) {
-                const float xh = (v[k] - mean) * r;
-                col[c + k] += d[k] * xh;
-                col_b[c + k] += d[k];
-                o[k] = (skip ? o[k] : 0.f) + r * (d[k] * a.w[c + k] - level - xh * along);
-            }
+            for (int k = 0; k < kV; ++k) o[k] = (skip ? o[k] : 0.f) + r * (d[k] * a.w[c + k] - level - (v[k] - mean) * r * along);
             Pack<T, kV>::store(dx + c, o);
         }
     }
+}
+
+// A thread per column.
+template <typename T>
+__global__ void __launch_bounds__(256) k_layer_norm_columns(const __grid_constant__ LnArgs a) {
+    pdl_wait();
+    pdl_trigger();
+    const int c = blockIdx.x * 256 + threadIdx.x;
+    if (c >= a.D) return;
+    float w = 0.f, b = 0.f;
+    for (size_t t = blockIdx.y; t < a.T; t += 8 * (size_t)gridDim.y) {
+        float x[8], d[8];
+        float2 s[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const size_t u = t + k * (size_t)gridDim.y;
+            x[k] = d[k] = 0.f;
+            s[k] = make_float2(0.f, 0.f);
+            if (u >= a.T) continue;
+            x[k] = to_f(static_cast<const T*>(a.x)[u * a.ld_x + c]);
+            d[k] = to_f(static_cast<const T*>(a.dn)[u * a.ld_dn + c]);
+            s[k] = a.stats[u];
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            w = fmaf(d[k], (x[k] - s[k].x) * s[k].y, w);
+            b += d[k];
+        }
+    }
+    float* part = a.part + blockIdx.y * 2 * part_width(a.D);
+    part[c] = w;
+    part[part_width(a.D) + c] = b;
 }
 
 // The mean of 32 elements of the current row's image of input 0, the same in every warp.  The image has 32 elements at least.
@@ -435,6 +481,7 @@ struct Plan {
     bool ring, warp;                 // warp: a warp per row
     int threads, elems;              // of a CTA; elements that a thread owns
     int grid, stages;
+    int parts;                       // rows of partial column sums
     uint32_t row_bytes;
     size_t smem;
 };
@@ -468,20 +515,23 @@ Plan plan_of(const Mat (&m)[N], size_t es, uint64_t T, uint64_t D, bool back) {
         p.smem = kRingCtl + p.stages * row;
     }
     if (!p.ring) {
-        const uint64_t cap = back ? kBackCtas : kSms * 8;
-        p.grid = (int)(T < cap ? T : cap);
+        p.grid = (int)std::min<uint64_t>(T, kSms * 8);
+        if (back) {        // four CTAs an SM for the columns
+            const uint64_t blocks = (D + 255) / 256, parts = std::max<uint64_t>(1, 4 * kSms / blocks);
+            p.parts = (int)std::min(std::min<uint64_t>(parts, kColumnParts), (T + 7) / 8);
+        }
         return p;
     }
     if (p.warp) {
         const uint64_t want = (T + kRowWarps - 1) / kRowWarps, all = (uint64_t)kSms * ctas;
-        p.grid = (int)(want < all ? want : all);
+        p.parts = p.grid = (int)(want < all ? want : all);
         return p;
     }
     if (back)          // at least two rows per CTA, whose column sums cost as much as a row
         while (ctas > 1 && kSms * ctas * 2 > T) --ctas;
     const size_t all = (size_t)kSms * ctas / period * period;       // a multiple of the period: rows of a CTA are cut alike
     const size_t want = (T + period - 1) / period * period;
-    p.grid = (int)(want < all ? want : all);
+    p.parts = p.grid = (int)(want < all ? want : all);
     return p;
 }
 
@@ -495,12 +545,15 @@ cudaError_t run_ring(LnArgs a, bool back, const Plan& p, cudaStream_t s) {
     return launch_kernel(back ? k_layer_norm_back<T, kP, kWarp> : k_layer_norm<T, kP, kWarp>, p.grid, p.threads, p.smem, s, true, a);
 }
 template <typename T, int kV>
-cudaError_t run_plain(const LnArgs& a, bool back, int grid, cudaStream_t s) {
-    return launch_kernel(back ? k_layer_norm_back_plain<T, kV> : k_layer_norm_plain<T, kV>, grid, 256, 0, s, true, a);
+cudaError_t run_plain(const LnArgs& a, bool back, const Plan& p, cudaStream_t s) {
+    if (!back) return launch_kernel(k_layer_norm_plain<T, kV>, p.grid, 256, 0, s, true, a);
+    cudaError_t e = launch_kernel(k_layer_norm_stats<T, kV>, p.grid, 256, 0, s, true, a);
+    if (e == cudaSuccess) e = launch_kernel(k_layer_norm_columns<T>, dim3((unsigned)((a.D + 255) / 256), p.parts), 256, 0, s, true, a);
+    return e != cudaSuccess ? e : launch_kernel(k_layer_norm_back_plain<T, kV>, p.grid, 256, 0, s, true, a);
 }
 template <typename T>
 cudaError_t run(const LnArgs& a, bool back, bool wide, const Plan& p, cudaStream_t s) {
-    if (!p.ring) return wide ? run_plain<T, kVec<T>>(a, back, p.grid, s) : run_plain<T, 1>(a, back, p.grid, s);
+    if (!p.ring) return wide ? run_plain<T, kVec<T>>(a, back, p, s) : run_plain<T, 1>(a, back, p, s);
     if (p.warp && p.elems == 8) return run_ring<T, 8, true>(a, back, p, s);
     if constexpr (warp_row(sizeof(T)) > 256)
         if (p.warp) return run_ring<T, 16, true>(a, back, p, s);
@@ -544,8 +597,9 @@ extern "C" int abs_layer_norm(const void* x, uint64_t ld_x, const float* w, cons
     return e == cudaSuccess ? ABS_OK : thread_error(ABS_ECUDA, cudaGetErrorString(e));
 }
 
-extern "C" size_t abs_layer_norm_workspace(uint64_t tokens, uint64_t width) {
-    uint64_t most = kBackCtas;
+// Partial column sums; behind them the rows' mean and r.
+static size_t part_bytes(uint64_t tokens, uint64_t width) {
+    uint64_t most = kColumnParts;
     for (size_t es : {2, 4}) {           // of either type
         int threads = 0, elems = 0;
         const uint64_t ring = ring_shape(es, width, true, &threads, &elems) ? (uint64_t)kSms * ring_ctas(true, threads, elems) : 0;
@@ -554,6 +608,7 @@ extern "C" size_t abs_layer_norm_workspace(uint64_t tokens, uint64_t width) {
     const uint64_t rows = (tokens + 7) / 8 * 8;
     return ((size_t)(rows < most ? rows : most) * 2 * part_width(width) * 4 + 255) / 256 * 256 + 256;
 }
+extern "C" size_t abs_layer_norm_workspace(uint64_t tokens, uint64_t width) { return part_bytes(tokens, width) + up256(tokens * sizeof(float2)); }
 
 extern "C" int abs_layer_norm_backward(const void* dn, uint64_t ld_dn, const void* x, uint64_t ld_x, const void* dskip, uint64_t ld_dskip, const float* w, float eps,
                                        uint32_t dtype, uint64_t tokens, uint64_t width, void* dx, uint64_t ld_dx, float* dw, float* db, int accumulate,
@@ -573,6 +628,7 @@ extern "C" int abs_layer_norm_backward(const void* dn, uint64_t ld_dn, const voi
     LnArgs a{};
     a.x = x; a.ld_x = ld_x; a.dn = dn; a.ld_dn = ld_dn; a.skip = dskip; a.ld_skip = ld_dskip; a.w = w; a.eps = eps; a.inv_d = 1.f / (float)width;
     a.T = tokens; a.D = (int)width; a.out = dx; a.ld_out = ld_dx; a.part = static_cast<float*>(workspace);
+    a.stats = reinterpret_cast<float2*>(static_cast<char*>(workspace) + part_bytes(tokens, width));
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     cudaError_t e = cudaSuccess;
     Plan p{};
@@ -582,6 +638,6 @@ extern "C" int abs_layer_norm_backward(const void* dn, uint64_t ld_dn, const voi
         const bool wide = rows_aligned(m, es, width);
         e = dtype == ABS_F32 ? run<float>(a, true, wide, p, s) : run<bf16>(a, true, wide, p, s);
     }
-    if (e == cudaSuccess) e = launch_column_sums(a.part, p.grid, (int)width, dw, db, accumulate, s);
+    if (e == cudaSuccess) e = launch_column_sums(a.part, p.parts, (int)width, dw, db, accumulate, s);
     return e == cudaSuccess ? ABS_OK : thread_error(ABS_ECUDA, cudaGetErrorString(e));
 }
