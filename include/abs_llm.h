@@ -3,7 +3,7 @@
  *
  * The library's own gradient (abs_accumulate_mlp) is that of a small classifier.  A model that is trained with
  * Algorithm 1 but brings its own forward and backward pass hands its flat gradient to abs_accumulate; these calls are
- * the parts of such a pass that are not matrix products of plain operands:
+ * the parts of such a pass:
  *     abs_policy_loss             clipped policy loss with a KL term, from logits to the gradient of the logits
  *     abs_preference_loss         paired preference loss, likewise
  *     abs_residual_norm           norm behind a block, gate, scaled residual, norm in front of the next block
@@ -146,8 +146,7 @@ int abs_ckpt8_wgrad(const int8_t *q, const uint8_t *e, const void *dy, uint64_t 
 int abs_embed(const int32_t *ids, uint64_t tokens, const float *table, uint64_t ld_table, uint64_t vocab, uint64_t width, float scale,
               uint32_t dtype, void *y, uint64_t ld_y, void *stream);
 
-/* dtable[v, :] = scale sum over the tokens with id v of dy[t, :], in the tokens' order; every row is written, those of no token
- * with zeros.  accumulate != 0: added to what the table holds, rows of no token are not touched.
+/* dtable[v, :] = scale sum over the tokens with id v of dy[t, :]; every row is written, those of no token with zeros.  accumulate != 0: added to what the table holds, rows of no token are not touched.
  *   dy [tokens, width] of `dtype`; dtable [vocab, width] fp32, ld_dtable >= width, 4-byte aligned (a slice of a flat gradient).
  * Limits as for abs_embed.  workspace: abs_embed_backward_workspace() bytes. */
 size_t abs_embed_backward_workspace(uint64_t tokens, uint64_t vocab, uint64_t width);

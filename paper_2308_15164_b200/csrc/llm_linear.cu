@@ -695,7 +695,7 @@ __global__ void __launch_bounds__(256) k_activation_backward(const T* dy, size_t
     pdl_trigger();
     const size_t per_row = ((size_t)width + 7) / 8;
     for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < rows * per_row; i += (size_t)gridDim.x * 256) {
-        const size_t t = i / per_row;
+        const size_t t = rows * per_row >> 32 ? i / per_row : (uint32_t)i / (uint32_t)per_row;
         const int c = (int)(i - t * per_row) * 8, n = min(8, width - c);
         const T* p = dy + t * ld_dy + c;
         const bf16* q = z + t * ld_z + c;
