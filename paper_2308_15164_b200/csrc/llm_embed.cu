@@ -306,7 +306,7 @@ struct SumArgs {
     const uint2* list;
     const void* dy;
     size_t ld_dy;
-    int tokens, vocab, D;
+    int tokens, vocab;
     float scale;
     float* out;
     size_t ld_out;
@@ -658,7 +658,7 @@ extern "C" int abs_embed_backward(const void* dy, uint64_t ld_dy, uint32_t dtype
         if (e != cudaSuccess) return thread_error(ABS_ECUDA, cudaGetErrorString(e));
     }
     SumArgs q{};
-    q.list = a.buf[(p.passes - 1) & 1]; q.dy = dy; q.ld_dy = ld_dy; q.tokens = (int)tokens; q.vocab = (int)vocab; q.D = (int)width; q.scale = scale;
+    q.list = a.buf[(p.passes - 1) & 1]; q.dy = dy; q.ld_dy = ld_dy; q.tokens = (int)tokens; q.vocab = (int)vocab; q.scale = scale;
     q.out = dtable; q.ld_out = ld_dtable; q.accumulate = accumulate != 0; q.chunk = p.chunk; q.chunks = p.chunks;
     q.part = reinterpret_cast<float*>(ws + 2 * p.list_bytes + p.count_bytes); q.width = p.width;
     const int32_t* all = few ? ids : nullptr;
