@@ -218,33 +218,37 @@ struct FinishOne {
 // 64 along K.  Roles in each CTA:
 //   warp 0      TMA producer, up to kStages runs ahead
 //   warp 1      (first CTA only) MMA issuer: four tcgen05.mma.cta_group::2 (M 256, N 256, K 16) per run into one of two TMEM accumulators
-//   the others  epilogue, four warps for the rows, 64 or 128 columns each: bf16 results straight from TMEM, a row a thread, 16 columns and
-//               32 bytes at a time, with the reads of the next columns under way (through a staging tile in shared memory the results
-//               took a tenth of its bandwidth from the product: 266 -> 254 us); fp32 results are sums of several accumulators (kSegmentRuns)
+//   the others  epilogue, four warps for the rows, a row a thread, 16 columns at a time with the reads of the next ones under way (through a
+//               staging tile in shared memory the results took a tenth of its bandwidth from the product: 266 -> 254 us)
+//                 kSum    eight warps of 128 columns add up an item's segments (kSegmentRuns) in registers
+//                 else    bf16 results of items of one segment straight from TMEM, sixteen warps of 64 columns (8192 x 256 x 8192: 57 us,
+//                         through registers with eight warps 97)
 // Items are dealt out round-robin to the pairs: the whole tiles, as many as fill all pairs equally often, then the rest, each cut along K
 // into `splits` parts so that they too keep all pairs busy; k_linear_join adds those up in order and does the elementwise work.
 // Launched in plain stream order, and starts no successor early (see llm_ckpt8.cu).  Every wait on a barrier is bounded.
 // Bound by the tensor core where there is enough to do, and by the power limit in a loop: a library's bf16 product of the same operands alone took
-// (us, this kernel / the library): 8192 x 2048 x 8192 172 / 170, with GELU and z kept 206; 8192 x 8192 x 8192 738 / 674; gradient of the input
-// 8192 x 8192 x 2048 194 / 187; of the weight, with sums of 12 runs, 209 / 187.  Few tokens: 8 us for one tile of one run (launch in plain
-// order, tensor memory, first copies, epilogue), 16 runs of K 4 more.
+// (us, this kernel / the library): 8192 x 8192 x 8192 774 / 674; gradient of the input 8192 x 8192 x 2048 202 / 187; of the weight, with sums of 12 runs,
+// 209 / 187; 8192 x 2048 x 8192 211, with GELU 225, and z kept 238.  Few tokens: 8 us for one tile of one run (launch in plain order, tensor memory,
+// first copies, epilogue), 16 runs of K 4 more.
 // ------------------------------------------------------------------------------------------------
 constexpr int kTM = 256, kTN = 256, kTK = 64;    // of a pair
 constexpr int kStages = 5;
 constexpr int kHalf = kTK * 128 * 2;             // bytes of an operand's share of a CTA and run
 constexpr int kPitch = 20;                       // floats of a staged row of 16: 16-byte pieces, eight rows on different banks
-// fp32 outputs: sums out of TMEM every kSegmentRuns runs, since the tensor core drops low bits at each of its additions.  Weight gradient of 8192
-// tokens, error of the result's norm / us of 8192 x 8192 x 2048: 12 runs 7e-7 / 215, 24 1.5e-6 / 210, 32 2.1e-6 / 208, never 8.6e-6 / 206.  bf16 ones are
-// rounded to 2^-9 anyway, and go straight from TMEM: without the sums the epilogue's registers do not spill.
-constexpr int kSegmentRuns = 12;
+// Sums are taken out of TMEM every kSegmentRuns runs and added up in fp32, since the tensor core drops low bits at each of its additions: without, the
+// error grows with K (positive terms, K 16384: up to 8e-5).  Weight gradient of 8192 tokens, error of the result's norm / us of 8192 x 8192 x 2048: 12 runs
+// 7e-7 / 215, 24 1.5e-6 / 210, 32 2.1e-6 / 208, never 8.6e-6 / 206.  bf16 results, which are rounded to 2^-9, take 16 runs: with 12, a K of 1024 would need
+// two segments (7 x 1024 x 1024 with GELU 15.4 us, in two 18.4; 8192 x 2048 x 8192 211 and 214; never 200).
 template <typename T>
-constexpr bool kSum = sizeof(T) == 4;
-template <typename T>
-constexpr int kEpiWarps = kSum<T> ? 8 : 16;
-template <typename T>
-constexpr int kWarpCols = kTN / (kEpiWarps<T> / 4);  // columns of an epilogue warp
-template <typename T>
-constexpr int kThreads = 64 + kEpiWarps<T> * 32;
+constexpr int kSegmentRuns = sizeof(T) == 4 ? 12 : 16;
+template <bool kSum>
+constexpr int kEpiWarps = kSum ? 8 : 16;
+template <bool kSum>
+constexpr int kFirstEpi = kSum ? 4 : 2;                          // the epilogue's first warp
+template <bool kSum>
+constexpr int kWarpCols = kTN / (kEpiWarps<kSum> / 4);           // columns of an epilogue warp
+template <bool kSum>
+constexpr int kThreads = (kFirstEpi<kSum> + kEpiWarps<kSum>) * 32;
 constexpr int kSms = 148;
 constexpr uint64_t kSizeMax = 0x7fffffc0ull;
 constexpr int kMinRuns = 12;     // runs of 64 that a part of a cut tile has at least: shorter ones do not pay for the join (some 7 us)
@@ -324,11 +328,12 @@ __device__ __forceinline__ uint64_t operand_desc(uint32_t at, int k16) {
     return kMn ? umma_desc_mn_sw128(at + k16 * 2048, kHalf / 2) : umma_desc_k_sw128(at + k16 * 32);
 }
 
-template <int kEpi, uint32_t kAct, typename T>
-__global__ void __launch_bounds__(kThreads<T>, 1) k_linear(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_b,
+template <int kEpi, uint32_t kAct, typename T, bool kSum>
+__global__ void __launch_bounds__(kThreads<kSum>, 1) k_linear(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_b,
                                                         const __grid_constant__ LinArgs a) {
     constexpr bool kAMn = kEpi == kWgrad, kBMn = kEpi != kDgrad;
-    constexpr int kSegment = kSum<T> ? kSegmentRuns : 1 << 30;       // runs that the tensor core adds up on its own
+    static_assert(kSum || sizeof(T) == 2, "");
+    constexpr int kCols = kWarpCols<kSum>;
     extern __shared__ uint8_t smem_raw[];
     LinSmem& s = *reinterpret_cast<LinSmem*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
@@ -347,7 +352,7 @@ __global__ void __launch_bounds__(kThreads<T>, 1) k_linear(const __grid_constant
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(&s.acc_full[i], 1);
-            mbar_init(&s.acc_empty[i], 2 * kEpiWarps<T>);       // the epilogue warps of each CTA
+            mbar_init(&s.acc_empty[i], 2 * kEpiWarps<kSum>);       // the epilogue warps of each CTA
         }
         s.failed = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -381,53 +386,58 @@ __global__ void __launch_bounds__(kThreads<T>, 1) k_linear(const __grid_constant
         return q;
     };
 
-    if (warp == 0) {
-        if (lane == 0) {                             // ---- TMA producer
-            uint32_t st = 0, round = 0;
-            for (int it = pair; it < items && !*failed; it += pairs) {
-                const Item q = item_of(it);
-                for (int kb = q.kb0; kb < q.kb1; ++kb) {
-                    if (round > 0 && !mbar_wait(&s.empty[st], (round - 1) & 1)) { *failed = 1; break; }
-                    if (rank == 0) mbar_expect_tx(&s.full[st], 4 * kHalf);
-                    load_operand<kAMn>(s.a[st], &tm_a, q.m0 + rank * 128, kb * kTK, &s.full[st]);
-                    load_operand<kBMn>(s.b[st], &tm_b, q.n0 + rank * 128, kb * kTK, &s.full[st]);
-                    if (++st == kStages) { st = 0; ++round; }
-                }
-            }
-            if (*failed && rank == 0)                // copies in flight land before the CTAs' shared memory is released
-                for (uint32_t i = 0; i < kStages; ++i) mbar_wait(&s.full[i], (round + (i < st ? 0u : 1u)) & 1u, 4096u);
-        }
-    } else if (warp == 1) {
-        if (lane == 0 && rank == 0) {                // ---- MMA issuer
-            constexpr uint32_t idesc = umma_idesc_bf16(kTM, kTN) | (kAMn ? 1u << 15 : 0u) | (kBMn ? 1u << 16 : 0u);
-            uint32_t st = 0, phase = 0;
-            int i = 0;                               // segments so far: every other one in the same accumulator
-            bool ok = true;
-            for (int it = pair; it < items && ok; it += pairs) {
-                const Item q = item_of(it);
-                for (int kb0 = q.kb0; kb0 < q.kb1 && ok; kb0 += min(kSegment, q.kb1 - kb0), ++i) {
-                    const int ab = i & 1, kb1 = kb0 + min(kSegment, q.kb1 - kb0);
-                    if (i >= 2 && !mbar_wait(&s.acc_empty[ab], ((i / 2) - 1) & 1)) { ok = false; break; }
-                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                    for (int kb = kb0; kb < kb1; ++kb) {
-                        if (!mbar_wait(&s.full[st], phase)) { ok = false; break; }
-                        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                        const uint32_t a0 = smem_u32(s.a[st]), b0 = smem_u32(s.b[st]);
-#pragma unroll
-                        for (int k = 0; k < kTK / 16; ++k)
-                            umma2_bf16(tmem + ab * kTN, operand_desc<kAMn>(a0, k), operand_desc<kBMn>(b0, k), idesc, kb > kb0 || k > 0);
-                        umma2_commit(&s.empty[st]);
-                        if (++st == kStages) { st = 0; phase ^= 1u; }
+    // With sums a thread of the epilogue needs more registers than there are for all: of 384 x 168 at launch, 128 x 72 + 256 x 208.
+    if (warp < kFirstEpi<kSum>) {
+        if constexpr (kSum) asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+        if (warp == 0) {
+            if (lane == 0) {                             // ---- TMA producer
+                uint32_t st = 0, round = 0;
+                for (int it = pair; it < items && !*failed; it += pairs) {
+                    const Item q = item_of(it);
+                    for (int kb = q.kb0; kb < q.kb1; ++kb) {
+                        if (round > 0 && !mbar_wait(&s.empty[st], (round - 1) & 1)) { *failed = 1; break; }
+                        if (rank == 0) mbar_expect_tx(&s.full[st], 4 * kHalf);
+                        load_operand<kAMn>(s.a[st], &tm_a, q.m0 + rank * 128, kb * kTK, &s.full[st]);
+                        load_operand<kBMn>(s.b[st], &tm_b, q.n0 + rank * 128, kb * kTK, &s.full[st]);
+                        if (++st == kStages) { st = 0; ++round; }
                     }
-                    if (ok) umma2_commit(&s.acc_full[ab]);
                 }
+                if (*failed && rank == 0)                // copies in flight land before the CTAs' shared memory is released
+                    for (uint32_t i = 0; i < kStages; ++i) mbar_wait(&s.full[i], (round + (i < st ? 0u : 1u)) & 1u, 4096u);
             }
-            if (!ok) *failed = 1;
+        } else if (warp == 1) {
+            if (lane == 0 && rank == 0) {                // ---- MMA issuer
+                constexpr uint32_t idesc = umma_idesc_bf16(kTM, kTN) | (kAMn ? 1u << 15 : 0u) | (kBMn ? 1u << 16 : 0u);
+                uint32_t st = 0, phase = 0;
+                int i = 0;                               // segments so far: every other one in the same accumulator
+                bool ok = true;
+                for (int it = pair; it < items && ok; it += pairs) {
+                    const Item q = item_of(it);
+                    for (int kb0 = q.kb0; kb0 < q.kb1 && ok; kb0 += kSegmentRuns<T>, ++i) {
+                        const int ab = i & 1, kb1 = min(q.kb1, kb0 + kSegmentRuns<T>);
+                        if (i >= 2 && !mbar_wait(&s.acc_empty[ab], ((i / 2) - 1) & 1)) { ok = false; break; }
+                        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                        for (int kb = kb0; kb < kb1; ++kb) {
+                            if (!mbar_wait(&s.full[st], phase)) { ok = false; break; }
+                            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                            const uint32_t a0 = smem_u32(s.a[st]), b0 = smem_u32(s.b[st]);
+    #pragma unroll
+                            for (int k = 0; k < kTK / 16; ++k)
+                                umma2_bf16(tmem + ab * kTN, operand_desc<kAMn>(a0, k), operand_desc<kBMn>(b0, k), idesc, kb > kb0 || k > 0);
+                            umma2_commit(&s.empty[st]);
+                            if (++st == kStages) { st = 0; phase ^= 1u; }
+                        }
+                        if (ok) umma2_commit(&s.acc_full[ab]);
+                    }
+                }
+                if (!ok) *failed = 1;
+            }
+            __syncwarp();
         }
-        __syncwarp();
-    } else {                                         // ---- epilogue: four warps for the rows, kWarpCols columns each
-        const int qd = warp % 4, part_col = (warp - 2) / 4 * kWarpCols<T>;
-        float* stage = s.out[warp - 2];
+    } else {                                         // ---- epilogue: four warps for the rows, kCols columns each
+        if constexpr (kSum) asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+        const int qd = warp % 4, part_col = (warp - kFirstEpi<kSum>) / 4 * kCols;
+        float* stage = s.out[warp - kFirstEpi<kSum>];
         const int row = rank * 128 + qd * 32;        // of the tile
         const uint32_t lanes = tmem + ((uint32_t)(qd * 32) << 16) + (uint32_t)part_col;
         int i = 0;
@@ -435,13 +445,12 @@ __global__ void __launch_bounds__(kThreads<T>, 1) k_linear(const __grid_constant
         for (int it = pair; it < items && ok; it += pairs) {
             const Item q = item_of(it);
             float* part = q.part >= 0 ? a.part + ((size_t)q.part * kTM + row) * kTN + part_col : nullptr;
-            const int rows = min(32, a.M - (q.m0 + row)), col0 = q.n0 + part_col, cols = min(kWarpCols<T>, a.N - col0);
-            constexpr int kC = kSum<T> ? 8 : 16;     // columns at a time, as the registers allow
-            using Work = Finish<kEpi, kAct, T, kC>;
+            const int rows = min(32, a.M - (q.m0 + row)), col0 = q.n0 + part_col, cols = min(kCols, a.N - col0);
+            using Work = Finish<kEpi, kAct, T, 16>;  // 16 columns at a time
             const bool mine = lane < rows;           // a thread has a row of the tile
             auto whole = [&](int c) { return a.wide && !part && c * 16 + 16 <= cols; };
-            auto load = [&](Work& f, int c, int half) {
-                if (whole(c) && mine) f.load(a, q.m0 + row + lane, col0 + c * 16 + half * 8);
+            auto load = [&](Work& f, int c) {
+                if (whole(c) && mine) f.load(a, q.m0 + row + lane, col0 + c * 16);
             };
             // the 16 columns of chunk c
             auto emit = [&](Work& f, int c, float2 (&v)[8]) {
@@ -452,16 +461,7 @@ __global__ void __launch_bounds__(kThreads<T>, 1) k_linear(const __grid_constant
                         for (int j = 0; j < 4; ++j)
                             *reinterpret_cast<float4*>(part + (size_t)lane * kTN + c * 16 + 4 * j) = make_float4(v[2 * j].x, v[2 * j].y, v[2 * j + 1].x, v[2 * j + 1].y);
                 } else if (whole(c)) {
-                    if constexpr (kC == 16) {
-                        if (mine) f(a, q.m0 + row + lane, col0 + c * 16, v);
-                    } else {
-#pragma unroll
-                        for (int half = 0; half < 2; ++half) {
-                            float2 u[4] = {v[half * 4], v[half * 4 + 1], v[half * 4 + 2], v[half * 4 + 3]};
-                            load(f, c, half);
-                            if (mine) f(a, q.m0 + row + lane, col0 + c * 16 + half * 8, u);
-                        }
-                    }
+                    if (mine) f(a, q.m0 + row + lane, col0 + c * 16, v);
                 } else {                             // a column a thread, two rows at a time, through the staging tile
 #pragma unroll
                     for (int j = 0; j < 4; ++j)
@@ -470,7 +470,7 @@ __global__ void __launch_bounds__(kThreads<T>, 1) k_linear(const __grid_constant
                     const int col = col0 + c * 16 + lane % 16;
                     if (c * 16 + lane % 16 < cols) {
                         const float bias = kEpi == kForward && a.bias ? __ldg(a.bias + col) : 0.f;
-                        constexpr int kRows = kSum<T> || (kEpi == kDgrad && kAct != ABS_ACT_NONE) ? 8 : 16;
+                        constexpr int kRows = kSum || (kEpi == kDgrad && kAct != ABS_ACT_NONE) ? 8 : 16;
 #pragma unroll 1
                         for (int k0 = lane / 16; k0 < rows; k0 += 2 * kRows) {
                             FinishOne<kEpi, kAct, T> one[kRows];     // the reads of as many rows are in flight together
@@ -485,49 +485,55 @@ __global__ void __launch_bounds__(kThreads<T>, 1) k_linear(const __grid_constant
                     __syncwarp();
                 }
             };
-            if constexpr (kSum<T>) {
-                float2 sum[kWarpCols<T> / 16][8];
+            if constexpr (kSum) {
+                float2 sum[kCols / 16][8];
 #pragma unroll
-                for (int c = 0; c < kWarpCols<T> / 16; ++c)
+                for (int c = 0; c < kCols / 16; ++c)
 #pragma unroll
                     for (int j = 0; j < 8; ++j) sum[c][j] = both(0.f);
-                for (int kb0 = q.kb0; kb0 < q.kb1; kb0 += kSegmentRuns, ++i) {
+                for (int kb0 = q.kb0; kb0 < q.kb1; kb0 += kSegmentRuns<T>, ++i) {
                     const int ab = i & 1;
                     ok = __all_sync(0xffffffffu, mbar_wait(&s.acc_full[ab], (i / 2) & 1) && !*failed);
                     if (!ok) break;
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll
-                    for (int c = 0; c < kWarpCols<T> / 16; ++c) {
-                        uint32_t v[16];
-                        tmem_ld_16(lanes + (uint32_t)(ab * kTN + c * 16), v);
+                    for (int c = 0; c < kCols / 16; c += 2) {
+                        uint32_t v[32];
+                        tmem_ld_32(lanes + (uint32_t)(ab * kTN + c * 16), v);
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) sum[c][j] = add2(sum[c][j], make_float2(__uint_as_float(v[2 * j]), __uint_as_float(v[2 * j + 1])));
+                        for (int j = 0; j < 16; ++j)
+                            sum[c + j / 8][j % 8] = add2(sum[c + j / 8][j % 8], make_float2(__uint_as_float(v[2 * j]), __uint_as_float(v[2 * j + 1])));
                     }
                     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                     __syncwarp();
                     if (lane == 0) arrive_first(&s.acc_empty[ab]);
                 }
                 if (!ok) break;
-                Work f;
+                Work f, next;
+                load(f, 0);
 #pragma unroll
-                for (int c = 0; c < kWarpCols<T> / 16; ++c) emit(f, c, sum[c]);
+                for (int c = 0; c < kCols / 16; ++c) {
+                    if (c + 1 < kCols / 16) load(next, c + 1);
+                    emit(f, c, sum[c]);
+                    f = next;
+                }
             } else {
                 const int ab = i & 1;
                 Work f, next;
-                load(f, 0, 0);                       // while the product runs
+                load(f, 0);                       // while the product runs
                 ok = __all_sync(0xffffffffu, mbar_wait(&s.acc_full[ab], (i / 2) & 1) && !*failed);
                 if (!ok) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll
-                for (int c = 0; c < kWarpCols<T> / 16; ++c) {
+                for (int c = 0; c < kCols / 16; ++c) {
                     uint32_t u[16];
                     tmem_ld_16(lanes + (uint32_t)(ab * kTN + c * 16), u);
-                    if (c == kWarpCols<T> / 16 - 1) {
+                    if (c == kCols / 16 - 1) {
                         asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                         __syncwarp();
                         if (lane == 0) arrive_first(&s.acc_empty[ab]);
                     } else {
-                        load(next, c + 1, 0);
+                        load(next, c + 1);
                     }
                     float2 v[8];
 #pragma unroll
@@ -766,17 +772,29 @@ int bias_parts(uint64_t T, uint64_t N) {
     return (int)std::max<uint64_t>(1, std::min((T + 63) / 64, want));
 }
 
+// No tile, or part of one, has more runs than the tensor core adds up on its own.
+bool one_segment(const LinArgs& a) {
+    const int all = (a.K + kTK - 1) / kTK;
+    return (a.join && a.whole == 0 ? a.kb_per_split : all) <= kSegmentRuns<bf16>;
+}
+
 cudaError_t copy_rows(const Operand& o, uint64_t to_ld, bf16* to, cudaStream_t s) {
     return launch_kernel(k_copy_rows, (int)std::min<size_t>(o.rows, kSms * 16), 128, 0, s, true, static_cast<const bf16*>(o.p), (size_t)o.ld, (int)o.cols, (size_t)to_ld,
                          (size_t)o.rows, to);
 }
 
-template <int kEpi, uint32_t kAct, typename T>
-cudaError_t run_act(const CUtensorMap& ta, const CUtensorMap& tb, const LinArgs& a, cudaStream_t s) {
-    cudaError_t e = allow_smem<k_linear<kEpi, kAct, T>>();
+template <int kEpi, uint32_t kAct, typename T, bool kSum>
+cudaError_t run_tiles(const CUtensorMap& ta, const CUtensorMap& tb, const LinArgs& a, cudaStream_t s) {
+    const cudaError_t e = allow_smem<k_linear<kEpi, kAct, T, kSum>>();
     if (e != cudaSuccess) return e;
     const int grid = 2 * std::min(a.whole + a.rest * a.splits, kSms / 2);
-    e = launch_cluster(k_linear<kEpi, kAct, T>, grid, 2, kThreads<T>, sizeof(LinSmem) + 1024, s, ta, tb, a);
+    return launch_cluster(k_linear<kEpi, kAct, T, kSum>, grid, 2, kThreads<kSum>, sizeof(LinSmem) + 1024, s, ta, tb, a);
+}
+template <int kEpi, uint32_t kAct, typename T>
+cudaError_t run_act(const CUtensorMap& ta, const CUtensorMap& tb, const LinArgs& a, cudaStream_t s) {
+    cudaError_t e;
+    if constexpr (sizeof(T) == 2) e = one_segment(a) ? run_tiles<kEpi, kAct, T, false>(ta, tb, a, s) : run_tiles<kEpi, kAct, T, true>(ta, tb, a, s);
+    else e = run_tiles<kEpi, kAct, T, true>(ta, tb, a, s);
     if (e == cudaSuccess && a.join) e = launch_kernel(k_linear_join<kEpi, kAct, T>, std::min(a.rest * kTM / 8, kSms * 8), 256, 0, s, false, a);
     return e;
 }
