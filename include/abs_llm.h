@@ -174,6 +174,7 @@ int abs_layer_norm_backward(const void *dn, uint64_t ld_dn, const void *x, uint6
 #define ABS_ACT_RELU 1u  /* max(z, 0); slope 0 at 0                          */
 #define ABS_ACT_GELU 2u  /* z Phi(z), Phi the normal distribution function   */
 #define ABS_ACT_SILU 3u  /* z / (1 + exp(-z))                                */
+/* At minus infinity GELU and SiLU, and their slopes, are their limit 0; a NaN stays one. */
 
 /* A linear layer on the tcgen05 tensor cores, operands bf16, sums fp32:
  *     z = x w + bias      y = act(z) + residual

@@ -62,15 +62,24 @@ __device__ __forceinline__ void normal_tail(float2 z, float2& E, float2& q, floa
     q = mul2(p, E);
     m = make_float2(fminf(w.x, 14.f), fminf(w.y, 14.f));
 }
-// sigmoid(z) and 1 - sigmoid(z), each to its own precision.
-__device__ __forceinline__ void sigmoids(float2 z, float2& s, float2& rest) {
-    float2 v = mul2(z, both(-1.4426950408889634f));
-    v.x = v.x > 126.f ? 126.f : v.x;             // keeps a NaN
-    v.y = v.y > 126.f ? 126.f : v.y;
-    const float2 e = exp2_of(v), d = add2(e, both(1.f));
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(s.x) : "f"(d.x));
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(s.y) : "f"(d.y));
-    rest = mul2(e, s);
+// |v|, at most `most`; a NaN stays one.
+__device__ __forceinline__ float2 limited(float2 v, float most) {
+    float2 w;
+    asm("min.NaN.f32 %0, %1, %2;" : "=f"(w.x) : "f"(fabsf(v.x)), "f"(most));
+    asm("min.NaN.f32 %0, %1, %2;" : "=f"(w.y) : "f"(fabsf(v.y)), "f"(most));
+    return w;
+}
+// sigmoid(z) and 1 - sigmoid(z), each to its own precision, from e^-|z|: the smaller one falls to zero far out (where the exponential does: |z| > 87).
+// w: |z| up to 126, to be multiplied by what may be zero.
+__device__ __forceinline__ void sigmoids(float2 z, float2& s, float2& rest, float2& w) {
+    w = limited(z, 126.f);
+    const float2 e = exp2_of(mul2(w, both(-1.4426950408889634f))), d = add2(e, both(1.f));
+    float2 r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r.x) : "f"(d.x));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r.y) : "f"(d.y));
+    const float2 small = mul2(e, r);
+    s = make_float2(z.x > 0.f ? r.x : small.x, z.y > 0.f ? r.y : small.y);
+    rest = make_float2(z.x > 0.f ? small.x : r.x, z.y > 0.f ? small.y : r.y);
 }
 template <uint32_t kAct>
 __device__ __forceinline__ float2 activate(float2 z) {
@@ -81,9 +90,9 @@ __device__ __forceinline__ float2 activate(float2 z) {
         return fma2(make_float2(-m.x, -m.y), q, make_float2(fmaxf(z.x, 0.f), fmaxf(z.y, 0.f)));
     }
     if (kAct == ABS_ACT_SILU) {
-        float2 s, rest;
-        sigmoids(z, s, rest);
-        return mul2(z, s);
+        float2 s, rest, w;
+        sigmoids(z, s, rest, w);
+        return mul2(make_float2(z.x > 0.f ? z.x : -w.x, z.y > 0.f ? z.y : -w.y), s);
     }
     return z;
 }
@@ -96,10 +105,10 @@ __device__ __forceinline__ float2 slope(float2 z) {
         const float2 phi = make_float2(z.x > 0.f ? 1.f - q.x : q.x, z.y > 0.f ? 1.f - q.y : q.y);
         return fma2(make_float2(copysignf(m.x, z.x), copysignf(m.y, z.y)), mul2(E, both(0.3989422804014327f * 0x1p-24f)), phi);
     }
-    if (kAct == ABS_ACT_SILU) {                  // s (1 + z (1 - s)); beyond 126 one of the factors is 0
-        float2 s, rest;
-        sigmoids(z, s, rest);
-        return mul2(s, fma2(make_float2(fminf(fmaxf(z.x, -126.f), 126.f), fminf(fmaxf(z.y, -126.f), 126.f)), rest, both(1.f)));
+    if (kAct == ABS_ACT_SILU) {                  // s (1 + z (1 - s))
+        float2 s, rest, w;
+        sigmoids(z, s, rest, w);
+        return mul2(s, fma2(make_float2(copysignf(w.x, z.x), copysignf(w.y, z.y)), rest, both(1.f)));
     }
     return both(1.f);
 }
