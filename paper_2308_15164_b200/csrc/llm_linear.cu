@@ -41,27 +41,6 @@ struct LinArgs {
 };
 
 // ---- activations, two numbers at a time
-// Phi(-|z|) = exp(-z^2 / 2) P(1 / (1 + 0.35 |z|)) with P of degree 7 fitted to the smallest relative error over 0 <= |z| <= 13.5 (beyond, the
-// exponential underflows), so that the lower tail keeps its precision: 3e-7, in fp32 6e-7.  E: 2^24 times the exponential (which then stays above the unit's flush to zero), q: Phi(-|z|), m: |z| up to 14 (q is next to
-// nothing from there on, also times an infinity).
-__device__ __forceinline__ void normal_tail(float2 z, float2& E, float2& q, float2& m) {
-    const float2 w = make_float2(fabsf(z.x), fabsf(z.y)), d = fma2(w, both(0.35f), both(1.f));
-    float2 t;
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(t.x) : "f"(d.x));
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(t.y) : "f"(d.y));
-    E = exp2_of(fma2(mul2(z, z), both(-0.72134752044448170f), both(24.f)));
-    constexpr float k = 0x1p-24f;
-    float2 p;
-    p = fma2(t, both(0.04894255149557414f * k), both(-0.20211968521483073f * k));
-    p = fma2(p, t, both(0.24064142309471856f * k));
-    p = fma2(p, t, both(-0.017023902126677096f * k));
-    p = fma2(p, t, both(0.15596167730976151f * k));
-    p = fma2(p, t, both(0.1333550587912772f * k));
-    p = fma2(p, t, both(0.14027034589594403f * k));
-    p = fma2(p, t, both(-2.731542404448325e-05f * k));
-    q = mul2(p, E);
-    m = make_float2(fminf(w.x, 14.f), fminf(w.y, 14.f));
-}
 // |v|, at most `most`; a NaN stays one.
 __device__ __forceinline__ float2 limited(float2 v, float most) {
     float2 w;
@@ -69,12 +48,47 @@ __device__ __forceinline__ float2 limited(float2 v, float most) {
     asm("min.NaN.f32 %0, %1, %2;" : "=f"(w.y) : "f"(fabsf(v.y)), "f"(most));
     return w;
 }
+// Phi(-|z|) = exp(-z^2 / 2) P(1 / (1 + 0.35 |z|)) with P of degree 7 fitted to the smallest relative error over 0 <= |z| <= 13.5, so that the lower tail
+// keeps its precision: 3e-7, in fp32 6e-7.  The exponential as the square of exp(-z^2 / 4), which stays within the unit's range as far as there is
+// something to see, with what the roundings of z^2 and of the exponent leave out (without: 2e-6 at |z| = 8, 8e-6 at 12).  All together 1.4e-6 at most.
+// E: the exponential, q: Phi(-|z|), w: |z| up to 16, where both are zero.
+__device__ __forceinline__ void normal_tail(float2 z, float2& E, float2& q, float2& w) {
+    constexpr double k = 0.36067376022224085;                // log2(e) / 4
+    constexpr float kHi = (float)k, kLo = (float)(k - (double)kHi);
+    w = limited(z, 16.f);
+    const float2 d = fma2(w, both(0.35f), both(1.f));
+    float2 t;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(t.x) : "f"(d.x));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(t.y) : "f"(d.y));
+    const float2 h = mul2(w, w), minus = make_float2(-h.x, -h.y), v = mul2(minus, both(kHi));
+    float2 rest = fma2(minus, both(kHi), make_float2(-v.x, -v.y));          // of the exponent
+    rest = fma2(fma2(w, w, minus), both(-kHi), rest);
+    rest = fma2(minus, both(kLo), rest);
+    const float2 e = exp2_of(v);
+    E = mul2(e, e);
+    E = fma2(mul2(rest, both(1.3862943611198906f)), E, E);
+    float2 p;
+    p = fma2(t, both(0.04894255149557414f), both(-0.20211968521483073f));
+    p = fma2(p, t, both(0.24064142309471856f));
+    p = fma2(p, t, both(-0.017023902126677096f));
+    p = fma2(p, t, both(0.15596167730976151f));
+    p = fma2(p, t, both(0.1333550587912772f));
+    p = fma2(p, t, both(0.14027034589594403f));
+    p = fma2(p, t, both(-2.731542404448325e-05f));
+    q = mul2(p, E);
+}
 // sigmoid(z) and 1 - sigmoid(z), each to its own precision, from e^-|z|: the smaller one falls to zero far out (where the exponential does: |z| > 87).
 // w: |z| up to 126, to be multiplied by what may be zero.
 __device__ __forceinline__ void sigmoids(float2 z, float2& s, float2& rest, float2& w) {
     w = limited(z, 126.f);
-    const float2 e = exp2_of(mul2(w, both(-1.4426950408889634f))), d = add2(e, both(1.f));
-    float2 r;
+    constexpr double k = 1.4426950408889634;                 // log2(e)
+    constexpr float kHi = (float)k, kLo = (float)(k - (double)kHi);
+    const float2 minus = make_float2(-w.x, -w.y), v = mul2(minus, both(kHi));
+    // what the rounding of the exponent leaves out (without: 8e-7 at |z| = 12)
+    const float2 left = fma2(minus, both(kLo), fma2(minus, both(kHi), make_float2(-v.x, -v.y)));
+    float2 e = exp2_of(v), r;
+    e = fma2(mul2(left, both(0.6931471805599453f)), e, e);
+    const float2 d = add2(e, both(1.f));
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r.x) : "f"(d.x));
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r.y) : "f"(d.y));
     const float2 small = mul2(e, r);
@@ -85,9 +99,9 @@ template <uint32_t kAct>
 __device__ __forceinline__ float2 activate(float2 z) {
     if (kAct == ABS_ACT_RELU) return make_float2(z.x > 0.f ? z.x : z.x == z.x ? 0.f : z.x, z.y > 0.f ? z.y : z.y == z.y ? 0.f : z.y);
     if (kAct == ABS_ACT_GELU) {                  // max(z, 0) - |z| Phi(-|z|)
-        float2 E, q, m;
-        normal_tail(z, E, q, m);
-        return fma2(make_float2(-m.x, -m.y), q, make_float2(fmaxf(z.x, 0.f), fmaxf(z.y, 0.f)));
+        float2 E, q, w;
+        normal_tail(z, E, q, w);
+        return fma2(make_float2(-w.x, -w.y), q, make_float2(fmaxf(z.x, 0.f), fmaxf(z.y, 0.f)));
     }
     if (kAct == ABS_ACT_SILU) {
         float2 s, rest, w;
@@ -100,10 +114,10 @@ template <uint32_t kAct>
 __device__ __forceinline__ float2 slope(float2 z) {
     if (kAct == ABS_ACT_RELU) return make_float2(z.x > 0.f ? 1.f : z.x == z.x ? 0.f : z.x, z.y > 0.f ? 1.f : z.y == z.y ? 0.f : z.y);
     if (kAct == ABS_ACT_GELU) {                  // Phi(z) + z phi(z)
-        float2 E, q, m;
-        normal_tail(z, E, q, m);
+        float2 E, q, w;
+        normal_tail(z, E, q, w);
         const float2 phi = make_float2(z.x > 0.f ? 1.f - q.x : q.x, z.y > 0.f ? 1.f - q.y : q.y);
-        return fma2(make_float2(copysignf(m.x, z.x), copysignf(m.y, z.y)), mul2(E, both(0.3989422804014327f * 0x1p-24f)), phi);
+        return fma2(make_float2(copysignf(w.x, z.x), copysignf(w.y, z.y)), mul2(E, both(0.3989422804014327f)), phi);
     }
     if (kAct == ABS_ACT_SILU) {                  // s (1 + z (1 - s))
         float2 s, rest, w;

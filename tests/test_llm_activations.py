@@ -60,3 +60,26 @@ def test_infinities_and_what_is_no_number(llm, act):
     for s in slopes(llm, z, act):
         up, down, none = s[:, 0].tolist()
         assert up == 1 and down == 0 and none != none
+
+
+# Roundings of fp32, 2^-24 of the value, one after the other.  The fast exponential is right to four of them, the reciprocal to two.
+# GELU: the exponential's square 8 + 1, what its argument leaves out 1; the polynomial and its argument 10.4 (evaluated in fp32 beside 64 bits), the reciprocal
+# in it 1.3 more; two products 2.
+GELU = 24 * R.U32
+# SiLU: the exponential 4 + 1, 1 + it 1, the reciprocal 2, two products 2.
+SILU = 10 * R.U32
+
+
+@pytest.mark.parametrize("act", ["gelu", "silu"])
+def test_precision_of_32_bit_results(llm, act):
+    """Relative to the value, in the lower tail too; a slope relative to its terms, which have opposite signs below zero."""
+    z = every_number()
+    z = z[(z.abs() <= 13) & (z.abs() > 2.0 ** -40)][:, None]
+    d = R.d(z)
+    y, want = R.d(value(llm, z, act)), R.act(act, d)
+    bad = (y - want).abs() / want.abs()
+    assert float(bad.max()) <= (GELU if act == "gelu" else SILU), float(d[bad.argmax()])
+    s, want = R.d(slopes(llm, z, act)[0]), R.slope(act, d)
+    size = R.phi(d) + d.abs() * torch.exp(-0.5 * d * d) * 0.4 if act == "gelu" else torch.sigmoid(d) * (1 + d.abs() * torch.sigmoid(-d))
+    bad = (s - want).abs() / size
+    assert float(bad.max()) <= (GELU + 2 * R.U32 if act == "gelu" else 2 * SILU), float(d[bad.argmax()])
