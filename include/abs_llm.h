@@ -218,7 +218,8 @@ int abs_activation_backward(const void *dy, uint64_t ld_dy, uint32_t dtype, cons
 /* Gated linear recurrence, every channel on its own, a_t = sigmoid(g_t), over packed sequences:
  *   sequence q holds the rows offsets[q] .. offsets[q + 1] - 1; before its first row h is h0[q] (h0 NULL: 0)
  *   x, g [tokens, width] of `dtype`;  y [tokens, width] of `dtype` out: h_t (may be x or g, with the same leading dimension); rows of no
- *   sequence are zero.  The state itself stays fp32.
+ *   sequence are zero.  The state itself stays fp32.  No gate is zero: an infinite state stays infinite; no number of one sequence reaches
+ *   another.
  *   offsets [seqs + 1] int32 on the device, ascending, values outside [0, tokens] are clamped; empty sequences are allowed.
  *   NULL: one sequence of all rows (seqs = 1).
  *   h0, last [seqs, width] fp32, packed; last out (NULL: not wanted): h behind the last row (of an empty sequence h0); not h0 itself.

@@ -82,10 +82,20 @@ struct alignas(16) Map {
 };
 __device__ __forceinline__ Map identity() { return {make_float2(1.f, 1.f), make_float2(0.f, 0.f)}; }
 __device__ __forceinline__ bool forgets(float A) { return __float_as_uint(A) == 0x80000000u; }
+__device__ __forceinline__ bool no_number(float2 v) { return v.x != v.x || v.y != v.y; }
+// A s + B.  No gate is zero, so that an infinite state stays infinite; behind so many rows that their A has fallen to zero, the product with it
+// is a NaN.  kInfinite: with that in mind.  The runs of maps below are gone through without, and once more where they end in a NaN.
+template <bool kInfinite>
+__device__ __forceinline__ float2 along(float2 A, float2 s, float2 B) {
+    float2 r = fma2(A, s, B);
+    if (kInfinite && A.x == 0.f && isinf(s.x)) r.x = s.x + B.x;
+    if (kInfinite && A.y == 0.f && isinf(s.y)) r.y = s.y + B.y;
+    return r;
+}
 // m followed by `then`; kForgets: either may forget what is in front of it.
-template <bool kForgets>
+template <bool kForgets, bool kInfinite = false>
 __device__ __forceinline__ Map compose(Map m, Map then) {
-    Map r{mul2(m.A, then.A), fma2(then.A, m.B, then.B)};
+    Map r{mul2(m.A, then.A), along<kInfinite>(then.A, m.B, then.B)};
     if (kForgets && forgets(then.A.x)) {
         r.A.x = then.A.x;
         r.B.x = then.B.x;
@@ -96,9 +106,9 @@ __device__ __forceinline__ Map compose(Map m, Map then) {
     }
     return r;
 }
-template <bool kForgets>
+template <bool kForgets, bool kInfinite = false>
 __device__ __forceinline__ float2 apply(Map m, float2 s) {
-    float2 r = fma2(m.A, s, m.B);
+    float2 r = along<kInfinite>(m.A, s, m.B);
     if (kForgets && forgets(m.A.x)) r.x = m.B.x;
     if (kForgets && forgets(m.A.y)) r.y = m.B.y;
     return r;
@@ -229,10 +239,18 @@ __global__ void __launch_bounds__(kWarps * 32, kCtasOf<kBack, kMaps>) k_recurren
             for (int i = 0; i < 8; ++i)
                 if (k + i < k1) run = compose<true>(run, v[i]);
         }
+        if (no_number(run.B)) {
+            run = identity();
+            for (int k = k0; k < k1; ++k) run = compose<true, true>(run, p[(size_t)k * a.strips * 32]);
+        }
         s.front[warp][lane] = run;
         __syncthreads();
 #pragma unroll
         for (int w = 0; w < kWarps; ++w) start = apply<true>(s.front[w][lane], start);
+        if (no_number(start)) {
+            start = both(0.f);
+            for (int w = 0; w < kWarps; ++w) start = apply<true, true>(s.front[w][lane], start);
+        }
     }
 
     const bool plain_strip = (strip + 1) * kCols <= a.D && a.pairs;
@@ -341,11 +359,18 @@ __global__ void __launch_bounds__(kWarps * 32, kCtasOf<kBack, kMaps>) k_recurren
 #pragma unroll
                     for (int w = 1; w < kWarps; ++w) whole = compose<false>(whole, of[32 * w]);
                 }
-                behind = compose<false>(whole, behind);          // nothing begins in the tiles behind
+                const Map last = behind;
+                behind = compose<false>(whole, last);            // nothing begins in the tiles behind
+                if (no_number(behind.B)) {
+                    whole = of[0];
+                    for (int w = 1; w < kWarps; ++w) whole = compose<true, true>(whole, of[32 * w]);
+                    behind = compose<false, true>(whole, last);
+                }
             }
             if (any_begins) break;
         } else {
-            float2 state = start;
+            const float2 front = start;
+            float2 state = front;
             if (any_begins) {
 #pragma unroll
                 for (int w = 0; w < kWarps; ++w) {
@@ -358,6 +383,10 @@ __global__ void __launch_bounds__(kWarps * 32, kCtasOf<kBack, kMaps>) k_recurren
                     if (w == warp) state = start;
                     start = apply<false>(of[32 * w], start);
                 }
+            }
+            if (no_number(state)) {
+                state = front;
+                for (int w = 0; w < warp; ++w) state = apply<true, true>(of[32 * w], state);
             }
             // ---- 3
             auto finish = [&](auto all) {
@@ -404,6 +433,10 @@ __global__ void __launch_bounds__(kWarps * 32, kCtasOf<kBack, kMaps>) k_recurren
             };
             if (plain) finish(std::true_type());
             else finish(std::false_type());
+            if (no_number(start)) {
+                start = front;
+                for (int w = 0; w < kWarps; ++w) start = apply<true, true>(of[32 * w], start);
+            }
         }
         if (++stage == kStages) {
             stage = 0;
