@@ -72,8 +72,11 @@ __device__ __forceinline__ void gate_of(float2 g, float2& a, float2& rest, bf16)
 __device__ __forceinline__ void gate_of(float2 g, float2& a, float2& rest, float) {
     const float2 e = make_float2(expf(g.x < -87.f ? 87.f : -g.x), expf(g.y < -87.f ? 87.f : -g.y));
     const float2 d = add2(e, both(1.f));         // at most 2^126
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(a.x) : "f"(d.x));
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(a.y) : "f"(d.y));
+    float2 r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r.x) : "f"(d.x));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r.y) : "f"(d.y));
+    // a step of Newton's method: half a unit in the last place, as a division has, instead of one (a state lives through many gates)
+    a = fma2(r, fma2(make_float2(-d.x, -d.y), r, both(1.f)), r);
     rest = mul2(e, a);
 }
 // The maps of two columns.
