@@ -28,17 +28,17 @@ namespace {
 constexpr int kWarps = 8, kCols = 64;    // of a tile; a lane owns two columns
 constexpr int kSms = 148;
 constexpr uint64_t kSizeMax = 0x7ffffc00ull;
-// Rows of a warp, 16 forward and 8 backward (bf16): 32 KB of inputs for a tile, backward 16 KB in the first pass.  us, 65536 x 1024 one sequence
-// forward / 16384 x 4096 of 24 sequences backward, bf16: as here 118 / 156; forward first pass with 8 rows a warp and four CTAs an SM 131; backward
-// first pass with 16 160; backward with three CTAs an SM and two tiles in flight 193; forward with 8 rows and four CTAs 138.
+// Rows of a warp, 16 forward and 8 backward (bf16): 32 KB of inputs for a tile, backward 16 KB in the first pass; three tiles in flight.  CTAs of an SM: as
+// many as its shared memory holds.  us, 65536 x 1024 one sequence forward / 16384 x 4096 of 24 sequences backward, bf16: as here 118 / 152; forward first
+// pass with two tiles in flight and three CTAs an SM 131 (the SMs that are free first take three, others are left with one); with 8 rows a warp and four CTAs
+// 131; backward first pass with 16 160; backward with three CTAs an SM and two tiles in flight 193; forward with 8 rows and four CTAs 138.
 template <typename T, bool kBack, bool kMaps>
 constexpr int kRowsOf = (kBack ? 8 : 16) * 2 / (int)sizeof(T);
 template <typename T, bool kBack, bool kMaps>
 constexpr int kTileOf = kWarps * kRowsOf<T, kBack, kMaps>;
+constexpr int kStages = 3;               // tiles in flight
 template <bool kBack, bool kMaps>
-constexpr int kStagesOf = kMaps && !kBack ? 2 : 3;
-template <bool kBack, bool kMaps>
-constexpr int kCtasOf = !kMaps ? 2 : kBack ? 4 : 3;      // of an SM
+constexpr int kCtasOf = kBack && kMaps ? 3 : 2;          // of an SM
 template <bool kBack, bool kMaps>
 constexpr int kStageBytes = kBack && kMaps ? 16384 : 32768;
 constexpr int kTileMin = kTileOf<float, true, false>;
@@ -163,13 +163,22 @@ __device__ __forceinline__ int sequence_from(const RecArgs& a, int q, int t) {
     return q;
 }
 
+template <bool kMaps>
 struct RecSmem {
     Map map[2][kWarps][32];                      // of a warp's rows, by the tile's parity
-    Map front[kWarps][32];                       // of the segments in front, a run of them for each warp
-    alignas(8) uint64_t full[3];
+    Map front[kMaps ? 1 : kWarps][kMaps ? 1 : 32];       // second pass: of the segments in front, a run of them for each warp
+    alignas(8) uint64_t full[kStages];
     int failed[2];
 };
-constexpr size_t kRecSmem = (sizeof(RecSmem) + 127) / 128 * 128;
+template <bool kMaps>
+constexpr size_t kRecSmem = (sizeof(RecSmem<kMaps>) + 127) / 128 * 128;
+// Dynamic shared memory of a CTA; where the lanes read memory no tiles.
+template <bool kBack, bool kMaps>
+constexpr size_t smem_bytes(bool tma) { return kRecSmem<kMaps> + (tma ? kStages * kStageBytes<kBack, kMaps> : 0) + 128; }
+// The CTAs that the plan counts on fit (of an SM's 228 KB, 1 KB a CTA is the system's).
+template <bool kBack, bool kMaps>
+constexpr bool kFits = kCtasOf<kBack, kMaps> * (smem_bytes<kBack, kMaps>(true) + 1024) <= 228 * 1024;
+static_assert(kFits<false, false> && kFits<false, true> && kFits<true, false> && kFits<true, true>, "");
 
 // A CTA takes a segment of a strip of 64 columns, tile by tile (kTileOf rows in scan order: backward from the last one).
 //   kMaps   the segment's map: from its last tile to its first, or to the first in which a sequence begins (nothing in front of that
@@ -183,14 +192,14 @@ template <typename T, uint32_t kKind, bool kBack, bool kTma, bool kMaps>
 __global__ void __launch_bounds__(kWarps * 32, kCtasOf<kBack, kMaps>) k_recurrence(const __grid_constant__ RecArgs a, const __grid_constant__ CUtensorMap tm_g,
                                                                             const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_dy,
                                                                             const __grid_constant__ CUtensorMap tm_y) {
-    constexpr int kRows = kRowsOf<T, kBack, kMaps>, kTile = kTileOf<T, kBack, kMaps>, kStages = kStagesOf<kBack, kMaps>;
+    constexpr int kRows = kRowsOf<T, kBack, kMaps>, kTile = kTileOf<T, kBack, kMaps>;
     constexpr int kInput = kTile * kCols * (int)sizeof(T);       // bytes of an input's tile
     constexpr int kInputs = kBack && !kMaps ? 4 : 2;
     static_assert(kInput * kInputs == kStageBytes<kBack, kMaps>, "");
     enum { kG, kIn, kX, kY };                                    // kIn: x, backward dy; kX backward only
     extern __shared__ uint8_t raw[];
-    RecSmem& s = *reinterpret_cast<RecSmem*>((reinterpret_cast<uintptr_t>(raw) + 127) & ~(uintptr_t)127);
-    uint8_t* const ring = reinterpret_cast<uint8_t*>(&s) + kRecSmem;
+    RecSmem<kMaps>& s = *reinterpret_cast<RecSmem<kMaps>*>((reinterpret_cast<uintptr_t>(raw) + 127) & ~(uintptr_t)127);
+    uint8_t* const ring = reinterpret_cast<uint8_t*>(&s) + kRecSmem<kMaps>;
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const int strip = blockIdx.x % a.strips, index = blockIdx.x / a.strips, seg = kMaps ? index / a.parts : index;
     // its rows in scan order, the first pass's from the segment's last part on
@@ -487,8 +496,8 @@ bool encode_tiles(CUtensorMap* tm, const void* p, size_t ld, size_t es, const Re
 }
 
 // Segments of a strip: as many as fill the GPU once, or twice where that leaves fewer SMs idle.  One where that fills more than 60 % of
-// it, since two and more are read twice (but for what lies in front of a sequence's begin).  In the first pass, whose CTAs are smaller,
-// a segment is cut again.
+// it, since two and more are read twice (but for what lies in front of a sequence's begin).  In the first pass, which fills the GPU with the segments
+// but one, a segment is cut again where that leaves room.
 template <typename T, bool kBack>
 void cut_segments(RecArgs& a) {
     constexpr int kTile = kTileOf<T, kBack, false>, kMapTile = kTileOf<T, kBack, true>, kResident = kSms * kCtasOf<kBack, false>;
@@ -520,7 +529,7 @@ cudaError_t run_pass(const RecArgs& a, cudaStream_t s) {
     const cudaError_t e = allow_smem<k_recurrence<T, kKind, kBack, kTma, kMaps>>();
     if (e != cudaSuccess) return e;
     return launch_kernel(k_recurrence<T, kKind, kBack, kTma, kMaps>, (kMaps ? (a.segs - 1) * a.parts : a.segs) * a.strips, kWarps * 32,
-                         kRecSmem + (kTma ? kStagesOf<kBack, kMaps> * kStageBytes<kBack, kMaps> : 0) + 128, s, true, a, g, x, dy, y);
+                         smem_bytes<kBack, kMaps>(kTma), s, true, a, g, x, dy, y);
 }
 template <typename T, uint32_t kKind, bool kBack, bool kTma>
 cudaError_t run_passes(const RecArgs& a, cudaStream_t s) {
