@@ -247,7 +247,8 @@ int abs_recurrence_step(const void *x, uint64_t ld_x, const void *g, uint64_t ld
                         uint64_t seqs, uint64_t width, void *y, uint64_t ld_y, float *out, void *stream);
 
 /* Blocks until `stream` has finished and reports the device-side status of the calls of this header on the current
- * device: ABS_OK, ABS_ECUDA, or once ABS_ETIMEOUT (a bounded wait inside a kernel ran out; its tile was not written). */
+ * device: ABS_OK, ABS_ECUDA, or once ABS_ETIMEOUT (a bounded wait inside a kernel ran out: its tile was not written, nor
+ * what the norms, the linear layer and the recurrence would form from it; sums that are added to hold what they held). */
 int abs_llm_check(void *stream);
 
 #ifdef __cplusplus

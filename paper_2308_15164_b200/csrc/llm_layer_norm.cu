@@ -447,6 +447,7 @@ __global__ void __launch_bounds__(kWarp ? kRowWarps * 32 : ring_threads(true, kP
         asm volatile("cp.async.wait_all;" ::: "memory");
         __syncwarp();
     }
+    if (r.without(part, 2 * (int)part_width(a.D))) return;
 #pragma unroll
     for (int j = 0; j < kP; ++j)
         if (r.has(j))
@@ -473,7 +474,6 @@ __global__ void __launch_bounds__(kWarp ? kRowWarps * 32 : ring_threads(true, kP
             part[c] = v;
         }
     }
-    if (!r.ok) report_timeout();
 }
 
 // How a call is launched.  ring: all matrices aligned alike and the row within the pieces that a CTA's threads own.

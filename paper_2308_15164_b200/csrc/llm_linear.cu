@@ -244,7 +244,7 @@ struct FinishOne {
 //   the others  epilogue, four warps for the rows, a row a thread, 16 columns at a time with the reads of the next ones under way (through a
 //               staging tile in shared memory the results took a tenth of its bandwidth from the product: 266 -> 254 us)
 //                 kSum    eight warps of 128 columns add up an item's segments (kSegmentRuns) in registers
-//                 else    bf16 results of items of one segment straight from TMEM, sixteen warps of 64 columns (8192 x 256 x 8192: 57 us,
+//                 else    bf16 results of whole tiles of one segment straight from TMEM, sixteen warps of 64 columns (8192 x 256 x 8192: 57 us,
 //                         through registers with eight warps 97)
 // Items are dealt out round-robin to the pairs: the whole tiles, as many as fill all pairs equally often, then the rest, each cut along K
 // into `splits` parts so that they too keep all pairs busy; k_linear_join adds those up in order and does the elementwise work.
@@ -351,6 +351,15 @@ __device__ __forceinline__ uint64_t operand_desc(uint32_t at, int k16) {
     return kMn ? umma_desc_mn_sw128(at + k16 * 2048, kHalf / 2) : umma_desc_k_sw128(at + k16 * 32);
 }
 
+// This CTA has given up: its rows of the pair's partial sums are missing.  A call of its own, out of the way of the kernel's registers.
+__device__ __noinline__ void gave_up(const LinArgs& a) {
+    if (threadIdx.x == 0) report_timeout();
+    if (!a.join) return;
+    float* const first = a.part + (size_t)cluster_rank() * 128 * kTN;
+    for (int it = blockIdx.x / 2; it < a.whole + a.rest * a.splits; it += gridDim.x / 2)
+        for (int k = threadIdx.x; k < 128 * kTN && it >= a.whole; k += blockDim.x) first[(size_t)(it - a.whole) * kTM * kTN + k] = __uint_as_float(kUnformed);
+}
+
 template <int kEpi, uint32_t kAct, typename T, bool kSum>
 __global__ void __launch_bounds__(kThreads<kSum>, 1) k_linear(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_b,
                                                         const __grid_constant__ LinArgs a) {
@@ -399,7 +408,7 @@ __global__ void __launch_bounds__(kThreads<kSum>, 1) k_linear(const __grid_const
         if (it >= a.whole) {
             const int r = it - a.whole;
             tile = a.whole + r % a.rest;
-            if (a.join) {
+            if (kSum && a.join) {
                 q.part = r;
                 q.kb0 = min(kb_total, r / a.rest * a.kb_per_split);
                 q.kb1 = min(kb_total, q.kb0 + a.kb_per_split);
@@ -467,7 +476,7 @@ __global__ void __launch_bounds__(kThreads<kSum>, 1) k_linear(const __grid_const
         bool ok = true;
         for (int it = pair; it < items && ok; it += pairs) {
             const Item q = item_of(it);
-            float* part = q.part >= 0 ? a.part + ((size_t)q.part * kTM + row) * kTN + part_col : nullptr;
+            float* part = kSum && q.part >= 0 ? a.part + ((size_t)q.part * kTM + row) * kTN + part_col : nullptr;
             const int rows = min(32, a.M - (q.m0 + row)), col0 = q.n0 + part_col, cols = min(kCols, a.N - col0);
             using Work = Finish<kEpi, kAct, T, 16>;  // 16 columns at a time
             const bool mine = lane < rows;           // a thread has a row of the tile
@@ -572,12 +581,20 @@ __global__ void __launch_bounds__(kThreads<kSum>, 1) k_linear(const __grid_const
     __syncwarp();
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     cluster_sync();                                  // no CTA leaves while the other's arrivals or MMAs may still reach it
-    if (threadIdx.x == 0 && *failed) report_timeout();
+    if constexpr (kSum) {
+        if (*failed) gave_up(a);
+    } else {
+        if (threadIdx.x == 0 && *failed) report_timeout();
+    }
     if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
 }
 
-// The tiles that were cut: their partial sums added up in order.  A warp per row of a tile: eight columns a thread, or, where rows are
-// not aligned, every 32nd one.
+__device__ __forceinline__ bool no_number(const float2 (&v)[4]) {
+    const float2 s = add2(add2(v[0], v[1]), add2(v[2], v[3]));
+    return s.x != s.x || s.y != s.y;
+}
+// The tiles that were cut: their partial sums added up in order; where one is missing (the sum is a NaN then) nothing is written.  A warp per row of a
+// tile: eight columns a thread, or, where rows are not aligned, every 32nd one.
 template <int kEpi, uint32_t kAct, typename T>
 __global__ void __launch_bounds__(256) k_linear_join(const __grid_constant__ LinArgs a) {
     pdl_wait();
@@ -604,6 +621,12 @@ __global__ void __launch_bounds__(256) k_linear_join(const __grid_constant__ Lin
                 v[2] = add2(v[2], make_float2(hi.x, hi.y));
                 v[3] = add2(v[3], make_float2(hi.z, hi.w));
             }
+            if (no_number(v)) {
+                bool missing = false;
+#pragma unroll 1
+                for (int k = 0; k < a.splits * 8; ++k) missing = missing || unformed(p[k / 8 * step + k % 8]);
+                if (missing) continue;
+            }
             f(a, row, col, v);
             continue;
         }
@@ -617,10 +640,16 @@ __global__ void __launch_bounds__(256) k_linear_join(const __grid_constant__ Lin
 #pragma unroll
             for (int c = 0; c < 8; ++c)
                 if (c * 32 + lane < n) v[c] += from[k * step + c * 32 + lane];
+        uint32_t missing = 0;                        // a bit per column
+        const float all = ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
+        if (all != all)
+#pragma unroll 1
+            for (int k = 0; k < a.splits * 8; ++k)
+                if (k % 8 * 32 + lane < n && unformed(from[k / 8 * step + k % 8 * 32 + lane])) missing |= 1u << k % 8;
 #pragma unroll
         for (int c = 0; c < 8; ++c) {
             const int col = n0 + c * 32 + lane;
-            if (c * 32 + lane < n) one[c](a, row, col, kEpi == kForward && a.bias ? a.bias[col] : 0.f, v[c]);
+            if (c * 32 + lane < n && !(missing >> c & 1)) one[c](a, row, col, kEpi == kForward && a.bias ? a.bias[col] : 0.f, v[c]);
         }
     }
 }
@@ -795,11 +824,8 @@ int bias_parts(uint64_t T, uint64_t N) {
     return (int)std::max<uint64_t>(1, std::min((T + 63) / 64, want));
 }
 
-// No tile, or part of one, has more runs than the tensor core adds up on its own.
-bool one_segment(const LinArgs& a) {
-    const int all = (a.K + kTK - 1) / kTK;
-    return (a.join && a.whole == 0 ? a.kb_per_split : all) <= kSegmentRuns<bf16>;
-}
+// Whole tiles of no more runs than the tensor core adds up on its own.
+bool one_segment(const LinArgs& a) { return !a.join && (a.K + kTK - 1) / kTK <= kSegmentRuns<bf16>; }
 
 cudaError_t copy_rows(const Operand& o, uint64_t to_ld, bf16* to, cudaStream_t s) {
     return launch_kernel(k_copy_rows, (int)std::min<size_t>(o.rows, kSms * 16), 128, 0, s, true, static_cast<const bf16*>(o.p), (size_t)o.ld, (int)o.cols, (size_t)to_ld,

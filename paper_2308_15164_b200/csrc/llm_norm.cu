@@ -498,6 +498,7 @@ __global__ void __launch_bounds__(kWarp ? kRowWarps * 32 : ring_threads(true, kP
         asm volatile("cp.async.wait_all;" ::: "memory");
         __syncwarp();
     }
+    if (r.without(part, 2 * (int)part_width(a.D))) return;
 #pragma unroll
     for (int j = 0; j < kP; ++j)
         if (r.has(j))
@@ -526,7 +527,6 @@ __global__ void __launch_bounds__(kWarp ? kRowWarps * 32 : ring_threads(true, kP
             part[c] = v;
         }
     }
-    if (!r.ok) report_timeout();
 }
 
 // Column sums over the CTAs of part[cta][which][c], 32 columns per CTA, joined in a fixed order: eight threads with a piece of 16 bytes
@@ -561,7 +561,13 @@ __global__ void __launch_bounds__(1024) k_column_sums(const float* part, int n, 
 #pragma unroll
     for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
     const int cc = blockIdx.x * 32 + r;
-    if (lane != 0 || cc >= D) return;
+    if (cc >= D) return;
+    if (s != s) {                                                  // a partial sum that its kernel could not form: nothing is written
+        bool missing = false;
+        for (int i = lane; i < n; i += 32) missing = missing || unformed(part[(size_t)i * 2 * width + blockIdx.y * width + cc]);
+        if (__any_sync(0xffffffffu, missing)) return;
+    }
+    if (lane != 0) return;
     auto put = [&](float* out, float v) { out[cc] = accumulate ? out[cc] + v : v; };
     if (blockIdx.y == 0) put(dw_pre, s);
     else {

@@ -238,10 +238,12 @@ __global__ void __launch_bounds__(kWarps * 32, kCtasOf<kBack, kMaps>) k_recurren
     const int c = strip * kCols + lane * 2, n = min(max(a.D - c, 0), 2);
     Map behind = identity();                                     // kMaps, warp 0: of the tiles so far
     float2 start = both(0.f);                                    // else: the state in front of the tile
+    bool failed = false;
     if (!kMaps && seg > 0) {
         const int all = seg * a.parts, per = (all + kWarps - 1) / kWarps, k0 = warp * per, k1 = min(k0 + per, all);
         const Map* p = a.maps + (size_t)strip * 32 + lane;
         Map run = identity();
+        bool missing = false;                                    // a CTA of the first pass gave up
         for (int k = k0; k < k1; k += 8) {
             Map v[8];
 #pragma unroll
@@ -249,14 +251,17 @@ __global__ void __launch_bounds__(kWarps * 32, kCtasOf<kBack, kMaps>) k_recurren
                 if (k + i < k1) v[i] = p[(size_t)(k + i) * a.strips * 32];
 #pragma unroll
             for (int i = 0; i < 8; ++i)
-                if (k + i < k1) run = compose<true>(run, v[i]);
+                if (k + i < k1) {
+                    missing = missing || unformed(v[i].A.x);
+                    run = compose<true>(run, v[i]);
+                }
         }
         if (no_number(run.B)) {
             run = identity();
             for (int k = k0; k < k1; ++k) run = compose<true, true>(run, p[(size_t)k * a.strips * 32]);
         }
         s.front[warp][lane] = run;
-        __syncthreads();
+        failed = __syncthreads_or(missing) != 0;
 #pragma unroll
         for (int w = 0; w < kWarps; ++w) start = apply<true>(s.front[w][lane], start);
         if (no_number(start)) {
@@ -269,8 +274,7 @@ __global__ void __launch_bounds__(kWarps * 32, kCtasOf<kBack, kMaps>) k_recurren
     int from = 0, to = 0;                                        // a sequence that the warp has met
     int stage = 0;
     uint32_t phase = 0;
-    bool failed = false;
-    for (int i = 0; i < tiles; ++i) {
+    for (int i = 0; i < tiles && !failed; ++i) {
         const int u0 = tile_row(i) + warp * kRows;        // first row of the warp, in scan order
         auto row = [&](int r) { return kBack ? a.T - 1 - (u0 + r) : u0 + r; };
         // rows inside one sequence, nearly all there are: none needs a look of its own.  Otherwise: which are in a sequence, and which are the
@@ -456,7 +460,8 @@ __global__ void __launch_bounds__(kWarps * 32, kCtasOf<kBack, kMaps>) k_recurren
         }
     }
     if constexpr (kMaps) {
-        if (warp == 0 && !failed) a.maps[((size_t)index * a.strips + strip) * 32 + lane] = behind;
+        if (failed) behind.A = both(__uint_as_float(kUnformed));
+        if (warp == 0) a.maps[((size_t)index * a.strips + strip) * 32 + lane] = behind;
     } else if (seg == 0 && a.after && (a.T == 0 || a.offsets)) { // sequences without rows
         for (int q = warp; q < a.seqs; q += kWarps)
             if (begin_of(a, q + 1) <= begin_of(a, q))

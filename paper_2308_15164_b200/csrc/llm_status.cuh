@@ -3,6 +3,7 @@
 #pragma once
 
 #include <cuda_runtime.h>
+#include <stdint.h>
 
 #include "abs_sgd.h"
 
@@ -11,6 +12,10 @@ namespace abs_sgd {
 static __device__ int g_llm_status;
 
 __device__ __forceinline__ void report_timeout() { atomicExch(&g_llm_status, ABS_ETIMEOUT); }
+
+// What a kernel that gave up leaves for the kernel behind it in place of a number: a NaN that is the result of no arithmetic (that one is 0x7fffffff).
+constexpr uint32_t kUnformed = 0x7fd5a5a5u;
+__device__ __forceinline__ bool unformed(float v) { return __float_as_uint(v) == kUnformed; }
 
 // Blocks until `s` has finished; *status: the word, which is zero afterwards.
 static inline cudaError_t take_status(int* status, cudaStream_t s) {

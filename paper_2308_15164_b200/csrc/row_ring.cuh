@@ -6,6 +6,7 @@
 
 #include "bulk_copy.cuh"
 #include "llm_host.h"
+#include "llm_status.cuh"
 #include "row_ops.cuh"
 
 namespace abs_sgd {
@@ -21,6 +22,7 @@ struct RingCtl {
     alignas(16) float red[3][6][16]; // [reduction][number][warp]
     alignas(8) uint64_t full[kRingMax];
     unsigned done;                   // warps that have read the current row
+    unsigned gave_up;                // a wait for a row's image has run out
 };
 constexpr size_t kRingCtl = (sizeof(RingCtl) + 15) / 16 * 16;
 
@@ -109,7 +111,7 @@ struct Ring {
         if (!kWarp) {
             for (int i = tid; i < 18 * 16; i += blockDim.x) (&ctl->red[0][0][0])[i] = 0.f;
             if (tid == 0) {
-                ctl->done = 0;
+                ctl->done = ctl->gave_up = 0;
                 for (int i = 0; i < stages; ++i) mbar_init(&ctl->full[i], 1);
                 asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
             }
@@ -165,7 +167,17 @@ struct Ring {
             else asm volatile("cp.async.wait_group 3;" ::: "memory");
             return;
         }
-        if (bytes != 0 && !mbar_wait(&ctl->full[st], phase, ok ? kSpinLimit : 1u)) ok = false;
+        if (bytes != 0 && !mbar_wait(&ctl->full[st], phase, ok ? kSpinLimit : 1u)) {
+            ok = false;
+            ctl->gave_up = 1;
+        }
+    }
+    // Behind the last row: the CTA's sums over its rows cannot be formed (the rows' own synchronisations have made it known).  Marks them so.
+    __device__ __forceinline__ bool without(float* sums, int n) const {
+        if (kWarp || !*(volatile unsigned*)&ctl->gave_up) return false;
+        for (int i = threadIdx.x; i < n; i += blockDim.x) sums[i] = __uint_as_float(kUnformed);
+        if (threadIdx.x == 0) report_timeout();
+        return true;
     }
     __device__ __forceinline__ void next() {
         if (++st == stages) { st = 0; phase ^= 1u; }
