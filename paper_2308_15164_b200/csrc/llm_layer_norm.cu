@@ -29,14 +29,17 @@ constexpr int ring_threads(bool back, int elems) { return back && elems == 32 ? 
 constexpr int warp_ctas(bool back, int elems) { return back ? 2 : elems == 8 ? 4 : 3; }
 constexpr size_t warp_row(size_t es) { return es == 2 ? 384 : 256; }
 // Elements of a thread: what a row costs a thread beside its elements (reductions, waits, addresses, some 150 instructions forward and 300
-// backward) is spread over them, but fewer leave more warps.  us with 16 / 32, bf16: forward 16384 x 4096 69 / 51, 8192 x 8192 80 / 54,
-// 16384 x 2048 36 / 31; backward with dskip 16384 x 4096 122 / 119, 8192 x 8192 133 / 126, 16384 x 6144 206 / 218, 16384 x 2048 66 / 68.  fp32 (half
-// the elements a byte) 8192 x 4096 46 / 50, backward 91 / 91, 1003 x 1537 5.1 / 6.4, 11.5 / 12.6.
+// backward) is spread over them, but fewer leave more warps.  us with 16 / 32, bf16, 2^26 elements forward and 2^25 backward with dskip:
+//     columns       392        512        520        768       1024       1536       2048       4096       8192
+//     forward    80 / 98    63 / 75   123 / 83    84 / 61    66 / 54    68 / 63    71 / 55    74 / 54    86 / 57
+//     columns       512       1024       2048       3584       4000       4096       4608       6144       6152       7168       8192
+//     backward   64 / 88    63 / 68    65 / 70    72 / 74    69 / 71    70 / 71    92 / 99    81 / 86    86 / 86    81 / 79    78 / 77
+// (without dskip the same borders; forward rows of 520 to 1024 columns, but few of them: 16 elements up to a tenth faster).  fp32 (half the elements a
+// byte) forward 512 columns 46 / 83, 2048 47 / 58, 8192 56 / 61; backward 512 38 / 55, 2048 36 / 40, 8192 45 / 46.
 constexpr int ring_elems(bool back, size_t es, size_t D) {
     if (D <= 8 * 32) return 8;
     if (es == 4) return D <= 16 * 512 ? 16 : 32;
-    if (!back) return D <= 1024 ? 16 : 32;
-    return D <= 3840 || (D > 4096 && D <= 6144) ? 16 : 32;
+    return D <= (back ? 6144 : 512) ? 16 : 32;
 }
 
 struct LnArgs {

@@ -174,10 +174,14 @@ struct Ring {
     }
     // Behind the last row: the CTA's sums over its rows cannot be formed (the rows' own synchronisations have made it known).  Marks them so.
     __device__ __forceinline__ bool without(float* sums, int n) const {
-        if (kWarp || !*(volatile unsigned*)&ctl->gave_up) return false;
-        for (int i = threadIdx.x; i < n; i += blockDim.x) sums[i] = __uint_as_float(kUnformed);
-        if (threadIdx.x == 0) report_timeout();
-        return true;
+        if constexpr (!kWarp) {
+            if (*(volatile unsigned*)&ctl->gave_up) {
+                for (int i = threadIdx.x; i < n; i += blockDim.x) sums[i] = __uint_as_float(kUnformed);
+                if (threadIdx.x == 0) report_timeout();
+                return true;
+            }
+        }
+        return false;
     }
     __device__ __forceinline__ void next() {
         if (++st == stages) { st = 0; phase ^= 1u; }
