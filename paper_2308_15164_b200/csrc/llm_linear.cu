@@ -276,9 +276,11 @@ constexpr int kSms = 148;
 constexpr uint64_t kSizeMax = 0x7fffffc0ull;
 constexpr int kMinRuns = 12;     // runs of 64 that a part of a cut tile has at least: shorter ones do not pay for the join (some 7 us)
 // Where rows of the output, residual or z are not 16-byte aligned the epilogue moves single elements; if it has to read some, they are read
-// in many small parts.  Up to kFewTiles tiles, which keep few SMs busy, that is left to k_linear_join, on all of them, and K is cut down to
-// kMinRunsJoin runs: 515 x 1000 x 1111 with residual 25 -> 21 us (without 18.6 / 20.6: stays).
-constexpr int kFewTiles = 37, kMinRunsJoin = 4;
+// in many small parts.  Up to kFewTiles tiles, a quarter of what keeps all SMs busy, that is left to k_linear_join, on all of them, and K is cut down to
+// kMinRunsJoin runs.  us with / without: forward with residual, K 1024, 4 tiles 24.6 / 26.6, 16 tiles 24.6 / 26.7, 24 tiles 30.7 / 28.0; input gradient through
+// GELU 20.5 / 26.6, 22.6 / 26.6, 28.7 / 26.6; weight gradient of 1024 tokens added to what is there 22.5 / 27.6, 23.6 / 28.6, 26.7 / 28.7; K 256, 512 and 2048
+// alike.  With 8 runs instead of 4: 515 x 1000 x 1111 26.6 instead of 24.6.
+constexpr int kFewTiles = 18, kMinRunsJoin = 4;
 
 struct LinSmem {
     alignas(1024) uint8_t a[kStages][kHalf];
