@@ -146,7 +146,8 @@ int abs_ckpt8_wgrad(const int8_t *q, const uint8_t *e, const void *dy, uint64_t 
 int abs_embed(const int32_t *ids, uint64_t tokens, const float *table, uint64_t ld_table, uint64_t vocab, uint64_t width, float scale,
               uint32_t dtype, void *y, uint64_t ld_y, void *stream);
 
-/* dtable[v, :] = scale sum over the tokens with id v of dy[t, :]; every row is written, those of no token with zeros.  accumulate != 0: added to what the table holds, rows of no token are not touched.
+/* dtable[v, :] = scale sum over the tokens with id v of dy[t, :]; every row is written, those of no token with zeros.  accumulate != 0: added to what the table holds (by the memory's own addition, to
+ * which numbers below 2^-126 are zero), rows of no token are not touched.
  *   dy [tokens, width] of `dtype`; dtable [vocab, width] fp32, ld_dtable >= width, 4-byte aligned (a slice of a flat gradient).
  * Limits as for abs_embed.  workspace: abs_embed_backward_workspace() bytes. */
 size_t abs_embed_backward_workspace(uint64_t tokens, uint64_t vocab, uint64_t width);

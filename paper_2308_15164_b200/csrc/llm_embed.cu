@@ -2,8 +2,8 @@
 //
 // Forward: a gather of rows, bound by memory.  Backward: the tokens are sorted by id (a stable radix sort, so that a row's tokens
 // stay in their order), the sorted list is cut into chunks of equal length, each summed row by row; a row whose tokens pass a
-// chunk's border leaves partial sums that a last kernel adds up in order.  No atomics: equal inputs give equal bits, and a token
-// that fills half the micro-batch costs no more than the others.
+// chunk's border leaves partial sums that a last kernel adds up in order.  No additions whose order could change: equal inputs give
+// equal bits, and a token that fills half the micro-batch costs no more than the others.
 #include <math.h>
 
 #include <algorithm>
@@ -318,7 +318,8 @@ struct SumArgs {
 };
 
 // A row's sum; accumulate: one addition for each element, by the memory (nobody else adds to it, so that the order is no matter; read, added and
-// written by the thread, a chunk's rows wait for one another: 16 us instead of 5 for 8192 x 64).
+// written by the thread, a chunk's rows wait for one another: 16 us instead of 5 for 8192 x 64).  The memory takes numbers below 2^-126 for zero, what it
+// adds, what it adds to and what comes out.
 template <int kE>
 __device__ __forceinline__ void put_row(const SumArgs& a, uint32_t id, int j, const float (&sum)[kE]) {
     float* p = a.out + (size_t)id * a.ld_out + (size_t)j * kE;
