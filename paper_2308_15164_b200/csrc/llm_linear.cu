@@ -255,10 +255,10 @@ struct FinishOne {
 // Items are dealt out round-robin to the pairs: the whole tiles, as many as fill all pairs equally often, then the rest, each cut along K
 // into `splits` parts so that they too keep all pairs busy; k_linear_join adds those up in order and does the elementwise work.
 // Launched in plain stream order, and starts no successor early (see llm_ckpt8.cu).  Every wait on a barrier is bounded.
-// Bound by the tensor core where there is enough to do, and by the power limit in a loop: a library's bf16 product of the same operands alone took
-// (us, this kernel / the library): 8192 x 8192 x 8192 774 / 674; gradient of the input 8192 x 8192 x 2048 202 / 187; of the weight, with sums of 12 runs,
-// 209 / 187; 8192 x 2048 x 8192 211, with GELU 225, and z kept 238.  Few tokens: 8 us for one tile of one run (launch in plain order, tensor memory,
-// first copies, epilogue), 16 runs of K 4 more.
+// Bound by the tensor core and what feeds it where there is enough to do (the results' way out takes a tenth of it), and by the power limit in a loop.  A
+// library's bf16 product of the same operands alone took (us, this kernel / the library, few calls after a pause): 8192 x 2048 x 8192 197 / 175, with GELU 220,
+// and z kept 229, as fp32 204; 8192 x 8192 x 8192 759 / 659; gradient of the input 8192 x 8192 x 2048 199 / 182; of the weight, 2048 x 8192 of 8192 tokens,
+// 198 / 181.  Few tokens: 8 us for one tile of one run (launch in plain order, tensor memory, first copies, epilogue), 16 runs of K 4 more.
 // ------------------------------------------------------------------------------------------------
 constexpr int kTM = 256, kTN = 256, kTK = 64;    // of a pair
 constexpr int kStages = 5;
@@ -267,7 +267,7 @@ constexpr int kPitch = 20;                       // floats of a staged row of 16
 // Sums are taken out of TMEM every kSegmentRuns runs and added up in fp32, since the tensor core drops low bits at each of its additions: without, the
 // error grows with K (positive terms, K 16384: up to 8e-5).  Weight gradient of 8192 tokens, error of the result's norm / us of 8192 x 8192 x 2048: 12 runs
 // 7e-7 / 215, 24 1.5e-6 / 210, 32 2.1e-6 / 208, never 8.6e-6 / 206.  bf16 results, which are rounded to 2^-9, take 16 runs: with 12, a K of 1024 would need
-// two segments (7 x 1024 x 1024 with GELU 15.4 us, in two 18.4; 8192 x 2048 x 8192 211 and 214; never 200).
+// two segments (7 x 1024 x 1024 with GELU 15.4 us, in two 18.4; 8192 x 2048 x 8192 211 and 214, in one of any length 200).
 template <typename T>
 constexpr int kSegmentRuns = sizeof(T) == 4 ? 12 : 16;
 template <bool kSum>
